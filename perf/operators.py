@@ -245,7 +245,7 @@ def run(s):
         if kind == "slots":
             ptd.prompt_slots(s.prompt, s.cache, s.slots, s.positions, s.status, s.pages)
         elif kind == "append":
-            ptd.prompt_rope_append(s.cache, 0, s.slots, s.positions, s.q, s.kn, s.vn, s.q_out, ROPE_BASE, s.status)
+            ptd.prompt_rope_append(s.prompt, s.cache, 0, s.slots, s.positions, s.q, s.kn, s.vn, s.q_out, ROPE_BASE, s.status)
         else:
             ptd.prompt_attention(s.prompt, s.cache, 0, s.q, s.out, s.status, workspace=s.workspace)
     elif kind == "slots":
