@@ -21,7 +21,10 @@
  * rotary encoding and the tree's K/V into the cache), ptd_lm_head_topk (the LM-head
  * product with a fused top-k: the logits are never written),
  * ptd_verify_and_compact (the last two as one launch) and ptd_tree_verify_step (the
- * whole step: attention, top-k, verification and compaction on one stream)
+ * whole step: attention, top-k, verification and compaction on one stream).  The prompts that come
+ * before the first tree (and plain decoding) have ptd_prompt_slots (pages, block tables, cache
+ * slots and positions of new tokens), ptd_prompt_rope_append (rotary encoding, K/V into those
+ * slots) and ptd_prompt_attention (causal attention of packed sequences over the cache)
  *
  * Conventions shared by every call
  *   - Pointers are DEVICE pointers unless a comment says "host".  The caller owns
@@ -61,7 +64,9 @@ typedef enum {
   PTD_ERR_CUDA = 4,          /* a CUDA runtime call or kernel launch failed              */
   PTD_ERR_TIMEOUT = 5,       /* (device) a bounded on-chip wait gave up; outputs invalid  */
   PTD_ERR_WORKSPACE = 6,     /* workspace pointer null or smaller than required          */
-  PTD_ERR_POOL_FULL = 7      /* (device) a candidate-pool merge was refused: no room     */
+  PTD_ERR_POOL_FULL = 7,     /* (device) a candidate-pool merge was refused: no room     */
+  PTD_ERR_INVALID_BATCH = 8, /* (device) a packed batch's offsets, lengths, pages or slots are out of range */
+  PTD_ERR_NO_PAGES = 9       /* (device) ptd_prompt_slots was refused: too few free pages */
 } ptd_status;
 
 typedef enum { PTD_F32 = 0, PTD_BF16 = 1 } ptd_dtype;
@@ -489,6 +494,92 @@ ptd_status ptd_pipeline_create(const ptd_kv_cache* cache, const ptd_tree* trees,
 ptd_status ptd_pipeline_submit(ptd_pipeline* pipeline, const ptd_host_io* io, int64_t* ticket);
 ptd_status ptd_pipeline_wait(ptd_pipeline* pipeline, int64_t ticket);
 ptd_status ptd_pipeline_destroy(ptd_pipeline* pipeline);
+
+/* ---- Prompts and decoding without a tree ----
+ *
+ * A packed batch of new tokens: whole prompts, chunks of prompts, or single tokens.  Sequence b owns
+ * the tokens [token_offsets[b], token_offsets[b+1]) (none is allowed); its i-th token sits at position
+ * C_b + i, with C_b = ctx_lens[b] tokens in the cache before it, and, as a tree's nodes do, in cache slot
+ * C_b + i.  total_tokens is the number of rows that the buffers have: token_offsets[B] may be smaller
+ * (a batch padded to a captured size), and what lies behind the last sequence is padding. */
+#define PTD_MAX_PROMPT_BATCH 8192
+typedef struct {
+  int32_t batch;                /* host: B, 1 .. PTD_MAX_PROMPT_BATCH                   */
+  int32_t total_tokens;         /* host: rows of the token buffers, >= token_offsets[B] */
+  int32_t max_tokens;           /* host: upper bound of a sequence's new tokens (>= 1)  */
+  int32_t max_ctx;              /* host: upper bound of every ctx_lens[b] (>= 0)        */
+  const int32_t* token_offsets; /* [B+1], token_offsets[0] >= 0, non-decreasing         */
+  const int32_t* ctx_lens;      /* [B]                                                  */
+} ptd_prompt;
+
+/* The free pages of a paged cache, and the pages that each sequence of a batch holds. */
+typedef struct {
+  int32_t* free_pages;          /* [num_pages], a stack: entries [0, free_count[0]) are free pages */
+  const int32_t* free_count;    /* [1]                                                  */
+  const int32_t* held;          /* [B], leading entries of the sequence's block-table row in use */
+  int32_t* new_held;            /* [B], must not overlap held                           */
+  int32_t* new_free_count;      /* [1], must not overlap free_count                     */
+  int32_t* block_table;         /* [B][max_pages]: the cache's own block table, writable */
+} ptd_page_pool;
+
+/* Cache slots and positions of a batch's new tokens, and (with `pages`) the pages for them.
+ *   slots [total_tokens]: token n's row within a layer of the cache: block_table[b][p / page_size] *
+ *     page_size + p % page_size for a paged cache, b * seq_capacity + p for a contiguous one, with p its
+ *     position; -1 for padding.   positions [total_tokens]: p; -1 for padding.
+ *   pages (may be NULL; paged caches only): first every sequence is made to hold exactly
+ *     ceil((C_b + n_b) / page_size) pages.  A sequence that holds more (a rejected draft's, a finished
+ *     request's: C_b = n_b = 0) gives the last ones back: in (sequence, index) order they go on top of the
+ *     stack of free pages.  Then the sequences that hold fewer take pages from the top, in (sequence, index)
+ *     order, into the next entries of their block-table row.  new_held and new_free_count receive the pages
+ *     held and free after the call (the next call's held and free_count); no other entry of block_table and
+ *     free_pages changes, so that a call on the same state writes the same.
+ *     If there are too few free pages (PTD_ERR_NO_PAGES in dev_status), or held, free_count or a sequence is out
+ *     of range (PTD_ERR_INVALID_BATCH), nothing moves: new_held = held, new_free_count = free_count and every
+ *     slot and position is -1.
+ *   Without `pages` a sequence out of range (n_b outside 0 .. max_tokens, C_b outside 0 .. max_ctx, more
+ *     positions than the cache's row holds, offsets outside the batch) sets PTD_ERR_INVALID_BATCH and its
+ *     tokens get -1.  In both forms so does a token whose page number is outside the cache.
+ * free_count, held, the offsets and ctx_lens must not overlap what the call writes.  A cache layer has fewer
+ * than 2^31 rows.  One launch. */
+ptd_status ptd_prompt_slots(const ptd_prompt* prompt, const ptd_kv_cache* cache, const ptd_page_pool* pages,
+                            int32_t* slots, int32_t* positions, int32_t* dev_status, void* stream);
+
+/* Rotary encoding of a batch's new tokens and their K/V into the cache, in one layer.  Token n, at position
+ * positions[n]: q_out[n] = q[n] rotated, k[n] rotated and v[n] as it is go to row slots[n] of the layer (both
+ * as ptd_prompt_slots writes them; the rotation is ptd_tree_rope_append's).  A token with slot -1 (padding)
+ * writes nothing; another slot outside the layer sets PTD_ERR_INVALID_BATCH and writes nothing.
+ *   q [total_tokens][num_q_heads][D], k, v [total_tokens][num_kv_heads][D], cache->dtype: a token's heads are
+ *     back to back, tokens q_stride, k_stride, v_stride elements apart (at least a token's elements), e.g.
+ *     views of one fused product's rows.
+ *   q_out: as q, q_out_stride apart; it may be q itself (same pointer and stride), and overlaps q, k, v
+ *     in no other way.  slots of different tokens differ.
+ * D even, at most 256.  One launch. */
+ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t layer,
+                                  const int32_t* slots, const int32_t* positions, const void* q, int64_t q_stride,
+                                  int32_t num_q_heads, const void* k, int64_t k_stride, const void* v,
+                                  int64_t v_stride, float rope_base, void* q_out, int64_t q_out_stride,
+                                  int32_t* dev_status, void* stream);
+
+/* Causal attention of a batch's new tokens over one layer of the cache: for token i of sequence b
+ * (n = token_offsets[b] + i) and query head h (KV head h / (Hq / Hkv))
+ *     out[n][h] = sum_j softmax_j(scale * <q[n][h], K[b][j]>) V[b][j],   j in [0, C_b + i].
+ * The new tokens' own K/V are in the cache already (ptd_prompt_rope_append).
+ *   q [total_tokens][num_q_heads][D], tokens q_stride elements apart; out [total_tokens][num_q_heads][D] back to
+ *     back; both of cache->dtype and 16-byte aligned, q_stride times the element size a multiple of 16.
+ *     fp32 accumulation and softmax statistics; the weights are rounded to bf16 for a bf16 cache.
+ *   Rows behind the last sequence are left as they were, as are those of a sequence out of range (see
+ *     ptd_prompt_slots; PTD_ERR_INVALID_BATCH).  A page number outside the cache sets PTD_ERR_INVALID_BATCH too:
+ *     the sequence's outputs are then unspecified.
+ *   K and V of a token are read for the tokens that see it only: an infinity or NaN in a later one changes nothing.
+ *   scale: <= 0 selects 1/sqrt(D).  D: as ptd_tree_attention (128 for bf16; 32, 64 or 128 for fp32).
+ *   workspace: scratch of ptd_prompt_attention_workspace_size bytes, 16-byte aligned, for batches of few rows,
+ *     whose keys are split between CTAs (partials merged by a second kernel); with less (even none) the
+ *     call runs unsplit.  Calls that may overlap on the GPU need scratch of their own.
+ * One launch, or two where keys are split. */
+size_t ptd_prompt_attention_workspace_size(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t num_q_heads);
+ptd_status ptd_prompt_attention(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t layer, const void* q,
+                                int64_t q_stride, int32_t num_q_heads, float scale, void* out, void* workspace,
+                                size_t workspace_bytes, int32_t* dev_status, void* stream);
 
 /* Diagnostic of the failure path: one thread waits on an mbarrier that nothing arrives on,
  * through the bounded wait every kernel here uses; after its limit (2 s of %globaltimer)

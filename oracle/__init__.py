@@ -7,6 +7,7 @@ from .ptd_oracle import (  # noqa: F401
     CandidatePool,
     InvalidTree,
     ancestor_sets,
+    causal_attention,
     check_forest,
     check_tree,
     children_sets,
@@ -16,6 +17,8 @@ from .ptd_oracle import (  # noqa: F401
     kv_compact,
     lm_head_logits,
     lm_head_topk,
+    prompt_pages,
+    prompt_slots,
     softmax_row,
     topk,
     topk_rows,

@@ -36,6 +36,9 @@ cites the passage it follows:
                                  set by |pi(v)|, here C + |pi(v)| - 1 after the
                                  committed prefix; the rotary encoding itself is the
                                  model's (RoFormer's rotation, rotate-half layout).
+  prompt_pages, prompt_slots, causal_attention
+                                 the pass that puts the prefix X into the cache before
+                                 the first tree (no passage: plain causal decoding).
   CandidatePool ................ Sec. 3.1 "Draft Extraction via Merging" (the merge
                                  M(T, T') of two trees with the same root value) and
                                  Alg. 1 step 4; Sec. 3.2 and Alg. 1 step 1 (retrieve
@@ -507,6 +510,56 @@ def rope(x, positions, base: float) -> np.ndarray:
     c, s = np.cos(ang)[:, None, :], np.sin(ang)[:, None, :]
     a, b = x[..., :half], x[..., half:]
     return np.concatenate([a * c - b * s, a * s + b * c], axis=-1)
+
+
+# ---------------------------------------------------------------------------
+# Prompts: pages, cache slots and causal attention of packed new tokens
+# ---------------------------------------------------------------------------
+
+def prompt_pages(ctx, new, held, table, free, page_size: int):
+    """Every sequence made to hold exactly the pages of ctx + new positions: what is too many goes back on the
+    stack `free` (a list, top last) in (sequence, index) order, then what is missing is taken from its top in
+    the same order.  Returns (table, held, free), or None if there are too few free pages."""
+    table, stack = [list(r) for r in table], list(free)
+    need = [-(-(c + n) // page_size) for c, n in zip(ctx, new)]
+    for b, row in enumerate(table):
+        stack.extend(row[need[b]:held[b]])
+    if sum(max(0, w - h) for w, h in zip(need, held)) > len(stack):
+        return None
+    for b, row in enumerate(table):
+        for i in range(held[b], need[b]):
+            row[i] = stack.pop()
+    return table, need, stack
+
+
+def prompt_slots(ctx, new, table, page_size: int):
+    """(slots, positions) of the new tokens, sequence after sequence: paged with `table`'s rows, or contiguous
+    with page_size = -capacity."""
+    slots, positions = [], []
+    for b, (c, n) in enumerate(zip(ctx, new)):
+        for p in range(c, c + n):
+            positions.append(p)
+            slots.append(table[b][p // page_size] * page_size + p % page_size if page_size > 0 else -page_size * b + p)
+    return slots, positions
+
+
+def causal_attention(q, k, v, ctx: int, scale: float | None = None):
+    """q [n, Hq, D] at positions ctx, ctx + 1, ..; k, v [>= ctx + n, Hkv, D].  Token i attends to the positions
+    0 .. ctx + i.  Returns (o, size): o [n, Hq, D] float64, and the sums of the weighted |v| in its place."""
+    q, k, v = (np.asarray(x, np.float64) for x in (q, k, v))
+    n, Hq, D = q.shape
+    G = Hq // k.shape[1]
+    scale = 1.0 / math.sqrt(D) if scale is None else scale
+    o, size = np.zeros_like(q), np.zeros_like(q)
+    for h in range(Hq):
+        for i in range(n):
+            m = ctx + i + 1
+            s = scale * (k[:m, h // G] @ q[i, h])
+            w = np.exp(s - s.max())
+            w /= w.sum()
+            o[i, h] = w @ v[:m, h // G]
+            size[i, h] = w @ np.abs(v[:m, h // G])
+    return o, size
 
 
 # ---------------------------------------------------------------------------

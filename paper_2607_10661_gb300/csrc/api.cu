@@ -18,6 +18,7 @@
 #include "pool.cuh"
 #include "tree_rope.cuh"
 #include "lm_head.cuh"
+#include "prompt.cuh"
 
 namespace ptd {
 cudaError_t launch_bounded_wait_check(int32_t* dev_status, cudaStream_t stream);
@@ -295,6 +296,10 @@ const char* ptd_status_string(ptd_status s) {
       return "workspace missing or too small";
     case PTD_ERR_POOL_FULL:
       return "candidate pool full: merge refused";
+    case PTD_ERR_INVALID_BATCH:
+      return "invalid batch (offsets, lengths, pages or slots out of range)";
+    case PTD_ERR_NO_PAGES:
+      return "too few free pages: slots refused";
   }
   return "unknown status";
 }
@@ -666,6 +671,19 @@ ptd_status ptd_pool_retrieve(const void* pool, int32_t capacity, const int32_t* 
   return st;
 }
 
+namespace {
+// base^(-2j/D), j < D/2, as fp32 pairs from double.
+ptd::RopeFreqs rope_freqs(float base, int D) {
+  ptd::RopeFreqs f = {};
+  for (int j = 0; j < D / 2; ++j) {
+    const double x = std::pow((double)base, -2.0 * j / D);
+    f.hi[j] = (float)x;
+    f.lo[j] = (float)(x - (double)f.hi[j]);
+  }
+  return f;
+}
+}  // namespace
+
 ptd_status ptd_tree_rope_append(const ptd_tree* tree, const ptd_kv_cache* cache, int32_t layer_begin,
                                 int32_t num_layers, void* q, int32_t num_q_heads, const void* k, const void* v,
                                 float rope_base, int32_t* positions_out, int32_t* dev_status, void* stream) {
@@ -681,21 +699,197 @@ ptd_status ptd_tree_rope_append(const ptd_tree* tree, const ptd_kv_cache* cache,
   const size_t es = dtype_size(cache->dtype);
   if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) % es != 0)
     return PTD_ERR_INVALID_ARG;
-  ptd::RopeFreqs f = {};
-  for (int j = 0; j < D / 2; ++j) {
-    const double x = std::pow((double)rope_base, -2.0 * j / D);
-    f.hi[j] = (float)x;
-    f.lo[j] = (float)(x - (double)f.hi[j]);
-  }
   st = cuda_status(ptd::launch_tree_rope(tree->node_offsets, tree->parents, tree->ctx_lens, tree->batch,
                                          tree->total_nodes, cache->dtype == PTD_BF16, D, num_q_heads, hkv, q, k, v,
                                          cache->k, cache->v, layer_begin, num_layers, cache->page_size,
                                          cache->seq_capacity,
-                                         cache->num_pages, cache->block_table, cache->max_pages, f, positions_out,
+                                         cache->num_pages, cache->block_table, cache->max_pages, rope_freqs(rope_base, D), positions_out,
                                          dev_status, num_sms_of_current_device(),
                                          static_cast<cudaStream_t>(stream)));
   if (st == PTD_OK) g_last_launches = 1;
   return st;
+}
+
+namespace {
+ptd_status check_prompt(const ptd_prompt* p) {
+  if (!p || p->batch < 1 || p->total_tokens < 1 || p->max_tokens < 1 || p->max_ctx < 0 || !p->token_offsets || !p->ctx_lens ||
+      (int64_t)p->max_ctx + p->max_tokens > INT32_MAX)
+    return PTD_ERR_INVALID_ARG;
+  return p->batch <= PTD_MAX_PROMPT_BATCH ? PTD_OK : PTD_ERR_UNSUPPORTED;
+}
+
+ptd::PromptBounds prompt_bounds(const ptd_prompt* p, const ptd_kv_cache* c) {
+  return {p->total_tokens, p->max_tokens, p->max_ctx,
+          c->page_size > 0 ? (int64_t)c->max_pages * c->page_size : (int64_t)c->seq_capacity};
+}
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
+// Checked arguments of a prompt attention without its tensors: the sizes and the plan's part.
+ptd_status check_prompt_attention(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t hq) {
+  ptd_status st = check_prompt(prompt);
+  if (st != PTD_OK) return st;
+  if ((st = check_cache(cache)) != PTD_OK) return st;
+  if (hq < 1 || hq % cache->num_kv_heads != 0) return PTD_ERR_INVALID_ARG;
+  const int D = cache->head_dim;
+  if (cache->dtype == PTD_BF16 ? D != 128 : (D != 32 && D != 64 && D != 128)) return PTD_ERR_UNSUPPORTED;
+  return PTD_OK;
+}
+
+ptd::PromptAttnParams prompt_attention_params(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t hq) {
+  ptd::PromptAttnParams p = {};
+  p.k = cache->k;
+  p.v = cache->v;
+  p.token_offsets = prompt->token_offsets;
+  p.ctx_lens = prompt->ctx_lens;
+  p.block_table = cache->block_table;
+  p.bounds = prompt_bounds(prompt, cache);
+  p.batch = prompt->batch;
+  p.hq = hq;
+  p.hkv = cache->num_kv_heads;
+  p.head_dim = cache->head_dim;
+  p.page_size = cache->page_size;
+  p.seq_capacity = cache->seq_capacity;
+  p.num_pages = cache->num_pages;
+  p.max_pages = cache->max_pages;
+  return p;
+}
+}  // namespace
+
+ptd_status ptd_prompt_slots(const ptd_prompt* prompt, const ptd_kv_cache* cache, const ptd_page_pool* pages,
+                            int32_t* slots, int32_t* positions, int32_t* dev_status, void* stream) {
+  g_last_launches = 0;
+  ptd_status st = check_prompt(prompt);
+  if (st != PTD_OK) return st;
+  if ((st = check_cache(cache)) != PTD_OK) return st;
+  if (!slots || !positions || !dev_status) return PTD_ERR_INVALID_ARG;
+  if (cache_rows_per_layer(cache, prompt->batch) > INT32_MAX) return PTD_ERR_UNSUPPORTED;
+  ptd::PromptSlotsParams p = {};
+  if (pages) {
+    if (cache->page_size == 0 || !pages->free_pages || !pages->free_count || !pages->held || !pages->new_held ||
+        !pages->new_free_count || pages->block_table != cache->block_table)
+      return PTD_ERR_INVALID_ARG;
+    if ((int64_t)prompt->batch * cache->max_pages > INT32_MAX) return PTD_ERR_UNSUPPORTED;
+    // what the call reads while it writes: other CTAs still read it
+    const size_t B4 = (size_t)prompt->batch * 4, N4 = (size_t)prompt->total_tokens * 4;
+    const void* read[4] = {prompt->token_offsets, prompt->ctx_lens, pages->held, pages->free_count};
+    const size_t nread[4] = {B4 + 4, B4, B4, 4};
+    const void* written[6] = {pages->new_held, pages->new_free_count, slots, positions, pages->free_pages, pages->block_table};
+    const size_t nwritten[6] = {B4, 4, N4, N4, (size_t)cache->num_pages * 4, B4 * cache->max_pages};
+    for (int i = 0; i < 6; ++i) {
+      for (int j = 0; j < 4; ++j)
+        if (overlap(written[i], nwritten[i], read[j], nread[j])) return PTD_ERR_INVALID_ARG;
+      for (int j = 0; j < i; ++j)
+        if (overlap(written[i], nwritten[i], written[j], nwritten[j])) return PTD_ERR_INVALID_ARG;
+    }
+    p.free_pages = pages->free_pages;
+    p.free_count = pages->free_count;
+    p.held = pages->held;
+    p.new_held = pages->new_held;
+    p.new_free_count = pages->new_free_count;
+    p.table_out = pages->block_table;
+  }
+  p.token_offsets = prompt->token_offsets;
+  p.ctx_lens = prompt->ctx_lens;
+  p.batch = prompt->batch;
+  p.bounds = prompt_bounds(prompt, cache);
+  p.page_size = cache->page_size;
+  p.seq_capacity = cache->seq_capacity;
+  p.num_pages = cache->num_pages;
+  p.max_pages = cache->max_pages;
+  p.block_table = cache->block_table;
+  p.slots = slots;
+  p.positions = positions;
+  p.dev_status = dev_status;
+  st = cuda_status(ptd::launch_prompt_slots(p, num_sms_of_current_device(), static_cast<cudaStream_t>(stream)));
+  if (st == PTD_OK) g_last_launches = 1;
+  return st;
+}
+
+ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t layer,
+                                  const int32_t* slots, const int32_t* positions, const void* q, int64_t q_stride,
+                                  int32_t num_q_heads, const void* k, int64_t k_stride, const void* v,
+                                  int64_t v_stride, float rope_base, void* q_out, int64_t q_out_stride,
+                                  int32_t* dev_status, void* stream) {
+  g_last_launches = 0;
+  ptd_status st = check_prompt(prompt);
+  if (st != PTD_OK) return st;
+  if ((st = check_cache(cache)) != PTD_OK) return st;
+  const int D = cache->head_dim, hkv = cache->num_kv_heads;
+  const int64_t qe = (int64_t)num_q_heads * D, ke = (int64_t)hkv * D;
+  if (layer < 0 || layer >= cache->num_layers || num_q_heads < hkv || num_q_heads % hkv != 0 || D % 2 != 0 ||
+      D / 2 > ptd::kMaxRopeHalf || !slots || !positions || !q || !k || !v || !q_out || !dev_status || q_stride < qe ||
+      q_out_stride < qe || k_stride < ke || v_stride < ke || !(rope_base > 1.f) || !std::isfinite(rope_base))
+    return PTD_ERR_INVALID_ARG;
+  const size_t es = dtype_size(cache->dtype);
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) |
+       reinterpret_cast<uintptr_t>(q_out)) % es != 0)
+    return PTD_ERR_INVALID_ARG;
+  if (q_out == q && q_out_stride != q_stride) return PTD_ERR_INVALID_ARG;   // rows would overlap other rows
+  ptd::PromptRopeParams p = {};
+  p.slots = slots;
+  p.positions = positions;
+  p.n_tokens = prompt->total_tokens;
+  p.head_dim = D;
+  p.hq = num_q_heads;
+  p.hkv = hkv;
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.q_out = q_out;
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.q_out_stride = q_out_stride;
+  p.layer_rows = cache_rows_per_layer(cache, prompt->batch);
+  const size_t layer_bytes = (size_t)layer * p.layer_rows * ke * es;
+  p.k_layer = static_cast<uint8_t*>(cache->k) + layer_bytes;
+  p.v_layer = static_cast<uint8_t*>(cache->v) + layer_bytes;
+  p.dev_status = dev_status;
+  st = cuda_status(ptd::launch_prompt_rope(p, cache->dtype == PTD_BF16, rope_freqs(rope_base, D),
+                                           num_sms_of_current_device(), static_cast<cudaStream_t>(stream)));
+  if (st == PTD_OK) g_last_launches = 1;
+  return st;
+}
+
+size_t ptd_prompt_attention_workspace_size(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t num_q_heads) {
+  if (check_prompt_attention(prompt, cache, num_q_heads) != PTD_OK) return 0;
+  ptd::PromptAttnParams p = prompt_attention_params(prompt, cache, num_q_heads);
+  return ptd::plan_prompt_attention(p, cache->dtype == PTD_BF16, SIZE_MAX, num_sms_of_current_device());
+}
+
+ptd_status ptd_prompt_attention(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t layer, const void* q,
+                                int64_t q_stride, int32_t num_q_heads, float scale, void* out, void* workspace,
+                                size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  g_last_launches = 0;
+  ptd_status st = check_prompt_attention(prompt, cache, num_q_heads);
+  if (st != PTD_OK) return st;
+  const int D = cache->head_dim;
+  const size_t es = dtype_size(cache->dtype);
+  if (layer < 0 || layer >= cache->num_layers || !q || !out || !dev_status || q_stride < (int64_t)num_q_heads * D ||
+      !aligned16(q) || !aligned16(out) || (q_stride * (int64_t)es) % 16 != 0)
+    return PTD_ERR_INVALID_ARG;
+  ptd::PromptAttnParams p = prompt_attention_params(prompt, cache, num_q_heads);
+  p.q = q;
+  p.out = out;
+  p.q_stride = q_stride;
+  p.layer = layer;
+  p.dev_status = dev_status;
+  const float sc = scale > 0.f ? scale : 1.0f / std::sqrt((float)D);
+  p.scale_log2 = sc * 1.4426950408889634f;
+  p.part_o = static_cast<float*>(workspace);
+  const bool bf16 = cache->dtype == PTD_BF16;
+  ptd::plan_prompt_attention(p, bf16, workspace != nullptr && aligned16(workspace) ? workspace_bytes : 0,
+                             num_sms_of_current_device());
+  if ((int64_t)p.blocks * p.tile_heads * p.splits > INT32_MAX) return PTD_ERR_UNSUPPORTED;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((st = cuda_status(ptd::launch_prompt_attn_simt(p, bf16, s))) != PTD_OK) return st;
+  if (p.splits > 1 && (st = cuda_status(ptd::launch_prompt_attn_merge(p, bf16, s))) != PTD_OK) return st;
+  g_last_launches = p.splits > 1 ? 2 : 1;
+  return PTD_OK;
 }
 
 ptd_status ptd_check_bounded_wait(int32_t* dev_status, void* stream) {

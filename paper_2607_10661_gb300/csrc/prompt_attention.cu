@@ -1,0 +1,124 @@
+// Prompt attention: the choice of tiles and of the cut of the keys, and the merge of the pieces.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "launch.cuh"
+#include "prompt_attention.cuh"
+#include "ptd_device.cuh"
+
+namespace ptd {
+namespace pa {
+
+constexpr int kMergeThreads = 256;
+
+// The rows of one split block, from its pieces: O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s, M the
+// maximum of the m_s (a row that saw no key of a piece has l_s = 0, and its O_s was not written).  One CTA a
+// block and head tile; a thread takes one row and four columns at a time, consecutive threads consecutive
+// rows, as the partials lie.  Bound by the latency of the chain unit, (m, l), partials.
+template <typename T>
+__global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const PromptAttnParams p) {
+  __shared__ Unit unit_s;
+  __shared__ int found_s;
+  if (threadIdx.x == 0) grid_launch_dependents();
+  grid_dependency_wait();
+  if (threadIdx.x < 32) {
+    auto seq = [&](int b) { return blocks_of(p, b); };
+    const int max_key = p.batch == 1 ? 0 : max_block_key(seq, p.batch);
+    Unit u;
+    const bool found = find_unit(p, seq, max_key, blockIdx.x, u);
+    if (threadIdx.x == 0) {
+      if (found) unit_s = u;
+      found_s = found;
+    }
+  }
+  __syncthreads();
+  if (!found_s) return;
+  const Unit u = unit_s;
+  const int rows = u.tokens * p.sub, groups = p.head_dim / 4, used = p.tile_tokens * p.sub;
+  const int block_rows = p.block_tokens / p.tile_tokens * p.tile_rows;
+  const size_t piece0 = (size_t)blockIdx.x * p.splits;
+  auto empty = [&](int s) {
+    int k0, k1;
+    piece_range(u.tiles, s, p.splits, k0, k1);
+    return k0 == k1;
+  };
+  for (int e = threadIdx.x; e < rows * groups; e += kMergeThreads) {
+    const int c = e / rows, r = e - c * rows;
+    const int at = r / used * p.tile_rows + r % used;
+    const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + piece0 * block_rows + at;
+    const float4* po = reinterpret_cast<const float4*>(p.part_o) + (piece0 * groups + c) * block_rows + at;
+    float M = -INFINITY, L = 0.f;
+    for (int s = 0; s < p.splits; ++s) {
+      if (empty(s)) continue;
+      const float2 x = __ldcg(ml + (size_t)s * block_rows);
+      if (!(x.y == 0.f)) M = fmaxf(M, x.x);
+    }
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < p.splits; ++s) {
+      if (empty(s)) continue;
+      const float2 x = __ldcg(ml + (size_t)s * block_rows);
+      if (x.y == 0.f) continue;   // (not l > 0: a NaN among the scores has to reach the output)
+      const float w = exp2f(x.x - M);
+      const float4 o = __ldcg(po + (size_t)s * groups * block_rows);
+      L += w * x.y;
+      acc.x += w * o.x;
+      acc.y += w * o.y;
+      acc.z += w * o.z;
+      acc.w += w * o.w;
+    }
+    const float inv = 1.f / L;
+    T* dst = static_cast<T*>(p.out) + ((size_t)(u.row0 + r / p.sub) * p.hq + u.head0 + r % p.sub) * p.head_dim + c * 4;
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+    } else {
+      *reinterpret_cast<float4*>(dst) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    }
+  }
+}
+
+// The largest divisor of `group` that is at most `most`.
+int largest_divisor(int group, int most) {
+  for (int d = group < most ? group : most; d > 1; --d)
+    if (group % d == 0) return d;
+  return 1;
+}
+
+}  // namespace pa
+
+size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int sms) {
+  const int tile_rows = 64, tiles = 1, group = p.hq / p.hkv;
+  (void)bf16;
+  p.tile_rows = tile_rows;
+  p.key_tile = 64;
+  p.sub = pa::largest_divisor(group, tile_rows);
+  p.tile_heads = p.hq / p.sub;
+  p.tiles_per_kv = group / p.sub;
+  p.tile_tokens = tile_rows / p.sub;
+  p.block_tokens = tiles * p.tile_tokens;
+  const int64_t w = p.block_tokens, N = p.bounds.n_total, B = p.batch;
+  const int64_t by_total = N / w + B, by_longest = B * ((p.bounds.max_tokens + w - 1) / w);
+  p.blocks = (int)(by_total < by_longest ? by_total : by_longest);
+  const int64_t units = (int64_t)p.blocks * p.tile_heads;
+  const int64_t key_tiles = ((int64_t)p.bounds.max_ctx + p.bounds.max_tokens + p.key_tile - 1) / p.key_tile;
+  // as many pieces as give every SM one, of two key tiles or more
+  int64_t splits = units > 0 ? sms / units : 1;
+  if (splits > key_tiles / 2) splits = key_tiles / 2;
+  p.splits = splits < 1 ? 1 : (int)splits;
+  const size_t bytes = p.splits == 1 ? 0 : (size_t)units * p.splits * tiles * tile_rows * (p.head_dim + 2) * sizeof(float);
+  if (bytes > scratch) {
+    p.splits = 1;
+    return 0;
+  }
+  if (bytes > 0) p.part_ml = p.part_o + (size_t)units * p.splits * tiles * tile_rows * p.head_dim;
+  return bytes;
+}
+
+cudaError_t launch_prompt_attn_merge(const PromptAttnParams& p, bool bf16, cudaStream_t stream) {
+  const auto kernel = bf16 ? pa::prompt_merge_kernel<__nv_bfloat16> : pa::prompt_merge_kernel<float>;
+  return launch_chained(kernel, dim3((unsigned)(p.blocks * p.tile_heads)), dim3(pa::kMergeThreads), 0, stream, 0, p);
+}
+
+}  // namespace ptd

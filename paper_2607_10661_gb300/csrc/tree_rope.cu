@@ -26,63 +26,16 @@
 
 #include "launch.cuh"
 #include "ptd_device.cuh"
+#include "rope_parts.cuh"
 #include "row_division.cuh"
 #include "tree_rope.cuh"
 
 namespace ptd {
 namespace tr {
 
+using namespace rope;
+
 constexpr int kThreads = 256;
-
-template <typename T>
-__device__ __forceinline__ float ld(const T* p);
-template <>
-__device__ __forceinline__ float ld<float>(const float* p) { return *p; }
-template <>
-__device__ __forceinline__ float ld<__nv_bfloat16>(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-template <typename T>
-__device__ __forceinline__ void st(T* p, float x);
-template <>
-__device__ __forceinline__ void st<float>(float* p, float x) { *p = x; }
-template <>
-__device__ __forceinline__ void st<__nv_bfloat16>(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
-
-// One 16-byte vector of T: 16 / sizeof(T) elements, widened to fp32.
-template <typename T>
-struct Vec {
-  static constexpr int N = 16 / sizeof(T);
-  float x[N];
-};
-template <typename T>
-__device__ __forceinline__ Vec<T> unpack16(const uint4& u) {
-  Vec<T> r;
-  if constexpr (sizeof(T) == 2) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      r.x[2 * i] = __uint_as_float(w[i] << 16);
-      r.x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-  } else {
-    r.x[0] = __uint_as_float(u.x), r.x[1] = __uint_as_float(u.y), r.x[2] = __uint_as_float(u.z),
-    r.x[3] = __uint_as_float(u.w);
-  }
-  return r;
-}
-template <typename T>
-__device__ __forceinline__ uint4 pack16(const Vec<T>& r) {
-  if constexpr (sizeof(T) == 2) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(r.x[2 * i], r.x[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&h);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-  } else {
-    return make_uint4(__float_as_uint(r.x[0]), __float_as_uint(r.x[1]), __float_as_uint(r.x[2]), __float_as_uint(r.x[3]));
-  }
-}
 
 // What every thread of a CTA works out for its node: the tree, the position and the cache row.
 struct Place {
@@ -142,18 +95,8 @@ __device__ __forceinline__ bool find_place(const int32_t* node_offsets, const in
 }
 
 // cos and sin of pos * f_j for j < half, into shared memory (the caller's barrier follows).
-__device__ __forceinline__ void make_table(const RopeFreqs& freqs, int pos_i, int half, float* cos_s, float* sin_s) {
-  for (int j = threadIdx.x; j < half; j += kThreads) {
-    // angle = pos * (hi + lo) = a_hi + a_err (a_err exact up to pos * lo's rounding); sin
-    // and cos of a_hi, corrected to first order in a_err (|a_err| < 1e-3)
-    const float pos = (float)pos_i, fh = freqs.hi[j];
-    const float a_hi = __fmul_rn(pos, fh);
-    const float a_err = fmaf(pos, fh, -a_hi) + pos * freqs.lo[j];
-    float s0, c0;
-    sincosf(a_hi, &s0, &c0);
-    sin_s[j] = fmaf(a_err, c0, s0);
-    cos_s[j] = fmaf(-a_err, s0, c0);
-  }
+__device__ __forceinline__ void make_table(const RopeFreqs& freqs, int pos, int half, float* cos_s, float* sin_s) {
+  for (int j = threadIdx.x; j < half; j += kThreads) turn_of<false>(freqs, pos, j, cos_s[j], sin_s[j]);
 }
 
 // Rows of 16-byte vectors.  A row of q, k or v is cut into items of two vectors, columns j and

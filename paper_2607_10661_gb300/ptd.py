@@ -20,11 +20,13 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libptd.so")
 
 OK, INVALID_ARG, INVALID_TREE, UNSUPPORTED, CUDA_ERROR, TIMEOUT, WORKSPACE, POOL_FULL = range(8)
+INVALID_BATCH, NO_PAGES = 8, 9
 F32, BF16 = 0, 1
 MAX_TREE_NODES = 128
 MAX_TOPK = 16
 MAX_EXPAND = 16
 POOL_KIDS = 8
+MAX_PROMPT_BATCH = 8192
 
 EXPORTED = (
     "ptd_attention_workspace_size", "ptd_tree_attention", "ptd_topk_draft", "ptd_verify_greedy",
@@ -34,7 +36,8 @@ EXPORTED = (
     "ptd_tree_rope_append", "ptd_lm_head_topk_workspace_size", "ptd_lm_head_topk", "ptd_pipeline_create",
     "ptd_pipeline_submit", "ptd_pipeline_wait", "ptd_pipeline_destroy", "ptd_check_bounded_wait",
     "ptd_step_workspace_size", "ptd_step_topk_policy", "ptd_step_tail", "ptd_attention_plan",
-    "ptd_tree_attention_as",
+    "ptd_tree_attention_as", "ptd_prompt_slots", "ptd_prompt_rope_append", "ptd_prompt_attention_workspace_size",
+    "ptd_prompt_attention",
 )
 ATTN_AUTO, ATTN_UNIT, ATTN_CUT, ATTN_CLUSTER, ATTN_F32_CORES, ATTN_F32_TENSOR = range(6)
 
@@ -66,6 +69,16 @@ class _StepArgs(ctypes.Structure):
                 ("accept_len", ctypes.c_void_p), ("bonus_token", ctypes.c_void_p),
                 ("new_ctx_lens", ctypes.c_void_p), ("dev_status", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
                 ("workspace_bytes", ctypes.c_size_t)]
+
+
+class _Prompt(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("total_tokens", ctypes.c_int32), ("max_tokens", ctypes.c_int32),
+                ("max_ctx", ctypes.c_int32), ("token_offsets", ctypes.c_void_p), ("ctx_lens", ctypes.c_void_p)]
+
+
+class _PagePool(ctypes.Structure):
+    _fields_ = [("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p), ("held", ctypes.c_void_p),
+                ("new_held", ctypes.c_void_p), ("new_free_count", ctypes.c_void_p), ("block_table", ctypes.c_void_p)]
 
 
 class _HostIO(ctypes.Structure):
@@ -148,6 +161,15 @@ def lib() -> ctypes.CDLL:
         L.ptd_tree_verify_step.argtypes = [P(_Tree), P(_Cache), P(_StepArgs), vp]
         L.ptd_tree_verify_step_host.restype = ctypes.c_int
         L.ptd_tree_verify_step_host.argtypes = [P(_Tree), P(_Cache), P(_StepArgs), P(_HostIO), vp]
+        L.ptd_prompt_slots.restype = ctypes.c_int
+        L.ptd_prompt_slots.argtypes = [P(_Prompt), P(_Cache), P(_PagePool), vp, vp, vp, vp]
+        L.ptd_prompt_rope_append.restype = ctypes.c_int
+        L.ptd_prompt_rope_append.argtypes = [P(_Prompt), P(_Cache), i32, vp, vp, vp, i64, i32, vp, i64, vp, i64, f32, vp,
+                                             i64, vp, vp]
+        L.ptd_prompt_attention_workspace_size.restype = sz
+        L.ptd_prompt_attention_workspace_size.argtypes = [P(_Prompt), P(_Cache), i32]
+        L.ptd_prompt_attention.restype = ctypes.c_int
+        L.ptd_prompt_attention.argtypes = [P(_Prompt), P(_Cache), i32, vp, i64, i32, f32, vp, vp, sz, vp, vp]
         _lib = L
     return _lib
 
@@ -569,6 +591,125 @@ def tree_rope_append(tree: Tree, cache: KVCache, layer_begin: int, q: torch.Tens
                                     None if positions_out is None else _dev(positions_out, "positions_out", torch.int32),
                                     _dev(dev_status, "dev_status", torch.int32), _stream(stream))
     _check(st, "ptd_tree_rope_append")
+    return last_launch_count()
+
+
+class Prompt:
+    """A packed batch of new tokens in device memory (token_offsets [B+1], ctx_lens [B], int32); total_tokens is
+    the number of rows of the token buffers (padding rows behind the last sequence included)."""
+
+    def __init__(self, token_offsets: torch.Tensor, ctx_lens: torch.Tensor, total_tokens: int, max_tokens: int,
+                 max_ctx: int):
+        self.token_offsets, self.ctx_lens = token_offsets, ctx_lens
+        self.batch, self.total_tokens = ctx_lens.numel(), int(total_tokens)
+        if token_offsets.numel() != self.batch + 1:
+            raise ValueError("token_offsets needs one entry more than ctx_lens")
+        self.c = _Prompt(self.batch, self.total_tokens, int(max_tokens), int(max_ctx),
+                         _dev(token_offsets, "token_offsets", torch.int32), _dev(ctx_lens, "ctx_lens", torch.int32))
+
+
+class PagePool:
+    """The free pages of a paged cache (a stack of free_count pages) and the pages that each sequence holds;
+    new_held and new_free_count receive the counts after a prompt_slots call."""
+
+    def __init__(self, free_pages: torch.Tensor, free_count: torch.Tensor, held: torch.Tensor, new_held: torch.Tensor,
+                 new_free_count: torch.Tensor):
+        if new_held.numel() != held.numel():
+            raise ValueError("held and new_held need an entry per sequence")
+        self.free_pages, self.free_count, self.held = free_pages, free_count, held
+        self.new_held, self.new_free_count = new_held, new_free_count
+        self.ptrs = tuple(_dev(t, n, torch.int32) for t, n in (
+            (free_pages, "free_pages"), (free_count, "free_count"), (held, "held"), (new_held, "new_held"),
+            (new_free_count, "new_free_count")))
+
+
+def _one_device(*tensors):
+    """A guard that makes the tensors' device the current one (ValueError if they are on several)."""
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1:
+        raise ValueError(f"tensors on several devices: {sorted(map(str, devices))}")
+    return torch.cuda.device(devices.pop())
+
+
+def _rows3(t: torch.Tensor, name: str, dtype, rows: int, heads: Optional[int], dim: int):
+    """Pointer, token stride and heads of a [rows, heads, dim] tensor whose tokens may be apart."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 3 or t.shape[0] != rows or t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} must be [{rows}, {'heads' if heads is None else heads}, {dim}], got {tuple(t.shape)}")
+    h, stride = t.shape[1], t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1] * dim)
+    if (dim > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != dim) or stride < h * dim:
+        raise ValueError(f"{name}: a token's heads must be back to back")
+    return t.data_ptr(), stride, h
+
+
+def prompt_slots(prompt: Prompt, cache: KVCache, slots: torch.Tensor, positions: torch.Tensor, dev_status: torch.Tensor,
+                 pages: Optional[PagePool] = None, stream=None) -> int:
+    """ptd_prompt_slots: slots, positions [total_tokens] int32; with `pages`, the block table's new entries too."""
+    n = prompt.total_tokens
+    for t, nm in ((slots, "slots"), (positions, "positions")):
+        if t.numel() != n:
+            raise ValueError(f"{nm} needs total_tokens = {n} entries")
+    pool = None
+    if pages is not None:
+        if cache.block_table is None:
+            raise ValueError("a page pool needs a paged cache")
+        if cache.block_table.shape[0] != prompt.batch or pages.held.numel() != prompt.batch:
+            raise ValueError("block_table and held need a row per sequence")
+        if pages.free_pages.numel() != cache.c.num_pages:
+            raise ValueError("free_pages needs an entry per page of the cache")
+        pool = _PagePool(*pages.ptrs, cache.block_table.data_ptr())
+    with _one_device(slots, positions, dev_status, prompt.ctx_lens, cache.k, pages.held if pages is not None else None):
+        st = lib().ptd_prompt_slots(ctypes.byref(prompt.c), ctypes.byref(cache.c), None if pool is None else ctypes.byref(pool),
+                                    _dev(slots, "slots", torch.int32), _dev(positions, "positions", torch.int32),
+                                    _dev(dev_status, "dev_status", torch.int32), _stream(stream))
+    _check(st, "ptd_prompt_slots")
+    return last_launch_count()
+
+
+def prompt_rope_append(prompt: Prompt, cache: KVCache, layer: int, slots: torch.Tensor, positions: torch.Tensor,
+                       q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_out: torch.Tensor, rope_base: float,
+                       dev_status: torch.Tensor, stream=None) -> int:
+    """ptd_prompt_rope_append: q, q_out [N, Hq, D], k, v [N, Hkv, D] (token strides are free: views of a fused
+    product's rows); q_out may be q."""
+    n, d, dt = prompt.total_tokens, cache.head_dim, cache.k.dtype
+    qp, qs, hq = _rows3(q, "q", dt, n, None, d)
+    kp, ks, _ = _rows3(k, "k", dt, n, cache.num_kv_heads, d)
+    vp, vs, _ = _rows3(v, "v", dt, n, cache.num_kv_heads, d)
+    op, os_, _ = _rows3(q_out, "q_out", dt, n, hq, d)
+    if slots.numel() != n or positions.numel() != n:
+        raise ValueError(f"slots and positions need total_tokens = {n} entries")
+    with _one_device(q, k, v, q_out, slots, positions, dev_status, cache.k):
+        st = lib().ptd_prompt_rope_append(ctypes.byref(prompt.c), ctypes.byref(cache.c), int(layer),
+                                          _dev(slots, "slots", torch.int32), _dev(positions, "positions", torch.int32),
+                                          qp, qs, hq, kp, ks, vp, vs, float(rope_base), op, os_,
+                                          _dev(dev_status, "dev_status", torch.int32), _stream(stream))
+    _check(st, "ptd_prompt_rope_append")
+    return last_launch_count()
+
+
+def prompt_attention_workspace_size(prompt: Prompt, cache: KVCache, num_q_heads: int) -> int:
+    return int(lib().ptd_prompt_attention_workspace_size(ctypes.byref(prompt.c), ctypes.byref(cache.c), int(num_q_heads)))
+
+
+def prompt_attention(prompt: Prompt, cache: KVCache, layer: int, q: torch.Tensor, out: torch.Tensor,
+                     dev_status: torch.Tensor, scale: float = 0.0, workspace: Optional[torch.Tensor] = None,
+                     stream=None) -> int:
+    """ptd_prompt_attention: q [N, Hq, D] (its token stride is free), out [N, Hq, D] contiguous."""
+    n, d, dt = prompt.total_tokens, cache.head_dim, cache.k.dtype
+    qp, qs, hq = _rows3(q, "q", dt, n, None, d)
+    if tuple(out.shape) != (n, hq, d):
+        raise ValueError(f"out must be [{n}, {hq}, {d}]")
+    with _one_device(q, out, dev_status, workspace, cache.k, prompt.ctx_lens):
+        st = lib().ptd_prompt_attention(ctypes.byref(prompt.c), ctypes.byref(cache.c), int(layer), qp, qs, hq, float(scale),
+                                        _dev(out, "out", dt), None if workspace is None else _dev(workspace, "workspace"),
+                                        0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                        _dev(dev_status, "dev_status", torch.int32), _stream(stream))
+    _check(st, "ptd_prompt_attention")
     return last_launch_count()
 
 

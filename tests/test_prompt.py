@@ -1,0 +1,204 @@
+"""The prompt path without a GPU: the numbering of the attention's work units (csrc/prompt_geometry.cuh, compiled
+for the host) against a sort, the host's refusals, and the oracle's own examples."""
+import ctypes
+import os
+import random
+import subprocess
+
+import numpy as np
+import pytest
+
+import oracle
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+SOURCE = r"""
+#include <cstdio>
+#include "prompt_geometry.cuh"
+// stdin: width batch, then (ctx, tokens) per sequence; prints every block in order, and whether the first
+// number past them is refused.
+int main() {
+  int width, batch;
+  while (std::scanf("%d %d", &width, &batch) == 2) {
+    static int ctx[4096], n[4096];
+    int max_key = 0, total = 0;
+    for (int b = 0; b < batch; ++b) {
+      if (std::scanf("%d %d", ctx + b, n + b) != 2) return 1;
+      const ptd::PromptBlocks s = ptd::prompt_blocks(ctx[b], n[b], width);
+      if (s.first + s.count > max_key) max_key = s.first + s.count;
+      total += s.count;
+    }
+    auto seq = [&](int b) { return ptd::prompt_blocks(ctx[b], n[b], width); };
+    int b, i;
+    for (int u = 0; u < total; ++u) {
+      if (!ptd::find_prompt_block(ptd::OneLane{}, seq, batch, max_key, u, &b, &i)) return 1;
+      std::printf("%d,%d ", b, i);
+    }
+    std::printf("%d\n", ptd::find_prompt_block(ptd::OneLane{}, seq, batch, max_key, total, &b, &i) ||
+                            ptd::find_prompt_block(ptd::OneLane{}, seq, batch, max_key, -1, &b, &i));
+  }
+  return 0;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import __graft_entry__
+    from paper_2607_10661_gb300 import ptd
+
+    __graft_entry__.build()
+    return ptd.lib()
+
+
+def test_blocks_are_numbered_longest_first(tmp_path):
+    rng = random.Random(5)
+    cases = [(64, [(0, 0)]), (64, [(5, 1)]), (64, [(100, 640)]), (1, [(3, 4), (0, 9), (5, 0), (2, 2)]),
+             (256, [(0, 0), (0, 0)])]
+    for _ in range(60):
+        seqs = [(rng.choice([0, rng.randrange(5000)]), rng.choice([0, 1, rng.randrange(3000)]))
+                for _ in range(rng.randrange(1, 70))]
+        cases.append((rng.choice([2, 10, 25, 36, 64, 256]), seqs))
+    src, exe = tmp_path / "geometry.cpp", tmp_path / "geometry"
+    src.write_text(SOURCE)
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I", os.path.join(ROOT, "paper_2607_10661_gb300", "csrc"), str(src),
+                    "-o", str(exe)], check=True)
+    text = "\n".join(f"{w} {len(s)} " + " ".join(f"{c} {n}" for c, n in s) for w, s in cases)
+    r = subprocess.run([str(exe)], input=text, capture_output=True, text=True)
+    assert r.returncode == 0
+    for (width, seqs), line in zip(cases, r.stdout.strip("\n").split("\n")):
+        blocks = [(-(c // width + i), b, i) for b, (c, n) in enumerate(seqs) for i in range(-(-n // width))]
+        want = [f"{b},{i}" for _, b, i in sorted(blocks)] + ["0"]
+        assert line.split() == want, (width, seqs)
+
+
+def test_sequences_out_of_bounds(tmp_path):
+    src, exe = tmp_path / "ok.cpp", tmp_path / "ok"
+    src.write_text(r"""
+#include <cstdio>
+#include "prompt_geometry.cuh"
+int main() {
+  const ptd::PromptBounds p = {100, 40, 1000, 1020};
+  const int c[][4] = {{0, 40, 0, 1},   {0, 41, 0, 0},    {60, 100, 980, 1}, {60, 100, 981, 0}, {61, 101, 0, 0},
+                      {-1, 3, 0, 0},   {5, 4, 0, 0},     {5, 5, 1000, 1},   {5, 5, 1001, 0},   {5, 6, -1, 0},
+                      {0, 0, 0, 1},    {2147483647, -2147483647, 0, 0},     {0, 20, 1000, 1},  {0, 21, 1000, 0}};
+  for (auto& x : c)
+    if (ptd::prompt_sequence_ok(p, x[0], x[1], x[2]) != (x[3] == 1)) return std::printf("%d %d %d\n", x[0], x[1], x[2]), 1;
+  return 0;
+}
+""")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I", os.path.join(ROOT, "paper_2607_10661_gb300", "csrc"), str(src),
+                    "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout
+
+
+A = 1 << 24   # stands for device memory: host checks never read it
+
+
+def _prompt(ptd, batch=2, total=10, max_tokens=8, max_ctx=100, offsets=A, ctx=A + 4096):
+    return ptd._Prompt(batch, total, max_tokens, max_ctx, offsets, ctx)
+
+
+def _cache(ptd, page=16, dtype=None, hkv=8, d=128, layers=2, num_pages=40, max_pages=10, k=2 * A):
+    dt = ptd.BF16 if dtype is None else dtype
+    return ptd._Cache(k, 3 * A, dt, layers, hkv, d, page, 0 if page else 300, num_pages if page else 0,
+                      A + 8192 if page else None, max_pages if page else 0)
+
+
+def test_prompt_slots_refusals(lib):
+    from paper_2607_10661_gb300 import ptd
+
+    def call(prompt, cache, pool="default", slots=4 * A, positions=5 * A, status=6 * A):
+        if pool == "default":
+            pool = ptd._PagePool(7 * A, 8 * A, 9 * A, 10 * A, 11 * A, cache.block_table)
+        return lib.ptd_prompt_slots(ctypes.byref(prompt) if prompt else None, ctypes.byref(cache),
+                                    ctypes.byref(pool) if pool else None, slots, positions, status, None)
+
+    ok_p, ok_c = _prompt(ptd), _cache(ptd)
+    bad = ptd.INVALID_ARG
+    assert call(None, ok_c) == bad
+    for p in (_prompt(ptd, batch=0), _prompt(ptd, total=0), _prompt(ptd, max_tokens=0), _prompt(ptd, max_ctx=-1),
+              _prompt(ptd, offsets=None), _prompt(ptd, ctx=None), _prompt(ptd, max_tokens=2**31 - 1)):
+        assert call(p, ok_c) == bad
+    assert call(_prompt(ptd, batch=8193), ok_c) == ptd.UNSUPPORTED
+    assert call(ok_p, ok_c, slots=None) == bad and call(ok_p, ok_c, positions=None) == bad
+    assert call(ok_p, ok_c, status=None) == bad
+    assert call(ok_p, _cache(ptd, page=0), pool=ptd._PagePool(7 * A, 8 * A, 9 * A, 10 * A, 11 * A, None)) == bad
+    assert call(ok_p, _cache(ptd, page=24)) == ptd.UNSUPPORTED
+    assert call(ok_p, _cache(ptd, num_pages=1 << 28)) == ptd.UNSUPPORTED            # 2^32 rows a layer
+    assert call(_prompt(ptd, batch=4096), _cache(ptd, max_pages=1 << 20)) == ptd.UNSUPPORTED
+    for i in range(6):   # each member missing
+        m = [7 * A, 8 * A, 9 * A, 10 * A, 11 * A, ok_c.block_table]
+        m[i] = None
+        assert call(ok_p, ok_c, pool=ptd._PagePool(*m)) == bad
+    t = ok_c.block_table
+    for m in ((7 * A, 8 * A, 9 * A, 9 * A, 11 * A, t), (7 * A, 8 * A, 9 * A, 9 * A + 4, 11 * A, t),   # new_held on held
+              (7 * A, 8 * A, 9 * A, 10 * A, 8 * A, t),                                                # new count on count
+              (7 * A, 7 * A + 8, 9 * A, 10 * A, 11 * A, t),                                           # count in the stack
+              (7 * A, 8 * A, 9 * A, 10 * A, 11 * A, 12 * A),                                          # another table
+              (4 * A + 8, 8 * A, 9 * A, 10 * A, 11 * A, t)):                                          # slots on the stack
+        assert call(ok_p, ok_c, pool=ptd._PagePool(*m)) == bad, m
+
+
+def test_prompt_rope_append_refusals(lib):
+    from paper_2607_10661_gb300 import ptd
+
+    def call(cache=None, layer=0, slots=4 * A, positions=5 * A, q=7 * A, qs=4096, hq=32, k=8 * A, ks=1024, v=9 * A, vs=1024,
+             base=1e4, out=10 * A, outs=4096, status=6 * A):
+        return lib.ptd_prompt_rope_append(ctypes.byref(_prompt(ptd)), ctypes.byref(cache or _cache(ptd)), layer, slots,
+                                          positions, q, qs, hq, k, ks, v, vs, base, out, outs, status, None)
+
+    for kw in (dict(layer=-1), dict(layer=2), dict(slots=None), dict(positions=None), dict(q=None), dict(k=None),
+               dict(v=None), dict(out=None), dict(status=None), dict(qs=4095), dict(ks=1023), dict(vs=0), dict(outs=-4096),
+               dict(hq=30), dict(hq=0), dict(base=1.0), dict(base=float("inf")), dict(base=float("nan")),
+               dict(q=7 * A + 1), dict(out=10 * A + 1), dict(out=7 * A, qs=5000),
+               dict(cache=_cache(ptd, d=127, hkv=16), qs=10**6, ks=10**6, vs=10**6),
+               dict(cache=_cache(ptd, d=264), qs=10**6, outs=10**6, ks=10**6, vs=10**6)):
+        assert call(**kw) == ptd.INVALID_ARG, kw
+    # cache rows of 24 bytes: not a multiple of 16
+    assert call(cache=_cache(ptd, dtype=ptd.F32, hkv=1, d=6)) == ptd.UNSUPPORTED
+
+
+def test_prompt_attention_refusals(lib):
+    from paper_2607_10661_gb300 import ptd
+
+    def call(prompt=None, cache=None, layer=0, q=7 * A, qs=4096, hq=32, out=8 * A, status=6 * A):
+        return lib.ptd_prompt_attention(ctypes.byref(prompt or _prompt(ptd)), ctypes.byref(cache or _cache(ptd)), layer, q, qs,
+                                        hq, 0.0, out, None, 0, status, None)
+
+    for kw in (dict(layer=-1), dict(layer=2), dict(q=None), dict(out=None), dict(status=None), dict(qs=4095), dict(qs=4097),
+               dict(hq=30), dict(hq=0), dict(q=7 * A + 2), dict(out=8 * A + 8), dict(prompt=_prompt(ptd, batch=0)),
+               dict(cache=_cache(ptd, k=2 * A + 8))):
+        assert call(**kw) == ptd.INVALID_ARG, kw
+    for kw in (dict(cache=_cache(ptd, d=64)), dict(cache=_cache(ptd, dtype=ptd.F32, d=96)), dict(cache=_cache(ptd, page=8)),
+               dict(prompt=_prompt(ptd, batch=8193))):
+        assert call(**kw) == ptd.UNSUPPORTED, kw
+    size = lambda p, c, hq=32: lib.ptd_prompt_attention_workspace_size(ctypes.byref(p), ctypes.byref(c), hq)
+    assert size(_prompt(ptd), _cache(ptd), 30) == 0 and size(_prompt(ptd), _cache(ptd, d=64)) == 0
+    # a token far into a sequence: its keys are split; a prompt that fills the SMs by itself: none
+    assert size(_prompt(ptd, 1, 1, 1, 30000), _cache(ptd, page=0)) > 0
+    assert size(_prompt(ptd, 1, 20000, 20000, 0), _cache(ptd, page=0)) == 0
+
+
+def test_oracle_pages_by_hand():
+    """Pages of 16: sequence 0 (20 + 13 positions) has 2 pages and needs 3, sequence 1 is finished and gives 7 and
+    9 back, sequence 2 is new and needs 2, sequence 3 stays in its page."""
+    table = [[4, 2, -1], [7, 9, -1], [-1, -1, -1], [5, -1, -1]]
+    t, held, free = oracle.prompt_pages([20, 0, 0, 3], [13, 0, 17, 1], [2, 2, 0, 1], table, [11, 8], 16)
+    assert t == [[4, 2, 9], [7, 9, -1], [7, 8, -1], [5, -1, -1]] and held == [3, 0, 2, 1] and free == [11]
+    assert oracle.prompt_pages([20, 0, 0, 3], [13, 0, 65, 1], [2, 2, 0, 1], [r + [-1] * 3 for r in table], [11, 8], 16) is None
+    slots, pos = oracle.prompt_slots([20, 0, 0, 3], [13, 0, 17, 1], t, 16)
+    assert slots[:13] == [2 * 16 + 4 + i for i in range(12)] + [9 * 16] and pos[:13] == list(range(20, 33))
+    assert slots[13:] == [7 * 16 + i for i in range(16)] + [8 * 16, 5 * 16 + 3] and pos[-1] == 3
+    assert oracle.prompt_slots([2, 5], [2, 1], None, -50)[0] == [2, 3, 55]
+
+
+def test_oracle_causal_attention_is_a_chain_tree():
+    rng = np.random.default_rng(1)
+    q, k, v = rng.standard_normal((9, 4, 8)), rng.standard_normal((14, 2, 8)), rng.standard_normal((14, 2, 8))
+    o, size = oracle.causal_attention(q, k, v, 5)
+    want = oracle.tree_attention(q, k, v, [-1] + list(range(8)), 5)
+    assert np.abs(o - want).max() < 1e-14 and (size >= np.abs(o) - 1e-15).all()
+    one, _ = oracle.causal_attention(q[:1], k, v, 0)
+    assert np.array_equal(one[0], np.repeat(v[0], 2, axis=0))
