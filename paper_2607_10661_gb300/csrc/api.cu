@@ -886,7 +886,26 @@ ptd_status ptd_prompt_attention(const ptd_prompt* prompt, const ptd_kv_cache* ca
                              num_sms_of_current_device());
   if ((int64_t)p.blocks * p.tile_heads * p.splits > INT32_MAX) return PTD_ERR_UNSUPPORTED;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if ((st = cuda_status(ptd::launch_prompt_attn_simt(p, bf16, s))) != PTD_OK) return st;
+  if (bf16) {
+    if (cache_rows_per_layer(cache, prompt->batch) * cache->num_layers > INT32_MAX) return PTD_ERR_UNSUPPORTED;
+    CUtensorMap map_k, map_v, map_q;
+    const uint32_t box_rows = (uint32_t)(cache->page_size > 0 ? cache->page_size : 128);
+    PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
+    if (!enc || !encode_cache(&map_k, cache, prompt->batch, cache->k, 64, box_rows, true) ||
+        !encode_cache(&map_v, cache, prompt->batch, cache->v, 64, box_rows, true))
+      return PTD_ERR_CUDA;
+    const cuuint32_t estride[3] = {1, 1, 1}, qbox[3] = {64, (cuuint32_t)p.sub, (cuuint32_t)p.tile_tokens};
+    const cuuint64_t qdim[3] = {(cuuint64_t)D, (cuuint64_t)num_q_heads, (cuuint64_t)prompt->total_tokens};
+    const cuuint64_t qstep[2] = {(cuuint64_t)D * 2, (cuuint64_t)q_stride * 2};
+    if (enc(&map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), qdim, qstep, qbox, estride,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return PTD_ERR_CUDA;
+    st = cuda_status(ptd::launch_prompt_attn_tc(map_k, map_v, map_q, p, s));
+  } else {
+    st = cuda_status(ptd::launch_prompt_attn_simt(p, s));
+  }
+  if (st != PTD_OK) return st;
   if (p.splits > 1 && (st = cuda_status(ptd::launch_prompt_attn_merge(p, bf16, s))) != PTD_OK) return st;
   g_last_launches = p.splits > 1 ? 2 : 1;
   return PTD_OK;

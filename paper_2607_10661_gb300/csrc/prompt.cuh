@@ -80,8 +80,13 @@ struct PromptAttnParams {
 // tile_heads, tiles_per_kv, tile_tokens, block_tokens, tile_rows, key_tile, blocks and splits.  Returns the
 // scratch that the cut takes (0: unsplit).
 size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int sms);
-cudaError_t launch_prompt_attn_simt(const PromptAttnParams& p, bool bf16, cudaStream_t stream);
-// The merge of split blocks, after it.
+// bf16, D = 128.  map_k, map_v: boxes of 64 columns of one KV head and 128 rows (or a page's); map_q: of 64
+// columns, `sub` heads and tile_tokens tokens; 128-byte swizzle.
+cudaError_t launch_prompt_attn_tc(const CUtensorMap& map_k, const CUtensorMap& map_v, const CUtensorMap& map_q,
+                                  const PromptAttnParams& p, cudaStream_t stream);
+// fp32, D = 32, 64 or 128.
+cudaError_t launch_prompt_attn_simt(const PromptAttnParams& p, cudaStream_t stream);
+// The merge of split blocks, after either.
 cudaError_t launch_prompt_attn_merge(const PromptAttnParams& p, bool bf16, cudaStream_t stream);
 
 }  // namespace ptd

@@ -89,10 +89,9 @@ int largest_divisor(int group, int most) {
 }  // namespace pa
 
 size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int sms) {
-  const int tile_rows = 64, tiles = 1, group = p.hq / p.hkv;
-  (void)bf16;
+  const int tile_rows = bf16 ? 128 : 64, tiles = bf16 ? 2 : 1, group = p.hq / p.hkv;   // M tiles of a block
   p.tile_rows = tile_rows;
-  p.key_tile = 64;
+  p.key_tile = bf16 ? 128 : 64;
   p.sub = pa::largest_divisor(group, tile_rows);
   p.tile_heads = p.hq / p.sub;
   p.tiles_per_kv = group / p.sub;

@@ -1,4 +1,4 @@
-// Causal attention of packed new tokens over the cache, on the CUDA cores.
+// Causal attention of packed new tokens over an fp32 cache, on the CUDA cores.
 //
 // Rows r = token * sub + head of one block of tokens under `sub` query heads of one KV head (64 rows) meet
 // the block's keys in tiles of 64: S = Q K^T, softmax with a running maximum and sum in fp32, O += P V.
@@ -6,7 +6,6 @@
 // Q, K, V and P are in shared memory, O and the statistics in registers.  Key tiles that some row does not
 // see in full take a path that leaves hidden products out, so that what lies in hidden slots (not even an
 // infinity or a NaN of V) never meets a weight of 0.
-#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include <cmath>
@@ -15,7 +14,6 @@
 #include "launch.cuh"
 #include "prompt_attention.cuh"
 #include "ptd_device.cuh"
-#include "rope_parts.cuh"
 
 namespace ptd {
 namespace pa {
@@ -25,17 +23,16 @@ constexpr int kRows = 64;
 constexpr int kKeys = 64;
 constexpr int kPitchP = kKeys + 4;
 
-template <typename T, int D>
+template <int D>
 struct Simt {
   static constexpr int kPitch = D + 4;   // of Q and K rows: 16-byte reads of eight rows meet every bank once
   static constexpr size_t kSmem = (size_t)((kRows + kKeys) * kPitch + kKeys * D + kRows * kPitchP) * sizeof(float);
 };
 
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(kThreads) prompt_simt_kernel(const PromptAttnParams p) {
-  using namespace rope;
   extern __shared__ __align__(16) float smem_f[];
-  constexpr int kPitch = Simt<T, D>::kPitch, V = Vec<T>::N;
+  constexpr int kPitch = Simt<D>::kPitch;
   constexpr int VC = D / 16 < 4 ? D / 16 : 4, NB = D / (16 * VC);   // O columns: nb * 16 VC + x VC + i
   float* Qs = smem_f;
   float* Ks = Qs + kRows * kPitch;
@@ -72,14 +69,13 @@ __global__ void __launch_bounds__(kThreads) prompt_simt_kernel(const PromptAttnP
   const Unit u = unit_s;
   const int rows = u.tokens * p.sub, end = u.ctx + u.token0 + u.tokens;
   // 16-byte chunks of a row: Q
-  for (int e = t; e < kRows * (D / V); e += kThreads) {
-    const int r = e / (D / V), c = (e - r * (D / V)) * V;
-    Vec<T> q = {};
+  for (int e = t; e < kRows * (D / 4); e += kThreads) {
+    const int r = e / (D / 4), c = (e - r * (D / 4)) * 4;
+    float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
     if (r < rows)
-      q = unpack16<T>(*reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + (size_t)(u.row0 + r / p.sub) * p.q_stride +
-                                                      (size_t)(u.head0 + r % p.sub) * D + c));
-#pragma unroll
-    for (int i = 0; i < V; ++i) Qs[r * kPitch + c + i] = q.x[i];
+      q = *reinterpret_cast<const float4*>(static_cast<const float*>(p.q) + (size_t)(u.row0 + r / p.sub) * p.q_stride +
+                                           (size_t)(u.head0 + r % p.sub) * D + c);
+    *reinterpret_cast<float4*>(Qs + r * kPitch + c) = q;
   }
   int last[4];   // the last key that each of this thread's rows sees
 #pragma unroll
@@ -97,9 +93,9 @@ __global__ void __launch_bounds__(kThreads) prompt_simt_kernel(const PromptAttnP
   for (int kt = u.tile0; kt < u.tile1; ++kt) {
     const int key0 = kt * kKeys;
     __syncthreads();   // the tile before has been read
-    for (int e = t; e < kKeys * (D / V); e += kThreads) {
-      const int j = e / (D / V), c = (e - j * (D / V)) * V, key = key0 + j;
-      Vec<T> k = {}, v = {};
+    for (int e = t; e < kKeys * (D / 4); e += kThreads) {
+      const int j = e / (D / 4), c = (e - j * (D / 4)) * 4, key = key0 + j;
+      float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
       if (key < end) {
         size_t row;
         bool there = true;
@@ -112,17 +108,14 @@ __global__ void __launch_bounds__(kThreads) prompt_simt_kernel(const PromptAttnP
         }
         if (there) {
           const size_t at = (row * p.hkv + u.kv) * D + c;
-          k = unpack16<T>(*reinterpret_cast<const uint4*>(static_cast<const T*>(p.k) + at));
-          v = unpack16<T>(*reinterpret_cast<const uint4*>(static_cast<const T*>(p.v) + at));
+          k = *reinterpret_cast<const float4*>(static_cast<const float*>(p.k) + at);
+          v = *reinterpret_cast<const float4*>(static_cast<const float*>(p.v) + at);
         } else {
           atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
         }
       }
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        Ks[j * kPitch + c + i] = k.x[i];
-        Vs[j * D + c + i] = v.x[i];
-      }
+      *reinterpret_cast<float4*>(Ks + j * kPitch + c) = k;
+      *reinterpret_cast<float4*>(Vs + j * D + c) = v;
     }
     __syncthreads();
     float s[4][4];
@@ -224,31 +217,30 @@ __global__ void __launch_bounds__(kThreads) prompt_simt_kernel(const PromptAttnP
         }
     } else {
       const float inv = 1.f / l[a];
-      T* dst = static_cast<T*>(p.out) + ((size_t)(u.row0 + r / p.sub) * p.hq + u.head0 + r % p.sub) * D;
+      float* dst = static_cast<float*>(p.out) + ((size_t)(u.row0 + r / p.sub) * p.hq + u.head0 + r % p.sub) * D;
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int i = 0; i < VC; ++i) st(dst + b * 16 * VC + x * VC + i, o[a][b][i] * inv);
+        for (int i = 0; i < VC; ++i) dst[b * 16 * VC + x * VC + i] = o[a][b][i] * inv;
     }
   }
 }
 
 }  // namespace pa
 
-cudaError_t launch_prompt_attn_simt(const PromptAttnParams& p, bool bf16, cudaStream_t stream) {
+cudaError_t launch_prompt_attn_simt(const PromptAttnParams& p, cudaStream_t stream) {
   const dim3 grid((unsigned)(p.blocks * p.tile_heads * p.splits));
-#define PTD_SIMT_LAUNCH(T, D)                                                                                          \
+#define PTD_SIMT_LAUNCH(D)                                                                                          \
   do {                                                                                                                 \
-    const auto kernel = pa::prompt_simt_kernel<T, D>;                                                                  \
+    const auto kernel = pa::prompt_simt_kernel<D>;                                                                  \
     const cudaError_t e =                                                                                              \
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pa::Simt<T, D>::kSmem);         \
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pa::Simt<D>::kSmem);         \
     if (e != cudaSuccess) return e;                                                                                    \
-    return launch_chained(kernel, grid, dim3(pa::kThreads), pa::Simt<T, D>::kSmem, stream, 0, p);                      \
+    return launch_chained(kernel, grid, dim3(pa::kThreads), pa::Simt<D>::kSmem, stream, 0, p);                      \
   } while (0)
-  if (bf16) PTD_SIMT_LAUNCH(__nv_bfloat16, 128);
-  if (p.head_dim == 32) PTD_SIMT_LAUNCH(float, 32);
-  if (p.head_dim == 64) PTD_SIMT_LAUNCH(float, 64);
-  PTD_SIMT_LAUNCH(float, 128);
+  if (p.head_dim == 32) PTD_SIMT_LAUNCH(32);
+  if (p.head_dim == 64) PTD_SIMT_LAUNCH(64);
+  PTD_SIMT_LAUNCH(128);
 #undef PTD_SIMT_LAUNCH
 }
 

@@ -1,0 +1,590 @@
+// Causal attention of packed new tokens over the cache on the 5th-generation tensor cores (tcgen05 + TMEM +
+// TMA), bf16, D = 128.
+//
+// Work.  `sub` query heads of one KV head and `tile_tokens` tokens form the rows r = token * sub + head of an
+// M tile (128 rows), two M tiles a block, so that 2 * 128 rows share every K and V tile of 128 keys; a block
+// meets only the tiles that its last token sees, each M tile only those that its own does.  A work unit is a
+// (block, head tile), or a piece of its keys (partials, merged by prompt_merge_kernel).  Units are numbered
+// longest first over the whole batch (prompt_geometry.cuh); the grid has one CTA per unit, and a resident CTA
+// takes the numbers of CTAs that have not started yet (cluster launch control), so that the SMs' shares
+// even out whatever the lengths, and a unit's first loads and its set-up run beside the unit before it.
+//
+// Warps (384 threads):
+//   0       TMA producer: K, V (a ring of two stages each), Q of the next unit.
+//   1       TMEM allocator and MMA issuer: S_t = Q_t K^T, O_t += P_t V, in the order
+//             S_0, S_1 | PV_0, S_0', PV_1, S_1' | ...
+//           so that one M tile's softmax runs beside the other's products.
+//   2 - 9   softmax of M tile 0 (2 - 5) and 1 (6 - 9), a thread a row: running maximum, moved only when
+//           exceeded by 2^8, exp2, bf16 weights over S in TMEM, fp32 row sum; O / l at the end.
+//   10      scheduler: the next unit.
+//   11      V check: of key tiles that some row sees in part, infinities and NaN of V are set to 0 (a
+//           weight of 0 must not meet them) and noted; the rows that see such a key add it at the end.
+// TMEM: S_0 | S_1 | O_0 | O_1, 128 fp32 columns each; P_t lies over the first 64 columns of S_t.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "attention_tc.cuh"
+#include "launch.cuh"
+#include "prompt_attention.cuh"
+#include "ptd_device.cuh"
+
+namespace ptd {
+namespace pt {
+
+using pa::Unit;
+using tc::kHalfBytes;
+using tc::kTileBytes;
+
+constexpr int kThreads = 384;
+constexpr int kStages = 2;   // K tiles, and V tiles
+constexpr uint32_t kOffQ = 0;
+constexpr uint32_t kOffK = 2 * kTileBytes;
+constexpr uint32_t kOffV = kOffK + kStages * kTileBytes;
+constexpr uint32_t kOffBar = kOffV + kStages * kTileBytes;
+enum Bar {
+  kFullK = 0,
+  kEmptyK = kFullK + kStages,
+  kFullV = kEmptyK + kStages,
+  kEmptyV = kFullV + kStages,
+  kLoadV = kEmptyV + kStages,   // a V tile that is checked first has landed
+  kSFull = kLoadV + kStages,
+  kPFull = kSFull + 2,
+  kOFull = kPFull + 2,
+  kQFull = kOFull + 2,
+  kQEmpty = kQFull + 2,
+  kSegFull = kQEmpty + 2,
+  kSegEmpty = kSegFull + 2,
+  kClaim = kSegEmpty + 2,
+  kDrain,
+  kBars
+};
+constexpr uint32_t kOffTmemPtr = kOffBar + kBars * 8;
+constexpr uint32_t kOffAbort = kOffTmemPtr + 4;
+constexpr uint32_t kOffClaim = (kOffAbort + 4 + 15) / 16 * 16;   // the scheduler's answer, 16 bytes
+
+// A unit as the roles need it.
+struct Seg {
+  int valid;
+  int b, row0, ctx, token0, tokens, head0, kv;
+  int piece;             // its number among the partials
+  int kt0;               // first key tile
+  int n[2];              // key tiles of either M tile (0: not there, or no keys in this piece)
+  int edge;              // first key tile that some row sees in part
+  int bad;               // the V check found infinities or NaN
+};
+constexpr uint32_t kOffSeg = kOffClaim + 16;
+constexpr int kMaxCached = 512;   // sequences whose blocks are kept in shared memory
+constexpr uint32_t kOffSeqs = kOffSeg + 2 * sizeof(Seg);
+constexpr uint32_t kSmemUsed = kOffSeqs + kMaxCached * sizeof(PromptBlocks);
+constexpr uint32_t kSmemBytes = kSmemUsed + 1024;   // slack to align the base to 1024 B
+static_assert(kSmemBytes <= 232448, "shared memory budget");
+
+// Ask for the number of a CTA of this grid that has not started (16 bytes to `dst`, counted on `bar`).
+__device__ __forceinline__ void claim_cta(uint32_t dst, uint32_t bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(dst),
+               "r"(bar)
+               : "memory");
+}
+// Its blockIdx.x, or -1 if there was none.
+__device__ __forceinline__ int claimed_cta(uint32_t src) {
+  int x;
+  asm volatile(
+      "{\n\t.reg .b128 answer;\n\t.reg .pred got;\n\t.reg .b32 y, z, w;\n\tld.shared.b128 answer, [%1];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 got, answer;\n\tmov.b32 %0, -1;\n\t"
+      "@got clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%0, y, z, w}, answer;\n\t}"
+      : "=r"(x)
+      : "r"(src)
+      : "memory");
+  return x;
+}
+
+// Softmax of one key tile of this thread's row: S (TMEM at tS) becomes the bf16 P over its first 64 columns,
+// against the reference maximum m_run (log2 units), which only moves up, and only when a 32-column chunk
+// exceeds it by more than 2^8; then the row sum, O (TMEM at tO, if `has_o`) and the P chunks already written
+// are rescaled.  With need_mask (warp-uniform) the row sees the tile's keys 0 .. last.  Warp-collective.
+__device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool has_o, bool need_mask, int last, float sl2,
+                                             float& m_run, float& l_run) {
+  const unsigned long long sl2x2 = f2_pack(sl2, sl2);
+  uint32_t r[32];
+  unsigned long long sum = f2_pack(0.f, 0.f);
+#pragma unroll 1
+  for (int c = 0; c < 4; ++c) {
+    tmem_ld32(tS + (uint32_t)c * 32u, r);
+    tmem_ld_wait();
+    if (need_mask) {
+      const int n = last - c * 32;   // the chunk's last visible key
+      const uint32_t seen = n < 0 ? 0u : (n >= 31 ? 0xFFFFFFFFu : (2u << n) - 1u);
+#pragma unroll
+      for (int e = 0; e < 32; ++e) r[e] = ((seen >> e) & 1u) ? r[e] : __float_as_uint(-INFINITY);
+    }
+    float a0 = -INFINITY, a1 = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 32; e += 4) {
+      a0 = fmax3(a0, __uint_as_float(r[e]), __uint_as_float(r[e + 1]));
+      a1 = fmax3(a1, __uint_as_float(r[e + 2]), __uint_as_float(r[e + 3]));
+    }
+    const float cm = fmaxf(a0, a1) * sl2;
+    const bool raise = cm > m_run + tc::kRescaleLog2;
+    if (__any_sync(0xffffffffu, raise)) {   // (a rescale's TMEM accesses are warp-collective)
+      float alpha = 1.f;
+      if (raise) {
+        alpha = m_run == -INFINITY ? 0.f : ptx_exp2(m_run - cm);
+        m_run = cm;
+      }
+      float s0, s1;
+      f2_unpack(sum, s0, s1);
+      sum = f2_pack(s0 * alpha, s1 * alpha);
+      l_run *= alpha;
+      tc::rescale_tmem(tO, tS, has_o ? 8 : 0, c, alpha);
+    }
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;   // -inf only while nothing is visible
+    const unsigned long long negm = f2_pack(-m_use, -m_use);
+    uint32_t pk[16];
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+      float x0, x1;
+      f2_unpack(f2_fma(f2_pack(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), sl2x2, negm), x0, x1);
+      const float p0 = ptx_exp2(x0), p1 = ptx_exp2(x1);
+      sum = f2_add(sum, f2_pack(p0, p1));
+      pk[e >> 1] = pack_bf16x2(p0, p1);
+    }
+    tmem_st16(tS + (uint32_t)c * 16u, pk);   // P chunk c: columns [16c, 16c+16) of S
+  }
+  float s0, s1;
+  f2_unpack(sum, s0, s1);
+  l_run += s0 + s1;
+  tmem_st_wait();
+  tc_fence_before();
+}
+
+__device__ __forceinline__ bool bf16_pair_finite(uint32_t w) {
+  return (w & 0x7F80u) != 0x7F80u && (w & 0x7F800000u) != 0x7F800000u;
+}
+
+template <bool kPaged>
+__global__ void __launch_bounds__(kThreads, 1)
+    prompt_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                     const __grid_constant__ CUtensorMap map_q, const PromptAttnParams p) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint32_t base = smem_u32(smem_raw);
+  const uint32_t pad = (1024u - (base & 1023u)) & 1023u;
+  uint8_t* smem = smem_raw + pad;
+  base += pad;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  auto bar = [&](int i) { return base + kOffBar + 8u * (uint32_t)i; };
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kOffAbort);
+  Seg* segs = reinterpret_cast<Seg*>(smem + kOffSeg);
+  const int used = p.tile_tokens * p.sub;   // rows of an M tile
+
+  // set-up that reads no global memory: it may overlap the stream's previous grid
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kBars; ++i) {
+      const int count = i >= kPFull && i < kPFull + 2 ? 4 : (i >= kSegEmpty && i < kSegEmpty + 2 ? 11 : 1);
+      mbar_init(bar(i), count);
+    }
+    *abort_flag = 0;
+    fence_mbar_init();
+    prefetch_tensormap(&map_k);
+    prefetch_tensormap(&map_v);
+    prefetch_tensormap(&map_q);
+  }
+  if (warp == 1) {
+    tmem_alloc(base + kOffTmemPtr, tc::kTmemCols);
+    tmem_relinquish();
+    tc_fence_before();
+  }
+  if (used < 128) {   // rows that no load writes: finite, so that they cost no rescaling
+    for (int i = threadIdx.x; i < 2 * 2 * (128 - used) * 8; i += kThreads) {
+      const int c = i & 7, r = (i >> 3) % (128 - used), h = (i >> 3) / (128 - used);
+      st_shared_v4(base + kOffQ + (uint32_t)h * kHalfBytes + (uint32_t)(used + r) * 128u + (uint32_t)c * 16u, 0, 0, 0, 0);
+    }
+    fence_proxy_async_smem();
+  }
+  grid_dependency_wait();   // every input and output belongs to the stream's previous work
+  __syncthreads();
+  tc_fence_after();
+  if (threadIdx.x == 0) grid_launch_dependents();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + kOffTmemPtr);
+
+  // The unit of a role's turn `it` (two slots), as long as there is one.
+  auto wait_seg = [&](int it) -> const volatile Seg* {
+    if (!mbar_wait_warp(bar(kSegFull + (it & 1)), (uint32_t)(it >> 1) & 1u, abort_flag, p.dev_status)) return nullptr;
+    const volatile Seg* s = segs + (it & 1);
+    return s->valid ? s : nullptr;
+  };
+  auto free_seg = [&](int it) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(kSegEmpty + (it & 1)));
+  };
+
+  if (warp == 1) {
+    // ================================================================ MMA issuer
+    const uint32_t dq = (uint32_t)smem_desc_sw128(base + kOffQ, 16, 1024), dk = (uint32_t)smem_desc_sw128(base + kOffK, 16, 1024),
+                   dv = (uint32_t)smem_desc_sw128(base + kOffV, kHalfBytes, 1024);
+    const uint32_t leader = lane == 0 ? 1u : 0u;
+    auto commit = [&](int b) {
+      if (leader) mma_commit(bar(b));
+    };
+    auto wait = [&](int b, int uses) { return mbar_wait_warp(bar(b), (uint32_t)uses & 1u, abort_flag, p.dev_status); };
+    bool ok = true;
+    int kc = 0, vc = 0, pc[2] = {0, 0}, qc[2] = {0, 0};   // tiles taken from the rings, P and Q taken
+    for (int it = 0; ok; ++it) {
+      const volatile Seg* sg = wait_seg(it);
+      if (sg == nullptr) break;
+      const int n0 = sg->n[0], n1 = sg->n[1], n = max(n0, n1);
+      free_seg(it);
+      auto tiles = [&](int t) { return t ? n1 : n0; };
+      auto issue_s = [&](int t, int j) {   // S_t of key tile j (K in its stage), Q_t free after the last
+        tc::issue_s(leader, tmem + (uint32_t)t * 128u, dq + (uint32_t)t * (kTileBytes >> 4),
+                    dk + (uint32_t)(kc % kStages) * (kTileBytes >> 4));
+        commit(kSFull + t);
+        if (j + 1 == tiles(t)) commit(kQEmpty + t);
+      };
+      if (!(ok = wait(kFullK + kc % kStages, kc / kStages))) break;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (tiles(t) > 0 && ok) {
+          if (!(ok = wait(kQFull + t, qc[t]))) break;
+          ++qc[t];
+          tc_fence_after();
+          issue_s(t, 0);
+        }
+      }
+      commit(kEmptyK + kc % kStages);
+      ++kc;
+      for (int j = 0; j < n && ok; ++j, ++vc) {
+        if (!(ok = wait(kFullV + vc % kStages, vc / kStages))) break;
+        const bool more = j + 1 < n;
+        if (more && !(ok = wait(kFullK + kc % kStages, kc / kStages))) break;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (j >= tiles(t)) continue;
+          if (!(ok = wait(kPFull + t, pc[t]))) break;
+          ++pc[t];
+          tc_fence_after();
+          tc::issue_pv(leader, tmem + (uint32_t)t * 128u, dv + (uint32_t)(vc % kStages) * (kTileBytes >> 4), j > 0);
+          if (t == 1 || j >= n1) commit(kEmptyV + vc % kStages);   // V of this stage is no longer read
+          if (j + 1 < tiles(t)) issue_s(t, j + 1); else commit(kOFull + t);
+        }
+        if (more) {
+          commit(kEmptyK + kc % kStages);
+          ++kc;
+        }
+      }
+    }
+    if (lane == 0 && *abort_flag) {
+      // error path: let the tensor core finish what was issued before TMEM is freed
+      mma_commit(bar(kDrain));
+      mbar_drain(bar(kDrain), 0, 100000000ull);
+    }
+  } else if (warp == 0) {
+    // ================================================================ TMA producer
+    bool ok = true;
+    int kc = 0, vc = 0, qc[2] = {0, 0}, loads[kStages] = {0, 0};
+    for (int it = 0; ok; ++it) {
+      const volatile Seg* sg = wait_seg(it);
+      if (sg == nullptr) break;
+      const int b = sg->b, kv = sg->kv, kt0 = sg->kt0, edge = sg->edge, head0 = sg->head0, row0 = sg->row0;
+      const int nq[2] = {sg->n[0], sg->n[1]}, n = max(nq[0], nq[1]), end = sg->ctx + sg->token0 + sg->tokens;
+      free_seg(it);
+      for (int j = 0; j < n && ok; ++j) {
+        if (lane == 0) {
+          const int t0 = (kt0 + j) * 128;
+          int page[kPaged ? 8 : 1];   // first rows of the tile's pages (before the cache for a bad one: TMA fills zeros)
+          int pages = 1;
+          if (kPaged) {
+            const int per = 128 / p.page_size, first = t0 / p.page_size;
+            pages = min(per, pages_for(end, p.page_size) - first);
+            const int* bt = p.block_table + (size_t)b * p.max_pages + first;
+#pragma unroll
+            for (int g = 0; g < (kPaged ? 8 : 1); ++g) {
+              page[g] = 0;
+              if (g < pages) {
+                const int x = bt[g];
+                const bool there = x >= 0 && x < p.num_pages;
+                if (!there) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
+                page[g] = there ? (p.layer * p.num_pages + x) * p.page_size : -128;
+              }
+            }
+          }
+          auto load = [&](uint32_t dst, const CUtensorMap* map, uint32_t full) {
+            if (!kPaged) {
+              const int row = (p.layer * p.batch + b) * p.seq_capacity + t0;
+              mbar_arrive_expect_tx(full, kTileBytes);
+              tma_load_3d(dst, map, full, 0, kv, row);
+              tma_load_3d(dst + kHalfBytes, map, full, 64, kv, row);
+            } else {
+              mbar_arrive_expect_tx(full, (uint32_t)(pages * 2 * p.page_size * 128));
+#pragma unroll
+              for (int g = 0; g < (kPaged ? 8 : 1); ++g) {
+                if (g < pages) {
+                  const uint32_t off = (uint32_t)(g * p.page_size * 128);
+                  tma_load_3d(dst + off, map, full, 0, kv, page[g]);
+                  tma_load_3d(dst + kHalfBytes + off, map, full, 64, kv, page[g]);
+                }
+              }
+            }
+          };
+          auto wait = [&](int bb, int uses) { return mbar_wait(bar(bb), ((uint32_t)uses & 1u) ^ 1u, abort_flag, p.dev_status); };
+          const int ks = kc % kStages, vs = vc % kStages;
+          ok = wait(kEmptyK + ks, kc / kStages);
+          if (ok) load(base + kOffK + (uint32_t)ks * kTileBytes, &map_k, bar(kFullK + ks));
+          if (j == 0) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              if (ok && nq[t] > 0 && (ok = wait(kQEmpty + t, qc[t]))) {
+                const uint32_t dst = base + kOffQ + (uint32_t)t * kTileBytes;
+                mbar_arrive_expect_tx(bar(kQFull + t), (uint32_t)used * 256u);
+                tma_load_3d(dst, &map_q, bar(kQFull + t), 0, head0, row0 + t * p.tile_tokens);
+                tma_load_3d(dst + kHalfBytes, &map_q, bar(kQFull + t), 64, head0, row0 + t * p.tile_tokens);
+              }
+            }
+          }
+          if (ok && (ok = wait(kEmptyV + vs, vc / kStages)))
+            load(base + kOffV + (uint32_t)vs * kTileBytes, &map_v, bar(kt0 + j >= edge ? kLoadV + vs : kFullV + vs));
+        }
+        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+        if (ok) {
+          if (kt0 + j >= edge) ++loads[vc % kStages];
+          ++kc, ++vc;
+          if (j == 0) qc[0] += nq[0] > 0, qc[1] += nq[1] > 0;
+        }
+      }
+    }
+    if (lane == 0 && *abort_flag) {
+      // drain the copies already issued (bounded) before the CTA can exit
+      for (int s = 0; s < kStages; ++s) {
+        if (kc > s) mbar_drain(bar(kFullK + s), (uint32_t)((kc - 1 - s) / kStages) & 1u, 100000000ull);
+        if (vc > s) mbar_drain(bar(kFullV + s), (uint32_t)((vc - 1 - s) / kStages) & 1u, 100000000ull);
+        if (loads[s] > 0) mbar_drain(bar(kLoadV + s), (uint32_t)(loads[s] - 1) & 1u, 100000000ull);
+        if (qc[s] > 0) mbar_drain(bar(kQFull + s), (uint32_t)(qc[s] - 1) & 1u, 100000000ull);
+      }
+    }
+  } else if (warp == 10) {
+    // ================================================================ scheduler
+    PromptBlocks* cached = reinterpret_cast<PromptBlocks*>(smem + kOffSeqs);
+    bool bad = false;
+    for (int b = lane; b < p.batch; b += 32) {
+      if (b < kMaxCached) cached[b] = pa::blocks_of(p, b);
+      bad = bad || !prompt_sequence_ok(p.bounds, p.token_offsets[b], p.token_offsets[b + 1], p.ctx_lens[b]);
+    }
+    if (bad) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
+    __syncwarp();
+    auto seq = [&](int b) { return b < kMaxCached ? cached[b] : pa::blocks_of(p, b); };
+    const int max_key = p.batch == 1 ? 0 : pa::max_block_key(seq, p.batch);
+    bool ok = true, pending = false;
+    int x = (int)blockIdx.x, claims = 0;
+    for (int it = 0; ok; ++it) {
+      if (!mbar_wait_warp(bar(kSegEmpty + (it & 1)), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, p.dev_status)) break;
+      Unit u;
+      bool found = false;
+      int piece = 0;
+      while (ok) {   // until a unit with keys, or the end of the grid
+        if (pending) {
+          ok = mbar_wait_warp(bar(kClaim), (uint32_t)(claims - 1) & 1u, abort_flag, p.dev_status);
+          if (!ok) break;
+          pending = false;
+          x = claimed_cta(base + kOffClaim);
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        if (x < 0) break;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(bar(kClaim), 16);
+          claim_cta(base + kOffClaim, bar(kClaim));
+        }
+        pending = true;
+        ++claims;
+        piece = x;
+        if (pa::find_unit(p, seq, max_key, x / p.splits, u)) {
+          pa::piece_range(u.tiles, x % p.splits, p.splits, u.tile0, u.tile1);
+          found = u.tile1 > u.tile0;
+        }
+        if (found) break;
+      }
+      if (!ok) break;
+      if (lane == 0) {
+        Seg s = {};
+        s.valid = found;
+        if (found) {
+          s.b = u.b;
+          s.row0 = u.row0;
+          s.ctx = u.ctx;
+          s.token0 = u.token0;
+          s.tokens = u.tokens;
+          s.head0 = u.head0;
+          s.kv = u.kv;
+          s.piece = piece;
+          s.kt0 = u.tile0;
+          s.edge = (u.ctx + u.token0 + 1) / 128;
+          // M tile 0's last token may see fewer tiles than the block's
+          const int first = (u.ctx + u.token0 + min(u.tokens, p.tile_tokens) + 127) / 128;
+          s.n[0] = max(0, min(first, u.tile1) - u.tile0);
+          s.n[1] = u.tokens > p.tile_tokens ? u.tile1 - u.tile0 : 0;
+        }
+        segs[it & 1] = s;
+        mbar_arrive(bar(kSegFull + (it & 1)));
+      }
+      __syncwarp();
+      if (!found) break;
+    }
+    if (pending && lane == 0) mbar_drain(bar(kClaim), (uint32_t)(claims - 1) & 1u, 100000000ull);
+  } else if (warp == 11) {
+    // ================================================================ V check
+    bool ok = true;
+    int vc = 0, loads[kStages] = {0, 0};
+    for (int it = 0; ok; ++it) {
+      const volatile Seg* sg = wait_seg(it);
+      if (sg == nullptr) break;
+      const int n = max(sg->n[0], sg->n[1]), kt0 = sg->kt0, edge = sg->edge, end = sg->ctx + sg->token0 + sg->tokens;
+      vc += max(0, min(n, edge - kt0));
+      for (int j = max(0, edge - kt0); j < n && ok; ++j, ++vc) {
+        const int vs = vc % kStages;
+        if (!(ok = mbar_wait_warp(bar(kLoadV + vs), (uint32_t)loads[vs] & 1u, abort_flag, p.dev_status))) break;
+        ++loads[vs];
+        uint8_t* tile = smem + kOffV + (size_t)vs * kTileBytes;
+        const int last = end - (kt0 + j) * 128;   // rows of the sequence in this tile
+        bool bad = false;
+#pragma unroll 4
+        for (int i = lane; i < 2048; i += 32) {   // 16-byte chunks: 128 rows x 8 of one half, then of the other
+          uint4* at = reinterpret_cast<uint4*>(tile) + i;
+          uint4 v = *at;
+          if (bf16_pair_finite(v.x) && bf16_pair_finite(v.y) && bf16_pair_finite(v.z) && bf16_pair_finite(v.w)) continue;
+          bad = bad || ((i >> 3) & 127) < last;
+          uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u;
+            if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0xFFFFu;
+          }
+          *at = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        fence_proxy_async_smem();
+        if (__any_sync(0xffffffffu, bad) && lane == 0) segs[it & 1].bad = 1;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kFullV + vs));
+      }
+      free_seg(it);
+    }
+  } else {
+    // ================================================================ softmax / epilogue
+    const int t = (warp - 2) >> 2;
+    const int row = (warp & 3) * 32 + lane;   // = TMEM lane this warp may access
+    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t tS = tmem + lane_base + (uint32_t)t * 128u, tO = tS + 256u;
+    const int my_token = t * p.tile_tokens + row / p.sub, my_head = row % p.sub;
+    const bool in_tile = row < used;
+    int tiles = 0, outs = 0;
+    for (int it = 0;; ++it) {
+      const volatile Seg* sg = wait_seg(it);
+      if (sg == nullptr) break;
+      const int n = sg->n[t], kt0 = sg->kt0, tokens = sg->tokens, q0 = sg->ctx + sg->token0;
+      const int pos = q0 + min(my_token, tokens - 1);   // the last key that this row sees
+      const bool row_valid = in_tile && my_token < tokens;
+      const int whole = (q0 + t * p.tile_tokens + 1) / 128;   // first key tile that some row sees in part
+      float m_run = -INFINITY, l_run = 0.f;
+      bool ok = true;
+      for (int j = 0; j < n; ++j, ++tiles) {
+        if (!(ok = mbar_wait_warp(bar(kSFull + t), (uint32_t)tiles & 1u, abort_flag, p.dev_status))) break;
+        tc_fence_after();
+        softmax_tile(tS, tO, j > 0, kt0 + j >= whole, pos - (kt0 + j) * 128, p.scale_log2, m_run, l_run);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kPFull + t));
+      }
+      if (!ok) break;
+      if (n > 0) {
+        if (!mbar_wait_warp(bar(kOFull + t), (uint32_t)outs & 1u, abort_flag, p.dev_status)) break;
+        ++outs;
+        tc_fence_after();
+      }
+      const size_t row0 = (size_t)sg->row0, head0 = (size_t)sg->head0, piece = (size_t)sg->piece;
+      const bool bad = sg->bad != 0;
+      // infinities and NaN of V that the check took out: added to the rows that see them
+      auto add_bad = [&](int c, float (&o)[32]) {
+        const int b = sg->b, end_key = min(pos, (kt0 + n) * 128 - 1);
+        for (int key = max(kt0, sg->edge) * 128; key <= end_key; ++key) {
+          size_t r;
+          if (kPaged) {
+            const int pg = p.block_table[(size_t)b * p.max_pages + key / p.page_size];
+            if (pg < 0 || pg >= p.num_pages) continue;
+            r = ((size_t)p.layer * p.num_pages + pg) * p.page_size + key % p.page_size;
+          } else {
+            r = ((size_t)p.layer * p.batch + b) * p.seq_capacity + key;
+          }
+          const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + (r * p.hkv + sg->kv) * 128 + c * 32;
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            const float x = __bfloat162float(v[e]);
+            if (!isfinite(x)) o[e] += x;
+          }
+        }
+      };
+      if (p.splits == 1) {
+        const float inv = 1.f / l_run;
+        uint4* dst = reinterpret_cast<uint4*>(p.out) + ((row0 + my_token) * p.hq + head0 + my_head) * 16;
+#pragma unroll 1
+        for (int c = 0; c < 4 && n > 0; ++c) {
+          uint32_t r[32];
+          tmem_ld32(tO + (uint32_t)c * 32u, r);
+          tmem_ld_wait();
+          if (row_valid) {
+            float o[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(r[e]) * inv;
+            if (bad) add_bad(c, o);
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+              dst[c * 4 + g] = make_uint4(pack_bf16x2(o[8 * g], o[8 * g + 1]), pack_bf16x2(o[8 * g + 2], o[8 * g + 3]),
+                                          pack_bf16x2(o[8 * g + 4], o[8 * g + 5]), pack_bf16x2(o[8 * g + 6], o[8 * g + 7]));
+          }
+          __syncwarp();
+        }
+      } else {
+        float4* po = reinterpret_cast<float4*>(p.part_o) + piece * 32 * 256 + t * 128 + row;
+        if (row_valid)
+          reinterpret_cast<float2*>(p.part_ml)[piece * 256 + t * 128 + row] =
+              n > 0 ? make_float2(m_run, l_run) : make_float2(-INFINITY, 0.f);
+#pragma unroll 1
+        for (int c = 0; c < 4 && n > 0; ++c) {
+          uint32_t r[32];
+          tmem_ld32(tO + (uint32_t)c * 32u, r);
+          tmem_ld_wait();
+          if (row_valid) {
+            float o[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(r[e]);
+            if (bad) add_bad(c, o);
+#pragma unroll
+            for (int g = 0; g < 8; ++g)
+              po[(size_t)(c * 8 + g) * 256] = make_float4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
+          }
+          __syncwarp();
+        }
+      }
+      tc_fence_before();
+      free_seg(it);
+    }
+  }
+
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, tc::kTmemCols);
+  }
+}
+
+}  // namespace pt
+
+cudaError_t launch_prompt_attn_tc(const CUtensorMap& map_k, const CUtensorMap& map_v, const CUtensorMap& map_q,
+                                  const PromptAttnParams& p, cudaStream_t stream) {
+  const auto kernel = p.page_size > 0 ? pt::prompt_tc_kernel<true> : pt::prompt_tc_kernel<false>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pt::kSmemBytes);
+  if (e != cudaSuccess) return e;
+  return launch_chained(kernel, dim3((unsigned)(p.blocks * p.tile_heads * p.splits)), dim3(pt::kThreads), pt::kSmemBytes,
+                        stream, 0, map_k, map_v, map_q, p);
+}
+
+}  // namespace ptd
