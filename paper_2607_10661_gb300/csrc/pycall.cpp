@@ -17,12 +17,14 @@
 namespace {
 
 PyObject *g_tensor, *g_i32, *g_f32, *g_bf16, *g_raw_stream, *g_get_device;
-PyObject *s_is_cuda, *s_is_contiguous, *s_dtype, *s_data_ptr, *s_nbytes, *s_shape, *s_stride, *s_c;
+PyObject *s_is_cuda, *s_is_contiguous, *s_dtype, *s_data_ptr, *s_nbytes, *s_shape, *s_stride, *s_c, *s_get_device, *s_k,
+    *s_block_table, *s_sizes;
 
 #define PTD_FUNCTIONS(X)                                                                                            \
   X(ptd_tree_attention) X(ptd_topk_draft) X(ptd_verify_greedy) X(ptd_kv_compact) X(ptd_verify_sampling)             \
   X(ptd_verify_and_compact) X(ptd_draft_tree_update) X(ptd_pool_merge) X(ptd_pool_retrieve) X(ptd_tree_rope_append) \
-  X(ptd_lm_head_topk) X(ptd_tree_verify_step) X(ptd_last_launch_count)
+  X(ptd_lm_head_topk) X(ptd_tree_verify_step) X(ptd_prompt_slots) X(ptd_prompt_rope_append) X(ptd_prompt_attention)   \
+  X(ptd_last_launch_count)
 #define PTD_DECLARE(f) decltype(&f) p_##f;
 PTD_FUNCTIONS(PTD_DECLARE)
 #undef PTD_DECLARE
@@ -131,6 +133,70 @@ struct Args {
     }
     Py_XDECREF(s);
     if (PyErr_Occurred() || unit != 1 || *stride < *cols) {
+      fail();
+      return nullptr;
+    }
+    return pointer(o);
+  }
+  // The device of the tensors seen by on(): the prompt calls run on it only where it is the current one.
+  int64_t device = -1;
+  void on(PyObject* o) {
+    if (!ok) return;
+    PyObject* r = (PyObject*)Py_TYPE(o) == g_tensor ? PyObject_CallMethodNoArgs(o, s_get_device) : nullptr;
+    const int64_t d = r != nullptr && PyLong_CheckExact(r) ? PyLong_AsLongLong(r) : -1;
+    Py_XDECREF(r);
+    if (PyErr_Occurred() || d < 0 || (device >= 0 && d != device)) fail();
+    device = d;
+  }
+  void on_attr(PyObject* o, PyObject* name) {
+    if (!ok) return;
+    PyObject* t = PyObject_GetAttr(o, name);
+    if (t == nullptr) fail(); else on(t);
+    Py_XDECREF(t);
+  }
+  void on_current() {
+    if (!ok) return;
+    PyObject* d = PyObject_CallNoArgs(g_get_device);
+    if (d == nullptr || !PyLong_CheckExact(d) || PyLong_AsLongLong(d) != device) fail();
+    Py_XDECREF(d);
+  }
+  // an int32 tensor of `count` elements
+  int32_t* i32_of(int64_t count) {
+    PyObject* o = next();
+    void* p = tensor_of(o, g_i32);
+    if (!ok) return nullptr;
+    on(o);
+    PyObject* r = ok ? PyObject_GetAttr(o, s_nbytes) : nullptr;
+    if (r == nullptr || !PyLong_CheckExact(r) || PyLong_AsLongLong(r) != 4 * count) fail();
+    Py_XDECREF(r);
+    return static_cast<int32_t*>(p);
+  }
+  // a [rows, heads, dim] tensor whose tokens may be apart, a token's heads back to back (*heads 0: any)
+  void* rows3(PyObject* dtype, int64_t rows, int64_t dim, int64_t* heads, int64_t* stride) {
+    PyObject* o = next();
+    if (!ok || (PyObject*)Py_TYPE(o) != g_tensor || !attr_true(o, s_is_cuda, false) || dtype_of(o) != dtype) {
+      fail();
+      return nullptr;
+    }
+    on(o);
+    PyObject* d = PyObject_GetAttr(o, s_shape);
+    PyObject* s = PyObject_CallMethodNoArgs(o, s_stride);
+    bool good = d != nullptr && s != nullptr && PyTuple_Check(d) && PyTuple_Check(s) && PyTuple_GET_SIZE(d) == 3 &&
+                PyTuple_GET_SIZE(s) == 3;
+    if (good) {
+      int64_t n[3], st[3];
+      for (int k = 0; k < 3; ++k) {
+        n[k] = PyLong_AsLongLong(PyTuple_GET_ITEM(d, k));
+        st[k] = PyLong_AsLongLong(PyTuple_GET_ITEM(s, k));
+      }
+      good = n[0] == rows && n[2] == dim && n[1] > 0 && (*heads == 0 || n[1] == *heads) && (dim == 1 || st[2] == 1) &&
+             (n[1] == 1 || st[1] == dim) && st[0] >= n[1] * dim;
+      *heads = n[1];
+      *stride = st[0];
+    }
+    Py_XDECREF(d);
+    Py_XDECREF(s);
+    if (PyErr_Occurred() || !good) {
       fail();
       return nullptr;
     }
@@ -452,6 +518,98 @@ PyObject* lm_head_topk(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                  val, ws, wsb, status, s));
 }
 
+// (prompt, cache, pages, slots, positions, dev_status, stream)
+PyObject* prompt_slots(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 7);
+  if (!g.ok) Py_RETURN_NONE;
+  const ptd_prompt* prompt = g.structure<ptd_prompt>();
+  const ptd_kv_cache* cache = g.structure<ptd_kv_cache>();
+  if (!g.ok) Py_RETURN_NONE;
+  const ptd_page_pool* held = a[2] == Py_None ? (g.next(), nullptr) : g.structure<ptd_page_pool>();
+  if (!g.ok) Py_RETURN_NONE;
+  ptd_page_pool pool = {};
+  if (held != nullptr) {   // sizes: (sequences, pages, device) of the pool's tensors
+    PyObject* sizes = PyObject_GetAttr(a[2], s_sizes);
+    PyObject* table = PyObject_GetAttr(a[1], s_block_table);
+    int64_t rows = 0, cols = 0;
+    if (sizes == nullptr || table == nullptr || table == Py_None || !PyTuple_CheckExact(sizes) || PyTuple_GET_SIZE(sizes) != 3 ||
+        PyLong_AsLongLong(PyTuple_GET_ITEM(sizes, 0)) != prompt->batch ||
+        PyLong_AsLongLong(PyTuple_GET_ITEM(sizes, 1)) != cache->num_pages) {
+      g.fail();
+    } else {
+      g.device = PyLong_AsLongLong(PyTuple_GET_ITEM(sizes, 2));
+      g.dims2(table, &rows, &cols);
+      if (rows != prompt->batch) g.ok = false;
+    }
+    Py_XDECREF(sizes);
+    Py_XDECREF(table);
+    pool = *held;
+    pool.block_table = const_cast<int32_t*>(cache->block_table);
+  }
+  int32_t* slots = g.i32_of(prompt->total_tokens);
+  int32_t* positions = g.i32_of(prompt->total_tokens);
+  g.on(a[5]);
+  int32_t* status = g.i32();
+  g.on_attr(a[1], s_k);
+  g.on_current();
+  void* s = g.stream();
+  if (!g.ok) Py_RETURN_NONE;
+  PTD_CALL(p_ptd_prompt_slots(prompt, cache, held != nullptr ? &pool : nullptr, slots, positions, status, s));
+}
+
+// (prompt, cache, layer, slots, positions, q, k, v, q_out, rope_base, dev_status, stream)
+PyObject* prompt_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 12);
+  if (!g.ok) Py_RETURN_NONE;
+  const ptd_prompt* prompt = g.structure<ptd_prompt>();
+  const ptd_kv_cache* cache = g.structure<ptd_kv_cache>();
+  if (!g.ok) Py_RETURN_NONE;
+  PyObject* dt = cache->dtype == PTD_BF16 ? g_bf16 : g_f32;
+  const int32_t layer = g.num();
+  const int32_t* slots = g.i32_of(prompt->total_tokens);
+  const int32_t* positions = g.i32_of(prompt->total_tokens);
+  int64_t hq = 0, hkv = cache->num_kv_heads, qs, ks, vs, os;
+  const void* q = g.rows3(dt, prompt->total_tokens, cache->head_dim, &hq, &qs);
+  const void* k = g.rows3(dt, prompt->total_tokens, cache->head_dim, &hkv, &ks);
+  const void* v = g.rows3(dt, prompt->total_tokens, cache->head_dim, &hkv, &vs);
+  void* out = g.rows3(dt, prompt->total_tokens, cache->head_dim, &hq, &os);
+  const float base = g.real();
+  g.on(a[10]);
+  int32_t* status = g.i32();
+  g.on_attr(a[1], s_k);
+  g.on_current();
+  void* s = g.stream();
+  if (!g.ok || hq != (int32_t)hq) Py_RETURN_NONE;
+  PTD_CALL(p_ptd_prompt_rope_append(prompt, cache, layer, slots, positions, q, qs, (int32_t)hq, k, ks, v, vs, base, out, os,
+                                    status, s));
+}
+
+// (prompt, cache, layer, q, out, dev_status, scale, workspace, stream)
+PyObject* prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 9);
+  if (!g.ok) Py_RETURN_NONE;
+  const ptd_prompt* prompt = g.structure<ptd_prompt>();
+  const ptd_kv_cache* cache = g.structure<ptd_kv_cache>();
+  if (!g.ok) Py_RETURN_NONE;
+  PyObject* dt = cache->dtype == PTD_BF16 ? g_bf16 : g_f32;
+  const int32_t layer = g.num();
+  int64_t hq = 0, qs, os = 0;
+  const void* q = g.rows3(dt, prompt->total_tokens, cache->head_dim, &hq, &qs);
+  void* out = g.rows3(dt, prompt->total_tokens, cache->head_dim, &hq, &os);
+  if (os != hq * cache->head_dim && prompt->total_tokens > 1) g.ok = false;   // out is contiguous
+  g.on(a[5]);
+  int32_t* status = g.i32();
+  const float scale = g.real();
+  size_t wsb;
+  if (a[7] != Py_None) g.on(a[7]);
+  void* ws = g.optional(&wsb);
+  g.on_attr(a[1], s_k);
+  g.on_current();
+  void* s = g.stream();
+  if (!g.ok || hq != (int32_t)hq) Py_RETURN_NONE;
+  PTD_CALL(p_ptd_prompt_attention(prompt, cache, layer, q, qs, (int32_t)hq, scale, out, ws, wsb, status, s));
+}
+
 // load(path of libptd.so, Tensor type, int32, float32, bfloat16, raw stream getter, device getter)
 PyObject* load(PyObject*, PyObject* args) {
   const char* path;
@@ -488,6 +646,9 @@ PyMethodDef methods[] = {PTD_METHOD(tree_attention),
                          PTD_METHOD(pool_retrieve),
                          PTD_METHOD(tree_rope_append),
                          PTD_METHOD(lm_head_topk),
+                         PTD_METHOD(prompt_slots),
+                         PTD_METHOD(prompt_rope_append),
+                         PTD_METHOD(prompt_attention),
                          {"load", load, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ptdcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -503,5 +664,9 @@ PyMODINIT_FUNC PyInit__ptdcall(void) {
   s_shape = PyUnicode_InternFromString("shape");
   s_stride = PyUnicode_InternFromString("stride");
   s_c = PyUnicode_InternFromString("c");
+  s_get_device = PyUnicode_InternFromString("get_device");
+  s_k = PyUnicode_InternFromString("k");
+  s_block_table = PyUnicode_InternFromString("block_table");
+  s_sizes = PyUnicode_InternFromString("sizes");
   return PyModule_Create(&module);
 }

@@ -618,9 +618,11 @@ class PagePool:
             raise ValueError("held and new_held need an entry per sequence")
         self.free_pages, self.free_count, self.held = free_pages, free_count, held
         self.new_held, self.new_free_count = new_held, new_free_count
-        self.ptrs = tuple(_dev(t, n, torch.int32) for t, n in (
+        self.c = _PagePool(*(_dev(t, n, torch.int32) for t, n in (
             (free_pages, "free_pages"), (free_count, "free_count"), (held, "held"), (new_held, "new_held"),
-            (new_free_count, "new_free_count")))
+            (new_free_count, "new_free_count"))), None)
+        with _one_device(free_pages, free_count, held, new_held, new_free_count):
+            self.sizes = (held.numel(), free_pages.numel(), held.get_device())
 
 
 def _one_device(*tensors):
@@ -650,6 +652,10 @@ def _rows3(t: torch.Tensor, name: str, dtype, rows: int, heads: Optional[int], d
 def prompt_slots(prompt: Prompt, cache: KVCache, slots: torch.Tensor, positions: torch.Tensor, dev_status: torch.Tensor,
                  pages: Optional[PagePool] = None, stream=None) -> int:
     """ptd_prompt_slots: slots, positions [total_tokens] int32; with `pages`, the block table's new entries too."""
+    r = (_calls or _native()).prompt_slots(prompt, cache, pages, slots, positions, dev_status,
+                                           stream if stream is None else _stream(stream))
+    if r is not None:
+        return _launched(r, "ptd_prompt_slots")
     n = prompt.total_tokens
     for t, nm in ((slots, "slots"), (positions, "positions")):
         if t.numel() != n:
@@ -658,11 +664,12 @@ def prompt_slots(prompt: Prompt, cache: KVCache, slots: torch.Tensor, positions:
     if pages is not None:
         if cache.block_table is None:
             raise ValueError("a page pool needs a paged cache")
-        if cache.block_table.shape[0] != prompt.batch or pages.held.numel() != prompt.batch:
+        if cache.block_table.shape[0] != prompt.batch or pages.sizes[0] != prompt.batch:
             raise ValueError("block_table and held need a row per sequence")
-        if pages.free_pages.numel() != cache.c.num_pages:
+        if pages.sizes[1] != cache.c.num_pages:
             raise ValueError("free_pages needs an entry per page of the cache")
-        pool = _PagePool(*pages.ptrs, cache.block_table.data_ptr())
+        c = pages.c
+        pool = _PagePool(c.free_pages, c.free_count, c.held, c.new_held, c.new_free_count, cache.block_table.data_ptr())
     with _one_device(slots, positions, dev_status, prompt.ctx_lens, cache.k, pages.held if pages is not None else None):
         st = lib().ptd_prompt_slots(ctypes.byref(prompt.c), ctypes.byref(cache.c), None if pool is None else ctypes.byref(pool),
                                     _dev(slots, "slots", torch.int32), _dev(positions, "positions", torch.int32),
@@ -676,6 +683,10 @@ def prompt_rope_append(prompt: Prompt, cache: KVCache, layer: int, slots: torch.
                        dev_status: torch.Tensor, stream=None) -> int:
     """ptd_prompt_rope_append: q, q_out [N, Hq, D], k, v [N, Hkv, D] (token strides are free: views of a fused
     product's rows); q_out may be q."""
+    r = (_calls or _native()).prompt_rope_append(prompt, cache, layer, slots, positions, q, k, v, q_out, rope_base, dev_status,
+                                                 stream if stream is None else _stream(stream))
+    if r is not None:
+        return _launched(r, "ptd_prompt_rope_append")
     n, d, dt = prompt.total_tokens, cache.head_dim, cache.k.dtype
     qp, qs, hq = _rows3(q, "q", dt, n, None, d)
     kp, ks, _ = _rows3(k, "k", dt, n, cache.num_kv_heads, d)
@@ -700,6 +711,10 @@ def prompt_attention(prompt: Prompt, cache: KVCache, layer: int, q: torch.Tensor
                      dev_status: torch.Tensor, scale: float = 0.0, workspace: Optional[torch.Tensor] = None,
                      stream=None) -> int:
     """ptd_prompt_attention: q [N, Hq, D] (its token stride is free), out [N, Hq, D] contiguous."""
+    r = (_calls or _native()).prompt_attention(prompt, cache, layer, q, out, dev_status, scale, workspace,
+                                               stream if stream is None else _stream(stream))
+    if r is not None:
+        return _launched(r, "ptd_prompt_attention")
     n, d, dt = prompt.total_tokens, cache.head_dim, cache.k.dtype
     qp, qs, hq = _rows3(q, "q", dt, n, None, d)
     if tuple(out.shape) != (n, hq, d):

@@ -630,3 +630,44 @@ def test_binding_refuses_wrong_tensors():
     with pytest.raises(ValueError):
         ptd.prompt_slots(x.prompt, x.cache, torch.zeros(3, **I32), torch.zeros(4, **I32), x.status)
     assert int(x.status) == 0 and (x.out == 7.0).all()
+
+
+def test_native_and_ctypes_paths_agree(monkeypatch):
+    """Each prompt call is taken natively (kernels launched, not None), and gives what the ctypes path gives."""
+    calls, taken = ptd._native(), {}
+
+    class Record:
+        def __getattr__(self, name):
+            def call(*a):
+                taken[name] = getattr(calls, name)(*a)
+                return taken[name]
+
+            return call
+
+    class Refuse:
+        def __getattr__(self, name):
+            return lambda *a: None
+
+    def run_all():
+        x = Batch([(30, 40), (0, 3), (700, 1)], 8, 2, page=16, seed=70, pad=2)
+        free = torch.arange(x.num_pages, **I32)
+        held = torch.tensor([2, 0, 44], **I32)
+        pool = ptd.PagePool(free, torch.tensor([3], **I32), held, torch.empty_like(held), torch.zeros(1, **I32))
+        slots, pos = torch.empty(x.N, **I32), torch.empty(x.N, **I32)
+        n = [ptd.prompt_slots(x.prompt, x.cache, slots, pos, x.status, pool), ptd.prompt_slots(x.prompt, x.cache, slots, pos, x.status)]
+        q, k, v = x.q, x.q[:, :2].contiguous(), x.q[:, 2:4].contiguous()
+        out = torch.zeros_like(q)
+        n.append(ptd.prompt_rope_append(x.prompt, x.cache, 0, slots, pos, q, k, v, out, 1e4, x.status))
+        x.q = out
+        n.append(x.attend())
+        assert int(x.status) == ptd.NO_PAGES   # three pages are too few: refused, then slots of the table as it is
+        return n, [slots, pos, pool.new_held, x.k.nan_to_num(), x.v.nan_to_num(), out, x.out.nan_to_num()]
+
+    monkeypatch.setattr(ptd, "_calls", Record())
+    native = run_all()
+    assert set(taken) == {"prompt_slots", "prompt_rope_append", "prompt_attention"} and all(r > 0 for r in taken.values())
+    monkeypatch.setattr(ptd, "_calls", Refuse())
+    plain = run_all()
+    assert native[0] == plain[0]
+    for i, (a, b) in enumerate(zip(native[1], plain[1])):
+        assert torch.equal(a, b), i

@@ -202,3 +202,72 @@ def test_oracle_causal_attention_is_a_chain_tree():
     assert np.abs(o - want).max() < 1e-14 and (size >= np.abs(o) - 1e-15).all()
     one, _ = oracle.causal_attention(q[:1], k, v, 0)
     assert np.array_equal(one[0], np.repeat(v[0], 2, axis=0))
+
+
+@pytest.mark.parametrize("name,count", [("prompt_slots", 7), ("prompt_rope_append", 12), ("prompt_attention", 9)])
+def test_native_prompt_calls_leave_other_arguments_alone(lib, name, count):
+    """Host tensors, plain objects and wrong counts are not taken (None: nothing was enqueued)."""
+    import torch
+
+    from paper_2607_10661_gb300 import ptd
+
+    f = getattr(ptd._native(), name)
+    host = torch.zeros((2, 4), dtype=torch.int32)
+    for filler in (host, None, 3, [1, 2], 0.5):
+        assert f(*([filler] * count)) is None
+    assert f() is None and f(*([host] * (count + 1))) is None
+
+
+def _native_with(ptd, monkeypatch, tensors_on, current):
+    """The native calls with a stand-in tensor type on device `tensors_on` while `current` is the current device."""
+    import torch
+
+    class Fake:
+        is_cuda, dtype, nbytes, shape = True, torch.int32, 40, (10, 2, 128)
+
+        def __init__(self, dtype=torch.int32, device=tensors_on):
+            self.dtype, self.device_ = dtype, device
+
+        def is_contiguous(self):
+            return True
+
+        def data_ptr(self):
+            return A
+
+        def stride(self):
+            return (256, 128, 1)
+
+        def get_device(self):
+            return self.device_
+
+    calls = ptd._native()
+    calls.load(ptd.LIB_PATH, Fake, torch.int32, torch.float32, torch.bfloat16, lambda d: 0, lambda: current)
+    return calls, Fake
+
+
+def test_native_prompt_calls_keep_to_the_current_device(lib, monkeypatch):
+    """Tensors of another device than the current one, or of several, are left to the path that changes the
+    device or raises (the calls that are taken here end at the library's own checks: no layer 9, no status)."""
+    import torch
+
+    from paper_2607_10661_gb300 import ptd
+
+    class Holder:
+        def __init__(self, c, k=None):
+            self.c, self.k, self.block_table = c, k, None
+
+    try:
+        for here, current, stray in ((0, 0, None), (1, 1, None), (1, 0, None), (0, 0, "k"), (0, 0, "q")):
+            calls, Fake = _native_with(ptd, monkeypatch, here, current)
+            prompt = Holder(_prompt(ptd))
+            cache = Holder(_cache(ptd, page=0, hkv=2), Fake(torch.bfloat16, 1 - here if stray == "k" else here))
+            q, x, i = Fake(torch.bfloat16, 1 - here if stray == "q" else here), Fake(torch.bfloat16), Fake()
+            taken = here == current and stray is None
+            want = -ptd.INVALID_ARG if taken else None
+            assert calls.prompt_attention(prompt, cache, 9, q, x, i, 0.0, None, 0) == want
+            assert calls.prompt_rope_append(prompt, cache, 9, i, i, q, x, x, x, 1e4, i, 0) == want
+            prompt.c.batch = 0   # refused by the library
+            assert calls.prompt_slots(prompt, cache, None, i, i, i, 0) == (want if stray != "q" else -ptd.INVALID_ARG)
+    finally:
+        ptd._calls = None
+        ptd._native()
