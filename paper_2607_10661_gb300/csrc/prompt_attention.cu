@@ -13,17 +13,19 @@ namespace ptd {
 namespace pa {
 
 constexpr int kMergeThreads = 256;
+constexpr int kMergeBatch = 4;   // pieces whose partials are in flight at a time
 
 // The rows of one split block, from its pieces: O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s, M the
-// maximum of the m_s (a row that saw no key of a piece has l_s = 0, and its O_s was not written).  One CTA a
-// block and head tile; a thread takes one row and four columns at a time, consecutive threads consecutive
-// rows, as the partials lie.  Bound by the latency of the chain unit, (m, l), partials.
+// maximum of the m_s (a row that saw no key of a piece has l_s = 0, and its O_s was not written).  Block x of the
+// grid is a (block, head tile), y a share of its rows and columns: a thread takes one row and four columns,
+// consecutive threads consecutive rows, as the partials lie.  Bound by the latency of the chain unit, (m, l),
+// partials; the unit is found while the attention still runs.
 template <typename T>
 __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const PromptAttnParams p) {
   __shared__ Unit unit_s;
   __shared__ int found_s;
   if (threadIdx.x == 0) grid_launch_dependents();
-  grid_dependency_wait();
+  // (the batch's arrays were complete before the attention let this grid be placed)
   if (threadIdx.x < 32) {
     auto seq = [&](int b) { return blocks_of(p, b); };
     const int max_key = p.batch == 1 ? 0 : max_block_key(seq, p.batch);
@@ -35,6 +37,7 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
     }
   }
   __syncthreads();
+  grid_dependency_wait();   // the partials belong to the attention
   if (!found_s) return;
   const Unit u = unit_s;
   const int rows = u.tokens * p.sub, groups = p.head_dim / 4, used = p.tile_tokens * p.sub;
@@ -45,29 +48,39 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
     piece_range(u.tiles, s, p.splits, k0, k1);
     return k0 == k1;
   };
-  for (int e = threadIdx.x; e < rows * groups; e += kMergeThreads) {
+  for (int e = blockIdx.y * kMergeThreads + threadIdx.x; e < rows * groups; e += gridDim.y * kMergeThreads) {
     const int c = e / rows, r = e - c * rows;
     const int at = r / used * p.tile_rows + r % used;
     const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + piece0 * block_rows + at;
     const float4* po = reinterpret_cast<const float4*>(p.part_o) + (piece0 * groups + c) * block_rows + at;
     float M = -INFINITY, L = 0.f;
-    for (int s = 0; s < p.splits; ++s) {
-      if (empty(s)) continue;
-      const float2 x = __ldcg(ml + (size_t)s * block_rows);
-      if (!(x.y == 0.f)) M = fmaxf(M, x.x);
-    }
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < p.splits; ++s) {
-      if (empty(s)) continue;
-      const float2 x = __ldcg(ml + (size_t)s * block_rows);
-      if (x.y == 0.f) continue;   // (not l > 0: a NaN among the scores has to reach the output)
-      const float w = exp2f(x.x - M);
-      const float4 o = __ldcg(po + (size_t)s * groups * block_rows);
-      L += w * x.y;
-      acc.x += w * o.x;
-      acc.y += w * o.y;
-      acc.z += w * o.z;
-      acc.w += w * o.w;
+    for (int s0 = 0; s0 < p.splits; s0 += kMergeBatch) {   // the loads of a batch are in flight together
+      float2 x[kMergeBatch];
+      float4 o[kMergeBatch];
+#pragma unroll
+      for (int i = 0; i < kMergeBatch; ++i) {
+        const bool there = s0 + i < p.splits && !empty(s0 + i);
+        x[i] = there ? __ldcg(ml + (size_t)(s0 + i) * block_rows) : make_float2(-INFINITY, 0.f);
+        if (there) o[i] = __ldcg(po + (size_t)(s0 + i) * groups * block_rows);
+      }
+      float m = M;
+#pragma unroll
+      for (int i = 0; i < kMergeBatch; ++i)
+        if (!(x[i].y == 0.f)) m = fmaxf(m, x[i].x);   // (not l > 0: a NaN among the scores has to reach the output)
+      const float old = M == -INFINITY ? 0.f : exp2f(M - m);
+      M = m;
+      L *= old, acc.x *= old, acc.y *= old, acc.z *= old, acc.w *= old;
+#pragma unroll
+      for (int i = 0; i < kMergeBatch; ++i) {
+        if (x[i].y == 0.f) continue;
+        const float w = exp2f(x[i].x - M);
+        L += w * x[i].y;
+        acc.x += w * o[i].x;
+        acc.y += w * o[i].y;
+        acc.z += w * o[i].z;
+        acc.w += w * o[i].w;
+      }
     }
     const float inv = 1.f / L;
     T* dst = static_cast<T*>(p.out) + ((size_t)(u.row0 + r / p.sub) * p.hq + u.head0 + r % p.sub) * p.head_dim + c * 4;
@@ -117,7 +130,9 @@ size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int
 
 cudaError_t launch_prompt_attn_merge(const PromptAttnParams& p, bool bf16, cudaStream_t stream) {
   const auto kernel = bf16 ? pa::prompt_merge_kernel<__nv_bfloat16> : pa::prompt_merge_kernel<float>;
-  return launch_chained(kernel, dim3((unsigned)(p.blocks * p.tile_heads)), dim3(pa::kMergeThreads), 0, stream, 0, p);
+  int64_t rows = (int64_t)(p.bounds.max_tokens < p.block_tokens ? p.bounds.max_tokens : p.block_tokens) * p.sub;
+  const unsigned shares = (unsigned)((rows * (p.head_dim / 4) + pa::kMergeThreads - 1) / pa::kMergeThreads);
+  return launch_chained(kernel, dim3((unsigned)(p.blocks * p.tile_heads), shares), dim3(pa::kMergeThreads), 0, stream, 0, p);
 }
 
 }  // namespace ptd

@@ -9,16 +9,16 @@
 // takes the numbers of CTAs that have not started yet (cluster launch control), so that the SMs' shares
 // even out whatever the lengths, and a unit's first loads and its set-up run beside the unit before it.
 //
-// Warps (384 threads):
+// Warps (384 threads; the first four give registers to the others):
 //   0       TMA producer: K, V (a ring of two stages each), Q of the next unit.
 //   1       TMEM allocator and MMA issuer: S_t = Q_t K^T, O_t += P_t V, in the order
 //             S_0, S_1 | PV_0, S_0', PV_1, S_1' | ...
 //           so that one M tile's softmax runs beside the other's products.
-//   2 - 9   softmax of M tile 0 (2 - 5) and 1 (6 - 9), a thread a row: running maximum, moved only when
-//           exceeded by 2^8, exp2, bf16 weights over S in TMEM, fp32 row sum; O / l at the end.
-//   10      scheduler: the next unit.
-//   11      V check: of key tiles that some row sees in part, infinities and NaN of V are set to 0 (a
+//   2       scheduler: the next unit, claimed when the producer has asked for the last tile of this one.
+//   3       V check: of key tiles that some row sees in part, infinities and NaN of V are set to 0 (a
 //           weight of 0 must not meet them) and noted; the rows that see such a key add it at the end.
+//   4 - 11  softmax of M tile 0 (4 - 7) and 1 (8 - 11), a thread a row: running maximum, moved only when
+//           exceeded by 2^8, exp2, bf16 weights over S in TMEM, fp32 row sum; O / l at the end.
 // TMEM: S_0 | S_1 | O_0 | O_1, 128 fp32 columns each; P_t lies over the first 64 columns of S_t.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -40,6 +40,10 @@ using tc::kTileBytes;
 
 constexpr int kThreads = 384;
 constexpr int kStages = 2;   // K tiles, and V tiles
+// Registers a thread: 168 at launch (384 threads), then 88 for warps 0 - 3 and 208 for the softmax warps,
+// which hold a row's 128 scores: 128 * 88 + 256 * 208 = 384 * 168.
+constexpr int kRegsLaunch = 168, kRegsFew = 88, kRegsMany = 208;
+static_assert(128 * kRegsFew + 256 * kRegsMany <= kThreads * kRegsLaunch, "register split");
 constexpr uint32_t kOffQ = 0;
 constexpr uint32_t kOffK = 2 * kTileBytes;
 constexpr uint32_t kOffV = kOffK + kStages * kTileBytes;
@@ -58,6 +62,7 @@ enum Bar {
   kSegFull = kQEmpty + 2,
   kSegEmpty = kSegFull + 2,
   kClaim = kSegEmpty + 2,
+  kLoaded,              // the producer has asked for all tiles of a unit
   kDrain,
   kBars
 };
@@ -101,60 +106,76 @@ __device__ __forceinline__ int claimed_cta(uint32_t src) {
   return x;
 }
 
+// O (TMEM at tO) times alpha, kept out of the hot loop.  Warp-collective.
+static __device__ __noinline__ void rescale_o(uint32_t tO, float alpha) {
+#pragma unroll 1
+  for (int q = 0; q < 8; ++q) {
+    uint32_t o[16];
+    tmem_ld16(tO + (uint32_t)q * 16u, o);
+    tmem_ld_wait();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+    tmem_st16(tO + (uint32_t)q * 16u, o);
+  }
+  tmem_st_wait();
+}
+
 // Softmax of one key tile of this thread's row: S (TMEM at tS) becomes the bf16 P over its first 64 columns,
-// against the reference maximum m_run (log2 units), which only moves up, and only when a 32-column chunk
-// exceeds it by more than 2^8; then the row sum, O (TMEM at tO, if `has_o`) and the P chunks already written
-// are rescaled.  With need_mask (warp-uniform) the row sees the tile's keys 0 .. last.  Warp-collective.
+// against the reference maximum m_run (log2 units), which only moves up, and only when exceeded by more than
+// 2^8; then the row sum and O (TMEM at tO, if `has_o`) are rescaled.  With need_mask (warp-uniform) the row sees
+// the tile's keys 0 .. last.  The whole row is in registers: one maximum and one vote a tile, and then exponentials
+// and packing without a dependence between chunks.  Warp-collective.
 __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool has_o, bool need_mask, int last, float sl2,
                                              float& m_run, float& l_run) {
-  const unsigned long long sl2x2 = f2_pack(sl2, sl2);
-  uint32_t r[32];
-  unsigned long long sum = f2_pack(0.f, 0.f);
-#pragma unroll 1
-  for (int c = 0; c < 4; ++c) {
-    tmem_ld32(tS + (uint32_t)c * 32u, r);
-    tmem_ld_wait();
-    if (need_mask) {
+  uint32_t r[4][32];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) tmem_ld32(tS + (uint32_t)c * 32u, r[c]);
+  tmem_ld_wait();
+  if (need_mask) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
       const int n = last - c * 32;   // the chunk's last visible key
       const uint32_t seen = n < 0 ? 0u : (n >= 31 ? 0xFFFFFFFFu : (2u << n) - 1u);
 #pragma unroll
-      for (int e = 0; e < 32; ++e) r[e] = ((seen >> e) & 1u) ? r[e] : __float_as_uint(-INFINITY);
+      for (int e = 0; e < 32; ++e) r[c][e] = ((seen >> e) & 1u) ? r[c][e] : __float_as_uint(-INFINITY);
     }
-    float a0 = -INFINITY, a1 = -INFINITY;
+  }
+  float a[4];
 #pragma unroll
-    for (int e = 0; e < 32; e += 4) {
-      a0 = fmax3(a0, __uint_as_float(r[e]), __uint_as_float(r[e + 1]));
-      a1 = fmax3(a1, __uint_as_float(r[e + 2]), __uint_as_float(r[e + 3]));
+  for (int c = 0; c < 4; ++c) {
+    a[c] = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) a[c] = fmax3(a[c], __uint_as_float(r[c][e]), __uint_as_float(r[c][e + 1]));
+  }
+  const float cm = fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])) * sl2;
+  const bool raise = cm > m_run + tc::kRescaleLog2;
+  if (__any_sync(0xffffffffu, raise)) {   // (a rescale's TMEM accesses are warp-collective)
+    float alpha = 1.f;
+    if (raise) {
+      alpha = m_run == -INFINITY ? 0.f : ptx_exp2(m_run - cm);
+      m_run = cm;
     }
-    const float cm = fmaxf(a0, a1) * sl2;
-    const bool raise = cm > m_run + tc::kRescaleLog2;
-    if (__any_sync(0xffffffffu, raise)) {   // (a rescale's TMEM accesses are warp-collective)
-      float alpha = 1.f;
-      if (raise) {
-        alpha = m_run == -INFINITY ? 0.f : ptx_exp2(m_run - cm);
-        m_run = cm;
-      }
-      float s0, s1;
-      f2_unpack(sum, s0, s1);
-      sum = f2_pack(s0 * alpha, s1 * alpha);
-      l_run *= alpha;
-      tc::rescale_tmem(tO, tS, has_o ? 8 : 0, c, alpha);
-    }
-    const float m_use = m_run == -INFINITY ? 0.f : m_run;   // -inf only while nothing is visible
-    const unsigned long long negm = f2_pack(-m_use, -m_use);
+    l_run *= alpha;
+    if (has_o) rescale_o(tO, alpha);
+  }
+  const float m_use = m_run == -INFINITY ? 0.f : m_run;   // -inf only while nothing is visible
+  const unsigned long long negm = f2_pack(-m_use, -m_use), sl2x2 = f2_pack(sl2, sl2);
+  unsigned long long sum[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
     uint32_t pk[16];
 #pragma unroll
     for (int e = 0; e < 32; e += 2) {
       float x0, x1;
-      f2_unpack(f2_fma(f2_pack(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), sl2x2, negm), x0, x1);
+      f2_unpack(f2_fma(f2_pack(__uint_as_float(r[c][e]), __uint_as_float(r[c][e + 1])), sl2x2, negm), x0, x1);
       const float p0 = ptx_exp2(x0), p1 = ptx_exp2(x1);
-      sum = f2_add(sum, f2_pack(p0, p1));
+      sum[(e >> 1) & 1] = f2_add(sum[(e >> 1) & 1], f2_pack(p0, p1));
       pk[e >> 1] = pack_bf16x2(p0, p1);
     }
     tmem_st16(tS + (uint32_t)c * 16u, pk);   // P chunk c: columns [16c, 16c+16) of S
   }
   float s0, s1;
-  f2_unpack(sum, s0, s1);
+  f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
   l_run += s0 + s1;
   tmem_st_wait();
   tc_fence_before();
@@ -220,258 +241,255 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) mbar_arrive(bar(kSegEmpty + (it & 1)));
   };
 
-  if (warp == 1) {
-    // ================================================================ MMA issuer
-    const uint32_t dq = (uint32_t)smem_desc_sw128(base + kOffQ, 16, 1024), dk = (uint32_t)smem_desc_sw128(base + kOffK, 16, 1024),
-                   dv = (uint32_t)smem_desc_sw128(base + kOffV, kHalfBytes, 1024);
-    const uint32_t leader = lane == 0 ? 1u : 0u;
-    auto commit = [&](int b) {
-      if (leader) mma_commit(bar(b));
-    };
-    auto wait = [&](int b, int uses) { return mbar_wait_warp(bar(b), (uint32_t)uses & 1u, abort_flag, p.dev_status); };
-    bool ok = true;
-    int kc = 0, vc = 0, pc[2] = {0, 0}, qc[2] = {0, 0};   // tiles taken from the rings, P and Q taken
-    for (int it = 0; ok; ++it) {
-      const volatile Seg* sg = wait_seg(it);
-      if (sg == nullptr) break;
-      const int n0 = sg->n[0], n1 = sg->n[1], n = max(n0, n1);
-      free_seg(it);
-      auto tiles = [&](int t) { return t ? n1 : n0; };
-      auto issue_s = [&](int t, int j) {   // S_t of key tile j (K in its stage), Q_t free after the last
-        tc::issue_s(leader, tmem + (uint32_t)t * 128u, dq + (uint32_t)t * (kTileBytes >> 4),
-                    dk + (uint32_t)(kc % kStages) * (kTileBytes >> 4));
-        commit(kSFull + t);
-        if (j + 1 == tiles(t)) commit(kQEmpty + t);
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
+    if (warp == 1) {
+      // ================================================================ MMA issuer
+      const uint32_t dq = (uint32_t)smem_desc_sw128(base + kOffQ, 16, 1024), dk = (uint32_t)smem_desc_sw128(base + kOffK, 16, 1024),
+                     dv = (uint32_t)smem_desc_sw128(base + kOffV, kHalfBytes, 1024);
+      const uint32_t leader = lane == 0 ? 1u : 0u;
+      auto commit = [&](int b) {
+        if (leader) mma_commit(bar(b));
       };
-      if (!(ok = wait(kFullK + kc % kStages, kc / kStages))) break;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (tiles(t) > 0 && ok) {
-          if (!(ok = wait(kQFull + t, qc[t]))) break;
-          ++qc[t];
-          tc_fence_after();
-          issue_s(t, 0);
-        }
-      }
-      commit(kEmptyK + kc % kStages);
-      ++kc;
-      for (int j = 0; j < n && ok; ++j, ++vc) {
-        if (!(ok = wait(kFullV + vc % kStages, vc / kStages))) break;
-        const bool more = j + 1 < n;
-        if (more && !(ok = wait(kFullK + kc % kStages, kc / kStages))) break;
-#pragma unroll
+      auto wait = [&](int b, int uses) { return mbar_wait_warp(bar(b), (uint32_t)uses & 1u, abort_flag, p.dev_status); };
+      bool ok = true;
+      int kc = 0, vc = 0, pc[2] = {0, 0}, qc[2] = {0, 0};   // tiles taken from the rings, P and Q taken
+      for (int it = 0; ok; ++it) {
+        const volatile Seg* sg = wait_seg(it);
+        if (sg == nullptr) break;
+        const int n0 = sg->n[0], n1 = sg->n[1], n = max(n0, n1);
+        free_seg(it);
+        auto tiles = [&](int t) { return t ? n1 : n0; };
+        auto issue_s = [&](int t, int j) {   // S_t of key tile j (K in its stage), Q_t free after the last
+          tc::issue_s(leader, tmem + (uint32_t)t * 128u, dq + (uint32_t)t * (kTileBytes >> 4),
+                      dk + (uint32_t)(kc % kStages) * (kTileBytes >> 4));
+          commit(kSFull + t);
+          if (j + 1 == tiles(t)) commit(kQEmpty + t);
+        };
+        if (!(ok = wait(kFullK + kc % kStages, kc / kStages))) break;
+  #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          if (j >= tiles(t)) continue;
-          if (!(ok = wait(kPFull + t, pc[t]))) break;
-          ++pc[t];
-          tc_fence_after();
-          tc::issue_pv(leader, tmem + (uint32_t)t * 128u, dv + (uint32_t)(vc % kStages) * (kTileBytes >> 4), j > 0);
-          if (t == 1 || j >= n1) commit(kEmptyV + vc % kStages);   // V of this stage is no longer read
-          if (j + 1 < tiles(t)) issue_s(t, j + 1); else commit(kOFull + t);
+          if (tiles(t) > 0 && ok) {
+            if (!(ok = wait(kQFull + t, qc[t]))) break;
+            ++qc[t];
+            tc_fence_after();
+            issue_s(t, 0);
+          }
         }
-        if (more) {
-          commit(kEmptyK + kc % kStages);
-          ++kc;
+        commit(kEmptyK + kc % kStages);
+        ++kc;
+        for (int j = 0; j < n && ok; ++j, ++vc) {
+          if (!(ok = wait(kFullV + vc % kStages, vc / kStages))) break;
+          const bool more = j + 1 < n;
+          if (more && !(ok = wait(kFullK + kc % kStages, kc / kStages))) break;
+  #pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (j >= tiles(t)) continue;
+            if (!(ok = wait(kPFull + t, pc[t]))) break;
+            ++pc[t];
+            tc_fence_after();
+            tc::issue_pv(leader, tmem + (uint32_t)t * 128u, dv + (uint32_t)(vc % kStages) * (kTileBytes >> 4), j > 0);
+            if (t == 1 || j >= n1) commit(kEmptyV + vc % kStages);   // V of this stage is no longer read
+            if (j + 1 < tiles(t)) issue_s(t, j + 1); else commit(kOFull + t);
+          }
+          if (more) {
+            commit(kEmptyK + kc % kStages);
+            ++kc;
+          }
         }
       }
-    }
-    if (lane == 0 && *abort_flag) {
-      // error path: let the tensor core finish what was issued before TMEM is freed
-      mma_commit(bar(kDrain));
-      mbar_drain(bar(kDrain), 0, 100000000ull);
-    }
-  } else if (warp == 0) {
-    // ================================================================ TMA producer
-    bool ok = true;
-    int kc = 0, vc = 0, qc[2] = {0, 0}, loads[kStages] = {0, 0};
-    for (int it = 0; ok; ++it) {
-      const volatile Seg* sg = wait_seg(it);
-      if (sg == nullptr) break;
-      const int b = sg->b, kv = sg->kv, kt0 = sg->kt0, edge = sg->edge, head0 = sg->head0, row0 = sg->row0;
-      const int nq[2] = {sg->n[0], sg->n[1]}, n = max(nq[0], nq[1]), end = sg->ctx + sg->token0 + sg->tokens;
-      free_seg(it);
-      for (int j = 0; j < n && ok; ++j) {
-        if (lane == 0) {
-          const int t0 = (kt0 + j) * 128;
-          int page[kPaged ? 8 : 1];   // first rows of the tile's pages (before the cache for a bad one: TMA fills zeros)
-          int pages = 1;
+      if (lane == 0 && *abort_flag) {
+        // error path: let the tensor core finish what was issued before TMEM is freed
+        mma_commit(bar(kDrain));
+        mbar_drain(bar(kDrain), 0, 100000000ull);
+      }
+    } else if (warp == 0) {
+      // ================================================================ TMA producer
+      // A lane copies one half (64 columns) of one page's rows, or of the tile's 128 rows.
+      bool ok = true;
+      int kc = 0, vc = 0, qc[2] = {0, 0}, loads[kStages] = {0, 0};
+      const int half = lane & 1, page_at = lane >> 1, per_tile = kPaged ? 128 / p.page_size : 1;
+      const uint32_t copy_at = (uint32_t)half * kHalfBytes + (kPaged ? (uint32_t)(page_at * p.page_size) * 128u : 0u);
+      auto wait = [&](int b, int uses) { return mbar_wait_warp(bar(b), ((uint32_t)uses & 1u) ^ 1u, abort_flag, p.dev_status); };
+      for (int it = 0; ok; ++it) {
+        const volatile Seg* sg = wait_seg(it);
+        if (sg == nullptr) break;
+        const int b = sg->b, kv = sg->kv, kt0 = sg->kt0, edge = sg->edge, head0 = sg->head0, row0 = sg->row0;
+        const int nq[2] = {sg->n[0], sg->n[1]}, n = max(nq[0], nq[1]);
+        const int end_page = kPaged ? pages_for(sg->ctx + sg->token0 + sg->tokens, p.page_size) : 0;
+        free_seg(it);
+        const int* bt = kPaged ? p.block_table + (size_t)b * p.max_pages : nullptr;
+        // this lane's page in key tile j (read one tile ahead, so that no copy waits for it)
+        auto page_of = [&](int j) {
+          const int g = (kt0 + j) * per_tile + page_at;
+          return kPaged && j < n && page_at < per_tile && g < end_page ? bt[g] : -1;
+        };
+        int next_page = page_of(0);
+        for (int j = 0; j < n && ok; ++j, ++kc, ++vc) {
+          const int ks = kc % kStages, vs = vc % kStages, t0 = (kt0 + j) * 128;
+          int row = 0, copies = 1;   // first row of this lane's copy; pages of the tile
+          bool mine = lane < 2;
           if (kPaged) {
-            const int per = 128 / p.page_size, first = t0 / p.page_size;
-            pages = min(per, pages_for(end, p.page_size) - first);
-            const int* bt = p.block_table + (size_t)b * p.max_pages + first;
-#pragma unroll
-            for (int g = 0; g < (kPaged ? 8 : 1); ++g) {
-              page[g] = 0;
-              if (g < pages) {
-                const int x = bt[g];
-                const bool there = x >= 0 && x < p.num_pages;
-                if (!there) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
-                page[g] = there ? (p.layer * p.num_pages + x) * p.page_size : -128;
-              }
-            }
+            copies = min(per_tile, end_page - (kt0 + j) * per_tile);
+            mine = page_at < copies;
+            const bool there = next_page >= 0 && next_page < p.num_pages;
+            if (mine && !there) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
+            row = there ? (p.layer * p.num_pages + next_page) * p.page_size : -128;   // (-128: TMA fills zeros)
+            next_page = page_of(j + 1);
+          } else {
+            row = (p.layer * p.batch + b) * p.seq_capacity + t0;
           }
           auto load = [&](uint32_t dst, const CUtensorMap* map, uint32_t full) {
-            if (!kPaged) {
-              const int row = (p.layer * p.batch + b) * p.seq_capacity + t0;
-              mbar_arrive_expect_tx(full, kTileBytes);
-              tma_load_3d(dst, map, full, 0, kv, row);
-              tma_load_3d(dst + kHalfBytes, map, full, 64, kv, row);
-            } else {
-              mbar_arrive_expect_tx(full, (uint32_t)(pages * 2 * p.page_size * 128));
-#pragma unroll
-              for (int g = 0; g < (kPaged ? 8 : 1); ++g) {
-                if (g < pages) {
-                  const uint32_t off = (uint32_t)(g * p.page_size * 128);
-                  tma_load_3d(dst + off, map, full, 0, kv, page[g]);
-                  tma_load_3d(dst + kHalfBytes + off, map, full, 64, kv, page[g]);
-                }
-              }
-            }
+            if (lane == 0) mbar_arrive_expect_tx(full, kPaged ? (uint32_t)(copies * p.page_size) * 256u : kTileBytes);
+            __syncwarp();
+            if (mine) tma_load_3d(dst + copy_at, map, full, half * 64, kv, row);
           };
-          auto wait = [&](int bb, int uses) { return mbar_wait(bar(bb), ((uint32_t)uses & 1u) ^ 1u, abort_flag, p.dev_status); };
-          const int ks = kc % kStages, vs = vc % kStages;
-          ok = wait(kEmptyK + ks, kc / kStages);
-          if (ok) load(base + kOffK + (uint32_t)ks * kTileBytes, &map_k, bar(kFullK + ks));
+          if (!(ok = wait(kEmptyK + ks, kc / kStages))) break;
+          load(base + kOffK + (uint32_t)ks * kTileBytes, &map_k, bar(kFullK + ks));
           if (j == 0) {
-#pragma unroll
+  #pragma unroll
             for (int t = 0; t < 2; ++t) {
-              if (ok && nq[t] > 0 && (ok = wait(kQEmpty + t, qc[t]))) {
-                const uint32_t dst = base + kOffQ + (uint32_t)t * kTileBytes;
-                mbar_arrive_expect_tx(bar(kQFull + t), (uint32_t)used * 256u);
-                tma_load_3d(dst, &map_q, bar(kQFull + t), 0, head0, row0 + t * p.tile_tokens);
-                tma_load_3d(dst + kHalfBytes, &map_q, bar(kQFull + t), 64, head0, row0 + t * p.tile_tokens);
-              }
+              if (!ok || nq[t] == 0 || !(ok = wait(kQEmpty + t, qc[t]))) continue;
+              ++qc[t];
+              if (lane == 0) mbar_arrive_expect_tx(bar(kQFull + t), (uint32_t)used * 256u);
+              __syncwarp();
+              if (lane < 2)
+                tma_load_3d(base + kOffQ + (uint32_t)t * kTileBytes + (uint32_t)half * kHalfBytes, &map_q, bar(kQFull + t),
+                            half * 64, head0, row0 + t * p.tile_tokens);
+            }
+            if (!ok) {
+              ++kc;
+              break;
             }
           }
-          if (ok && (ok = wait(kEmptyV + vs, vc / kStages)))
-            load(base + kOffV + (uint32_t)vs * kTileBytes, &map_v, bar(kt0 + j >= edge ? kLoadV + vs : kFullV + vs));
-        }
-        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-        if (ok) {
-          if (kt0 + j >= edge) ++loads[vc % kStages];
-          ++kc, ++vc;
-          if (j == 0) qc[0] += nq[0] > 0, qc[1] += nq[1] > 0;
-        }
-      }
-    }
-    if (lane == 0 && *abort_flag) {
-      // drain the copies already issued (bounded) before the CTA can exit
-      for (int s = 0; s < kStages; ++s) {
-        if (kc > s) mbar_drain(bar(kFullK + s), (uint32_t)((kc - 1 - s) / kStages) & 1u, 100000000ull);
-        if (vc > s) mbar_drain(bar(kFullV + s), (uint32_t)((vc - 1 - s) / kStages) & 1u, 100000000ull);
-        if (loads[s] > 0) mbar_drain(bar(kLoadV + s), (uint32_t)(loads[s] - 1) & 1u, 100000000ull);
-        if (qc[s] > 0) mbar_drain(bar(kQFull + s), (uint32_t)(qc[s] - 1) & 1u, 100000000ull);
-      }
-    }
-  } else if (warp == 10) {
-    // ================================================================ scheduler
-    PromptBlocks* cached = reinterpret_cast<PromptBlocks*>(smem + kOffSeqs);
-    bool bad = false;
-    for (int b = lane; b < p.batch; b += 32) {
-      if (b < kMaxCached) cached[b] = pa::blocks_of(p, b);
-      bad = bad || !prompt_sequence_ok(p.bounds, p.token_offsets[b], p.token_offsets[b + 1], p.ctx_lens[b]);
-    }
-    if (bad) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
-    __syncwarp();
-    auto seq = [&](int b) { return b < kMaxCached ? cached[b] : pa::blocks_of(p, b); };
-    const int max_key = p.batch == 1 ? 0 : pa::max_block_key(seq, p.batch);
-    bool ok = true, pending = false;
-    int x = (int)blockIdx.x, claims = 0;
-    for (int it = 0; ok; ++it) {
-      if (!mbar_wait_warp(bar(kSegEmpty + (it & 1)), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, p.dev_status)) break;
-      Unit u;
-      bool found = false;
-      int piece = 0;
-      while (ok) {   // until a unit with keys, or the end of the grid
-        if (pending) {
-          ok = mbar_wait_warp(bar(kClaim), (uint32_t)(claims - 1) & 1u, abort_flag, p.dev_status);
-          if (!ok) break;
-          pending = false;
-          x = claimed_cta(base + kOffClaim);
-          fence_proxy_async_smem();
-          __syncwarp();
-        }
-        if (x < 0) break;
-        if (lane == 0) {
-          mbar_arrive_expect_tx(bar(kClaim), 16);
-          claim_cta(base + kOffClaim, bar(kClaim));
-        }
-        pending = true;
-        ++claims;
-        piece = x;
-        if (pa::find_unit(p, seq, max_key, x / p.splits, u)) {
-          pa::piece_range(u.tiles, x % p.splits, p.splits, u.tile0, u.tile1);
-          found = u.tile1 > u.tile0;
-        }
-        if (found) break;
-      }
-      if (!ok) break;
-      if (lane == 0) {
-        Seg s = {};
-        s.valid = found;
-        if (found) {
-          s.b = u.b;
-          s.row0 = u.row0;
-          s.ctx = u.ctx;
-          s.token0 = u.token0;
-          s.tokens = u.tokens;
-          s.head0 = u.head0;
-          s.kv = u.kv;
-          s.piece = piece;
-          s.kt0 = u.tile0;
-          s.edge = (u.ctx + u.token0 + 1) / 128;
-          // M tile 0's last token may see fewer tiles than the block's
-          const int first = (u.ctx + u.token0 + min(u.tokens, p.tile_tokens) + 127) / 128;
-          s.n[0] = max(0, min(first, u.tile1) - u.tile0);
-          s.n[1] = u.tokens > p.tile_tokens ? u.tile1 - u.tile0 : 0;
-        }
-        segs[it & 1] = s;
-        mbar_arrive(bar(kSegFull + (it & 1)));
-      }
-      __syncwarp();
-      if (!found) break;
-    }
-    if (pending && lane == 0) mbar_drain(bar(kClaim), (uint32_t)(claims - 1) & 1u, 100000000ull);
-  } else if (warp == 11) {
-    // ================================================================ V check
-    bool ok = true;
-    int vc = 0, loads[kStages] = {0, 0};
-    for (int it = 0; ok; ++it) {
-      const volatile Seg* sg = wait_seg(it);
-      if (sg == nullptr) break;
-      const int n = max(sg->n[0], sg->n[1]), kt0 = sg->kt0, edge = sg->edge, end = sg->ctx + sg->token0 + sg->tokens;
-      vc += max(0, min(n, edge - kt0));
-      for (int j = max(0, edge - kt0); j < n && ok; ++j, ++vc) {
-        const int vs = vc % kStages;
-        if (!(ok = mbar_wait_warp(bar(kLoadV + vs), (uint32_t)loads[vs] & 1u, abort_flag, p.dev_status))) break;
-        ++loads[vs];
-        uint8_t* tile = smem + kOffV + (size_t)vs * kTileBytes;
-        const int last = end - (kt0 + j) * 128;   // rows of the sequence in this tile
-        bool bad = false;
-#pragma unroll 4
-        for (int i = lane; i < 2048; i += 32) {   // 16-byte chunks: 128 rows x 8 of one half, then of the other
-          uint4* at = reinterpret_cast<uint4*>(tile) + i;
-          uint4 v = *at;
-          if (bf16_pair_finite(v.x) && bf16_pair_finite(v.y) && bf16_pair_finite(v.z) && bf16_pair_finite(v.w)) continue;
-          bad = bad || ((i >> 3) & 127) < last;
-          uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u;
-            if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0xFFFFu;
+          if (!(ok = wait(kEmptyV + vs, vc / kStages))) {
+            ++kc;
+            break;
           }
-          *at = make_uint4(w[0], w[1], w[2], w[3]);
+          const bool check = kt0 + j >= edge;
+          load(base + kOffV + (uint32_t)vs * kTileBytes, &map_v, bar(check ? kLoadV + vs : kFullV + vs));
+          if (check) ++loads[vs];
         }
-        fence_proxy_async_smem();
-        if (__any_sync(0xffffffffu, bad) && lane == 0) segs[it & 1].bad = 1;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(kFullV + vs));
+        if (ok && lane == 0) mbar_arrive(bar(kLoaded));
       }
-      free_seg(it);
+      if (lane == 0 && *abort_flag) {
+        // drain the copies already issued (bounded) before the CTA can exit
+        for (int s = 0; s < kStages; ++s) {
+          if (kc > s) mbar_drain(bar(kFullK + (kc - 1 - s) % kStages), (uint32_t)((kc - 1 - s) / kStages) & 1u, 100000000ull);
+          if (vc > s) mbar_drain(bar(kFullV + (vc - 1 - s) % kStages), (uint32_t)((vc - 1 - s) / kStages) & 1u, 100000000ull);
+          if (loads[s] > 0) mbar_drain(bar(kLoadV + s), (uint32_t)(loads[s] - 1) & 1u, 100000000ull);
+          if (qc[s] > 0) mbar_drain(bar(kQFull + s), (uint32_t)(qc[s] - 1) & 1u, 100000000ull);
+        }
+      }
+    } else if (warp == 2) {
+      // ================================================================ scheduler
+      PromptBlocks* cached = reinterpret_cast<PromptBlocks*>(smem + kOffSeqs);
+      bool bad = false;
+      for (int b = lane; b < p.batch; b += 32) {
+        if (b < kMaxCached) cached[b] = pa::blocks_of(p, b);
+        bad = bad || !prompt_sequence_ok(p.bounds, p.token_offsets[b], p.token_offsets[b + 1], p.ctx_lens[b]);
+      }
+      if (bad) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
+      __syncwarp();
+      auto seq = [&](int b) { return b < kMaxCached ? cached[b] : pa::blocks_of(p, b); };
+      const int max_key = p.batch == 1 ? 0 : pa::max_block_key(seq, p.batch);
+      bool ok = true;
+      int x = (int)blockIdx.x, claims = 0;
+      for (int it = 0; ok; ++it) {
+        if (!mbar_wait_warp(bar(kSegEmpty + (it & 1)), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, p.dev_status)) break;
+        if (it > 0 && !mbar_wait_warp(bar(kLoaded), (uint32_t)(it - 1) & 1u, abort_flag, p.dev_status)) break;
+        Unit u;
+        bool found = false;
+        for (bool first = it == 0; !found; first = false) {   // until a unit with keys, or the end of the grid
+          if (!first) {
+            if (lane == 0) {
+              mbar_arrive_expect_tx(bar(kClaim), 16);
+              claim_cta(base + kOffClaim, bar(kClaim));
+            }
+            ok = mbar_wait_warp(bar(kClaim), (uint32_t)claims & 1u, abort_flag, p.dev_status);
+            if (!ok) {
+              if (lane == 0) mbar_drain(bar(kClaim), (uint32_t)claims & 1u, 100000000ull);
+              break;
+            }
+            ++claims;
+            x = claimed_cta(base + kOffClaim);
+            fence_proxy_async_smem();
+            __syncwarp();
+          }
+          if (x < 0) break;
+          if (pa::find_unit(p, seq, max_key, x / p.splits, u)) {
+            pa::piece_range(u.tiles, x % p.splits, p.splits, u.tile0, u.tile1);
+            found = u.tile1 > u.tile0;
+          }
+        }
+        if (!ok) break;
+        if (lane == 0) {
+          Seg s = {};
+          s.valid = found;
+          if (found) {
+            s.b = u.b;
+            s.row0 = u.row0;
+            s.ctx = u.ctx;
+            s.token0 = u.token0;
+            s.tokens = u.tokens;
+            s.head0 = u.head0;
+            s.kv = u.kv;
+            s.piece = x;
+            s.kt0 = u.tile0;
+            s.edge = (u.ctx + u.token0 + 1) / 128;
+            // M tile 0's last token may see fewer tiles than the block's
+            const int first = (u.ctx + u.token0 + min(u.tokens, p.tile_tokens) + 127) / 128;
+            s.n[0] = max(0, min(first, u.tile1) - u.tile0);
+            s.n[1] = u.tokens > p.tile_tokens ? u.tile1 - u.tile0 : 0;
+          }
+          segs[it & 1] = s;
+          mbar_arrive(bar(kSegFull + (it & 1)));
+        }
+        __syncwarp();
+        if (!found) break;
+      }
+    } else {
+      // ================================================================ V check
+      bool ok = true;
+      int vc = 0, loads[kStages] = {0, 0};
+      for (int it = 0; ok; ++it) {
+        const volatile Seg* sg = wait_seg(it);
+        if (sg == nullptr) break;
+        const int n = max(sg->n[0], sg->n[1]), kt0 = sg->kt0, edge = sg->edge, end = sg->ctx + sg->token0 + sg->tokens;
+        vc += max(0, min(n, edge - kt0));
+        for (int j = max(0, edge - kt0); j < n && ok; ++j, ++vc) {
+          const int vs = vc % kStages;
+          if (!(ok = mbar_wait_warp(bar(kLoadV + vs), (uint32_t)loads[vs] & 1u, abort_flag, p.dev_status))) break;
+          ++loads[vs];
+          uint8_t* tile = smem + kOffV + (size_t)vs * kTileBytes;
+          const int last = end - (kt0 + j) * 128;   // rows of the sequence in this tile
+          bool bad = false;
+  #pragma unroll 4
+          for (int i = lane; i < 2048; i += 32) {   // 16-byte chunks: 128 rows x 8 of one half, then of the other
+            uint4* at = reinterpret_cast<uint4*>(tile) + i;
+            uint4 v = *at;
+            if (bf16_pair_finite(v.x) && bf16_pair_finite(v.y) && bf16_pair_finite(v.z) && bf16_pair_finite(v.w)) continue;
+            bad = bad || ((i >> 3) & 127) < last;
+            uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  #pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u;
+              if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0xFFFFu;
+            }
+            *at = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+          fence_proxy_async_smem();
+          if (__any_sync(0xffffffffu, bad) && lane == 0) segs[it & 1].bad = 1;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(kFullV + vs));
+        }
+        free_seg(it);
+      }
     }
   } else {
     // ================================================================ softmax / epilogue
-    const int t = (warp - 2) >> 2;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsMany));
+    const int t = (warp - 4) >> 2;
     const int row = (warp & 3) * 32 + lane;   // = TMEM lane this warp may access
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + lane_base + (uint32_t)t * 128u, tO = tS + 256u;
@@ -485,12 +503,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int pos = q0 + min(my_token, tokens - 1);   // the last key that this row sees
       const bool row_valid = in_tile && my_token < tokens;
       const int whole = (q0 + t * p.tile_tokens + 1) / 128;   // first key tile that some row sees in part
+      // a warp without rows leaves what it finds: its rows of O are not read
+      const bool any_row = (warp & 3) * 32 < min(used, (tokens - t * p.tile_tokens) * p.sub);
       float m_run = -INFINITY, l_run = 0.f;
       bool ok = true;
       for (int j = 0; j < n; ++j, ++tiles) {
         if (!(ok = mbar_wait_warp(bar(kSFull + t), (uint32_t)tiles & 1u, abort_flag, p.dev_status))) break;
         tc_fence_after();
-        softmax_tile(tS, tO, j > 0, kt0 + j >= whole, pos - (kt0 + j) * 128, p.scale_log2, m_run, l_run);
+        if (any_row) softmax_tile(tS, tO, j > 0, kt0 + j >= whole, pos - (kt0 + j) * 128, p.scale_log2, m_run, l_run);
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(kPFull + t));
       }
