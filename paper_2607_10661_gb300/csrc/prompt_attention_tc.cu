@@ -10,15 +10,15 @@
 // even out whatever the lengths, and a unit's first loads and its set-up run beside the unit before it.
 //
 // Warps (384 threads; the first four give registers to the others):
-//   0       TMA producer: K, V (a ring of two stages each), Q of the next unit.
-//   1       TMEM allocator and MMA issuer: S_t = Q_t K^T, O_t += P_t V, in the order
-//             S_0, S_1 | PV_0, S_0', PV_1, S_1' | ...
-//           so that one M tile's softmax runs beside the other's products.
-//   2       scheduler: the next unit, claimed when the producer has asked for the last tile of this one.
+//   0       scheduler and TMA producer: claims the next unit when the last tiles of this one are asked for;
+//           K and V tiles into a ring of five, Q.
+//   1, 2    MMA issuers of M tile 0 and 1: S_t = Q_t K^T, then PV_t, S_t' | PV_t', S_t'' | .., in turns, so that
+//           one M tile's softmax runs beside the other's products.  Products go out at the tensor core's pace:
+//           an issuer's waits and commits would leave the pipe idle, so the other is let go a few products early.
 //   3       V check: of key tiles that some row sees in part, infinities and NaN of V are set to 0 (a
 //           weight of 0 must not meet them) and noted; the rows that see such a key add it at the end.
 //   4 - 11  softmax of M tile 0 (4 - 7) and 1 (8 - 11), a thread a row: running maximum, moved only when
-//           exceeded by 2^8, exp2, bf16 weights over S in TMEM, fp32 row sum; O / l at the end.
+//           exceeded by 2^8, exp2, bf16 weights over S in TMEM (told in two halves), fp32 row sum; O / l at the end.
 // TMEM: S_0 | S_1 | O_0 | O_1, 128 fp32 columns each; P_t lies over the first 64 columns of S_t.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -39,32 +39,32 @@ using tc::kHalfBytes;
 using tc::kTileBytes;
 
 constexpr int kThreads = 384;
-constexpr int kStages = 2;   // K tiles, and V tiles
-// Registers a thread: 168 at launch (384 threads), then 88 for warps 0 - 3 and 208 for the softmax warps,
-// which hold a row's 128 scores: 128 * 88 + 256 * 208 = 384 * 168.
-constexpr int kRegsLaunch = 168, kRegsFew = 88, kRegsMany = 208;
+constexpr int kTiles = 5;    // of the ring of K and V tiles
+constexpr int kSteps = 8;    // barriers for steps whose tiles have been read: more than steps that tiles are held for
+// Registers a thread: 168 at launch (384 threads), then 96 for warps 0 - 3 and 200 for the softmax warps,
+// which hold a row's 128 scores: 128 * 96 + 256 * 200 <= 384 * 168.
+constexpr int kRegsLaunch = 168, kRegsFew = 96, kRegsMany = 200;
 static_assert(128 * kRegsFew + 256 * kRegsMany <= kThreads * kRegsLaunch, "register split");
 constexpr uint32_t kOffQ = 0;
-constexpr uint32_t kOffK = 2 * kTileBytes;
-constexpr uint32_t kOffV = kOffK + kStages * kTileBytes;
-constexpr uint32_t kOffBar = kOffV + kStages * kTileBytes;
+constexpr uint32_t kOffRing = 2 * kTileBytes;
+constexpr uint32_t kOffBar = kOffRing + kTiles * kTileBytes;
+// The ring takes a unit's tiles as K_0 | V_0, K_1 | V_1, K_2 | .. | V_n-1; a step is what lies between two bars:
+// its tiles are free when its products are done, which one commit tells.
 enum Bar {
-  kFullK = 0,
-  kEmptyK = kFullK + kStages,
-  kFullV = kEmptyK + kStages,
-  kEmptyV = kFullV + kStages,
-  kLoadV = kEmptyV + kStages,   // a V tile that is checked first has landed
-  kSFull = kLoadV + kStages,
-  kPFull = kSFull + 2,
+  kFull = 0,
+  kLoadV = kFull + kTiles,    // a V tile that is checked before it counts as full
+  kDone = kLoadV + kTiles,    // steps, in turn, by both issuers
+  kSFull = kDone + kSteps,
+  kPHalf = kSFull + 2,        // P of a tile's first 64 keys, by its four warps, and the issuer's turn, by the other issuer
+  kPFull = kPHalf + 2,        // of the others, by the four warps
   kOFull = kPFull + 2,
   kQFull = kOFull + 2,
   kQEmpty = kQFull + 2,
   kSegFull = kQEmpty + 2,
   kSegEmpty = kSegFull + 2,
   kClaim = kSegEmpty + 2,
-  kLoaded,              // the producer has asked for all tiles of a unit
   kDrain,
-  kBars
+  kBars = kDrain + 2
 };
 constexpr uint32_t kOffTmemPtr = kOffBar + kBars * 8;
 constexpr uint32_t kOffAbort = kOffTmemPtr + 4;
@@ -81,7 +81,7 @@ struct Seg {
   int bad;               // the V check found infinities or NaN
 };
 constexpr uint32_t kOffSeg = kOffClaim + 16;
-constexpr int kMaxCached = 512;   // sequences whose blocks are kept in shared memory
+constexpr int kMaxCached = 160;   // sequences whose blocks are kept in shared memory
 constexpr uint32_t kOffSeqs = kOffSeg + 2 * sizeof(Seg);
 constexpr uint32_t kSmemUsed = kOffSeqs + kMaxCached * sizeof(PromptBlocks);
 constexpr uint32_t kSmemBytes = kSmemUsed + 1024;   // slack to align the base to 1024 B
@@ -126,7 +126,7 @@ static __device__ __noinline__ void rescale_o(uint32_t tO, float alpha) {
 // the tile's keys 0 .. last.  The whole row is in registers: one maximum and one vote a tile, and then exponentials
 // and packing without a dependence between chunks.  Warp-collective.
 __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool has_o, bool need_mask, int last, float sl2,
-                                             float& m_run, float& l_run) {
+                                             float& m_run, float& l_run, uint32_t half_bar) {
   uint32_t r[4][32];
 #pragma unroll
   for (int c = 0; c < 4; ++c) tmem_ld32(tS + (uint32_t)c * 32u, r[c]);
@@ -173,6 +173,12 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool has_
       pk[e >> 1] = pack_bf16x2(p0, p1);
     }
     tmem_st16(tS + (uint32_t)c * 16u, pk);   // P chunk c: columns [16c, 16c+16) of S
+    if (c == 1) {   // the products of the first 64 keys may start
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if ((threadIdx.x & 31) == 0) mbar_arrive(half_bar);
+    }
   }
   float s0, s1;
   f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
@@ -180,6 +186,24 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool has_
   tmem_st_wait();
   tc_fence_before();
 }
+
+// Instructions [kBegin, kEnd) of the eight of S_t = Q_t K^T, and of O_t (+)= P_t V (see tc::issue_s, issue_pv).
+template <int kBegin, int kEnd>
+__device__ __forceinline__ void issue_s(uint32_t leader, uint32_t s_tmem, uint32_t q_desc, uint32_t k_desc) {
+#pragma unroll
+  for (int kk = kBegin; kk < kEnd; ++kk) {
+    const uint32_t o = (uint32_t)(kk >> 2) * (kHalfBytes >> 4) + (uint32_t)(kk & 3) * 2u;
+    mma_ss_if(leader, s_tmem, q_desc + o, k_desc + o, tc::kDescHi, tc::kIdescS, kk > 0 ? 1u : 0u);
+  }
+}
+template <int kBegin, int kEnd>
+__device__ __forceinline__ void issue_pv(uint32_t leader, uint32_t s_tmem, uint32_t v_desc, bool acc) {
+#pragma unroll
+  for (int kk = kBegin; kk < kEnd; ++kk)
+    mma_ts_if(leader, s_tmem + 256u, s_tmem + (uint32_t)kk * 8u, v_desc + (uint32_t)kk * 128u, tc::kDescHi, tc::kIdescPV,
+              (acc || kk > 0) ? 1u : 0u);
+}
+constexpr int kEarly = 5;   // products of a group of eight before the other issuer is let go
 
 __device__ __forceinline__ bool bf16_pair_finite(uint32_t w) {
   return (w & 0x7F80u) != 0x7F80u && (w & 0x7F800000u) != 0x7F800000u;
@@ -203,7 +227,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   // set-up that reads no global memory: it may overlap the stream's previous grid
   if (threadIdx.x == 0) {
     for (int i = 0; i < kBars; ++i) {
-      const int count = i >= kPFull && i < kPFull + 2 ? 4 : (i >= kSegEmpty && i < kSegEmpty + 2 ? 11 : 1);
+      const int count = i >= kDone && i < kDone + kSteps ? 2 : i >= kPHalf && i < kPHalf + 2 ? 5
+                        : i >= kPFull && i < kPFull + 2 ? 4 : i >= kSegEmpty && i < kSegEmpty + 2 ? 11 : 1;
       mbar_init(bar(i), count);
     }
     *abort_flag = 0;
@@ -243,146 +268,99 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
-    if (warp == 1) {
-      // ================================================================ MMA issuer
-      const uint32_t dq = (uint32_t)smem_desc_sw128(base + kOffQ, 16, 1024), dk = (uint32_t)smem_desc_sw128(base + kOffK, 16, 1024),
-                     dv = (uint32_t)smem_desc_sw128(base + kOffV, kHalfBytes, 1024);
-      const uint32_t leader = lane == 0 ? 1u : 0u;
+    if (warp == 1 || warp == 2) {
+      // ================================================================ MMA issuer of M tile t
+      const int t = warp - 1;
+      const uint32_t dq = (uint32_t)smem_desc_sw128(base + kOffQ + (uint32_t)t * kTileBytes, 16, 1024);
+      const uint32_t dk = (uint32_t)smem_desc_sw128(base + kOffRing, 16, 1024);
+      const uint32_t dv = (uint32_t)smem_desc_sw128(base + kOffRing, kHalfBytes, 1024);
+      const uint32_t s_tmem = tmem + (uint32_t)t * 128u, leader = lane == 0 ? 1u : 0u;
       auto commit = [&](int b) {
         if (leader) mma_commit(bar(b));
       };
       auto wait = [&](int b, int uses) { return mbar_wait_warp(bar(b), (uint32_t)uses & 1u, abort_flag, p.dev_status); };
       bool ok = true;
-      int kc = 0, vc = 0, pc[2] = {0, 0}, qc[2] = {0, 0};   // tiles taken from the rings, P and Q taken
+      int steps = 0, ps = 0, qs = 0;   // steps, P and Q taken
+      int at = 0;                      // ring place of the next tile
+      uint32_t phase = 0;              // the ring's turn
+      auto take = [&](uint32_t& tile) {   // waits for the next tile; its descriptor offset
+        if (!wait(kFull + at, (int)phase)) return false;
+        tile = (uint32_t)at * (kTileBytes >> 4);
+        if (++at == kTiles) at = 0, phase ^= 1u;
+        return true;
+      };
+      auto step_done = [&](bool issued) {   // the step's tiles are free when its products are done
+        if (issued) commit(kDone + steps % kSteps); else if (leader) mbar_arrive(bar(kDone + steps % kSteps));
+        ++steps;
+      };
       for (int it = 0; ok; ++it) {
         const volatile Seg* sg = wait_seg(it);
         if (sg == nullptr) break;
-        const int n0 = sg->n[0], n1 = sg->n[1], n = max(n0, n1);
+        const int n = max(sg->n[0], sg->n[1]), mine = sg->n[t], both = min(sg->n[0], sg->n[1]);
         free_seg(it);
-        auto tiles = [&](int t) { return t ? n1 : n0; };
-        auto issue_s = [&](int t, int j) {   // S_t of key tile j (K in its stage), Q_t free after the last
-          tc::issue_s(leader, tmem + (uint32_t)t * 128u, dq + (uint32_t)t * (kTileBytes >> 4),
-                      dk + (uint32_t)(kc % kStages) * (kTileBytes >> 4));
-          commit(kSFull + t);
-          if (j + 1 == tiles(t)) commit(kQEmpty + t);
+        uint32_t k_tile = 0, v_tile = 0;
+        // While both M tiles have products they take turns: M tile 1's of step j after 0's, 0's of step
+        // j + 1 after 1's of step j.  A turn that waits for nobody is the issuer's own arrival.
+        auto pass_turn = [&](int j) {
+          if (leader && (t == 0 ? j < both : j + 1 < both)) mbar_arrive(bar(kPHalf + (t ^ 1)));
         };
-        if (!(ok = wait(kFullK + kc % kStages, kc / kStages))) break;
-  #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (tiles(t) > 0 && ok) {
-            if (!(ok = wait(kQFull + t, qc[t]))) break;
-            ++qc[t];
-            tc_fence_after();
-            issue_s(t, 0);
-          }
+        if (!(ok = take(k_tile))) break;
+        if (mine > 0) {
+          if (!(ok = wait(kQFull + t, qs++))) break;
+          tc_fence_after();
+          issue_s<0, 8>(leader, s_tmem, dq, dk + k_tile);
+          commit(kSFull + t);
+          if (mine == 1) commit(kQEmpty + t);
         }
-        commit(kEmptyK + kc % kStages);
-        ++kc;
-        for (int j = 0; j < n && ok; ++j, ++vc) {
-          if (!(ok = wait(kFullV + vc % kStages, vc / kStages))) break;
-          const bool more = j + 1 < n;
-          if (more && !(ok = wait(kFullK + kc % kStages, kc / kStages))) break;
-  #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            if (j >= tiles(t)) continue;
-            if (!(ok = wait(kPFull + t, pc[t]))) break;
-            ++pc[t];
+        step_done(mine > 0);
+        for (int j = 0; j < n; ++j) {
+          if (leader && j < mine && (t == 0 ? j == 0 || j >= both : j >= both)) mbar_arrive(bar(kPHalf + t));
+          if (!(ok = take(v_tile))) break;
+          if (j + 1 < n && !(ok = take(k_tile))) break;
+          if (j < mine) {
+            if (!(ok = wait(kPHalf + t, ps))) break;
             tc_fence_after();
-            tc::issue_pv(leader, tmem + (uint32_t)t * 128u, dv + (uint32_t)(vc % kStages) * (kTileBytes >> 4), j > 0);
-            if (t == 1 || j >= n1) commit(kEmptyV + vc % kStages);   // V of this stage is no longer read
-            if (j + 1 < tiles(t)) issue_s(t, j + 1); else commit(kOFull + t);
+            issue_pv<0, 4>(leader, s_tmem, dv + v_tile, j > 0);
+            if (!(ok = wait(kPFull + t, ps++))) break;
+            tc_fence_after();
+            issue_pv<4, kEarly>(leader, s_tmem, dv + v_tile, j > 0);
+            if (j + 1 == mine) pass_turn(j);
+            issue_pv<kEarly, 8>(leader, s_tmem, dv + v_tile, j > 0);
+            if (j + 1 < mine) {
+              issue_s<0, kEarly>(leader, s_tmem, dq, dk + k_tile);
+              pass_turn(j);
+              issue_s<kEarly, 8>(leader, s_tmem, dq, dk + k_tile);
+              commit(kSFull + t);
+              if (j + 2 == mine) commit(kQEmpty + t);
+            } else {
+              commit(kOFull + t);
+            }
           }
-          if (more) {
-            commit(kEmptyK + kc % kStages);
-            ++kc;
-          }
+          step_done(j < mine);
         }
       }
       if (lane == 0 && *abort_flag) {
         // error path: let the tensor core finish what was issued before TMEM is freed
-        mma_commit(bar(kDrain));
-        mbar_drain(bar(kDrain), 0, 100000000ull);
+        mma_commit(bar(kDrain + t));
+        mbar_drain(bar(kDrain + t), 0, 100000000ull);
       }
     } else if (warp == 0) {
-      // ================================================================ TMA producer
+      // ================================================================ scheduler and TMA producer
       // A lane copies one half (64 columns) of one page's rows, or of the tile's 128 rows.
       bool ok = true;
-      int kc = 0, vc = 0, qc[2] = {0, 0}, loads[kStages] = {0, 0};
+      int at = 0, qc[2] = {0, 0};   // ring place of the next tile, Q tiles copied
+      uint32_t armed = 0, checked = 0;   // a bit per ring place: its barrier's turn (full; loaded, for the check)
+      int steps = 0, done = 0;      // steps begun, and known to be done
+      int step_of = -1;             // lane i: the step of the tile in ring place i
       const int half = lane & 1, page_at = lane >> 1, per_tile = kPaged ? 128 / p.page_size : 1;
       const uint32_t copy_at = (uint32_t)half * kHalfBytes + (kPaged ? (uint32_t)(page_at * p.page_size) * 128u : 0u);
-      auto wait = [&](int b, int uses) { return mbar_wait_warp(bar(b), ((uint32_t)uses & 1u) ^ 1u, abort_flag, p.dev_status); };
-      for (int it = 0; ok; ++it) {
-        const volatile Seg* sg = wait_seg(it);
-        if (sg == nullptr) break;
-        const int b = sg->b, kv = sg->kv, kt0 = sg->kt0, edge = sg->edge, head0 = sg->head0, row0 = sg->row0;
-        const int nq[2] = {sg->n[0], sg->n[1]}, n = max(nq[0], nq[1]);
-        const int end_page = kPaged ? pages_for(sg->ctx + sg->token0 + sg->tokens, p.page_size) : 0;
-        free_seg(it);
-        const int* bt = kPaged ? p.block_table + (size_t)b * p.max_pages : nullptr;
-        // this lane's page in key tile j (read one tile ahead, so that no copy waits for it)
-        auto page_of = [&](int j) {
-          const int g = (kt0 + j) * per_tile + page_at;
-          return kPaged && j < n && page_at < per_tile && g < end_page ? bt[g] : -1;
-        };
-        int next_page = page_of(0);
-        for (int j = 0; j < n && ok; ++j, ++kc, ++vc) {
-          const int ks = kc % kStages, vs = vc % kStages, t0 = (kt0 + j) * 128;
-          int row = 0, copies = 1;   // first row of this lane's copy; pages of the tile
-          bool mine = lane < 2;
-          if (kPaged) {
-            copies = min(per_tile, end_page - (kt0 + j) * per_tile);
-            mine = page_at < copies;
-            const bool there = next_page >= 0 && next_page < p.num_pages;
-            if (mine && !there) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
-            row = there ? (p.layer * p.num_pages + next_page) * p.page_size : -128;   // (-128: TMA fills zeros)
-            next_page = page_of(j + 1);
-          } else {
-            row = (p.layer * p.batch + b) * p.seq_capacity + t0;
-          }
-          auto load = [&](uint32_t dst, const CUtensorMap* map, uint32_t full) {
-            if (lane == 0) mbar_arrive_expect_tx(full, kPaged ? (uint32_t)(copies * p.page_size) * 256u : kTileBytes);
-            __syncwarp();
-            if (mine) tma_load_3d(dst + copy_at, map, full, half * 64, kv, row);
-          };
-          if (!(ok = wait(kEmptyK + ks, kc / kStages))) break;
-          load(base + kOffK + (uint32_t)ks * kTileBytes, &map_k, bar(kFullK + ks));
-          if (j == 0) {
-  #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-              if (!ok || nq[t] == 0 || !(ok = wait(kQEmpty + t, qc[t]))) continue;
-              ++qc[t];
-              if (lane == 0) mbar_arrive_expect_tx(bar(kQFull + t), (uint32_t)used * 256u);
-              __syncwarp();
-              if (lane < 2)
-                tma_load_3d(base + kOffQ + (uint32_t)t * kTileBytes + (uint32_t)half * kHalfBytes, &map_q, bar(kQFull + t),
-                            half * 64, head0, row0 + t * p.tile_tokens);
-            }
-            if (!ok) {
-              ++kc;
-              break;
-            }
-          }
-          if (!(ok = wait(kEmptyV + vs, vc / kStages))) {
-            ++kc;
-            break;
-          }
-          const bool check = kt0 + j >= edge;
-          load(base + kOffV + (uint32_t)vs * kTileBytes, &map_v, bar(check ? kLoadV + vs : kFullV + vs));
-          if (check) ++loads[vs];
-        }
-        if (ok && lane == 0) mbar_arrive(bar(kLoaded));
-      }
-      if (lane == 0 && *abort_flag) {
-        // drain the copies already issued (bounded) before the CTA can exit
-        for (int s = 0; s < kStages; ++s) {
-          if (kc > s) mbar_drain(bar(kFullK + (kc - 1 - s) % kStages), (uint32_t)((kc - 1 - s) / kStages) & 1u, 100000000ull);
-          if (vc > s) mbar_drain(bar(kFullV + (vc - 1 - s) % kStages), (uint32_t)((vc - 1 - s) / kStages) & 1u, 100000000ull);
-          if (loads[s] > 0) mbar_drain(bar(kLoadV + s), (uint32_t)(loads[s] - 1) & 1u, 100000000ull);
-          if (qc[s] > 0) mbar_drain(bar(kQFull + s), (uint32_t)(qc[s] - 1) & 1u, 100000000ull);
-        }
-      }
-    } else if (warp == 2) {
-      // ================================================================ scheduler
+      // waits until the next ring place is free
+      auto place = [&]() {
+        const int last = __shfl_sync(0xffffffffu, step_of, at);
+        for (; done <= last; ++done)
+          if (!mbar_wait_warp(bar(kDone + done % kSteps), (uint32_t)(done / kSteps) & 1u, abort_flag, p.dev_status)) return false;
+        return true;
+      };
       PromptBlocks* cached = reinterpret_cast<PromptBlocks*>(smem + kOffSeqs);
       bool bad = false;
       for (int b = lane; b < p.batch; b += 32) {
@@ -393,85 +371,155 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       auto seq = [&](int b) { return b < kMaxCached ? cached[b] : pa::blocks_of(p, b); };
       const int max_key = p.batch == 1 ? 0 : pa::max_block_key(seq, p.batch);
-      bool ok = true;
-      int x = (int)blockIdx.x, claims = 0;
+      int x = (int)blockIdx.x, claims = 0;   // the unit's number; claims made
+      bool claimed = false;                  // the last one has not been read yet
+      auto claim = [&]() {
+        if (lane == 0) {
+          mbar_arrive_expect_tx(bar(kClaim), 16);
+          claim_cta(base + kOffClaim, bar(kClaim));
+        }
+        claimed = true;
+        ++claims;
+      };
       for (int it = 0; ok; ++it) {
         if (!mbar_wait_warp(bar(kSegEmpty + (it & 1)), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, p.dev_status)) break;
-        if (it > 0 && !mbar_wait_warp(bar(kLoaded), (uint32_t)(it - 1) & 1u, abort_flag, p.dev_status)) break;
         Unit u;
         bool found = false;
         for (bool first = it == 0; !found; first = false) {   // until a unit with keys, or the end of the grid
           if (!first) {
-            if (lane == 0) {
-              mbar_arrive_expect_tx(bar(kClaim), 16);
-              claim_cta(base + kOffClaim, bar(kClaim));
-            }
-            ok = mbar_wait_warp(bar(kClaim), (uint32_t)claims & 1u, abort_flag, p.dev_status);
-            if (!ok) {
-              if (lane == 0) mbar_drain(bar(kClaim), (uint32_t)claims & 1u, 100000000ull);
-              break;
-            }
-            ++claims;
+            if (!claimed) claim();
+            if (!(ok = mbar_wait_warp(bar(kClaim), (uint32_t)(claims - 1) & 1u, abort_flag, p.dev_status))) break;
+            claimed = false;
             x = claimed_cta(base + kOffClaim);
             fence_proxy_async_smem();
             __syncwarp();
+            if (x < 0) break;
           }
-          if (x < 0) break;
           if (pa::find_unit(p, seq, max_key, x / p.splits, u)) {
             pa::piece_range(u.tiles, x % p.splits, p.splits, u.tile0, u.tile1);
             found = u.tile1 > u.tile0;
           }
         }
         if (!ok) break;
+        const int b = u.b, kv = u.kv, kt0 = u.tile0, head0 = u.head0, row0 = u.row0, end = u.ctx + u.token0 + u.tokens;
+        const int edge = (u.ctx + u.token0 + 1) / 128;
+        // M tile 0's last token may see fewer tiles than the block's
+        const int tiles0 = (u.ctx + u.token0 + min(u.tokens, p.tile_tokens) + 127) / 128;
+        const int nq[2] = {max(0, min(tiles0, u.tile1) - kt0), u.tokens > p.tile_tokens ? u.tile1 - kt0 : 0};
+        const int n = max(nq[0], nq[1]);
         if (lane == 0) {
           Seg s = {};
           s.valid = found;
           if (found) {
-            s.b = u.b;
-            s.row0 = u.row0;
+            s.b = b;
+            s.row0 = row0;
             s.ctx = u.ctx;
             s.token0 = u.token0;
             s.tokens = u.tokens;
-            s.head0 = u.head0;
-            s.kv = u.kv;
+            s.head0 = head0;
+            s.kv = kv;
             s.piece = x;
-            s.kt0 = u.tile0;
-            s.edge = (u.ctx + u.token0 + 1) / 128;
-            // M tile 0's last token may see fewer tiles than the block's
-            const int first = (u.ctx + u.token0 + min(u.tokens, p.tile_tokens) + 127) / 128;
-            s.n[0] = max(0, min(first, u.tile1) - u.tile0);
-            s.n[1] = u.tokens > p.tile_tokens ? u.tile1 - u.tile0 : 0;
+            s.kt0 = kt0;
+            s.edge = edge;
+            s.n[0] = nq[0];
+            s.n[1] = nq[1];
           }
           segs[it & 1] = s;
           mbar_arrive(bar(kSegFull + (it & 1)));
         }
         __syncwarp();
         if (!found) break;
+        const int end_page = kPaged ? pages_for(end, p.page_size) : 0;
+        const int* bt = kPaged ? p.block_table + (size_t)b * p.max_pages : nullptr;
+        // this lane's page of key tile j (read a step ahead, so that no copy waits for it)
+        auto page_of = [&](int j) {
+          const int g = (kt0 + j) * per_tile + page_at;
+          return kPaged && j < n && page_at < per_tile && g < end_page ? bt[g] : -1;
+        };
+        auto pages_in = [&](int j) { return kPaged ? min(per_tile, end_page - (kt0 + j) * per_tile) : 1; };
+        // first row of this lane's copy of tile j
+        auto row_of = [&](int j, int page) {
+          if (!kPaged) return (p.layer * p.batch + b) * p.seq_capacity + (kt0 + j) * 128;
+          const bool there = page >= 0 && page < p.num_pages;
+          if (!there && page_at < pages_in(j)) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
+          return there ? (p.layer * p.num_pages + page) * p.page_size : -128;   // (-128: TMA fills zeros)
+        };
+        auto copy = [&](const CUtensorMap* map, bool check, int j, int row) {   // tile j into the next ring place
+          const uint32_t full = bar((check ? kLoadV : kFull) + at);
+          if (lane == 0)
+            mbar_arrive_expect_tx(full, kPaged ? (uint32_t)(pages_in(j) * p.page_size) * 256u : kTileBytes);
+          __syncwarp();
+          if (page_at < pages_in(j))
+            tma_load_3d(base + kOffRing + (uint32_t)at * kTileBytes + copy_at, map, full, half * 64, kv, row);
+          if (lane == at) step_of = steps;
+          armed ^= 1u << at;
+          if (check) checked ^= 1u << at;
+          if (++at == kTiles) at = 0;
+        };
+        int next_page = page_of(0), row_v = 0;
+        for (int j = -1; j < n && ok; ++j, ++steps) {   // V of tile j and K of tile j + 1
+          const int row_k = j + 1 < n ? row_of(j + 1, next_page) : 0;
+          next_page = page_of(j + 2);
+          if (j == n - 1) claim();
+          if (j >= 0) {
+            if (!(ok = place())) break;
+            copy(&map_v, kt0 + j >= edge, j, row_v);
+          }
+          if (j + 1 < n) {
+            if (!(ok = place())) break;
+            copy(&map_k, false, j + 1, row_k);
+          }
+          row_v = row_k;
+          if (j == -1) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              if (!ok || nq[t] == 0 ||
+                  !(ok = mbar_wait_warp(bar(kQEmpty + t), ((uint32_t)qc[t] & 1u) ^ 1u, abort_flag, p.dev_status)))
+                continue;
+              ++qc[t];
+              if (lane == 0) mbar_arrive_expect_tx(bar(kQFull + t), (uint32_t)used * 256u);
+              __syncwarp();
+              if (lane < 2)
+                tma_load_3d(base + kOffQ + (uint32_t)t * kTileBytes + (uint32_t)half * kHalfBytes, &map_q, bar(kQFull + t),
+                            half * 64, head0, row0 + t * p.tile_tokens);
+            }
+          }
+        }
+      }
+      if (lane == 0 && *abort_flag) {
+        // drain the copies already issued (bounded) before the CTA can exit
+        for (int s = 0; s < kTiles; ++s) {
+          mbar_drain(bar(kFull + s), ((armed >> s) & 1u) ^ 1u, 100000000ull);
+          mbar_drain(bar(kLoadV + s), ((checked >> s) & 1u) ^ 1u, 100000000ull);
+        }
+        for (int t = 0; t < 2; ++t)
+          if (qc[t] > 0) mbar_drain(bar(kQFull + t), (uint32_t)(qc[t] - 1) & 1u, 100000000ull);
+        if (claims > 0) mbar_drain(bar(kClaim), (uint32_t)(claims - 1) & 1u, 100000000ull);
       }
     } else {
       // ================================================================ V check
       bool ok = true;
-      int vc = 0, loads[kStages] = {0, 0};
+      int tiles = 0;            // of the ring before this unit's
+      uint32_t checked = 0;     // a bit per ring place: its barrier's turn
       for (int it = 0; ok; ++it) {
         const volatile Seg* sg = wait_seg(it);
         if (sg == nullptr) break;
         const int n = max(sg->n[0], sg->n[1]), kt0 = sg->kt0, edge = sg->edge, end = sg->ctx + sg->token0 + sg->tokens;
-        vc += max(0, min(n, edge - kt0));
-        for (int j = max(0, edge - kt0); j < n && ok; ++j, ++vc) {
-          const int vs = vc % kStages;
-          if (!(ok = mbar_wait_warp(bar(kLoadV + vs), (uint32_t)loads[vs] & 1u, abort_flag, p.dev_status))) break;
-          ++loads[vs];
-          uint8_t* tile = smem + kOffV + (size_t)vs * kTileBytes;
+        for (int j = max(0, edge - kt0); j < n && ok; ++j) {
+          const int vs = (tiles + 2 * j + 1) % kTiles;   // (the tiles go K_0, V_0, K_1, V_1, ..)
+          if (!(ok = mbar_wait_warp(bar(kLoadV + vs), (checked >> vs) & 1u, abort_flag, p.dev_status))) break;
+          checked ^= 1u << vs;
+          uint8_t* tile = smem + kOffRing + (size_t)vs * kTileBytes;
           const int last = end - (kt0 + j) * 128;   // rows of the sequence in this tile
           bool bad = false;
-  #pragma unroll 4
+#pragma unroll 4
           for (int i = lane; i < 2048; i += 32) {   // 16-byte chunks: 128 rows x 8 of one half, then of the other
             uint4* at = reinterpret_cast<uint4*>(tile) + i;
             uint4 v = *at;
             if (bf16_pair_finite(v.x) && bf16_pair_finite(v.y) && bf16_pair_finite(v.z) && bf16_pair_finite(v.w)) continue;
             bad = bad || ((i >> 3) & 127) < last;
             uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  #pragma unroll
+#pragma unroll
             for (int e = 0; e < 4; ++e) {
               if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u;
               if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0xFFFFu;
@@ -481,8 +529,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           fence_proxy_async_smem();
           if (__any_sync(0xffffffffu, bad) && lane == 0) segs[it & 1].bad = 1;
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar(kFullV + vs));
+          if (lane == 0) mbar_arrive(bar(kFull + vs));
         }
+        tiles = (tiles + 2 * n) % kTiles;
         free_seg(it);
       }
     }
@@ -510,7 +559,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int j = 0; j < n; ++j, ++tiles) {
         if (!(ok = mbar_wait_warp(bar(kSFull + t), (uint32_t)tiles & 1u, abort_flag, p.dev_status))) break;
         tc_fence_after();
-        if (any_row) softmax_tile(tS, tO, j > 0, kt0 + j >= whole, pos - (kt0 + j) * 128, p.scale_log2, m_run, l_run);
+        if (any_row)
+          softmax_tile(tS, tO, j > 0, kt0 + j >= whole, pos - (kt0 + j) * 128, p.scale_log2, m_run, l_run, bar(kPHalf + t));
+        else if (lane == 0)
+          mbar_arrive(bar(kPHalf + t));
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(kPFull + t));
       }
