@@ -69,7 +69,8 @@ struct PromptAttnParams {
   int tile_tokens;             // tokens per M tile (tile_tokens * sub rows of it are used)
   int block_tokens;            // tokens per block: one or two M tiles
   int tile_rows;               // rows of an M tile in the partials
-  int key_tile;                // keys per tile
+  int key_tile, key_tile_log2; // keys per tile
+  int level_step;              // of the blocks' order (prompt_geometry.cuh)
   int blocks;                  // upper bound of the batch's blocks of tokens (per head tile)
   int splits;                  // pieces that a block's keys are cut into
   int page_size, seq_capacity, num_pages, max_pages;
@@ -77,7 +78,7 @@ struct PromptAttnParams {
 };
 
 // Chooses the tiles and the cut of the keys from the host-known sizes, with `scratch` bytes at hand: sets sub,
-// tile_heads, tiles_per_kv, tile_tokens, block_tokens, tile_rows, key_tile, blocks and splits.  Returns the
+// tile_heads, tiles_per_kv, tile_tokens, block_tokens, tile_rows, key_tile, level_step, blocks and splits.  Returns the
 // scratch that the cut takes (0: unsplit).
 size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int sms);
 // bf16, D = 128.  map_k, map_v: boxes of 64 columns of one KV head and 128 rows (or a page's); map_q: of 64

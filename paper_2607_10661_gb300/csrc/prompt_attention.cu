@@ -27,10 +27,9 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
   if (threadIdx.x == 0) grid_launch_dependents();
   // (the batch's arrays were complete before the attention let this grid be placed)
   if (threadIdx.x < 32) {
-    auto seq = [&](int b) { return blocks_of(p, b); };
-    const int max_key = p.batch == 1 ? 0 : max_block_key(seq, p.batch);
+    Units units(p);
     Unit u;
-    const bool found = find_unit(p, seq, max_key, blockIdx.x, u);
+    const bool found = units.find(p, blockIdx.x, u);
     if (threadIdx.x == 0) {
       if (found) unit_s = u;
       found_s = found;
@@ -104,12 +103,14 @@ int largest_divisor(int group, int most) {
 size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int sms) {
   const int tile_rows = bf16 ? 128 : 64, tiles = bf16 ? 2 : 1, group = p.hq / p.hkv;   // M tiles of a block
   p.tile_rows = tile_rows;
-  p.key_tile = bf16 ? 128 : 64;
+  p.key_tile_log2 = bf16 ? 7 : 6;
+  p.key_tile = 1 << p.key_tile_log2;
   p.sub = pa::largest_divisor(group, tile_rows);
   p.tile_heads = p.hq / p.sub;
   p.tiles_per_kv = group / p.sub;
   p.tile_tokens = tile_rows / p.sub;
   p.block_tokens = tiles * p.tile_tokens;
+  p.level_step = prompt_level_step(p.bounds.max_ctx, p.bounds.max_tokens, p.block_tokens);
   const int64_t w = p.block_tokens, N = p.bounds.n_total, B = p.batch;
   const int64_t by_total = N / w + B, by_longest = B * ((p.bounds.max_tokens + w - 1) / w);
   p.blocks = (int)(by_total < by_longest ? by_total : by_longest);

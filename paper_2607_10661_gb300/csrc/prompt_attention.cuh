@@ -26,42 +26,41 @@ __device__ __forceinline__ void piece_range(int tiles, int s, int S, int& k0, in
   k1 = (int)((int64_t)tiles * (s + 1) / S);
 }
 
-// Sequence b's blocks (none if it is out of range).
-__device__ __forceinline__ PromptBlocks blocks_of(const PromptAttnParams& p, int b) {
+// Sequence b of the batch.
+__device__ __forceinline__ PromptSequence load_sequence(const PromptAttnParams& p, int b) {
   const int off0 = p.token_offsets[b], off1 = p.token_offsets[b + 1], ctx = p.ctx_lens[b];
-  return prompt_sequence_ok(p.bounds, off0, off1, ctx) ? prompt_blocks(ctx, off1 - off0, p.block_tokens) : PromptBlocks{0, 0};
+  if (!prompt_sequence_ok(p.bounds, off0, off1, ctx)) return {0, 0, 0, {0, 0}};
+  return {off0, off1 - off0, ctx, prompt_blocks(ctx, off1 - off0, p.block_tokens)};
 }
 
-// A key above every block's (a warp's answer); `seq` as find_prompt_block takes it.
-template <typename Seq>
-__device__ __forceinline__ int max_block_key(const Seq& seq, int batch) {
-  int m = 0;
-  for (int b = threadIdx.x & 31; b < batch; b += 32) {
-    const PromptBlocks s = seq(b);
-    m = max(m, s.first + s.count);
+// A warp's walk over the batch's units.  Batches of up to 32 sequences are in registers, one a lane.
+struct Units {
+  PromptSequence mine;
+  PromptCursor cur;
+  __device__ __forceinline__ Units(const PromptAttnParams& p) : mine{0, 0, 0, {0, 0}}, cur{0, 0, 0} {
+    const int lane = threadIdx.x & 31;
+    if (lane < p.batch) mine = load_sequence(p, lane);
   }
-  return (int)__reduce_max_sync(0xffffffffu, (unsigned)m);
-}
-
-// Block y / tile_heads of the batch under head tile y % tile_heads, with all of its keys (a warp's answer).
-// False: there is none.
-template <typename Seq>
-__device__ __forceinline__ bool find_unit(const PromptAttnParams& p, const Seq& seq, int max_key, int y, Unit& u) {
-  const int block = y / p.tile_heads, tile = y - block * p.tile_heads;
-  int i;
-  if (!find_prompt_block(WarpLanes{}, seq, p.batch, max_key, block, &u.b, &i)) return false;
-  const int off0 = p.token_offsets[u.b], n = p.token_offsets[u.b + 1] - off0;
-  u.ctx = p.ctx_lens[u.b];
-  u.token0 = i * p.block_tokens;
-  u.tokens = min(p.block_tokens, n - u.token0);
-  u.row0 = off0 + u.token0;
-  u.head0 = tile * p.sub;
-  u.kv = tile / p.tiles_per_kv;
-  u.tiles = (u.ctx + u.token0 + u.tokens + p.key_tile - 1) / p.key_tile;
-  u.tile0 = 0;
-  u.tile1 = u.tiles;
-  return true;
-}
+  // Block y / tile_heads of the batch under head tile y % tile_heads, with all of its keys (every lane gets it).
+  // False: there is none.
+  __device__ __forceinline__ bool find(const PromptAttnParams& p, int y, Unit& u) {
+    const int block = (int)((unsigned)y / (unsigned)p.tile_heads), tile = y - block * p.tile_heads;
+    int i;
+    PromptSequence s;
+    auto load = [&](int b) { return p.batch <= 32 ? mine : load_sequence(p, b); };
+    if (!find_prompt_block(WarpLanes{}, load, p.batch, p.level_step, block, cur, u.b, i, s)) return false;
+    u.ctx = s.ctx;
+    u.token0 = i * p.block_tokens;
+    u.tokens = min(p.block_tokens, s.tokens - u.token0);
+    u.row0 = s.row0 + u.token0;
+    u.head0 = tile * p.sub;
+    u.kv = (int)((unsigned)tile / (unsigned)p.tiles_per_kv);
+    u.tiles = (u.ctx + u.token0 + u.tokens + p.key_tile - 1) >> p.key_tile_log2;
+    u.tile0 = 0;
+    u.tile1 = u.tiles;
+    return true;
+  }
+};
 
 }  // namespace pa
 }  // namespace ptd

@@ -45,16 +45,15 @@ __global__ void __launch_bounds__(kThreads) prompt_simt_kernel(const PromptAttnP
   grid_dependency_wait();
   const int split = blockIdx.x % p.splits;
   if (t < 32) {
-    auto seq = [&](int b) { return blocks_of(p, b); };
-    const int max_key = p.batch == 1 ? 0 : max_block_key(seq, p.batch);
     if (blockIdx.x == 0) {   // malformed sequences are reported here, and have no blocks
       bool bad = false;
       for (int b = t; b < p.batch; b += 32)
         bad = bad || !prompt_sequence_ok(p.bounds, p.token_offsets[b], p.token_offsets[b + 1], p.ctx_lens[b]);
       if (bad) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
     }
+    Units units(p);
     Unit u;
-    bool found = find_unit(p, seq, max_key, blockIdx.x / p.splits, u);
+    bool found = units.find(p, blockIdx.x / p.splits, u);
     if (found) {
       piece_range(u.tiles, split, p.splits, u.tile0, u.tile1);
       found = u.tile1 > u.tile0;

@@ -70,6 +70,16 @@ constexpr uint32_t kOffTmemPtr = kOffBar + kBars * 8;
 constexpr uint32_t kOffAbort = kOffTmemPtr + 4;
 constexpr uint32_t kOffClaim = (kOffAbort + 4 + 15) / 16 * 16;   // the scheduler's answer, 16 bytes
 
+// A bounded wait of a warp (mbar_wait_warp), its loop out of line: the roles' code together is larger than the
+// instruction caches, and what is not run often should not lie between what is.
+static __device__ __forceinline__ bool wait_longer(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* dev_status) {
+  return mbar_wait_warp(bar, parity, abort_flag, dev_status);
+}
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* dev_status) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return wait_longer(bar, parity, abort_flag, dev_status);
+}
+
 // A unit as the roles need it.
 struct Seg {
   int valid;
@@ -81,9 +91,7 @@ struct Seg {
   int bad;               // the V check found infinities or NaN
 };
 constexpr uint32_t kOffSeg = kOffClaim + 16;
-constexpr int kMaxCached = 160;   // sequences whose blocks are kept in shared memory
-constexpr uint32_t kOffSeqs = kOffSeg + 2 * sizeof(Seg);
-constexpr uint32_t kSmemUsed = kOffSeqs + kMaxCached * sizeof(PromptBlocks);
+constexpr uint32_t kSmemUsed = kOffSeg + 2 * sizeof(Seg);
 constexpr uint32_t kSmemBytes = kSmemUsed + 1024;   // slack to align the base to 1024 B
 static_assert(kSmemBytes <= 232448, "shared memory budget");
 
@@ -205,8 +213,34 @@ __device__ __forceinline__ void issue_pv(uint32_t leader, uint32_t s_tmem, uint3
 }
 constexpr int kEarly = 5;   // products of a group of eight before the other issuer is let go
 
-__device__ __forceinline__ bool bf16_pair_finite(uint32_t w) {
-  return (w & 0x7F80u) != 0x7F80u && (w & 0x7F800000u) != 0x7F800000u;
+// Bit 15 of either half: the bf16 there is an infinity or NaN.
+__device__ __forceinline__ uint32_t exponent_full(uint32_t w) { return (w & 0x7F807F80u) + 0x00800080u; }
+__device__ __forceinline__ uint32_t finite_or_zero(uint32_t w) {
+  if ((w & 0x7F80u) == 0x7F80u) w &= 0xFFFF0000u;
+  if ((w & 0x7F800000u) == 0x7F800000u) w &= 0xFFFFu;
+  return w;
+}
+
+// 32 outputs of a row (columns c ..) plus the infinities and NaN of V at keys [key0, key1], which the V check
+// took out of the products.
+template <bool kPaged>
+__device__ __forceinline__ void add_bad(const PromptAttnParams& p, float* o, int b, int kv, int c, int key0, int key1) {
+  for (int key = key0; key <= key1; ++key) {
+    size_t r;
+    if (kPaged) {
+      const int pg = p.block_table[(size_t)b * p.max_pages + key / p.page_size];
+      if (pg < 0 || pg >= p.num_pages) continue;
+      r = ((size_t)p.layer * p.num_pages + pg) * p.page_size + key % p.page_size;
+    } else {
+      r = ((size_t)p.layer * p.batch + b) * p.seq_capacity + key;
+    }
+    const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + (r * p.hkv + kv) * 128 + c;
+#pragma unroll 1
+    for (int e = 0; e < 32; ++e) {
+      const float x = __bfloat162float(v[e]);
+      if (!isfinite(x)) o[e] += x;
+    }
+  }
 }
 
 template <bool kPaged>
@@ -257,7 +291,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   // The unit of a role's turn `it` (two slots), as long as there is one.
   auto wait_seg = [&](int it) -> const volatile Seg* {
-    if (!mbar_wait_warp(bar(kSegFull + (it & 1)), (uint32_t)(it >> 1) & 1u, abort_flag, p.dev_status)) return nullptr;
+    if (!wait_warp(bar(kSegFull + (it & 1)), (uint32_t)(it >> 1) & 1u, abort_flag, p.dev_status)) return nullptr;
     const volatile Seg* s = segs + (it & 1);
     return s->valid ? s : nullptr;
   };
@@ -278,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       auto commit = [&](int b) {
         if (leader) mma_commit(bar(b));
       };
-      auto wait = [&](int b, int uses) { return mbar_wait_warp(bar(b), (uint32_t)uses & 1u, abort_flag, p.dev_status); };
+      auto wait = [&](int b, int uses) { return wait_warp(bar(b), (uint32_t)uses & 1u, abort_flag, p.dev_status); };
       bool ok = true;
       int steps = 0, ps = 0, qs = 0;   // steps, P and Q taken
       int at = 0;                      // ring place of the next tile
@@ -353,24 +387,21 @@ __global__ void __launch_bounds__(kThreads, 1)
       int steps = 0, done = 0;      // steps begun, and known to be done
       int step_of = -1;             // lane i: the step of the tile in ring place i
       const int half = lane & 1, page_at = lane >> 1, per_tile = kPaged ? 128 / p.page_size : 1;
+      const int page_log2 = kPaged ? 31 - __clz(p.page_size) : 0;
       const uint32_t copy_at = (uint32_t)half * kHalfBytes + (kPaged ? (uint32_t)(page_at * p.page_size) * 128u : 0u);
       // waits until the next ring place is free
       auto place = [&]() {
         const int last = __shfl_sync(0xffffffffu, step_of, at);
         for (; done <= last; ++done)
-          if (!mbar_wait_warp(bar(kDone + done % kSteps), (uint32_t)(done / kSteps) & 1u, abort_flag, p.dev_status)) return false;
+          if (!wait_warp(bar(kDone + done % kSteps), (uint32_t)(done / kSteps) & 1u, abort_flag, p.dev_status)) return false;
         return true;
       };
-      PromptBlocks* cached = reinterpret_cast<PromptBlocks*>(smem + kOffSeqs);
+      pa::Units units(p);
       bool bad = false;
-      for (int b = lane; b < p.batch; b += 32) {
-        if (b < kMaxCached) cached[b] = pa::blocks_of(p, b);
+      for (int b = lane; b < p.batch; b += 32)
         bad = bad || !prompt_sequence_ok(p.bounds, p.token_offsets[b], p.token_offsets[b + 1], p.ctx_lens[b]);
-      }
       if (bad) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
       __syncwarp();
-      auto seq = [&](int b) { return b < kMaxCached ? cached[b] : pa::blocks_of(p, b); };
-      const int max_key = p.batch == 1 ? 0 : pa::max_block_key(seq, p.batch);
       int x = (int)blockIdx.x, claims = 0;   // the unit's number; claims made
       bool claimed = false;                  // the last one has not been read yet
       auto claim = [&]() {
@@ -382,26 +413,27 @@ __global__ void __launch_bounds__(kThreads, 1)
         ++claims;
       };
       for (int it = 0; ok; ++it) {
-        if (!mbar_wait_warp(bar(kSegEmpty + (it & 1)), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, p.dev_status)) break;
+        if (!wait_warp(bar(kSegEmpty + (it & 1)), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, p.dev_status)) break;
         Unit u;
         bool found = false;
         for (bool first = it == 0; !found; first = false) {   // until a unit with keys, or the end of the grid
           if (!first) {
             if (!claimed) claim();
-            if (!(ok = mbar_wait_warp(bar(kClaim), (uint32_t)(claims - 1) & 1u, abort_flag, p.dev_status))) break;
+            if (!(ok = wait_warp(bar(kClaim), (uint32_t)(claims - 1) & 1u, abort_flag, p.dev_status))) break;
             claimed = false;
             x = claimed_cta(base + kOffClaim);
             fence_proxy_async_smem();
             __syncwarp();
             if (x < 0) break;
           }
-          if (pa::find_unit(p, seq, max_key, x / p.splits, u)) {
-            pa::piece_range(u.tiles, x % p.splits, p.splits, u.tile0, u.tile1);
+          const int y = (int)((unsigned)x / (unsigned)p.splits);
+          if (units.find(p, y, u)) {
+            if (p.splits > 1) pa::piece_range(u.tiles, x - y * p.splits, p.splits, u.tile0, u.tile1);
             found = u.tile1 > u.tile0;
           }
         }
         if (!ok) break;
-        const int b = u.b, kv = u.kv, kt0 = u.tile0, head0 = u.head0, row0 = u.row0, end = u.ctx + u.token0 + u.tokens;
+        const int b = u.b, kv = u.kv, kt0 = u.tile0, head0 = u.head0, row0 = u.row0;
         const int edge = (u.ctx + u.token0 + 1) / 128;
         // M tile 0's last token may see fewer tiles than the block's
         const int tiles0 = (u.ctx + u.token0 + min(u.tokens, p.tile_tokens) + 127) / 128;
@@ -429,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         __syncwarp();
         if (!found) break;
-        const int end_page = kPaged ? pages_for(end, p.page_size) : 0;
+        const int end_page = kPaged ? (u.ctx + u.token0 + u.tokens + p.page_size - 1) >> page_log2 : 0;
         const int* bt = kPaged ? p.block_table + (size_t)b * p.max_pages : nullptr;
         // this lane's page of key tile j (read a step ahead, so that no copy waits for it)
         auto page_of = [&](int j) {
@@ -474,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
               if (!ok || nq[t] == 0 ||
-                  !(ok = mbar_wait_warp(bar(kQEmpty + t), ((uint32_t)qc[t] & 1u) ^ 1u, abort_flag, p.dev_status)))
+                  !(ok = wait_warp(bar(kQEmpty + t), ((uint32_t)qc[t] & 1u) ^ 1u, abort_flag, p.dev_status)))
                 continue;
               ++qc[t];
               if (lane == 0) mbar_arrive_expect_tx(bar(kQFull + t), (uint32_t)used * 256u);
@@ -504,30 +536,34 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int it = 0; ok; ++it) {
         const volatile Seg* sg = wait_seg(it);
         if (sg == nullptr) break;
-        const int n = max(sg->n[0], sg->n[1]), kt0 = sg->kt0, edge = sg->edge, end = sg->ctx + sg->token0 + sg->tokens;
-        for (int j = max(0, edge - kt0); j < n && ok; ++j) {
-          const int vs = (tiles + 2 * j + 1) % kTiles;   // (the tiles go K_0, V_0, K_1, V_1, ..)
-          if (!(ok = mbar_wait_warp(bar(kLoadV + vs), (checked >> vs) & 1u, abort_flag, p.dev_status))) break;
+        const int n = max(sg->n[0], sg->n[1]), kt0 = sg->kt0, edge = sg->edge;
+        const int first = sg->ctx + sg->token0 + 1, end = first - 1 + sg->tokens;   // keys that only some see
+        for (int j = max(0, edge - kt0); j < n; ++j) {
+          int vs = tiles + 2 * j + 1;   // (the tiles go K_0, V_0, K_1, V_1, ..)
+          vs -= vs / kTiles * kTiles;
+          if (!(ok = wait_warp(bar(kLoadV + vs), (checked >> vs) & 1u, abort_flag, p.dev_status))) break;
           checked ^= 1u << vs;
-          uint8_t* tile = smem + kOffRing + (size_t)vs * kTileBytes;
-          const int last = end - (kt0 + j) * 128;   // rows of the sequence in this tile
-          bool bad = false;
+          // 16-byte chunks: rows of the first half (64 columns), then of the second.  Rows that all of the block's
+          // tokens see stay as they are, rows behind the block's last token become 0.
+          uint4* tile = reinterpret_cast<uint4*>(smem + kOffRing + (size_t)vs * kTileBytes);
+          const int r0 = max(0, first - (kt0 + j) * 128), r1 = min(128, end - (kt0 + j) * 128);
+          const int half = ((lane >> 3) & 1) * 1024;   // two rows a turn, sixteen lanes each
+          for (int r = r1 + (lane >> 4); r < 128; r += 2) tile[half + r * 8 + (lane & 7)] = make_uint4(0, 0, 0, 0);
+          uint32_t bad = 0u;
 #pragma unroll 4
-          for (int i = lane; i < 2048; i += 32) {   // 16-byte chunks: 128 rows x 8 of one half, then of the other
-            uint4* at = reinterpret_cast<uint4*>(tile) + i;
-            uint4 v = *at;
-            if (bf16_pair_finite(v.x) && bf16_pair_finite(v.y) && bf16_pair_finite(v.z) && bf16_pair_finite(v.w)) continue;
-            bad = bad || ((i >> 3) & 127) < last;
-            uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u;
-              if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0xFFFFu;
+          for (int r = r0 + (lane >> 4); r < r1; r += 2) {
+            const uint4 v = tile[half + r * 8 + (lane & 7)];
+            bad |= exponent_full(v.x) | exponent_full(v.y) | exponent_full(v.z) | exponent_full(v.w);
+          }
+          if (__any_sync(0xffffffffu, (bad & 0x80008000u) != 0u)) {
+            for (int r = r0 + (lane >> 4); r < r1; r += 2) {
+              uint4 v = tile[half + r * 8 + (lane & 7)];
+              v.x = finite_or_zero(v.x), v.y = finite_or_zero(v.y), v.z = finite_or_zero(v.z), v.w = finite_or_zero(v.w);
+              tile[half + r * 8 + (lane & 7)] = v;
             }
-            *at = make_uint4(w[0], w[1], w[2], w[3]);
+            if (lane == 0) segs[it & 1].bad = 1;
           }
           fence_proxy_async_smem();
-          if (__any_sync(0xffffffffu, bad) && lane == 0) segs[it & 1].bad = 1;
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(kFull + vs));
         }
@@ -557,7 +593,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       float m_run = -INFINITY, l_run = 0.f;
       bool ok = true;
       for (int j = 0; j < n; ++j, ++tiles) {
-        if (!(ok = mbar_wait_warp(bar(kSFull + t), (uint32_t)tiles & 1u, abort_flag, p.dev_status))) break;
+        if (!(ok = wait_warp(bar(kSFull + t), (uint32_t)tiles & 1u, abort_flag, p.dev_status))) break;
         tc_fence_after();
         if (any_row)
           softmax_tile(tS, tO, j > 0, kt0 + j >= whole, pos - (kt0 + j) * 128, p.scale_log2, m_run, l_run, bar(kPHalf + t));
@@ -568,37 +604,20 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!ok) break;
       if (n > 0) {
-        if (!mbar_wait_warp(bar(kOFull + t), (uint32_t)outs & 1u, abort_flag, p.dev_status)) break;
+        if (!wait_warp(bar(kOFull + t), (uint32_t)outs & 1u, abort_flag, p.dev_status)) break;
         ++outs;
         tc_fence_after();
       }
-      const size_t row0 = (size_t)sg->row0, head0 = (size_t)sg->head0, piece = (size_t)sg->piece;
       const bool bad = sg->bad != 0;
-      // infinities and NaN of V that the check took out: added to the rows that see them
-      auto add_bad = [&](int c, float (&o)[32]) {
-        const int b = sg->b, end_key = min(pos, (kt0 + n) * 128 - 1);
-        for (int key = max(kt0, sg->edge) * 128; key <= end_key; ++key) {
-          size_t r;
-          if (kPaged) {
-            const int pg = p.block_table[(size_t)b * p.max_pages + key / p.page_size];
-            if (pg < 0 || pg >= p.num_pages) continue;
-            r = ((size_t)p.layer * p.num_pages + pg) * p.page_size + key % p.page_size;
-          } else {
-            r = ((size_t)p.layer * p.batch + b) * p.seq_capacity + key;
-          }
-          const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + (r * p.hkv + sg->kv) * 128 + c * 32;
-#pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            const float x = __bfloat162float(v[e]);
-            if (!isfinite(x)) o[e] += x;
-          }
-        }
-      };
-      if (p.splits == 1) {
-        const float inv = 1.f / l_run;
-        uint4* dst = reinterpret_cast<uint4*>(p.out) + ((row0 + my_token) * p.hq + head0 + my_head) * 16;
+      const float inv = p.splits == 1 ? 1.f / l_run : 1.f;   // a piece stays unnormalised
+      uint4* dst = reinterpret_cast<uint4*>(p.out) + (((size_t)sg->row0 + my_token) * p.hq + sg->head0 + my_head) * 16;
+      float4* po = reinterpret_cast<float4*>(p.part_o) + (size_t)sg->piece * 32 * 256 + t * 128 + row;
+      if (p.splits > 1 && row_valid)
+        reinterpret_cast<float2*>(p.part_ml)[(size_t)sg->piece * 256 + t * 128 + row] =
+            n > 0 ? make_float2(m_run, l_run) : make_float2(-INFINITY, 0.f);
+      if (n > 0 && any_row) {
 #pragma unroll 1
-        for (int c = 0; c < 4 && n > 0; ++c) {
+        for (int c = 0; c < 4; ++c) {
           uint32_t r[32];
           tmem_ld32(tO + (uint32_t)c * 32u, r);
           tmem_ld_wait();
@@ -606,32 +625,24 @@ __global__ void __launch_bounds__(kThreads, 1)
             float o[32];
 #pragma unroll
             for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(r[e]) * inv;
-            if (bad) add_bad(c, o);
+            if (bad) {
+              float ob[32];
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-              dst[c * 4 + g] = make_uint4(pack_bf16x2(o[8 * g], o[8 * g + 1]), pack_bf16x2(o[8 * g + 2], o[8 * g + 3]),
-                                          pack_bf16x2(o[8 * g + 4], o[8 * g + 5]), pack_bf16x2(o[8 * g + 6], o[8 * g + 7]));
-          }
-          __syncwarp();
-        }
-      } else {
-        float4* po = reinterpret_cast<float4*>(p.part_o) + piece * 32 * 256 + t * 128 + row;
-        if (row_valid)
-          reinterpret_cast<float2*>(p.part_ml)[piece * 256 + t * 128 + row] =
-              n > 0 ? make_float2(m_run, l_run) : make_float2(-INFINITY, 0.f);
-#pragma unroll 1
-        for (int c = 0; c < 4 && n > 0; ++c) {
-          uint32_t r[32];
-          tmem_ld32(tO + (uint32_t)c * 32u, r);
-          tmem_ld_wait();
-          if (row_valid) {
-            float o[32];
+              for (int e = 0; e < 32; ++e) ob[e] = o[e];
+              add_bad<kPaged>(p, ob, sg->b, sg->kv, c * 32, max(kt0, sg->edge) * 128, min(pos, (kt0 + n) * 128 - 1));
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(r[e]);
-            if (bad) add_bad(c, o);
+              for (int e = 0; e < 32; ++e) o[e] = ob[e];
+            }
+            if (p.splits == 1) {
 #pragma unroll
-            for (int g = 0; g < 8; ++g)
-              po[(size_t)(c * 8 + g) * 256] = make_float4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
+              for (int g = 0; g < 4; ++g)
+                dst[c * 4 + g] = make_uint4(pack_bf16x2(o[8 * g], o[8 * g + 1]), pack_bf16x2(o[8 * g + 2], o[8 * g + 3]),
+                                            pack_bf16x2(o[8 * g + 4], o[8 * g + 5]), pack_bf16x2(o[8 * g + 6], o[8 * g + 7]));
+            } else {
+#pragma unroll
+              for (int g = 0; g < 8; ++g)
+                po[(size_t)(c * 8 + g) * 256] = make_float4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
+            }
           }
           __syncwarp();
         }

@@ -39,46 +39,69 @@ PTD_HD int blocks_from(const PromptBlocks& s, int m) {
   return c < 0 ? 0 : (c > s.count ? s.count : c);
 }
 
-// Block number u of a batch in descending order of key (longest first, equal keys by sequence): its sequence
-// and place in it.  With F(m) the number of blocks of key >= m, its key is the largest m with F(m) > u.
-// `lanes` walks the sequences: one lane on the host, a warp's 32 on the device, where every lane gets the
-// answer; seq(b) gives sequence b's blocks; max_key is above every key.  False: no such block.
-template <typename Lanes, typename Seq>
-PTD_HD bool find_prompt_block(const Lanes& lanes, const Seq& seq, int batch, int max_key, int u, int* b_out, int* i_out) {
-  if (batch == 1) {
-    const PromptBlocks s = seq(0);
-    *b_out = 0;
-    *i_out = s.count - 1 - u;
-    return u >= 0 && u < s.count;
-  }
-  auto from = [&](int m) {
-    int c = 0;
-    for (int b = lanes.id(); b < batch; b += lanes.count()) c += blocks_from(seq(b), m);
-    return lanes.sum(c);
-  };
-  if (u < 0 || from(0) <= u) return false;
-  int lo = 0, hi = max_key;   // F(lo) > u >= F(hi)
-  while (hi - lo > 1) {
-    const int mid = lo + (hi - lo) / 2;
-    if (from(mid) > u) lo = mid; else hi = mid;
-  }
-  int left = u - from(lo + 1);   // its place among the sequences that have a block of key lo
-  for (int b0 = 0; b0 < batch; b0 += lanes.count()) {
-    const int b = b0 + lanes.id();
-    bool has = false;
-    if (b < batch) {
-      const PromptBlocks s = seq(b);
-      has = s.first <= lo && lo < s.first + s.count;
+// A sequence of the batch: its first row and number of new tokens, context and blocks (none if out of range).
+struct PromptSequence {
+  int row0, tokens, ctx;
+  PromptBlocks blocks;
+};
+
+// The blocks of a batch are numbered by level, highest first: a block's level is its key / level_step, 32 levels
+// in all (the long ones first, so that what is taken last is short).  Within a level they go by sequence, and
+// a sequence's by falling key.  Batches of more than kOrderedBatch sequences have one level: their many
+// blocks even out, and the levels would cost a walk over the batch each.
+constexpr int kLevels = 32;
+constexpr int kOrderedBatch = 128;
+PTD_HD int prompt_level_step(int max_ctx, int max_tokens, int width) { return (max_ctx / width + max_tokens / width + 2) / kLevels + 1; }
+
+// Where the last search ended: a search for a later block of the same level goes on from there.
+struct PromptCursor {
+  int level, b0, before;   // blocks of the level in the sequences below b0
+};
+
+// Block number u: its sequence b, that sequence, and the block's place in it.  `lanes` walks the sequences: one
+// lane on the host, a warp's 32 on the device, where every lane gets the answer; load(b) gives sequence b and
+// is called with b = lane modulo their number.  False: there is no such block.
+template <typename Lanes, typename Load>
+PTD_HD bool find_prompt_block(const Lanes& lanes, const Load& load, int batch, int level_step, int u, PromptCursor& cur,
+                              int& b_out, int& i_out, PromptSequence& seq_out) {
+  if (u < 0) return false;
+  int level = 0, above = 0;   // u's level, and the blocks of higher ones
+  const bool levels = batch > 1 && batch <= kOrderedBatch;
+  if (levels) {
+    auto from = [&](int l) {   // blocks of level l and higher
+      int c = 0;
+#pragma unroll 1
+      for (int b = lanes.id(); b < batch; b += lanes.count()) c += blocks_from(load(b).blocks, l * level_step);
+      return lanes.sum(c);
+    };
+    int hi = kLevels;          // from(level) > u >= above = from(hi), where there is such a block
+#pragma unroll 1
+    while (hi - level > 1) {
+      const int mid = (level + hi) >> 1, c = from(mid);
+      if (c > u) level = mid; else hi = mid, above = c;
     }
-    const uint32_t hit = lanes.ballot(has);
-    const int n = lanes.popcount(hit);
-    if (left < n) {
-      const int q = b0 + lanes.nth(hit, left);
-      *b_out = q;
-      *i_out = lo - seq(q).first;
+  }
+  const int m0 = level * level_step, m1 = levels && level + 1 < kLevels ? m0 + level_step : INT32_MAX;
+  const int left = u - above;
+  if (cur.level != level || cur.before > left) cur = {level, 0, 0};
+#pragma unroll 1
+  for (; cur.b0 < batch; cur.b0 += lanes.count()) {
+    const int b = cur.b0 + lanes.id();
+    PromptSequence s = {0, 0, 0, {0, 0}};
+    if (b < batch) s = load(b);
+    const int n = levels ? blocks_from(s.blocks, m0) - blocks_from(s.blocks, m1) : s.blocks.count;
+    const int upto = cur.before + lanes.scan(n);
+    const int src = lanes.first(left < upto);
+    if (src >= 0) {
+      seq_out = {lanes.get(s.row0, src), lanes.get(s.tokens, src), lanes.get(s.ctx, src),
+                 {lanes.get(s.blocks.first, src), lanes.get(s.blocks.count, src)}};
+      const int behind = left - (lanes.get(upto, src) - lanes.get(n, src));   // blocks of its own before u
+      const int end = seq_out.blocks.first + seq_out.blocks.count;
+      b_out = cur.b0 + src;
+      i_out = (end < m1 ? end : m1) - 1 - seq_out.blocks.first - behind;
       return true;
     }
-    left -= n;
+    cur.before = lanes.get(upto, lanes.count() - 1);
   }
   return false;
 }
@@ -87,9 +110,9 @@ struct OneLane {
   PTD_HD int id() const { return 0; }
   PTD_HD int count() const { return 1; }
   PTD_HD int sum(int x) const { return x; }
-  PTD_HD uint32_t ballot(bool p) const { return p ? 1u : 0u; }
-  PTD_HD int popcount(uint32_t x) const { return (int)x; }
-  PTD_HD int nth(uint32_t, int) const { return 0; }
+  PTD_HD int scan(int x) const { return x; }
+  PTD_HD int first(bool p) const { return p ? 0 : -1; }
+  PTD_HD int get(int x, int) const { return x; }
 };
 
 #ifdef __CUDACC__
@@ -97,9 +120,16 @@ struct WarpLanes {
   __device__ __forceinline__ int id() const { return threadIdx.x & 31; }
   __device__ __forceinline__ int count() const { return 32; }
   __device__ __forceinline__ int sum(int x) const { return (int)__reduce_add_sync(0xffffffffu, (unsigned)x); }
-  __device__ __forceinline__ uint32_t ballot(bool p) const { return __ballot_sync(0xffffffffu, p); }
-  __device__ __forceinline__ int popcount(uint32_t x) const { return __popc(x); }
-  __device__ __forceinline__ int nth(uint32_t x, int k) const { return __fns(x, 0, k + 1); }
+  __device__ __forceinline__ int scan(int x) const {   // inclusive
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (id() >= o) x += y;
+    }
+    return x;
+  }
+  __device__ __forceinline__ int first(bool p) const { return __ffs(__ballot_sync(0xffffffffu, p)) - 1; }
+  __device__ __forceinline__ int get(int x, int lane) const { return __shfl_sync(0xffffffffu, x, lane); }
 };
 #endif
 

@@ -15,27 +15,38 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SOURCE = r"""
 #include <cstdio>
 #include "prompt_geometry.cuh"
-// stdin: width batch, then (ctx, tokens) per sequence; prints every block in order, and whether the first
-// number past them is refused.
+// stdin: width batch max_ctx max_tokens, then (ctx, tokens) per sequence; prints every block in order (found from
+// the start, and from where the one before was found), and whether the first number past them is refused.
 int main() {
-  int width, batch;
-  while (std::scanf("%d %d", &width, &batch) == 2) {
+  int width, batch, max_ctx, max_tokens;
+  while (std::scanf("%d %d %d %d", &width, &batch, &max_ctx, &max_tokens) == 4) {
     static int ctx[4096], n[4096];
-    int max_key = 0, total = 0;
+    int total = 0;
     for (int b = 0; b < batch; ++b) {
       if (std::scanf("%d %d", ctx + b, n + b) != 2) return 1;
-      const ptd::PromptBlocks s = ptd::prompt_blocks(ctx[b], n[b], width);
-      if (s.first + s.count > max_key) max_key = s.first + s.count;
-      total += s.count;
+      total += ptd::prompt_blocks(ctx[b], n[b], width).count;
     }
-    auto seq = [&](int b) { return ptd::prompt_blocks(ctx[b], n[b], width); };
-    int b, i;
-    for (int u = 0; u < total; ++u) {
-      if (!ptd::find_prompt_block(ptd::OneLane{}, seq, batch, max_key, u, &b, &i)) return 1;
+    auto load = [&](int b) { return ptd::PromptSequence{7 * b, n[b], ctx[b], ptd::prompt_blocks(ctx[b], n[b], width)}; };
+    const int step = ptd::prompt_level_step(max_ctx, max_tokens, width);
+    ptd::PromptCursor on = {0, 0, 0};
+    ptd::PromptSequence s;
+    int b, i, b2, i2;
+    for (int u = 0; u <= total; ++u) {
+      ptd::PromptCursor fresh = {0, 0, 0};
+      const bool found = ptd::find_prompt_block(ptd::OneLane{}, load, batch, step, u, fresh, b, i, s);
+      if (found != (u < total)) return 1;
+      if (u % 3 == 1 && u < total) continue;   // (a CTA does not get every number)
+      if (ptd::find_prompt_block(ptd::OneLane{}, load, batch, step, u, on, b2, i2, s) != found) return 1;
+      if (found && (b2 != b || i2 != i || s.row0 != 7 * b || s.tokens != n[b] || s.ctx != ctx[b])) return 1;
+      if (found) std::printf("%d,%d ", b, i);
+    }
+    for (int u = 1; u < total; u += 3) {
+      ptd::PromptCursor fresh = {0, 0, 0};
+      if (!ptd::find_prompt_block(ptd::OneLane{}, load, batch, step, u, fresh, b, i, s)) return 1;
       std::printf("%d,%d ", b, i);
     }
-    std::printf("%d\n", ptd::find_prompt_block(ptd::OneLane{}, seq, batch, max_key, total, &b, &i) ||
-                            ptd::find_prompt_block(ptd::OneLane{}, seq, batch, max_key, -1, &b, &i));
+    ptd::PromptCursor fresh = {0, 0, 0};
+    std::printf("%d\n", ptd::find_prompt_block(ptd::OneLane{}, load, batch, step, -1, fresh, b, i, s));
   }
   return 0;
 }
@@ -54,7 +65,8 @@ def lib():
 def test_blocks_are_numbered_longest_first(tmp_path):
     rng = random.Random(5)
     cases = [(64, [(0, 0)]), (64, [(5, 1)]), (64, [(100, 640)]), (1, [(3, 4), (0, 9), (5, 0), (2, 2)]),
-             (256, [(0, 0), (0, 0)])]
+             (256, [(0, 0), (0, 0)]), (2, [(rng.randrange(4000), 1) for _ in range(128)]),
+             (2, [(rng.randrange(4000), rng.randrange(3)) for _ in range(129)])]
     for _ in range(60):
         seqs = [(rng.choice([0, rng.randrange(5000)]), rng.choice([0, 1, rng.randrange(3000)]))
                 for _ in range(rng.randrange(1, 70))]
@@ -63,12 +75,18 @@ def test_blocks_are_numbered_longest_first(tmp_path):
     src.write_text(SOURCE)
     subprocess.run(["g++", "-O2", "-std=c++17", "-I", os.path.join(ROOT, "paper_2607_10661_gb300", "csrc"), str(src),
                     "-o", str(exe)], check=True)
-    text = "\n".join(f"{w} {len(s)} " + " ".join(f"{c} {n}" for c, n in s) for w, s in cases)
+    bounds = [(max(c for c, _ in s) + rng.choice([0, 700]), max(1, max(n for _, n in s))) for _, s in cases]
+    text = "\n".join(f"{w} {len(s)} {mc} {mn} " + " ".join(f"{c} {n}" for c, n in s)
+                     for (w, s), (mc, mn) in zip(cases, bounds))
     r = subprocess.run([str(exe)], input=text, capture_output=True, text=True)
     assert r.returncode == 0
-    for (width, seqs), line in zip(cases, r.stdout.strip("\n").split("\n")):
-        blocks = [(-(c // width + i), b, i) for b, (c, n) in enumerate(seqs) for i in range(-(-n // width))]
-        want = [f"{b},{i}" for _, b, i in sorted(blocks)] + ["0"]
+    for (width, seqs), (mc, mn), line in zip(cases, bounds, r.stdout.strip("\n").split("\n")):
+        step = (mc // width + mn // width + 2) // 32 + 1
+        level = lambda c, i: (c // width + i) // step if 1 < len(seqs) <= 128 else 0
+        blocks = sorted((-level(c, i), b, -i) for b, (c, n) in enumerate(seqs) for i in range(-(-n // width)))
+        assert all(-l < 32 for l, _, _ in blocks)
+        order = [f"{b},{-i}" for _, b, i in blocks]
+        want = [x for u, x in enumerate(order) if u % 3 != 1] + order[1::3] + ["0"]
         assert line.split() == want, (width, seqs)
 
 
