@@ -71,6 +71,7 @@ struct PromptAttnParams {
   int tile_rows;               // rows of an M tile in the partials
   int key_tile, key_tile_log2; // keys per tile
   int level_step;              // of the blocks' order (prompt_geometry.cuh)
+  IndexDivisor by_block, by_heads, by_kv, by_splits, by_sub;   // block_tokens, tile_heads, tiles_per_kv, splits, sub
   int blocks;                  // upper bound of the batch's blocks of tokens (per head tile)
   int splits;                  // pieces that a block's keys are cut into
   int page_size, seq_capacity, num_pages, max_pages;

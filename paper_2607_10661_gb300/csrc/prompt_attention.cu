@@ -110,6 +110,10 @@ size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int
   p.tiles_per_kv = group / p.sub;
   p.tile_tokens = tile_rows / p.sub;
   p.block_tokens = tiles * p.tile_tokens;
+  p.by_block = index_divisor(p.block_tokens);
+  p.by_heads = index_divisor(p.tile_heads);
+  p.by_kv = index_divisor(p.tiles_per_kv);
+  p.by_sub = index_divisor(p.sub);
   p.level_step = prompt_level_step(p.bounds.max_ctx, p.bounds.max_tokens, p.block_tokens);
   const int64_t w = p.block_tokens, N = p.bounds.n_total, B = p.batch;
   const int64_t by_total = N / w + B, by_longest = B * ((p.bounds.max_tokens + w - 1) / w);
@@ -123,8 +127,10 @@ size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int
   const size_t bytes = p.splits == 1 ? 0 : (size_t)units * p.splits * tiles * tile_rows * (p.head_dim + 2) * sizeof(float);
   if (bytes > scratch) {
     p.splits = 1;
+    p.by_splits = index_divisor(1);
     return 0;
   }
+  p.by_splits = index_divisor(p.splits);
   if (bytes > 0) p.part_ml = p.part_o + (size_t)units * p.splits * tiles * tile_rows * p.head_dim;
   return bytes;
 }

@@ -43,17 +43,12 @@ __global__ void __launch_bounds__(kThreads) prompt_simt_kernel(const PromptAttnP
   const int t = threadIdx.x, x = t & 15, y = t >> 4;
   if (t == 0) grid_launch_dependents();
   grid_dependency_wait();
-  const int split = blockIdx.x % p.splits;
+  const int block = divide((int)blockIdx.x, p.by_splits), split = (int)blockIdx.x - block * p.splits;
   if (t < 32) {
-    if (blockIdx.x == 0) {   // malformed sequences are reported here, and have no blocks
-      bool bad = false;
-      for (int b = t; b < p.batch; b += 32)
-        bad = bad || !prompt_sequence_ok(p.bounds, p.token_offsets[b], p.token_offsets[b + 1], p.ctx_lens[b]);
-      if (bad) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
-    }
     Units units(p);
+    if (units.bad) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
     Unit u;
-    bool found = units.find(p, blockIdx.x / p.splits, u);
+    bool found = units.find(p, block, u);
     if (found) {
       piece_range(u.tiles, split, p.splits, u.tile0, u.tile1);
       found = u.tile1 > u.tile0;

@@ -10,7 +10,7 @@
 // even out whatever the lengths, and a unit's first loads and its set-up run beside the unit before it.
 //
 // Warps (384 threads; the first four give registers to the others):
-//   0       scheduler and TMA producer: claims the next unit when the last tiles of this one are asked for;
+//   0       scheduler and TMA producer: claims the next unit before the last tiles of this one are asked for;
 //           K and V tiles into a ring of five, Q.
 //   1, 2    MMA issuers of M tile 0 and 1: S_t = Q_t K^T, then PV_t, S_t' | PV_t', S_t'' | .., in turns, so that
 //           one M tile's softmax runs beside the other's products.  Products go out at the tensor core's pace:
@@ -41,9 +41,9 @@ using tc::kTileBytes;
 constexpr int kThreads = 384;
 constexpr int kTiles = 5;    // of the ring of K and V tiles
 constexpr int kSteps = 8;    // barriers for steps whose tiles have been read: more than steps that tiles are held for
-// Registers a thread: 168 at launch (384 threads), then 96 for warps 0 - 3 and 200 for the softmax warps,
-// which hold a row's 128 scores: 128 * 96 + 256 * 200 <= 384 * 168.
-constexpr int kRegsLaunch = 168, kRegsFew = 96, kRegsMany = 200;
+// Registers a thread: 168 at launch (384 threads), then 104 for warps 0 - 3 and 200 for the softmax warps,
+// which hold a row's 128 scores: 128 * 104 + 256 * 200 = 384 * 168.
+constexpr int kRegsLaunch = 168, kRegsFew = 104, kRegsMany = 200;
 static_assert(128 * kRegsFew + 256 * kRegsMany <= kThreads * kRegsLaunch, "register split");
 constexpr uint32_t kOffQ = 0;
 constexpr uint32_t kOffRing = 2 * kTileBytes;
@@ -212,6 +212,22 @@ __device__ __forceinline__ void issue_pv(uint32_t leader, uint32_t s_tmem, uint3
               (acc || kk > 0) ? 1u : 0u);
 }
 constexpr int kEarly = 5;   // products of a group of eight before the other issuer is let go
+
+// 64 bytes of a row.  A warp's rows lie apart, so a store costs a pass a row whatever its width: 32 bytes at a
+// time where the output allows.
+__device__ __forceinline__ void store_row(uint4* dst, const uint32_t (&w)[16], bool wide) {
+  if (wide) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + 2 * g), "r"(w[8 * g]),
+                   "r"(w[8 * g + 1]), "r"(w[8 * g + 2]), "r"(w[8 * g + 3]), "r"(w[8 * g + 4]), "r"(w[8 * g + 5]),
+                   "r"(w[8 * g + 6]), "r"(w[8 * g + 7])
+                   : "memory");
+  } else {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) dst[g] = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
+  }
+}
 
 // Bit 15 of either half: the bf16 there is an infinity or NaN.
 __device__ __forceinline__ uint32_t exponent_full(uint32_t w) { return (w & 0x7F807F80u) + 0x00800080u; }
@@ -397,10 +413,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         return true;
       };
       pa::Units units(p);
-      bool bad = false;
-      for (int b = lane; b < p.batch; b += 32)
-        bad = bad || !prompt_sequence_ok(p.bounds, p.token_offsets[b], p.token_offsets[b + 1], p.ctx_lens[b]);
-      if (bad) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
+      if (units.bad) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
       __syncwarp();
       int x = (int)blockIdx.x, claims = 0;   // the unit's number; claims made
       bool claimed = false;                  // the last one has not been read yet
@@ -412,111 +425,125 @@ __global__ void __launch_bounds__(kThreads, 1)
         claimed = true;
         ++claims;
       };
-      for (int it = 0; ok; ++it) {
-        if (!wait_warp(bar(kSegEmpty + (it & 1)), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, p.dev_status)) break;
-        Unit u;
-        bool found = false;
-        for (bool first = it == 0; !found; first = false) {   // until a unit with keys, or the end of the grid
-          if (!first) {
-            if (!claimed) claim();
-            if (!(ok = wait_warp(bar(kClaim), (uint32_t)(claims - 1) & 1u, abort_flag, p.dev_status))) break;
-            claimed = false;
-            x = claimed_cta(base + kOffClaim);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (x < 0) break;
-          }
-          const int y = (int)((unsigned)x / (unsigned)p.splits);
-          if (units.find(p, y, u)) {
-            if (p.splits > 1) pa::piece_range(u.tiles, x - y * p.splits, p.splits, u.tile0, u.tile1);
-            found = u.tile1 > u.tile0;
-          }
-        }
-        if (!ok) break;
-        const int b = u.b, kv = u.kv, kt0 = u.tile0, head0 = u.head0, row0 = u.row0;
-        const int edge = (u.ctx + u.token0 + 1) / 128;
-        // M tile 0's last token may see fewer tiles than the block's
-        const int tiles0 = (u.ctx + u.token0 + min(u.tokens, p.tile_tokens) + 127) / 128;
-        const int nq[2] = {max(0, min(tiles0, u.tile1) - kt0), u.tokens > p.tile_tokens ? u.tile1 - kt0 : 0};
-        const int n = max(nq[0], nq[1]);
-        if (lane == 0) {
-          Seg s = {};
-          s.valid = found;
-          if (found) {
-            s.b = b;
-            s.row0 = row0;
-            s.ctx = u.ctx;
-            s.token0 = u.token0;
-            s.tokens = u.tokens;
-            s.head0 = head0;
-            s.kv = kv;
-            s.piece = x;
-            s.kt0 = kt0;
-            s.edge = edge;
-            s.n[0] = nq[0];
-            s.n[1] = nq[1];
-          }
-          segs[it & 1] = s;
-          mbar_arrive(bar(kSegFull + (it & 1)));
-        }
+      // The walk: steps of a unit (V of tile j and K of tile j + 1, j = -1 .. n - 1), and before its last ones
+      // the claim and the search of the next, so that its first copies follow at once.
+      Unit u;                      // the next unit, once it is known
+      bool search = true, found = false;
+      int it = 0, j = 0, n = 0, search_at = 0, b = 0, kv = 0, kt0 = 0, edge = 0, head0 = 0, row0 = 0, end_page = 0;
+      int nq[2] = {0, 0}, next_page = -1, row_v = 0;
+      const int* bt = nullptr;
+      // this lane's page of key tile i (read a step ahead, so that no copy waits for it)
+      auto page_of = [&](int i) {
+        const int g = (kt0 + i) * per_tile + page_at;
+        return kPaged && i < n && page_at < per_tile && g < end_page ? bt[g] : -1;
+      };
+      auto pages_in = [&](int i) { return kPaged ? min(per_tile, end_page - (kt0 + i) * per_tile) : 1; };
+      // first row of this lane's copy of tile i
+      auto row_of = [&](int i, int page) {
+        if (!kPaged) return (p.layer * p.batch + b) * p.seq_capacity + (kt0 + i) * 128;
+        const bool there = page >= 0 && page < p.num_pages;
+        if (!there && page_at < pages_in(i)) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
+        return there ? (p.layer * p.num_pages + page) * p.page_size : -128;   // (-128: TMA fills zeros)
+      };
+      auto copy = [&](const CUtensorMap* map, bool check, int i, int row) {   // tile i into the next ring place
+        const uint32_t full = bar((check ? kLoadV : kFull) + at);
+        if (lane == 0)
+          mbar_arrive_expect_tx(full, kPaged ? (uint32_t)(pages_in(i) * p.page_size) * 256u : kTileBytes);
         __syncwarp();
-        if (!found) break;
-        const int end_page = kPaged ? (u.ctx + u.token0 + u.tokens + p.page_size - 1) >> page_log2 : 0;
-        const int* bt = kPaged ? p.block_table + (size_t)b * p.max_pages : nullptr;
-        // this lane's page of key tile j (read a step ahead, so that no copy waits for it)
-        auto page_of = [&](int j) {
-          const int g = (kt0 + j) * per_tile + page_at;
-          return kPaged && j < n && page_at < per_tile && g < end_page ? bt[g] : -1;
-        };
-        auto pages_in = [&](int j) { return kPaged ? min(per_tile, end_page - (kt0 + j) * per_tile) : 1; };
-        // first row of this lane's copy of tile j
-        auto row_of = [&](int j, int page) {
-          if (!kPaged) return (p.layer * p.batch + b) * p.seq_capacity + (kt0 + j) * 128;
-          const bool there = page >= 0 && page < p.num_pages;
-          if (!there && page_at < pages_in(j)) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
-          return there ? (p.layer * p.num_pages + page) * p.page_size : -128;   // (-128: TMA fills zeros)
-        };
-        auto copy = [&](const CUtensorMap* map, bool check, int j, int row) {   // tile j into the next ring place
-          const uint32_t full = bar((check ? kLoadV : kFull) + at);
-          if (lane == 0)
-            mbar_arrive_expect_tx(full, kPaged ? (uint32_t)(pages_in(j) * p.page_size) * 256u : kTileBytes);
-          __syncwarp();
-          if (page_at < pages_in(j))
-            tma_load_3d(base + kOffRing + (uint32_t)at * kTileBytes + copy_at, map, full, half * 64, kv, row);
-          if (lane == at) step_of = steps;
-          armed ^= 1u << at;
-          if (check) checked ^= 1u << at;
-          if (++at == kTiles) at = 0;
-        };
-        int next_page = page_of(0), row_v = 0;
-        for (int j = -1; j < n && ok; ++j, ++steps) {   // V of tile j and K of tile j + 1
-          const int row_k = j + 1 < n ? row_of(j + 1, next_page) : 0;
-          next_page = page_of(j + 2);
-          if (j == n - 1) claim();
-          if (j >= 0) {
-            if (!(ok = place())) break;
-            copy(&map_v, kt0 + j >= edge, j, row_v);
-          }
-          if (j + 1 < n) {
-            if (!(ok = place())) break;
-            copy(&map_k, false, j + 1, row_k);
-          }
-          row_v = row_k;
-          if (j == -1) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-              if (!ok || nq[t] == 0 ||
-                  !(ok = wait_warp(bar(kQEmpty + t), ((uint32_t)qc[t] & 1u) ^ 1u, abort_flag, p.dev_status)))
-                continue;
-              ++qc[t];
-              if (lane == 0) mbar_arrive_expect_tx(bar(kQFull + t), (uint32_t)used * 256u);
+        if (page_at < pages_in(i))
+          tma_load_3d(base + kOffRing + (uint32_t)at * kTileBytes + copy_at, map, full, half * 64, kv, row);
+        if (lane == at) step_of = steps;
+        armed ^= 1u << at;
+        if (check) checked ^= 1u << at;
+        if (++at == kTiles) at = 0;
+      };
+      while (ok) {
+        if (search) {   // a unit with keys, or the end of the grid
+          search = found = false;
+          for (bool first = claims == 0 && it == 0; !found; first = false) {
+            if (!first) {
+              if (!claimed) claim();
+              if (!(ok = wait_warp(bar(kClaim), (uint32_t)(claims - 1) & 1u, abort_flag, p.dev_status))) break;
+              claimed = false;
+              x = claimed_cta(base + kOffClaim);
+              fence_proxy_async_smem();
               __syncwarp();
-              if (lane < 2)
-                tma_load_3d(base + kOffQ + (uint32_t)t * kTileBytes + (uint32_t)half * kHalfBytes, &map_q, bar(kQFull + t),
-                            half * 64, head0, row0 + t * p.tile_tokens);
+              if (x < 0) break;
+            }
+            const int y = divide(x, p.by_splits);
+            if (units.find(p, y, u)) {
+              if (p.splits > 1) pa::piece_range(u.tiles, x - y * p.splits, p.splits, u.tile0, u.tile1);
+              found = u.tile1 > u.tile0;
             }
           }
+          if (!ok) break;
         }
+        if (j == n) {   // the unit's tiles are all asked for
+          if (!(ok = wait_warp(bar(kSegEmpty + (it & 1)), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, p.dev_status))) break;
+          b = u.b, kv = u.kv, kt0 = u.tile0, head0 = u.head0, row0 = u.row0;
+          edge = (u.ctx + u.token0 + 1) / 128;
+          // M tile 0's last token may see fewer tiles than the block's
+          const int tiles0 = (u.ctx + u.token0 + min(u.tokens, p.tile_tokens) + 127) / 128;
+          nq[0] = max(0, min(tiles0, u.tile1) - kt0), nq[1] = u.tokens > p.tile_tokens ? u.tile1 - kt0 : 0;
+          n = max(nq[0], nq[1]);
+          if (lane == 0) {
+            Seg s = {};
+            s.valid = found;
+            if (found) {
+              s.b = b;
+              s.row0 = row0;
+              s.ctx = u.ctx;
+              s.token0 = u.token0;
+              s.tokens = u.tokens;
+              s.head0 = head0;
+              s.kv = kv;
+              s.piece = x;
+              s.kt0 = kt0;
+              s.edge = edge;
+              s.n[0] = nq[0];
+              s.n[1] = nq[1];
+            }
+            segs[it & 1] = s;
+            mbar_arrive(bar(kSegFull + (it & 1)));
+          }
+          __syncwarp();
+          if (!found) break;
+          ++it;
+          j = -1;
+          search_at = n > 2 ? n - 2 : n - 1;
+          end_page = kPaged ? (u.ctx + u.token0 + u.tokens + p.page_size - 1) >> page_log2 : 0;
+          bt = kPaged ? p.block_table + (size_t)b * p.max_pages : nullptr;
+          next_page = page_of(0);
+        }
+        const int row_k = j + 1 < n ? row_of(j + 1, next_page) : 0;
+        next_page = page_of(j + 2);
+        if (j >= 0) {
+          if (!(ok = place())) break;
+          copy(&map_v, kt0 + j >= edge, j, row_v);
+        }
+        if (j + 1 < n) {
+          if (!(ok = place())) break;
+          copy(&map_k, false, j + 1, row_k);
+        }
+        row_v = row_k;
+        if (j == -1) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (!ok || nq[t] == 0 ||
+                !(ok = wait_warp(bar(kQEmpty + t), ((uint32_t)qc[t] & 1u) ^ 1u, abort_flag, p.dev_status)))
+              continue;
+            ++qc[t];
+            if (lane == 0) mbar_arrive_expect_tx(bar(kQFull + t), (uint32_t)used * 256u);
+            __syncwarp();
+            if (lane < 2)
+              tma_load_3d(base + kOffQ + (uint32_t)t * kTileBytes + (uint32_t)half * kHalfBytes, &map_q, bar(kQFull + t),
+                          half * 64, head0, row0 + t * p.tile_tokens);
+          }
+        }
+        if (j == search_at - 1) claim();
+        search = j == search_at;
+        ++steps;
+        ++j;
       }
       if (lane == 0 && *abort_flag) {
         // drain the copies already issued (bounded) before the CTA can exit
@@ -578,7 +605,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int row = (warp & 3) * 32 + lane;   // = TMEM lane this warp may access
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + lane_base + (uint32_t)t * 128u, tO = tS + 256u;
-    const int my_token = t * p.tile_tokens + row / p.sub, my_head = row % p.sub;
+    const int my_token = t * p.tile_tokens + divide(row, p.by_sub), my_head = row - divide(row, p.by_sub) * p.sub;
     const bool in_tile = row < used;
     int tiles = 0, outs = 0;
     for (int it = 0;; ++it) {
@@ -611,6 +638,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool bad = sg->bad != 0;
       const float inv = p.splits == 1 ? 1.f / l_run : 1.f;   // a piece stays unnormalised
       uint4* dst = reinterpret_cast<uint4*>(p.out) + (((size_t)sg->row0 + my_token) * p.hq + sg->head0 + my_head) * 16;
+      const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0;
       float4* po = reinterpret_cast<float4*>(p.part_o) + (size_t)sg->piece * 32 * 256 + t * 128 + row;
       if (p.splits > 1 && row_valid)
         reinterpret_cast<float2*>(p.part_ml)[(size_t)sg->piece * 256 + t * 128 + row] =
@@ -634,10 +662,10 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int e = 0; e < 32; ++e) o[e] = ob[e];
             }
             if (p.splits == 1) {
+              uint32_t w[16];
 #pragma unroll
-              for (int g = 0; g < 4; ++g)
-                dst[c * 4 + g] = make_uint4(pack_bf16x2(o[8 * g], o[8 * g + 1]), pack_bf16x2(o[8 * g + 2], o[8 * g + 3]),
-                                            pack_bf16x2(o[8 * g + 4], o[8 * g + 5]), pack_bf16x2(o[8 * g + 6], o[8 * g + 7]));
+              for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(o[2 * e], o[2 * e + 1]);
+              store_row(dst + c * 4, w, wide);
             } else {
 #pragma unroll
               for (int g = 0; g < 8; ++g)

@@ -4,6 +4,8 @@
 
 #include <cstdint>
 
+#include "row_division.cuh"
+
 #ifdef __CUDACC__
 #define PTD_HD __host__ __device__ __forceinline__
 #else
@@ -31,7 +33,9 @@ PTD_HD int pages_for(int64_t len, int page_size) { return (int)((len + page_size
 struct PromptBlocks {
   int first, count;
 };
-PTD_HD PromptBlocks prompt_blocks(int ctx, int tokens, int width) { return {ctx / width, (tokens + width - 1) / width}; }
+PTD_HD PromptBlocks prompt_blocks(int ctx, int tokens, int width, IndexDivisor by_width) {
+  return {divide(ctx, by_width), divide(tokens + width - 1, by_width)};
+}
 
 // Blocks of one sequence with key >= m.
 PTD_HD int blocks_from(const PromptBlocks& s, int m) {
@@ -53,37 +57,36 @@ constexpr int kLevels = 32;
 constexpr int kOrderedBatch = 128;
 PTD_HD int prompt_level_step(int max_ctx, int max_tokens, int width) { return (max_ctx / width + max_tokens / width + 2) / kLevels + 1; }
 
-// Where the last search ended: a search for a later block of the same level goes on from there.
+PTD_HD bool prompt_has_levels(int batch) { return batch > 1 && batch <= kOrderedBatch; }
+
+// Where the last search ended: a search for a later block goes on from there.
 struct PromptCursor {
-  int level, b0, before;   // blocks of the level in the sequences below b0
+  int level, upto, above;   // a level, the blocks of it and higher ones, and of higher ones (upto 0: none known)
+  int b0, before;           // a sequence, and the blocks of the level in the sequences before it
 };
 
 // Block number u: its sequence b, that sequence, and the block's place in it.  `lanes` walks the sequences: one
 // lane on the host, a warp's 32 on the device, where every lane gets the answer; load(b) gives sequence b and
-// is called with b = lane modulo their number.  False: there is no such block.
-template <typename Lanes, typename Load>
-PTD_HD bool find_prompt_block(const Lanes& lanes, const Load& load, int batch, int level_step, int u, PromptCursor& cur,
-                              int& b_out, int& i_out, PromptSequence& seq_out) {
+// is called with b = lane modulo their number; level_of(u, upto, above) gives u's level, the blocks of it and
+// higher levels (upto > u where there is such a block) and of higher ones.  False: there is no such block.
+template <typename Lanes, typename Load, typename LevelOf>
+PTD_HD bool find_prompt_block(const Lanes& lanes, const Load& load, const LevelOf& level_of, int batch, int level_step, int u,
+                              PromptCursor& cur, int& b_out, int& i_out, PromptSequence& seq_out) {
   if (u < 0) return false;
-  int level = 0, above = 0;   // u's level, and the blocks of higher ones
-  const bool levels = batch > 1 && batch <= kOrderedBatch;
-  if (levels) {
-    auto from = [&](int l) {   // blocks of level l and higher
-      int c = 0;
-#pragma unroll 1
-      for (int b = lanes.id(); b < batch; b += lanes.count()) c += blocks_from(load(b).blocks, l * level_step);
-      return lanes.sum(c);
-    };
-    int hi = kLevels;          // from(level) > u >= above = from(hi), where there is such a block
-#pragma unroll 1
-    while (hi - level > 1) {
-      const int mid = (level + hi) >> 1, c = from(mid);
-      if (c > u) level = mid; else hi = mid, above = c;
-    }
+  if (batch == 1) {
+    seq_out = load(0);
+    b_out = 0;
+    i_out = seq_out.blocks.count - 1 - u;
+    return i_out >= 0;
   }
+  const bool levels = prompt_has_levels(batch);
+  if (levels && (u >= cur.upto || u < cur.above)) {
+    cur.b0 = cur.before = 0;
+    cur.level = level_of(u, cur.upto, cur.above);
+  }
+  const int level = cur.level, left = u - cur.above;
+  if (cur.before > left) cur.b0 = cur.before = 0;
   const int m0 = level * level_step, m1 = levels && level + 1 < kLevels ? m0 + level_step : INT32_MAX;
-  const int left = u - above;
-  if (cur.level != level || cur.before > left) cur = {level, 0, 0};
 #pragma unroll 1
   for (; cur.b0 < batch; cur.b0 += lanes.count()) {
     const int b = cur.b0 + lanes.id();

@@ -35,4 +35,28 @@ PTD_HOST_DEVICE int divide_by_group(int m, GroupDivisor d) {
 #endif
 }
 
+// n / d for every 0 <= n < 2^31 and d >= 1: with 2^s the least power of two >= d and mul = ceil(2^(31 + s) / d) =
+// (2^(31 + s) + e) / d, 0 <= e < d <= 2^s, n e < 2^(31 + s), so floor(n mul / 2^(31 + s)) is exact; mul fits in
+// 32 bits as d > 2^(s - 1).  mul 0: d = 1.
+struct IndexDivisor {
+  uint32_t mul;
+  uint32_t shift;   // s - 1
+};
+
+inline IndexDivisor index_divisor(int d) {
+  if (d <= 1) return {0u, 0u};
+  uint32_t s = 1;
+  while ((1ll << s) < d) ++s;
+  return {(uint32_t)(((1ull << (31 + s)) + (unsigned)d - 1) / (unsigned)d), s - 1};
+}
+
+PTD_HOST_DEVICE int divide(int n, IndexDivisor d) {
+  if (d.mul == 0u) return n;
+#ifdef __CUDA_ARCH__
+  return (int)(__umulhi((uint32_t)n, d.mul) >> d.shift);
+#else
+  return (int)((((uint64_t)(uint32_t)n * d.mul) >> 32) >> d.shift);
+#endif
+}
+
 }  // namespace ptd

@@ -24,29 +24,40 @@ int main() {
     int total = 0;
     for (int b = 0; b < batch; ++b) {
       if (std::scanf("%d %d", ctx + b, n + b) != 2) return 1;
-      total += ptd::prompt_blocks(ctx[b], n[b], width).count;
+      total += ptd::prompt_blocks(ctx[b], n[b], width, ptd::index_divisor(width)).count;
     }
-    auto load = [&](int b) { return ptd::PromptSequence{7 * b, n[b], ctx[b], ptd::prompt_blocks(ctx[b], n[b], width)}; };
+    auto load = [&](int b) { return ptd::PromptSequence{7 * b, n[b], ctx[b], ptd::prompt_blocks(ctx[b], n[b], width, ptd::index_divisor(width))}; };
     const int step = ptd::prompt_level_step(max_ctx, max_tokens, width);
-    ptd::PromptCursor on = {0, 0, 0};
+    auto from = [&](int level) {
+      int c = 0;
+      for (int b = 0; b < batch; ++b) c += ptd::blocks_from(load(b).blocks, level * step);
+      return c;
+    };
+    auto level_of = [&](int u, int& upto, int& above) {
+      int level = 31;
+      while (level > 0 && from(level) <= u) --level;
+      upto = from(level), above = level < 31 ? from(level + 1) : 0;
+      return level;
+    };
+    ptd::PromptCursor on = {0, 0, 0, 0, 0};
     ptd::PromptSequence s;
     int b, i, b2, i2;
     for (int u = 0; u <= total; ++u) {
-      ptd::PromptCursor fresh = {0, 0, 0};
-      const bool found = ptd::find_prompt_block(ptd::OneLane{}, load, batch, step, u, fresh, b, i, s);
+      ptd::PromptCursor fresh = {0, 0, 0, 0, 0};
+      const bool found = ptd::find_prompt_block(ptd::OneLane{}, load, level_of, batch, step, u, fresh, b, i, s);
       if (found != (u < total)) return 1;
       if (u % 3 == 1 && u < total) continue;   // (a CTA does not get every number)
-      if (ptd::find_prompt_block(ptd::OneLane{}, load, batch, step, u, on, b2, i2, s) != found) return 1;
+      if (ptd::find_prompt_block(ptd::OneLane{}, load, level_of, batch, step, u, on, b2, i2, s) != found) return 1;
       if (found && (b2 != b || i2 != i || s.row0 != 7 * b || s.tokens != n[b] || s.ctx != ctx[b])) return 1;
       if (found) std::printf("%d,%d ", b, i);
     }
     for (int u = 1; u < total; u += 3) {
-      ptd::PromptCursor fresh = {0, 0, 0};
-      if (!ptd::find_prompt_block(ptd::OneLane{}, load, batch, step, u, fresh, b, i, s)) return 1;
+      ptd::PromptCursor fresh = {0, 0, 0, 0, 0};
+      if (!ptd::find_prompt_block(ptd::OneLane{}, load, level_of, batch, step, u, fresh, b, i, s)) return 1;
       std::printf("%d,%d ", b, i);
     }
-    ptd::PromptCursor fresh = {0, 0, 0};
-    std::printf("%d\n", ptd::find_prompt_block(ptd::OneLane{}, load, batch, step, -1, fresh, b, i, s));
+    ptd::PromptCursor fresh = {0, 0, 0, 0, 0};
+    std::printf("%d\n", ptd::find_prompt_block(ptd::OneLane{}, load, level_of, batch, step, -1, fresh, b, i, s));
   }
   return 0;
 }
@@ -88,6 +99,31 @@ def test_blocks_are_numbered_longest_first(tmp_path):
         order = [f"{b},{-i}" for _, b, i in blocks]
         want = [x for u, x in enumerate(order) if u % 3 != 1] + order[1::3] + ["0"]
         assert line.split() == want, (width, seqs)
+
+
+def test_index_division_is_exact(tmp_path):
+    src, exe = tmp_path / "divide.cpp", tmp_path / "divide"
+    src.write_text(r"""
+#include <cstdio>
+#include "row_division.cuh"
+int main() {
+  for (int64_t d = 1; d < (1ll << 31); d += d < 5000 ? 1 : d / 97 + 1) {
+    const ptd::IndexDivisor x = ptd::index_divisor((int)d);
+    const int64_t top = (1ll << 31) - 1;
+    const int64_t qs[] = {0, 1, 2, 1000, 65535, top / d - 1, top / d};
+    for (int64_t q : qs) {
+      const int64_t ns[] = {q * d - 1, q * d, q * d + d / 2, q * d + d - 1, top};
+      for (int64_t n : ns)
+        if (n >= 0 && n <= top && ptd::divide((int)n, x) != n / d) return std::printf("%ld / %ld\n", (long)n, (long)d), 1;
+    }
+  }
+  return 0;
+}
+""")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I", os.path.join(ROOT, "paper_2607_10661_gb300", "csrc"), str(src),
+                    "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout
 
 
 def test_sequences_out_of_bounds(tmp_path):
