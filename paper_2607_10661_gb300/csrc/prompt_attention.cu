@@ -13,43 +13,43 @@ namespace ptd {
 namespace pa {
 
 constexpr int kMergeThreads = 256;
-constexpr int kMergeBatch = 4;   // pieces whose partials are in flight at a time
+constexpr int kMergeBatch = 8;   // pieces whose partials are in flight at a time
 
 // The rows of one split block, from its pieces: O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s, M the
-// maximum of the m_s (a row that saw no key of a piece has l_s = 0, and its O_s was not written).  Block x of the
-// grid is a (block, head tile), y a share of its rows and columns: a thread takes one row and four columns,
-// consecutive threads consecutive rows, as the partials lie.  Bound by the latency of the chain unit, (m, l),
-// partials; the unit is found while the attention still runs.
+// maximum of the m_s (a row that saw no key of a piece has l_s = 0, and its O_s was not written).  x of the grid is
+// a block's place and head tile, y a share of its rows and columns: a thread takes one row and four columns,
+// consecutive threads consecutive rows, as the partials lie.  Bound by the latency of the chain sequence, (m, l),
+// partials; the sequence is found before the wait for the attention.
 template <typename T>
 __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const PromptAttnParams p) {
-  __shared__ Unit unit_s;
-  __shared__ int found_s;
   if (threadIdx.x == 0) grid_launch_dependents();
   // (the batch's arrays were complete before the attention let this grid be placed)
-  if (threadIdx.x < 32) {
-    Units units(p);
-    Unit u;
-    const bool found = units.find(p, blockIdx.x, u);
-    if (threadIdx.x == 0) {
-      if (found) unit_s = u;
-      found_s = found;
-    }
+  const int lane = threadIdx.x & 31;
+  const int place = divide((int)blockIdx.x, p.by_heads), tile = (int)blockIdx.x - place * p.tile_heads;
+  int row0 = 0, tokens = 0, ctx = 0;
+  bool bad, found = false;
+  for (int b0 = 0; b0 < p.batch && !found; b0 += 32) {   // every warp looks for the sequence
+    const int b = b0 + lane;
+    PromptSequence s = {0, 0, 0, {0, 0}};
+    if (b < p.batch) s = load_sequence(p, b, bad);
+    const int i = place - block_place(s.row0, b, p.by_block);
+    const int src = WarpLanes{}.first(i >= 0 && i < s.blocks.count);
+    if (src < 0) continue;
+    found = true;
+    const int at = __shfl_sync(0xffffffffu, i, src) * p.block_tokens;
+    row0 = __shfl_sync(0xffffffffu, s.row0, src) + at;
+    tokens = min(p.block_tokens, __shfl_sync(0xffffffffu, s.tokens, src) - at);
+    ctx = __shfl_sync(0xffffffffu, s.ctx, src) + at;
   }
-  __syncthreads();
   grid_dependency_wait();   // the partials belong to the attention
-  if (!found_s) return;
-  const Unit u = unit_s;
-  const int rows = u.tokens * p.sub, groups = p.head_dim / 4, used = p.tile_tokens * p.sub;
+  if (!found) return;
+  const int tiles = (ctx + tokens + p.key_tile - 1) >> p.key_tile_log2;
+  const int rows = tokens * p.sub, groups = p.head_dim / 4, used = p.tile_tokens * p.sub;
   const int block_rows = p.block_tokens / p.tile_tokens * p.tile_rows;
   const size_t piece0 = (size_t)blockIdx.x * p.splits;
-  auto empty = [&](int s) {
-    int k0, k1;
-    piece_range(u.tiles, s, p.splits, k0, k1);
-    return k0 == k1;
-  };
   for (int e = blockIdx.y * kMergeThreads + threadIdx.x; e < rows * groups; e += gridDim.y * kMergeThreads) {
     const int c = e / rows, r = e - c * rows;
-    const int at = r / used * p.tile_rows + r % used;
+    const int at = r < used ? r : p.tile_rows + r - used;
     const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + piece0 * block_rows + at;
     const float4* po = reinterpret_cast<const float4*>(p.part_o) + (piece0 * groups + c) * block_rows + at;
     float M = -INFINITY, L = 0.f;
@@ -59,9 +59,10 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
       float4 o[kMergeBatch];
 #pragma unroll
       for (int i = 0; i < kMergeBatch; ++i) {
-        const bool there = s0 + i < p.splits && !empty(s0 + i);
-        x[i] = there ? __ldcg(ml + (size_t)(s0 + i) * block_rows) : make_float2(-INFINITY, 0.f);
-        if (there) o[i] = __ldcg(po + (size_t)(s0 + i) * groups * block_rows);
+        int k0 = 0, k1 = 0;   // a piece without keys wrote nothing
+        if (s0 + i < p.splits) piece_range(tiles, s0 + i, p.splits, p.by_splits, k0, k1);
+        x[i] = k1 > k0 ? __ldcg(ml + (size_t)(s0 + i) * block_rows) : make_float2(-INFINITY, 0.f);
+        if (k1 > k0) o[i] = __ldcg(po + (size_t)(s0 + i) * groups * block_rows);
       }
       float m = M;
 #pragma unroll
@@ -82,7 +83,8 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
       }
     }
     const float inv = 1.f / L;
-    T* dst = static_cast<T*>(p.out) + ((size_t)(u.row0 + r / p.sub) * p.hq + u.head0 + r % p.sub) * p.head_dim + c * 4;
+    const int token = divide(r, p.by_sub), head = tile * p.sub + r - token * p.sub;
+    T* dst = static_cast<T*>(p.out) + ((size_t)(row0 + token) * p.hq + head) * p.head_dim + c * 4;
     if constexpr (sizeof(T) == 2) {
       *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
     } else {

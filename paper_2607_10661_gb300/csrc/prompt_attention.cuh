@@ -16,15 +16,21 @@ struct Unit {
   int row0;                // token0's row in q and out
   int ctx;                 // C_b
   int head0, kv;           // first query head, KV head
+  int place;               // of its partials: block_place * tile_heads + head tile
   int tiles;               // key tiles of the block
   int tile0, tile1;        // those of this piece
 };
 
-// Key tiles [k0, k1) of piece s of S.
-__device__ __forceinline__ void piece_range(int tiles, int s, int S, int& k0, int& k1) {
-  k0 = (int)((int64_t)tiles * s / S);
-  k1 = (int)((int64_t)tiles * (s + 1) / S);
+// Key tiles [k0, k1) of piece s of S: the first tiles % S pieces have one more than the others.
+__device__ __forceinline__ void piece_range(int tiles, int s, int S, IndexDivisor by_splits, int& k0, int& k1) {
+  const int q = divide(tiles, by_splits), rest = tiles - q * S;
+  k0 = s * q + min(s, rest);
+  k1 = k0 + q + (s < rest ? 1 : 0);
 }
+
+// Where the partials of a sequence's first block lie, counted in blocks; its others follow.  The places grow with
+// the sequence and are below total_tokens / block_tokens + batch.
+__device__ __forceinline__ int block_place(int row0, int b, IndexDivisor by_block) { return divide(row0, by_block) + b; }
 
 // Sequence b of the batch.
 __device__ __forceinline__ PromptSequence load_sequence(const PromptAttnParams& p, int b, bool& bad) {
@@ -77,6 +83,7 @@ struct Units {
     u.row0 = s.row0 + u.token0;
     u.head0 = tile * p.sub;
     u.kv = divide(tile, p.by_kv);
+    u.place = (block_place(s.row0, u.b, p.by_block) + i) * p.tile_heads + tile;
     u.tiles = (u.ctx + u.token0 + u.tokens + p.key_tile - 1) >> p.key_tile_log2;
     u.tile0 = 0;
     u.tile1 = u.tiles;

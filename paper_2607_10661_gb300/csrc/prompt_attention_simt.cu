@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(kThreads) prompt_simt_kernel(const PromptAttnP
     Unit u;
     bool found = units.find(p, block, u);
     if (found) {
-      piece_range(u.tiles, split, p.splits, u.tile0, u.tile1);
+      piece_range(u.tiles, split, p.splits, p.by_splits, u.tile0, u.tile1);
       found = u.tile1 > u.tile0;
     }
     if (t == 0) {
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kThreads) prompt_simt_kernel(const PromptAttnP
     for (int w = 1; w < 16; w <<= 1) l[a] += __shfl_xor_sync(0xffffffffu, l[a], w);
     if (r >= rows) continue;
     if (p.splits > 1) {
-      const size_t piece = blockIdx.x;
+      const size_t piece = (size_t)u.place * p.splits + split;
       if (x == 0) reinterpret_cast<float2*>(p.part_ml)[piece * kRows + r] = make_float2(m[a], l[a]);
 #pragma unroll
       for (int b = 0; b < NB; ++b)

@@ -428,6 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // The walk: steps of a unit (V of tile j and K of tile j + 1, j = -1 .. n - 1), and before its last ones
       // the claim and the search of the next, so that its first copies follow at once.
       Unit u;                      // the next unit, once it is known
+      int piece = 0;
       bool search = true, found = false;
       int it = 0, j = 0, n = 0, search_at = 0, b = 0, kv = 0, kt0 = 0, edge = 0, head0 = 0, row0 = 0, end_page = 0;
       int nq[2] = {0, 0}, next_page = -1, row_v = 0;
@@ -472,7 +473,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             const int y = divide(x, p.by_splits);
             if (units.find(p, y, u)) {
-              if (p.splits > 1) pa::piece_range(u.tiles, x - y * p.splits, p.splits, u.tile0, u.tile1);
+              if (p.splits > 1) {
+                piece = x - y * p.splits;
+                pa::piece_range(u.tiles, piece, p.splits, p.by_splits, u.tile0, u.tile1);
+              }
               found = u.tile1 > u.tile0;
             }
           }
@@ -497,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               s.tokens = u.tokens;
               s.head0 = head0;
               s.kv = kv;
-              s.piece = x;
+              s.piece = u.place * p.splits + piece;
               s.kt0 = kt0;
               s.edge = edge;
               s.n[0] = nq[0];
