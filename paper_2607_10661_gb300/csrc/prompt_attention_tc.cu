@@ -80,6 +80,14 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
   return wait_longer(bar, parity, abort_flag, dev_status);
 }
 
+// One lane of the warp, always the same; the compiler knows such a branch to be one thread's, and its copies then
+// cost 17 cycles to issue instead of 60.
+__device__ __forceinline__ bool elect_lane() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
+
 // A unit as the roles need it.
 struct Seg {
   int valid;
@@ -195,21 +203,29 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool has_
   tc_fence_before();
 }
 
-// Instructions [kBegin, kEnd) of the eight of S_t = Q_t K^T, and of O_t (+)= P_t V (see tc::issue_s, issue_pv).
+// Instructions [kBegin, kEnd) of the eight of S_t = Q_t K^T, and of O_t (+)= P_t V (see tc::issue_s, issue_pv), from
+// one elected lane: against a lane chosen by a predicate on each instruction 16384 tokens of 64/8 heads take 2472 us
+// instead of 2653, 8192 of 32/8 heads 300 instead of 330 (graph replays).
 template <int kBegin, int kEnd>
-__device__ __forceinline__ void issue_s(uint32_t leader, uint32_t s_tmem, uint32_t q_desc, uint32_t k_desc) {
+__device__ __forceinline__ void issue_s(uint32_t s_tmem, uint32_t q_desc, uint32_t k_desc) {
+  if (elect_lane()) {
 #pragma unroll
-  for (int kk = kBegin; kk < kEnd; ++kk) {
-    const uint32_t o = (uint32_t)(kk >> 2) * (kHalfBytes >> 4) + (uint32_t)(kk & 3) * 2u;
-    mma_ss_if(leader, s_tmem, q_desc + o, k_desc + o, tc::kDescHi, tc::kIdescS, kk > 0 ? 1u : 0u);
+    for (int kk = kBegin; kk < kEnd; ++kk) {
+      const uint32_t o = (uint32_t)(kk >> 2) * (kHalfBytes >> 4) + (uint32_t)(kk & 3) * 2u;
+      mma_ss_if(1u, s_tmem, q_desc + o, k_desc + o, tc::kDescHi, tc::kIdescS, kk > 0 ? 1u : 0u);
+    }
   }
+  __syncwarp();
 }
 template <int kBegin, int kEnd>
-__device__ __forceinline__ void issue_pv(uint32_t leader, uint32_t s_tmem, uint32_t v_desc, bool acc) {
+__device__ __forceinline__ void issue_pv(uint32_t s_tmem, uint32_t v_desc, bool acc) {
+  if (elect_lane()) {
 #pragma unroll
-  for (int kk = kBegin; kk < kEnd; ++kk)
-    mma_ts_if(leader, s_tmem + 256u, s_tmem + (uint32_t)kk * 8u, v_desc + (uint32_t)kk * 128u, tc::kDescHi, tc::kIdescPV,
-              (acc || kk > 0) ? 1u : 0u);
+    for (int kk = kBegin; kk < kEnd; ++kk)
+      mma_ts_if(1u, s_tmem + 256u, s_tmem + (uint32_t)kk * 8u, v_desc + (uint32_t)kk * 128u, tc::kDescHi, tc::kIdescPV,
+                (acc || kk > 0) ? 1u : 0u);
+  }
+  __syncwarp();
 }
 constexpr int kEarly = 5;   // products of a group of eight before the other issuer is let go
 
@@ -259,10 +275,12 @@ __device__ __forceinline__ void add_bad(const PromptAttnParams& p, float* o, int
   }
 }
 
-template <bool kPaged>
+// kPages: 0 for a contiguous cache, else the most pages that a key tile has (2: pages of 64 and 128, 8: of 16 and 32).
+template <int kPages>
 __global__ void __launch_bounds__(kThreads, 1)
     prompt_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                      const __grid_constant__ CUtensorMap map_q, const PromptAttnParams p) {
+  constexpr bool kPaged = kPages > 0;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint32_t base = smem_u32(smem_raw);
   const uint32_t pad = (1024u - (base & 1023u)) & 1023u;
@@ -324,9 +342,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t dq = (uint32_t)smem_desc_sw128(base + kOffQ + (uint32_t)t * kTileBytes, 16, 1024);
       const uint32_t dk = (uint32_t)smem_desc_sw128(base + kOffRing, 16, 1024);
       const uint32_t dv = (uint32_t)smem_desc_sw128(base + kOffRing, kHalfBytes, 1024);
-      const uint32_t s_tmem = tmem + (uint32_t)t * 128u, leader = lane == 0 ? 1u : 0u;
+      const uint32_t s_tmem = tmem + (uint32_t)t * 128u;
       auto commit = [&](int b) {
-        if (leader) mma_commit(bar(b));
+        if (elect_lane()) mma_commit(bar(b));
+        __syncwarp();
+      };
+      auto arrive = [&](int b) {
+        if (elect_lane()) mbar_arrive(bar(b));
+        __syncwarp();
       };
       auto wait = [&](int b, int uses) { return wait_warp(bar(b), (uint32_t)uses & 1u, abort_flag, p.dev_status); };
       bool ok = true;
@@ -340,7 +363,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         return true;
       };
       auto step_done = [&](bool issued) {   // the step's tiles are free when its products are done
-        if (issued) commit(kDone + steps % kSteps); else if (leader) mbar_arrive(bar(kDone + steps % kSteps));
+        if (issued) commit(kDone + steps % kSteps); else arrive(kDone + steps % kSteps);
         ++steps;
       };
       for (int it = 0; ok; ++it) {
@@ -352,34 +375,34 @@ __global__ void __launch_bounds__(kThreads, 1)
         // While both M tiles have products they take turns: M tile 1's of step j after 0's, 0's of step
         // j + 1 after 1's of step j.  A turn that waits for nobody is the issuer's own arrival.
         auto pass_turn = [&](int j) {
-          if (leader && (t == 0 ? j < both : j + 1 < both)) mbar_arrive(bar(kPHalf + (t ^ 1)));
+          if (t == 0 ? j < both : j + 1 < both) arrive(kPHalf + (t ^ 1));
         };
         if (!(ok = take(k_tile))) break;
         if (mine > 0) {
           if (!(ok = wait(kQFull + t, qs++))) break;
           tc_fence_after();
-          issue_s<0, 8>(leader, s_tmem, dq, dk + k_tile);
+          issue_s<0, 8>(s_tmem, dq, dk + k_tile);
           commit(kSFull + t);
           if (mine == 1) commit(kQEmpty + t);
         }
         step_done(mine > 0);
         for (int j = 0; j < n; ++j) {
-          if (leader && j < mine && (t == 0 ? j == 0 || j >= both : j >= both)) mbar_arrive(bar(kPHalf + t));
+          if (j < mine && (t == 0 ? j == 0 || j >= both : j >= both)) arrive(kPHalf + t);
           if (!(ok = take(v_tile))) break;
           if (j + 1 < n && !(ok = take(k_tile))) break;
           if (j < mine) {
             if (!(ok = wait(kPHalf + t, ps))) break;
             tc_fence_after();
-            issue_pv<0, 4>(leader, s_tmem, dv + v_tile, j > 0);
+            issue_pv<0, 4>(s_tmem, dv + v_tile, j > 0);
             if (!(ok = wait(kPFull + t, ps++))) break;
             tc_fence_after();
-            issue_pv<4, kEarly>(leader, s_tmem, dv + v_tile, j > 0);
+            issue_pv<4, kEarly>(s_tmem, dv + v_tile, j > 0);
             if (j + 1 == mine) pass_turn(j);
-            issue_pv<kEarly, 8>(leader, s_tmem, dv + v_tile, j > 0);
+            issue_pv<kEarly, 8>(s_tmem, dv + v_tile, j > 0);
             if (j + 1 < mine) {
-              issue_s<0, kEarly>(leader, s_tmem, dq, dk + k_tile);
+              issue_s<0, kEarly>(s_tmem, dq, dk + k_tile);
               pass_turn(j);
-              issue_s<kEarly, 8>(leader, s_tmem, dq, dk + k_tile);
+              issue_s<kEarly, 8>(s_tmem, dq, dk + k_tile);
               commit(kSFull + t);
               if (j + 2 == mine) commit(kQEmpty + t);
             } else {
@@ -389,22 +412,20 @@ __global__ void __launch_bounds__(kThreads, 1)
           step_done(j < mine);
         }
       }
-      if (lane == 0 && *abort_flag) {
+      if (elect_lane() && *abort_flag) {
         // error path: let the tensor core finish what was issued before TMEM is freed
         mma_commit(bar(kDrain + t));
         mbar_drain(bar(kDrain + t), 0, 100000000ull);
       }
     } else if (warp == 0) {
       // ================================================================ scheduler and TMA producer
-      // A lane copies one half (64 columns) of one page's rows, or of the tile's 128 rows.
       bool ok = true;
       int at = 0, qc[2] = {0, 0};   // ring place of the next tile, Q tiles copied
       uint32_t armed = 0, checked = 0;   // a bit per ring place: its barrier's turn (full; loaded, for the check)
       int steps = 0, done = 0;      // steps begun, and known to be done
       int step_of = -1;             // lane i: the step of the tile in ring place i
-      const int half = lane & 1, page_at = lane >> 1, per_tile = kPaged ? 128 / p.page_size : 1;
-      const int page_log2 = kPaged ? 31 - __clz(p.page_size) : 0;
-      const uint32_t copy_at = (uint32_t)half * kHalfBytes + (kPaged ? (uint32_t)(page_at * p.page_size) * 128u : 0u);
+      const int page_log2 = kPaged ? 31 - __clz(p.page_size) : 0, per_tile = kPaged ? 128 >> page_log2 : 1;
+      const uint32_t page_bytes = kPaged ? (uint32_t)p.page_size * 128u : 0u;   // of half the columns
       // waits until the next ring place is free
       auto place = [&]() {
         const int last = __shfl_sync(0xffffffffu, step_of, at);
@@ -435,24 +456,42 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int* bt = nullptr;
       // this lane's page of key tile i (read a step ahead, so that no copy waits for it)
       auto page_of = [&](int i) {
-        const int g = (kt0 + i) * per_tile + page_at;
-        return kPaged && i < n && page_at < per_tile && g < end_page ? bt[g] : -1;
+        const int g = (kt0 + i) * per_tile + lane;
+        return kPaged && i < n && lane < per_tile && g < end_page ? bt[g] : -1;
       };
       auto pages_in = [&](int i) { return kPaged ? min(per_tile, end_page - (kt0 + i) * per_tile) : 1; };
-      // first row of this lane's copy of tile i
+      // first row of this lane's page of tile i, or of the tile
       auto row_of = [&](int i, int page) {
         if (!kPaged) return (p.layer * p.batch + b) * p.seq_capacity + (kt0 + i) * 128;
         const bool there = page >= 0 && page < p.num_pages;
-        if (!there && page_at < pages_in(i)) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
+        if (!there && lane < pages_in(i)) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
         return there ? (p.layer * p.num_pages + page) * p.page_size : -128;   // (-128: TMA fills zeros)
       };
       auto copy = [&](const CUtensorMap* map, bool check, int i, int row) {   // tile i into the next ring place
-        const uint32_t full = bar((check ? kLoadV : kFull) + at);
-        if (lane == 0)
-          mbar_arrive_expect_tx(full, kPaged ? (uint32_t)(pages_in(i) * p.page_size) * 256u : kTileBytes);
+        const uint32_t full = bar((check ? kLoadV : kFull) + at), dst = base + kOffRing + (uint32_t)at * kTileBytes;
+        if constexpr (kPaged) {
+          const int pages = pages_in(i);
+          int rows[kPages > 0 ? kPages : 1];
+#pragma unroll
+          for (int g = 0; g < kPages; ++g) rows[g] = __shfl_sync(0xffffffffu, row, g);
+          if (elect_lane()) {
+            mbar_arrive_expect_tx(full, (uint32_t)pages * page_bytes * 2u);
+#pragma unroll
+            for (int g = 0; g < kPages; ++g) {
+              if (g < pages) {
+                tma_load_3d(dst + (uint32_t)g * page_bytes, map, full, 0, kv, rows[g]);
+                tma_load_3d(dst + (uint32_t)g * page_bytes + kHalfBytes, map, full, 64, kv, rows[g]);
+              }
+            }
+          }
+        } else {
+          if (elect_lane()) {
+            mbar_arrive_expect_tx(full, kTileBytes);
+            tma_load_3d(dst, map, full, 0, kv, row);
+            tma_load_3d(dst + kHalfBytes, map, full, 64, kv, row);
+          }
+        }
         __syncwarp();
-        if (page_at < pages_in(i))
-          tma_load_3d(base + kOffRing + (uint32_t)at * kTileBytes + copy_at, map, full, half * 64, kv, row);
         if (lane == at) step_of = steps;
         armed ^= 1u << at;
         if (check) checked ^= 1u << at;
@@ -537,11 +576,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 !(ok = wait_warp(bar(kQEmpty + t), ((uint32_t)qc[t] & 1u) ^ 1u, abort_flag, p.dev_status)))
               continue;
             ++qc[t];
-            if (lane == 0) mbar_arrive_expect_tx(bar(kQFull + t), (uint32_t)used * 256u);
+            if (elect_lane()) {
+              const uint32_t dst = base + kOffQ + (uint32_t)t * kTileBytes;
+              mbar_arrive_expect_tx(bar(kQFull + t), (uint32_t)used * 256u);
+              tma_load_3d(dst, &map_q, bar(kQFull + t), 0, head0, row0 + t * p.tile_tokens);
+              tma_load_3d(dst + kHalfBytes, &map_q, bar(kQFull + t), 64, head0, row0 + t * p.tile_tokens);
+            }
             __syncwarp();
-            if (lane < 2)
-              tma_load_3d(base + kOffQ + (uint32_t)t * kTileBytes + (uint32_t)half * kHalfBytes, &map_q, bar(kQFull + t),
-                          half * 64, head0, row0 + t * p.tile_tokens);
           }
         }
         if (j == search_at - 1) claim();
@@ -695,7 +736,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 cudaError_t launch_prompt_attn_tc(const CUtensorMap& map_k, const CUtensorMap& map_v, const CUtensorMap& map_q,
                                   const PromptAttnParams& p, cudaStream_t stream) {
-  const auto kernel = p.page_size > 0 ? pt::prompt_tc_kernel<true> : pt::prompt_tc_kernel<false>;
+  const auto kernel = p.page_size == 0 ? pt::prompt_tc_kernel<0> : (p.page_size >= 64 ? pt::prompt_tc_kernel<2> : pt::prompt_tc_kernel<8>);
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pt::kSmemBytes);
   if (e != cudaSuccess) return e;
   return launch_chained(kernel, dim3((unsigned)(p.blocks * p.tile_heads * p.splits)), dim3(pt::kThreads), pt::kSmemBytes,
