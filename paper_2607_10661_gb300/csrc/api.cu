@@ -884,7 +884,7 @@ ptd_status ptd_prompt_attention(const ptd_prompt* prompt, const ptd_kv_cache* ca
   const bool bf16 = cache->dtype == PTD_BF16;
   ptd::plan_prompt_attention(p, bf16, workspace != nullptr && aligned16(workspace) ? workspace_bytes : 0,
                              num_sms_of_current_device());
-  if ((int64_t)p.blocks * p.tile_heads * p.splits > INT32_MAX) return PTD_ERR_UNSUPPORTED;
+  if ((int64_t)p.places * p.tile_heads * p.splits > INT32_MAX) return PTD_ERR_UNSUPPORTED;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (bf16) {
     if (cache_rows_per_layer(cache, prompt->batch) * cache->num_layers > INT32_MAX) return PTD_ERR_UNSUPPORTED;

@@ -73,13 +73,14 @@ struct PromptAttnParams {
   int level_step;              // of the blocks' order (prompt_geometry.cuh)
   IndexDivisor by_block, by_heads, by_kv, by_splits, by_sub;   // block_tokens, tile_heads, tiles_per_kv, splits, sub
   int blocks;                  // upper bound of the batch's blocks of tokens (per head tile)
-  int splits;                  // pieces that a block's keys are cut into
+  int places;                  // of the blocks' partials (per head tile)
+  int splits, piece_tiles;     // a block's keys are cut into pieces of piece_tiles key tiles, at most `splits` (1: uncut)
   int page_size, seq_capacity, num_pages, max_pages;
   float scale_log2;            // scale * log2(e)
 };
 
 // Chooses the tiles and the cut of the keys from the host-known sizes, with `scratch` bytes at hand: sets sub,
-// tile_heads, tiles_per_kv, tile_tokens, block_tokens, tile_rows, key_tile, level_step, blocks and splits.  Returns the
+// tile_heads, tiles_per_kv, tile_tokens, block_tokens, tile_rows, key_tile, level_step, blocks, piece_tiles and splits.  Returns the
 // scratch that the cut takes (0: unsplit).
 size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int sms);
 // bf16, D = 128.  map_k, map_v: boxes of 64 columns of one KV head and 128 rows (or a page's); map_q: of 64

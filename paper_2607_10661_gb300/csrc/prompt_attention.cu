@@ -44,6 +44,7 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
   grid_dependency_wait();   // the partials belong to the attention
   if (!found) return;
   const int tiles = (ctx + tokens + p.key_tile - 1) >> p.key_tile_log2;
+  if (tiles <= p.piece_tiles) return;   // one piece: written by the attention
   const int rows = tokens * p.sub, groups = p.head_dim / 4, used = p.tile_tokens * p.sub;
   const int block_rows = p.block_tokens / p.tile_tokens * p.tile_rows;
   const size_t piece0 = (size_t)blockIdx.x * p.splits;
@@ -54,15 +55,14 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
     const float4* po = reinterpret_cast<const float4*>(p.part_o) + (piece0 * groups + c) * block_rows + at;
     float M = -INFINITY, L = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = 0; s0 < p.splits; s0 += kMergeBatch) {   // the loads of a batch are in flight together
+    for (int s0 = 0; s0 * p.piece_tiles < tiles; s0 += kMergeBatch) {   // the loads of a batch are in flight together
       float2 x[kMergeBatch];
       float4 o[kMergeBatch];
 #pragma unroll
       for (int i = 0; i < kMergeBatch; ++i) {
-        int k0 = 0, k1 = 0;   // a piece without keys wrote nothing
-        if (s0 + i < p.splits) piece_range(tiles, s0 + i, p.splits, p.by_splits, k0, k1);
-        x[i] = k1 > k0 ? __ldcg(ml + (size_t)(s0 + i) * block_rows) : make_float2(-INFINITY, 0.f);
-        if (k1 > k0) o[i] = __ldcg(po + (size_t)(s0 + i) * groups * block_rows);
+        const bool there = (s0 + i) * p.piece_tiles < tiles;
+        x[i] = there ? __ldcg(ml + (size_t)(s0 + i) * block_rows) : make_float2(-INFINITY, 0.f);
+        if (there) o[i] = __ldcg(po + (size_t)(s0 + i) * groups * block_rows);
       }
       float m = M;
 #pragma unroll
@@ -100,6 +100,19 @@ int largest_divisor(int group, int most) {
   return 1;
 }
 
+// Key tiles per piece: all of them (uncut) where the units fill the SMs, else as many pieces of the longest sequence
+// as give every SM one; one more where that is two or three and the batch may be ragged.  Measured (us by length,
+// the rule's in brackets): one token after 4096 of 32/8 heads, 8 units of 33 tiles, 1: 17.5, [2: 12.7], 4: 12.8, 8:
+// 15.7, uncut 42; after 32768, 10: 42.6, [14: 34.6], 17: 33.0, 20: 34.3; eight ragged contexts up to 4096, 5: 27.3, [11:
+// 25.7], 14: 27.4, 17: 30.8, uncut 48; four equal ones, 7: 27.1, [9: 22.5], 12: 24.2; sixteen (128 units) 17: 59.1, [uncut
+// 50.4]; 61 tokens of 64/8 heads after 32707, 20: 71.6, [29: 54], 40: 62; 256 tokens after 8192, 14: 52, [17: 41], 25: 51.
+int choose_piece(int64_t units, int64_t key_tiles, int batch, int sms) {
+  if (units == 0 || units >= sms || key_tiles < 2) return (int)key_tiles;
+  int64_t pieces = sms / units;
+  if (batch > 1 && (pieces == 2 || pieces == 3)) ++pieces;
+  return (int)((key_tiles + pieces - 1) / pieces);
+}
+
 }  // namespace pa
 
 size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int sms) {
@@ -117,23 +130,22 @@ size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int
   p.by_kv = index_divisor(p.tiles_per_kv);
   p.by_sub = index_divisor(p.sub);
   p.level_step = prompt_level_step(p.bounds.max_ctx, p.bounds.max_tokens, p.block_tokens);
-  const int64_t w = p.block_tokens, N = p.bounds.n_total, B = p.batch;
-  const int64_t by_total = N / w + B, by_longest = B * ((p.bounds.max_tokens + w - 1) / w);
+  const int64_t w = p.block_tokens, B = p.batch;
+  const int64_t by_total = prompt_places(p.bounds.n_total, p.batch, p.block_tokens), by_longest = B * ((p.bounds.max_tokens + w - 1) / w);
   p.blocks = (int)(by_total < by_longest ? by_total : by_longest);
+  p.places = (int)by_total;
   const int64_t units = (int64_t)p.blocks * p.tile_heads;
   const int64_t key_tiles = ((int64_t)p.bounds.max_ctx + p.bounds.max_tokens + p.key_tile - 1) / p.key_tile;
-  // as many pieces as give every SM one, of two key tiles or more
-  int64_t splits = units > 0 ? sms / units : 1;
-  if (splits > key_tiles / 2) splits = key_tiles / 2;
-  p.splits = splits < 1 ? 1 : (int)splits;
-  const size_t bytes = p.splits == 1 ? 0 : (size_t)units * p.splits * tiles * tile_rows * (p.head_dim + 2) * sizeof(float);
+  p.piece_tiles = pa::choose_piece(units, key_tiles, p.batch, sms);
+  p.splits = (int)((key_tiles + p.piece_tiles - 1) / p.piece_tiles);
+  const size_t bytes = p.splits == 1 ? 0 : (size_t)p.places * p.tile_heads * p.splits * tiles * tile_rows * (p.head_dim + 2) * sizeof(float);
   if (bytes > scratch) {
     p.splits = 1;
-    p.by_splits = index_divisor(1);
-    return 0;
+    p.piece_tiles = (int)key_tiles;
   }
   p.by_splits = index_divisor(p.splits);
-  if (bytes > 0) p.part_ml = p.part_o + (size_t)units * p.splits * tiles * tile_rows * p.head_dim;
+  if (p.splits == 1) return 0;
+  p.part_ml = p.part_o + (size_t)p.places * p.tile_heads * p.splits * tiles * tile_rows * p.head_dim;
   return bytes;
 }
 
@@ -141,7 +153,7 @@ cudaError_t launch_prompt_attn_merge(const PromptAttnParams& p, bool bf16, cudaS
   const auto kernel = bf16 ? pa::prompt_merge_kernel<__nv_bfloat16> : pa::prompt_merge_kernel<float>;
   int64_t rows = (int64_t)(p.bounds.max_tokens < p.block_tokens ? p.bounds.max_tokens : p.block_tokens) * p.sub;
   const unsigned shares = (unsigned)((rows * (p.head_dim / 4) + pa::kMergeThreads - 1) / pa::kMergeThreads);
-  return launch_chained(kernel, dim3((unsigned)(p.blocks * p.tile_heads), shares), dim3(pa::kMergeThreads), 0, stream, 0, p);
+  return launch_chained(kernel, dim3((unsigned)(p.places * p.tile_heads), shares), dim3(pa::kMergeThreads), 0, stream, 0, p);
 }
 
 }  // namespace ptd

@@ -16,21 +16,10 @@ struct Unit {
   int row0;                // token0's row in q and out
   int ctx;                 // C_b
   int head0, kv;           // first query head, KV head
-  int place;               // of its partials: block_place * tile_heads + head tile
-  int tiles;               // key tiles of the block
-  int tile0, tile1;        // those of this piece
+  int tile0, tile1;        // key tiles of the piece
+  bool whole;              // all that the block has: no partials
+  int place;               // of the partials: (the block's place * tile_heads + head tile) * splits + piece
 };
-
-// Key tiles [k0, k1) of piece s of S: the first tiles % S pieces have one more than the others.
-__device__ __forceinline__ void piece_range(int tiles, int s, int S, IndexDivisor by_splits, int& k0, int& k1) {
-  const int q = divide(tiles, by_splits), rest = tiles - q * S;
-  k0 = s * q + min(s, rest);
-  k1 = k0 + q + (s < rest ? 1 : 0);
-}
-
-// Where the partials of a sequence's first block lie, counted in blocks; its others follow.  The places grow with
-// the sequence and are below total_tokens / block_tokens + batch.
-__device__ __forceinline__ int block_place(int row0, int b, IndexDivisor by_block) { return divide(row0, by_block) + b; }
 
 // Sequence b of the batch.
 __device__ __forceinline__ PromptSequence load_sequence(const PromptAttnParams& p, int b, bool& bad) {
@@ -63,9 +52,10 @@ struct Units {
       }
     }
   }
-  // Block y / tile_heads of the batch under head tile y % tile_heads, with all of its keys (every lane gets it).
-  // False: there is none.
-  __device__ __forceinline__ bool find(const PromptAttnParams& p, int y, Unit& u) {
+  // Unit number x: piece x % splits of block (x / splits) / tile_heads of the batch under head tile (x / splits) %
+  // tile_heads (every lane gets it).  False: there is none.
+  __device__ __forceinline__ bool find(const PromptAttnParams& p, int x, Unit& u) {
+    const int y = divide(x, p.by_splits), piece = x - y * p.splits;
     const int block = divide(y, p.by_heads), tile = y - block * p.tile_heads;
     int i;
     PromptSequence s;
@@ -83,11 +73,12 @@ struct Units {
     u.row0 = s.row0 + u.token0;
     u.head0 = tile * p.sub;
     u.kv = divide(tile, p.by_kv);
-    u.place = (block_place(s.row0, u.b, p.by_block) + i) * p.tile_heads + tile;
-    u.tiles = (u.ctx + u.token0 + u.tokens + p.key_tile - 1) >> p.key_tile_log2;
-    u.tile0 = 0;
-    u.tile1 = u.tiles;
-    return true;
+    const int tiles = (u.ctx + u.token0 + u.tokens + p.key_tile - 1) >> p.key_tile_log2;
+    u.tile0 = piece * p.piece_tiles;
+    u.tile1 = min(tiles, u.tile0 + p.piece_tiles);
+    u.whole = u.tile0 == 0 && u.tile1 == tiles;
+    u.place = ((block_place(s.row0, u.b, p.by_block) + i) * p.tile_heads + tile) * p.splits + piece;
+    return u.tile1 > u.tile0;
   }
 };
 

@@ -43,16 +43,11 @@ __global__ void __launch_bounds__(kThreads) prompt_simt_kernel(const PromptAttnP
   const int t = threadIdx.x, x = t & 15, y = t >> 4;
   if (t == 0) grid_launch_dependents();
   grid_dependency_wait();
-  const int block = divide((int)blockIdx.x, p.by_splits), split = (int)blockIdx.x - block * p.splits;
   if (t < 32) {
     Units units(p);
     if (units.bad) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
     Unit u;
-    bool found = units.find(p, block, u);
-    if (found) {
-      piece_range(u.tiles, split, p.splits, p.by_splits, u.tile0, u.tile1);
-      found = u.tile1 > u.tile0;
-    }
+    const bool found = units.find(p, blockIdx.x, u);
     if (t == 0) {
       if (found) unit_s = u;
       found_s = found;
@@ -199,8 +194,8 @@ __global__ void __launch_bounds__(kThreads) prompt_simt_kernel(const PromptAttnP
 #pragma unroll
     for (int w = 1; w < 16; w <<= 1) l[a] += __shfl_xor_sync(0xffffffffu, l[a], w);
     if (r >= rows) continue;
-    if (p.splits > 1) {
-      const size_t piece = (size_t)u.place * p.splits + split;
+    if (!u.whole) {
+      const size_t piece = u.place;
       if (x == 0) reinterpret_cast<float2*>(p.part_ml)[piece * kRows + r] = make_float2(m[a], l[a]);
 #pragma unroll
       for (int b = 0; b < NB; ++b)

@@ -92,7 +92,7 @@ __device__ __forceinline__ bool elect_lane() {
 struct Seg {
   int valid;
   int b, row0, ctx, token0, tokens, head0, kv;
-  int piece;             // its number among the partials
+  int piece;             // place of its partials, -1: it is a whole block
   int kt0;               // first key tile
   int n[2];              // key tiles of either M tile (0: not there, or no keys in this piece)
   int edge;              // first key tile that some row sees in part
@@ -449,7 +449,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       // The walk: steps of a unit (V of tile j and K of tile j + 1, j = -1 .. n - 1), and before its last ones
       // the claim and the search of the next, so that its first copies follow at once.
       Unit u;                      // the next unit, once it is known
-      int piece = 0;
       bool search = true, found = false;
       int it = 0, j = 0, n = 0, search_at = 0, b = 0, kv = 0, kt0 = 0, edge = 0, head0 = 0, row0 = 0, end_page = 0;
       int nq[2] = {0, 0}, next_page = -1, row_v = 0;
@@ -510,14 +509,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               __syncwarp();
               if (x < 0) break;
             }
-            const int y = divide(x, p.by_splits);
-            if (units.find(p, y, u)) {
-              if (p.splits > 1) {
-                piece = x - y * p.splits;
-                pa::piece_range(u.tiles, piece, p.splits, p.by_splits, u.tile0, u.tile1);
-              }
-              found = u.tile1 > u.tile0;
-            }
+            found = units.find(p, x, u);
           }
           if (!ok) break;
         }
@@ -540,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               s.tokens = u.tokens;
               s.head0 = head0;
               s.kv = kv;
-              s.piece = u.place * p.splits + piece;
+              s.piece = u.whole ? -1 : u.place;
               s.kt0 = kt0;
               s.edge = edge;
               s.n[0] = nq[0];
@@ -681,12 +673,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_after();
       }
       const bool bad = sg->bad != 0;
-      const float inv = p.splits == 1 ? 1.f / l_run : 1.f;   // a piece stays unnormalised
+      const int piece = sg->piece;
+      const float inv = piece < 0 ? 1.f / l_run : 1.f;   // a piece stays unnormalised
       uint4* dst = reinterpret_cast<uint4*>(p.out) + (((size_t)sg->row0 + my_token) * p.hq + sg->head0 + my_head) * 16;
       const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0;
-      float4* po = reinterpret_cast<float4*>(p.part_o) + (size_t)sg->piece * 32 * 256 + t * 128 + row;
-      if (p.splits > 1 && row_valid)
-        reinterpret_cast<float2*>(p.part_ml)[(size_t)sg->piece * 256 + t * 128 + row] =
+      float4* po = reinterpret_cast<float4*>(p.part_o) + (size_t)max(piece, 0) * 32 * 256 + t * 128 + row;
+      if (piece >= 0 && row_valid)
+        reinterpret_cast<float2*>(p.part_ml)[(size_t)piece * 256 + t * 128 + row] =
             n > 0 ? make_float2(m_run, l_run) : make_float2(-INFINITY, 0.f);
       if (n > 0 && any_row) {
 #pragma unroll 1
@@ -706,7 +699,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
               for (int e = 0; e < 32; ++e) o[e] = ob[e];
             }
-            if (p.splits == 1) {
+            if (piece < 0) {
               uint32_t w[16];
 #pragma unroll
               for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(o[2 * e], o[2 * e + 1]);

@@ -49,6 +49,12 @@ struct PromptSequence {
   PromptBlocks blocks;
 };
 
+// Where a sequence's first block lies among the batch's partials, counted in blocks; its others follow.  The places
+// of different blocks differ (a sequence of c blocks takes more than (c - 1) * width rows, and the sequence number
+// adds one), and are below prompt_places: the first row of the last sequence's last block is below n_total.
+PTD_HD int block_place(int row0, int b, IndexDivisor by_width) { return divide(row0, by_width) + b; }
+PTD_HD int64_t prompt_places(int n_total, int batch, int width) { return (int64_t)n_total / width + batch; }
+
 // The blocks of a batch are numbered by level, highest first: a block's level is its key / level_step, 32 levels
 // in all (the long ones first, so that what is taken last is short).  Within a level they go by sequence, and
 // a sequence's by falling key.  Batches of more than kOrderedBatch sequences have one level: their many

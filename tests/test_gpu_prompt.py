@@ -129,6 +129,9 @@ CASES = {
     "long-split-contiguous": dict(seqs=[(2047, 2), (10, 1), (4000, 90)], hq=8, hkv=2),
     "bounds-above-lengths": dict(seqs=[(40, 30), (0, 2)], hq=8, hkv=2, page=16, pad=90, max_ctx=3000, max_tokens=800),
     "many-sequences": dict(seqs=[(i % 37, i % 5) for i in range(700)], hq=4, hkv=2, page=16),
+    "decoding-64-split": dict(seqs=[(300 + 37 * i, 1) for i in range(64)], hq=16, hkv=2, page=16),
+    "ordered-100": dict(seqs=[(17 * i % 701, 1 + i % 3) for i in range(100)], hq=8, hkv=1, page=32, max_ctx=2000),
+    "f32-decoding-split": dict(seqs=[(200 + 11 * i, 1) for i in range(40)], hq=2, hkv=2, d=32, dtype=F32),
     "f32-64": dict(seqs=RAGGED, hq=4, hkv=4, d=64, dtype=F32, pad=2),
     "f32-32-paged": dict(seqs=[(0, 70), (500, 3), (64, 64)], hq=6, hkv=2, d=32, page=16, dtype=F32),
     "f32-128-gqa": dict(seqs=[(33, 65), (0, 200), (900, 1)], hq=8, hkv=2, d=128, page=64, dtype=F32),

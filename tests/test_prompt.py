@@ -77,7 +77,8 @@ def test_blocks_are_numbered_longest_first(tmp_path):
     rng = random.Random(5)
     cases = [(64, [(0, 0)]), (64, [(5, 1)]), (64, [(100, 640)]), (1, [(3, 4), (0, 9), (5, 0), (2, 2)]),
              (256, [(0, 0), (0, 0)]), (2, [(rng.randrange(4000), 1) for _ in range(128)]),
-             (2, [(rng.randrange(4000), rng.randrange(3)) for _ in range(129)])]
+             (2, [(rng.randrange(4000), rng.randrange(3)) for _ in range(129)]),
+             (32, [(1000, 1)] * 64), (2, [(9, 1)] * 100)]
     for _ in range(60):
         seqs = [(rng.choice([0, rng.randrange(5000)]), rng.choice([0, 1, rng.randrange(3000)]))
                 for _ in range(rng.randrange(1, 70))]
