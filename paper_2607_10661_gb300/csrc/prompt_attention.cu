@@ -100,27 +100,25 @@ int largest_divisor(int group, int most) {
   return 1;
 }
 
-// Key tiles per piece: all of them (uncut) where the units fill the SMs, else as many pieces of the longest sequence
-// as give every SM one; one more where that is two or three and the batch may be ragged.  Measured (us by length,
-// the rule's in brackets): one token after 4096 of 32/8 heads, 8 units of 33 tiles, 1: 17.5, [2: 12.7], 4: 12.8, 8:
-// 15.7, uncut 42; after 32768, 10: 42.6, [14: 34.6], 17: 33.0, 20: 34.3; eight ragged contexts up to 4096, 5: 27.3, [11:
-// 25.7], 14: 27.4, 17: 30.8, uncut 48; four equal ones, 7: 27.1, [9: 22.5], 12: 24.2; sixteen (128 units) 17: 59.1, [uncut
-// 50.4]; 61 tokens of 64/8 heads after 32707, 20: 71.6, [29: 54], 40: 62; 256 tokens after 8192, 14: 52, [17: 41], 25: 51.
-int choose_piece(int64_t units, int64_t key_tiles, int batch, int sms) {
-  if (units == 0 || units >= sms || key_tiles < 2) return (int)key_tiles;
-  int64_t pieces = sms / units;
+// Key tiles per piece: all of them (uncut) where the units fill `slots` places, else as many pieces of the longest
+// sequence as give every place one; one more where that is two or three and the batch may be ragged.
+int choose_piece(int64_t units, int64_t key_tiles, int batch, int64_t slots) {
+  if (units == 0 || units >= slots || key_tiles < 2) return (int)key_tiles;
+  int64_t pieces = slots / units;
   if (batch > 1 && (pieces == 2 || pieces == 3)) ++pieces;
   return (int)((key_tiles + pieces - 1) / pieces);
 }
 
 }  // namespace pa
 
-size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int sms) {
-  const int tile_rows = bf16 ? 128 : 64, tiles = bf16 ? 2 : 1, group = p.hq / p.hkv;   // M tiles of a block
+namespace pa {
+// Tiles, blocks and the cut, for blocks of `tiles` M tiles of tile_rows rows, on `slots` places.
+void plan_tiles(PromptAttnParams& p, int tile_rows, int tiles, int key_tile_log2, int64_t slots) {
+  const int group = p.hq / p.hkv;
   p.tile_rows = tile_rows;
-  p.key_tile_log2 = bf16 ? 7 : 6;
-  p.key_tile = 1 << p.key_tile_log2;
-  p.sub = pa::largest_divisor(group, tile_rows);
+  p.key_tile_log2 = key_tile_log2;
+  p.key_tile = 1 << key_tile_log2;
+  p.sub = largest_divisor(group, tile_rows);
   p.tile_heads = p.hq / p.sub;
   p.tiles_per_kv = group / p.sub;
   p.tile_tokens = tile_rows / p.sub;
@@ -130,22 +128,45 @@ size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int
   p.by_kv = index_divisor(p.tiles_per_kv);
   p.by_sub = index_divisor(p.sub);
   p.level_step = prompt_level_step(p.bounds.max_ctx, p.bounds.max_tokens, p.block_tokens);
-  const int64_t w = p.block_tokens, B = p.batch;
-  const int64_t by_total = prompt_places(p.bounds.n_total, p.batch, p.block_tokens), by_longest = B * ((p.bounds.max_tokens + w - 1) / w);
-  p.blocks = (int)(by_total < by_longest ? by_total : by_longest);
-  p.places = (int)by_total;
-  const int64_t units = (int64_t)p.blocks * p.tile_heads;
-  const int64_t key_tiles = ((int64_t)p.bounds.max_ctx + p.bounds.max_tokens + p.key_tile - 1) / p.key_tile;
-  p.piece_tiles = pa::choose_piece(units, key_tiles, p.batch, sms);
+  const int64_t places = prompt_places(p.bounds.n_total, p.batch, p.block_tokens);
+  const int64_t longest = (int64_t)p.batch * ((p.bounds.max_tokens + p.block_tokens - 1) / p.block_tokens);
+  p.blocks = (int)(places < longest ? places : longest);
+  p.places = (int)places;
+  const int64_t key_tiles = ((int64_t)p.bounds.max_ctx + p.bounds.max_tokens + p.key_tile - 1) >> key_tile_log2;
+  p.piece_tiles = choose_piece((int64_t)p.blocks * p.tile_heads, key_tiles, p.batch, slots);
   p.splits = (int)((key_tiles + p.piece_tiles - 1) / p.piece_tiles);
-  const size_t bytes = p.splits == 1 ? 0 : (size_t)p.places * p.tile_heads * p.splits * tiles * tile_rows * (p.head_dim + 2) * sizeof(float);
+}
+}  // namespace pa
+
+size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int sms) {
+  if (bf16) {
+    // A CTA an SM.  Measured (us by the pieces' length, the rule's in brackets): one token after 4096 of 32/8 heads, 8
+    // units of 33 tiles, 1: 17.5, [2: 12.7], 4: 12.8, 8: 15.7, uncut 42; after 32768, 10: 42.6, [14: 34.6], 17: 33.0, 20: 34.3;
+    // eight ragged contexts up to 4096, 5: 27.3, [11: 25.7], 14: 27.4, 17: 30.8, uncut 48; four equal ones, 7: 27.1,
+    // [9: 22.5], 12: 24.2; sixteen (128 units) 17: 59.1, [uncut 50.4]; 61 tokens of 64/8 heads after 32707, 20: 71.6, [29: 54],
+    // 40: 62; 256 tokens after 8192, 14: 52, [17: 41], 25: 51.
+    pa::plan_tiles(p, 128, 2, 7, sms);
+  } else if ((int64_t)p.bounds.max_tokens * (p.hq / p.hkv) <= 16) {
+    // Blocks of 16 rows, four CTAs an SM: one token after 2000 in four sequences of 8 heads, D = 64, 28.5 us (blocks
+    // of 64 rows 32.3); pieces of 1: 30.5, [2: 28.5], 4: 37.0, 8: 52.
+    pa::plan_tiles(p, 16, 1, 6, 4 * (int64_t)sms);
+  } else {
+    // Blocks of 64 rows, one CTA an SM for D = 128, else two; prompts see half of their keys on average, so that twice
+    // the pieces are asked for.  500 tokens of 8 heads, D = 64, [1: 19], 2: 25, 4: 40; 50 tokens after 1500 of 32/8 heads,
+    // D = 128, 3: 68, 6: 59, [7: 66], 10: 92.  (128 rows a block: 2048 tokens of 8 heads, D = 64, 254 us, 64 rows 236;
+    // D = 128, 452 and 266.)
+    const int64_t slots = (p.head_dim == 128 ? 1 : 2) * (int64_t)sms;
+    pa::plan_tiles(p, 64, 1, 6, p.bounds.max_tokens > p.bounds.max_ctx ? 2 * slots : slots);
+  }
+  const size_t rows = (size_t)p.places * p.tile_heads * p.splits * (p.block_tokens / p.tile_tokens) * p.tile_rows;
+  const size_t bytes = p.splits == 1 ? 0 : rows * (p.head_dim + 2) * sizeof(float);
   if (bytes > scratch) {
+    p.piece_tiles *= p.splits;
     p.splits = 1;
-    p.piece_tiles = (int)key_tiles;
   }
   p.by_splits = index_divisor(p.splits);
   if (p.splits == 1) return 0;
-  p.part_ml = p.part_o + (size_t)p.places * p.tile_heads * p.splits * tiles * tile_rows * p.head_dim;
+  p.part_ml = p.part_o + rows * p.head_dim;
   return bytes;
 }
 
