@@ -718,6 +718,13 @@ ptd_status check_prompt(const ptd_prompt* p) {
   return p->batch <= PTD_MAX_PROMPT_BATCH ? PTD_OK : PTD_ERR_UNSUPPORTED;
 }
 
+// (a paged cache's page sizes are powers of two)
+int page_log2(const ptd_kv_cache* c) {
+  int n = 0;
+  while ((2 << n) <= c->page_size) ++n;
+  return n;
+}
+
 ptd::PromptBounds prompt_bounds(const ptd_prompt* p, const ptd_kv_cache* c) {
   return {p->total_tokens, p->max_tokens, p->max_ctx,
           c->page_size > 0 ? (int64_t)c->max_pages * c->page_size : (int64_t)c->seq_capacity};
@@ -752,6 +759,7 @@ ptd::PromptAttnParams prompt_attention_params(const ptd_prompt* prompt, const pt
   p.hkv = cache->num_kv_heads;
   p.head_dim = cache->head_dim;
   p.page_size = cache->page_size;
+  p.page_log2 = page_log2(cache);
   p.seq_capacity = cache->seq_capacity;
   p.num_pages = cache->num_pages;
   p.max_pages = cache->max_pages;
@@ -797,6 +805,7 @@ ptd_status ptd_prompt_slots(const ptd_prompt* prompt, const ptd_kv_cache* cache,
   p.batch = prompt->batch;
   p.bounds = prompt_bounds(prompt, cache);
   p.page_size = cache->page_size;
+  p.page_log2 = page_log2(cache);
   p.seq_capacity = cache->seq_capacity;
   p.num_pages = cache->num_pages;
   p.max_pages = cache->max_pages;

@@ -17,7 +17,7 @@ struct PromptSlotsParams {
   const int32_t* ctx_lens;
   int batch;
   PromptBounds bounds;
-  int page_size, seq_capacity, num_pages, max_pages;
+  int page_size, page_log2, seq_capacity, num_pages, max_pages;
   const int32_t* block_table;
   // the page pool: free_pages NULL without one
   int32_t* free_pages;
@@ -75,7 +75,7 @@ struct PromptAttnParams {
   int blocks;                  // upper bound of the batch's blocks of tokens (per head tile)
   int places;                  // of the blocks' partials (per head tile)
   int splits, piece_tiles;     // a block's keys are cut into pieces of piece_tiles key tiles, at most `splits` (1: uncut)
-  int page_size, seq_capacity, num_pages, max_pages;
+  int page_size, page_log2, seq_capacity, num_pages, max_pages;
   float scale_log2;            // scale * log2(e)
 };
 

@@ -78,9 +78,9 @@ __global__ void __launch_bounds__(kThreads) prompt_simt_kernel(const PromptAttnP
     int64_t row = -1;
     if (key < end) {
       if (p.page_size > 0) {
-        const int page = p.block_table[(size_t)u.b * p.max_pages + key / p.page_size];
+        const int page = p.block_table[(size_t)u.b * p.max_pages + (key >> p.page_log2)];
         if (page >= 0 && page < p.num_pages)
-          row = ((int64_t)p.layer * p.num_pages + page) * p.page_size + key % p.page_size;
+          row = ((int64_t)p.layer * p.num_pages + page) * p.page_size + (key & (p.page_size - 1));
         else
           atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
       } else {

@@ -260,9 +260,9 @@ __device__ __forceinline__ void add_bad(const PromptAttnParams& p, float* o, int
   for (int key = key0; key <= key1; ++key) {
     size_t r;
     if (kPaged) {
-      const int pg = p.block_table[(size_t)b * p.max_pages + key / p.page_size];
+      const int pg = p.block_table[(size_t)b * p.max_pages + (key >> p.page_log2)];
       if (pg < 0 || pg >= p.num_pages) continue;
-      r = ((size_t)p.layer * p.num_pages + pg) * p.page_size + key % p.page_size;
+      r = ((size_t)p.layer * p.num_pages + pg) * p.page_size + (key & (p.page_size - 1));
     } else {
       r = ((size_t)p.layer * p.batch + b) * p.seq_capacity + key;
     }
@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t armed = 0, checked = 0;   // a bit per ring place: its barrier's turn (full; loaded, for the check)
       int steps = 0, done = 0;      // steps begun, and known to be done
       int step_of = -1;             // lane i: the step of the tile in ring place i
-      const int page_log2 = kPaged ? 31 - __clz(p.page_size) : 0, per_tile = kPaged ? 128 >> page_log2 : 1;
+      const int per_tile = kPaged ? 128 >> p.page_log2 : 1;
       const uint32_t page_bytes = kPaged ? (uint32_t)p.page_size * 128u : 0u;   // of half the columns
       // waits until the next ring place is free
       auto place = [&]() {
@@ -546,7 +546,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           ++it;
           j = -1;
           search_at = n > 2 ? n - 2 : n - 1;
-          end_page = kPaged ? (u.ctx + u.token0 + u.tokens + p.page_size - 1) >> page_log2 : 0;
+          end_page = kPaged ? (u.ctx + u.token0 + u.tokens + p.page_size - 1) >> p.page_log2 : 0;
           bt = kPaged ? p.block_table + (size_t)b * p.max_pages : nullptr;
           next_page = page_of(0);
         }

@@ -25,9 +25,6 @@ PTD_HD bool prompt_sequence_ok(const PromptBounds& p, int off0, int off1, int ct
          (int64_t)ctx + (off1 - off0) <= p.capacity;
 }
 
-// Pages for `len` positions.
-PTD_HD int pages_for(int64_t len, int page_size) { return (int)((len + page_size - 1) / page_size); }
-
 // A sequence's blocks of `width` tokens, as the attention orders them: block i of a sequence has the key
 // first + i, first = ctx / width, which grows with the keys it sees.
 struct PromptBlocks {

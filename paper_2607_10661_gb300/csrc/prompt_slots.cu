@@ -62,7 +62,8 @@ __global__ void __launch_bounds__(kThreads) prompt_slots_kernel(const PromptSlot
   const int per = (B + kThreads - 1) / kThreads, b0 = min(B, t * per), b1 = min(B, b0 + per);
   bool bad = kPool && (f < 0 || f > p.num_pages);
   unsigned long long sum = 0ull;   // pages taken << 32 | given
-  auto need_of = [&](int b) { return pages_for((int64_t)ctx[b] + (off[b + 1] - off[b]), p.page_size); };
+  // (a valid sequence's positions fit its table row, and so an int)
+  auto need_of = [&](int b) { return (ctx[b] + (off[b + 1] - off[b]) + p.page_size - 1) >> p.page_log2; };
   for (int b = b0; b < b1; ++b) {
     const bool ok = prompt_sequence_ok(p.bounds, off[b], off[b + 1], ctx[b]) &&
                     (!kPool || (held[b] >= 0 && held[b] <= p.max_pages));
@@ -125,14 +126,16 @@ __global__ void __launch_bounds__(kThreads) prompt_slots_kernel(const PromptSlot
   };
   auto taken = [&](int r) { return r < G ? given(G - 1 - r) : p.free_pages[f - 1 - (r - G)]; };
   if (kPool && !refused) {
-    const int step = gridDim.x * kThreads;
-    for (int r = blockIdx.x * kThreads + t; r < T; r += step) {
+    // the last CTAs first: the first ones have the tokens
+    const int step = gridDim.x * kThreads, r0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kThreads + t;
+    for (int r = r0; r < T; r += step) {
       const int b = last_at_most(takes, B, r);
       p.table_out[(size_t)b * p.max_pages + held[b] + (r - takes[b])] = taken(r);
     }
-    for (int r = blockIdx.x * kThreads + t; r < G - T; r += step) p.free_pages[f + r] = given(r);
+    for (int r = r0; r < G - T; r += step) p.free_pages[f + r] = given(r);
   }
-  const int n0 = blockIdx.x * tokens_per_cta, n1 = min(p.bounds.n_total, n0 + tokens_per_cta);
+  const int n0 = (int)min((int64_t)p.bounds.n_total, (int64_t)blockIdx.x * tokens_per_cta);
+  const int n1 = min(p.bounds.n_total, n0 + tokens_per_cta);
   for (int n = n0 + t; n < n1; n += kThreads) {
     int slot = -1, pos = -1;
     if (!refused && n >= off[0] && n < off[B]) {
@@ -142,10 +145,10 @@ __global__ void __launch_bounds__(kThreads) prompt_slots_kernel(const PromptSlot
         if (p.page_size == 0) {
           slot = b * p.seq_capacity + pos;
         } else {
-          const int i = pos / p.page_size;
+          const int i = pos >> p.page_log2;
           const int page = !kPool || i < held[b] ? p.block_table[(size_t)b * p.max_pages + i] : taken(takes[b] + i - held[b]);
           if (page >= 0 && page < p.num_pages) {
-            slot = page * p.page_size + pos % p.page_size;
+            slot = (page << p.page_log2) + (pos & (p.page_size - 1));
           } else {
             pos = -1;
             atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
@@ -166,6 +169,7 @@ cudaError_t launch_prompt_slots(const PromptSlotsParams& p, int sms, cudaStream_
   int ctas = (p.bounds.n_total + ps::kThreads - 1) / ps::kThreads;
   if (ctas > sms) ctas = sms;
   const int per = (p.bounds.n_total + ctas - 1) / ctas;
+  if (pool && ctas < 4) ctas = 4;   // the pages move beside the tokens, not before them
   const auto kernel = pool ? ps::prompt_slots_kernel<true> : ps::prompt_slots_kernel<false>;
   if (smem > 48 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
