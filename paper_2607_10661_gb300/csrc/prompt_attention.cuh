@@ -47,6 +47,7 @@ struct Units {
       if (b < p.batch) s = load_sequence(p, b, bad);
       if (b0 == 0) mine = s;
       if (prompt_has_levels(p.batch)) {
+#pragma unroll 1
         for (int i = 0; i < min(32, p.batch - b0); ++i)
           from_level += blocks_from({__shfl_sync(0xffffffffu, s.blocks.first, i), __shfl_sync(0xffffffffu, s.blocks.count, i)}, m);
       }

@@ -23,6 +23,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <climits>
 #include <cmath>
 #include <cstdint>
 
@@ -70,14 +71,18 @@ constexpr uint32_t kOffTmemPtr = kOffBar + kBars * 8;
 constexpr uint32_t kOffAbort = kOffTmemPtr + 4;
 constexpr uint32_t kOffClaim = (kOffAbort + 4 + 15) / 16 * 16;   // the scheduler's answer, 16 bytes
 
-// A bounded wait of a warp (mbar_wait_warp), its loop out of line: the roles' code together is larger than the
-// instruction caches, and what is not run often should not lie between what is.
-static __device__ __forceinline__ bool wait_longer(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* dev_status) {
-  return mbar_wait_warp(bar, parity, abort_flag, dev_status);
-}
+// A bounded wait of a warp for the barrier's phase: false when it, or another role, has given up.  A try_wait that
+// finds the phase open sleeps until it ends, for 1.95 us at most (measured), so that 2^20 tries are 2 s.  (The roles'
+// code is larger than the near instruction caches: a short loop in place of mbar_wait_warp's clock.)
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* dev_status) {
-  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  return wait_longer(bar, parity, abort_flag, dev_status);
+#pragma unroll 1
+  for (int tries = 0; tries < (1 << 20); ++tries) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if (__any_sync(0xffffffffu, *abort_flag != 0)) return false;
+  }
+  *abort_flag = 1;
+  atomicMax(dev_status, (int)PTD_ERR_TIMEOUT);
+  return false;
 }
 
 // One lane of the warp, always the same; the compiler knows such a branch to be one thread's, and its copies then
@@ -148,12 +153,13 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool has_
   for (int c = 0; c < 4; ++c) tmem_ld32(tS + (uint32_t)c * 32u, r[c]);
   tmem_ld_wait();
   if (need_mask) {
+    const int all = (int)__reduce_min_sync(0xffffffffu, (unsigned)max(last, 0));   // what every row of the warp sees
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      const int n = last - c * 32;   // the chunk's last visible key
-      const uint32_t seen = n < 0 ? 0u : (n >= 31 ? 0xFFFFFFFFu : (2u << n) - 1u);
+      if (all < c * 32 + 31) {
 #pragma unroll
-      for (int e = 0; e < 32; ++e) r[c][e] = ((seen >> e) & 1u) ? r[c][e] : __float_as_uint(-INFINITY);
+        for (int e = 0; e < 32; ++e) r[c][e] = c * 32 + e <= last ? r[c][e] : __float_as_uint(-INFINITY);
+      }
     }
   }
   float a[4];
@@ -229,19 +235,16 @@ __device__ __forceinline__ void issue_pv(uint32_t s_tmem, uint32_t v_desc, bool 
 }
 constexpr int kEarly = 5;   // products of a group of eight before the other issuer is let go
 
-// 64 bytes of a row.  A warp's rows lie apart, so a store costs a pass a row whatever its width: 32 bytes at a
+// 32 bytes of a row.  A warp's rows lie apart, so a store costs a pass a row whatever its width: 32 bytes at a
 // time where the output allows.
-__device__ __forceinline__ void store_row(uint4* dst, const uint32_t (&w)[16], bool wide) {
+__device__ __forceinline__ void store_row(uint4* dst, const uint32_t (&w)[8], bool wide) {
   if (wide) {
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + 2 * g), "r"(w[8 * g]),
-                   "r"(w[8 * g + 1]), "r"(w[8 * g + 2]), "r"(w[8 * g + 3]), "r"(w[8 * g + 4]), "r"(w[8 * g + 5]),
-                   "r"(w[8 * g + 6]), "r"(w[8 * g + 7])
-                   : "memory");
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
   } else {
-#pragma unroll
-    for (int g = 0; g < 4; ++g) dst[g] = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
+    dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
   }
 }
 
@@ -253,7 +256,7 @@ __device__ __forceinline__ uint32_t finite_or_zero(uint32_t w) {
   return w;
 }
 
-// 32 outputs of a row (columns c ..) plus the infinities and NaN of V at keys [key0, key1], which the V check
+// 16 outputs of a row (columns c ..) plus the infinities and NaN of V at keys [key0, key1], which the V check
 // took out of the products.
 template <bool kPaged>
 __device__ __forceinline__ void add_bad(const PromptAttnParams& p, float* o, int b, int kv, int c, int key0, int key1) {
@@ -268,7 +271,7 @@ __device__ __forceinline__ void add_bad(const PromptAttnParams& p, float* o, int
     }
     const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + (r * p.hkv + kv) * 128 + c;
 #pragma unroll 1
-    for (int e = 0; e < 32; ++e) {
+    for (int e = 0; e < 16; ++e) {
       const float x = __bfloat162float(v[e]);
       if (!isfinite(x)) o[e] += x;
     }
@@ -436,7 +439,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       pa::Units units(p);
       if (units.bad) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
       __syncwarp();
-      int x = (int)blockIdx.x, claims = 0;   // the unit's number; claims made
+      constexpr int kNoUnit = INT_MAX;
+      int x = (int)blockIdx.x, claims = 0;   // the next unit's number, if it is known; claims made
       bool claimed = false;                  // the last one has not been read yet
       auto claim = [&]() {
         if (lane == 0) {
@@ -499,8 +503,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       while (ok) {
         if (search) {   // a unit with keys, or the end of the grid
           search = found = false;
-          for (bool first = claims == 0 && it == 0; !found; first = false) {
-            if (!first) {
+#pragma unroll 1
+          while (!found) {
+            if (x == kNoUnit) {   // (the first unit is the CTA's own)
               if (!claimed) claim();
               if (!(ok = wait_warp(bar(kClaim), (uint32_t)(claims - 1) & 1u, abort_flag, p.dev_status))) break;
               claimed = false;
@@ -510,6 +515,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (x < 0) break;
             }
             found = units.find(p, x, u);
+            x = kNoUnit;
           }
           if (!ok) break;
         }
@@ -552,14 +558,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         const int row_k = j + 1 < n ? row_of(j + 1, next_page) : 0;
         next_page = page_of(j + 2);
-        if (j >= 0) {
-          if (!(ok = place())) break;
-          copy(&map_v, kt0 + j >= edge, j, row_v);
+#pragma unroll 1
+        for (int k = 0; k < 2 && ok; ++k) {   // V of tile j, then K of tile j + 1
+          const int i = j + k;
+          if (i < 0 || i >= n) continue;
+          if ((ok = place())) copy(k ? &map_k : &map_v, k == 0 && kt0 + j >= edge, i, k ? row_k : row_v);
         }
-        if (j + 1 < n) {
-          if (!(ok = place())) break;
-          copy(&map_k, false, j + 1, row_k);
-        }
+        if (!ok) break;
         row_v = row_k;
         if (j == -1) {
 #pragma unroll
@@ -612,9 +617,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint4* tile = reinterpret_cast<uint4*>(smem + kOffRing + (size_t)vs * kTileBytes);
           const int r0 = max(0, first - (kt0 + j) * 128), r1 = min(128, end - (kt0 + j) * 128);
           const int half = ((lane >> 3) & 1) * 1024;   // two rows a turn, sixteen lanes each
+#pragma unroll 8
           for (int r = r1 + (lane >> 4); r < 128; r += 2) tile[half + r * 8 + (lane & 7)] = make_uint4(0, 0, 0, 0);
           uint32_t bad = 0u;
-#pragma unroll 4
+#pragma unroll 8
           for (int r = r0 + (lane >> 4); r < r1; r += 2) {
             const uint4 v = tile[half + r * 8 + (lane & 7)];
             bad |= exponent_full(v.x) | exponent_full(v.y) | exponent_full(v.z) | exponent_full(v.w);
@@ -675,39 +681,40 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool bad = sg->bad != 0;
       const int piece = sg->piece;
       const float inv = piece < 0 ? 1.f / l_run : 1.f;   // a piece stays unnormalised
-      uint4* dst = reinterpret_cast<uint4*>(p.out) + (((size_t)sg->row0 + my_token) * p.hq + sg->head0 + my_head) * 16;
-      const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0;
       float4* po = reinterpret_cast<float4*>(p.part_o) + (size_t)max(piece, 0) * 32 * 256 + t * 128 + row;
       if (piece >= 0 && row_valid)
         reinterpret_cast<float2*>(p.part_ml)[(size_t)piece * 256 + t * 128 + row] =
             n > 0 ? make_float2(m_run, l_run) : make_float2(-INFINITY, 0.f);
       if (n > 0 && any_row) {
+        const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0;
+        uint4* dst = reinterpret_cast<uint4*>(p.out) + (((size_t)sg->row0 + my_token) * p.hq + sg->head0 + my_head) * 16;
 #pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
-          uint32_t r[32];
-          tmem_ld32(tO + (uint32_t)c * 32u, r);
+        for (int c = 0; c < 8; ++c) {
+          uint32_t r[16];
+          tmem_ld16(tO + (uint32_t)c * 16u, r);
           tmem_ld_wait();
+          if (bad && row_valid) {
+            float ob[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) ob[e] = __uint_as_float(r[e]) * inv;
+            add_bad<kPaged>(p, ob, sg->b, sg->kv, c * 16, max(kt0, sg->edge) * 128, min(pos, (kt0 + n) * 128 - 1));
+#pragma unroll
+            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(ob[e]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * inv);
+          }
           if (row_valid) {
-            float o[32];
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(r[e]) * inv;
-            if (bad) {
-              float ob[32];
-#pragma unroll
-              for (int e = 0; e < 32; ++e) ob[e] = o[e];
-              add_bad<kPaged>(p, ob, sg->b, sg->kv, c * 32, max(kt0, sg->edge) * 128, min(pos, (kt0 + n) * 128 - 1));
-#pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = ob[e];
-            }
             if (piece < 0) {
-              uint32_t w[16];
+              uint32_t w[8];
 #pragma unroll
-              for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(o[2 * e], o[2 * e + 1]);
-              store_row(dst + c * 4, w, wide);
+              for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]));
+              store_row(dst + c * 2, w, wide);
             } else {
 #pragma unroll
-              for (int g = 0; g < 8; ++g)
-                po[(size_t)(c * 8 + g) * 256] = make_float4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
+              for (int g = 0; g < 4; ++g)
+                po[(size_t)(c * 4 + g) * 256] = make_float4(__uint_as_float(r[4 * g]), __uint_as_float(r[4 * g + 1]),
+                                                            __uint_as_float(r[4 * g + 2]), __uint_as_float(r[4 * g + 3]));
             }
           }
           __syncwarp();
