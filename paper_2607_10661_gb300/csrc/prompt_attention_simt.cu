@@ -56,8 +56,8 @@ __global__ void __launch_bounds__(kThreads) prompt_simt_kernel(const PromptAttnP
   __shared__ int found_s;
   __shared__ int64_t key_row[2][kKeys];   // cache rows of a tile's keys, -1: none
   const int t = threadIdx.x, x = t & 15, y = t >> 4;
-  if (t == 0) grid_launch_dependents();
   grid_dependency_wait();
+  if (t == 0) grid_launch_dependents();   // (after the wait: the merge reads the batch's arrays before its own)
   if (t < 32) {
     Units units(p);
     if (units.bad) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
