@@ -503,16 +503,18 @@ ptd_status ptd_pipeline_destroy(ptd_pipeline* pipeline);
  * C_b + i.  total_tokens is the number of rows that the buffers have: token_offsets[B] may be smaller
  * (a batch padded to a captured size), and what lies behind the last sequence is padding. */
 #define PTD_MAX_PROMPT_BATCH 8192
+#define PTD_MAX_PROMPT_TOKENS (1 << 30) /* of total_tokens, and of max_ctx + max_tokens */
 typedef struct {
   int32_t batch;                /* host: B, 1 .. PTD_MAX_PROMPT_BATCH                   */
-  int32_t total_tokens;         /* host: rows of the token buffers, >= token_offsets[B] */
+  int32_t total_tokens;         /* host: rows of the token buffers, >= token_offsets[B], >= 1 */
   int32_t max_tokens;           /* host: upper bound of a sequence's new tokens (>= 1)  */
   int32_t max_ctx;              /* host: upper bound of every ctx_lens[b] (>= 0)        */
   const int32_t* token_offsets; /* [B+1], token_offsets[0] >= 0, non-decreasing         */
   const int32_t* ctx_lens;      /* [B]                                                  */
 } ptd_prompt;
 
-/* The free pages of a paged cache, and the pages that each sequence of a batch holds. */
+/* The free pages of a paged cache, and the pages that each sequence of a batch holds (a page is free, or held by
+ * one sequence, or outside the pool's care). */
 typedef struct {
   int32_t* free_pages;          /* [num_pages], a stack: entries [0, free_count[0]) are free pages */
   const int32_t* free_count;    /* [1]                                                  */
@@ -539,8 +541,8 @@ typedef struct {
  *   Without `pages` a sequence out of range (n_b outside 0 .. max_tokens, C_b outside 0 .. max_ctx, more
  *     positions than the cache's row holds, offsets outside the batch) sets PTD_ERR_INVALID_BATCH and its
  *     tokens get -1.  In both forms so does a token whose page number is outside the cache.
- * free_count, held, the offsets and ctx_lens must not overlap what the call writes.  A cache layer has fewer
- * than 2^31 rows.  One launch. */
+ * What the call writes overlaps nothing else that it reads or writes (PTD_ERR_INVALID_ARG).  A cache layer has
+ * fewer than 2^31 rows.  One launch. */
 ptd_status ptd_prompt_slots(const ptd_prompt* prompt, const ptd_kv_cache* cache, const ptd_page_pool* pages,
                             int32_t* slots, int32_t* positions, int32_t* dev_status, void* stream);
 
@@ -553,7 +555,7 @@ ptd_status ptd_prompt_slots(const ptd_prompt* prompt, const ptd_kv_cache* cache,
  *     views of one fused product's rows.
  *   q_out: as q, q_out_stride apart; it may be q itself (same pointer and stride), and overlaps q, k, v
  *     in no other way.  slots of different tokens differ.
- * D even, at most 256.  One launch. */
+ * D even, at most 256; (num_q_heads + 2 num_kv_heads) * D below 2^31.  One launch. */
 ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t layer,
                                   const int32_t* slots, const int32_t* positions, const void* q, int64_t q_stride,
                                   int32_t num_q_heads, const void* k, int64_t k_stride, const void* v,
@@ -565,7 +567,8 @@ ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* 
  *     out[n][h] = sum_j softmax_j(scale * <q[n][h], K[b][j]>) V[b][j],   j in [0, C_b + i].
  * The new tokens' own K/V are in the cache already (ptd_prompt_rope_append).
  *   q [total_tokens][num_q_heads][D], tokens q_stride elements apart; out [total_tokens][num_q_heads][D] back to
- *     back; both of cache->dtype and 16-byte aligned, q_stride times the element size a multiple of 16.
+ *     back; both of cache->dtype and 16-byte aligned, q_stride times the element size a multiple of 16; out
+ *     overlaps no input.
  *     fp32 accumulation and softmax statistics; the weights are rounded to bf16 for a bf16 cache.
  *   Rows behind the last sequence are left as they were, as are those of a sequence out of range (see
  *     ptd_prompt_slots; PTD_ERR_INVALID_BATCH).  A page number outside the cache sets PTD_ERR_INVALID_BATCH too:

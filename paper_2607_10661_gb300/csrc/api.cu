@@ -712,10 +712,13 @@ ptd_status ptd_tree_rope_append(const ptd_tree* tree, const ptd_kv_cache* cache,
 
 namespace {
 ptd_status check_prompt(const ptd_prompt* p) {
-  if (!p || p->batch < 1 || p->total_tokens < 1 || p->max_tokens < 1 || p->max_ctx < 0 || !p->token_offsets || !p->ctx_lens ||
-      (int64_t)p->max_ctx + p->max_tokens > INT32_MAX)
+  if (!p || p->batch < 1 || p->total_tokens < 1 || p->max_tokens < 1 || p->max_ctx < 0 || !p->token_offsets || !p->ctx_lens)
     return PTD_ERR_INVALID_ARG;
-  return p->batch <= PTD_MAX_PROMPT_BATCH ? PTD_OK : PTD_ERR_UNSUPPORTED;
+  // (2^30: a position or a row plus a tile, a page or a CTA's share stays an int)
+  return p->batch <= PTD_MAX_PROMPT_BATCH && p->total_tokens <= PTD_MAX_PROMPT_TOKENS &&
+                 (int64_t)p->max_ctx + p->max_tokens <= PTD_MAX_PROMPT_TOKENS
+             ? PTD_OK
+             : PTD_ERR_UNSUPPORTED;
 }
 
 // (a paged cache's page sizes are powers of two)
@@ -781,18 +784,22 @@ ptd_status ptd_prompt_slots(const ptd_prompt* prompt, const ptd_kv_cache* cache,
         !pages->new_free_count || pages->block_table != cache->block_table)
       return PTD_ERR_INVALID_ARG;
     if ((int64_t)prompt->batch * cache->max_pages > INT32_MAX) return PTD_ERR_UNSUPPORTED;
-    // what the call reads while it writes: other CTAs still read it
-    const size_t B4 = (size_t)prompt->batch * 4, N4 = (size_t)prompt->total_tokens * 4;
-    const void* read[4] = {prompt->token_offsets, prompt->ctx_lens, pages->held, pages->free_count};
-    const size_t nread[4] = {B4 + 4, B4, B4, 4};
-    const void* written[6] = {pages->new_held, pages->new_free_count, slots, positions, pages->free_pages, pages->block_table};
-    const size_t nwritten[6] = {B4, 4, N4, N4, (size_t)cache->num_pages * 4, B4 * cache->max_pages};
-    for (int i = 0; i < 6; ++i) {
-      for (int j = 0; j < 4; ++j)
-        if (overlap(written[i], nwritten[i], read[j], nread[j])) return PTD_ERR_INVALID_ARG;
-      for (int j = 0; j < i; ++j)
-        if (overlap(written[i], nwritten[i], written[j], nwritten[j])) return PTD_ERR_INVALID_ARG;
-    }
+  }
+  // what is written overlaps nothing else that the call touches: other CTAs still read it, or write it too
+  const size_t B4 = (size_t)prompt->batch * 4, N4 = (size_t)prompt->total_tokens * 4;
+  const size_t table = cache->page_size > 0 ? B4 * cache->max_pages : 0;
+  const struct Range {
+    const void* at;
+    size_t bytes;
+  } ranges[10] = {{slots, N4}, {positions, N4}, {pages ? pages->new_held : nullptr, B4}, {pages ? pages->new_free_count : nullptr, 4},
+                  {pages ? pages->free_pages : nullptr, (size_t)cache->num_pages * 4}, {table ? cache->block_table : nullptr, table},
+                  {prompt->token_offsets, B4 + 4}, {prompt->ctx_lens, B4}, {pages ? pages->held : nullptr, B4},
+                  {pages ? pages->free_count : nullptr, 4}};
+  for (int i = 0; i < (pages ? 6 : 2); ++i)   // (written: the first two, and with a pool the first six)
+    for (int j = i + 1; j < 10; ++j)
+      if (ranges[i].at && ranges[j].at && overlap(ranges[i].at, ranges[i].bytes, ranges[j].at, ranges[j].bytes))
+        return PTD_ERR_INVALID_ARG;
+  if (pages) {
     p.free_pages = pages->free_pages;
     p.free_count = pages->free_count;
     p.held = pages->held;
@@ -833,6 +840,7 @@ ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* 
       D / 2 > ptd::kMaxRopeHalf || !slots || !positions || !q || !k || !v || !q_out || !dev_status || q_stride < qe ||
       q_out_stride < qe || k_stride < ke || v_stride < ke || !(rope_base > 1.f) || !std::isfinite(rope_base))
     return PTD_ERR_INVALID_ARG;
+  if (qe + 2 * ke > INT32_MAX) return PTD_ERR_UNSUPPORTED;   // a token's elements, counted in an int
   const size_t es = dtype_size(cache->dtype);
   if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) |
        reinterpret_cast<uintptr_t>(q_out)) % es != 0)

@@ -18,7 +18,7 @@ namespace {
 
 PyObject *g_tensor, *g_i32, *g_f32, *g_bf16, *g_raw_stream, *g_get_device;
 PyObject *s_is_cuda, *s_is_contiguous, *s_dtype, *s_data_ptr, *s_nbytes, *s_shape, *s_stride, *s_c, *s_get_device, *s_k,
-    *s_block_table, *s_sizes;
+    *s_block_table, *s_sizes, *s_ctx_lens;
 
 #define PTD_FUNCTIONS(X)                                                                                            \
   X(ptd_tree_attention) X(ptd_topk_draft) X(ptd_verify_greedy) X(ptd_kv_compact) X(ptd_verify_sampling)             \
@@ -550,6 +550,7 @@ PyObject* prompt_slots(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int32_t* positions = g.i32_of(prompt->total_tokens);
   g.on(a[5]);
   int32_t* status = g.i32();
+  g.on_attr(a[0], s_ctx_lens);
   g.on_attr(a[1], s_k);
   g.on_current();
   void* s = g.stream();
@@ -603,6 +604,7 @@ PyObject* prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   size_t wsb;
   if (a[7] != Py_None) g.on(a[7]);
   void* ws = g.optional(&wsb);
+  g.on_attr(a[0], s_ctx_lens);
   g.on_attr(a[1], s_k);
   g.on_current();
   void* s = g.stream();
@@ -667,6 +669,7 @@ PyMODINIT_FUNC PyInit__ptdcall(void) {
   s_get_device = PyUnicode_InternFromString("get_device");
   s_k = PyUnicode_InternFromString("k");
   s_block_table = PyUnicode_InternFromString("block_table");
+  s_ctx_lens = PyUnicode_InternFromString("ctx_lens");
   s_sizes = PyUnicode_InternFromString("sizes");
   return PyModule_Create(&module);
 }

@@ -26,7 +26,7 @@ MAX_TREE_NODES = 128
 MAX_TOPK = 16
 MAX_EXPAND = 16
 POOL_KIDS = 8
-MAX_PROMPT_BATCH = 8192
+MAX_PROMPT_BATCH, MAX_PROMPT_TOKENS = 8192, 1 << 30
 
 EXPORTED = (
     "ptd_attention_workspace_size", "ptd_tree_attention", "ptd_topk_draft", "ptd_verify_greedy",
@@ -606,6 +606,7 @@ class Prompt:
             raise ValueError("token_offsets needs one entry more than ctx_lens")
         self.c = _Prompt(self.batch, self.total_tokens, int(max_tokens), int(max_ctx),
                          _dev(token_offsets, "token_offsets", torch.int32), _dev(ctx_lens, "ctx_lens", torch.int32))
+        _one_device(token_offsets, ctx_lens)
 
 
 class PagePool:

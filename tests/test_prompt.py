@@ -174,9 +174,15 @@ def test_prompt_slots_refusals(lib):
     bad = ptd.INVALID_ARG
     assert call(None, ok_c) == bad
     for p in (_prompt(ptd, batch=0), _prompt(ptd, total=0), _prompt(ptd, max_tokens=0), _prompt(ptd, max_ctx=-1),
-              _prompt(ptd, offsets=None), _prompt(ptd, ctx=None), _prompt(ptd, max_tokens=2**31 - 1)):
+              _prompt(ptd, offsets=None), _prompt(ptd, ctx=None)):
         assert call(p, ok_c) == bad
-    assert call(_prompt(ptd, batch=8193), ok_c) == ptd.UNSUPPORTED
+    for p in (_prompt(ptd, batch=8193), _prompt(ptd, max_tokens=2**31 - 1), _prompt(ptd, max_ctx=2**30 - 7),
+              _prompt(ptd, total=2**30 + 1)):
+        assert call(p, ok_c) == ptd.UNSUPPORTED
+    for pool in (None, "default"):   # slots on positions, the offsets, the contexts, the block table
+        assert call(ok_p, ok_c, pool=pool, positions=4 * A + 36) == bad
+        for at in (A + 8, A + 4096 - 36, A + 8192 + 76):
+            assert call(ok_p, ok_c, pool=pool, slots=at) == bad and call(ok_p, ok_c, pool=pool, positions=at) == bad
     assert call(ok_p, ok_c, slots=None) == bad and call(ok_p, ok_c, positions=None) == bad
     assert call(ok_p, ok_c, status=None) == bad
     assert call(ok_p, _cache(ptd, page=0), pool=ptd._PagePool(7 * A, 8 * A, 9 * A, 10 * A, 11 * A, None)) == bad
@@ -211,6 +217,8 @@ def test_prompt_rope_append_refusals(lib):
                dict(cache=_cache(ptd, d=127, hkv=16), qs=10**6, ks=10**6, vs=10**6),
                dict(cache=_cache(ptd, d=264), qs=10**6, outs=10**6, ks=10**6, vs=10**6)):
         assert call(**kw) == ptd.INVALID_ARG, kw
+    # 2^31 elements a token
+    assert call(hq=2**24 - 16, qs=2**31, outs=2**31) == ptd.UNSUPPORTED
     # cache rows of 24 bytes: not a multiple of 16
     assert call(cache=_cache(ptd, dtype=ptd.F32, hkv=1, d=6)) == ptd.UNSUPPORTED
 
@@ -308,19 +316,21 @@ def test_native_prompt_calls_keep_to_the_current_device(lib, monkeypatch):
     from paper_2607_10661_gb300 import ptd
 
     class Holder:
-        def __init__(self, c, k=None):
-            self.c, self.k, self.block_table = c, k, None
+        def __init__(self, c, k=None, ctx_lens=None):
+            self.c, self.k, self.block_table, self.ctx_lens = c, k, None, ctx_lens
 
     try:
-        for here, current, stray in ((0, 0, None), (1, 1, None), (1, 0, None), (0, 0, "k"), (0, 0, "q")):
+        for here, current, stray in ((0, 0, None), (1, 1, None), (1, 0, None), (0, 0, "k"), (0, 0, "q"), (0, 0, "ctx")):
             calls, Fake = _native_with(ptd, monkeypatch, here, current)
-            prompt = Holder(_prompt(ptd))
+            prompt = Holder(_prompt(ptd), None, Fake(device=1 - here if stray == "ctx" else here))
             cache = Holder(_cache(ptd, page=0, hkv=2), Fake(torch.bfloat16, 1 - here if stray == "k" else here))
             q, x, i = Fake(torch.bfloat16, 1 - here if stray == "q" else here), Fake(torch.bfloat16), Fake()
             taken = here == current and stray is None
             want = -ptd.INVALID_ARG if taken else None
             assert calls.prompt_attention(prompt, cache, 9, q, x, i, 0.0, None, 0) == want
-            assert calls.prompt_rope_append(prompt, cache, 9, i, i, q, x, x, x, 1e4, i, 0) == want
+            # (the rotary call reads nothing of the batch on the device)
+            assert calls.prompt_rope_append(prompt, cache, 9, i, i, q, x, x, x, 1e4, i, 0) == \
+                (want if stray != "ctx" else -ptd.INVALID_ARG)
             prompt.c.batch = 0   # refused by the library
             assert calls.prompt_slots(prompt, cache, None, i, i, i, 0) == (want if stray != "q" else -ptd.INVALID_ARG)
     finally:
