@@ -21,9 +21,10 @@ struct Unit {
   int place;               // of the partials: (the block's place * tile_heads + head tile) * splits + piece
 };
 
-// Sequence b of the batch.
+// Sequence b of the batch (read from L2, which has it before any grid that waits for the batch's writer goes on: the
+// merge reads it before its own wait).
 __device__ __forceinline__ PromptSequence load_sequence(const PromptAttnParams& p, int b, bool& bad) {
-  const int off0 = p.token_offsets[b], off1 = p.token_offsets[b + 1], ctx = p.ctx_lens[b];
+  const int off0 = __ldcg(p.token_offsets + b), off1 = __ldcg(p.token_offsets + b + 1), ctx = __ldcg(p.ctx_lens + b);
   if (!prompt_sequence_ok(p.bounds, off0, off1, ctx)) {
     bad = true;
     return {0, 0, 0, {0, 0}};
