@@ -391,7 +391,9 @@ def _rope_tolerance(x, y, dtype):
 @pytest.mark.parametrize("dtype,hq,hkv,d,page,positions", [
     (BF16, 32, 8, 128, 16, [0, 1, 7, 131071, 4096, 40000]), (F32, 8, 8, 64, 0, [0, 5, 100000, 3]),
     (BF16, 10, 2, 128, 32, list(range(100, 1300))), (BF16, 3, 1, 48, 16, [9, 8, 70000]), (F32, 4, 2, 6, 0, [4, 11, 2]),
-    (F32, 32, 8, 128, 64, list(range(50))), (BF16, 4, 4, 256, 16, [33] * 3)])
+    (F32, 32, 8, 128, 64, list(range(50))), (BF16, 4, 4, 256, 16, [33] * 3),
+    # more tokens than places for CTAs: rows of several rounds, several tokens a CTA
+    (F32, 64, 8, 128, 0, list(range(700))), (BF16, 4, 2, 64, 16, list(range(6500))), (BF16, 2, 1, 32, 0, list(range(12001)))])
 @pytest.mark.parametrize("fused", [False, True])
 def test_rope_append_matches_oracle(dtype, hq, hkv, d, page, positions, fused):
     n, pad, layers = len(positions), 3, 2
