@@ -13,8 +13,7 @@
 //   0       scheduler and TMA producer: claims the next unit before the last tiles of this one are asked for;
 //           K and V tiles into a ring of five, Q.
 //   1, 2    MMA issuers of M tile 0 and 1: S_t = Q_t K^T, then PV_t, S_t' | PV_t', S_t'' | .., in turns, so that
-//           one M tile's softmax runs beside the other's products.  Products go out at the tensor core's pace:
-//           an issuer's waits and commits would leave the pipe idle, so the other is let go a few products early.
+//           one M tile's softmax runs beside the other's products.
 //   3       V check: of key tiles that some row sees in part, infinities and NaN of V are set to 0 (a
 //           weight of 0 must not meet them) and noted; the rows that see such a key add it at the end.
 //   4 - 11  softmax of M tile 0 (4 - 7) and 1 (8 - 11), a thread a row: running maximum, moved only when
@@ -209,14 +208,13 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool has_
   tc_fence_before();
 }
 
-// Instructions [kBegin, kEnd) of the eight of S_t = Q_t K^T, and of O_t (+)= P_t V (see tc::issue_s, issue_pv), from
+// The eight instructions of S_t = Q_t K^T, and [kBegin, kEnd) of those of O_t (+)= P_t V (see tc::issue_s, issue_pv), from
 // one elected lane: against a lane chosen by a predicate on each instruction 16384 tokens of 64/8 heads take 2472 us
 // instead of 2653, 8192 of 32/8 heads 300 instead of 330 (graph replays).
-template <int kBegin, int kEnd>
 __device__ __forceinline__ void issue_s(uint32_t s_tmem, uint32_t q_desc, uint32_t k_desc) {
   if (elect_lane()) {
 #pragma unroll
-    for (int kk = kBegin; kk < kEnd; ++kk) {
+    for (int kk = 0; kk < 8; ++kk) {
       const uint32_t o = (uint32_t)(kk >> 2) * (kHalfBytes >> 4) + (uint32_t)(kk & 3) * 2u;
       mma_ss_if(1u, s_tmem, q_desc + o, k_desc + o, tc::kDescHi, tc::kIdescS, kk > 0 ? 1u : 0u);
     }
@@ -233,10 +231,9 @@ __device__ __forceinline__ void issue_pv(uint32_t s_tmem, uint32_t v_desc, bool 
   }
   __syncwarp();
 }
-constexpr int kEarly = 5;   // products of a group of eight before the other issuer is let go
 
 // 32 bytes of a row.  A warp's rows lie apart, so a store costs a pass a row whatever its width: 32 bytes at a
-// time where the output allows.
+// time where the output allows (16 at a time: ragged prompts 33.7 us instead of 30.5, 4096 tokens 87.8 instead of 84.4).
 __device__ __forceinline__ void store_row(uint4* dst, const uint32_t (&w)[8], bool wide) {
   if (wide) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]),
@@ -278,7 +275,8 @@ __device__ __forceinline__ void add_bad(const PromptAttnParams& p, float* o, int
   }
 }
 
-// kPages: 0 for a contiguous cache, else the most pages that a key tile has (2: pages of 64 and 128, 8: of 16 and 32).
+// kPages: 0 for a contiguous cache, else the most pages that a key tile has (2: pages of 64 and 128, 8: of 16 and 32;
+// 4096 tokens of 32/8 heads in pages of 128 take 84.4 us with 2 and 90.2 with 8).
 template <int kPages>
 __global__ void __launch_bounds__(kThreads, 1)
     prompt_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -384,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (mine > 0) {
           if (!(ok = wait(kQFull + t, qs++))) break;
           tc_fence_after();
-          issue_s<0, 8>(s_tmem, dq, dk + k_tile);
+          issue_s(s_tmem, dq, dk + k_tile);
           commit(kSFull + t);
           if (mine == 1) commit(kQEmpty + t);
         }
@@ -399,13 +397,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             issue_pv<0, 4>(s_tmem, dv + v_tile, j > 0);
             if (!(ok = wait(kPFull + t, ps++))) break;
             tc_fence_after();
-            issue_pv<4, kEarly>(s_tmem, dv + v_tile, j > 0);
-            if (j + 1 == mine) pass_turn(j);
-            issue_pv<kEarly, 8>(s_tmem, dv + v_tile, j > 0);
+            issue_pv<4, 8>(s_tmem, dv + v_tile, j > 0);
+            if (j + 1 < mine) issue_s(s_tmem, dq, dk + k_tile);
+            pass_turn(j);
             if (j + 1 < mine) {
-              issue_s<0, kEarly>(s_tmem, dq, dk + k_tile);
-              pass_turn(j);
-              issue_s<kEarly, 8>(s_tmem, dq, dk + k_tile);
               commit(kSFull + t);
               if (j + 2 == mine) commit(kQEmpty + t);
             } else {
