@@ -575,10 +575,10 @@ ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* 
  *     the sequence's outputs are then unspecified.
  *   K and V of a token are read for the tokens that see it only: an infinity or NaN in a later one changes nothing.
  *   scale: <= 0 selects 1/sqrt(D).  D: as ptd_tree_attention (128 for bf16; 32, 64 or 128 for fp32).
- *   workspace: scratch of ptd_prompt_attention_workspace_size bytes, 16-byte aligned, for batches of few rows,
- *     whose keys are split between CTAs (partials merged by a second kernel); with less (even none) the
- *     call runs unsplit.  Calls that may overlap on the GPU need scratch of their own.
- * One launch, or two where keys are split. */
+ *   workspace: scratch of ptd_prompt_attention_workspace_size bytes (of the current device), 16-byte aligned, for
+ *     batches of few rows, whose keys are split between CTAs (partials merged by a second kernel); with less
+ *     (even none) the call runs unsplit.  Calls that may overlap on the GPU need scratch of their own.
+ * One launch, or two where keys may be split. */
 size_t ptd_prompt_attention_workspace_size(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t num_q_heads);
 ptd_status ptd_prompt_attention(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t layer, const void* q,
                                 int64_t q_stride, int32_t num_q_heads, float scale, void* out, void* workspace,

@@ -923,8 +923,9 @@ ptd_status ptd_prompt_attention(const ptd_prompt* prompt, const ptd_kv_cache* ca
     st = cuda_status(ptd::launch_prompt_attn_simt(p, s));
   }
   if (st != PTD_OK) return st;
-  if (p.splits > 1 && (st = cuda_status(ptd::launch_prompt_attn_merge(p, bf16, s))) != PTD_OK) return st;
-  g_last_launches = p.splits > 1 ? 2 : 1;
+  const bool cut = p.splits > 1 || p.cut_ctas > 0;
+  if (cut && (st = cuda_status(ptd::launch_prompt_attn_merge(p, bf16, s))) != PTD_OK) return st;
+  g_last_launches = cut ? 2 : 1;
   return PTD_OK;
 }
 

@@ -15,7 +15,7 @@ namespace pa {
 constexpr int kMergeThreads = 256;
 constexpr int kMergeBatch = 8;   // pieces whose partials are in flight at a time
 
-// The rows of one split block, from its pieces: O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s, M the
+// The rows of one split block (by pieces of one length, or by the lengths on the device), from its pieces: O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s, M the
 // maximum of the m_s (a row that saw no key of a piece has l_s = 0, and its O_s was not written).  x of the grid is
 // a block's place and head tile, y a share of its rows and columns: a thread takes one row and four columns,
 // consecutive threads consecutive rows, as the partials lie.  Bound by the latency of the chain sequence, (m, l),
@@ -29,41 +29,64 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
   const int place = divide((int)blockIdx.x, p.by_heads), tile = (int)blockIdx.x - place * p.tile_heads;
   int row0 = 0, tokens = 0, ctx = 0;
   bool bad = false, found = false;
-  for (int b0 = 0; b0 < p.batch && !found; b0 += 32) {   // every warp looks for the sequence
-    const int b = b0 + lane;
+  int pieces = 0;              // of the block: the first at place `first`, piece s at rest + s * step
+  size_t first = 0, rest = 0;
+  int step = 1;
+  if (p.cut_ctas > 0) {        // (place: the sequence)
     PromptSequence s = {0, 0, 0, {0, 0}};
-    if (b < p.batch) s = load_sequence(p, b, bad);
-    const int i = place - block_place(s.row0, b, p.by_block);
-    const int src = WarpLanes{}.first(i >= 0 && i < s.blocks.count);
-    if (src < 0) continue;
-    found = true;
-    const int at = __shfl_sync(0xffffffffu, i, src) * p.block_tokens;
-    row0 = __shfl_sync(0xffffffffu, s.row0, src) + at;
-    tokens = min(p.block_tokens, __shfl_sync(0xffffffffu, s.tokens, src) - at);
-    ctx = __shfl_sync(0xffffffffu, s.ctx, src) + at;
+    if (lane < p.batch) s = load_sequence(p, lane, bad);
+    const LengthCut by_lengths(p, s, place, bad);
+    const PromptCut cut = by_lengths.cut;
+    s = load_sequence(p, place, bad);
+    row0 = s.row0, tokens = s.tokens, ctx = s.ctx;
+    const int n = sequence_tiles(p, s), x = by_lengths.before + tile * n;
+    if (cut.shares > 0 && n > 0) {
+      const int c = share_of(x, cut);
+      pieces = share_of(x + n - 1, cut) - c + 1;
+      found = true;
+      rest = 2 * (size_t)c, step = 2;
+      first = rest + (share_begin(c, cut) < x ? 1 : 0);
+    }
+  } else {
+    for (int b0 = 0; b0 < p.batch && !found; b0 += 32) {   // every warp looks for the sequence
+      const int b = b0 + lane;
+      PromptSequence s = {0, 0, 0, {0, 0}};
+      if (b < p.batch) s = load_sequence(p, b, bad);
+      const int i = place - block_place(s.row0, b, p.by_block);
+      const int src = WarpLanes{}.first(i >= 0 && i < s.blocks.count);
+      if (src < 0) continue;
+      found = true;
+      const int at = __shfl_sync(0xffffffffu, i, src) * p.block_tokens;
+      row0 = __shfl_sync(0xffffffffu, s.row0, src) + at;
+      tokens = min(p.block_tokens, __shfl_sync(0xffffffffu, s.tokens, src) - at);
+      ctx = __shfl_sync(0xffffffffu, s.ctx, src) + at;
+    }
   }
   grid_dependency_wait();   // the partials belong to the attention
   if (!found) return;
-  const int tiles = (ctx + tokens + p.key_tile - 1) >> p.key_tile_log2;
-  if (tiles <= p.piece_tiles) return;   // one piece: written by the attention
+  if (p.cut_ctas == 0) {
+    pieces = (((ctx + tokens + p.key_tile - 1) >> p.key_tile_log2) + p.piece_tiles - 1) / p.piece_tiles;
+    first = rest = (size_t)blockIdx.x * p.splits;
+  }
+  if (pieces <= 1) return;   // written by the attention
   const int rows = tokens * p.sub, groups = p.head_dim / 4, used = p.tile_tokens * p.sub;
   const int block_rows = p.block_tokens / p.tile_tokens * p.tile_rows;
-  const size_t piece0 = (size_t)blockIdx.x * p.splits;
   for (int e = blockIdx.y * kMergeThreads + threadIdx.x; e < rows * groups; e += gridDim.y * kMergeThreads) {
     const int c = e / rows, r = e - c * rows;
     const int at = r < used ? r : p.tile_rows + r - used;
-    const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + piece0 * block_rows + at;
-    const float4* po = reinterpret_cast<const float4*>(p.part_o) + (piece0 * groups + c) * block_rows + at;
+    const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + at;
+    const float4* po = reinterpret_cast<const float4*>(p.part_o) + (size_t)c * block_rows + at;
     float M = -INFINITY, L = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = 0; s0 * p.piece_tiles < tiles; s0 += kMergeBatch) {   // the loads of a batch are in flight together
+    for (int s0 = 0; s0 < pieces; s0 += kMergeBatch) {   // the loads of a batch are in flight together
       float2 x[kMergeBatch];
       float4 o[kMergeBatch];
 #pragma unroll
       for (int i = 0; i < kMergeBatch; ++i) {
-        const bool there = (s0 + i) * p.piece_tiles < tiles;
-        x[i] = there ? __ldcg(ml + (size_t)(s0 + i) * block_rows) : make_float2(-INFINITY, 0.f);
-        if (there) o[i] = __ldcg(po + (size_t)(s0 + i) * groups * block_rows);
+        const bool there = s0 + i < pieces;
+        const size_t piece = s0 + i == 0 ? first : rest + (size_t)(s0 + i) * step;
+        x[i] = there ? __ldcg(ml + piece * block_rows) : make_float2(-INFINITY, 0.f);
+        if (there) o[i] = __ldcg(po + piece * groups * block_rows);
       }
       float m = M;
 #pragma unroll
@@ -139,14 +162,40 @@ void plan_tiles(PromptAttnParams& p, int tile_rows, int tiles, int key_tile_log2
 }
 }  // namespace pa
 
+int prompt_most_shares(const PromptAttnParams& p) {
+  const int64_t tiles = (((int64_t)p.bounds.max_ctx + p.bounds.max_tokens + p.key_tile - 1) >> p.key_tile_log2) * p.batch * p.tile_heads;
+  return (int)(tiles / 2 < p.cut_ctas ? tiles / 2 : p.cut_ctas);
+}
+
 size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int sms) {
+  p.cut_ctas = 0;
   if (bf16) {
-    // A CTA an SM.  Measured (us by the pieces' length, the rule's in brackets): one token after 4096 of 32/8 heads, 8
-    // units of 33 tiles, 1: 17.5, [2: 12.7], 4: 12.8, 8: 15.7, uncut 42; after 32768, 10: 42.6, [14: 34.6], 17: 33.0, 20: 34.3;
-    // eight ragged contexts up to 4096, 5: 27.3, [11: 25.7], 14: 27.4, 17: 30.8, uncut 48; four equal ones, 7: 27.1,
-    // [9: 22.5], 12: 24.2; sixteen (128 units) 17: 59.1, [uncut 50.4]; 61 tokens of 64/8 heads after 32707, 20: 71.6, [29: 54],
-    // 40: 62; 256 tokens after 8192, 14: 52, [17: 41], 25: 51.
+    // A CTA an SM.  Pieces of one length (us by their key tiles, the rule's in brackets): one token after 4096 of 32/8
+    // heads, 8 units of 33 tiles, 1: 17.5, [2: 12.7], 4: 12.8, 8: 15.7, uncut 42; after 32768, 10: 42.6, [14: 34.6], 17: 33.0,
+    // 20: 34.3; 61 tokens of 64/8 heads after 32707, 20: 71.6, [29: 54], 40: 62; 256 tokens after 8192, 14: 52, [17: 41], 25: 51.
     pa::plan_tiles(p, 128, 2, 7, sms);
+    // Several sequences of one block each (decoding): cut by the lengths on the device, where as many units as two rounds
+    // of CTAs may gain by it.  One token of 32/8 heads (us, pieces of one length or uncut in brackets): 8 ragged contexts up
+    // to 4096 22.3 [24.6], equal ones 30.9 [42.0], 12 ragged 28.6 [50.5], 16 ragged up to 8000 53.4 [93.2], 24 equal ones
+    // of 8000 129.6 [183.5], 32 of 4000 92.2 [99.6]; what it loses: the merge's launch where the units stay whole, 18 of
+    // 2000 31.6 [30.5], and the search, 2 of 4000 15.5 [14.6], 32 ragged up to 4000 56.5 [53.1].
+    const int64_t units = (int64_t)p.batch * p.tile_heads;
+    const int64_t key_tiles = ((int64_t)p.bounds.max_ctx + p.bounds.max_tokens + p.key_tile - 1) >> p.key_tile_log2;
+    if (p.batch > 1 && p.bounds.max_tokens <= p.block_tokens && units <= 2 * (int64_t)sms && key_tiles > (units > sms ? 15 : 4) &&
+        sms <= kMostCutCtas && units * key_tiles <= kMostCutTiles) {
+      p.piece_tiles = (int)key_tiles;
+      p.splits = 1;
+      p.by_splits = index_divisor(1);
+      p.cut_ctas = sms;
+      const size_t rows = 2 * (size_t)prompt_most_shares(p) * 256;
+      const size_t bytes = rows * (p.head_dim + 2) * sizeof(float);
+      if (bytes <= scratch) {
+        p.part_ml = p.part_o + rows * p.head_dim;
+        return bytes;
+      }
+      p.cut_ctas = 0;
+      return 0;
+    }
   } else if ((int64_t)p.bounds.max_tokens * (p.hq / p.hkv) <= 16) {
     // Blocks of 16 rows, four CTAs an SM: one token after 2000 in four sequences of 8 heads, D = 64, 28.5 us (blocks
     // of 64 rows 32.3); pieces of 1: 30.5, [2: 28.5], 4: 37.0, 8: 52.
@@ -175,7 +224,8 @@ cudaError_t launch_prompt_attn_merge(const PromptAttnParams& p, bool bf16, cudaS
   const auto kernel = bf16 ? pa::prompt_merge_kernel<__nv_bfloat16> : pa::prompt_merge_kernel<float>;
   int64_t rows = (int64_t)(p.bounds.max_tokens < p.block_tokens ? p.bounds.max_tokens : p.block_tokens) * p.sub;
   const unsigned shares = (unsigned)((rows * (p.head_dim / 4) + pa::kMergeThreads - 1) / pa::kMergeThreads);
-  return launch_chained(kernel, dim3((unsigned)(p.places * p.tile_heads), shares), dim3(pa::kMergeThreads), 0, stream, 0, p);
+  const int blocks = p.cut_ctas > 0 ? p.batch : p.places;
+  return launch_chained(kernel, dim3((unsigned)(blocks * p.tile_heads), shares), dim3(pa::kMergeThreads), 0, stream, 0, p);
 }
 
 }  // namespace ptd

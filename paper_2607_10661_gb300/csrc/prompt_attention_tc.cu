@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (x < 0) break;
             }
             found = units.find(p, x, u);
-            x = kNoUnit;
+            if (!found || !units.more(x)) x = kNoUnit;
           }
           if (!ok) break;
         }
@@ -577,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
           }
         }
-        if (j == search_at - 1) claim();
+        if (j == search_at - 1 && x == kNoUnit) claim();
         search = j == search_at;
         ++steps;
         ++j;
@@ -734,7 +734,8 @@ cudaError_t launch_prompt_attn_tc(const CUtensorMap& map_k, const CUtensorMap& m
   const auto kernel = p.page_size == 0 ? pt::prompt_tc_kernel<0> : (p.page_size >= 64 ? pt::prompt_tc_kernel<2> : pt::prompt_tc_kernel<8>);
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pt::kSmemBytes);
   if (e != cudaSuccess) return e;
-  return launch_chained(kernel, dim3((unsigned)(p.blocks * p.tile_heads * p.splits)), dim3(pt::kThreads), pt::kSmemBytes,
+  const int units = p.blocks * p.tile_heads * p.splits, shares = p.cut_ctas > 0 ? prompt_most_shares(p) : 0;
+  return launch_chained(kernel, dim3((unsigned)(units > shares ? units : shares)), dim3(pt::kThreads), pt::kSmemBytes,
                         stream, 0, map_k, map_v, map_q, p);
 }
 

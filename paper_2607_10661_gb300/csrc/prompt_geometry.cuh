@@ -62,6 +62,35 @@ PTD_HD int prompt_level_step(int max_ctx, int max_tokens, int width) { return (m
 
 PTD_HD bool prompt_has_levels(int batch) { return batch > 1 && batch <= kOrderedBatch; }
 
+// Batches whose sequences are one block each (decoding) may be cut by the lengths on the device, so that the SMs' work
+// evens out: the key tiles of all units, sequence after sequence and head tile after head tile, in equal shares, one a
+// CTA.  A unit that is not in one share has partials, at place 2 c if it begins share c, else 2 c + 1.
+struct PromptCut {
+  int shares, tiles;   // shares 0: the units are better left whole
+};
+constexpr int kMostCutCtas = 255, kMostCutTiles = 1 << 24;   // their product stays in 32 bits
+
+// The cut for `ctas` CTAs at a time: `tiles` key tiles of `units` units (at most two rounds of them), the longest of
+// `longest`.  In eighths of a key tile: units whole, the longest, or two of the mean length and a change of unit; in
+// shares, a share, partials and their merge, and a change of unit at each unit's end.
+constexpr uint32_t kMergeCost = 4, kChangeCost = 8;
+PTD_HD PromptCut prompt_cut(int tiles_, int units_, int longest_, int ctas_) {
+  const uint32_t tiles = (uint32_t)tiles_, units = (uint32_t)units_, longest = (uint32_t)longest_, ctas = (uint32_t)ctas_;
+  if (tiles < 2u) return {0, tiles_};
+  uint32_t whole = 8u * longest;
+  if (units > ctas) {
+    const uint32_t two = 16u * tiles / units;
+    whole = (whole > two ? whole : two) + kChangeCost;
+  }
+  const uint32_t shares = tiles / 2u < ctas ? tiles / 2u : ctas;
+  const uint32_t even = (8u * tiles + kChangeCost * units) / shares + kMergeCost + kChangeCost;
+  return {even < whole ? (int)shares : 0, tiles_};
+}
+PTD_HD int share_begin(int c, const PromptCut& cut) { return (int)((uint32_t)c * (uint32_t)cut.tiles / (uint32_t)cut.shares); }
+PTD_HD int share_of(int x, const PromptCut& cut) {   // the share that has tile x
+  return (int)((((uint32_t)x + 1u) * (uint32_t)cut.shares - 1u) / (uint32_t)cut.tiles);
+}
+
 // Where the last search ended: a search for a later block goes on from there.
 struct PromptCursor {
   int level, upto, above;   // a level, the blocks of it and higher ones, and of higher ones (upto 0: none known)

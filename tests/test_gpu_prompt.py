@@ -130,6 +130,13 @@ CASES = {
     "bounds-above-lengths": dict(seqs=[(40, 30), (0, 2)], hq=8, hkv=2, page=16, pad=90, max_ctx=3000, max_tokens=800),
     "many-sequences": dict(seqs=[(i % 37, i % 5) for i in range(700)], hq=4, hkv=2, page=16),
     "decoding-64-split": dict(seqs=[(300 + 37 * i, 1) for i in range(64)], hq=16, hkv=2, page=16),
+    "even-ragged-decoding": dict(seqs=[(5000, 1), (1, 1), (0, 0), (3000, 1), (127, 1), (700, 1)], hq=32, hkv=8, page=16, pad=2),
+    "even-equal-contiguous": dict(seqs=[(4095, 1)] * 8, hq=32, hkv=8),
+    "even-chunks-two-m-tiles": dict(seqs=[(4000, 60), (2900, 33), (100, 64), (6000, 1)], hq=16, hkv=4, page=64, layers=2, layer=1),
+    "even-40-sequences": dict(seqs=[(0, 1)] * 33 + [(9000, 2), (0, 0), (7000, 1), (256, 1), (6500, 2), (128, 1), (127, 1)],
+                              hq=8, hkv=1, page=32),
+    "even-uncut": dict(seqs=[(900 + i, 1) for i in range(16)], hq=32, hkv=8, page=128, max_ctx=20000),
+    "even-group5": dict(seqs=[(2500, 3), (2600, 50)], hq=10, hkv=2, page=16),
     "ordered-100": dict(seqs=[(17 * i % 701, 1 + i % 3) for i in range(100)], hq=8, hkv=1, page=32, max_ctx=2000),
     "f32-decoding-split": dict(seqs=[(200 + 11 * i, 1) for i in range(40)], hq=2, hkv=2, d=32, dtype=F32),
     "f32-64": dict(seqs=RAGGED, hq=4, hkv=4, d=64, dtype=F32, pad=2),

@@ -102,6 +102,82 @@ def test_blocks_are_numbered_longest_first(tmp_path):
         assert line.split() == want, (width, seqs)
 
 
+def test_even_shares_cover_every_unit_once(tmp_path):
+    """The shares cut the units' key tiles without gaps; the merge finds a unit's pieces where their CTAs put them, at
+    places of their own."""
+    src, exe = tmp_path / "shares.cpp", tmp_path / "shares"
+    src.write_text(r"""
+#include <cstdio>
+#include <vector>
+#include "prompt_geometry.cuh"
+int main() {
+  int ctas, units, cut = 0;
+  while (std::scanf("%d %d", &ctas, &units) == 2) {
+    std::vector<int> n(units), first(units);
+    int tiles = 0, longest = 0, there = 0;
+    for (int i = 0; i < units; ++i) {
+      if (std::scanf("%d", &n[i]) != 1) return 1;
+      first[i] = tiles;
+      tiles += n[i], there += n[i] > 0, longest = n[i] > longest ? n[i] : longest;
+    }
+    const ptd::PromptCut c0 = ptd::prompt_cut(tiles, there, longest, ctas);
+    const int shares = c0.shares;
+    if (shares == 0) continue;
+    ++cut;
+    if (shares < 0 || shares > ctas || shares > tiles / 2) return 2;
+    std::vector<std::vector<int>> pieces(units);   // places, in order
+    std::vector<int> taken(2 * shares, 0);
+    int next = 0;
+    for (int c = 0; c < shares; ++c) {
+      const int x0 = ptd::share_begin(c, c0), x1 = ptd::share_begin(c + 1, c0);
+      if (x0 != next || x1 <= x0) return 3;
+      for (int i = 0; i < units; ++i) {
+        const int a = x0 > first[i] ? x0 : first[i], b = x1 < first[i] + n[i] ? x1 : first[i] + n[i];
+        if (a >= b) continue;
+        if (a == first[i] && b == first[i] + n[i]) continue;   // whole
+        const int place = 2 * c + (a > x0 ? 1 : 0);
+        if (taken[place]++) return 4;
+        pieces[i].push_back(place);
+      }
+      next = x1;
+    }
+    if (next != tiles) return 5;
+    for (int i = 0; i < units; ++i) {
+      if (n[i] == 0) continue;
+      const int c = ptd::share_of(first[i], c0), count = ptd::share_of(first[i] + n[i] - 1, c0) - c + 1;
+      if (count == 1) {
+        if (!pieces[i].empty()) return 6;
+        continue;
+      }
+      if ((int)pieces[i].size() != count) return 7;
+      for (int s = 0; s < count; ++s)
+        if (pieces[i][s] != (s ? 2 * (c + s) : 2 * c + (ptd::share_begin(c, c0) < first[i] ? 1 : 0))) return 8;
+    }
+  }
+  if (ptd::prompt_cut(0, 0, 0, 152).shares != 0 || ptd::prompt_cut(1, 1, 1, 152).shares != 0) return 9;
+  const int most = ptd::kMostCutTiles;   // (no product leaves 32 bits)
+  for (int units : {8, 100, 300, 510}) {
+    const ptd::PromptCut c = ptd::prompt_cut(most, units, most / 2, 255);
+    if (c.shares != 255 || ptd::share_begin(255, c) != most || ptd::share_of(most - 1, c) != 254 || ptd::share_of(0, c) != 0)
+      return 10;
+  }
+  std::printf("%d\n", cut);
+  return 0;
+}
+""")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I", os.path.join(ROOT, "paper_2607_10661_gb300", "csrc"), str(src),
+                    "-o", str(exe)], check=True)
+    rng = random.Random(9)
+    cases = [(152, [20]), (152, [5000] * 8), (152, [33, 0, 1, 2] * 16), (3, [7, 8]), (1, [5, 6]), (152, [33] * 256),
+             (255, [1 << 20] * 16), (152, [63] * 8), (152, [9] * 75), (152, [9] * 77)]
+    for _ in range(400):
+        top = rng.choice([2, 8, 40, 300])
+        cases.append((rng.choice([1, 2, 7, 148, 152]), [rng.randrange(top + 1) for _ in range(rng.randrange(1, 400))]))
+    r = subprocess.run([str(exe)], input="\n".join(f"{c} {len(n)} " + " ".join(map(str, n)) for c, n in cases),
+                       capture_output=True, text=True)
+    assert r.returncode == 0 and int(r.stdout) > 50, (r.returncode, r.stdout)
+
+
 def test_index_division_is_exact(tmp_path):
     src, exe = tmp_path / "divide.cpp", tmp_path / "divide"
     src.write_text(r"""
