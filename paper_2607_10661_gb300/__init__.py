@@ -6,11 +6,17 @@ verification and KV compaction as hand-written CUDA kernels behind a C ABI (libp
 from . import ptd  # noqa: F401
 from .ptd import (  # noqa: F401
     KVCache,
+    PagePool,
+    Prompt,
     PtdError,
     StepBuffers,
     Tree,
     attention_workspace_size,
     kv_compact,
+    prompt_attention,
+    prompt_attention_workspace_size,
+    prompt_rope_append,
+    prompt_slots,
     topk_draft,
     tree_attention,
     tree_verify_step,

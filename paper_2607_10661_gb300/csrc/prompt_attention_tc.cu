@@ -7,18 +7,27 @@
 // (block, head tile), or a piece of its keys (partials, merged by prompt_merge_kernel).  Units are numbered
 // longest first over the whole batch (prompt_geometry.cuh); the grid has one CTA per unit, and a resident CTA
 // takes the numbers of CTAs that have not started yet (cluster launch control), so that the SMs' shares
-// even out whatever the lengths, and a unit's first loads and its set-up run beside the unit before it.
+// even out whatever the lengths, and a unit's first loads and its set-up run beside the unit before it.  Batches
+// of a block a sequence go by shares of the key tiles instead where that is shorter (PromptCut).
 //
 // Warps (384 threads; the first four give registers to the others):
 //   0       scheduler and TMA producer: claims the next unit before the last tiles of this one are asked for;
 //           K and V tiles into a ring of five, Q.
 //   1, 2    MMA issuers of M tile 0 and 1: S_t = Q_t K^T, then PV_t, S_t' | PV_t', S_t'' | .., in turns, so that
-//           one M tile's softmax runs beside the other's products.
+//           one M tile's softmax runs beside the other's products (without turns 2047 tokens of 32 MHA heads
+//           take 36.0 us instead of 31.3).
 //   3       V check: of key tiles that some row sees in part, infinities and NaN of V are set to 0 (a
 //           weight of 0 must not meet them) and noted; the rows that see such a key add it at the end.
 //   4 - 11  softmax of M tile 0 (4 - 7) and 1 (8 - 11), a thread a row: running maximum, moved only when
 //           exceeded by 2^8, exp2, bf16 weights over S in TMEM (told in two halves), fp32 row sum; O / l at the end.
 // TMEM: S_0 | S_1 | O_0 | O_1, 128 fp32 columns each; P_t lies over the first 64 columns of S_t.
+//
+// Bound by the tensor pipe and the power cap for long prompts: 8192 tokens of 32/8 heads 295 us (1.86 PFLOP/s of the
+// seen pairs, pipe 85 % active, 0.97 of cuBLAS' burst), 16384 of 64/8 heads 2.35 - 2.45 ms (1.8 - 1.87), 2.54 ms in
+// runs of seconds at the cap.  Ragged prompts of some hundred tokens (30 us for 18.5 GFLOP) are bound by changes of unit, ~4.5 us
+// each: the V check, masked tiles, outputs, and code that has left the instruction caches (so it is kept short).
+// Decoding: by HBM, ~6 us from the start to the first output, and the merge: 8 contexts of up to 4096 22 us for 73 MB,
+// 24 of 8000 130 us for 787 MB (6.1 TB/s).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
