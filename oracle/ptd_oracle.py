@@ -549,7 +549,7 @@ def causal_attention(q, k, v, ctx: int, scale: float | None = None):
     q, k, v = (np.asarray(x, np.float64) for x in (q, k, v))
     n, Hq, D = q.shape
     G = Hq // k.shape[1]
-    scale = 1.0 / math.sqrt(D) if scale is None else scale
+    scale = D ** -0.5 if scale is None else scale
     o, size = np.zeros_like(q), np.zeros_like(q)
     for h in range(Hq):
         for i in range(n):
