@@ -607,6 +607,38 @@ def test_captured_steps_with_changing_lengths():
         assert (o[at:] == 7.0).all()
 
 
+def test_captured_decoding_is_cut_anew_at_each_replay():
+    """One captured decoding call over lengths that change on the device: cut into shares or not, sequences that drop
+    out, and one out of range, whose row stays as it was."""
+    x = Batch([(6000, 1)] * 5, 16, 4, page=32, pad=3, seed=70)
+    ws = x.workspace()
+    gr = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr):
+        assert ptd.prompt_attention(x.prompt, x.cache, 0, x.q, x.out, x.status, workspace=ws) == 2
+    for ctx, new in (([6000] * 5, [1] * 5), ([0, 5999, 127, 2000, 128], [1] * 5), ([3, 1, 0, 100, 20], [1] * 5),
+                     ([4000, 0, 0, 10, 900], [1, 0, 0, 1, 1]), ([0] * 5, [0] * 5), ([700, 6001, 5000, 3000, 9], [1] * 5)):
+        bad = [c > 6000 for c in ctx]
+        off = np.concatenate([[0], np.cumsum(new)])
+        x.ctx_lens.copy_(torch.tensor(ctx, dtype=torch.int32))
+        x.token_offsets.copy_(torch.tensor(off, dtype=torch.int32))
+        x.out.fill_(7.0)
+        x.status.zero_()
+        ws.fill_(255)
+        gr.replay()
+        torch.cuda.synchronize()
+        assert int(x.status) == (ptd.INVALID_BATCH if any(bad) else 0)
+        for b in range(5):
+            if new[b] and bad[b]:
+                assert (x.out[off[b]] == 7.0).all()
+            elif new[b]:
+                k, v = x.kv(b)
+                q = x.q[off[b]:off[b] + 1].double().cpu().numpy()
+                ref, size = oracle.causal_attention(q, k, v, ctx[b])
+                tol = _attention_tolerance(q, k, v, ref, size, BF16)
+                assert (np.abs(x.out[off[b]:off[b] + 1].double().cpu().numpy() - ref) <= tol).all()
+        assert (x.out[off[-1]:] == 7.0).all()
+
+
 def test_calls_on_two_streams():
     """Batches with scratch of their own on two streams at once."""
     xs = [Batch([(3000 + 500 * i, 2), (40, 9)], 8, 2, page=16, seed=50 + i) for i in range(2)]
