@@ -75,6 +75,8 @@ struct PromptAttnParams {
   int blocks;                  // upper bound of the batch's blocks of tokens (per head tile)
   int places;                  // of the blocks' partials (per head tile)
   int cut_ctas;                // CTAs at a time of a cut by the lengths on the device (PromptCut); 0: none
+  int most_shares;             // of such a cut: what the scratch and the grid have room for
+  CutCosts costs;
   int splits, piece_tiles;     // a block's keys are cut into pieces of piece_tiles key tiles, at most `splits` (1: uncut)
   int page_size, page_log2, seq_capacity, num_pages, max_pages;
   float scale_log2;            // scale * log2(e)
@@ -84,8 +86,6 @@ struct PromptAttnParams {
 // tile_heads, tiles_per_kv, tile_tokens, block_tokens, tile_rows, key_tile, level_step, blocks, piece_tiles, splits and cut_ctas.
 // Returns the scratch that the cut takes (0: unsplit).
 size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int sms);
-// The most shares that a cut by the lengths may have (cut_ctas > 0).
-int prompt_most_shares(const PromptAttnParams& p);
 // bf16, D = 128.  map_k, map_v: boxes of 64 columns of one KV head and 128 rows (or a page's); map_q: of 64
 // columns, `sub` heads and tile_tokens tokens; 128-byte swizzle.
 cudaError_t launch_prompt_attn_tc(const CUtensorMap& map_k, const CUtensorMap& map_v, const CUtensorMap& map_q,

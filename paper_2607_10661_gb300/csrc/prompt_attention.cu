@@ -13,41 +13,122 @@ namespace ptd {
 namespace pa {
 
 constexpr int kMergeThreads = 256;
-constexpr int kMergeBatch = 8;   // pieces whose partials are in flight at a time
+
+// The pieces of a block: the first has its partials at place `first`, piece s at rest + s * step.
+struct Pieces {
+  int count;
+  size_t first, rest;
+  int step;
+};
+
+// Part `part` of `parts` of the merge of a block (its first row in out row0, head tile `tile`): a thread takes a row and four
+// columns of kAt blocks of elements at a time, kPieces pieces of each, all of whose loads are in flight together.
+template <typename T, int kAt, int kPieces>
+__device__ __forceinline__ void merge_part(const PromptAttnParams& p, const Pieces& from, int row0, int tokens, int tile, int part,
+                                           int parts) {
+  const int rows = tokens * p.sub, groups = p.head_dim / 4, used = p.tile_tokens * p.sub;
+  const int block_rows = p.block_tokens / p.tile_tokens * p.tile_rows, apart = parts * kMergeThreads;
+#pragma unroll 1
+  for (int e0 = part * kMergeThreads + threadIdx.x; e0 < rows * groups; e0 += kAt * apart) {
+    const float2* ml[kAt];
+    const float4* po[kAt];
+    float M[kAt], L[kAt];
+    float4 acc[kAt];
+#pragma unroll
+    for (int k = 0; k < kAt; ++k) {
+      const int e = min(e0 + k * apart, rows * groups - 1), c = e / rows, r = e - c * rows;   // (behind the last: the last)
+      const int at = r < used ? r : p.tile_rows + r - used;
+      ml[k] = reinterpret_cast<const float2*>(p.part_ml) + at;
+      po[k] = reinterpret_cast<const float4*>(p.part_o) + (size_t)c * block_rows + at;
+      M[k] = -INFINITY, L[k] = 0.f;
+      acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    for (int s0 = 0; s0 < from.count; s0 += kPieces) {
+      float2 x[kAt][kPieces];
+      float4 o[kAt][kPieces];
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const bool there = s0 + i < from.count;
+        const size_t piece = s0 + i == 0 ? from.first : from.rest + (size_t)(s0 + i) * from.step;
+#pragma unroll
+        for (int k = 0; k < kAt; ++k) {
+          x[k][i] = there ? __ldcg(ml[k] + piece * block_rows) : make_float2(-INFINITY, 0.f);
+          if (there) o[k][i] = __ldcg(po[k] + piece * groups * block_rows);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kAt; ++k) {
+        float m = M[k];
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i)
+          if (!(x[k][i].y == 0.f)) m = fmaxf(m, x[k][i].x);   // (not l > 0: a NaN among the scores has to reach the output)
+        const float old = M[k] == -INFINITY ? 0.f : exp2f(M[k] - m);
+        M[k] = m;
+        L[k] *= old, acc[k].x *= old, acc[k].y *= old, acc[k].z *= old, acc[k].w *= old;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          if (x[k][i].y == 0.f) continue;
+          const float w = exp2f(x[k][i].x - m);
+          L[k] += w * x[k][i].y;
+          acc[k].x += w * o[k][i].x;
+          acc[k].y += w * o[k][i].y;
+          acc[k].z += w * o[k][i].z;
+          acc[k].w += w * o[k][i].w;
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kAt; ++k) {
+      const int e = e0 + k * apart, c = e / rows, r = e - c * rows;
+      if (e >= rows * groups) break;
+      const float inv = 1.f / L[k];
+      const int token = divide(r, p.by_sub), head = tile * p.sub + r - token * p.sub;
+      T* dst = static_cast<T*>(p.out) + ((size_t)(row0 + token) * p.hq + head) * p.head_dim + c * 4;
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<uint2*>(dst) =
+            make_uint2(pack_bf16x2(acc[k].x * inv, acc[k].y * inv), pack_bf16x2(acc[k].z * inv, acc[k].w * inv));
+      } else {
+        *reinterpret_cast<float4*>(dst) = make_float4(acc[k].x * inv, acc[k].y * inv, acc[k].z * inv, acc[k].w * inv);
+      }
+    }
+  }
+}
 
 // The rows of one split block (by pieces of one length, or by the lengths on the device), from its pieces: O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s, M the
 // maximum of the m_s (a row that saw no key of a piece has l_s = 0, and its O_s was not written).  x of the grid is
-// a block's place and head tile, y a share of its rows and columns: a thread takes one row and four columns,
-// consecutive threads consecutive rows, as the partials lie.  Bound by the latency of the chain sequence, (m, l),
+// a block's place and head tile, or a boundary between shares of the cells, y a share of its rows and columns;
+// consecutive threads take consecutive rows, as the partials lie.  Bound by the latency of the chain sequence, (m, l),
 // partials; the sequence is found before the wait for the attention.
-template <typename T>
-__global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const PromptAttnParams p) {
+template <typename T, bool kMany>
+__global__ void __launch_bounds__(kMergeThreads, kMany ? 2 : 1) prompt_merge_kernel(const PromptAttnParams p) {
   if (threadIdx.x == 0) grid_launch_dependents();
   // (the attention lets this grid be placed after its own wait, so that the batch's arrays are complete in L2, where
   // load_sequence reads them; waiting first costs 0.5 us: eight contexts of 4096 24.75 -> 25.3)
   const int lane = threadIdx.x & 31;
-  const int place = divide((int)blockIdx.x, p.by_heads), tile = (int)blockIdx.x - place * p.tile_heads;
-  int row0 = 0, tokens = 0, ctx = 0;
+  int tile = 0, row0 = 0, tokens = 0, ctx = 0;
   bool bad = false, found = false;
-  int pieces = 0;              // of the block: the first at place `first`, piece s at rest + s * step
-  size_t first = 0, rest = 0;
-  int step = 1;
-  if (p.cut_ctas > 0) {        // (place: the sequence)
-    PromptSequence s = {0, 0, 0, {0, 0}};
-    if (lane < p.batch) s = load_sequence(p, lane, bad);
-    const LengthCut by_lengths(p, s, place, bad);
-    const PromptCut cut = by_lengths.cut;
-    s = load_sequence(p, place, bad);
-    row0 = s.row0, tokens = s.tokens, ctx = s.ctx;
-    const int n = sequence_tiles(p, s), x = by_lengths.before + tile * n;
-    if (cut.shares > 0 && n > 0) {
-      const int c = share_of(x, cut);
-      pieces = share_of(x + n - 1, cut) - c + 1;
+  Pieces from = {0, 0, 0, 1};
+  int part = blockIdx.y, parts = gridDim.y;
+  if (p.cut_ctas > 0) {        // x: a boundary between shares; the boundaries that cut a unit share its merge
+    PromptSequence mine = {0, 0, 0, {0, 0}};
+    if (lane < p.batch) mine = load_sequence(p, lane, bad);
+    const PromptCut cut = cut_by_lengths(p, mine, bad);
+    const int c = (int)blockIdx.x, at = c + 1 < cut.shares ? share_begin(c + 1, cut) : 0;
+    int b0 = 0, before = 0;
+    CutUnit u;
+    if (at > 0 && find_cut_unit(p, mine, at, b0, before, u) && at > u.first && at < u.first + u.tiles) {
+      tile = u.head;
+      row0 = u.s.row0 + u.i * p.block_tokens;
+      tokens = min(p.block_tokens, u.s.tokens - u.i * p.block_tokens);
+      const int c0 = share_of(u.first, cut), count = share_of(u.first + u.tiles - 1, cut) - c0 + 1;
+      from = {count, 2 * (size_t)c0 + (share_begin(c0, cut) < u.first ? 1 : 0), 2 * (size_t)c0, 2};
       found = true;
-      rest = 2 * (size_t)c, step = 2;
-      first = rest + (share_begin(c, cut) < x ? 1 : 0);
+      part += (c - c0) * (int)gridDim.y;
+      parts *= count - 1;
     }
   } else {
+    const int place = divide((int)blockIdx.x, p.by_heads);
+    tile = (int)blockIdx.x - place * p.tile_heads;
     for (int b0 = 0; b0 < p.batch && !found; b0 += 32) {   // every warp looks for the sequence
       const int b = b0 + lane;
       PromptSequence s = {0, 0, 0, {0, 0}};
@@ -65,56 +146,14 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
   grid_dependency_wait();   // the partials belong to the attention
   if (!found) return;
   if (p.cut_ctas == 0) {
-    pieces = (((ctx + tokens + p.key_tile - 1) >> p.key_tile_log2) + p.piece_tiles - 1) / p.piece_tiles;
-    first = rest = (size_t)blockIdx.x * p.splits;
+    from.count = (((ctx + tokens + p.key_tile - 1) >> p.key_tile_log2) + p.piece_tiles - 1) / p.piece_tiles;
+    from.first = from.rest = (size_t)blockIdx.x * p.splits;
   }
-  if (pieces <= 1) return;   // written by the attention
-  const int rows = tokens * p.sub, groups = p.head_dim / 4, used = p.tile_tokens * p.sub;
-  const int block_rows = p.block_tokens / p.tile_tokens * p.tile_rows;
-  for (int e = blockIdx.y * kMergeThreads + threadIdx.x; e < rows * groups; e += gridDim.y * kMergeThreads) {
-    const int c = e / rows, r = e - c * rows;
-    const int at = r < used ? r : p.tile_rows + r - used;
-    const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + at;
-    const float4* po = reinterpret_cast<const float4*>(p.part_o) + (size_t)c * block_rows + at;
-    float M = -INFINITY, L = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = 0; s0 < pieces; s0 += kMergeBatch) {   // the loads of a batch are in flight together
-      float2 x[kMergeBatch];
-      float4 o[kMergeBatch];
-#pragma unroll
-      for (int i = 0; i < kMergeBatch; ++i) {
-        const bool there = s0 + i < pieces;
-        const size_t piece = s0 + i == 0 ? first : rest + (size_t)(s0 + i) * step;
-        x[i] = there ? __ldcg(ml + piece * block_rows) : make_float2(-INFINITY, 0.f);
-        if (there) o[i] = __ldcg(po + piece * groups * block_rows);
-      }
-      float m = M;
-#pragma unroll
-      for (int i = 0; i < kMergeBatch; ++i)
-        if (!(x[i].y == 0.f)) m = fmaxf(m, x[i].x);   // (not l > 0: a NaN among the scores has to reach the output)
-      const float old = M == -INFINITY ? 0.f : exp2f(M - m);
-      M = m;
-      L *= old, acc.x *= old, acc.y *= old, acc.z *= old, acc.w *= old;
-#pragma unroll
-      for (int i = 0; i < kMergeBatch; ++i) {
-        if (x[i].y == 0.f) continue;
-        const float w = exp2f(x[i].x - M);
-        L += w * x[i].y;
-        acc.x += w * o[i].x;
-        acc.y += w * o[i].y;
-        acc.z += w * o[i].z;
-        acc.w += w * o[i].w;
-      }
-    }
-    const float inv = 1.f / L;
-    const int token = divide(r, p.by_sub), head = tile * p.sub + r - token * p.sub;
-    T* dst = static_cast<T*>(p.out) + ((size_t)(row0 + token) * p.hq + head) * p.head_dim + c * 4;
-    if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-    } else {
-      *reinterpret_cast<float4*>(dst) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-    }
-  }
+  if (from.count <= 1) return;   // written by the attention
+  if (kMany && from.count == 2)
+    merge_part<T, 4, 2>(p, from, row0, tokens, tile, part, parts);
+  else
+    merge_part<T, 1, 8>(p, from, row0, tokens, tile, part, parts);
 }
 
 // The largest divisor of `group` that is at most `most`.
@@ -162,11 +201,6 @@ void plan_tiles(PromptAttnParams& p, int tile_rows, int tiles, int key_tile_log2
 }
 }  // namespace pa
 
-int prompt_most_shares(const PromptAttnParams& p) {
-  const int64_t tiles = (((int64_t)p.bounds.max_ctx + p.bounds.max_tokens + p.key_tile - 1) >> p.key_tile_log2) * p.batch * p.tile_heads;
-  return (int)(tiles / 2 < p.cut_ctas ? tiles / 2 : p.cut_ctas);
-}
-
 size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int sms) {
   p.cut_ctas = 0;
   if (bf16) {
@@ -179,22 +213,24 @@ size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int
     // to 4096 22.3 [24.6], equal ones 30.9 [42.0], 12 ragged 28.6 [50.5], 16 ragged up to 8000 53.4 [93.2], 24 equal ones
     // of 8000 129.6 [183.5], 32 of 4000 92.2 [99.6]; what it loses: the merge's launch where the units stay whole, 18 of
     // 2000 31.6 [30.5], and the search, 2 of 4000 15.5 [14.6], 32 ragged up to 4000 56.5 [53.1].
-    const int64_t units = (int64_t)p.batch * p.tile_heads;
+    const int64_t units = (int64_t)p.blocks * p.tile_heads;
     const int64_t key_tiles = ((int64_t)p.bounds.max_ctx + p.bounds.max_tokens + p.key_tile - 1) >> p.key_tile_log2;
-    if (p.batch > 1 && p.bounds.max_tokens <= p.block_tokens && units <= 2 * (int64_t)sms && key_tiles > (units > sms ? 15 : 4) &&
-        sms <= kMostCutCtas && units * key_tiles <= kMostCutTiles) {
+    if (p.batch > 1 || p.bounds.max_tokens > p.block_tokens) {
       p.piece_tiles = (int)key_tiles;
       p.splits = 1;
       p.by_splits = index_divisor(1);
+      const int used = (p.bounds.max_tokens < p.block_tokens ? p.bounds.max_tokens : p.block_tokens) * p.sub;   // rows
+      p.costs = {used * 6 / 256, 1 + used / 128};
+      if (units > 2 * (int64_t)sms || key_tiles <= p.costs.merge + p.costs.unit + (units > sms ? 14 : 3) || sms > kMostCutCtas ||
+          units * (key_tiles + p.costs.unit) > kMostCutCells)
+        return 0;
+      const int64_t cells = units * (key_tiles + p.costs.unit);
+      p.most_shares = (int)(cells / 2 < sms ? cells / 2 : sms);
+      const size_t rows = 2 * (size_t)p.most_shares * 256, bytes = rows * (p.head_dim + 2) * sizeof(float);
+      if (bytes > scratch) return 0;
       p.cut_ctas = sms;
-      const size_t rows = 2 * (size_t)prompt_most_shares(p) * 256;
-      const size_t bytes = rows * (p.head_dim + 2) * sizeof(float);
-      if (bytes <= scratch) {
-        p.part_ml = p.part_o + rows * p.head_dim;
-        return bytes;
-      }
-      p.cut_ctas = 0;
-      return 0;
+      p.part_ml = p.part_o + rows * p.head_dim;
+      return bytes;
     }
   } else if ((int64_t)p.bounds.max_tokens * (p.hq / p.hkv) <= 16) {
     // Blocks of 16 rows, four CTAs an SM: one token after 2000 in four sequences of 8 heads, D = 64, 28.5 us (blocks
@@ -221,11 +257,13 @@ size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int
 }
 
 cudaError_t launch_prompt_attn_merge(const PromptAttnParams& p, bool bf16, cudaStream_t stream) {
-  const auto kernel = bf16 ? pa::prompt_merge_kernel<__nv_bfloat16> : pa::prompt_merge_kernel<float>;
-  int64_t rows = (int64_t)(p.bounds.max_tokens < p.block_tokens ? p.bounds.max_tokens : p.block_tokens) * p.sub;
+  const int64_t rows = (int64_t)(p.bounds.max_tokens < p.block_tokens ? p.bounds.max_tokens : p.block_tokens) * p.sub;
   const unsigned shares = (unsigned)((rows * (p.head_dim / 4) + pa::kMergeThreads - 1) / pa::kMergeThreads);
-  const int blocks = p.cut_ctas > 0 ? p.batch : p.places;
-  return launch_chained(kernel, dim3((unsigned)(blocks * p.tile_heads), shares), dim3(pa::kMergeThreads), 0, stream, 0, p);
+  const bool many = p.cut_ctas > 0 && shares > 4;
+  const auto kernel = !bf16 ? pa::prompt_merge_kernel<float, false>
+                            : many ? pa::prompt_merge_kernel<__nv_bfloat16, true> : pa::prompt_merge_kernel<__nv_bfloat16, false>;
+  const int blocks = p.cut_ctas > 0 ? p.most_shares : p.places * p.tile_heads;
+  return launch_chained(kernel, dim3((unsigned)blocks, p.cut_ctas > 0 ? (shares + 15) / 16 : shares), dim3(pa::kMergeThreads), 0, stream, 0, p);
 }
 
 }  // namespace ptd

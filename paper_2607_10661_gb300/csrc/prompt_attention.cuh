@@ -32,31 +32,81 @@ __device__ __forceinline__ PromptSequence load_sequence(const PromptAttnParams& 
   return {off0, off1 - off0, ctx, prompt_blocks(ctx, off1 - off0, p.block_tokens, p.by_block)};
 }
 
-// Key tiles of a sequence of one block.
-__device__ __forceinline__ int sequence_tiles(const PromptAttnParams& p, const PromptSequence& s) {
-  return s.tokens > 0 ? (s.ctx + s.tokens + p.key_tile - 1) >> p.key_tile_log2 : 0;
+// Key tiles of a unit of block i of a sequence, and cells of all its blocks under one head tile.
+__device__ __forceinline__ int block_tiles(const PromptAttnParams& p, const PromptSequence& s, int i) {
+  return (s.ctx + min((i + 1) * p.block_tokens, s.tokens) + p.key_tile - 1) >> p.key_tile_log2;
+}
+__device__ __forceinline__ int sequence_cells(const PromptAttnParams& p, const PromptSequence& s) {
+  int n = 0;
+#pragma unroll 1
+  for (int i = 0; i < s.blocks.count; ++i) n += block_tiles(p, s, i) + p.costs.unit;
+  return n;
 }
 
-// The cut of the batch by its lengths (prompt_geometry.cuh), and how many key tiles come before sequence `of`; `mine` is
-// sequence `lane`.  Warp-collective.
-struct LengthCut {
-  PromptCut cut;
-  int before;
-  __device__ __forceinline__ LengthCut(const PromptAttnParams& p, const PromptSequence& mine, int of, bool& bad) : before(0) {
-    const int lane = threadIdx.x & 31;
-    int units = 0, longest = 0, tiles = 0;
+// The cut of the batch by its lengths (prompt_geometry.cuh); `mine` is sequence `lane`.  Warp-collective.
+__device__ __forceinline__ PromptCut cut_by_lengths(const PromptAttnParams& p, const PromptSequence& mine, bool& bad) {
+  int units = 0, longest = 0, shortest = kMostCutCells, cells = 0;
 #pragma unroll 1
-    for (int b0 = 0; b0 < p.batch; b0 += 32) {
-      const int b = b0 + lane, n = b < p.batch ? sequence_tiles(p, b0 == 0 ? mine : load_sequence(p, b, bad)) : 0;
-      tiles += (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
-      before += (int)__reduce_add_sync(0xffffffffu, b < of ? (unsigned)n : 0u);
-      units += __popc(__ballot_sync(0xffffffffu, n > 0));
-      longest = max(longest, (int)__reduce_max_sync(0xffffffffu, (unsigned)n));
+  for (int b0 = 0; b0 < p.batch; b0 += 32) {
+    const int b = b0 + (threadIdx.x & 31);
+    PromptSequence s = mine;
+    if (b0 > 0 && b < p.batch) s = load_sequence(p, b, bad);
+    if (b >= p.batch) s.blocks.count = 0;
+    units += s.blocks.count;
+    cells += sequence_cells(p, s);
+    if (s.blocks.count > 0) {
+      longest = max(longest, block_tiles(p, s, s.blocks.count - 1) + p.costs.unit);
+      shortest = min(shortest, block_tiles(p, s, 0) + p.costs.unit);
     }
-    before *= p.tile_heads;
-    cut = prompt_cut(tiles * p.tile_heads, units * p.tile_heads, longest, p.cut_ctas);
   }
+  units = (int)__reduce_add_sync(0xffffffffu, (unsigned)units);
+  cells = (int)__reduce_add_sync(0xffffffffu, (unsigned)cells);
+  longest = (int)__reduce_max_sync(0xffffffffu, (unsigned)longest);
+  shortest = (int)__reduce_min_sync(0xffffffffu, (unsigned)shortest);
+  return prompt_cut(cells * p.tile_heads, units * p.tile_heads, longest, shortest, p.cut_ctas, p.most_shares, p.costs);
+}
+
+// The unit of a cell: sequence, block, head tile, its first cell and how many key tiles it has.
+struct CutUnit {
+  int b, i, head, first, tiles;
+  PromptSequence s;
 };
+// Of cell `at`; b0 and before (0 at first): a group of 32 sequences and the cells before it, moved on.  False: there is
+// none.  Warp-collective.
+__device__ __forceinline__ bool find_cut_unit(const PromptAttnParams& p, const PromptSequence& mine, int at, int& b0, int& before,
+                                              CutUnit& u) {
+#pragma unroll 1
+  for (;; b0 += 32) {
+    const int b = b0 + (threadIdx.x & 31);
+    bool bad = false;
+    PromptSequence s = mine;
+    if (b0 > 0 && b < p.batch) s = load_sequence(p, b, bad);
+    if (b >= p.batch) s.blocks.count = 0;
+    const int n = sequence_cells(p, s) * p.tile_heads, upto = before + WarpLanes{}.scan(n);
+    const int src = WarpLanes{}.first(at < upto);
+    if (src < 0) {
+      if (b0 + 32 >= p.batch) return false;
+      before = __shfl_sync(0xffffffffu, upto, 31);
+      continue;
+    }
+    u.b = b0 + src;
+    u.s = {__shfl_sync(0xffffffffu, s.row0, src), __shfl_sync(0xffffffffu, s.tokens, src), __shfl_sync(0xffffffffu, s.ctx, src),
+           {__shfl_sync(0xffffffffu, s.blocks.first, src), __shfl_sync(0xffffffffu, s.blocks.count, src)}};
+    u.first = __shfl_sync(0xffffffffu, upto - n, src);
+    u.tiles = block_tiles(p, u.s, 0);
+    u.i = 0;
+    int cells = u.tiles + p.costs.unit;
+#pragma unroll 1
+    while (at >= u.first + cells * p.tile_heads) {   // (ends: the sequence has `at`)
+      u.first += cells * p.tile_heads;
+      u.tiles = block_tiles(p, u.s, ++u.i);
+      cells = u.tiles + p.costs.unit;
+    }
+    u.head = (int)((uint32_t)(at - u.first) / (uint32_t)cells);
+    u.first += u.head * cells;
+    return true;
+  }
+}
 
 // A warp's walk over the batch's units.  Batches of up to 32 sequences are in registers, one a lane (one sequence
 // alone in every lane); lane l also keeps how many blocks have level l or a higher one.
@@ -65,14 +115,14 @@ struct Units {
   PromptCursor cur;
   int from_level;
   PromptCut cut;                      // by the lengths
-  int share, begin, at, end;          // the share last asked for: its key tiles, and the next of them
-  int b0, before;                     // the sequence group of `at`, and the key tiles before it
+  int share, begin, at, end;          // the share last asked for: its cells, and the next of them
+  int b0, before;                     // the sequence group of `at`, and the cells before it
   bool bad;   // some sequence is out of range (of those that the lane has looked at)
   __device__ __forceinline__ Units(const PromptAttnParams& p)
       : mine{0, 0, 0, {0, 0}}, cur{0, 0, 0, 0, 0}, from_level(0), cut{0, 0}, share(-1), bad(false) {
     const int lane = threadIdx.x & 31, m = lane * p.level_step;
     if (p.batch == 1 || lane < p.batch) mine = load_sequence(p, p.batch == 1 ? 0 : lane, bad);
-    if (p.cut_ctas > 0) cut = LengthCut(p, mine, 0, bad).cut;
+    if (p.cut_ctas > 0) cut = cut_by_lengths(p, mine, bad);
     if (!prompt_has_levels(p.batch) || cut.shares > 0) {
 #pragma unroll 1
       for (int b = lane + 32; p.cut_ctas == 0 && b < p.batch; b += 32) load_sequence(p, b, bad);
@@ -96,35 +146,23 @@ struct Units {
       end = share_begin(x + 1, cut);
       b0 = before = 0;
     }
-    if (at >= end) return false;
-#pragma unroll 1
-    for (;; b0 += 32) {
-      const int b = b0 + (threadIdx.x & 31);
-      PromptSequence s = {0, 0, 0, {0, 0}};
-      if (b < p.batch) s = p.batch <= 32 ? mine : load_sequence(p, b, bad);
-      const int t = sequence_tiles(p, s), upto = before + WarpLanes{}.scan(t * p.tile_heads);
-      const int src = WarpLanes{}.first(at < upto);
-      if (src < 0) {
-        before = __shfl_sync(0xffffffffu, upto, 31);
-        if (b0 + 32 >= p.batch) return false;
-        continue;
-      }
-      const int n = __shfl_sync(0xffffffffu, t, src), in = at - (__shfl_sync(0xffffffffu, upto, src) - n * p.tile_heads);
-      const int tile = (int)((uint32_t)in / (uint32_t)n);
-      u.b = b0 + src;
-      u.ctx = __shfl_sync(0xffffffffu, s.ctx, src);
-      u.token0 = 0;
-      u.tokens = __shfl_sync(0xffffffffu, s.tokens, src);
-      u.row0 = __shfl_sync(0xffffffffu, s.row0, src);
-      u.head0 = tile * p.sub;
-      u.kv = divide(tile, p.by_kv);
-      u.tile0 = in - tile * n;
-      u.tile1 = min(n, u.tile0 + end - at);
-      u.whole = u.tile0 == 0 && u.tile1 == n;
+    CutUnit w;
+    do {
+      if (at >= end || !find_cut_unit(p, mine, at, b0, before, w)) return false;
+      u.tile0 = at - w.first;
+      u.tile1 = min(w.tiles, u.tile0 + end - at);
       u.place = 2 * x + (at > begin ? 1 : 0);
-      at += u.tile1 - u.tile0;
-      return true;
-    }
+      at = w.first + w.tiles + p.costs.unit;
+    } while (u.tile1 <= u.tile0);   // the share begins behind the unit's key tiles
+    u.b = w.b;
+    u.ctx = w.s.ctx;
+    u.token0 = w.i * p.block_tokens;
+    u.tokens = min(p.block_tokens, w.s.tokens - u.token0);
+    u.row0 = w.s.row0 + u.token0;
+    u.head0 = w.head * p.sub;
+    u.kv = divide(w.head, p.by_kv);
+    u.whole = u.tile0 == 0 && u.tile1 == w.tiles;
+    return true;
   }
   __device__ __forceinline__ bool more(int x) const { return x == share && at < end; }   // of share x (share -1: none)
   // Unit number x: piece x % splits of block (x / splits) / tile_heads of the batch under head tile (x / splits) %

@@ -743,7 +743,7 @@ cudaError_t launch_prompt_attn_tc(const CUtensorMap& map_k, const CUtensorMap& m
   const auto kernel = p.page_size == 0 ? pt::prompt_tc_kernel<0> : (p.page_size >= 64 ? pt::prompt_tc_kernel<2> : pt::prompt_tc_kernel<8>);
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pt::kSmemBytes);
   if (e != cudaSuccess) return e;
-  const int units = p.blocks * p.tile_heads * p.splits, shares = p.cut_ctas > 0 ? prompt_most_shares(p) : 0;
+  const int units = p.blocks * p.tile_heads * p.splits, shares = p.cut_ctas > 0 ? p.most_shares : 0;
   return launch_chained(kernel, dim3((unsigned)(units > shares ? units : shares)), dim3(pt::kThreads), pt::kSmemBytes,
                         stream, 0, map_k, map_v, map_q, p);
 }

@@ -62,33 +62,36 @@ PTD_HD int prompt_level_step(int max_ctx, int max_tokens, int width) { return (m
 
 PTD_HD bool prompt_has_levels(int batch) { return batch > 1 && batch <= kOrderedBatch; }
 
-// Batches whose sequences are one block each (decoding) may be cut by the lengths on the device, so that the SMs' work
-// evens out: the key tiles of all units, sequence after sequence and head tile after head tile, in equal shares, one a
-// CTA.  A unit that is not in one share has partials, at place 2 c if it begins share c, else 2 c + 1.
+// Batches of few units may be cut by the lengths on the device, so that the SMs' work evens out.  A unit takes a cell a key
+// tile, and some more for its start and end; the cells of all units, sequence after sequence, block after block and head
+// tile after head tile, go in equal shares, one a CTA.  A unit whose key tiles are not in one share has partials, at
+// place 2 c if it begins share c, else 2 c + 1.
 struct PromptCut {
-  int shares, tiles;   // shares 0: the units are better left whole
+  int shares, cells;   // shares 0: the units are better left whole
 };
-constexpr int kMostCutCtas = 255, kMostCutTiles = 1 << 24;   // their product stays in 32 bits
+constexpr int kMostCutCtas = 255, kMostCutCells = 1 << 24;   // their product stays in 32 bits
+struct CutCosts {      // in cells
+  int merge, unit;     // of a CTA's partials of a unit and their merge; of a unit besides its key tiles
+};
 
-// The cut for `ctas` CTAs at a time: `tiles` key tiles of `units` units (at most two rounds of them), the longest of
-// `longest`.  In eighths of a key tile: units whole, the longest, or two of the mean length and a change of unit; in
-// shares, a share, partials and their merge, and a change of unit at each unit's end.
-constexpr uint32_t kMergeCost = 4, kChangeCost = 8;
-PTD_HD PromptCut prompt_cut(int tiles_, int units_, int longest_, int ctas_) {
-  const uint32_t tiles = (uint32_t)tiles_, units = (uint32_t)units_, longest = (uint32_t)longest_, ctas = (uint32_t)ctas_;
-  if (tiles < 2u) return {0, tiles_};
-  uint32_t whole = 8u * longest;
+// The cut for `ctas` CTAs at a time into at most `most` shares: `cells` of `units` units (at most two rounds of them), the
+// longest and the shortest of `longest` and `shortest` cells.  Whole units take the longest, or two of the mean or what is even and a short one.
+PTD_HD PromptCut prompt_cut(int cells_, int units_, int longest_, int shortest_, int ctas_, int most, CutCosts costs) {
+  const uint32_t cells = (uint32_t)cells_, units = (uint32_t)units_, ctas = (uint32_t)ctas_;
+  if (cells < 2u || most < 1 || cells > (uint32_t)kMostCutCells) return {0, cells_};   // (more: sequences that overlap)
+  uint32_t whole = 8u * (uint32_t)longest_;
   if (units > ctas) {
-    const uint32_t two = 16u * tiles / units;
-    whole = (whole > two ? whole : two) + kChangeCost;
+    const uint32_t two = 16u * cells / units, last = 8u * cells / ctas + 8u * (uint32_t)shortest_;
+    const uint32_t less = two < last ? two : last;
+    whole = whole > less ? whole : less;
   }
-  const uint32_t shares = tiles / 2u < ctas ? tiles / 2u : ctas;
-  const uint32_t even = (8u * tiles + kChangeCost * units) / shares + kMergeCost + kChangeCost;
-  return {even < whole ? (int)shares : 0, tiles_};
+  const uint32_t shares = cells / 2u < (uint32_t)most ? cells / 2u : (uint32_t)most;
+  const uint32_t even = 8u * ((uint32_t)(costs.merge + costs.unit)) + 8u * (cells + (uint32_t)costs.merge * units) / shares;
+  return {even < whole ? (int)shares : 0, cells_};
 }
-PTD_HD int share_begin(int c, const PromptCut& cut) { return (int)((uint32_t)c * (uint32_t)cut.tiles / (uint32_t)cut.shares); }
-PTD_HD int share_of(int x, const PromptCut& cut) {   // the share that has tile x
-  return (int)((((uint32_t)x + 1u) * (uint32_t)cut.shares - 1u) / (uint32_t)cut.tiles);
+PTD_HD int share_begin(int c, const PromptCut& cut) { return (int)((uint32_t)c * (uint32_t)cut.cells / (uint32_t)cut.shares); }
+PTD_HD int share_of(int x, const PromptCut& cut) {   // the share that has cell x
+  return (int)((((uint32_t)x + 1u) * (uint32_t)cut.shares - 1u) / (uint32_t)cut.cells);
 }
 
 // Where the last search ended: a search for a later block goes on from there.

@@ -137,6 +137,12 @@ CASES = {
                               hq=8, hkv=1, page=32),
     "even-uncut": dict(seqs=[(900 + i, 1) for i in range(16)], hq=32, hkv=8, page=128, max_ctx=20000),
     "even-group5": dict(seqs=[(2500, 3), (2600, 50)], hq=10, hkv=2, page=16),
+    "cut-decoding-and-chunk": dict(seqs=[(4000, 1), (3, 1), (0, 300), (2500, 1), (6000, 1)], hq=32, hkv=8, page=16, pad=3),
+    "cut-chunks-of-blocks": dict(seqs=[(3000, 200), (0, 0), (1500, 333), (40, 1)], hq=16, hkv=4),
+    "cut-one-chunk": dict(seqs=[(2500, 130)], hq=16, hkv=2, page=128),
+    "cut-short-prompts": dict(seqs=[(0, 512), (0, 100)], hq=8, hkv=8, page=64),
+    "cut-34-sequences": dict(seqs=[(0, 1)] * 31 + [(5000, 1), (0, 0), (3000, 150)], hq=8, hkv=1, page=32),
+    "cut-group5-blocks": dict(seqs=[(2000, 120), (2600, 50)], hq=10, hkv=2, page=16),
     "ordered-100": dict(seqs=[(17 * i % 701, 1 + i % 3) for i in range(100)], hq=8, hkv=1, page=32, max_ctx=2000),
     "f32-decoding-split": dict(seqs=[(200 + 11 * i, 1) for i in range(40)], hq=2, hkv=2, d=32, dtype=F32),
     "f32-64": dict(seqs=RAGGED, hq=4, hkv=4, d=64, dtype=F32, pad=2),

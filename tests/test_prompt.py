@@ -111,22 +111,25 @@ def test_even_shares_cover_every_unit_once(tmp_path):
 #include <vector>
 #include "prompt_geometry.cuh"
 int main() {
-  int ctas, units, cut = 0;
-  while (std::scanf("%d %d", &ctas, &units) == 2) {
+  int ctas, units, own, cut = 0;   // own: a unit's cells besides its key tiles
+  while (std::scanf("%d %d %d", &ctas, &own, &units) == 3) {
     std::vector<int> n(units), first(units);
-    int tiles = 0, longest = 0, there = 0;
+    int cells = 0, longest = 0, there = 0, shortest = 1 << 24;
     for (int i = 0; i < units; ++i) {
       if (std::scanf("%d", &n[i]) != 1) return 1;
-      first[i] = tiles;
-      tiles += n[i], there += n[i] > 0, longest = n[i] > longest ? n[i] : longest;
+      first[i] = cells;
+      if (n[i] == 0) continue;
+      cells += n[i] + own, ++there;
+      longest = n[i] + own > longest ? n[i] + own : longest;
+      shortest = n[i] + own < shortest ? n[i] + own : shortest;
     }
-    const ptd::PromptCut c0 = ptd::prompt_cut(tiles, there, longest, ctas);
+    const ptd::PromptCut c0 = ptd::prompt_cut(cells, there, longest, shortest, ctas, ctas, {1, own});
     const int shares = c0.shares;
     if (shares == 0) continue;
     ++cut;
-    if (shares < 0 || shares > ctas || shares > tiles / 2) return 2;
+    if (shares < 0 || shares > ctas || shares > cells / 2 || c0.cells != cells) return 2;
     std::vector<std::vector<int>> pieces(units);   // places, in order
-    std::vector<int> taken(2 * shares, 0);
+    std::vector<int> taken(2 * shares, 0), tiles(units, 0);
     int next = 0;
     for (int c = 0; c < shares; ++c) {
       const int x0 = ptd::share_begin(c, c0), x1 = ptd::share_begin(c + 1, c0);
@@ -134,6 +137,7 @@ int main() {
       for (int i = 0; i < units; ++i) {
         const int a = x0 > first[i] ? x0 : first[i], b = x1 < first[i] + n[i] ? x1 : first[i] + n[i];
         if (a >= b) continue;
+        tiles[i] += b - a;
         if (a == first[i] && b == first[i] + n[i]) continue;   // whole
         const int place = 2 * c + (a > x0 ? 1 : 0);
         if (taken[place]++) return 4;
@@ -141,25 +145,30 @@ int main() {
       }
       next = x1;
     }
-    if (next != tiles) return 5;
+    if (next != cells) return 5;
     for (int i = 0; i < units; ++i) {
+      if (tiles[i] != n[i]) return 6;
       if (n[i] == 0) continue;
       const int c = ptd::share_of(first[i], c0), count = ptd::share_of(first[i] + n[i] - 1, c0) - c + 1;
       if (count == 1) {
-        if (!pieces[i].empty()) return 6;
+        if (!pieces[i].empty()) return 7;
         continue;
       }
-      if ((int)pieces[i].size() != count) return 7;
+      if ((int)pieces[i].size() != count) return 8;
       for (int s = 0; s < count; ++s)
-        if (pieces[i][s] != (s ? 2 * (c + s) : 2 * c + (ptd::share_begin(c, c0) < first[i] ? 1 : 0))) return 8;
+        if (pieces[i][s] != (s ? 2 * (c + s) : 2 * c + (ptd::share_begin(c, c0) < first[i] ? 1 : 0))) return 9;
+      const int at = ptd::share_begin(c + 1, c0);   // the boundary at which the merge looks for it
+      if (at <= first[i] || at >= first[i] + n[i]) return 10;
     }
   }
-  if (ptd::prompt_cut(0, 0, 0, 152).shares != 0 || ptd::prompt_cut(1, 1, 1, 152).shares != 0) return 9;
-  const int most = ptd::kMostCutTiles;   // (no product leaves 32 bits)
+  if (ptd::prompt_cut(0, 0, 0, 1 << 24, 152, 152, {1, 1}).shares != 0 || ptd::prompt_cut(1, 1, 1, 1, 152, 152, {0, 0}).shares != 0) return 11;
+  const int most = ptd::kMostCutCells;   // (no product leaves 32 bits)
   for (int units : {8, 100, 300, 510}) {
-    const ptd::PromptCut c = ptd::prompt_cut(most, units, most / 2, 255);
+    const ptd::PromptCut c = ptd::prompt_cut(most, units, most / 2, 1, 255, 255, {4, 3});
     if (c.shares != 255 || ptd::share_begin(255, c) != most || ptd::share_of(most - 1, c) != 254 || ptd::share_of(0, c) != 0)
-      return 10;
+      return 12;
+    if (ptd::prompt_cut(most, units, most / 2, 1, 255, 9, {4, 3}).shares != 9) return 14;   // (no room for more)
+    if (ptd::prompt_cut(most + 1, units, most / 2, 1, 255, 255, {4, 3}).shares != 0) return 13;
   }
   std::printf("%d\n", cut);
   return 0;
@@ -169,11 +178,11 @@ int main() {
                     "-o", str(exe)], check=True)
     rng = random.Random(9)
     cases = [(152, [20]), (152, [5000] * 8), (152, [33, 0, 1, 2] * 16), (3, [7, 8]), (1, [5, 6]), (152, [33] * 256),
-             (255, [1 << 20] * 16), (152, [63] * 8), (152, [9] * 75), (152, [9] * 77)]
+             (255, [1 << 19] * 16), (152, [63] * 8), (152, [9] * 75), (152, [9] * 77)]
     for _ in range(400):
         top = rng.choice([2, 8, 40, 300])
         cases.append((rng.choice([1, 2, 7, 148, 152]), [rng.randrange(top + 1) for _ in range(rng.randrange(1, 400))]))
-    r = subprocess.run([str(exe)], input="\n".join(f"{c} {len(n)} " + " ".join(map(str, n)) for c, n in cases),
+    r = subprocess.run([str(exe)], input="\n".join(f"{c} {rng.randrange(4)} {len(n)} " + " ".join(map(str, n)) for c, n in cases),
                        capture_output=True, text=True)
     assert r.returncode == 0 and int(r.stdout) > 50, (r.returncode, r.stdout)
 
