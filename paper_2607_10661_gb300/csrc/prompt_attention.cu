@@ -204,15 +204,18 @@ void plan_tiles(PromptAttnParams& p, int tile_rows, int tiles, int key_tile_log2
 size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int sms) {
   p.cut_ctas = 0;
   if (bf16) {
-    // A CTA an SM.  Pieces of one length (us by their key tiles, the rule's in brackets): one token after 4096 of 32/8
-    // heads, 8 units of 33 tiles, 1: 17.5, [2: 12.7], 4: 12.8, 8: 15.7, uncut 42; after 32768, 10: 42.6, [14: 34.6], 17: 33.0,
-    // 20: 34.3; 61 tokens of 64/8 heads after 32707, 20: 71.6, [29: 54], 40: 62; 256 tokens after 8192, 14: 52, [17: 41], 25: 51.
+    // A CTA an SM.  One sequence of one block: pieces of one length, by the bounds (us by their key tiles, the rule's in
+    // brackets): one token after 4096 of 32/8 heads, 8 units of 33 tiles, 1: 17.5, [2: 12.7], 4: 12.8, 8: 15.7, uncut 42; after
+    // 32768, 10: 42.6, [14: 34.6], 17: 33.0, 20: 34.3; 60 tokens after 500, [1: 13.2], uncut 14.0.
     pa::plan_tiles(p, 128, 2, 7, sms);
-    // Several sequences of one block each (decoding): cut by the lengths on the device, where as many units as two rounds
-    // of CTAs may gain by it.  One token of 32/8 heads (us, pieces of one length or uncut in brackets): 8 ragged contexts up
-    // to 4096 22.3 [24.6], equal ones 30.9 [42.0], 12 ragged 28.6 [50.5], 16 ragged up to 8000 53.4 [93.2], 24 equal ones
-    // of 8000 129.6 [183.5], 32 of 4000 92.2 [99.6]; what it loses: the merge's launch where the units stay whole, 18 of
-    // 2000 31.6 [30.5], and the search, 2 of 4000 15.5 [14.6], 32 ragged up to 4000 56.5 [53.1].
+    // Else by the lengths on the device, or uncut (us of 32/8 heads; pieces of one length, which bounds alone give, or uncut in
+    // brackets): one token behind 8 ragged contexts up to 4096 22.2 [24.6], 8 equal ones 31.9 [42.0], 12 ragged 28.7 [50.5], 16
+    // ragged up to 8000 53.2 [93.2], 24 of 8000 126 [183], 32 of 4000 89.8 [99.6]; 8 tokens after 8000 beside a prompt of 512
+    // 61.5 [93.5], 4 after 16000 beside 512 76 [179], 2 chunks of 256 after 8192 67 [107], 61 tokens of 64/8 heads after 32707
+    // 51.5 [55.3].  Costs in key tiles, from these and from the cases on either side of the bound: 200 tokens after 1000
+    // uncut 21.6 [cut 23.6], after 1900 cut 25.8 [uncut 31.8], 2 of 200 after 500 uncut 16.5 [cut 18.4], 400 after 700 20.5
+    // [29.4], 800 after 1500 33.7 [43.7].  What it loses: the merge's launch where the units stay whole (18 contexts of
+    // 2000 32.0 [30.5], 800 tokens after 1500 36.0 [33.7]), uneven pieces of few equal ones (2 contexts of 2000 14.0 [11.7]).
     const int64_t units = (int64_t)p.blocks * p.tile_heads;
     const int64_t key_tiles = ((int64_t)p.bounds.max_ctx + p.bounds.max_tokens + p.key_tile - 1) >> p.key_tile_log2;
     if (p.batch > 1 || p.bounds.max_tokens > p.block_tokens) {

@@ -7,8 +7,8 @@
 // (block, head tile), or a piece of its keys (partials, merged by prompt_merge_kernel).  Units are numbered
 // longest first over the whole batch (prompt_geometry.cuh); the grid has one CTA per unit, and a resident CTA
 // takes the numbers of CTAs that have not started yet (cluster launch control), so that the SMs' shares
-// even out whatever the lengths, and a unit's first loads and its set-up run beside the unit before it.  Batches
-// of a block a sequence go by shares of the key tiles instead where that is shorter (PromptCut).
+// even out whatever the lengths, and a unit's first loads and its set-up run beside the unit before it.  Few units
+// go by equal shares of their key tiles instead where that is shorter (PromptCut).
 //
 // Warps (384 threads; the first four give registers to the others):
 //   0       scheduler and TMA producer: claims the next unit before the last tiles of this one are asked for;
@@ -27,7 +27,7 @@
 // runs of seconds at the cap.  Ragged prompts of some hundred tokens (30 us for 18.5 GFLOP) are bound by changes of unit, ~4.5 us
 // each: the V check, masked tiles, outputs, and code that has left the instruction caches (so it is kept short).
 // Decoding: by HBM, ~6 us from the start to the first output, and the merge: 8 contexts of up to 4096 22 us for 73 MB,
-// 24 of 8000 130 us for 787 MB (6.1 TB/s).
+// 24 of 8000 126 us for 787 MB (6.2 TB/s).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
