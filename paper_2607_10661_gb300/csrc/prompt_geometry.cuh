@@ -147,7 +147,6 @@ PTD_HD bool find_prompt_block(const Lanes& lanes, const Load& load, const LevelO
 struct OneLane {
   PTD_HD int id() const { return 0; }
   PTD_HD int count() const { return 1; }
-  PTD_HD int sum(int x) const { return x; }
   PTD_HD int scan(int x) const { return x; }
   PTD_HD int first(bool p) const { return p ? 0 : -1; }
   PTD_HD int get(int x, int) const { return x; }
@@ -157,7 +156,6 @@ struct OneLane {
 struct WarpLanes {
   __device__ __forceinline__ int id() const { return threadIdx.x & 31; }
   __device__ __forceinline__ int count() const { return 32; }
-  __device__ __forceinline__ int sum(int x) const { return (int)__reduce_add_sync(0xffffffffu, (unsigned)x); }
   __device__ __forceinline__ int scan(int x) const {   // inclusive
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {

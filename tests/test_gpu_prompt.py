@@ -645,6 +645,39 @@ def test_captured_decoding_is_cut_anew_at_each_replay():
         assert (x.out[off[-1]:] == 7.0).all()
 
 
+@pytest.mark.parametrize("dtype,hkv,d,capacity", [(BF16, 8, 128, 2_200_000), (F32, 8, 64, 4_300_000)])
+def test_offsets_past_32_bits(dtype, hkv, d, capacity):
+    """The second sequence of a contiguous cache begins 2^31 elements on: slots, append and attention."""
+    hq, ctx, new = 2 * hkv, [5, 130], [1, 3]
+    kc, vc = (torch.empty((1, 2, capacity, hkv, d), dtype=dtype, device=DEV) for _ in range(2))
+    assert kc[0, 0].numel() > 2 ** 31
+    g = torch.Generator(device=DEV).manual_seed(80)
+    rand = lambda *s: torch.randn(s, generator=g, device=DEV).to(dtype)
+    for b in range(2):
+        for c in (kc, vc):
+            c[0, b, :ctx[b]] = rand(ctx[b], hkv, d)
+    cache = ptd.KVCache(kc, vc, hkv, d)
+    prompt = ptd.Prompt(torch.tensor([0, 1, 4], **I32), torch.tensor(ctx, **I32), 4, 3, 130)
+    slots, pos, status = torch.empty(4, **I32), torch.empty(4, **I32), torch.zeros(1, **I32)
+    q, k, v = rand(4, hq, d), rand(4, hkv, d), rand(4, hkv, d)
+    out = torch.empty_like(q)
+    ptd.prompt_slots(prompt, cache, slots, pos, status)
+    ptd.prompt_rope_append(prompt, cache, 0, slots, pos, q, k, v, q, 1e4, status)
+    n = ptd.prompt_attention_workspace_size(prompt, cache, hq)
+    ptd.prompt_attention(prompt, cache, 0, q, out, status, workspace=torch.empty(max(n, 16), dtype=torch.uint8, device=DEV))
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    assert slots.tolist() == [5, capacity + 130, capacity + 131, capacity + 132] and pos.tolist() == [5, 130, 131, 132]
+    for b, rows in ((0, slice(0, 1)), (1, slice(1, 4))):
+        assert torch.equal(vc[0, b, ctx[b]:ctx[b] + new[b]], v[rows])
+        kb, vb, qb = (x.double().cpu().numpy() for x in (kc[0, b, :ctx[b] + new[b]], vc[0, b, :ctx[b] + new[b]], q[rows]))
+        want = oracle.rope(k[rows].double().cpu().numpy(), pos[rows].tolist(), 1e4)
+        assert (np.abs(kb[ctx[b]:] - want) <= _rope_tolerance(k[rows].double().cpu().numpy(), want, dtype)).all()
+        ref, size = oracle.causal_attention(qb, kb, vb, ctx[b])
+        tol = _attention_tolerance(qb, kb, vb, ref, size, dtype)
+        assert (np.abs(out[rows].double().cpu().numpy() - ref) <= tol).all()
+
+
 def test_calls_on_two_streams():
     """Batches with scratch of their own on two streams at once."""
     xs = [Batch([(3000 + 500 * i, 2), (40, 9)], 8, 2, page=16, seed=50 + i) for i in range(2)]
