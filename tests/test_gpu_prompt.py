@@ -142,6 +142,8 @@ CASES = {
     "cut-one-chunk": dict(seqs=[(2500, 130)], hq=16, hkv=2, page=128),
     "cut-short-prompts": dict(seqs=[(0, 512), (0, 100)], hq=8, hkv=8, page=64),
     "cut-34-sequences": dict(seqs=[(0, 1)] * 31 + [(5000, 1), (0, 0), (3000, 150)], hq=8, hkv=1, page=32),
+    "cut-200-sequences": dict(seqs=[(37 * i % 3001, 1 - i % 7 // 6) for i in range(200)], hq=4, hkv=1, page=16, pad=4),
+    "cut-two-rounds-of-one-length": dict(seqs=[(2600, 1)] * 22, hq=16, hkv=8, page=32),
     "cut-group5-blocks": dict(seqs=[(2000, 120), (2600, 50)], hq=10, hkv=2, page=16),
     "ordered-100": dict(seqs=[(17 * i % 701, 1 + i % 3) for i in range(100)], hq=8, hkv=1, page=32, max_ctx=2000),
     "f32-decoding-split": dict(seqs=[(200 + 11 * i, 1) for i in range(40)], hq=2, hkv=2, d=32, dtype=F32),
