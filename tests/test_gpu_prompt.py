@@ -221,6 +221,29 @@ def test_hidden_values_stay_hidden(dtype, d, value):
                 assert torch.isnan(seen).all(), b
 
 
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_hidden_values_stay_hidden_in_cut_units(value):
+    """The same where the lengths cut a unit: in its last, partly visible key tiles, and in a piece that all rows see."""
+    seqs, at = [(4000, 150), (3, 2), (5000, 40)], [4100, 4, 1000]
+    x = Batch(seqs, 16, 4, page=16, seed=16)
+    assert x.attend() == 2
+    clean = x.out.clone()
+    for which in ("v", "k"):
+        y = Batch(seqs, 16, 4, page=16, seed=16)
+        for b, p in enumerate(at):
+            getattr(y, which)[0].view(-1, 4, 128)[y.rows[b][p], :, 3:5] = value
+        y.attend()
+        for b, (c, n) in enumerate(seqs):
+            lo, first = y.off[b], y.off[b] + max(0, at[b] - c)
+            assert torch.equal(y.out[lo:first], clean[lo:first]), (which, b)
+            seen = y.out[first:y.off[b + 1]]
+            if which == "v":
+                assert torch.isfinite(seen[:, :, 5:]).all() and torch.isfinite(seen[:, :, :3]).all(), b
+                assert (torch.isnan(seen[:, :, 3:5]) if math.isnan(value) else seen[:, :, 3:5] == value).all(), b
+            elif math.isnan(value):
+                assert torch.isnan(seen).all(), b
+
+
 def test_attention_of_large_scores():
     """Scores of some hundreds, rising and falling along the keys: the running maximum moves in every tile."""
     x = Batch([(0, 300), (600, 40)], 8, 2, seed=15)
