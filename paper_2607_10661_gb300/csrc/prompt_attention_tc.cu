@@ -72,6 +72,7 @@ enum Bar {
   kSegFull = kQEmpty + 2,
   kSegEmpty = kSegFull + 2,
   kClaim = kSegEmpty + 2,
+  kEntry,                     // issuer 1 has begun a unit with turns
   kDrain,
   kBars = kDrain + 2
 };
@@ -364,6 +365,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       auto wait = [&](int b, int uses) { return wait_warp(bar(b), (uint32_t)uses & 1u, abort_flag, p.dev_status); };
       bool ok = true;
       int steps = 0, ps = 0, qs = 0;   // steps, P and Q taken
+      int entries = 0;                 // units with turns that issuer 1 was waited for in
       int at = 0;                      // ring place of the next tile
       uint32_t phase = 0;              // the ring's turn
       auto take = [&](uint32_t& tile) {   // waits for the next tile; its descriptor offset
@@ -382,11 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int n = max(sg->n[0], sg->n[1]), mine = sg->n[t], both = min(sg->n[0], sg->n[1]);
         free_seg(it);
         uint32_t k_tile = 0, v_tile = 0;
-        // While both M tiles have products they take turns: M tile 1's of step j after 0's, 0's of step
-        // j + 1 after 1's of step j.  A turn that waits for nobody is the issuer's own arrival.
-        auto pass_turn = [&](int j) {
-          if (t == 0 ? j < both : j + 1 < both) arrive(kPHalf + (t ^ 1));
-        };
+        if (tells_entry(t, both)) arrive(kEntry);
         if (!(ok = take(k_tile))) break;
         if (mine > 0) {
           if (!(ok = wait(kQFull + t, qs++))) break;
@@ -397,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         step_done(mine > 0);
         for (int j = 0; j < n; ++j) {
-          if (j < mine && (t == 0 ? j == 0 || j >= both : j >= both)) arrive(kPHalf + t);
+          if (j < mine && own_turn(t, j, both)) arrive(kPHalf + t);
           if (!(ok = take(v_tile))) break;
           if (j + 1 < n && !(ok = take(k_tile))) break;
           if (j < mine) {
@@ -408,7 +406,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc_fence_after();
             issue_pv<4, 8>(s_tmem, dv + v_tile, j > 0);
             if (j + 1 < mine) issue_s(s_tmem, dq, dk + k_tile);
-            pass_turn(j);
+            if (awaits_entry(t, j, both) && !(ok = wait(kEntry, entries++))) break;
+            if (passes_turn(t, j, both)) arrive(kPHalf + (t ^ 1));
             if (j + 1 < mine) {
               commit(kSFull + t);
               if (j + 2 == mine) commit(kQEmpty + t);

@@ -94,6 +94,18 @@ PTD_HD int share_of(int x, const PromptCut& cut) {   // the share that has cell 
   return (int)((((uint32_t)x + 1u) * (uint32_t)cut.shares - 1u) / (uint32_t)cut.cells);
 }
 
+// Turns of the attention's two issuers (prompt_attention_tc.cu).  M tile t's products of key tile j wait for its softmax
+// and for a turn, told on one barrier; `both` is how many key tiles of the unit both M tiles have.  While both have
+// products, M tile 1's of tile j come after 0's, and 0's of tile j + 1 after 1's of tile j; a turn that waits for nobody is
+// the issuer's own.  Within a unit every turn passed to the other is asked for by a turn got from it, so that it cannot
+// come early.  The first one of a unit is not: M tile 1 may still wait for its softmax in the unit before, whose barrier would
+// count the turn in place of a softmax warp.  So issuer 1 tells that it has begun a unit with turns, and issuer 0 waits
+// for that before it passes the first.
+PTD_HD bool own_turn(int t, int j, int both) { return t == 0 ? j == 0 || j >= both : j >= both; }
+PTD_HD bool passes_turn(int t, int j, int both) { return t == 0 ? j < both : j + 1 < both; }
+PTD_HD bool tells_entry(int t, int both) { return t == 1 && both > 0; }
+PTD_HD bool awaits_entry(int t, int j, int both) { return t == 0 && j == 0 && both > 0; }
+
 // Where the last search ended: a search for a later block goes on from there.
 struct PromptCursor {
   int level, upto, above;   // a level, the blocks of it and higher ones, and of higher ones (upto 0: none known)

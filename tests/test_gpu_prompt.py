@@ -779,3 +779,17 @@ def test_native_and_ctypes_paths_agree(monkeypatch):
     assert native[0] == plain[0]
     for i, (a, b) in enumerate(zip(native[1], plain[1])):
         assert torch.equal(a, b), i
+
+
+@pytest.mark.parametrize("seqs", [
+    # cut by the lengths: some shares begin at a key tile that only the second M tile sees, a unit with both follows
+    [(128 * (13 + 5 * i % 7) - 40, 64) for i in range(20)],
+    # whole units, several a CTA, the second M tile one key tile longer
+    [(88, 64)] * 90], ids=["cut", "whole"])
+def test_units_whose_second_m_tile_sees_more(seqs):
+    x = Batch(seqs, 16, 4, page=32, seed=71)
+    for _ in range(3):
+        x.out.fill_(7.0)
+        x.attend()
+        assert int(x.status) == 0
+        x.check()

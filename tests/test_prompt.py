@@ -187,6 +187,105 @@ int main() {
     assert r.returncode == 0 and int(r.stdout) > 50, (r.returncode, r.stdout)
 
 
+TURNS = r"""
+#include <cstdio>
+#include <unordered_set>
+#include <vector>
+#include "prompt_geometry.cuh"
+// Every interleaving of the two issuers and two softmax warps an M tile over a few units (n0, n1 key tiles), without the
+// ring, which only holds them back.  Barriers count arrivals; an arrival carries the phase that it is meant for, and a
+// wait passes on the phase's parity, as the hardware's does.  1: an arrival in another phase, or a wait let through by
+// another phase; 2: a state that nobody leaves.
+enum { kP = 0, kF = 2, kS = 4, kO = 6, kEntry = 8, kBars = 9 };
+struct Op { bool wait; int bar, phase; };
+const int counts[kBars] = {3, 3, 2, 2, 1, 1, 1, 1, 1};   // kP: two warps and the turn
+int main() {
+  const int kinds[8][2] = {{1, 0}, {2, 0}, {0, 1}, {0, 2}, {1, 1}, {1, 2}, {2, 2}, {2, 3}};
+  long states = 0;
+  for (int x = 0; x < 8 * 8 * 8; ++x) {
+    std::vector<Op> ops[6];
+    int first[2] = {0, 0}, outs[2] = {0, 0}, entries = 0;
+    for (int u = 0; u < 3; ++u) {
+      const int* n = kinds[u == 0 ? x % 8 : u == 1 ? x / 8 % 8 : x / 64];
+      const int both = n[0] < n[1] ? n[0] : n[1], all = n[0] < n[1] ? n[1] : n[0];
+      for (int t = 0; t < 2; ++t) {
+        std::vector<Op>& o = ops[t];
+        if (ptd::tells_entry(t, both)) o.push_back({false, kEntry, entries});
+        if (n[t] > 0) o.push_back({false, kS + t, first[t]});
+        for (int j = 0; j < all; ++j) {
+          if (j >= n[t]) continue;
+          if (ptd::own_turn(t, j, both)) o.push_back({false, kP + t, first[t] + j});
+          o.push_back({true, kP + t, first[t] + j});
+          o.push_back({true, kF + t, first[t] + j});
+#ifndef PTD_NO_ENTRY
+          if (ptd::awaits_entry(t, j, both)) o.push_back({true, kEntry, entries});
+#endif
+          if (ptd::passes_turn(t, j, both)) o.push_back({false, kP + (t ^ 1), first[t ^ 1] + j + t});
+          if (j + 1 < n[t]) o.push_back({false, kS + t, first[t] + j + 1}); else o.push_back({false, kO + t, outs[t]});
+        }
+        for (int w = 0; w < 2 && n[t] > 0; ++w) {
+          std::vector<Op>& q = ops[2 + 2 * t + w];
+          for (int j = 0; j < n[t]; ++j) {
+            q.push_back({true, kS + t, first[t] + j});
+            q.push_back({false, kP + t, first[t] + j});
+            q.push_back({false, kF + t, first[t] + j});
+          }
+          q.push_back({true, kO + t, outs[t]});
+        }
+      }
+      for (int t = 0; t < 2; ++t) first[t] += n[t], outs[t] += n[t] > 0;
+      entries += both > 0;
+    }
+    std::unordered_set<unsigned long long> seen = {0};
+    std::vector<unsigned long long> todo = {0};   // the processes' places, a byte each
+    while (!todo.empty()) {
+      const unsigned long long at = todo.back();
+      todo.pop_back();
+      ++states;
+      int arrived[kBars] = {};
+      for (int i = 0; i < 6; ++i)
+        for (int k = 0; k < (int)(at >> 8 * i & 255); ++k)
+          if (!ops[i][k].wait) ++arrived[ops[i][k].bar];
+      bool done = true, moved = false;
+      for (int i = 0; i < 6; ++i) {
+        const int k = (int)(at >> 8 * i & 255);
+        if (k == (int)ops[i].size()) continue;
+        done = false;
+        const Op& o = ops[i][k];
+        const int phase = arrived[o.bar] / counts[o.bar];
+        if (o.wait) {
+          if ((phase & 1) == (o.phase & 1)) continue;   // (the phase of this parity is open)
+          if (phase != o.phase + 1) return 1;
+        } else if (phase != o.phase) {
+          return 1;
+        }
+        moved = true;
+        const unsigned long long next = at + (1ull << 8 * i);
+        if (seen.insert(next).second) todo.push_back(next);
+      }
+      if (!moved && !done) return 2;
+    }
+  }
+  std::printf("%ld\n", states);
+  return 0;
+}
+"""
+
+
+def test_issuers_turns_meet_their_own_phase(tmp_path):
+    """No turn of one unit counts for a wait of another, whatever the order in which the warps run; and the model finds
+    the turn that comes early where issuer 0 does not wait for issuer 1 to begin a unit."""
+    src = tmp_path / "turns.cpp"
+    src.write_text(TURNS)
+    for name, flags, code in (("turns", [], 0), ("early", ["-DPTD_NO_ENTRY"], 1)):
+        exe = tmp_path / name
+        subprocess.run(["g++", "-O2", "-std=c++17", *flags, "-I", os.path.join(ROOT, "paper_2607_10661_gb300", "csrc"), str(src),
+                        "-o", str(exe)], check=True)
+        r = subprocess.run([str(exe)], capture_output=True, text=True)
+        assert r.returncode == code, (name, r.returncode, r.stdout)
+        assert code or int(r.stdout) > 10 ** 5
+
+
 def test_index_division_is_exact(tmp_path):
     src, exe = tmp_path / "divide.cpp", tmp_path / "divide"
     src.write_text(r"""
