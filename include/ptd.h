@@ -347,9 +347,8 @@ ptd_status ptd_pool_retrieve(const void* pool, int32_t capacity, const int32_t* 
  *   k, v [num_layers][N_tot][num_kv_heads][D]: k[l'] rotated, k[l'] and v[l'] written to
  *   cache layer l, slot C_b + i;
  * rotation: for j < D/2 the pair (x_j, x_{j+D/2}) turns by p * rope_base^(-2j/D)
- * (RoFormer's rotary encoding in the rotate-half layout of Llama-family models; the angle
- * is carried as an fp32 pair from inverse frequencies computed in double, about 1e-7
- * relative).  positions_out [N_tot] (device, may be NULL)
+ * (RoFormer's rotary encoding in the rotate-half layout of Llama-family models; its cosine
+ * and sine are within 2^-23 + p 2^-52 for any p).  positions_out [N_tot] (device, may be NULL)
  * receives p.  A tree that is not one, or a slot outside the cache (or a page outside the
  * pool), sets PTD_ERR_INVALID_TREE in dev_status; that node writes nothing.  q must not
  * alias k or v.  One launch, one CTA per node and group of layers.  This is what puts the tree's K/V

@@ -672,13 +672,14 @@ ptd_status ptd_pool_retrieve(const void* pool, int32_t capacity, const int32_t* 
 }
 
 namespace {
-// base^(-2j/D), j < D/2, as fp32 pairs from double.
+// base^(-2j/D) / 2 pi, j < D/2, in 2^-64: the power from double, at most 1 (2^63 of it is a whole number but for powers
+// below 2^-10, whose last bits do not matter), times 2^64 / pi.
 ptd::RopeFreqs rope_freqs(float base, int D) {
+  constexpr uint64_t kOverPi = 5871781006564002453ull;
   ptd::RopeFreqs f = {};
   for (int j = 0; j < D / 2; ++j) {
-    const double x = std::pow((double)base, -2.0 * j / D);
-    f.hi[j] = (float)x;
-    f.lo[j] = (float)(x - (double)f.hi[j]);
+    const uint64_t x = (uint64_t)(std::pow((double)base, -2.0 * j / D) * 0x1p63);
+    f.turns[j] = (uint64_t)(((unsigned __int128)x * kOverPi) >> 64);
   }
   return f;
 }

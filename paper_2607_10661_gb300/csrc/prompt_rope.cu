@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     if (!fits && first_slot != -1) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
   }
   for (int x = t; x < tokens * half; x += kThreads)
-    turn_of<true>(freqs, p.positions[n0 + x / half], x % half, cos_s[x], sin_s[x]);
+    turn_of(freqs, p.positions[n0 + x / half], x % half, cos_s[x], sin_s[x]);
   __syncthreads();
   for (int e0 = t;; load_items(e0)) {
 #pragma unroll
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kScalarThreads)
     if (t == 0 && slot != -1) atomicMax(p.dev_status, (int)PTD_ERR_INVALID_BATCH);
     return;
   }
-  for (int j = t; j < half; j += kScalarThreads) turn_of<true>(freqs, p.positions[n], j, cos_s[j], sin_s[j]);
+  for (int j = t; j < half; j += kScalarThreads) turn_of(freqs, p.positions[n], j, cos_s[j], sin_s[j]);
   __syncthreads();
   const T* q = static_cast<const T*>(p.q) + n * p.q_stride;
   const T* k = static_cast<const T*>(p.k) + n * p.k_stride;

@@ -62,19 +62,16 @@ __device__ __forceinline__ uint4 pack16(const Vec<T>& r) {
   }
 }
 
-// cos and sin of pos * f_j.  angle = pos * (hi + lo) = a_hi + e (e exact up to pos * lo's rounding); sin and
-// cos of a_hi, corrected to first order in e (|e| < 1e-3 up to angles of 16384), or to second order
-// (kFar: |e| < 2^-7 up to angles of 2^17, and e^3 / 6 is what is left).
-template <bool kFar>
-__device__ __forceinline__ void turn_of(const RopeFreqs& freqs, int pos_i, int j, float& c, float& s) {
-  const float pos = (float)pos_i, fh = freqs.hi[j];
-  const float a_hi = __fmul_rn(pos, fh);
-  const float a_err = fmaf(pos, fh, -a_hi) + pos * freqs.lo[j];
+// cos and sin of pos * f_j, f_j in 2^-64 turns: the product modulo 2^64 is the angle modulo a turn, with no loss for any
+// position but that of f_j itself (2^-53 of it, so pos * 2^-53 of the angle).  Its top 24 bits, a float, go through
+// sincospif, the next eight (|e| < 2^-21) are added to first order; what is left is 2^-32 of a turn.
+__device__ __forceinline__ void turn_of(const RopeFreqs& freqs, int pos, int j, float& c, float& s) {
+  const int turn = (int)(((unsigned long long)(long long)pos * freqs.turns[j]) >> 32);   // of 2^-32, in [-1/2, 1/2)
+  const float e = (float)(turn & 255) * (6.2831853f / 4294967296.f);
   float s0, c0;
-  sincosf(a_hi, &s0, &c0);
-  const float near = kFar ? fmaf(-0.5f * a_err, a_err, 1.f) : 1.f;
-  s = fmaf(a_err, c0, kFar ? s0 * near : s0);
-  c = fmaf(-a_err, s0, kFar ? c0 * near : c0);
+  sincospif((float)(turn & ~255) * (1.f / 2147483648.f), &s0, &c0);
+  s = fmaf(e, c0, s0);
+  c = fmaf(-e, s0, c0);
 }
 
 }  // namespace rope

@@ -6,9 +6,8 @@
 // (one load per thread), counts |pi(i)| by walking up (<= 128 shared-memory reads), builds the
 // node's D/2 (cos, sin) pairs once, then, with 16-byte vectors where rows allow, turns every pair
 // (x_j, x_{j+D/2}) of the node's query heads (in place) and key heads by p * base^(-2j/D)
-// (RoFormer's rotation, rotate-half layout; the angle p * f is carried as an fp32 pair
-// from a float-float f computed in double on the host, so that its rounding error is
-// corrected to first order after sincosf) and writes the rotated keys and the values into
+// (RoFormer's rotation, rotate-half layout; the angle's arithmetic is in rope_parts.cuh)
+// and writes the rotated keys and the values into
 // cache slot C_b + i of each layer (contiguous or paged); a slot outside the cache (or a
 // page number outside the pool) writes nothing and sets the status.
 //
@@ -96,7 +95,7 @@ __device__ __forceinline__ bool find_place(const int32_t* node_offsets, const in
 
 // cos and sin of pos * f_j for j < half, into shared memory (the caller's barrier follows).
 __device__ __forceinline__ void make_table(const RopeFreqs& freqs, int pos, int half, float* cos_s, float* sin_s) {
-  for (int j = threadIdx.x; j < half; j += kThreads) turn_of<false>(freqs, pos, j, cos_s[j], sin_s[j]);
+  for (int j = threadIdx.x; j < half; j += kThreads) turn_of(freqs, pos, j, cos_s[j], sin_s[j]);
 }
 
 // Rows of 16-byte vectors.  A row of q, k or v is cut into items of two vectors, columns j and

@@ -7,8 +7,7 @@
 namespace ptd {
 constexpr int kMaxRopeHalf = 128;   // D / 2 for D <= 256
 struct RopeFreqs {
-  float hi[kMaxRopeHalf];           // base^(-2i/D) = hi + lo, from double
-  float lo[kMaxRopeHalf];
+  unsigned long long turns[kMaxRopeHalf];   // base^(-2i/D) / 2 pi, in 2^-64
 };
 cudaError_t launch_tree_rope(const int32_t* node_offsets, const int32_t* parents, const int32_t* ctx_lens,
                              int batch, int n_total, bool bf16, int head_dim, int hq, int hkv, void* q, const void* k,

@@ -6,6 +6,7 @@ by 2^-8 of itself at most (bf16 caches), so S 2^-8; the output's rounding, |o| 2
 accumulated over D products in fp32 is off by D 2^-23 sum |q k| at most (a truncating accumulator), its scaling
 and the exponential by 2^-22 of the largest |score| + 2^-21, and a score's error e changes numerator and
 denominator by e each: 2 e S; fp32 sums over n keys add n 2^-24 S to each of both."""
+import decimal
 import math
 
 import numpy as np
@@ -793,3 +794,57 @@ def test_units_whose_second_m_tile_sees_more(seqs):
         x.attend()
         assert int(x.status) == 0
         x.check()
+
+
+PI = decimal.Decimal("3.14159265358979323846264338327950288419716939937510582097494459")
+
+
+def _exact_rope(x, positions, base):
+    """The rotation with angles of 60 digits.  An entry of the kernel's table is off by sincospif's 1 ulp (2^-24), the
+    rounding of its correction (2^-25) and 2^-32 turns, so below 2^-23, and by p times a frequency's error
+    (2^-53 of the power, and a little more where 2j/D is rounded): p 2^-52.  The products and their sum add 2^-23."""
+    with decimal.localcontext(decimal.Context(prec=60)):
+        half = x.shape[-1] // 2
+        freq = [decimal.Decimal(base) ** (decimal.Decimal(-2 * j) / (2 * half)) for j in range(half)]
+        angle = np.array([[float(p * f % (2 * PI)) for f in freq] for p in positions])
+    c, s = np.cos(angle)[:, None, :], np.sin(angle)[:, None, :]
+    a, b = x[..., :half], x[..., half:]
+    table = (2.0 ** -23 + np.array(positions, float) * 2.0 ** -52)[:, None, None]
+    size = (np.abs(a) + np.abs(b)) * (table + 2.0 ** -23)
+    return np.concatenate([a * c - b * s, a * s + b * c], -1), np.concatenate([size, size], -1)
+
+
+FAR = [0, 1, 2 ** 17, 2 ** 18 + 1, 2 ** 19, 2 ** 20, 2 ** 20 + 3, 2 ** 22 + 5, 2 ** 23 + 1, 2 ** 24 + 1, 2 ** 27 + 33, 2 ** 30 - 1]
+
+
+@pytest.mark.parametrize("base", [10000.0, 500000.0])
+@pytest.mark.parametrize("dtype,hq,hkv,d", [(BF16, 2, 1, 128), (F32, 2, 1, 128), (F32, 2, 2, 64), (F32, 2, 2, 6), (BF16, 1, 1, 256)])
+def test_far_positions_are_rotated_exactly(dtype, hq, hkv, d, base):
+    n = len(FAR)
+    g = torch.Generator(device=DEV).manual_seed(22)
+    kc, vc = (torch.zeros((1, 1, n, hkv, d), dtype=dtype, device=DEV) for _ in range(2))
+    q, k, v = (torch.randn((n, h, d), generator=g, device=DEV).to(dtype) for h in (hq, hkv, hkv))
+    prompt = ptd.Prompt(torch.tensor([0, n], **I32), torch.zeros(1, **I32), n, n, 0)
+    slots, pos, status, out = torch.arange(n, **I32), torch.tensor(FAR, **I32), torch.zeros(1, **I32), torch.empty_like(q)
+    ptd.prompt_rope_append(prompt, ptd.KVCache(kc, vc, hkv, d), 0, slots, pos, q, k, v, out, base, status)
+    assert int(status) == 0
+    for x, got in ((q, out), (k, kc[0, 0])):
+        want, tol = _exact_rope(x.double().cpu().numpy(), FAR, base)
+        tol += np.abs(want) * (2.0 ** -8 if dtype == BF16 else 2.0 ** -24)
+        assert (np.abs(got.double().cpu().numpy() - want) <= tol).all()
+
+
+def test_far_trees_are_rotated_exactly():
+    """A tree behind 2^24 + 1 committed tokens: the same table as a prompt's."""
+    ctx, hq, hkv, d, base = 2 ** 24 + 1, 2, 1, 8, 10000.0
+    kc, vc = (torch.zeros((1, 1, ctx + 8, hkv, d), device=DEV) for _ in range(2))
+    g = torch.Generator(device=DEV).manual_seed(23)
+    q, k, v = (torch.randn((4, h, d), generator=g, device=DEV) for h in (hq, hkv, hkv))
+    status, before = torch.zeros(1, **I32), q.double().cpu().numpy()
+    tree = ptd.Tree(torch.tensor([0, 4], **I32), torch.tensor([-1, 0, 0, 1], **I32), torch.tensor([ctx], **I32), 4, ctx)
+    ptd.tree_rope_append(tree, ptd.KVCache(kc, vc, hkv, d), 0, q, hq, k, v, base, status)
+    assert int(status) == 0
+    pos = [ctx, ctx + 1, ctx + 1, ctx + 2]
+    for x, got in ((before, q), (k.double().cpu().numpy(), kc[0, 0, ctx:ctx + 4])):
+        want, tol = _exact_rope(x, pos, base)
+        assert (np.abs(got.double().cpu().numpy() - want) <= tol + np.abs(want) * 2.0 ** -24).all()
