@@ -26,6 +26,9 @@ namespace ptd {
 namespace ps {
 
 constexpr int kThreads = 512;
+// Dynamic shared memory of the largest batch.  The limit belongs to the kernel, not to a launch: a call that set its own
+// batch's size could lower it between another thread's call and its launch.
+constexpr size_t kMostSmem = (5 * (size_t)PTD_MAX_PROMPT_BATCH + 1) * sizeof(int);
 
 // The last i in [0, n) with a[i] <= x (a[0] <= x; a non-decreasing).
 __device__ __forceinline__ int last_at_most(const int* a, int n, int x) {
@@ -175,7 +178,7 @@ cudaError_t launch_prompt_slots(const PromptSlotsParams& p, int sms, cudaStream_
   if (pool && ctas < 48) ctas = 48;
   const auto kernel = pool ? ps::prompt_slots_kernel<true> : ps::prompt_slots_kernel<false>;
   if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ps::kMostSmem);
     if (e != cudaSuccess) return e;
   }
   return launch_chained(kernel, dim3(ctas), dim3(ps::kThreads), smem, stream, 0, p, per);

@@ -8,6 +8,7 @@ and the exponential by 2^-22 of the largest |score| + 2^-21, and a score's error
 denominator by e each: 2 e S; fp32 sums over n keys add n 2^-24 S to each of both."""
 import decimal
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -848,3 +849,33 @@ def test_far_trees_are_rotated_exactly():
     for x, got in ((before, q), (k.double().cpu().numpy(), kc[0, 0, ctx:ctx + 4])):
         want, tol = _exact_rope(x, pos, base)
         assert (np.abs(got.double().cpu().numpy() - want) <= tol + np.abs(want) * 2.0 ** -24).all()
+
+
+def test_slots_of_small_and_large_batches_from_two_threads():
+    """Batches that need 54 KB and 160 KB of shared memory, from two threads at once: every call is enqueued."""
+    failed, sizes = [], (2700, 8192)
+
+    def work(batch):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                table = torch.arange(batch, **I32).view(batch, 1)
+                cache = _small_cache(batch, 16, table)
+                held = torch.ones(batch, **I32)
+                pool = ptd.PagePool(torch.full((batch,), -1, **I32), torch.zeros(1, **I32), held, torch.empty_like(held),
+                                    torch.zeros(1, **I32))
+                prompt = ptd.Prompt(torch.arange(batch + 1, **I32), torch.full((batch,), 3, **I32), batch, 1, 3)
+                slots, pos, status = torch.empty(batch, **I32), torch.empty(batch, **I32), torch.zeros(1, **I32)
+                for _ in range(3000):
+                    ptd.prompt_slots(prompt, cache, slots, pos, status, pool)
+                stream.synchronize()
+                assert int(status) == 0 and torch.equal(slots, torch.arange(batch, **I32) * 16 + 3)
+        except Exception as e:
+            failed.append((batch, repr(e)))
+
+    threads = [threading.Thread(target=work, args=(b,)) for b in sizes for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed

@@ -3,6 +3,7 @@ for the host) against a sort, the host's refusals, and the oracle's own examples
 import ctypes
 import os
 import random
+import re
 import subprocess
 
 import numpy as np
@@ -520,3 +521,16 @@ def test_native_prompt_calls_keep_to_the_current_device(lib, monkeypatch):
     finally:
         ptd._calls = None
         ptd._native()
+
+
+def test_no_call_sets_a_kernels_limits_by_its_own_size():
+    """Attributes belong to the kernel: threads that set them by their call's sizes undo one another's, so that every
+    limit of dynamic shared memory is a constant."""
+    csrc, found = os.path.join(ROOT, "paper_2607_10661_gb300", "csrc"), 0
+    for name in sorted(os.listdir(csrc)):
+        text = open(os.path.join(csrc, name)).read() if name.endswith((".cu", ".cuh")) else ""
+        for m in re.finditer(r"cudaFuncAttributeMaxDynamicSharedMemorySize,([^;]*);", text):
+            found += 1
+            value = re.sub(r"[\\\s]", "", m.group(1))
+            assert re.fullmatch(r"\(int\)([\w<>,]+::)*k[A-Z]\w*\)", value), (name, value)
+    assert found >= 8
