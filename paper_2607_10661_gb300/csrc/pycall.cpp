@@ -160,6 +160,18 @@ struct Args {
     if (d == nullptr || !PyLong_CheckExact(d) || PyLong_AsLongLong(d) != device) fail();
     Py_XDECREF(d);
   }
+  // The batch is the contiguous cache's, or has a row each in its block table (a batch below 1 is the library's to refuse).
+  void batch_of(PyObject* o, const ptd_prompt* prompt, const ptd_kv_cache* cache) {
+    if (!ok || prompt->batch < 1) return;
+    const bool paged = cache->page_size > 0;
+    PyObject* t = PyObject_GetAttr(o, paged ? s_block_table : s_k);
+    PyObject* d = t != nullptr ? PyObject_GetAttr(t, s_shape) : nullptr;
+    int64_t rows = -1;
+    if (d != nullptr && PyTuple_Check(d) && PyTuple_GET_SIZE(d) >= 2) rows = PyLong_AsLongLong(PyTuple_GET_ITEM(d, paged ? 0 : 1));
+    Py_XDECREF(d);
+    Py_XDECREF(t);
+    if (PyErr_Occurred() || (paged ? rows < prompt->batch : rows != prompt->batch)) fail();
+  }
   // an int32 tensor of `count` elements
   int32_t* i32_of(int64_t count) {
     PyObject* o = next();
@@ -524,6 +536,7 @@ PyObject* prompt_slots(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!g.ok) Py_RETURN_NONE;
   const ptd_prompt* prompt = g.structure<ptd_prompt>();
   const ptd_kv_cache* cache = g.structure<ptd_kv_cache>();
+  if (g.ok) g.batch_of(a[1], prompt, cache);
   if (!g.ok) Py_RETURN_NONE;
   const ptd_page_pool* held = a[2] == Py_None ? (g.next(), nullptr) : g.structure<ptd_page_pool>();
   if (!g.ok) Py_RETURN_NONE;
@@ -564,6 +577,7 @@ PyObject* prompt_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!g.ok) Py_RETURN_NONE;
   const ptd_prompt* prompt = g.structure<ptd_prompt>();
   const ptd_kv_cache* cache = g.structure<ptd_kv_cache>();
+  if (g.ok) g.batch_of(a[1], prompt, cache);
   if (!g.ok) Py_RETURN_NONE;
   PyObject* dt = cache->dtype == PTD_BF16 ? g_bf16 : g_f32;
   const int32_t layer = g.num();
@@ -591,6 +605,7 @@ PyObject* prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!g.ok) Py_RETURN_NONE;
   const ptd_prompt* prompt = g.structure<ptd_prompt>();
   const ptd_kv_cache* cache = g.structure<ptd_kv_cache>();
+  if (g.ok) g.batch_of(a[1], prompt, cache);
   if (!g.ok) Py_RETURN_NONE;
   PyObject* dt = cache->dtype == PTD_BF16 ? g_bf16 : g_f32;
   const int32_t layer = g.num();

@@ -634,6 +634,16 @@ def _one_device(*tensors):
     return torch.cuda.device(devices.pop())
 
 
+def _batch_of_cache(prompt: Prompt, cache: KVCache) -> None:
+    """A contiguous cache's rows belong to its own batch (they set a layer's size); a block table needs a row per
+    sequence."""
+    if cache.page_size:
+        if cache.block_table.shape[0] < prompt.batch:
+            raise ValueError(f"block_table has {cache.block_table.shape[0]} rows for {prompt.batch} sequences")
+    elif cache.k.shape[1] != prompt.batch:
+        raise ValueError(f"the cache has rows for {cache.k.shape[1]} sequences, the batch has {prompt.batch}")
+
+
 def _rows3(t: torch.Tensor, name: str, dtype, rows: int, heads: Optional[int], dim: int):
     """Pointer, token stride and heads of a [rows, heads, dim] tensor whose tokens may be apart."""
     if not isinstance(t, torch.Tensor):
@@ -657,6 +667,7 @@ def prompt_slots(prompt: Prompt, cache: KVCache, slots: torch.Tensor, positions:
                                            stream if stream is None else _stream(stream))
     if r is not None:
         return _launched(r, "ptd_prompt_slots")
+    _batch_of_cache(prompt, cache)
     n = prompt.total_tokens
     for t, nm in ((slots, "slots"), (positions, "positions")):
         if t.numel() != n:
@@ -688,6 +699,7 @@ def prompt_rope_append(prompt: Prompt, cache: KVCache, layer: int, slots: torch.
                                                  stream if stream is None else _stream(stream))
     if r is not None:
         return _launched(r, "ptd_prompt_rope_append")
+    _batch_of_cache(prompt, cache)
     n, d, dt = prompt.total_tokens, cache.head_dim, cache.k.dtype
     qp, qs, hq = _rows3(q, "q", dt, n, None, d)
     kp, ks, _ = _rows3(k, "k", dt, n, cache.num_kv_heads, d)
@@ -716,6 +728,7 @@ def prompt_attention(prompt: Prompt, cache: KVCache, layer: int, q: torch.Tensor
                                                stream if stream is None else _stream(stream))
     if r is not None:
         return _launched(r, "ptd_prompt_attention")
+    _batch_of_cache(prompt, cache)
     n, d, dt = prompt.total_tokens, cache.head_dim, cache.k.dtype
     qp, qs, hq = _rows3(q, "q", dt, n, None, d)
     if tuple(out.shape) != (n, hq, d):

@@ -879,3 +879,26 @@ def test_slots_of_small_and_large_batches_from_two_threads():
     for t in threads:
         t.join()
     assert not failed
+
+
+def test_batches_that_are_not_the_caches_are_refused():
+    """Two prompts into a contiguous cache of three sequences, or of one; a block table with too few rows."""
+    x, y = Batch([(3, 4), (0, 2)], 8, 2, seed=61), Batch([(3, 4), (0, 2)], 8, 2, page=16, seed=61)
+    slots, pos = torch.full((x.N,), 5, **I32), torch.full((x.N,), 5, **I32)
+    caches = [ptd.KVCache(x.k.repeat(2, 2, 1, 1, 1)[:, :n].contiguous(),
+                          x.v.repeat(2, 2, 1, 1, 1)[:, :n].contiguous(), 2, 128) for n in (1, 3)]
+    caches.append(ptd.KVCache(y.k, y.v, 2, 128, 16, y.table[:1].contiguous()))
+    k = x.q[:, :2].contiguous()
+    for cache in caches:
+        for call in (lambda: ptd.prompt_slots(x.prompt, cache, slots, pos, x.status),
+                     lambda: ptd.prompt_rope_append(x.prompt, cache, 0, slots, pos, x.q, k, k, x.out, 1e4, x.status),
+                     lambda: ptd.prompt_attention(x.prompt, cache, 0, x.q, x.out, x.status)):
+            with pytest.raises(ValueError, match="sequences"):
+                call()
+    torch.cuda.synchronize()
+    assert int(x.status) == 0 and (x.out == 7.0).all() and (slots == 5).all() and (pos == 5).all()
+    # more rows in the table than sequences in the batch are fine
+    more = ptd.KVCache(y.k, y.v, 2, 128, 16, torch.cat([y.table, torch.full_like(y.table[:1], -1)]))
+    y.cache = more
+    y.attend()
+    y.check()

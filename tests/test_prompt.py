@@ -534,3 +534,44 @@ def test_no_call_sets_a_kernels_limits_by_its_own_size():
             value = re.sub(r"[\\\s]", "", m.group(1))
             assert re.fullmatch(r"\(int\)([\w<>,]+::)*k[A-Z]\w*\)", value), (name, value)
     assert found >= 8
+
+
+def test_batches_that_are_not_the_caches_are_refused(lib, monkeypatch):
+    """A contiguous cache of another number of sequences (its layers would begin elsewhere), a block table of too few
+    rows: not taken natively, and a ValueError of each call otherwise."""
+    import types
+
+    import torch
+
+    from paper_2607_10661_gb300 import ptd
+
+    class Refuse:
+        def __getattr__(self, name):
+            return lambda *a: None
+
+    shapes = ((0, (2, 2), True), (0, (2, 1), False), (0, (2, 3), False), (16, (2, 10), True), (16, (3, 10), True),
+              (16, (1, 10), False))
+    try:
+        for page, shape, good in shapes:
+            calls, Fake = _native_with(ptd, monkeypatch, 0, 0)
+            i, x = Fake(), Fake(torch.bfloat16)
+            prompt = types.SimpleNamespace(c=_prompt(ptd), ctx_lens=Fake(), batch=2, total_tokens=10)
+            cache = types.SimpleNamespace(c=_cache(ptd, page=page, hkv=2), page_size=page, k=Fake(torch.bfloat16),
+                                          block_table=Fake() if page else None, head_dim=128, num_kv_heads=2)
+            (cache.block_table if page else cache.k).shape = shape if page else shape + (300, 2, 128)
+            want = -ptd.INVALID_ARG if good else None   # (taken: layer 9, slots on positions)
+            assert calls.prompt_attention(prompt, cache, 9, x, x, i, 0.0, None, 0) == want, shape
+            assert calls.prompt_rope_append(prompt, cache, 9, i, i, x, x, x, x, 1e4, i, 0) == want, shape
+            assert calls.prompt_slots(prompt, cache, None, i, i, i, 0) == want, shape
+            if good:
+                continue
+            with monkeypatch.context() as m:
+                m.setattr(ptd, "_calls", Refuse())
+                for call in (lambda: ptd.prompt_attention(prompt, cache, 9, x, x, i, stream=0),
+                             lambda: ptd.prompt_rope_append(prompt, cache, 9, i, i, x, x, x, x, 1e4, i, stream=0),
+                             lambda: ptd.prompt_slots(prompt, cache, i, i, i, stream=0)):
+                    with pytest.raises(ValueError, match="sequences"):
+                        call()
+    finally:
+        ptd._calls = None
+        ptd._native()
