@@ -553,7 +553,8 @@ ptd_status ptd_prompt_slots(const ptd_prompt* prompt, const ptd_kv_cache* cache,
  *     back to back, tokens q_stride, k_stride, v_stride elements apart (at least a token's elements), e.g.
  *     views of one fused product's rows.
  *   q_out: as q, q_out_stride apart; it may be q itself (same pointer and stride), and overlaps q, k, v
- *     in no other way.  slots of different tokens differ.
+ *     in no other way (PTD_ERR_INVALID_ARG; its rows may lie between theirs if the strides are the same).  slots of different
+ *     tokens differ.
  * D even, at most 256; (num_q_heads + 2 num_kv_heads) * D below 2^31.  One launch. */
 ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t layer,
                                   const int32_t* slots, const int32_t* positions, const void* q, int64_t q_stride,
@@ -567,7 +568,7 @@ ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* 
  * The new tokens' own K/V are in the cache already (ptd_prompt_rope_append).
  *   q [total_tokens][num_q_heads][D], tokens q_stride elements apart; out [total_tokens][num_q_heads][D] back to
  *     back; both of cache->dtype and 16-byte aligned, q_stride times the element size a multiple of 16; out
- *     overlaps no input.
+ *     and the workspace overlap no input and not one another (PTD_ERR_INVALID_ARG).
  *     fp32 accumulation and softmax statistics; the weights are rounded to bf16 for a bf16 cache.
  *   Rows behind the last sequence are left as they were, as are those of a sequence out of range (see
  *     ptd_prompt_slots; PTD_ERR_INVALID_BATCH).  A page number outside the cache sets PTD_ERR_INVALID_BATCH too:

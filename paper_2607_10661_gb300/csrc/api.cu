@@ -18,6 +18,7 @@
 #include "pool.cuh"
 #include "tree_rope.cuh"
 #include "lm_head.cuh"
+#include "memory_rows.cuh"
 #include "prompt.cuh"
 
 namespace ptd {
@@ -734,10 +735,22 @@ ptd::PromptBounds prompt_bounds(const ptd_prompt* p, const ptd_kv_cache* c) {
           c->page_size > 0 ? (int64_t)c->max_pages * c->page_size : (int64_t)c->seq_capacity};
 }
 
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
+// Whether one of the first `written` sets of rows meets another one (sets at NULL are not there).
+bool written_rows_meet(const ptd::MemoryRows* rows, int written, int all) {
+  for (int i = 0; i < written; ++i)
+    for (int j = i + 1; j < all; ++j)
+      if (rows[i].at && rows[j].at && ptd::rows_meet(rows[i], rows[j])) return true;
+  return false;
 }
+
+// Bytes of a layer's or a stack's K (or V), of a block table (0: contiguous).
+int64_t cache_bytes(const ptd_kv_cache* c, int batch, int layers) {
+  return cache_rows_per_layer(c, batch) * layers * c->num_kv_heads * c->head_dim * (int64_t)dtype_size(c->dtype);
+}
+int64_t table_bytes(const ptd_kv_cache* c, int batch) { return c->page_size > 0 ? (int64_t)batch * c->max_pages * 4 : 0; }
+
+// Tokens `stride` elements apart end within 62 bits.
+bool stride_fits(int64_t stride, int tokens, int64_t es) { return tokens == 1 || stride <= (INT64_MAX >> 1) / es / tokens; }
 
 // Checked arguments of a prompt attention without its tensors: the sizes and the plan's part.
 ptd_status check_prompt_attention(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t hq) {
@@ -787,19 +800,20 @@ ptd_status ptd_prompt_slots(const ptd_prompt* prompt, const ptd_kv_cache* cache,
     if ((int64_t)prompt->batch * cache->max_pages > INT32_MAX) return PTD_ERR_UNSUPPORTED;
   }
   // what is written overlaps nothing else that the call touches: other CTAs still read it, or write it too
-  const size_t B4 = (size_t)prompt->batch * 4, N4 = (size_t)prompt->total_tokens * 4;
-  const size_t table = cache->page_size > 0 ? B4 * cache->max_pages : 0;
-  const struct Range {
-    const void* at;
-    size_t bytes;
-  } ranges[10] = {{slots, N4}, {positions, N4}, {pages ? pages->new_held : nullptr, B4}, {pages ? pages->new_free_count : nullptr, 4},
-                  {pages ? pages->free_pages : nullptr, (size_t)cache->num_pages * 4}, {table ? cache->block_table : nullptr, table},
-                  {prompt->token_offsets, B4 + 4}, {prompt->ctx_lens, B4}, {pages ? pages->held : nullptr, B4},
-                  {pages ? pages->free_count : nullptr, 4}};
-  for (int i = 0; i < (pages ? 6 : 2); ++i)   // (written: the first two, and with a pool the first six)
-    for (int j = i + 1; j < 10; ++j)
-      if (ranges[i].at && ranges[j].at && overlap(ranges[i].at, ranges[i].bytes, ranges[j].at, ranges[j].bytes))
-        return PTD_ERR_INVALID_ARG;
+  const int64_t B4 = (int64_t)prompt->batch * 4, N4 = (int64_t)prompt->total_tokens * 4;
+  using ptd::memory_rows;
+  const ptd::MemoryRows rows[11] = {memory_rows(slots, N4),
+                                    memory_rows(positions, N4),
+                                    memory_rows(dev_status, 4),
+                                    memory_rows(pages ? pages->new_held : nullptr, B4),
+                                    memory_rows(pages ? pages->new_free_count : nullptr, 4),
+                                    memory_rows(pages ? pages->free_pages : nullptr, (int64_t)cache->num_pages * 4),
+                                    memory_rows(cache->block_table, table_bytes(cache, prompt->batch)),
+                                    memory_rows(prompt->token_offsets, B4 + 4),
+                                    memory_rows(prompt->ctx_lens, B4),
+                                    memory_rows(pages ? pages->held : nullptr, B4),
+                                    memory_rows(pages ? pages->free_count : nullptr, 4)};
+  if (written_rows_meet(rows, pages ? 7 : 3, 11)) return PTD_ERR_INVALID_ARG;
   if (pages) {
     p.free_pages = pages->free_pages;
     p.free_count = pages->free_count;
@@ -846,7 +860,17 @@ ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* 
   if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) |
        reinterpret_cast<uintptr_t>(q_out)) % es != 0)
     return PTD_ERR_INVALID_ARG;
-  if (q_out == q && q_out_stride != q_stride) return PTD_ERR_INVALID_ARG;   // rows would overlap other rows
+  const int N = prompt->total_tokens;
+  for (const int64_t stride : {q_stride, k_stride, v_stride, q_out_stride})
+    if (!stride_fits(stride, N, es)) return PTD_ERR_INVALID_ARG;
+  // q_out is q, or meets none of the three: other CTAs still read them
+  const auto rows_of = [&](const void* x, int64_t elements, int64_t stride) {
+    return ptd::memory_rows(x, elements * (int64_t)es, stride * (int64_t)es, N);
+  };
+  const bool in_place = q_out == q && (q_out_stride == q_stride || N == 1);
+  const ptd::MemoryRows rows[4] = {rows_of(q_out, qe, q_out_stride), rows_of(in_place ? nullptr : q, qe, q_stride),
+                                   rows_of(k, ke, k_stride), rows_of(v, ke, v_stride)};
+  if (written_rows_meet(rows, 1, 4)) return PTD_ERR_INVALID_ARG;
   ptd::PromptRopeParams p = {};
   p.slots = slots;
   p.positions = positions;
@@ -888,7 +912,7 @@ ptd_status ptd_prompt_attention(const ptd_prompt* prompt, const ptd_kv_cache* ca
   const int D = cache->head_dim;
   const size_t es = dtype_size(cache->dtype);
   if (layer < 0 || layer >= cache->num_layers || !q || !out || !dev_status || q_stride < (int64_t)num_q_heads * D ||
-      !aligned16(q) || !aligned16(out) || (q_stride * (int64_t)es) % 16 != 0)
+      !aligned16(q) || !aligned16(out) || !stride_fits(q_stride, prompt->total_tokens, es) || (q_stride * (int64_t)es) % 16 != 0)
     return PTD_ERR_INVALID_ARG;
   ptd::PromptAttnParams p = prompt_attention_params(prompt, cache, num_q_heads);
   p.q = q;
@@ -900,9 +924,23 @@ ptd_status ptd_prompt_attention(const ptd_prompt* prompt, const ptd_kv_cache* ca
   p.scale_log2 = sc * 1.4426950408889634f;
   p.part_o = static_cast<float*>(workspace);
   const bool bf16 = cache->dtype == PTD_BF16;
-  ptd::plan_prompt_attention(p, bf16, workspace != nullptr && aligned16(workspace) ? workspace_bytes : 0,
-                             num_sms_of_current_device());
+  const size_t used = ptd::plan_prompt_attention(p, bf16, workspace != nullptr && aligned16(workspace) ? workspace_bytes : 0,
+                                                 num_sms_of_current_device());
   if ((int64_t)p.places * p.tile_heads * p.splits > INT32_MAX) return PTD_ERR_UNSUPPORTED;
+  {   // out and the scratch overlap nothing else: other CTAs still read it
+    using ptd::memory_rows;
+    const int B = prompt->batch, N = prompt->total_tokens;
+    const int64_t row = (int64_t)num_q_heads * D * (int64_t)es, kv = cache_bytes(cache, B, cache->num_layers);
+    const ptd::MemoryRows rows[8] = {memory_rows(out, row * N),
+                                     memory_rows(used ? workspace : nullptr, (int64_t)used),
+                                     memory_rows(q, row, q_stride * (int64_t)es, N),
+                                     memory_rows(cache->k, kv),
+                                     memory_rows(cache->v, kv),
+                                     memory_rows(prompt->token_offsets, (int64_t)B * 4 + 4),
+                                     memory_rows(prompt->ctx_lens, (int64_t)B * 4),
+                                     memory_rows(cache->block_table, table_bytes(cache, B))};
+    if (written_rows_meet(rows, 2, 8)) return PTD_ERR_INVALID_ARG;
+  }
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (bf16) {
     if (cache_rows_per_layer(cache, prompt->batch) * cache->num_layers > INT32_MAX) return PTD_ERR_UNSUPPORTED;

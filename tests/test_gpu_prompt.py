@@ -902,3 +902,40 @@ def test_batches_that_are_not_the_caches_are_refused():
     y.cache = more
     y.attend()
     y.check()
+
+
+def test_rotated_queries_beside_their_inputs_and_overlaps():
+    """q_out may lie between the rows of q, k and v of one wide buffer, or be q; on part of them it is refused, as is an
+    attention whose output or scratch lies on what it reads."""
+    n, hq, hkv, d = 40, 8, 2, 128
+    g = torch.Generator(device=DEV).manual_seed(62)
+    w = torch.randn((n, (2 * hq + 2 * hkv) * d), generator=g, device=DEV).to(BF16)
+    q, k, v, out = (w[:, a * d:b * d].view(n, b - a, d) for a, b in ((0, 8), (8, 10), (10, 12), (12, 20)))
+    kc, vc = (torch.zeros((1, 1, n + 3000, hkv, d), dtype=BF16, device=DEV) for _ in range(2))
+    cache = ptd.KVCache(kc, vc, hkv, d)
+    prompt = ptd.Prompt(torch.tensor([0, n], **I32), torch.zeros(1, **I32), n, n, 0)
+    slots, pos, status = torch.arange(n, **I32), torch.arange(n, **I32), torch.zeros(1, **I32)
+    before, want = w.clone(), torch.empty((n, hq, d), dtype=BF16, device=DEV)
+    ptd.prompt_rope_append(prompt, cache, 0, slots, pos, q, k, v, want, 1e4, status)
+    ptd.prompt_rope_append(prompt, cache, 0, slots, pos, q, k, v, out, 1e4, status)
+    assert torch.equal(out, want) and torch.equal(w[:, :12 * d], before[:, :12 * d])
+    for on in (w[:, 4 * d:12 * d], w[:, 6 * d:14 * d], w[:, 11 * d:19 * d]):
+        with pytest.raises(ptd.PtdError):
+            ptd.prompt_rope_append(prompt, cache, 0, slots, pos, q, k, v, on.view(n, hq, d), 1e4, status)
+    flat = w.view(-1)
+    with pytest.raises(ptd.PtdError):
+        ptd.prompt_attention(prompt, cache, 0, q, flat[4 * d:4 * d + n * hq * d].view(n, hq, d), status)
+    with pytest.raises(ptd.PtdError):
+        ptd.prompt_attention(prompt, cache, 0, q, kc.view(-1)[d:d + n * hq * d].view(n, hq, d), status)
+    torch.cuda.synchronize()
+    assert torch.equal(w[:, :12 * d], before[:, :12 * d]) and int(status) == 0
+    far = ptd.Prompt(torch.tensor([0, 1], **I32), torch.tensor([2900], **I32), 1, 1, 2900)
+    size = ptd.prompt_attention_workspace_size(far, cache, hq)
+    assert size > 0
+    room = torch.zeros(hq * d + size // 2, dtype=BF16, device=DEV)   # a row of queries, then the scratch
+    one, query = torch.zeros((1, hq, d), dtype=BF16, device=DEV), room[:hq * d].view(1, hq, d)
+    with pytest.raises(ptd.PtdError):
+        ptd.prompt_attention(far, cache, 0, query, one, status, workspace=room[:size // 2])
+    ptd.prompt_attention(far, cache, 0, query, one, status, workspace=room[hq * d:])
+    torch.cuda.synchronize()
+    assert int(status) == 0

@@ -575,3 +575,90 @@ def test_batches_that_are_not_the_caches_are_refused(lib, monkeypatch):
     finally:
         ptd._calls = None
         ptd._native()
+
+
+def test_rows_in_memory_meet(tmp_path):
+    """Against the sets of bytes, for every pair of small sets of rows; only sets of different steps may be said to meet
+    where they interleave."""
+    src, exe = tmp_path / "rows.cpp", tmp_path / "rows"
+    src.write_text(r"""
+#include <cstdio>
+#include <vector>
+#include "memory_rows.cuh"
+int main() {
+  struct S { long at, bytes, step, count; };
+  std::vector<S> sets;
+  for (long bytes : {0, 1, 3, 5})
+    for (long step : {5, 6, 7, 12})
+      for (long count : {1, 2, 4})
+        sets.push_back({0, bytes, step, count});
+  auto covers = [](const S& s, long x) {
+    for (long i = 0; i < s.count; ++i)
+      if (x >= s.at + i * s.step && x < s.at + i * s.step + s.bytes) return true;
+    return false;
+  };
+  long met = 0, apart = 0;
+  for (const S& a0 : sets)
+    for (const S& b0 : sets)
+      for (long shift = -60; shift <= 60; ++shift) {
+        S a = a0, b = b0;
+        a.at = 100, b.at = 100 + shift;
+        bool want = false;
+        for (long x = 0; x < 300 && !want; ++x) want = covers(a, x) && covers(b, x);
+        const auto rows = [](const S& s) { return ptd::memory_rows(reinterpret_cast<const void*>(s.at), s.bytes, s.step, s.count); };
+        const bool got = ptd::rows_meet(rows(a), rows(b));
+        const bool exact = a.count == 1 || b.count == 1 || a.step == b.step;
+        if (exact ? got != want : want && !got) return std::printf("%ld+%ldx%ld/%ld %ld+%ldx%ld/%ld\n", a.at, a.bytes, a.count, a.step, b.at, b.bytes, b.count, b.step), 1;
+        ++(want ? met : apart);
+      }
+  const auto far = ptd::memory_rows(reinterpret_cast<const void*>(1l << 40), 256, 1l << 31, 1 << 30);   // spans 2^61
+  if (ptd::rows_meet(far, ptd::memory_rows(reinterpret_cast<const void*>((1l << 40) + (1l << 50) + 256), 300))) return 2;
+  if (!ptd::rows_meet(far, ptd::memory_rows(reinterpret_cast<const void*>((1l << 40) + (1l << 50) + 255), 300))) return 3;
+  std::printf("%ld %ld\n", met, apart);
+  return 0;
+}
+""")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I", os.path.join(ROOT, "paper_2607_10661_gb300", "csrc"), str(src),
+                    "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0 and min(map(int, r.stdout.split())) > 1000, (r.returncode, r.stdout)
+
+
+def test_overlaps_are_refused(lib):
+    """What a call writes on what it reads: refused before anything is launched."""
+    from paper_2607_10661_gb300 import ptd
+
+    p = _prompt(ptd)   # 10 tokens
+    paged, plain = _cache(ptd), _cache(ptd, page=0)
+    row, kv = 32 * 128 * 2, 1024 * 2
+
+    def rope(q=7 * A, qs=4096, k=8 * A, ks=1024, v=9 * A, vs=1024, out=10 * A, outs=4096):
+        return lib.ptd_prompt_rope_append(ctypes.byref(p), ctypes.byref(paged), 0, 4 * A, 5 * A, q, qs, 32, k, ks, v, vs, 1e4, out,
+                                          outs, 6 * A, None)
+
+    for kw in (dict(out=7 * A + row), dict(out=7 * A - 16), dict(out=7 * A + 10 * row - 16), dict(out=8 * A), dict(out=9 * A + kv),
+               dict(out=8 * A + 16 - 10 * row), dict(out=7 * A, k=7 * A + 4 * row), dict(out=7 * A, qs=6144, outs=6144, v=7 * A + row - 16, vs=6144),
+               dict(out=7 * A, qs=6144), dict(out=7 * A + 2 * row, qs=6144, outs=6144), dict(qs=2**62), dict(outs=2**61)):
+        assert rope(**kw) == ptd.INVALID_ARG, kw
+
+    def attention(cache=paged, q=7 * A, qs=4096, out=8 * A, ws=None, wsb=0, prompt=p):
+        return lib.ptd_prompt_attention(ctypes.byref(prompt), ctypes.byref(cache), 0, q, qs, 32, 0.0, out, ws, wsb, 6 * A, None)
+
+    layers = 2 * 40 * 16 * kv
+    for kw in (dict(out=7 * A), dict(out=7 * A + 16), dict(out=7 * A + 9 * row), dict(out=7 * A - 9 * row), dict(qs=6144, out=7 * A + 6144 * 2),
+               dict(out=2 * A), dict(out=2 * A + layers - 16), dict(out=3 * A + layers // 2), dict(out=A), dict(out=A + 4096), dict(out=A + 8192),
+               dict(cache=plain, out=3 * A + 2 * 300 * 2 * kv - 16), dict(qs=2**62)):
+        assert attention(**kw) == ptd.INVALID_ARG, kw
+    far = _prompt(ptd, 1, 1, 1, 30000)   # cut into pieces
+    long = _cache(ptd, max_pages=2000)
+    need = lib.ptd_prompt_attention_workspace_size(ctypes.byref(far), ctypes.byref(long), 32)
+    assert need > 0
+    for ws in (8 * A, 7 * A, 8 * A + 16 - need, 7 * A - need + 256, 2 * A + 64, A):
+        assert attention(cache=long, prompt=far, ws=ws, wsb=need) == ptd.INVALID_ARG, ws
+
+    t = paged.block_table
+    for pool in (None, ptd._PagePool(7 * A, 8 * A, 9 * A, 10 * A, 11 * A, t)):
+        on = [4 * A, 5 * A + 36, A, A + 4096, t + 4] + ([] if pool is None else [7 * A + 156, 8 * A, 9 * A + 4, 10 * A, 11 * A])
+        for status in on:
+            assert lib.ptd_prompt_slots(ctypes.byref(p), ctypes.byref(paged), ctypes.byref(pool) if pool else None, 4 * A, 5 * A,
+                                        status, None) == ptd.INVALID_ARG, status
