@@ -717,7 +717,8 @@ def prompt_rope_append(prompt: Prompt, cache: KVCache, layer: int, slots: torch.
 
 
 def prompt_attention_workspace_size(prompt: Prompt, cache: KVCache, num_q_heads: int) -> int:
-    return int(lib().ptd_prompt_attention_workspace_size(ctypes.byref(prompt.c), ctypes.byref(cache.c), int(num_q_heads)))
+    with _one_device(prompt.ctx_lens, cache.k):   # the device that the attention will run on
+        return int(lib().ptd_prompt_attention_workspace_size(ctypes.byref(prompt.c), ctypes.byref(cache.c), int(num_q_heads)))
 
 
 def prompt_attention(prompt: Prompt, cache: KVCache, layer: int, q: torch.Tensor, out: torch.Tensor,

@@ -662,3 +662,35 @@ def test_overlaps_are_refused(lib):
         for status in on:
             assert lib.ptd_prompt_slots(ctypes.byref(p), ctypes.byref(paged), ctypes.byref(pool) if pool else None, 4 * A, 5 * A,
                                         status, None) == ptd.INVALID_ARG, status
+
+
+def test_scratch_is_sized_for_the_tensors_device(monkeypatch):
+    """The size is asked for while the tensors' device is the current one; tensors of two devices are refused."""
+    import types
+
+    import torch
+
+    from paper_2607_10661_gb300 import ptd
+
+    current = [0]
+
+    class Guard:
+        def __init__(self, device):
+            self.device = device.index
+
+        def __enter__(self):
+            self.before, current[0] = current[0], self.device
+
+        def __exit__(self, *exc):
+            current[0] = self.before
+
+    asked = []
+    size = lambda *a: asked.append(current[0]) or 4096
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    monkeypatch.setattr(ptd, "lib", lambda: types.SimpleNamespace(ptd_prompt_attention_workspace_size=size))
+    on = lambda d: types.SimpleNamespace(device=torch.device("cuda", d))
+    prompt, cache = types.SimpleNamespace(c=_prompt(ptd), ctx_lens=on(1)), types.SimpleNamespace(c=_cache(ptd), k=on(1))
+    assert ptd.prompt_attention_workspace_size(prompt, cache, 32) == 4096 and asked == [1] and current == [0]
+    cache.k = on(0)
+    with pytest.raises(ValueError, match="devices"):
+        ptd.prompt_attention_workspace_size(prompt, cache, 32)
