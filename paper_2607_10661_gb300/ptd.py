@@ -295,6 +295,8 @@ class KVCache:
                  block_table: Optional[torch.Tensor] = None):
         if k.shape != v.shape or k.dtype != v.dtype:
             raise ValueError("k and v must have the same shape and dtype")
+        if len({t.device for t in (k, v, block_table) if t is not None}) > 1:   # (the calls look at k's)
+            raise ValueError("k, v and block_table on several devices")
         self.k, self.v, self.block_table = k, v, block_table
         self.num_layers = k.shape[0]
         self.num_kv_heads, self.head_dim, self.page_size = int(num_kv_heads), int(head_dim), int(page_size)

@@ -694,3 +694,19 @@ def test_scratch_is_sized_for_the_tensors_device(monkeypatch):
     cache.k = on(0)
     with pytest.raises(ValueError, match="devices"):
         ptd.prompt_attention_workspace_size(prompt, cache, 32)
+
+
+def test_a_cache_of_several_devices_is_refused():
+    """The prompt calls compare the other tensors' device with k's; v and the block table are on it too."""
+    import types
+
+    import torch
+
+    from paper_2607_10661_gb300 import ptd
+
+    on = lambda d: types.SimpleNamespace(shape=(1, 2, 16, 2, 128), dtype=torch.bfloat16, device=torch.device("cuda", d))
+    for k, v, table in ((0, 1, 0), (0, 0, 1), (1, 0, 0)):
+        with pytest.raises(ValueError, match="devices"):
+            ptd.KVCache(on(k), on(v), 2, 128, 16, on(table))
+    with pytest.raises(ValueError, match="devices"):
+        ptd.KVCache(on(0), on(1), 2, 128)
