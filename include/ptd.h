@@ -500,7 +500,9 @@ ptd_status ptd_pipeline_destroy(ptd_pipeline* pipeline);
  * the tokens [token_offsets[b], token_offsets[b+1]) (none is allowed); its i-th token sits at position
  * C_b + i, with C_b = ctx_lens[b] tokens in the cache before it, and, as a tree's nodes do, in cache slot
  * C_b + i.  A contiguous cache's layers have a row for each of these B sequences, no more and no fewer.  total_tokens is the number of rows that the buffers have: token_offsets[B] may be smaller
- * (a batch padded to a captured size), and what lies behind the last sequence is padding. */
+ * (a batch padded to a captured size), and what lies behind the last sequence is padding.  Where the offsets
+ * decrease somewhere, PTD_ERR_INVALID_BATCH is set and the results of the whole batch are unspecified: its
+ * sequences may overlap (nothing but the results is written). */
 #define PTD_MAX_PROMPT_BATCH 8192
 #define PTD_MAX_PROMPT_TOKENS (1 << 30) /* of total_tokens, and of max_ctx + max_tokens */
 typedef struct {

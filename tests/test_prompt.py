@@ -710,3 +710,58 @@ def test_a_cache_of_several_devices_is_refused():
             ptd.KVCache(on(k), on(v), 2, 128, 16, on(table))
     with pytest.raises(ValueError, match="devices"):
         ptd.KVCache(on(0), on(1), 2, 128)
+
+
+def test_partials_have_places_of_their_own(tmp_path):
+    """block_place + block: distinct over a batch's blocks and below prompt_places, with padding before, behind and in
+    the sequences' sizes; below it even where offsets decrease (sequences that are valid by themselves then overlap)."""
+    src, exe = tmp_path / "places.cpp", tmp_path / "places"
+    src.write_text(r"""
+#include <cstdio>
+#include <set>
+#include "prompt_geometry.cuh"
+int main() {
+  int width, total, batch, ordered, most = 0;
+  while (std::scanf("%d %d %d %d", &width, &total, &batch, &ordered) == 4) {
+    static int off[5000];
+    for (int b = 0; b <= batch; ++b)
+      if (std::scanf("%d", off + b) != 1) return 1;
+    const ptd::IndexDivisor by = ptd::index_divisor(width);
+    const ptd::PromptBounds bounds = {total, total, 0, total};
+    const long places = ptd::prompt_places(total, batch, width);
+    std::set<long> taken;
+    for (int b = 0; b < batch; ++b) {
+      if (!ptd::prompt_sequence_ok(bounds, off[b], off[b + 1], 0)) {
+        if (ordered) return 2;
+        continue;
+      }
+      const int count = ptd::prompt_blocks(0, off[b + 1] - off[b], width, by).count;
+      for (int i = 0; i < count; ++i) {
+        const long place = ptd::block_place(off[b], b, by) + i;
+        if (place < 0 || place >= places) return 3;
+        if (!taken.insert(place).second && ordered) return 4;
+        if (place == places - 1) ++most;
+      }
+    }
+  }
+  std::printf("%d\n", most);
+  return 0;
+}
+""")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I", os.path.join(ROOT, "paper_2607_10661_gb300", "csrc"), str(src),
+                    "-o", str(exe)], check=True)
+    rng = random.Random(14)
+    lines = ["2 128 128 1 " + " ".join(map(str, range(129))), "64 1 1 1 0 1", "64 128 2 1 0 64 128", "7 5 3 1 5 5 5 5"]
+    for _ in range(800):
+        width, batch = rng.choice([1, 2, 3, 10, 16, 25, 36, 64, 256]), rng.randrange(1, 200)
+        off = [rng.choice([0, rng.randrange(50)])]
+        for _ in range(batch):
+            off.append(off[-1] + rng.choice([0, 1, 1, rng.randrange(1, 3 * width + 2)]))
+        total = max(off[-1] + rng.choice([0, 0, rng.randrange(300)]), 1)
+        ordered = rng.random() < 0.7
+        if not ordered:
+            for _ in range(rng.randrange(1, 20)):
+                off[rng.randrange(batch + 1)] = rng.randrange(-3, total + 4)
+        lines.append(f"{width} {total} {batch} {int(ordered)} " + " ".join(map(str, off)))
+    r = subprocess.run([str(exe)], input="\n".join(lines), capture_output=True, text=True)
+    assert r.returncode == 0 and int(r.stdout) > 20, (r.returncode, r.stdout)   # (the last place is taken too)
