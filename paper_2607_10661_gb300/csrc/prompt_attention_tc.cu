@@ -82,10 +82,14 @@ constexpr uint32_t kOffClaim = (kOffAbort + 4 + 15) / 16 * 16;   // the schedule
 
 // A bounded wait of a warp for the barrier's phase: false when it, or another role, has given up.  A try_wait that
 // finds the phase open sleeps until it ends, for 1.95 us at most (measured), so that 2^20 tries are 2 s.  (The roles'
-// code is larger than the near instruction caches: a short loop in place of mbar_wait_warp's clock.)
+// code is larger than the near instruction caches: a short loop in place of mbar_wait_warp's clock.)  A wait that lasts
+// while other roles work on a whole unit (kUnitTries: 128 s) is as long as the unit's keys make it, ~1 us a key tile, and ends
+// at once where one of them has given up.
+constexpr int kTries = 1 << 20, kUnitTries = 1 << 26;
+template <int kMost = kTries>
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* dev_status) {
 #pragma unroll 1
-  for (int tries = 0; tries < (1 << 20); ++tries) {
+  for (int tries = 0; tries < kMost; ++tries) {
     if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
     if (__any_sync(0xffffffffu, *abort_flag != 0)) return false;
   }
@@ -336,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   // The unit of a role's turn `it` (two slots), as long as there is one.
   auto wait_seg = [&](int it) -> const volatile Seg* {
-    if (!wait_warp(bar(kSegFull + (it & 1)), (uint32_t)(it >> 1) & 1u, abort_flag, p.dev_status)) return nullptr;
+    if (!wait_warp<kUnitTries>(bar(kSegFull + (it & 1)), (uint32_t)(it >> 1) & 1u, abort_flag, p.dev_status)) return nullptr;
     const volatile Seg* s = segs + (it & 1);
     return s->valid ? s : nullptr;
   };
@@ -613,7 +617,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int j = max(0, edge - kt0); j < n; ++j) {
           int vs = tiles + 2 * j + 1;   // (the tiles go K_0, V_0, K_1, V_1, ..)
           vs -= vs / kTiles * kTiles;
-          if (!(ok = wait_warp(bar(kLoadV + vs), (checked >> vs) & 1u, abort_flag, p.dev_status))) break;
+          if (!(ok = wait_warp<kUnitTries>(bar(kLoadV + vs), (checked >> vs) & 1u, abort_flag, p.dev_status))) break;
           checked ^= 1u << vs;
           // 16-byte chunks: rows of the first half (64 columns), then of the second.  Rows that all of the block's
           // tokens see stay as they are, rows behind the block's last token become 0.

@@ -939,3 +939,28 @@ def test_rotated_queries_beside_their_inputs_and_overlaps():
     ptd.prompt_attention(far, cache, 0, query, one, status, workspace=room[hq * d:])
     torch.cuda.synchronize()
     assert int(status) == 0
+
+
+def test_a_unit_of_some_seconds():
+    """One token behind 2^29 positions without scratch: a single CTA reads them all (two pages, one after the other over and
+    over), some seconds long, while its roles without work wait.  The scores of the first page are 128, all others 0,
+    so that the others' weights are 0 in fp32 (e^-128) and the output is the mean of the first page's 128 values."""
+    ctx, page = 2 ** 29, 128
+    table = torch.full((1, ctx // page + 1), 1, **I32)
+    table[0, 0] = 0
+    g = torch.Generator(device=DEV).manual_seed(63)
+    k, v = torch.zeros((1, 2, page, 1, 128), dtype=BF16, device=DEV), torch.randn((1, 2, page, 1, 128), generator=g, device=DEV).to(BF16)
+    k[0, 0] = 1.0
+    q, out, status = torch.ones((1, 1, 128), dtype=BF16, device=DEV), torch.zeros((1, 1, 128), dtype=BF16, device=DEV), torch.zeros(1, **I32)
+    prompt = ptd.Prompt(torch.tensor([0, 1], **I32), torch.tensor([ctx], **I32), 1, 1, ctx)
+    a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    a.record()
+    assert ptd.prompt_attention(prompt, ptd.KVCache(k, v, 1, 128, page, table), 0, q, out, status, scale=1.0) == 1
+    b.record()
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    want = v[0, 0, :, 0].double().mean(0)
+    # 128 products summed in fp32 by truncation, and the output's rounding
+    tol = 128 * 2.0 ** -23 * v[0, 0, :, 0].double().abs().mean(0) + 2.0 ** -8 * want.abs() + 1e-30
+    assert ((out[0, 0].double() - want).abs() <= tol).all()
+    assert a.elapsed_time(b) > 2000.0   # longer than the waits between steps last
