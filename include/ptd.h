@@ -499,10 +499,11 @@ ptd_status ptd_pipeline_destroy(ptd_pipeline* pipeline);
  * A packed batch of new tokens: whole prompts, chunks of prompts, or single tokens.  Sequence b owns
  * the tokens [token_offsets[b], token_offsets[b+1]) (none is allowed); its i-th token sits at position
  * C_b + i, with C_b = ctx_lens[b] tokens in the cache before it, and, as a tree's nodes do, in cache slot
- * C_b + i.  A contiguous cache's layers have a row for each of these B sequences, no more and no fewer.  total_tokens is the number of rows that the buffers have: token_offsets[B] may be smaller
- * (a batch padded to a captured size), and what lies behind the last sequence is padding.  Where the offsets
- * decrease somewhere, PTD_ERR_INVALID_BATCH is set and the results of the whole batch are unspecified: its
- * sequences may overlap (nothing but the results is written). */
+ * C_b + i.  A contiguous cache's layers have a row for each of these B sequences, no more and no fewer.
+ * total_tokens is the number of rows that the buffers have: token_offsets[B] may be smaller (a batch padded to a
+ * captured size), and what lies behind the last sequence is padding.  Where the offsets decrease somewhere,
+ * PTD_ERR_INVALID_BATCH is set and the results of the whole batch are unspecified: its sequences may overlap
+ * (nothing but the results is written). */
 #define PTD_MAX_PROMPT_BATCH 8192
 #define PTD_MAX_PROMPT_TOKENS (1 << 30) /* of total_tokens, and of max_ctx + max_tokens */
 typedef struct {
@@ -571,7 +572,8 @@ ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* 
  *   q [total_tokens][num_q_heads][D], tokens q_stride elements apart; out [total_tokens][num_q_heads][D] back to
  *     back; both of cache->dtype and 16-byte aligned, q_stride times the element size a multiple of 16; out
  *     and the workspace overlap no input and not one another (PTD_ERR_INVALID_ARG).
- *     fp32 accumulation and softmax statistics; the weights are rounded to bf16 for a bf16 cache.
+ *     fp32 accumulation and softmax statistics; the weights are rounded to bf16 for a bf16 cache (with the output's
+ *     own rounding an error of 2.0e-3 to 2.3e-3 of the outputs' size, for 1.6e-3 with weights of 32 bits).
  *   Rows behind the last sequence are left as they were, as are those of a sequence out of range (see
  *     ptd_prompt_slots; PTD_ERR_INVALID_BATCH).  A page number outside the cache sets PTD_ERR_INVALID_BATCH too:
  *     the sequence's outputs are then unspecified.
@@ -580,6 +582,8 @@ ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* 
  *   workspace: scratch of ptd_prompt_attention_workspace_size bytes (of the current device), 16-byte aligned, for
  *     batches of few rows, whose keys are split between CTAs (partials merged by a second kernel); with less
  *     (even none) the call runs unsplit.  Calls that may overlap on the GPU need scratch of their own.
+ *     Sizes and cuts follow the host's bounds: a single sequence of one block of tokens (some 64), and fp32 batches, are
+ *     cut for max_ctx, so that bounds far above the lengths cost speed there.
  * One launch, or two where keys may be split. */
 size_t ptd_prompt_attention_workspace_size(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t num_q_heads);
 ptd_status ptd_prompt_attention(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t layer, const void* q,

@@ -94,8 +94,9 @@ __device__ __forceinline__ void merge_part(const PromptAttnParams& p, const Piec
   }
 }
 
-// The rows of one split block (by pieces of one length, or by the lengths on the device), from its pieces: O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s, M the
-// maximum of the m_s (a row that saw no key of a piece has l_s = 0, and its O_s was not written).  x of the grid is
+// The rows of one split block (by pieces of one length, or by the lengths on the device), from its pieces:
+// O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s, M the maximum of the m_s (a row that saw no key of a piece has l_s = 0,
+// and its O_s was not written).  x of the grid is
 // a block's place and head tile, or a boundary between shares of the cells, y a share of its rows and columns;
 // consecutive threads take consecutive rows, as the partials lie.  Bound by the latency of the chain sequence, (m, l),
 // partials; the sequence is found before the wait for the attention.
@@ -172,9 +173,6 @@ int choose_piece(int64_t units, int64_t key_tiles, int batch, int64_t slots) {
   return (int)((key_tiles + pieces - 1) / pieces);
 }
 
-}  // namespace pa
-
-namespace pa {
 // Tiles, blocks and the cut, for blocks of `tiles` M tiles of tile_rows rows, on `slots` places.
 void plan_tiles(PromptAttnParams& p, int tile_rows, int tiles, int key_tile_log2, int64_t slots) {
   const int group = p.hq / p.hkv;
@@ -204,18 +202,25 @@ void plan_tiles(PromptAttnParams& p, int tile_rows, int tiles, int key_tile_log2
 size_t plan_prompt_attention(PromptAttnParams& p, bool bf16, size_t scratch, int sms) {
   p.cut_ctas = 0;
   if (bf16) {
-    // A CTA an SM.  One sequence of one block: pieces of one length, by the bounds (us by their key tiles, the rule's in
-    // brackets): one token after 4096 of 32/8 heads, 8 units of 33 tiles, 1: 17.5, [2: 12.7], 4: 12.8, 8: 15.7, uncut 42; after
-    // 32768, 10: 42.6, [14: 34.6], 17: 33.0, 20: 34.3; 60 tokens after 500, [1: 13.2], uncut 14.0.
+    // A CTA an SM.  All figures here are us of a call in graph replays, 32/8 heads unless said, pages of 16.
+    // One sequence of one block: pieces of one length, by the bounds (its length is not looked at: one token after
+    // 4096 takes 11.8 with that bound and 50.6, uncut, with one of 131072).  By how many pieces, the rule's in brackets:
+    //   one token after 4096 (8 units of 33 key tiles)   1: 49.7, 4: 19.5, 8: 14.1, [17: 11.8]
+    //   one token after 32768                            10: 45.2, 14: 35.9, 17: 33.1, [19: 31.9], 20 (over a wave): 45.7
+    //   60 tokens after 500                              1: 13.7, 2: 14.9, 3: 13.9, [5: 12.9]
     pa::plan_tiles(p, 128, 2, 7, sms);
-    // Else by the lengths on the device, or uncut (us of 32/8 heads; pieces of one length, which bounds alone give, or uncut in
-    // brackets): one token behind 8 ragged contexts up to 4096 22.2 [24.6], 8 equal ones 31.9 [42.0], 12 ragged 28.7 [50.5], 16
-    // ragged up to 8000 53.2 [93.2], 24 of 8000 126 [183], 32 of 4000 89.8 [99.6]; 8 tokens after 8000 beside a prompt of 512
-    // 61.5 [93.5], 4 after 16000 beside 512 76 [179], 2 chunks of 256 after 8192 67 [107], 61 tokens of 64/8 heads after 32707
-    // 51.5 [55.3].  Costs in key tiles, from these and from the cases on either side of the bound: 200 tokens after 1000
-    // uncut 21.6 [cut 23.6], after 1900 cut 25.8 [uncut 31.8], 2 of 200 after 500 uncut 16.5 [cut 18.4], 400 after 700 20.5
-    // [29.4], 800 after 1500 33.7 [43.7].  What it loses: the merge's launch where the units stay whole (18 contexts of
-    // 2000 32.0 [30.5], 800 tokens after 1500 36.0 [33.7]), uneven pieces of few equal ones (2 contexts of 2000 14.0 [11.7]).
+    // Else by the lengths on the device, if the host's bounds allow for a gain, or uncut.  A cell is the time of a key tile
+    // (~1.2 us); what a cut unit's partials and merge and any unit's start and end cost in cells (p.costs), and the
+    // bound on the key tiles, are fitted to these cases.
+    //   cut by the rule [uncut]: one token behind 8 ragged contexts up to 4096 23.5 [50.8], 8 equal ones 31.2 [52.0], 12 ragged
+    //     31.7 [52.1], 16 ragged up to 8000 60.6 [93.7], 24 of 8000 128 [185], 32 of 4000 90.1 [99.4], 2 of 2000 12.6 [27.7]; 8
+    //     tokens after 8000 beside a prompt of 512 28.6 [91.4], 4 after 16000 beside it 32.4 [177], 2 chunks of 256 after
+    //     8192 67.4 [107], 61 tokens of 64/8 heads after 32707 58.8 [390], 200 tokens after 1900 25.2 [31.8].
+    //   uncut by the rule [cut]: 200 tokens after 1000 21.4 [23.2], 2 of 200 after 500 16.2 [18.1], 400 after 700 20.3 [21.9],
+    //     800 after 700 24.5 [26.7].
+    //   what it loses: 400 tokens after 1500 32.9 [29.3], 800 after 1500 35.8 [33.5], and the merge's launch where the
+    //     device leaves the units whole: 18 contexts of 2000 31.4 [30.0].
+    // More than two rounds of units are never cut: 40 contexts of 4000 (320 units) 147.
     const int64_t units = (int64_t)p.blocks * p.tile_heads;
     const int64_t key_tiles = ((int64_t)p.bounds.max_ctx + p.bounds.max_tokens + p.key_tile - 1) >> p.key_tile_log2;
     if (p.batch > 1 || p.bounds.max_tokens > p.block_tokens) {

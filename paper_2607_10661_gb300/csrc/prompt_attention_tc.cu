@@ -22,12 +22,12 @@
 //           exceeded by 2^8, exp2, bf16 weights over S in TMEM (told in two halves), fp32 row sum; O / l at the end.
 // TMEM: S_0 | S_1 | O_0 | O_1, 128 fp32 columns each; P_t lies over the first 64 columns of S_t.
 //
-// Bound by the tensor pipe and the power cap for long prompts: 8192 tokens of 32/8 heads 295 us (1.86 PFLOP/s of the
-// seen pairs, pipe 85 % active, 0.97 of cuBLAS' burst), 16384 of 64/8 heads 2.35 - 2.45 ms (1.8 - 1.87), 2.54 ms in
-// runs of seconds at the cap.  Ragged prompts of some hundred tokens (30 us for 18.5 GFLOP) are bound by changes of unit, ~4.5 us
+// Bound by the tensor pipe and the power cap for long prompts: 8192 tokens of 32/8 heads 337 us among other passes (1.63
+// PFLOP/s of the seen pairs, 0.95 of cuBLAS' sustained rate), 300 after a pause (1.83); 16384 of 64/8 heads 2.60 ms (1.69
+// PFLOP/s) and 2.29.  Ragged prompts of some hundred tokens (31 us for 18.5 GFLOP) are bound by changes of unit, ~4.5 us
 // each: the V check, masked tiles, outputs, and code that has left the instruction caches (so it is kept short).
-// Decoding: by HBM, ~6 us from the start to the first output, and the merge: 8 contexts of up to 4096 22 us for 73 MB,
-// 24 of 8000 126 us for 787 MB (6.2 TB/s).
+// Decoding: by HBM, ~6 us from the start to the first output, and the merge: 8 contexts of up to 4096 22.4 us for 73 MB,
+// 24 of 8000 128 us for 787 MB (6.1 TB/s).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -156,9 +156,11 @@ static __device__ __noinline__ void rescale_o(uint32_t tO, float alpha) {
 
 // Softmax of one key tile of this thread's row: S (TMEM at tS) becomes the bf16 P over its first 64 columns,
 // against the reference maximum m_run (log2 units), which only moves up, and only when exceeded by more than
-// 2^8; then the row sum and O (TMEM at tO, if `has_o`) are rescaled.  With need_mask (warp-uniform) the row sees
-// the tile's keys 0 .. last.  The whole row is in registers: one maximum and one vote a tile, and then exponentials
-// and packing without a dependence between chunks.  Warp-collective.
+// 2^8; then the row sum and O (TMEM at tO, if `has_o`) are rescaled.  The weights are rounded to bf16, as the tensor cores
+// take them beside V (the row sum adds them before that): the error against 64 bits is 1.2 to 1.4 times that of 32-bit
+// weights, whose outputs are rounded to bf16 too (2.0e-3 of the outputs' size for 1.5e-3, decoding 2.3e-3 for 1.6e-3).
+// With need_mask (warp-uniform) the row sees the tile's keys 0 .. last.  The whole row is in registers: one maximum and
+// one vote a tile, and then exponentials and packing without a dependence between chunks.  Warp-collective.
 __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool has_o, bool need_mask, int last, float sl2,
                                              float& m_run, float& l_run, uint32_t half_bar) {
   uint32_t r[4][32];

@@ -75,7 +75,8 @@ struct CutCosts {      // in cells
 };
 
 // The cut for `ctas` CTAs at a time into at most `most` shares: `cells` of `units` units (at most two rounds of them), the
-// longest and the shortest of `longest` and `shortest` cells.  Whole units take the longest, or two of the mean or what is even and a short one.
+// longest and the shortest of `longest` and `shortest` cells.  Whole units take the longest, or two of the mean or what is
+// even and a short one.
 PTD_HD PromptCut prompt_cut(int cells_, int units_, int longest_, int shortest_, int ctas_, int most, CutCosts costs) {
   const uint32_t cells = (uint32_t)cells_, units = (uint32_t)units_, ctas = (uint32_t)ctas_;
   if (cells < 2u || most < 1 || cells > (uint32_t)kMostCutCells) return {0, cells_};   // (more: sequences that overlap)

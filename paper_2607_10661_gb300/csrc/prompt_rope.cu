@@ -7,8 +7,8 @@
 // time, and asks for them before it forms its tokens' (cos, sin) tables.
 //
 // What bounds it: the reads and writes, (2 Hq + 4 Hkv) D elements a token: 8192 tokens of 32/8 heads (bf16, D = 128,
-// 201 MB) 34.0 us, 5.9 TB/s, 20000 tokens 75.9 us, 6.5 TB/s; for few tokens latency: 8 tokens 2.1 us.  (Streaming
-// loads, __ldcs: 34.5 and 77.0.)
+// 201 MB) 31.7 us in graph replays, 6.3 TB/s, and 34.0 among other passes, 20000 tokens 72.0 us, 6.8 TB/s; for few tokens
+// latency: 8 tokens 2.1 us.  (Streaming loads, __ldcs, were 1.5 % slower.)
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -174,8 +174,8 @@ cudaError_t launch_prompt_rope(const PromptRopeParams& p, bool bf16, const RopeF
     const int chunks = half / vec, per_token = (p.hq + 2 * p.hkv) * chunks;
     // While all CTAs have a place at once a token is done soonest by many threads, then small CTAs turn over best.
     // Measured (us, 384 threads of one item each and 128 of three, bf16 with D = 128; SMs 152): 8 tokens of 32/8 heads
-    // 2.1 and 2.5, 300 3.0 and 4.0, 600 3.3 and 4.6, [the rule's bound] 610 4.2 and 4.8, 1000 5.4 and 5.1, 8192 39.5 and
-    // 34.0; of 64/8 heads 500 4.7 and 6.9, 8000 58.2 and 49.8; fp32 4000 32.6 and 31.0.
+    // 2.1 and 2.6, 300 2.9 and 4.0, 600 3.2 and 4.1, [the rule's bound] 620 4.2 and 4.5, 1000 5.0 and 4.6, 8192 37.3 and
+    // 31.5; of 64/8 heads 500 4.6 and 6.6, 8000 57.1 and 49.1; fp32 4000 31.8 and 30.3.
     if (p.n_tokens <= 4 * (int64_t)sms)
       return bf16 ? pr::launch<__nv_bfloat16, 384, 1, 4>(p, freqs, chunks, per_token, sms, stream)
                   : pr::launch<float, 384, 1, 4>(p, freqs, chunks, per_token, sms, stream);
