@@ -400,6 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (mine == 1) commit(kQEmpty + t);
         }
         step_done(mine > 0);
+        if (awaits_entry(t, both) && !(ok = wait(kEntry, entries++))) break;
         for (int j = 0; j < n; ++j) {
           if (j < mine && own_turn(t, j, both)) arrive(kPHalf + t);
           if (!(ok = take(v_tile))) break;
@@ -412,7 +413,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc_fence_after();
             issue_pv<4, 8>(s_tmem, dv + v_tile, j > 0);
             if (j + 1 < mine) issue_s(s_tmem, dq, dk + k_tile);
-            if (awaits_entry(t, j, both) && !(ok = wait(kEntry, entries++))) break;
             if (passes_turn(t, j, both)) arrive(kPHalf + (t ^ 1));
             if (j + 1 < mine) {
               commit(kSFull + t);

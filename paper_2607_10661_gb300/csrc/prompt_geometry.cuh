@@ -101,11 +101,11 @@ PTD_HD int share_of(int x, const PromptCut& cut) {   // the share that has cell 
 // the issuer's own.  Within a unit every turn passed to the other is asked for by a turn got from it, so that it cannot
 // come early.  The first one of a unit is not: M tile 1 may still wait for its softmax in the unit before, whose barrier would
 // count the turn in place of a softmax warp.  So issuer 1 tells that it has begun a unit with turns, and issuer 0 waits
-// for that before it passes the first.
+// for that before its first product with V (it waits for M tile 0's softmax then anyway).
 PTD_HD bool own_turn(int t, int j, int both) { return t == 0 ? j == 0 || j >= both : j >= both; }
 PTD_HD bool passes_turn(int t, int j, int both) { return t == 0 ? j < both : j + 1 < both; }
 PTD_HD bool tells_entry(int t, int both) { return t == 1 && both > 0; }
-PTD_HD bool awaits_entry(int t, int j, int both) { return t == 0 && j == 0 && both > 0; }
+PTD_HD bool awaits_entry(int t, int both) { return t == 0 && both > 0; }
 
 // Where the last search ended: a search for a later block goes on from there.
 struct PromptCursor {

@@ -213,14 +213,14 @@ int main() {
         std::vector<Op>& o = ops[t];
         if (ptd::tells_entry(t, both)) o.push_back({false, kEntry, entries});
         if (n[t] > 0) o.push_back({false, kS + t, first[t]});
+#ifndef PTD_NO_ENTRY
+        if (ptd::awaits_entry(t, both)) o.push_back({true, kEntry, entries});
+#endif
         for (int j = 0; j < all; ++j) {
           if (j >= n[t]) continue;
           if (ptd::own_turn(t, j, both)) o.push_back({false, kP + t, first[t] + j});
           o.push_back({true, kP + t, first[t] + j});
           o.push_back({true, kF + t, first[t] + j});
-#ifndef PTD_NO_ENTRY
-          if (ptd::awaits_entry(t, j, both)) o.push_back({true, kEntry, entries});
-#endif
           if (ptd::passes_turn(t, j, both)) o.push_back({false, kP + (t ^ 1), first[t ^ 1] + j + t});
           if (j + 1 < n[t]) o.push_back({false, kS + t, first[t] + j + 1}); else o.push_back({false, kO + t, outs[t]});
         }
