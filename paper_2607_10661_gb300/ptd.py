@@ -304,10 +304,19 @@ class KVCache:
             num_pages, seq_capacity = k.shape[1], 0
             max_pages = block_table.shape[1]
             bt = _dev(block_table, "block_table", torch.int32)
+            self.sequences = block_table.shape[0]
         else:
             num_pages, seq_capacity, max_pages, bt = 0, k.shape[2], 0, None
+            self.sequences = k.shape[1]
         self.c = _Cache(_dev(k, "k"), _dev(v, "v"), _ptd_dtype(k.dtype), self.num_layers, self.num_kv_heads,
                         self.head_dim, self.page_size, seq_capacity, num_pages, bt, max_pages)
+
+
+def _trees_of_cache(tree: Tree, cache: KVCache, last_layer: int) -> None:
+    """More trees than the cache has sequences would run past it; with fewer, the layers behind a contiguous cache's first
+    would begin elsewhere (a layer's size is the batch's)."""
+    if tree.batch > cache.sequences or (not cache.page_size and last_layer > 0):
+        raise ValueError(f"the cache has rows for {cache.sequences} sequences, the batch has {tree.batch} trees")
 
 
 def attention_workspace_size(tree: Tree, cache: KVCache, num_q_heads: int, num_layers: Optional[int] = None) -> int:
@@ -325,6 +334,8 @@ def tree_attention(tree: Tree, cache: KVCache, q: torch.Tensor, out: torch.Tenso
                    scale: float = 0.0, workspace: Optional[torch.Tensor] = None, stream=None) -> int:
     """ptd_tree_attention; returns the number of kernels launched."""
     n = cache.num_layers if num_layers is None else num_layers
+    if tree.batch != cache.sequences:
+        _trees_of_cache(tree, cache, layer_begin + n - 1)
     r = (_calls or _native()).tree_attention(tree, cache, layer_begin, n, q, num_q_heads, scale, out, workspace, dev_status,
                                           stream if stream is None else _stream(stream))
     if r is not None:
@@ -356,6 +367,8 @@ def tree_attention_as(kernel: int, cluster_size: int, tree: Tree, cache: KVCache
                       workspace: Optional[torch.Tensor] = None, stream=None) -> int:
     """ptd_tree_attention_as: tree_attention by a named kernel (ATTN_*)."""
     n = cache.num_layers if num_layers is None else num_layers
+    if tree.batch != cache.sequences:
+        _trees_of_cache(tree, cache, layer_begin + n - 1)
     st = lib().ptd_tree_attention_as(ctypes.byref(tree.c), ctypes.byref(cache.c), layer_begin, n,
                                      _dev(q, "q", cache.k.dtype), num_q_heads, float(scale),
                                      _dev(out, "out", cache.k.dtype),
@@ -400,6 +413,8 @@ def verify_greedy(tree: Tree, tokens: torch.Tensor, target: torch.Tensor, target
 
 def kv_compact(tree: Tree, cache: KVCache, accepted: torch.Tensor, accept_len: torch.Tensor,
                new_ctx: torch.Tensor, stream=None) -> int:
+    if tree.batch != cache.sequences:
+        _trees_of_cache(tree, cache, cache.num_layers - 1)
     r = (_calls or _native()).kv_compact(tree, cache, accepted, accept_len, new_ctx,
                                       stream if stream is None else _stream(stream))
     if r is not None:
@@ -436,6 +451,8 @@ def verify_sampling(tree: Tree, tokens: torch.Tensor, logits: torch.Tensor, temp
 def verify_and_compact(tree: Tree, cache: KVCache, tokens: torch.Tensor, target: torch.Tensor, target_stride: int,
                        accepted: torch.Tensor, accept_len: torch.Tensor, bonus: torch.Tensor, new_ctx: torch.Tensor,
                        dev_status: torch.Tensor, stream=None) -> int:
+    if tree.batch != cache.sequences:
+        _trees_of_cache(tree, cache, cache.num_layers - 1)
     r = (_calls or _native()).verify_and_compact(tree, cache, tokens, target, target_stride, accepted, accept_len, bonus,
                                               new_ctx, dev_status, stream if stream is None else _stream(stream))
     if r is not None:
@@ -474,6 +491,8 @@ class StepBuffers:
 
 def tree_verify_step(tree: Tree, cache: KVCache, bufs: StepBuffers, stream=None) -> int:
     """ptd_tree_verify_step: attention, top-k, verification and compaction on device buffers."""
+    if tree.batch != cache.sequences:
+        _trees_of_cache(tree, cache, cache.num_layers - 1)
     r = (_calls or _native()).tree_verify_step(tree, cache, bufs, stream if stream is None else _stream(stream))
     if r is not None:
         return _launched(r, "ptd_tree_verify_step")
@@ -493,6 +512,8 @@ class HostIO:
 
 def tree_verify_step_host(tree: Tree, cache: KVCache, bufs: StepBuffers, io: HostIO, stream=None) -> int:
     """ptd_tree_verify_step_host: host inputs -> device step -> host results (asynchronous)."""
+    if tree.batch != cache.sequences:
+        _trees_of_cache(tree, cache, cache.num_layers - 1)
     st = lib().ptd_tree_verify_step_host(ctypes.byref(tree.c), ctypes.byref(cache.c), ctypes.byref(bufs.c),
                                          ctypes.byref(io.c), _stream(stream))
     _check(st, "ptd_tree_verify_step_host")
@@ -583,6 +604,8 @@ def tree_rope_append(tree: Tree, cache: KVCache, layer_begin: int, q: torch.Tens
     into cache layers layer_begin .. layer_begin + L - 1 (a 3-D q, k, v is one layer)."""
     dt = cache.k.dtype
     n_layers = q.shape[0] if q.dim() == 4 else 1
+    if tree.batch != cache.sequences:
+        _trees_of_cache(tree, cache, layer_begin + n_layers - 1)
     r = (_calls or _native()).tree_rope_append(tree, cache, layer_begin, n_layers, q, num_q_heads, k, v, rope_base,
                                             positions_out, dev_status, stream if stream is None else _stream(stream))
     if r is not None:
@@ -774,6 +797,9 @@ class Pipeline:
     tensors of at least 2 * L * N_tot * Hkv * D elements."""
 
     def __init__(self, cache: KVCache, trees, bufs, staging, stream=None):
+        for tree in trees[:2]:
+            if tree.batch != cache.sequences:
+                _trees_of_cache(tree, cache, cache.num_layers - 1)
         self.keep = (cache, trees, bufs, staging)
         tr = (_Tree * 2)(trees[0].c, trees[1].c)
         ar = (_StepArgs * 2)(bufs[0].c, bufs[1].c)

@@ -765,3 +765,48 @@ int main() {
         lines.append(f"{width} {total} {batch} {int(ordered)} " + " ".join(map(str, off)))
     r = subprocess.run([str(exe)], input="\n".join(lines), capture_output=True, text=True)
     assert r.returncode == 0 and int(r.stdout) > 20, (r.returncode, r.stdout)   # (the last place is taken too)
+
+
+def test_tree_calls_refuse_batches_beyond_the_cache(lib, monkeypatch):
+    """More trees than the cache's sequences, or fewer beyond the first layer of a contiguous cache: refused before
+    anything is called; the others go on to the call."""
+    import types
+
+    from paper_2607_10661_gb300 import ptd
+
+    class Reached(Exception):
+        pass
+
+    class Calls:
+        def __getattr__(self, name):
+            def call(*a):
+                raise Reached
+
+            return call
+
+    monkeypatch.setattr(ptd, "_calls", Calls())
+    monkeypatch.setattr(ptd, "lib", Calls)
+    monkeypatch.setattr(ptd, "_dev", lambda *a, **k: 0)
+    x = types.SimpleNamespace(dim=lambda: 3, c=ptd._StepArgs(), t=None)
+    io = types.SimpleNamespace(c=ptd._HostIO())
+    for page, sequences, batch, layers, layer, good in ((0, 3, 3, 2, 1, True), (0, 3, 4, 1, 0, False), (0, 3, 2, 1, 0, True),
+                                                        (0, 3, 2, 2, 1, False), (16, 3, 2, 2, 1, True), (16, 3, 4, 2, 0, False)):
+        tree = types.SimpleNamespace(batch=batch, c=ptd._Tree())
+        k = types.SimpleNamespace(dtype=None)
+        cache = types.SimpleNamespace(sequences=sequences, page_size=page, num_layers=layers, k=k, c=ptd._Cache())
+        for call in (lambda: ptd.tree_attention(tree, cache, x, x, 8, x, layer_begin=layer, num_layers=1, stream=0),
+                     lambda: ptd.tree_attention_as(1, 0, tree, cache, x, x, 8, x, layer_begin=layer, num_layers=1, stream=0),
+                     lambda: ptd.tree_rope_append(tree, cache, layer, x, 8, x, x, 1e4, x, stream=0),
+                     lambda: ptd.kv_compact(tree, cache, x, x, x, stream=0),
+                     lambda: ptd.verify_and_compact(tree, cache, x, x, 1, x, x, x, x, x, stream=0),
+                     lambda: ptd.tree_verify_step(tree, cache, x, stream=0),
+                     lambda: ptd.tree_verify_step_host(tree, cache, x, io, stream=0),
+                     lambda: ptd.Pipeline(cache, [tree, tree], [x, x], [types.SimpleNamespace(numel=lambda: 1, element_size=lambda: 1)] * 2,
+                                          stream=0)):
+            with pytest.raises(Reached if good else ValueError):
+                call()
+    # a lone first layer takes fewer trees
+    tree = types.SimpleNamespace(batch=2, c=ptd._Tree())
+    cache = types.SimpleNamespace(sequences=3, page_size=0, num_layers=2, k=k, c=ptd._Cache())
+    with pytest.raises(Reached):
+        ptd.tree_attention(tree, cache, x, x, 8, x, layer_begin=0, num_layers=1, stream=0)
