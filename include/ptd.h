@@ -24,7 +24,10 @@
  * whole step: attention, top-k, verification and compaction on one stream).  The prompts that come
  * before the first tree (and plain decoding) have ptd_prompt_slots (pages, block tables, cache
  * slots and positions of new tokens), ptd_prompt_rope_append (rotary encoding, K/V into those
- * slots) and ptd_prompt_attention (causal attention of packed sequences over the cache)
+ * slots) and ptd_prompt_attention (causal attention of packed sequences over the cache); several
+ * continuations of a request ptd_page_fork (sequences that share pages), with ptd_token_logprobs and
+ * ptd_lm_head_logprobs (log probabilities of tokens, entropies, alternatives).  Models that
+ * normalise their heads have ptd_tree_norm_rope_append and ptd_prompt_norm_rope_append.
  *
  * Conventions shared by every call
  *   - Pointers are DEVICE pointers unless a comment says "host".  The caller owns
@@ -66,7 +69,7 @@ typedef enum {
   PTD_ERR_WORKSPACE = 6,     /* workspace pointer null or smaller than required          */
   PTD_ERR_POOL_FULL = 7,     /* (device) a candidate-pool merge was refused: no room     */
   PTD_ERR_INVALID_BATCH = 8, /* (device) a packed batch's offsets, lengths, pages or slots are out of range */
-  PTD_ERR_NO_PAGES = 9       /* (device) ptd_prompt_slots was refused: too few free pages */
+  PTD_ERR_NO_PAGES = 9       /* (device) ptd_prompt_slots or ptd_page_fork was refused: too few free pages */
 } ptd_status;
 
 typedef enum { PTD_F32 = 0, PTD_BF16 = 1 } ptd_dtype;
@@ -357,6 +360,18 @@ ptd_status ptd_tree_rope_append(const ptd_tree* tree, const ptd_kv_cache* cache,
                                 int32_t num_layers, void* q, int32_t num_q_heads, const void* k, const void* v,
                                 float rope_base, int32_t* positions_out, int32_t* dev_status, void* stream);
 
+/* As ptd_tree_rope_append, of a model that normalises its query and key heads: in layer l' of the call a query head
+ * x becomes x_j * q_weight[l'][j] / sqrt(mean_j(x_j^2) + eps) before its rotation, a key head so with k_weight (in fp32,
+ * rounded once, behind the rotation); values are written as they are.
+ *   q_weight, k_weight [num_layers][D] of cache->dtype; eps finite, >= 0 (with 0 a head of zeros gives NaN);
+ *   q_out [num_layers][N_tot][num_q_heads][D]: may be q itself.  Else what is written (q_out, positions_out,
+ *   dev_status, the cache) overlaps nothing else that the call reads or writes (PTD_ERR_INVALID_ARG).
+ * (num_q_heads + 2 num_kv_heads) * D below 2^31.  One launch. */
+ptd_status ptd_tree_norm_rope_append(const ptd_tree* tree, const ptd_kv_cache* cache, int32_t layer_begin,
+                                     int32_t num_layers, const void* q, int32_t num_q_heads, const void* k, const void* v,
+                                     const void* q_weight, const void* k_weight, float eps, float rope_base, void* q_out,
+                                     int32_t* positions_out, int32_t* dev_status, void* stream);
+
 /* LM head with a fused top-k: for every node row r of hidden, the logits h_r W^T (the
  * model's next-token scores P(y_T | ...) of Alg. 1 step 2) and their k largest entries,
  * as ptd_topk_draft would give them (descending, the lower token first on equal values,
@@ -376,6 +391,33 @@ ptd_status ptd_lm_head_topk(const void* hidden, int32_t rows, int64_t hidden_str
                             int32_t vocab, int64_t weight_stride, int32_t d_model, int32_t k, int32_t* out_idx,
                             float* out_val, void* workspace, size_t workspace_bytes, int32_t* dev_status,
                             void* stream);
+
+/* Log probabilities of given tokens.  For row r, with z = logits[r] / temperature and p = softmax(z):
+ *   out_logprob [rows] fp32: log p of tokens[r] (-inf for a token outside the vocabulary, which has probability 0);
+ *   out_entropy [rows] fp32 (may be NULL): -sum p log p;
+ *   out_idx [rows][k] int32, out_val [rows][k] fp32: the k most probable tokens, in ptd_topk_draft's order (the lower one
+ *     first on equal logits), and their log p; k in 0 .. PTD_MAX_TOPK (with 0 both may be NULL), at most vocab.
+ * logits [rows][row_stride] bf16 or fp32, aligned to their elements; sums and exponentials in fp32: a log probability is
+ * within 2^-20 (1 + entropy + max z - z) of the exact one.  A logit of -inf (a masked token) has probability 0; a row of
+ * nothing else has log probabilities -inf and entropy 0.  A row with NaN or +inf has NaN for all but tokens
+ * outside the vocabulary.  The outputs overlap no input and not one another
+ * (PTD_ERR_INVALID_ARG).  temperature finite, > 0.  rows and vocab at most PTD_MAX_PROMPT_TOKENS.  One launch. */
+ptd_status ptd_token_logprobs(const void* logits, ptd_dtype dtype, int64_t rows, int32_t vocab, int64_t row_stride,
+                              const int32_t* tokens, float temperature, int32_t k, float* out_logprob, float* out_entropy,
+                              int32_t* out_idx, float* out_val, int32_t* dev_status, void* stream);
+
+/* As ptd_token_logprobs of the logits h_r W^T, which never reach memory: hidden and weight as ptd_lm_head_topk takes them,
+ * but any number of rows up to PTD_MAX_LOGPROB_ROWS (a prompt's tokens, a decoding batch).  Logits are accumulated in fp32 by
+ * the tensor cores in an order of their own (see ptd_lm_head_topk); in a row with NaN the indices are unspecified.
+ * workspace: ptd_lm_head_logprobs_workspace_size(rows, vocab, k) bytes (of the current device), 16-byte aligned, for the
+ * parts of each row; it and the outputs overlap no input and not one another.  Two launches: the product, and the
+ * merge of a row's parts. */
+#define PTD_MAX_LOGPROB_ROWS (1 << 22)
+size_t ptd_lm_head_logprobs_workspace_size(int32_t rows, int32_t vocab, int32_t k);
+ptd_status ptd_lm_head_logprobs(const void* hidden, int32_t rows, int64_t hidden_stride, const void* weight, int32_t vocab,
+                                int64_t weight_stride, int32_t d_model, const int32_t* tokens, float temperature, int32_t k,
+                                float* out_logprob, float* out_entropy, int32_t* out_idx, float* out_val, void* workspace,
+                                size_t workspace_bytes, int32_t* dev_status, void* stream);
 
 /* One whole tree-verify step on device buffers: attention over all cache layers,
  * top-k of the logits, greedy verification on top-k column 0, KV compaction.
@@ -548,6 +590,41 @@ typedef struct {
 ptd_status ptd_prompt_slots(const ptd_prompt* prompt, const ptd_kv_cache* cache, const ptd_page_pool* pages,
                             int32_t* slots, int32_t* positions, int32_t* dev_status, void* stream);
 
+/* What the sequences of a batch hold of a paged cache, and its free pages: the state that ptd_prompt_slots moves on
+ * (there as block_table, held, free_pages, free_count), in buffers of one caller-owned set. */
+typedef struct {
+  int32_t batch;                /* host: sequences, 1 .. PTD_MAX_PROMPT_BATCH           */
+  int32_t* block_table;         /* [batch][max_pages], max_pages the cache's            */
+  int32_t* held;                /* [batch], leading entries of the row in use           */
+  int32_t* free_pages;          /* [num_pages], a stack: entries [0, free_count[0])     */
+  int32_t* free_count;          /* [1]                                                  */
+} ptd_page_set;
+
+/* Forks of paged sequences (best of n, beams): target sequence b, of `to`, goes on from the first lens[b] positions of
+ * source sequence parents[b], of `from`; parents[b] = -1 (lens[b] unread) leaves it empty, and a source that is nobody's
+ * parent ends.  The batches may differ in size.  With P positions a page:
+ *   the row of b in to->block_table begins with the parent's first floor(lens[b] / P) pages, shared from now on with all who
+ *     have them, and, where positions are left, a page of b's own behind them: of the targets whose last, partial page is the
+ *     same page x, the lowest keeps x unless some target shares x as a full one; each other one takes a free page, into which
+ *     x's rows of its positions are copied (K and V, every layer).  to->held[b] = ceil(lens[b] / P); entries behind it
+ *     stay as they were.
+ *   to->free_pages and to->free_count: the stack of `from` without the pages taken (from its top, by target), then, on top,
+ *     the pages that source rows hold and no target does (by the lowest row that holds each, and index).
+ * New positions go behind lens[b], so into pages that are a sequence's own.  ptd_prompt_slots gives pages back without asking
+ * who else holds them: sequences that share pages end, or are cut below a shared page, by this call, and all that share a page
+ * are in the call (a prefix kept for later is a sequence of the batch).
+ * `from` is not written: a call on the same state writes the same.  What is written (the buffers of `to`, the cache, the
+ * workspace, dev_status) overlaps nothing else (PTD_ERR_INVALID_ARG).  Sizes, parents or page numbers out of range
+ * (lens[b] beyond the pages held among them) set PTD_ERR_INVALID_BATCH, too few free pages PTD_ERR_NO_PAGES: then
+ * to->held and to->free_count are zeros and nothing else of `to` or the cache is written.  Pages that are both held and free
+ * give unspecified results.
+ *   cache: its k, v and sizes; its block_table is not read.  A layer has fewer than 2^31 rows.
+ *   workspace: ptd_page_fork_workspace_size bytes, 16-byte aligned, in any state.
+ * Two launches: the plan, and the copies. */
+size_t ptd_page_fork_workspace_size(const ptd_kv_cache* cache, const ptd_page_set* from, const ptd_page_set* to);
+ptd_status ptd_page_fork(const ptd_kv_cache* cache, const ptd_page_set* from, const ptd_page_set* to, const int32_t* parents,
+                         const int32_t* lens, void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream);
+
 /* Rotary encoding of a batch's new tokens and their K/V into the cache, in one layer.  Token n, at position
  * positions[n]: q_out[n] = q[n] rotated, k[n] rotated and v[n] as it is go to row slots[n] of the layer (both
  * as ptd_prompt_slots writes them; the rotation is ptd_tree_rope_append's).  A token with slot -1 (padding)
@@ -564,6 +641,16 @@ ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* 
                                   int32_t num_q_heads, const void* k, int64_t k_stride, const void* v,
                                   int64_t v_stride, float rope_base, void* q_out, int64_t q_out_stride,
                                   int32_t* dev_status, void* stream);
+
+/* As ptd_prompt_rope_append, of a model that normalises its query and key heads (as ptd_tree_norm_rope_append does):
+ * q_weight, k_weight [D] of cache->dtype, eps finite and >= 0.  The cache, q_out and dev_status, which are written,
+ * overlap nothing else that the call reads or writes (PTD_ERR_INVALID_ARG; q_out may be q).  One launch. */
+ptd_status ptd_prompt_norm_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t layer,
+                                       const int32_t* slots, const int32_t* positions, const void* q, int64_t q_stride,
+                                       int32_t num_q_heads, const void* k, int64_t k_stride, const void* v,
+                                       int64_t v_stride, const void* q_weight, const void* k_weight, float eps,
+                                       float rope_base, void* q_out, int64_t q_out_stride, int32_t* dev_status,
+                                       void* stream);
 
 /* Causal attention of a batch's new tokens over one layer of the cache: for token i of sequence b
  * (n = token_offsets[b] + i) and query head h (KV head h / (Hq / Hkv))

@@ -18,8 +18,11 @@
 #include "pool.cuh"
 #include "tree_rope.cuh"
 #include "lm_head.cuh"
+#include "lm_logprobs.cuh"
 #include "memory_rows.cuh"
+#include "page_fork.cuh"
 #include "prompt.cuh"
+#include "token_logprobs.cuh"
 
 namespace ptd {
 cudaError_t launch_bounded_wait_check(int32_t* dev_status, cudaStream_t stream);
@@ -90,6 +93,16 @@ ptd_status check_cache(const ptd_kv_cache* c) {
 
 int64_t cache_rows_per_layer(const ptd_kv_cache* c, int batch) {
   return c->page_size > 0 ? (int64_t)c->num_pages * c->page_size : (int64_t)batch * c->seq_capacity;
+}
+
+// Tensor map of bf16 rows of `cols` columns, `stride` elements apart: boxes of 64 columns and box_rows rows.
+bool encode_rows(CUtensorMap* map, const void* base, int32_t rows, int32_t cols, int64_t stride, uint32_t box_rows) {
+  const PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
+  const cuuint32_t box[2] = {64, box_rows}, estride[2] = {1, 1};
+  const cuuint64_t dim[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, gstride[1] = {(cuuint64_t)stride * 2};
+  return enc && enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dim, gstride, box, estride,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Tensor map of a cache's K or V as [rows of all layers][KV heads][D], boxes of `cols` columns of
@@ -686,6 +699,50 @@ ptd::RopeFreqs rope_freqs(float base, int D) {
 }
 }  // namespace
 
+namespace {
+// A norm of the heads before a rotation: both weights, of the elements' alignment, and a finite eps >= 0.
+bool norms_ok(const void* q_weight, const void* k_weight, float eps, size_t es) {
+  return q_weight && k_weight && (reinterpret_cast<uintptr_t>(q_weight) | reinterpret_cast<uintptr_t>(k_weight)) % es == 0 &&
+         eps >= 0.f && std::isfinite(eps);
+}
+
+// Whether one of the first `written` sets of rows meets another one (sets at NULL are not there).
+bool written_rows_meet(const ptd::MemoryRows* rows, int written, int all) {
+  for (int i = 0; i < written; ++i)
+    for (int j = i + 1; j < all; ++j)
+      if (rows[i].at && rows[j].at && ptd::rows_meet(rows[i], rows[j])) return true;
+  return false;
+}
+
+// Bytes of a layer's or a stack's K (or V), of a block table (0: contiguous).
+int64_t cache_bytes(const ptd_kv_cache* c, int batch, int layers) {
+  return cache_rows_per_layer(c, batch) * layers * c->num_kv_heads * c->head_dim * (int64_t)dtype_size(c->dtype);
+}
+int64_t table_bytes(const ptd_kv_cache* c, int batch) { return c->page_size > 0 ? (int64_t)batch * c->max_pages * 4 : 0; }
+
+// ptd_tree_rope_append (no weights, q_out is q) and ptd_tree_norm_rope_append.
+ptd_status tree_rope_append(const ptd_tree* tree, const ptd_kv_cache* cache, int32_t layer_begin, int32_t num_layers,
+                            const void* q, int32_t num_q_heads, const void* k, const void* v, const ptd::HeadNorms& norms,
+                            float rope_base, void* q_out, int32_t* positions_out, int32_t* dev_status, void* stream) {
+  const int D = cache->head_dim, hkv = cache->num_kv_heads;
+  if (layer_begin < 0 || num_layers < 1 || num_layers > 65535 || layer_begin + num_layers > cache->num_layers ||
+      num_q_heads < hkv || num_q_heads % hkv != 0 || D % 2 != 0 ||
+      D / 2 > ptd::kMaxRopeHalf || !q || !k || !v || !dev_status || !(rope_base > 1.f) || !std::isfinite(rope_base))
+    return PTD_ERR_INVALID_ARG;
+  const size_t es = dtype_size(cache->dtype);
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) |
+       reinterpret_cast<uintptr_t>(q_out)) % es != 0)
+    return PTD_ERR_INVALID_ARG;
+  const ptd_status st = cuda_status(ptd::launch_tree_rope(
+      tree->node_offsets, tree->parents, tree->ctx_lens, tree->batch, tree->total_nodes, cache->dtype == PTD_BF16, D,
+      num_q_heads, hkv, q, q_out, k, v, norms, cache->k, cache->v, layer_begin, num_layers, cache->page_size,
+      cache->seq_capacity, cache->num_pages, cache->block_table, cache->max_pages, rope_freqs(rope_base, D), positions_out,
+      dev_status, num_sms_of_current_device(), static_cast<cudaStream_t>(stream)));
+  if (st == PTD_OK) g_last_launches = 1;
+  return st;
+}
+}  // namespace
+
 ptd_status ptd_tree_rope_append(const ptd_tree* tree, const ptd_kv_cache* cache, int32_t layer_begin,
                                 int32_t num_layers, void* q, int32_t num_q_heads, const void* k, const void* v,
                                 float rope_base, int32_t* positions_out, int32_t* dev_status, void* stream) {
@@ -693,23 +750,35 @@ ptd_status ptd_tree_rope_append(const ptd_tree* tree, const ptd_kv_cache* cache,
   ptd_status st = check_tree(tree);
   if (st != PTD_OK) return st;
   if ((st = check_cache(cache)) != PTD_OK) return st;
-  const int D = cache->head_dim, hkv = cache->num_kv_heads;
-  if (layer_begin < 0 || num_layers < 1 || num_layers > 65535 || layer_begin + num_layers > cache->num_layers ||
-      num_q_heads < hkv || num_q_heads % hkv != 0 || D % 2 != 0 ||
-      D / 2 > ptd::kMaxRopeHalf || !q || !k || !v || !dev_status || !(rope_base > 1.f) || !std::isfinite(rope_base))
+  return tree_rope_append(tree, cache, layer_begin, num_layers, q, num_q_heads, k, v, ptd::HeadNorms{}, rope_base, q,
+                          positions_out, dev_status, stream);
+}
+
+ptd_status ptd_tree_norm_rope_append(const ptd_tree* tree, const ptd_kv_cache* cache, int32_t layer_begin,
+                                     int32_t num_layers, const void* q, int32_t num_q_heads, const void* k, const void* v,
+                                     const void* q_weight, const void* k_weight, float eps, float rope_base, void* q_out,
+                                     int32_t* positions_out, int32_t* dev_status, void* stream) {
+  g_last_launches = 0;
+  ptd_status st = check_tree(tree);
+  if (st != PTD_OK) return st;
+  if ((st = check_cache(cache)) != PTD_OK) return st;
+  const int64_t es = (int64_t)dtype_size(cache->dtype), D = cache->head_dim, L = num_layers, N = tree->total_nodes;
+  if (!q_out || !norms_ok(q_weight, k_weight, eps, es) || num_layers < 1 || num_layers > 65535 || num_q_heads < 1)
     return PTD_ERR_INVALID_ARG;
-  const size_t es = dtype_size(cache->dtype);
-  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) % es != 0)
-    return PTD_ERR_INVALID_ARG;
-  st = cuda_status(ptd::launch_tree_rope(tree->node_offsets, tree->parents, tree->ctx_lens, tree->batch,
-                                         tree->total_nodes, cache->dtype == PTD_BF16, D, num_q_heads, hkv, q, k, v,
-                                         cache->k, cache->v, layer_begin, num_layers, cache->page_size,
-                                         cache->seq_capacity,
-                                         cache->num_pages, cache->block_table, cache->max_pages, rope_freqs(rope_base, D), positions_out,
-                                         dev_status, num_sms_of_current_device(),
-                                         static_cast<cudaStream_t>(stream)));
-  if (st == PTD_OK) g_last_launches = 1;
-  return st;
+  if (((int64_t)num_q_heads + 2 * (int64_t)cache->num_kv_heads) * D > INT32_MAX) return PTD_ERR_UNSUPPORTED;   // a node's elements
+  // what is written overlaps nothing else that the call touches: other CTAs still read it
+  const int64_t qb = L * N * num_q_heads * D * es, kb = L * N * cache->num_kv_heads * D * es;
+  const int64_t cb = cache_bytes(cache, tree->batch, cache->num_layers);
+  using ptd::memory_rows;
+  const ptd::MemoryRows rows[14] = {memory_rows(q_out, qb), memory_rows(positions_out, N * 4), memory_rows(dev_status, 4),
+                                    memory_rows(cache->k, cb), memory_rows(cache->v, cb), memory_rows(q == q_out ? nullptr : q, qb),
+                                    memory_rows(k, kb), memory_rows(v, kb), memory_rows(q_weight, L * D * es),
+                                    memory_rows(k_weight, L * D * es), memory_rows(tree->node_offsets, (int64_t)tree->batch * 4 + 4),
+                                    memory_rows(tree->parents, N * 4), memory_rows(tree->ctx_lens, (int64_t)tree->batch * 4),
+                                    memory_rows(cache->block_table, table_bytes(cache, tree->batch))};
+  if (written_rows_meet(rows, 5, 14)) return PTD_ERR_INVALID_ARG;
+  return tree_rope_append(tree, cache, layer_begin, num_layers, q, num_q_heads, k, v, ptd::HeadNorms{q_weight, k_weight, eps},
+                          rope_base, q_out, positions_out, dev_status, stream);
 }
 
 namespace {
@@ -734,20 +803,6 @@ ptd::PromptBounds prompt_bounds(const ptd_prompt* p, const ptd_kv_cache* c) {
   return {p->total_tokens, p->max_tokens, p->max_ctx,
           c->page_size > 0 ? (int64_t)c->max_pages * c->page_size : (int64_t)c->seq_capacity};
 }
-
-// Whether one of the first `written` sets of rows meets another one (sets at NULL are not there).
-bool written_rows_meet(const ptd::MemoryRows* rows, int written, int all) {
-  for (int i = 0; i < written; ++i)
-    for (int j = i + 1; j < all; ++j)
-      if (rows[i].at && rows[j].at && ptd::rows_meet(rows[i], rows[j])) return true;
-  return false;
-}
-
-// Bytes of a layer's or a stack's K (or V), of a block table (0: contiguous).
-int64_t cache_bytes(const ptd_kv_cache* c, int batch, int layers) {
-  return cache_rows_per_layer(c, batch) * layers * c->num_kv_heads * c->head_dim * (int64_t)dtype_size(c->dtype);
-}
-int64_t table_bytes(const ptd_kv_cache* c, int batch) { return c->page_size > 0 ? (int64_t)batch * c->max_pages * 4 : 0; }
 
 // Tokens `stride` elements apart end within 62 bits.
 bool stride_fits(int64_t stride, int tokens, int64_t es) { return tokens == 1 || stride <= (INT64_MAX >> 1) / es / tokens; }
@@ -840,12 +895,12 @@ ptd_status ptd_prompt_slots(const ptd_prompt* prompt, const ptd_kv_cache* cache,
   return st;
 }
 
-ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t layer,
-                                  const int32_t* slots, const int32_t* positions, const void* q, int64_t q_stride,
-                                  int32_t num_q_heads, const void* k, int64_t k_stride, const void* v,
-                                  int64_t v_stride, float rope_base, void* q_out, int64_t q_out_stride,
-                                  int32_t* dev_status, void* stream) {
-  g_last_launches = 0;
+namespace {
+// ptd_prompt_rope_append (no weights) and ptd_prompt_norm_rope_append.
+ptd_status prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t layer, const int32_t* slots,
+                              const int32_t* positions, const void* q, int64_t q_stride, int32_t num_q_heads, const void* k,
+                              int64_t k_stride, const void* v, int64_t v_stride, const ptd::HeadNorms& norms,
+                              float rope_base, void* q_out, int64_t q_out_stride, int32_t* dev_status, void* stream) {
   ptd_status st = check_prompt(prompt);
   if (st != PTD_OK) return st;
   if ((st = check_cache(cache)) != PTD_OK) return st;
@@ -871,6 +926,19 @@ ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* 
   const ptd::MemoryRows rows[4] = {rows_of(q_out, qe, q_out_stride), rows_of(in_place ? nullptr : q, qe, q_stride),
                                    rows_of(k, ke, k_stride), rows_of(v, ke, v_stride)};
   if (written_rows_meet(rows, 1, 4)) return PTD_ERR_INVALID_ARG;
+  if (norms.q_weight) {   // nor do the norms' weights and a token's rows meet what is written
+    const ptd::MemoryRows more[6] = {rows[0],
+                                     ptd::memory_rows(dev_status, 4),
+                                     ptd::memory_rows(norms.q_weight, D * (int64_t)es),
+                                     ptd::memory_rows(norms.k_weight, D * (int64_t)es),
+                                     ptd::memory_rows(slots, (int64_t)N * 4),
+                                     ptd::memory_rows(positions, (int64_t)N * 4)};
+    if (written_rows_meet(more, 2, 6)) return PTD_ERR_INVALID_ARG;
+    const int64_t cb = cache_bytes(cache, prompt->batch, cache->num_layers);
+    const ptd::MemoryRows reads[10] = {ptd::memory_rows(cache->k, cb), ptd::memory_rows(cache->v, cb), rows[0], rows_of(q, qe, q_stride),
+                                       rows[2], rows[3], more[2], more[3], more[4], more[5]};
+    if (written_rows_meet(reads, 2, 10)) return PTD_ERR_INVALID_ARG;
+  }
   ptd::PromptRopeParams p = {};
   p.slots = slots;
   p.positions = positions;
@@ -891,10 +959,36 @@ ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* 
   p.k_layer = static_cast<uint8_t*>(cache->k) + layer_bytes;
   p.v_layer = static_cast<uint8_t*>(cache->v) + layer_bytes;
   p.dev_status = dev_status;
+  p.norms = norms;
   st = cuda_status(ptd::launch_prompt_rope(p, cache->dtype == PTD_BF16, rope_freqs(rope_base, D),
                                            num_sms_of_current_device(), static_cast<cudaStream_t>(stream)));
   if (st == PTD_OK) g_last_launches = 1;
   return st;
+}
+}  // namespace
+
+ptd_status ptd_prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t layer,
+                                  const int32_t* slots, const int32_t* positions, const void* q, int64_t q_stride,
+                                  int32_t num_q_heads, const void* k, int64_t k_stride, const void* v,
+                                  int64_t v_stride, float rope_base, void* q_out, int64_t q_out_stride,
+                                  int32_t* dev_status, void* stream) {
+  g_last_launches = 0;
+  return prompt_rope_append(prompt, cache, layer, slots, positions, q, q_stride, num_q_heads, k, k_stride, v, v_stride,
+                            ptd::HeadNorms{}, rope_base, q_out, q_out_stride, dev_status, stream);
+}
+
+ptd_status ptd_prompt_norm_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t layer,
+                                       const int32_t* slots, const int32_t* positions, const void* q, int64_t q_stride,
+                                       int32_t num_q_heads, const void* k, int64_t k_stride, const void* v,
+                                       int64_t v_stride, const void* q_weight, const void* k_weight, float eps,
+                                       float rope_base, void* q_out, int64_t q_out_stride, int32_t* dev_status,
+                                       void* stream) {
+  g_last_launches = 0;
+  const ptd_status st = check_cache(cache);
+  if (st != PTD_OK) return st;
+  if (!norms_ok(q_weight, k_weight, eps, dtype_size(cache->dtype))) return PTD_ERR_INVALID_ARG;
+  return prompt_rope_append(prompt, cache, layer, slots, positions, q, q_stride, num_q_heads, k, k_stride, v, v_stride,
+                            ptd::HeadNorms{q_weight, k_weight, eps}, rope_base, q_out, q_out_stride, dev_status, stream);
 }
 
 size_t ptd_prompt_attention_workspace_size(const ptd_prompt* prompt, const ptd_kv_cache* cache, int32_t num_q_heads) {
@@ -994,25 +1088,191 @@ ptd_status ptd_lm_head_topk(const void* hidden, int32_t rows, int64_t hidden_str
   const int ctas = ptd::lm_head_ctas(num_sms_of_current_device(), vocab);
   if (!workspace || workspace_bytes < ptd::lm_head_workspace_bytes(ctas, rows) || !aligned16(workspace))
     return PTD_ERR_WORKSPACE;
-  PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
-  if (!enc) return PTD_ERR_CUDA;
   CUtensorMap map_h, map_w;
-  const cuuint32_t box[2] = {64, 128}, estride[2] = {1, 1};
-  const cuuint64_t hdim[2] = {(cuuint64_t)d_model, (cuuint64_t)rows};
-  const cuuint64_t hstride[1] = {(cuuint64_t)hidden_stride * 2};
-  const cuuint64_t wdim[2] = {(cuuint64_t)d_model, (cuuint64_t)vocab};
-  const cuuint64_t wstride[1] = {(cuuint64_t)weight_stride * 2};
-  if (enc(&map_h, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(hidden), hdim, hstride, box, estride,
-          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-    return PTD_ERR_CUDA;
-  if (enc(&map_w, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(weight), wdim, wstride, box, estride,
-          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+  if (!encode_rows(&map_h, hidden, rows, d_model, hidden_stride, 128) ||
+      !encode_rows(&map_w, weight, vocab, d_model, weight_stride, 128))
     return PTD_ERR_CUDA;
   const ptd_status st = cuda_status(ptd::launch_lm_head_topk(map_h, map_w, rows, d_model, vocab, k, out_idx, out_val,
                                                               workspace, ctas, dev_status,
                                                               static_cast<cudaStream_t>(stream)));
+  if (st == PTD_OK) g_last_launches = 2;
+  return st;
+}
+
+namespace {
+// log2(e) / temperature; 0 for a temperature that is not one.
+float logprob_scale(float temperature) {
+  if (!(temperature > 0.f) || !std::isfinite(temperature)) return 0.f;
+  const float s = (float)(1.4426950408889634 / (double)temperature);
+  return std::isfinite(s) ? s : 0.f;
+}
+
+// The outputs of the log probabilities of `rows` rows, which overlap no input (n_in sets of rows) and not one another.
+ptd_status check_logprob_outputs(int64_t rows, int32_t k, const int32_t* tokens, const float* logprob, const float* entropy,
+                                 const int32_t* top_idx, const float* top_val, const int32_t* dev_status,
+                                 const ptd::MemoryRows* inputs, int n_in) {
+  if (!tokens || !logprob || !dev_status || k < 0 || k > PTD_MAX_TOPK || (k > 0 && (!top_idx || !top_val))) return PTD_ERR_INVALID_ARG;
+  using ptd::memory_rows;
+  ptd::MemoryRows all[10] = {memory_rows(logprob, rows * 4),
+                             memory_rows(entropy, rows * 4),
+                             memory_rows(k > 0 ? top_idx : nullptr, rows * k * 4),
+                             memory_rows(k > 0 ? top_val : nullptr, rows * k * 4),
+                             memory_rows(dev_status, 4),
+                             memory_rows(tokens, rows * 4)};
+  for (int i = 0; i < n_in; ++i) all[6 + i] = inputs[i];
+  return written_rows_meet(all, 5, 6 + n_in) ? PTD_ERR_INVALID_ARG : PTD_OK;
+}
+}  // namespace
+
+ptd_status ptd_token_logprobs(const void* logits, ptd_dtype dtype, int64_t rows, int32_t vocab, int64_t row_stride,
+                              const int32_t* tokens, float temperature, int32_t k, float* out_logprob, float* out_entropy,
+                              int32_t* out_idx, float* out_val, int32_t* dev_status, void* stream) {
+  g_last_launches = 0;
+  const float scale = logprob_scale(temperature);
+  if (!logits || (dtype != PTD_BF16 && dtype != PTD_F32) || rows < 1 || vocab < 1 || vocab < k || row_stride < vocab || scale == 0.f)
+    return PTD_ERR_INVALID_ARG;
+  const int64_t es = (int64_t)dtype_size(dtype);
+  if (reinterpret_cast<uintptr_t>(logits) % es != 0 || row_stride > (INT64_MAX >> 1) / es / rows) return PTD_ERR_INVALID_ARG;
+  if (rows > PTD_MAX_PROMPT_TOKENS || vocab > PTD_MAX_PROMPT_TOKENS) return PTD_ERR_UNSUPPORTED;
+  const ptd::MemoryRows in[1] = {ptd::memory_rows(logits, vocab * es, row_stride * es, rows)};
+  ptd_status st = check_logprob_outputs(rows, k, tokens, out_logprob, out_entropy, out_idx, out_val, dev_status, in, 1);
+  if (st != PTD_OK) return st;
+  ptd::TokenLogprobsParams p = {};
+  p.logits = logits;
+  p.rows = rows;
+  p.row_stride = row_stride;
+  p.vocab = vocab;
+  p.k = k;
+  p.scale = scale;
+  p.inv_temperature = 1.f / temperature;
+  p.tokens = tokens;
+  p.logprob = out_logprob;
+  p.entropy = out_entropy;
+  p.top_idx = out_idx;
+  p.top_val = out_val;
+  p.dev_status = dev_status;
+  st = cuda_status(ptd::launch_token_logprobs(p, dtype == PTD_BF16, num_sms_of_current_device(), static_cast<cudaStream_t>(stream)));
+  if (st == PTD_OK) g_last_launches = 1;
+  return st;
+}
+
+size_t ptd_lm_head_logprobs_workspace_size(int32_t rows, int32_t vocab, int32_t k) {
+  if (rows < 1 || rows > PTD_MAX_LOGPROB_ROWS || vocab < 1 || vocab > PTD_MAX_PROMPT_TOKENS || k < 0 || k > PTD_MAX_TOPK) return 0;
+  return ptd::lm_logprobs_workspace_bytes(ptd::plan_lm_logprobs(rows, vocab, k, num_sms_of_current_device()), rows);
+}
+
+ptd_status ptd_lm_head_logprobs(const void* hidden, int32_t rows, int64_t hidden_stride, const void* weight, int32_t vocab,
+                                int64_t weight_stride, int32_t d_model, const int32_t* tokens, float temperature, int32_t k,
+                                float* out_logprob, float* out_entropy, int32_t* out_idx, float* out_val, void* workspace,
+                                size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  g_last_launches = 0;
+  const float scale = logprob_scale(temperature);
+  if (!hidden || !weight || rows < 1 || d_model < 64 || d_model % 64 != 0 || vocab < 1 || vocab < k || hidden_stride < d_model ||
+      weight_stride < d_model || hidden_stride % 8 != 0 || weight_stride % 8 != 0 || !aligned16(hidden) || !aligned16(weight) ||
+      scale == 0.f || hidden_stride > (INT64_MAX >> 2) / rows || weight_stride > (INT64_MAX >> 2) / vocab)
+    return PTD_ERR_INVALID_ARG;
+  if (rows > PTD_MAX_LOGPROB_ROWS || vocab > PTD_MAX_PROMPT_TOKENS) return PTD_ERR_UNSUPPORTED;
+  const ptd::LmLogprobsPlan plan = ptd::plan_lm_logprobs(rows, vocab, k, num_sms_of_current_device());
+  const size_t need = ptd::lm_logprobs_workspace_bytes(plan, rows);
+  const ptd::MemoryRows in[3] = {ptd::memory_rows(workspace, (int64_t)need),
+                                 ptd::memory_rows(hidden, (int64_t)d_model * 2, hidden_stride * 2, rows),
+                                 ptd::memory_rows(weight, (int64_t)d_model * 2, weight_stride * 2, vocab)};
+  ptd_status st = check_logprob_outputs(rows, k, tokens, out_logprob, out_entropy, out_idx, out_val, dev_status, in, 3);
+  if (st != PTD_OK) return st;
+  if (!workspace || workspace_bytes < need || !aligned16(workspace)) return PTD_ERR_WORKSPACE;
+  const ptd::MemoryRows scratch[4] = {in[0], in[1], in[2], ptd::memory_rows(tokens, (int64_t)rows * 4)};
+  if (written_rows_meet(scratch, 1, 4)) return PTD_ERR_INVALID_ARG;
+  CUtensorMap map_h, map_w;
+  if (!encode_rows(&map_h, hidden, rows, d_model, hidden_stride, ptd::kLmTileRows) ||
+      !encode_rows(&map_w, weight, vocab, d_model, weight_stride, plan.tile_tokens))
+    return PTD_ERR_CUDA;
+  ptd::LmLogprobsParams p = {};
+  p.rows = rows;
+  p.d_model = d_model;
+  p.vocab = vocab;
+  p.k = k;
+  p.scale = scale;
+  p.inv_temperature = 1.f / temperature;
+  p.tokens = tokens;
+  p.logprob = out_logprob;
+  p.entropy = out_entropy;
+  p.top_idx = out_idx;
+  p.top_val = out_val;
+  p.dev_status = dev_status;
+  p.plan = plan;
+  p.workspace = workspace;
+  st = cuda_status(ptd::launch_lm_logprobs(map_h, map_w, p, static_cast<cudaStream_t>(stream)));
+  if (st == PTD_OK) g_last_launches = 2;
+  return st;
+}
+
+namespace {
+ptd_status check_page_sets(const ptd_kv_cache* cache, const ptd_page_set* from, const ptd_page_set* to) {
+  const ptd_status st = check_cache(cache);
+  if (st != PTD_OK) return st;
+  if (!from || !to || cache->page_size == 0) return PTD_ERR_INVALID_ARG;
+  for (const ptd_page_set* s : {from, to}) {
+    if (s->batch < 1 || !s->block_table || !s->held || !s->free_pages || !s->free_count) return PTD_ERR_INVALID_ARG;
+    if (s->batch > PTD_MAX_PROMPT_BATCH || (int64_t)s->batch * cache->max_pages > INT32_MAX) return PTD_ERR_UNSUPPORTED;
+  }
+  return cache_rows_per_layer(cache, 1) > INT32_MAX || cache->num_pages > PTD_MAX_PROMPT_TOKENS / 2 ? PTD_ERR_UNSUPPORTED : PTD_OK;
+}
+}  // namespace
+
+size_t ptd_page_fork_workspace_size(const ptd_kv_cache* cache, const ptd_page_set* from, const ptd_page_set* to) {
+  if (check_page_sets(cache, from, to) != PTD_OK) return 0;
+  return ptd::page_fork_scratch_ints(cache->num_pages, from->batch, to->batch) * 4;
+}
+
+ptd_status ptd_page_fork(const ptd_kv_cache* cache, const ptd_page_set* from, const ptd_page_set* to, const int32_t* parents,
+                         const int32_t* lens, void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  g_last_launches = 0;
+  ptd_status st = check_page_sets(cache, from, to);
+  if (st != PTD_OK) return st;
+  if (!parents || !lens || !dev_status) return PTD_ERR_INVALID_ARG;
+  const size_t need = ptd_page_fork_workspace_size(cache, from, to);
+  // what is written overlaps nothing else that the call touches
+  const int64_t cb = cache_bytes(cache, 1, cache->num_layers), pages4 = (int64_t)cache->num_pages * 4;
+  using ptd::memory_rows;
+  const ptd::MemoryRows rows[14] = {memory_rows(to->block_table, table_bytes(cache, to->batch)),
+                                    memory_rows(to->held, (int64_t)to->batch * 4),
+                                    memory_rows(to->free_pages, pages4),
+                                    memory_rows(to->free_count, 4),
+                                    memory_rows(dev_status, 4),
+                                    memory_rows(workspace, (int64_t)need),
+                                    memory_rows(cache->k, cb),
+                                    memory_rows(cache->v, cb),
+                                    memory_rows(from->block_table, table_bytes(cache, from->batch)),
+                                    memory_rows(from->held, (int64_t)from->batch * 4),
+                                    memory_rows(from->free_pages, pages4),
+                                    memory_rows(from->free_count, 4),
+                                    memory_rows(parents, (int64_t)to->batch * 4),
+                                    memory_rows(lens, (int64_t)to->batch * 4)};
+  if (written_rows_meet(rows, 8, 14)) return PTD_ERR_INVALID_ARG;
+  if (!workspace || workspace_bytes < need || !aligned16(workspace)) return PTD_ERR_WORKSPACE;
+  ptd::PageForkParams p = {};
+  p.from_batch = from->batch;
+  p.to_batch = to->batch;
+  p.num_pages = cache->num_pages;
+  p.max_pages = cache->max_pages;
+  p.page_log2 = page_log2(cache);
+  p.table = from->block_table;
+  p.held = from->held;
+  p.free_pages = from->free_pages;
+  p.free_count = from->free_count;
+  p.new_table = to->block_table;
+  p.new_held = to->held;
+  p.new_free_pages = to->free_pages;
+  p.new_free_count = to->free_count;
+  p.parents = parents;
+  p.lens = lens;
+  p.k = cache->k;
+  p.v = cache->v;
+  p.num_layers = cache->num_layers;
+  p.row_bytes = (int64_t)cache->num_kv_heads * cache->head_dim * (int64_t)dtype_size(cache->dtype);
+  p.dev_status = dev_status;
+  p.scratch = static_cast<int32_t*>(workspace);
+  st = cuda_status(ptd::launch_page_fork(p, num_sms_of_current_device(), static_cast<cudaStream_t>(stream)));
   if (st == PTD_OK) g_last_launches = 2;
   return st;
 }

@@ -1,0 +1,348 @@
+// Log probabilities of given tokens, entropies and best alternatives from hidden states: the LM-head product with the
+// softmax statistics of row_sums.cuh as its epilogue.  The logits never reach memory.
+//
+// Tiles of 128 rows of H by 256 (or 128) rows of W, one CTA per SM:
+//   warp 0     TMA producer: per 64 columns of d_model the tile's rows of H and of W, 128-byte swizzle, into a ring;
+//   warp 1     allocates TMEM, one thread issues the MMAs (M 128, K 16, bf16 -> fp32) into one of two accumulators;
+//   warps 2-5  epilogue: TMEM lane r holds row r's logits; thread r keeps its row's sums, its best alternatives
+//              (64-bit keys: value, then the lower token) and its token's logit over the CTA's tiles of a phase.
+// A second kernel merges the parts that a row's CTAs left in the workspace.
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "launch.cuh"
+#include "lm_logprobs.cuh"
+#include "ptd_device.cuh"
+#include "row_sums.cuh"
+#include "topk_parts.cuh"
+
+namespace ptd {
+namespace ll {
+
+constexpr int kThreads = 192;
+constexpr uint32_t kTmemCols = 512;
+
+template <int kTile>   // tokens of a tile
+struct Smem {
+  static constexpr int kStages = kTile == 256 ? 4 : 7;
+  static constexpr uint32_t kHBytes = kLmTileRows * 128, kWBytes = kTile * 128, kStageBytes = kHBytes + kWBytes;
+  static constexpr uint32_t kOffBar = kStages * kStageBytes;
+  static constexpr int kNumBars = 2 * kStages + 5;   // full, empty, acc_full[2], acc_empty[2], drain
+  static constexpr uint32_t kOffTmemPtr = kOffBar + kNumBars * 8, kOffAbort = kOffTmemPtr + 4;
+  static constexpr uint32_t kBytes = kOffAbort + 16 + 1024;   // slack to align the base to 1024 B
+  static_assert(kBytes <= 232448, "shared memory budget");
+};
+// The parts of rows in the workspace: part (phase, cta) has 128 rows.
+struct Parts {
+  RowSums* sums;
+  uint64_t* keys;       // [part rows][KM]
+  float* token_logit;   // [rows]
+};
+__host__ __device__ __forceinline__ Parts parts_of(void* workspace, const LmLogprobsPlan& plan, int rows) {
+  const size_t part_rows = (size_t)((plan.row_tiles + plan.per_phase - 1) / plan.per_phase) * plan.ctas * kLmTileRows;
+  Parts p;
+  p.keys = static_cast<uint64_t*>(workspace);
+  p.sums = reinterpret_cast<RowSums*>(p.keys + part_rows * plan.keys);
+  p.token_logit = reinterpret_cast<float*>(p.sums + part_rows);
+  (void)rows;
+  return p;
+}
+
+// Insert key into a descending list of KM keys (0 = empty: below every real key).
+template <int KM>
+__device__ __forceinline__ void insert(uint64_t (&top)[KM], uint64_t key) {
+  if (key <= top[KM - 1]) return;
+  top[KM - 1] = key;
+#pragma unroll
+  for (int j = KM - 1; j > 0; --j) {
+    if (top[j] > top[j - 1]) {
+      const uint64_t x = top[j];
+      top[j] = top[j - 1];
+      top[j - 1] = x;
+    }
+  }
+}
+
+// The CTA's units, phase by phase: f(phase, row tile, first vocabulary tile, step).
+template <typename F>
+__device__ __forceinline__ void for_units(const LmLogprobsPlan& plan, F&& f) {
+  for (int phase = 0, t0 = 0; t0 < plan.row_tiles; ++phase, t0 += plan.per_phase) {
+    const int R = min(plan.per_phase, plan.row_tiles - t0), C = plan.ctas / R;
+    const int lane = (int)blockIdx.x / R;
+    if (lane < C && lane < plan.vocab_tiles)
+      if (!f(phase, t0 + (int)blockIdx.x % R, lane, C)) return;
+  }
+}
+
+template <int KM, int kTile>
+__global__ void __launch_bounds__(kThreads, 1)
+    lm_logprobs_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_constant__ CUtensorMap map_w,
+                       const __grid_constant__ LmLogprobsParams p) {
+  using S = Smem<kTile>;
+  constexpr int kStages = S::kStages;
+  constexpr uint32_t kIdesc = idesc_bf16_f32(kLmTileRows, kTile, 0, 0);
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint32_t base = smem_u32(smem_raw);
+  const uint32_t pad = (1024u - (base & 1023u)) & 1023u;
+  uint8_t* smem = smem_raw + pad;
+  base += pad;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto bar = [&](int i) { return base + S::kOffBar + 8u * (uint32_t)i; };
+  auto full_bar = [&](int s) { return bar(s); };
+  auto empty_bar = [&](int s) { return bar(kStages + s); };
+  auto accf_bar = [&](int b) { return bar(2 * kStages + b); };
+  auto acce_bar = [&](int b) { return bar(2 * kStages + 2 + b); };
+  const uint32_t drain_bar = bar(2 * kStages + 4);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::kOffAbort);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(accf_bar(b), 1);
+      mbar_init(acce_bar(b), 4);   // one arrival per epilogue warp
+    }
+    mbar_init(drain_bar, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(base + S::kOffTmemPtr, kTmemCols);
+    tmem_relinquish();
+    tc_fence_before();
+  }
+  grid_dependency_wait();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + S::kOffTmemPtr);
+  const int n_chunks = p.d_model / 64, vocab_tiles = p.plan.vocab_tiles;
+
+  if (warp == 0) {
+    // ================================================================ TMA producer
+    if (lane == 0) {
+      prefetch_tensormap(&map_h);
+      prefetch_tensormap(&map_w);
+      bool ok = true;
+      int s = 0, g = 0;   // ring position; chunks issued
+      uint32_t phase_bit = 1;
+      for_units(p.plan, [&](int, int row_tile, int tile, int step) {
+        for (; tile < vocab_tiles; tile += step) {
+          for (int c = 0; c < n_chunks; ++c) {
+            if (!(ok = mbar_wait(empty_bar(s), phase_bit, abort_flag, p.dev_status))) return false;
+            const uint32_t dst = base + (uint32_t)s * S::kStageBytes;
+            mbar_arrive_expect_tx(full_bar(s), S::kStageBytes);
+            tma_load_2d(dst, &map_h, full_bar(s), c * 64, row_tile * kLmTileRows);
+            tma_load_2d(dst + S::kHBytes, &map_w, full_bar(s), c * 64, tile * kTile);
+            ++g;
+            if (++s == kStages) s = 0, phase_bit ^= 1u;
+          }
+        }
+        return true;
+      });
+      if (!ok) {   // let the copies already issued land before the CTA can exit
+        for (int back = 1; back <= kStages && g - back >= 0; ++back)
+          mbar_drain(full_bar((g - back) % kStages), (uint32_t)(((g - back) / kStages) & 1), 100000000ull);
+      }
+    }
+  } else if (warp == 1) {
+    // ================================================================ MMA issuer
+    if (lane == 0) {
+      bool ok = true;
+      int s = 0, it = 0;
+      uint32_t phase_bit = 0;
+      for_units(p.plan, [&](int, int, int tile, int step) {
+        for (; tile < vocab_tiles; tile += step, ++it) {
+          const int buf = it & 1;
+          if (!(ok = mbar_wait(acce_bar(buf), (uint32_t)(((it >> 1) & 1) ^ 1), abort_flag, p.dev_status))) return false;
+          tc_fence_after();
+          const uint32_t d = tmem + (uint32_t)(buf * kTile);
+          for (int c = 0; c < n_chunks; ++c) {
+            if (!(ok = mbar_wait(full_bar(s), phase_bit, abort_flag, p.dev_status))) return false;
+            tc_fence_after();
+            const uint32_t a0 = base + (uint32_t)s * S::kStageBytes, b0 = a0 + S::kHBytes;
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              mma_bf16_ss(d, smem_desc_sw128(a0 + (uint32_t)kk * 32u, 16, 1024), smem_desc_sw128(b0 + (uint32_t)kk * 32u, 16, 1024),
+                          kIdesc, (c > 0 || kk > 0) ? 1u : 0u);
+            mma_commit(empty_bar(s));   // the stage is free once these MMAs have read it
+            if (++s == kStages) s = 0, phase_bit ^= 1u;
+          }
+          mma_commit(accf_bar(buf));
+        }
+        return true;
+      });
+      if (!ok) {   // let the tensor core finish what was issued before TMEM is freed
+        mma_commit(drain_bar);
+        mbar_drain(drain_bar, 0, 100000000ull);
+      }
+    }
+  } else {
+    // ================================================================ epilogue
+    const int wq = warp & 3;                     // TMEM lane quarter of this warp
+    const uint32_t lane_base = (uint32_t)(wq * 32) << 16;
+    const unsigned long long scale2 = f2_pack(p.scale, p.scale);
+    const Parts parts = parts_of(p.workspace, p.plan, p.rows);
+    int it = 0;
+    for_units(p.plan, [&](int phase, int row_tile, int tile, int step) {
+      const int r = wq * 32 + lane, row = row_tile * kLmTileRows + r;
+      const int token = row < p.rows ? p.tokens[row] : -1;
+      ThreadSums sums;
+      uint64_t top[KM > 0 ? KM : 1];
+#pragma unroll
+      for (int j = 0; j < KM; ++j) top[j] = 0ull;
+      float worst = -INFINITY;   // of a full list
+      for (; tile < vocab_tiles; tile += step, ++it) {
+        const int buf = it & 1;
+        if (!mbar_wait_warp(accf_bar(buf), (uint32_t)((it >> 1) & 1), abort_flag, p.dev_status)) return false;
+        tc_fence_after();
+        const int t0 = tile * kTile;
+#pragma unroll 1
+        for (int c0 = 0; c0 < kTile; c0 += 32) {
+          uint32_t v[32];
+          tmem_ld32(tmem + lane_base + (uint32_t)(buf * kTile + c0), v);
+          tmem_ld_wait();
+          const int tb = t0 + c0;
+          if (tb + 32 > p.vocab) {   // rows of W past the last one were read as zeros
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (tb + e >= p.vocab) v[e] = 0xFF800000u;   // -inf
+          }
+          float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int e = 0; e < 32; e += 8)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              m[q] = fmax3(m[q], __uint_as_float(v[e + 2 * q]), __uint_as_float(v[e + 2 * q + 1]));
+          const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+          sums.raise(most, p.scale);
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) sums.add2(__uint_as_float(v[e]), __uint_as_float(v[e + 1]), scale2);
+          if ((unsigned)(token - tb) < 32u) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (token == tb + e && token < p.vocab) parts.token_logit[row] = __uint_as_float(v[e]);
+          }
+          if constexpr (KM > 0) {
+            if (most > worst || top[KM - 1] == 0ull) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (tb + e < p.vocab) insert<KM>(top, topk::make_key(topk::ordered_bits(__uint_as_float(v[e])), (uint32_t)(tb + e)));
+              if (top[KM - 1] != 0ull) worst = topk::from_ordered((uint32_t)(top[KM - 1] >> 32));
+            }
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(acce_bar(buf));
+      }
+      if (row < p.rows) {
+        const size_t at = ((size_t)phase * p.plan.ctas + blockIdx.x) * kLmTileRows + r;
+        parts.sums[at] = sums.sums();
+#pragma unroll
+        for (int j = 0; j < KM; ++j) parts.keys[at * KM + j] = top[j];
+      }
+      return true;
+    });
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) grid_launch_dependents();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+// A warp per row: each lane merges some of the row's parts, then KM rounds of a warp-wide maximum (the owning lane pops its head).
+constexpr int kMergeThreads = 128;
+
+template <int KM>
+__global__ void __launch_bounds__(kMergeThreads) lm_logprobs_merge_kernel(const __grid_constant__ LmLogprobsParams p) {
+  if (threadIdx.x == 0) grid_launch_dependents();
+  grid_dependency_wait();
+  const int row = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (row >= p.rows) return;
+  const Parts parts = parts_of(p.workspace, p.plan, p.rows);
+  const int row_tile = row / kLmTileRows, phase = row_tile / p.plan.per_phase, t0 = phase * p.plan.per_phase;
+  const int R = min(p.plan.per_phase, p.plan.row_tiles - t0), C = min(p.plan.ctas / R, p.plan.vocab_tiles);
+  RowSums sums = {-INFINITY, 0.f, 0.f};
+  uint64_t top[KM > 0 ? KM : 1];
+#pragma unroll
+  for (int j = 0; j < KM; ++j) top[j] = 0ull;
+  for (int c = lane; c < C; c += 32) {
+    const size_t at = ((size_t)phase * p.plan.ctas + c * R + (row_tile - t0)) * kLmTileRows + row % kLmTileRows;
+    sums = merge_sums(sums, parts.sums[at], p.scale);
+    uint64_t list[KM > 0 ? KM : 1];   // read together: an insertion may end early, and the next load would wait for it
+#pragma unroll
+    for (int j = 0; j < KM; ++j) list[j] = parts.keys[at * KM + j];
+#pragma unroll
+    for (int j = 0; j < KM; ++j) insert(top, list[j]);
+  }
+  const RowResult result(merge_lanes(sums, 32, p.scale));
+  if (lane == 0) {
+    const int token = p.tokens[row];
+    p.logprob[row] = token >= 0 && token < p.vocab ? result.logprob(parts.token_logit[row], p.inv_temperature) : -INFINITY;
+    if (p.entropy != nullptr) p.entropy[row] = result.entropy;
+  }
+#pragma unroll
+  for (int j = 0; j < KM; ++j) {
+    const uint64_t best = topk::warp_max_u64(top[0]);
+    if (best != 0ull && top[0] == best) {   // keys are distinct
+#pragma unroll
+      for (int q = 0; q < KM - 1; ++q) top[q] = top[q + 1];
+      top[KM - 1] = 0ull;
+    }
+    if (lane == 0 && j < p.k) {
+      p.top_idx[(size_t)row * p.k + j] = (int32_t)(~(uint32_t)best);
+      p.top_val[(size_t)row * p.k + j] = result.logprob(topk::from_ordered((uint32_t)(best >> 32)), p.inv_temperature);
+    }
+  }
+}
+
+template <int KM, int kTile>
+cudaError_t launch(const CUtensorMap& map_h, const CUtensorMap& map_w, const LmLogprobsParams& p, cudaStream_t stream) {
+  cudaError_t e = cudaFuncSetAttribute(lm_logprobs_kernel<KM, kTile>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       (int)Smem<kTile>::kBytes);
+  if (e != cudaSuccess) return e;
+  e = launch_chained(lm_logprobs_kernel<KM, kTile>, dim3(p.plan.ctas), dim3(kThreads), Smem<kTile>::kBytes, stream, 0, map_h, map_w, p);
+  if (e != cudaSuccess) return e;
+  constexpr int kRows = kMergeThreads / 32;
+  return launch_chained(lm_logprobs_merge_kernel<KM>, dim3((p.rows + kRows - 1) / kRows), dim3(kMergeThreads), 0, stream, 0, p);
+}
+
+template <int KM>
+cudaError_t launch_tile(const CUtensorMap& map_h, const CUtensorMap& map_w, const LmLogprobsParams& p, cudaStream_t stream) {
+  return p.plan.tile_tokens == 256 ? launch<KM, 256>(map_h, map_w, p, stream) : launch<KM, 128>(map_h, map_w, p, stream);
+}
+
+}  // namespace ll
+
+LmLogprobsPlan plan_lm_logprobs(int rows, int vocab, int k, int sms) {
+  LmLogprobsPlan plan;
+  plan.row_tiles = (rows + kLmTileRows - 1) / kLmTileRows;
+  plan.per_phase = sms < 8 ? sms : 8;
+  plan.tile_tokens = plan.row_tiles > 1 ? 256 : 128;
+  plan.vocab_tiles = (vocab + plan.tile_tokens - 1) / plan.tile_tokens;
+  plan.keys = k == 0 ? 0 : (k <= 4 ? 4 : (k <= 8 ? 8 : 16));
+  const int64_t most = (int64_t)(plan.row_tiles < plan.per_phase ? plan.row_tiles : plan.per_phase) * plan.vocab_tiles;
+  plan.ctas = most < sms ? (int)most : sms;
+  return plan;
+}
+
+size_t lm_logprobs_workspace_bytes(const LmLogprobsPlan& plan, int rows) {
+  const size_t part_rows = (size_t)((plan.row_tiles + plan.per_phase - 1) / plan.per_phase) * plan.ctas * kLmTileRows;
+  return part_rows * (plan.keys * sizeof(uint64_t) + sizeof(RowSums)) + (size_t)rows * sizeof(float);
+}
+
+cudaError_t launch_lm_logprobs(const CUtensorMap& map_h, const CUtensorMap& map_w, const LmLogprobsParams& p, cudaStream_t stream) {
+  switch (p.plan.keys) {
+    case 0: return ll::launch_tile<0>(map_h, map_w, p, stream);
+    case 4: return ll::launch_tile<4>(map_h, map_w, p, stream);
+    case 8: return ll::launch_tile<8>(map_h, map_w, p, stream);
+    default: return ll::launch_tile<16>(map_h, map_w, p, stream);
+  }
+}
+
+}  // namespace ptd

@@ -45,6 +45,7 @@ struct PromptRopeParams {
   void* v_layer;
   int64_t layer_rows;
   int32_t* dev_status;
+  HeadNorms norms;    // weights [D]
 };
 cudaError_t launch_prompt_rope(const PromptRopeParams& p, bool bf16, const RopeFreqs& freqs, int sms,
                                cudaStream_t stream);

@@ -24,7 +24,8 @@ PyObject *s_is_cuda, *s_is_contiguous, *s_dtype, *s_data_ptr, *s_nbytes, *s_shap
   X(ptd_tree_attention) X(ptd_topk_draft) X(ptd_verify_greedy) X(ptd_kv_compact) X(ptd_verify_sampling)             \
   X(ptd_verify_and_compact) X(ptd_draft_tree_update) X(ptd_pool_merge) X(ptd_pool_retrieve) X(ptd_tree_rope_append) \
   X(ptd_lm_head_topk) X(ptd_tree_verify_step) X(ptd_prompt_slots) X(ptd_prompt_rope_append) X(ptd_prompt_attention)   \
-  X(ptd_last_launch_count)
+  X(ptd_prompt_norm_rope_append) X(ptd_tree_norm_rope_append) X(ptd_token_logprobs) X(ptd_lm_head_logprobs)          \
+  X(ptd_page_fork) X(ptd_last_launch_count)
 #define PTD_DECLARE(f) decltype(&f) p_##f;
 PTD_FUNCTIONS(PTD_DECLARE)
 #undef PTD_DECLARE
@@ -172,16 +173,69 @@ struct Args {
     Py_XDECREF(t);
     if (PyErr_Occurred() || (paged ? rows < prompt->batch : rows != prompt->batch)) fail();
   }
-  // an int32 tensor of `count` elements
-  int32_t* i32_of(int64_t count) {
+  // a tensor of `count` elements of 32 bits, an int32 one
+  void* word_of(PyObject* dtype, int64_t count) {
     PyObject* o = next();
-    void* p = tensor_of(o, g_i32);
+    void* p = tensor_of(o, dtype);
     if (!ok) return nullptr;
     on(o);
     PyObject* r = ok ? PyObject_GetAttr(o, s_nbytes) : nullptr;
     if (r == nullptr || !PyLong_CheckExact(r) || PyLong_AsLongLong(r) != 4 * count) fail();
     Py_XDECREF(r);
-    return static_cast<int32_t*>(p);
+    return p;
+  }
+  int32_t* i32_of(int64_t count) { return static_cast<int32_t*>(word_of(g_i32, count)); }
+  // the sizes of a tensor of 2 to 4 dimensions; how many there are
+  int dims(PyObject* o, int64_t (&d)[4]) {
+    d[0] = d[1] = d[2] = d[3] = 0;
+    if (!ok) return 0;
+    PyObject* s = PyObject_GetAttr(o, s_shape);
+    int n = 0;
+    if (s != nullptr && PyTuple_Check(s) && PyTuple_GET_SIZE(s) >= 1 && PyTuple_GET_SIZE(s) <= 4) {
+      n = (int)PyTuple_GET_SIZE(s);
+      for (int i = 0; i < n; ++i) d[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(s, i));
+    } else {
+      ok = false;
+    }
+    Py_XDECREF(s);
+    if (PyErr_Occurred()) fail();
+    return n;
+  }
+  // a contiguous tensor of `dtype`, of this shape
+  void* shaped(PyObject* dtype, int n, const int64_t* want) {
+    PyObject* o = next();
+    void* p = tensor_of(o, dtype);
+    if (!ok) return nullptr;
+    int64_t d[4];
+    if (dims(o, d) != n) ok = false;
+    for (int i = 0; i < n; ++i) ok = ok && d[i] == want[i];
+    on(o);
+    return p;
+  }
+  // log probabilities: tokens, out_logprob, out_entropy (or None), out_idx and out_val (or None) of `rows` rows
+  struct Logprobs {
+    const int32_t* tokens;
+    float *logprob, *entropy, *val;
+    int32_t* idx;
+    int32_t k;
+  };
+  Logprobs logprobs(int64_t rows) {
+    Logprobs x = {};
+    x.tokens = i32_of(rows);
+    x.logprob = static_cast<float*>(word_of(g_f32, rows));
+    x.entropy = a[i] == Py_None ? (next(), nullptr) : static_cast<float*>(word_of(g_f32, rows));
+    if (ok && a[i] == Py_None && a[i + 1] == Py_None) {
+      i += 2;
+      return x;
+    }
+    int64_t want[4] = {rows, 0, 0, 0}, k = 0;
+    dims2(a[i], &want[0], &k);
+    if (want[0] != rows || k < 1 || k > PTD_MAX_TOPK) ok = false;
+    want[1] = k;
+    x.k = (int32_t)k;
+    x.idx = static_cast<int32_t*>(shaped(g_i32, 2, want));
+    x.val = static_cast<float*>(shaped(g_f32, 2, want));
+    return x;
   }
   // a [rows, heads, dim] tensor whose tokens may be apart, a token's heads back to back (*heads 0: any)
   void* rows3(PyObject* dtype, int64_t rows, int64_t dim, int64_t* heads, int64_t* stride) {
@@ -627,6 +681,153 @@ PyObject* prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   PTD_CALL(p_ptd_prompt_attention(prompt, cache, layer, q, qs, (int32_t)hq, scale, out, ws, wsb, status, s));
 }
 
+// (prompt, cache, layer, slots, positions, q, k, v, q_out, q_weight, k_weight, eps, rope_base, dev_status, stream)
+PyObject* prompt_norm_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 15);
+  if (!g.ok) Py_RETURN_NONE;
+  const ptd_prompt* prompt = g.structure<ptd_prompt>();
+  const ptd_kv_cache* cache = g.structure<ptd_kv_cache>();
+  if (g.ok) g.batch_of(a[1], prompt, cache);
+  if (!g.ok) Py_RETURN_NONE;
+  PyObject* dt = cache->dtype == PTD_BF16 ? g_bf16 : g_f32;
+  const int32_t layer = g.num();
+  const int32_t* slots = g.i32_of(prompt->total_tokens);
+  const int32_t* positions = g.i32_of(prompt->total_tokens);
+  int64_t hq = 0, hkv = cache->num_kv_heads, qs, ks, vs, os;
+  const void* q = g.rows3(dt, prompt->total_tokens, cache->head_dim, &hq, &qs);
+  const void* k = g.rows3(dt, prompt->total_tokens, cache->head_dim, &hkv, &ks);
+  const void* v = g.rows3(dt, prompt->total_tokens, cache->head_dim, &hkv, &vs);
+  void* out = g.rows3(dt, prompt->total_tokens, cache->head_dim, &hq, &os);
+  const int64_t want[1] = {cache->head_dim};
+  const void* qw = g.shaped(dt, 1, want);
+  const void* kw = g.shaped(dt, 1, want);
+  const float eps = g.real(), base = g.real();
+  g.on(a[13]);
+  int32_t* status = g.i32();
+  g.on_attr(a[1], s_k);
+  g.on_current();
+  void* s = g.stream();
+  if (!g.ok || hq != (int32_t)hq) Py_RETURN_NONE;
+  PTD_CALL(p_ptd_prompt_norm_rope_append(prompt, cache, layer, slots, positions, q, qs, (int32_t)hq, k, ks, v, vs, qw, kw, eps,
+                                         base, out, os, status, s));
+}
+
+// (tree, cache, layer_begin, q, k, v, q_out, q_weight, k_weight, eps, rope_base, dev_status, positions_out, stream)
+PyObject* tree_norm_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 14);
+  if (!g.ok) Py_RETURN_NONE;
+  const ptd_tree* tree = g.structure<ptd_tree>();
+  const ptd_kv_cache* cache = g.structure<ptd_kv_cache>();
+  if (!g.ok) Py_RETURN_NONE;
+  PyObject* dt = cache->dtype == PTD_BF16 ? g_bf16 : g_f32;
+  const int32_t l0 = g.num();
+  if ((PyObject*)Py_TYPE(a[3]) != g_tensor) Py_RETURN_NONE;
+  int64_t d[4];
+  if (g.dims(a[3], d) != 4) Py_RETURN_NONE;
+  const int64_t q_shape[4] = {d[0], tree->total_nodes, d[2], cache->head_dim};
+  const int64_t kv_shape[4] = {d[0], tree->total_nodes, cache->num_kv_heads, cache->head_dim}, w_shape[2] = {d[0], cache->head_dim};
+  const void* q = g.shaped(dt, 4, q_shape);
+  const void* k = g.shaped(dt, 4, kv_shape);
+  const void* v = g.shaped(dt, 4, kv_shape);
+  void* out = g.shaped(dt, 4, q_shape);
+  const void* qw = g.shaped(dt, 2, w_shape);
+  const void* kw = g.shaped(dt, 2, w_shape);
+  const float eps = g.real(), base = g.real();
+  g.on(a[11]);
+  int32_t* status = g.i32();
+  int32_t* pos = a[12] == Py_None ? (g.next(), nullptr) : g.i32_of(tree->total_nodes);
+  g.on_attr(a[0], s_ctx_lens);
+  g.on_attr(a[1], s_k);
+  g.on_current();
+  void* s = g.stream();
+  if (!g.ok || d[0] != (int32_t)d[0] || d[2] != (int32_t)d[2]) Py_RETURN_NONE;
+  PTD_CALL(p_ptd_tree_norm_rope_append(tree, cache, l0, (int32_t)d[0], q, (int32_t)d[2], k, v, qw, kw, eps, base, out, pos,
+                                       status, s));
+}
+
+// (logits, tokens, out_logprob, out_entropy, out_idx, out_val, dev_status, temperature, stream)
+PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 9);
+  if (!g.ok) Py_RETURN_NONE;
+  PyObject* lg = g.next();
+  const ptd_dtype dt = g.kind(lg);
+  int64_t rows, vocab, stride;
+  const void* logits = g.rows2(lg, dt == PTD_BF16 ? g_bf16 : g_f32, &rows, &vocab, &stride);
+  g.on(lg);
+  if (!g.ok) Py_RETURN_NONE;
+  const Args::Logprobs x = g.logprobs(rows);
+  g.on(a[6]);
+  int32_t* status = g.i32();
+  const float temperature = g.real();
+  g.on_current();
+  void* s = g.stream();
+  if (!g.ok || vocab != (int32_t)vocab) Py_RETURN_NONE;
+  PTD_CALL(p_ptd_token_logprobs(logits, dt, rows, (int32_t)vocab, stride, x.tokens, temperature, x.k, x.logprob, x.entropy, x.idx,
+                                x.val, status, s));
+}
+
+// (hidden, weight, tokens, out_logprob, out_entropy, out_idx, out_val, workspace, dev_status, temperature, stream)
+PyObject* lm_head_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 11);
+  if (!g.ok) Py_RETURN_NONE;
+  int64_t rows, d, hstride, vocab, wd, wstride;
+  const void* hidden = g.rows2(g.next(), g_bf16, &rows, &d, &hstride);
+  if (!g.ok) Py_RETURN_NONE;
+  const void* weight = g.rows2(g.next(), g_bf16, &vocab, &wd, &wstride);
+  g.on(a[0]);
+  g.on(a[1]);
+  if (!g.ok) Py_RETURN_NONE;
+  const Args::Logprobs x = g.logprobs(rows);
+  size_t wsb;
+  if (a[7] == Py_None) Py_RETURN_NONE;
+  g.on(a[7]);
+  void* ws = g.optional(&wsb);
+  g.on(a[8]);
+  int32_t* status = g.i32();
+  const float temperature = g.real();
+  g.on_current();
+  void* s = g.stream();
+  if (!g.ok || d != wd || rows != (int32_t)rows || vocab != (int32_t)vocab || d != (int32_t)d) Py_RETURN_NONE;
+  PTD_CALL(p_ptd_lm_head_logprobs(hidden, (int32_t)rows, hstride, weight, (int32_t)vocab, wstride, (int32_t)d, x.tokens,
+                                  temperature, x.k, x.logprob, x.entropy, x.idx, x.val, ws, wsb, status, s));
+}
+
+// (cache, source, target, parents, lens, workspace, dev_status, stream)
+PyObject* page_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 8);
+  if (!g.ok) Py_RETURN_NONE;
+  const ptd_kv_cache* cache = g.structure<ptd_kv_cache>();
+  const ptd_page_set* from = g.structure<ptd_page_set>();
+  const ptd_page_set* to = g.structure<ptd_page_set>();
+  if (!g.ok) Py_RETURN_NONE;
+  for (int i = 1; i <= 2; ++i) {   // sizes: (entries of a row, pages, device) of the set's tensors
+    PyObject* sizes = PyObject_GetAttr(a[i], s_sizes);
+    if (sizes == nullptr || !PyTuple_CheckExact(sizes) || PyTuple_GET_SIZE(sizes) != 3 ||
+        PyLong_AsLongLong(PyTuple_GET_ITEM(sizes, 0)) != cache->max_pages ||
+        PyLong_AsLongLong(PyTuple_GET_ITEM(sizes, 1)) != cache->num_pages) {
+      g.fail();
+    } else {
+      const int64_t on = PyLong_AsLongLong(PyTuple_GET_ITEM(sizes, 2));
+      if (g.device >= 0 && g.device != on) g.ok = false;
+      g.device = on;
+    }
+    Py_XDECREF(sizes);
+  }
+  const int32_t* parents = g.i32_of(to->batch);
+  const int32_t* lens = g.i32_of(to->batch);
+  size_t wsb;
+  if (a[5] == Py_None) Py_RETURN_NONE;
+  g.on(a[5]);
+  void* ws = g.optional(&wsb);
+  g.on(a[6]);
+  int32_t* status = g.i32();
+  g.on_attr(a[0], s_k);
+  g.on_current();
+  void* s = g.stream();
+  if (!g.ok) Py_RETURN_NONE;
+  PTD_CALL(p_ptd_page_fork(cache, from, to, parents, lens, ws, wsb, status, s));
+}
+
 // load(path of libptd.so, Tensor type, int32, float32, bfloat16, raw stream getter, device getter)
 PyObject* load(PyObject*, PyObject* args) {
   const char* path;
@@ -666,6 +867,11 @@ PyMethodDef methods[] = {PTD_METHOD(tree_attention),
                          PTD_METHOD(prompt_slots),
                          PTD_METHOD(prompt_rope_append),
                          PTD_METHOD(prompt_attention),
+                         PTD_METHOD(prompt_norm_rope_append),
+                         PTD_METHOD(tree_norm_rope_append),
+                         PTD_METHOD(token_logprobs),
+                         PTD_METHOD(lm_head_logprobs),
+                         PTD_METHOD(page_fork),
                          {"load", load, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ptdcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -74,5 +74,44 @@ __device__ __forceinline__ void turn_of(const RopeFreqs& freqs, int pos, int j, 
   c = fmaf(-e, s0, c0);
 }
 
+// The norm of a head that lies across `lanes` lanes (a power of two, whole within its aligned group of lanes), each with
+// two vectors: 1 / sqrt(mean_D(x^2) + eps).  Every lane of the warp takes part; the lanes' sums meet pairwise, so that all
+// have the same.
+template <typename T>
+__device__ __forceinline__ float norm_of_head(const Vec<T>& x, const Vec<T>& y, int lanes, float inv_d, float eps) {
+  float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+  for (int i = 0; i < Vec<T>::N; ++i) s0 = fmaf(x.x[i], x.x[i], s0), s1 = fmaf(y.x[i], y.x[i], s1);
+  float s = s0 + s1;
+  for (int o = lanes >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return __frsqrt_rn(fmaf(s, inv_d, eps));
+}
+template <typename T>
+__device__ __forceinline__ void scale_by(Vec<T>& x, float r, const Vec<T>& w) {
+#pragma unroll
+  for (int i = 0; i < Vec<T>::N; ++i) x.x[i] *= r * w.x[i];
+}
+
+// Norm and rotation of a head's D elements by one warp, element by element (dst may be src: the warp has read the
+// row for the norm before it writes, and a pair before it writes that).
+template <typename T>
+__device__ __forceinline__ void norm_and_turn_row(const T* src, T* dst, const T* w, int D, float eps, const float* cos_s,
+                                                  const float* sin_s) {
+  const int lane = threadIdx.x & 31, half = D / 2;
+  float s = 0.f;
+  for (int i = lane; i < D; i += 32) {
+    const float x = ld(src + i);
+    s = fmaf(x, x, s);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  const float norm = __frsqrt_rn(fmaf(s, 1.f / (float)D, eps));
+  for (int j = lane; j < half; j += 32) {
+    const float a = ld(src + j) * (norm * ld(w + j)), b = ld(src + j + half) * (norm * ld(w + j + half));
+    st(dst + j, a * cos_s[j] - b * sin_s[j]);
+    st(dst + j + half, a * sin_s[j] + b * cos_s[j]);
+  }
+}
+
 }  // namespace rope
 }  // namespace ptd

@@ -1,0 +1,300 @@
+// Log probabilities of given tokens, entropies and the k best alternatives of rows of logits: one read of them.
+//
+// A row is cut into contiguous parts, one CTA each, the parts of a row a cluster.  Every thread keeps the sums of
+// row_sums.cuh over its vectors, against the largest logit that it has seen: a batch of vectors in registers gives a
+// maximum, then the exponentials.  The alternatives are selected as in topk.cu (a threshold from the maxima of 32 groups of
+// lanes, the few elements at or above it read again from L2, each placed by counting the larger ones); the parts' sums and
+// keys go to the shared memory of the cluster's first CTA, which writes the row.
+#include <cooperative_groups.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "launch.cuh"
+#include "ptd_device.cuh"
+#include "row_sums.cuh"
+#include "token_logprobs.cuh"
+#include "topk_parts.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace ptd {
+namespace tl {
+
+using namespace topk;
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMaxParts = 8, kMaxK = 16;
+constexpr int kCand = 256;         // candidate buffer (keys)
+constexpr int kLoads = 4;          // vectors of a thread in flight
+constexpr int kCtas = 5;           // of an SM
+constexpr int kTargetVec = 2048;   // 32 KB: the part that the cluster size aims at
+
+template <typename T, bool kCluster>
+__global__ void __launch_bounds__(kThreads, kCtas) token_logprobs_kernel(const __grid_constant__ TokenLogprobsParams p) {
+  constexpr int VN = Vec<T>::kN;
+  __shared__ __align__(16) uint64_t cand_s[kCand];
+  __shared__ __align__(16) uint64_t all_keys[kMaxParts * kMaxK];   // the parts' keys, in the cluster's first CTA
+  __shared__ RowSums all_sums[kMaxParts];                          // and their sums
+  __shared__ __align__(16) uint32_t group_max_s[32];
+  __shared__ __align__(8) uint64_t parts_bar_s;
+  __shared__ uint64_t round_s[kWarps];
+  __shared__ RowSums warp_sums[kWarps];
+  __shared__ int n_cand_s, abort_s;
+
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = (int)blockIdx.x, parts = (int)gridDim.x;   // the grid's x is one row's parts
+  const int64_t r = (int64_t)blockIdx.z * gridDim.y + blockIdx.y;
+  if (r >= p.rows) return;   // the whole cluster
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, k = p.k;
+  const uint32_t parts_bar = smem_u32(&parts_bar_s);
+  if (tid == 0) {
+    if (kCluster) {
+      mbar_init(parts_bar, (uint32_t)(parts * (k + 1)));   // an arrival per key and one per part's sums (the first CTA's is used)
+      fence_mbar_init();
+    }
+    abort_s = 0;
+    n_cand_s = 0;
+  }
+  if (kCluster && rank == 0 && tid < kMaxParts * kMaxK) all_keys[tid] = 0ull;
+  __syncthreads();
+  if (tid == 0) grid_launch_dependents();
+  if (kCluster) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  grid_dependency_wait();   // the logits and the outputs belong to the stream's previous work
+
+  // this CTA's part: the vector body starts at the row's first 16-byte boundary (head and tail
+  // elements outside it go to the first and last CTA one by one)
+  const T* row = static_cast<const T*>(p.logits) + r * p.row_stride;
+  int a0 = (int)(((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / sizeof(T));
+  if (a0 > p.vocab) a0 = p.vocab;
+  const int nvec = (p.vocab - a0) / VN;
+  const int a1 = a0 + nvec * VN;
+  const int v_begin = min(nvec, rank * p.per), nv = min(nvec, v_begin + p.per) - v_begin;
+  const uint4* vrow = reinterpret_cast<const uint4*>(row + a0) + v_begin;
+  const bool own_head = rank == 0 && tid == 0, own_tail = rank == parts - 1 && tid == kThreads - 1;
+
+  // 1. the sums; lane maxima, then of eight lanes
+  ThreadSums sums;
+  float vmax = -INFINITY;   // of the vectors alone
+  {
+    constexpr uint32_t kNone = VN == 8 ? kBf16x2NegInf : 0xFF800000u;   // -inf
+    const unsigned long long scale2 = f2_pack(p.scale, p.scale);
+#pragma unroll 1
+    for (int v0 = tid; v0 < nv; v0 += kLoads * kThreads) {
+      uint4 x[kLoads];
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        const int v = v0 + u * kThreads;
+        x[u] = v < nv ? __ldg(vrow + v) : make_uint4(kNone, kNone, kNone, kNone);
+      }
+      float m = vec_max<T>(x[0]);
+#pragma unroll
+      for (int u = 1; u < kLoads; ++u) m = fmaxf(m, vec_max<T>(x[u]));
+      vmax = fmaxf(vmax, m);
+      sums.raise(m, p.scale);
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        float f[8];
+        Vec<T>::unpack(x[u], f);
+#pragma unroll
+        for (int e = 0; e < VN; e += 2) sums.add2(f[e], f[e + 1], scale2);
+      }
+    }
+    auto add1 = [&](float f) {
+      sums.raise(f, p.scale);
+      sums.add2(f, -INFINITY, scale2);
+    };
+    if (own_head)
+      for (int i = 0; i < a0; ++i) add1(Vec<T>::scalar(row + i));
+    if (own_tail)
+      for (int i = a1; i < p.vocab; ++i) add1(Vec<T>::scalar(row + i));
+  }
+  {
+    const bool has_elems = tid < nv || (own_head && a0 > 0) || (own_tail && a1 < p.vocab);
+    uint32_t o = has_elems ? ordered_bits(sums.most) : 0u;
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) o = max(o, __shfl_xor_sync(0xffffffffu, o, d));
+    if ((lane & 7) == 0) group_max_s[warp * 4 + (lane >> 3)] = o;
+    const RowSums w = merge_lanes(sums.sums(), 32, p.scale);
+    if (lane == 0) warp_sums[warp] = w;
+  }
+  __syncthreads();
+
+  // 2. the threshold (0: fewer than k groups hold elements, so every element is a candidate)
+  float thr = INFINITY;
+  if (k > 0) {
+    const uint32_t kth = k <= 8 ? kth_largest_ord(group_max_s[lane], k) : kth_of_32(group_max_s, k);
+    thr = kth != 0u ? from_ordered(kth) : -INFINITY;
+  }
+
+  // 3. the candidates
+  auto push = [&](float f, uint32_t idx) {
+    const int at = atomicAdd(&n_cand_s, 1);
+    if (at < kCand) cand_s[at] = make_key(ordered_bits(f), idx);
+  };
+  if (k > 0) {
+    if (own_head)
+      for (int i = 0; i < a0; ++i) {
+        const float f = Vec<T>::scalar(row + i);
+        if (f >= thr) push(f, (uint32_t)i);
+      }
+    if (own_tail)
+      for (int i = a1; i < p.vocab; ++i) {
+        const float f = Vec<T>::scalar(row + i);
+        if (f >= thr) push(f, (uint32_t)i);
+      }
+    if (vmax >= thr) {   // about k lanes of the 256
+#pragma unroll 1
+      for (int v0 = tid; v0 < nv; v0 += kLoads * kThreads) {
+        uint4 x[kLoads];
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) x[u] = __ldg(vrow + min(v0 + u * kThreads, nv - 1));
+        if (*(volatile int*)&n_cand_s > kCand) break;   // the buffer is already lost
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+          const int v = v0 + u * kThreads;
+          if (v < nv && vec_max<T>(x[u]) >= thr) {
+            float f[8];
+            Vec<T>::unpack(x[u], f);
+            const uint32_t i0 = (uint32_t)(a0 + (v_begin + v) * VN);
+#pragma unroll
+            for (int e = 0; e < VN; ++e)
+              if (f[e] >= thr) push(f[e], i0 + e);
+          }
+        }
+      }
+    }
+  }
+  // meanwhile every warp merges the warps' sums (none is written before the next barrier)
+  const RowSums part = merge_lanes(warp_sums[lane & (kWarps - 1)], kWarps, p.scale);
+  __syncthreads();
+  uint64_t* dst_keys = nullptr;
+  uint32_t dst_bar = 0;
+  auto arrive = [&](int count) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(dst_bar), "r"(count) : "memory");
+  };
+  if constexpr (kCluster) {
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");   // the first CTA's keys and barrier are set up
+    dst_keys = cluster.map_shared_rank(all_keys, 0) + rank * kMaxK;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(dst_bar) : "r"(parts_bar));
+    if (tid == 0) {
+      cluster.map_shared_rank(all_sums, 0)[rank] = part;
+      arrive(1);
+    }
+  }
+  const RowResult whole(part);   // of a row in one part
+  auto write_entry = [&](int at, uint64_t key, const RowResult& result) {   // alternative `at` of the row
+    p.top_idx[r * k + at] = (int32_t)(~(uint32_t)(key & 0xFFFFFFFFull));
+    const uint32_t ord = (uint32_t)(key >> 32);
+    p.top_val[r * k + at] = result.logprob(ord != 0u ? from_ordered(ord) : __int_as_float(0x7fffffff), p.inv_temperature);   // 0: NaN
+  };
+  auto write_row = [&](const RowResult& result) {
+    const int token = p.tokens[r];
+    p.logprob[r] = token >= 0 && token < p.vocab ? result.logprob(Vec<T>::scalar(row + token), p.inv_temperature) : -INFINITY;
+    if (p.entropy != nullptr) p.entropy[r] = result.entropy;
+  };
+  if (k > 0) {
+    const int n = n_cand_s;
+    const int n_elems = nv * VN + (rank == 0 ? a0 : 0) + (rank == parts - 1 ? p.vocab - a1 : 0);
+    if (n <= kCand && n >= min(k, n_elems)) {
+      for (int i = tid; i < n; i += kThreads) {
+        const uint64_t key = cand_s[i];
+        int before = 0;
+        for (int j = 0; j < n; ++j) before += cand_s[j] > key ? 1 : 0;
+        if (before < k) {
+          if constexpr (kCluster) {
+            dst_keys[before] = key;
+            arrive(1);
+          } else {
+            write_entry(before, key, whole);
+          }
+        }
+      }
+      if (kCluster && n < k && tid == 0) arrive(k - n);   // fewer elements than k in this part
+    } else {
+      // k rounds over the part (long runs of equal values, or NaN; every thread takes part); 0 is below every number's order
+      uint64_t last = ~0ull;
+      for (int q = 0; q < k; ++q) {
+        uint64_t best = 0ull;
+        auto take = [&](float f, uint32_t idx) {
+          const uint64_t key = make_key(f == f ? ordered_bits(f) : 0u, idx);
+          if (key < last && key > best) best = key;
+        };
+        if (own_head)
+          for (int i = 0; i < a0; ++i) take(Vec<T>::scalar(row + i), (uint32_t)i);
+        if (own_tail)
+          for (int i = a1; i < p.vocab; ++i) take(Vec<T>::scalar(row + i), (uint32_t)i);
+        for (int v = tid; v < nv; v += kThreads) {
+          float f[8];
+          Vec<T>::unpack(__ldg(vrow + v), f);
+#pragma unroll
+          for (int e = 0; e < VN; ++e) take(f[e], (uint32_t)(a0 + (v_begin + v) * VN + e));
+        }
+        best = warp_max_u64(best);
+        if (lane == 0) round_s[warp] = best;
+        __syncthreads();
+        best = round_s[0];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) best = best > round_s[w] ? best : round_s[w];
+        if (tid == 0) {
+          if constexpr (kCluster) {
+            dst_keys[q] = best;
+            arrive(1);
+          } else {
+            write_entry(q, best, whole);
+          }
+        }
+        last = best;
+        __syncthreads();   // round_s is read
+      }
+    }
+  }
+  if constexpr (!kCluster) {
+    if (tid == 0) write_row(whole);
+  } else if (rank == 0 && tid < kMaxParts * kMaxK) {   // four warps
+    mbar_wait_cluster(parts_bar, 0u, &abort_s, p.dev_status);
+    __syncwarp();
+    const int at_part = lane & (kMaxParts - 1);
+    const RowResult result(merge_lanes(at_part < parts ? all_sums[at_part] : RowSums{-INFINITY, 0.f, 0.f}, kMaxParts, p.scale));
+    if (tid == 0) write_row(result);
+    const uint64_t key = all_keys[tid];
+    if (key != 0ull) {
+      int before = 0;
+      for (int c = 0; c < parts; ++c)
+        for (int j = 0; j < k; ++j) before += all_keys[c * kMaxK + j] > key ? 1 : 0;
+      if (before < k) write_entry(before, key, result);
+    }
+  }
+}
+
+// Parts of a row: 32 KB each, at most eight, and for many rows fewer (a power of two) while a part stays under 128 KB and
+// they are more than the CTAs that run at once.
+template <typename T>
+int row_parts(int vocab, int64_t rows, int sms) {
+  const int64_t by_size = ((int64_t)vocab / Vec<T>::kN + kTargetVec) / kTargetVec;
+  const int most = by_size > kMaxParts ? kMaxParts : (int)by_size;
+  const int64_t slots = (int64_t)kCtas * sms, bytes = (int64_t)vocab * (int64_t)sizeof(T);
+  if (rows * most <= slots) return most;
+  int parts = kMaxParts;
+  while (parts > 1 && (parts >= most || rows * parts > slots) && bytes / (parts / 2) <= 128000) parts /= 2;
+  return parts < most ? parts : most;
+}
+
+template <typename T>
+cudaError_t launch(TokenLogprobsParams p, int sms, cudaStream_t stream) {
+  const int parts = row_parts<T>(p.vocab, p.rows, sms);
+  p.per = (p.vocab / Vec<T>::kN + parts - 1) / parts;   // (rows off 16 bytes have one vector fewer)
+  const unsigned gy = (unsigned)(p.rows < 32768 ? p.rows : 32768), gz = (unsigned)((p.rows + gy - 1) / gy);
+  if (parts == 1)
+    return launch_chained(token_logprobs_kernel<T, false>, dim3(1, gy, gz), dim3(kThreads), 0, stream, 0, p);
+  return launch_chained(token_logprobs_kernel<T, true>, dim3((unsigned)parts, gy, gz), dim3(kThreads), 0, stream, (unsigned)parts, p);
+}
+
+}  // namespace tl
+
+cudaError_t launch_token_logprobs(TokenLogprobsParams p, bool bf16, int sms, cudaStream_t stream) {
+  return bf16 ? tl::launch<__nv_bfloat16>(p, sms, stream) : tl::launch<float>(p, sms, stream);
+}
+
+}  // namespace ptd

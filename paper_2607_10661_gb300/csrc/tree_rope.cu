@@ -103,11 +103,12 @@ __device__ __forceinline__ void make_table(const RopeFreqs& freqs, int pos, int 
 // time, and asks for the first kItems before it looks the node up, so that the reads (which
 // depend on no position) overlap the chain tree, parents, slot, angles.
 // kItems = 3 at four CTAs per SM; two at five where that saves a wave (see launch_tree_rope).
-template <typename T, int kItems>
+// kNorm: a head's items lie in neighbouring lanes (chunks is a power of two), which sum its squares.
+template <typename T, int kItems, bool kNorm>
 __global__ void __launch_bounds__(kThreads, kItems == 3 ? 4 : 5)
     tree_rope_kernel(const int32_t* node_offsets, const int32_t* parents, const int32_t* ctx_lens, int batch,
-                     int n_total, int num_layers, int layers_per_cta, int D, int hq, int hkv, T* q, const T* k, const T* v,
-                     T* k_cache, T* v_cache, int layer_begin, int page_size, int seq_capacity, int num_pages,
+                     int n_total, int num_layers, int layers_per_cta, int D, int hq, int hkv, const T* q, T* q_out,
+                     const T* k, const T* v, T* k_cache, T* v_cache, const HeadNorms norms, int layer_begin, int page_size, int seq_capacity, int num_pages,
                      const int32_t* block_table, int max_pages, const __grid_constant__ RopeFreqs freqs,
                      int32_t* positions_out, int32_t* dev_status, GroupDivisor by_layer, GroupDivisor by_chunks) {
   __shared__ int par_s[kThreads];
@@ -144,9 +145,12 @@ __global__ void __launch_bounds__(kThreads, kItems == 3 ? 4 : 5)
         const T* src = src_of(e);
         lo[u] = *reinterpret_cast<const uint4*>(src);   // plain loads: q is also written
         hi[u] = *reinterpret_cast<const uint4*>(src + half);
+      } else if constexpr (kNorm) {
+        lo[u] = hi[u] = make_uint4(0u, 0u, 0u, 0u);
       }
     }
   };
+  const float inv_d = 1.f / (float)D;
   load_items(t);
   Place at;
   if (!find_place(node_offsets, parents, ctx_lens, batch, n, page_size, seq_capacity, num_pages, block_table, max_pages,
@@ -160,12 +164,19 @@ __global__ void __launch_bounds__(kThreads, kItems == 3 ? 4 : 5)
 #pragma unroll
     for (int u = 0; u < kItems; ++u) {
       const int e = e0 + u * kThreads;
+      uint4 a = lo[u], b = hi[u];
+      float norm = 1.f;
+      if constexpr (kNorm) norm = norm_of_head(unpack16<T>(a), unpack16<T>(b), chunks, inv_d, norms.eps);   // every lane
       if (e >= items) continue;
       int lq, h, j;
       place_of(e, lq, h, j);
-      uint4 a = lo[u], b = hi[u];
       if (h < hq + hkv) {
-        const Vec<T> x = unpack16<T>(a), y = unpack16<T>(b);
+        Vec<T> x = unpack16<T>(a), y = unpack16<T>(b);
+        if constexpr (kNorm) {
+          const T* w = static_cast<const T*>(h < hq ? norms.q_weight : norms.k_weight) + (size_t)(l0 + lq) * D + j;
+          scale_by(x, norm, unpack16<T>(__ldg(reinterpret_cast<const uint4*>(w))));
+          scale_by(y, norm, unpack16<T>(__ldg(reinterpret_cast<const uint4*>(w + half))));
+        }
         Vec<T> rx, ry;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -178,7 +189,7 @@ __global__ void __launch_bounds__(kThreads, kItems == 3 ? 4 : 5)
       }
       T* dst;
       if (h < hq) {
-        dst = q + (((size_t)(l0 + lq) * n_total + n) * hq + h) * D + j;
+        dst = q_out + (((size_t)(l0 + lq) * n_total + n) * hq + h) * D + j;
       } else {
         const size_t crow = (size_t)(layer_begin + l0 + lq) * layer_rows + at.row;
         dst = h < hq + hkv ? k_cache + (crow * hkv + (h - hq)) * D + j : v_cache + (crow * hkv + (h - hq - hkv)) * D + j;
@@ -191,12 +202,13 @@ __global__ void __launch_bounds__(kThreads, kItems == 3 ? 4 : 5)
   }
 }
 
-// Rows that are not 16-byte vectors: one element at a time, one CTA per (node, layer).
-template <typename T>
+// Rows that are not 16-byte vectors (or heads that a norm cannot take from a warp's lanes): one element at a time, one
+// CTA per (node, layer).
+template <typename T, bool kNorm>
 __global__ void __launch_bounds__(kThreads)
     tree_rope_scalar_kernel(const int32_t* node_offsets, const int32_t* parents, const int32_t* ctx_lens, int batch,
-                            int n_total, int D, int hq, int hkv, T* q, const T* k, const T* v, T* k_cache, T* v_cache,
-                            int layer_begin, int page_size, int seq_capacity, int num_pages, const int32_t* block_table,
+                            int n_total, int D, int hq, int hkv, const T* q, T* q_out, const T* k, const T* v, T* k_cache,
+                            T* v_cache, const HeadNorms norms, int layer_begin, int page_size, int seq_capacity, int num_pages, const int32_t* block_table,
                             int max_pages, const __grid_constant__ RopeFreqs freqs, int32_t* positions_out,
                             int32_t* dev_status) {
   __shared__ int par_s[kThreads];
@@ -213,45 +225,57 @@ __global__ void __launch_bounds__(kThreads)
   make_table(freqs, at.pos, half, cos_s, sin_s);
   __syncthreads();
   const size_t layer_rows = page_size > 0 ? (size_t)num_pages * page_size : (size_t)batch * seq_capacity;
-  T* qn = q + ((size_t)lq * n_total + n) * hq * D;
+  const T* qn = q + ((size_t)lq * n_total + n) * hq * D;
+  T* qo = q_out + ((size_t)lq * n_total + n) * hq * D;
   const T* kn = k + ((size_t)lq * n_total + n) * hkv * D;
   const T* vn = v + ((size_t)lq * n_total + n) * hkv * D;
   const size_t crow = ((size_t)(layer_begin + lq) * layer_rows + at.row) * hkv * D;
-  for (int e = t; e < (hq + hkv) * half; e += kThreads) {
-    const bool isq = e < hq * half;
-    const int e2 = isq ? e : e - hq * half;
-    const int h = e2 / half, j = e2 - h * half;
-    const T* src = (isq ? (const T*)qn : kn) + (size_t)h * D;
-    T* dst = isq ? qn + (size_t)h * D : k_cache + crow + (size_t)h * D;
-    const float a = ld(src + j), bb = ld(src + j + half);
-    const float c = cos_s[j], s = sin_s[j];
-    st(dst + j, a * c - bb * s);
-    st(dst + j + half, a * s + bb * c);
+  if constexpr (kNorm) {   // a warp per head
+    for (int h = t >> 5; h < hq + hkv; h += kThreads / 32) {
+      const bool isq = h < hq;
+      const T* src = isq ? qn + (size_t)h * D : kn + (size_t)(h - hq) * D;
+      T* dst = isq ? qo + (size_t)h * D : k_cache + crow + (size_t)(h - hq) * D;
+      norm_and_turn_row(src, dst, static_cast<const T*>(isq ? norms.q_weight : norms.k_weight) + (size_t)lq * D, D, norms.eps,
+                        cos_s, sin_s);
+    }
+  } else {
+    for (int e = t; e < (hq + hkv) * half; e += kThreads) {
+      const bool isq = e < hq * half;
+      const int e2 = isq ? e : e - hq * half;
+      const int h = e2 / half, j = e2 - h * half;
+      const T* src = (isq ? qn : kn) + (size_t)h * D;
+      T* dst = isq ? qo + (size_t)h * D : k_cache + crow + (size_t)h * D;
+      const float a = ld(src + j), bb = ld(src + j + half);
+      const float c = cos_s[j], s = sin_s[j];
+      st(dst + j, a * c - bb * s);
+      st(dst + j + half, a * s + bb * c);
+    }
   }
   for (int e = t; e < hkv * D; e += kThreads) v_cache[crow + e] = vn[e];
 }
 
-}  // namespace tr
-
-cudaError_t launch_tree_rope(const int32_t* node_offsets, const int32_t* parents, const int32_t* ctx_lens,
-                             int batch, int n_total, bool bf16, int head_dim, int hq, int hkv, void* q, const void* k,
-                             const void* v, void* k_cache, void* v_cache, int layer_begin, int num_layers,
-                             int page_size, int seq_capacity, int num_pages, const int32_t* block_table, int max_pages,
-                             const RopeFreqs& freqs, int32_t* positions_out, int32_t* dev_status, int sms,
-                             cudaStream_t stream) {
+template <typename T, bool kNorm>
+cudaError_t launch_typed(const int32_t* node_offsets, const int32_t* parents, const int32_t* ctx_lens, int batch, int n_total,
+                         int head_dim, int hq, int hkv, const T* q, T* q_out, const T* k, const T* v, T* k_cache, T* v_cache,
+                         const HeadNorms& norms, int layer_begin, int num_layers, int page_size, int seq_capacity,
+                         int num_pages, const int32_t* block_table, int max_pages, const RopeFreqs& freqs,
+                         int32_t* positions_out, int32_t* dev_status, int sms, cudaStream_t stream) {
   const auto al16 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; };
-  const bool aligned = al16(q) && al16(k) && al16(v) && al16(k_cache) && al16(v_cache);
-  const int vec = bf16 ? 8 : 4;
+  const bool aligned = al16(q) && al16(q_out) && al16(k) && al16(v) && al16(k_cache) && al16(v_cache) &&
+                       al16(norms.q_weight) && al16(norms.k_weight);
+  constexpr int vec = 16 / (int)sizeof(T);
+  const int chunks = head_dim / 2 / vec;
+  const bool lanes = !kNorm || (chunks & (chunks - 1)) == 0;   // (at most 32: D <= 256)
   // (2^26 items a layer: the bound of the kernel's quotients)
-  if (aligned && (head_dim / 2) % vec == 0 && ((int64_t)hq + 2 * (int64_t)hkv) * (head_dim / 2 / vec) < (1 << 26)) {
+  if (aligned && (head_dim / 2) % vec == 0 && lanes && ((int64_t)hq + 2 * (int64_t)hkv) * chunks < (1 << 26)) {
     // As many layers a CTA as fill three items of its threads; twice that over more than two waves of CTAs
     // (few heads' remainders, and half the look-ups: 32 layers of 128 nodes, 64 / 8 heads, bf16 31.1 -> 26.9
     // us, 8 layers of ~345 nodes 19.3 -> 17.3).  A grid just above one wave of four CTAs per SM runs with
     // five (~650 nodes, one layer, 32 / 8 heads 6.1 -> 4.7 us, 64 / 8 heads 7.2 -> 6.5); with five everywhere
     // the others lose 5 % (geometric mean over 249 sizes).
-    const int chunks = head_dim / 2 / vec, per_layer = (hq + 2 * hkv) * chunks;
+    const int per_layer = (hq + 2 * hkv) * chunks;
     auto layers_of = [&](int items) {
-      const int l = items * tr::kThreads / per_layer;
+      const int l = items * kThreads / per_layer;
       return l < 1 ? 1 : (l > num_layers ? num_layers : l);
     };
     auto ctas_of = [&](int l) { return (int64_t)n_total * ((num_layers + l - 1) / l); };
@@ -261,29 +285,37 @@ cudaError_t launch_tree_rope(const int32_t* node_offsets, const int32_t* parents
     if (five) layers = layers_of(2);
     if (ctas > 2 * slots) layers = layers_of(6);
     const dim3 grid(n_total, (num_layers + layers - 1) / layers);
-#define PTD_ROPE_LAUNCH(T, ITEMS)                                                                                   \
-  return launch_chained(tr::tree_rope_kernel<T, ITEMS>, grid, dim3(tr::kThreads), 0, stream, 0, node_offsets, parents,     \
-                        ctx_lens, batch, n_total, num_layers, layers, head_dim, hq, hkv, static_cast<T*>(q),        \
-                        static_cast<const T*>(k), static_cast<const T*>(v), static_cast<T*>(k_cache),               \
-                        static_cast<T*>(v_cache), layer_begin, page_size, seq_capacity, num_pages, block_table,     \
-                        max_pages, freqs, positions_out, dev_status, group_divisor(per_layer), group_divisor(chunks))
-    if (bf16) {
-      if (five) PTD_ROPE_LAUNCH(__nv_bfloat16, 2);
-      PTD_ROPE_LAUNCH(__nv_bfloat16, 3);
-    }
-    if (five) PTD_ROPE_LAUNCH(float, 2);
-    PTD_ROPE_LAUNCH(float, 3);
-#undef PTD_ROPE_LAUNCH
+    return launch_chained(five ? tree_rope_kernel<T, 2, kNorm> : tree_rope_kernel<T, 3, kNorm>, grid, dim3(kThreads), 0, stream, 0,
+                          node_offsets, parents, ctx_lens, batch, n_total, num_layers, layers, head_dim, hq, hkv, q, q_out, k,
+                          v, k_cache, v_cache, norms, layer_begin, page_size, seq_capacity, num_pages, block_table, max_pages,
+                          freqs, positions_out, dev_status, group_divisor(per_layer), group_divisor(chunks));
   }
-  const dim3 grid(n_total, num_layers);
-#define PTD_ROPE_LAUNCH(T)                                                                                          \
-  return launch_chained(tr::tree_rope_scalar_kernel<T>, grid, dim3(tr::kThreads), 0, stream, 0, node_offsets,       \
-                        parents, ctx_lens, batch, n_total, head_dim, hq, hkv, static_cast<T*>(q),                   \
-                        static_cast<const T*>(k), static_cast<const T*>(v), static_cast<T*>(k_cache),               \
-                        static_cast<T*>(v_cache), layer_begin, page_size, seq_capacity, num_pages, block_table,     \
-                        max_pages, freqs, positions_out, dev_status)
-  if (bf16) PTD_ROPE_LAUNCH(__nv_bfloat16);
-  PTD_ROPE_LAUNCH(float);
+  return launch_chained(tree_rope_scalar_kernel<T, kNorm>, dim3(n_total, num_layers), dim3(kThreads), 0, stream, 0, node_offsets,
+                        parents, ctx_lens, batch, n_total, head_dim, hq, hkv, q, q_out, k, v, k_cache, v_cache, norms,
+                        layer_begin, page_size, seq_capacity, num_pages, block_table, max_pages, freqs, positions_out,
+                        dev_status);
+}
+
+}  // namespace tr
+
+cudaError_t launch_tree_rope(const int32_t* node_offsets, const int32_t* parents, const int32_t* ctx_lens,
+                             int batch, int n_total, bool bf16, int head_dim, int hq, int hkv, const void* q, void* q_out,
+                             const void* k, const void* v, const HeadNorms& norms, void* k_cache, void* v_cache,
+                             int layer_begin, int num_layers, int page_size, int seq_capacity, int num_pages,
+                             const int32_t* block_table, int max_pages, const RopeFreqs& freqs, int32_t* positions_out,
+                             int32_t* dev_status, int sms, cudaStream_t stream) {
+#define PTD_ROPE_LAUNCH(T, NORM)                                                                                       \
+  return tr::launch_typed<T, NORM>(node_offsets, parents, ctx_lens, batch, n_total, head_dim, hq, hkv,                 \
+                                   static_cast<const T*>(q), static_cast<T*>(q_out), static_cast<const T*>(k),         \
+                                   static_cast<const T*>(v), static_cast<T*>(k_cache), static_cast<T*>(v_cache), norms, \
+                                   layer_begin, num_layers, page_size, seq_capacity, num_pages, block_table, max_pages, \
+                                   freqs, positions_out, dev_status, sms, stream)
+  if (norms.q_weight != nullptr) {
+    if (bf16) PTD_ROPE_LAUNCH(__nv_bfloat16, true);
+    PTD_ROPE_LAUNCH(float, true);
+  }
+  if (bf16) PTD_ROPE_LAUNCH(__nv_bfloat16, false);
+  PTD_ROPE_LAUNCH(float, false);
 #undef PTD_ROPE_LAUNCH
 }
 

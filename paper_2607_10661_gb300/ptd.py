@@ -37,7 +37,8 @@ EXPORTED = (
     "ptd_pipeline_submit", "ptd_pipeline_wait", "ptd_pipeline_destroy", "ptd_check_bounded_wait",
     "ptd_step_workspace_size", "ptd_step_topk_policy", "ptd_step_tail", "ptd_attention_plan",
     "ptd_tree_attention_as", "ptd_prompt_slots", "ptd_prompt_rope_append", "ptd_prompt_attention_workspace_size",
-    "ptd_prompt_attention",
+    "ptd_prompt_attention", "ptd_tree_norm_rope_append", "ptd_prompt_norm_rope_append", "ptd_token_logprobs",
+    "ptd_lm_head_logprobs_workspace_size", "ptd_lm_head_logprobs", "ptd_page_fork_workspace_size", "ptd_page_fork",
 )
 ATTN_AUTO, ATTN_UNIT, ATTN_CUT, ATTN_CLUSTER, ATTN_F32_CORES, ATTN_F32_TENSOR = range(6)
 
@@ -79,6 +80,11 @@ class _Prompt(ctypes.Structure):
 class _PagePool(ctypes.Structure):
     _fields_ = [("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p), ("held", ctypes.c_void_p),
                 ("new_held", ctypes.c_void_p), ("new_free_count", ctypes.c_void_p), ("block_table", ctypes.c_void_p)]
+
+
+class _PageSet(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("block_table", ctypes.c_void_p), ("held", ctypes.c_void_p),
+                ("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p)]
 
 
 class _HostIO(ctypes.Structure):
@@ -170,6 +176,21 @@ def lib() -> ctypes.CDLL:
         L.ptd_prompt_attention_workspace_size.argtypes = [P(_Prompt), P(_Cache), i32]
         L.ptd_prompt_attention.restype = ctypes.c_int
         L.ptd_prompt_attention.argtypes = [P(_Prompt), P(_Cache), i32, vp, i64, i32, f32, vp, vp, sz, vp, vp]
+        L.ptd_tree_norm_rope_append.restype = ctypes.c_int
+        L.ptd_tree_norm_rope_append.argtypes = [P(_Tree), P(_Cache), i32, i32, vp, i32, vp, vp, vp, vp, f32, f32, vp, vp, vp, vp]
+        L.ptd_prompt_norm_rope_append.restype = ctypes.c_int
+        L.ptd_prompt_norm_rope_append.argtypes = [P(_Prompt), P(_Cache), i32, vp, vp, vp, i64, i32, vp, i64, vp, i64, vp, vp,
+                                                  f32, f32, vp, i64, vp, vp]
+        L.ptd_token_logprobs.restype = ctypes.c_int
+        L.ptd_token_logprobs.argtypes = [vp, ctypes.c_int, i64, i32, i64, vp, f32, i32, vp, vp, vp, vp, vp, vp]
+        L.ptd_lm_head_logprobs_workspace_size.restype = sz
+        L.ptd_lm_head_logprobs_workspace_size.argtypes = [i32, i32, i32]
+        L.ptd_lm_head_logprobs.restype = ctypes.c_int
+        L.ptd_lm_head_logprobs.argtypes = [vp, i32, i64, vp, i32, i64, i32, vp, f32, i32, vp, vp, vp, vp, vp, sz, vp, vp]
+        L.ptd_page_fork_workspace_size.restype = sz
+        L.ptd_page_fork_workspace_size.argtypes = [P(_Cache), P(_PageSet), P(_PageSet)]
+        L.ptd_page_fork.restype = ctypes.c_int
+        L.ptd_page_fork.argtypes = [P(_Cache), P(_PageSet), P(_PageSet), vp, vp, vp, sz, vp, vp]
         _lib = L
     return _lib
 
@@ -741,6 +762,68 @@ def prompt_rope_append(prompt: Prompt, cache: KVCache, layer: int, slots: torch.
     return last_launch_count()
 
 
+def prompt_norm_rope_append(prompt: Prompt, cache: KVCache, layer: int, slots: torch.Tensor, positions: torch.Tensor,
+                            q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_out: torch.Tensor, q_weight: torch.Tensor,
+                            k_weight: torch.Tensor, eps: float, rope_base: float, dev_status: torch.Tensor,
+                            stream=None) -> int:
+    """ptd_prompt_norm_rope_append: as prompt_rope_append, the heads normalised first; q_weight, k_weight [D]."""
+    r = (_calls or _native()).prompt_norm_rope_append(prompt, cache, layer, slots, positions, q, k, v, q_out, q_weight, k_weight,
+                                                      eps, rope_base, dev_status, stream if stream is None else _stream(stream))
+    if r is not None:
+        return _launched(r, "ptd_prompt_norm_rope_append")
+    _batch_of_cache(prompt, cache)
+    n, d, dt = prompt.total_tokens, cache.head_dim, cache.k.dtype
+    qp, qs, hq = _rows3(q, "q", dt, n, None, d)
+    kp, ks, _ = _rows3(k, "k", dt, n, cache.num_kv_heads, d)
+    vp, vs, _ = _rows3(v, "v", dt, n, cache.num_kv_heads, d)
+    op, os_, _ = _rows3(q_out, "q_out", dt, n, hq, d)
+    if slots.numel() != n or positions.numel() != n:
+        raise ValueError(f"slots and positions need total_tokens = {n} entries")
+    wq, wk = _shaped(q_weight, "q_weight", dt, (d,)), _shaped(k_weight, "k_weight", dt, (d,))
+    with _one_device(q, k, v, q_out, q_weight, k_weight, slots, positions, dev_status, cache.k):
+        st = lib().ptd_prompt_norm_rope_append(
+            ctypes.byref(prompt.c), ctypes.byref(cache.c), int(layer), _dev(slots, "slots", torch.int32),
+            _dev(positions, "positions", torch.int32), qp, qs, hq, kp, ks, vp, vs, wq, wk, float(eps), float(rope_base), op, os_,
+            _dev(dev_status, "dev_status", torch.int32), _stream(stream))
+    _check(st, "ptd_prompt_norm_rope_append")
+    return last_launch_count()
+
+
+def _shaped(t: torch.Tensor, name: str, dtype, shape) -> int:
+    """Device pointer of a contiguous tensor of this shape."""
+    p = _dev(t, name, dtype)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    return p
+
+
+def tree_norm_rope_append(tree: Tree, cache: KVCache, layer_begin: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                          q_out: torch.Tensor, q_weight: torch.Tensor, k_weight: torch.Tensor, eps: float, rope_base: float,
+                          dev_status: torch.Tensor, positions_out: Optional[torch.Tensor] = None, stream=None) -> int:
+    """ptd_tree_norm_rope_append: q, q_out [L, N_tot, Hq, D] (q_out may be q), k, v [L, N_tot, Hkv, D] into cache layers
+    layer_begin .. layer_begin + L - 1; q_weight, k_weight [L, D]."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise ValueError("q must be [layers, nodes, heads, head_dim]")
+    n_layers, n, hq, d, dt = q.shape[0], tree.total_nodes, q.shape[2], cache.head_dim, cache.k.dtype
+    if tree.batch != cache.sequences:
+        _trees_of_cache(tree, cache, layer_begin + n_layers - 1)
+    r = (_calls or _native()).tree_norm_rope_append(tree, cache, layer_begin, q, k, v, q_out, q_weight, k_weight, eps, rope_base,
+                                                    dev_status, positions_out, stream if stream is None else _stream(stream))
+    if r is not None:
+        return _launched(r, "ptd_tree_norm_rope_append")
+    heads, kv = (n_layers, n, hq, d), (n_layers, n, cache.num_kv_heads, d)
+    args = [_shaped(q, "q", dt, heads), hq, _shaped(k, "k", dt, kv), _shaped(v, "v", dt, kv),
+            _shaped(q_weight, "q_weight", dt, (n_layers, d)), _shaped(k_weight, "k_weight", dt, (n_layers, d)), float(eps),
+            float(rope_base), _shaped(q_out, "q_out", dt, heads),
+            None if positions_out is None else _shaped(positions_out, "positions_out", torch.int32, (n,)),
+            _dev(dev_status, "dev_status", torch.int32)]
+    with _one_device(q, k, v, q_out, q_weight, k_weight, positions_out, dev_status, tree.ctx_lens, cache.k):
+        st = lib().ptd_tree_norm_rope_append(ctypes.byref(tree.c), ctypes.byref(cache.c), int(layer_begin), n_layers, *args,
+                                             _stream(stream))
+    _check(st, "ptd_tree_norm_rope_append")
+    return last_launch_count()
+
+
 def prompt_attention_workspace_size(prompt: Prompt, cache: KVCache, num_q_heads: int) -> int:
     with _one_device(prompt.ctx_lens, cache.k):   # the device that the attention will run on
         return int(lib().ptd_prompt_attention_workspace_size(ctypes.byref(prompt.c), ctypes.byref(cache.c), int(num_q_heads)))
@@ -788,6 +871,113 @@ def lm_head_topk(hidden: torch.Tensor, weight: torch.Tensor, k: int, out_idx: to
                                 _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(),
                                 _dev(dev_status, "dev_status", torch.int32), _stream(stream))
     _check(st, "ptd_lm_head_topk")
+    return last_launch_count()
+
+
+def _logprob_outputs(rows: int, tokens, out_logprob, out_entropy, out_idx, out_val):
+    """k, and the pointers of a log probability call's tokens and outputs (entropy, and the alternatives together, may be None)."""
+    if (out_idx is None) != (out_val is None):
+        raise ValueError("out_idx and out_val are given together, or neither is")
+    k = 0
+    if out_idx is not None:
+        if out_idx.dim() != 2 or tuple(out_idx.shape) != tuple(out_val.shape):
+            raise ValueError("out_idx and out_val must be [rows, k]")
+        k = out_idx.shape[1]
+    return k, [_shaped(tokens, "tokens", torch.int32, (rows,)), _shaped(out_logprob, "out_logprob", torch.float32, (rows,)),
+               None if out_entropy is None else _shaped(out_entropy, "out_entropy", torch.float32, (rows,)),
+               None if out_idx is None else _shaped(out_idx, "out_idx", torch.int32, (rows, k)),
+               None if out_idx is None else _shaped(out_val, "out_val", torch.float32, (rows, k))]
+
+
+def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, out_logprob: torch.Tensor,
+                   out_entropy: Optional[torch.Tensor], out_idx: Optional[torch.Tensor], out_val: Optional[torch.Tensor],
+                   dev_status: torch.Tensor, temperature: float = 1.0, stream=None) -> int:
+    """ptd_token_logprobs: logits [rows, vocab] (bf16 or fp32, rows may be apart), tokens [rows] int32; out_logprob, out_entropy
+    [rows], out_val [rows, k] fp32, out_idx [rows, k] int32."""
+    r = (_calls or _native()).token_logprobs(logits, tokens, out_logprob, out_entropy, out_idx, out_val, dev_status, temperature,
+                                             stream if stream is None else _stream(stream))
+    if r is not None:
+        return _launched(r, "ptd_token_logprobs")
+    lp = _dev(logits, "logits", row_strided=True)
+    rows, vocab = logits.shape
+    k, (tk, pl, pe, pi, pv) = _logprob_outputs(rows, tokens, out_logprob, out_entropy, out_idx, out_val)
+    with _one_device(logits, tokens, out_logprob, out_entropy, out_idx, out_val, dev_status):
+        st = lib().ptd_token_logprobs(lp, _ptd_dtype(logits.dtype), rows, vocab, logits.stride(0), tk, float(temperature), k, pl, pe,
+                                      pi, pv, _dev(dev_status, "dev_status", torch.int32), _stream(stream))
+    _check(st, "ptd_token_logprobs")
+    return last_launch_count()
+
+
+def lm_head_logprobs_workspace_size(rows: int, vocab: int, k: int) -> int:
+    return int(lib().ptd_lm_head_logprobs_workspace_size(int(rows), int(vocab), int(k)))
+
+
+def lm_head_logprobs(hidden: torch.Tensor, weight: torch.Tensor, tokens: torch.Tensor, out_logprob: torch.Tensor,
+                     out_entropy: Optional[torch.Tensor], out_idx: Optional[torch.Tensor], out_val: Optional[torch.Tensor],
+                     workspace: torch.Tensor, dev_status: torch.Tensor, temperature: float = 1.0, stream=None) -> int:
+    """ptd_lm_head_logprobs: hidden [rows, d] and weight [vocab, d] bf16 (rows may be apart); the rest as token_logprobs."""
+    r = (_calls or _native()).lm_head_logprobs(hidden, weight, tokens, out_logprob, out_entropy, out_idx, out_val, workspace,
+                                               dev_status, temperature, stream if stream is None else _stream(stream))
+    if r is not None:
+        return _launched(r, "ptd_lm_head_logprobs")
+    hp = _dev(hidden, "hidden", torch.bfloat16, row_strided=True)
+    wp = _dev(weight, "weight", torch.bfloat16, row_strided=True)
+    if hidden.shape[1] != weight.shape[1]:
+        raise ValueError("hidden [rows, d] and weight [vocab, d] must share d")
+    rows, d = hidden.shape
+    k, (tk, pl, pe, pi, pv) = _logprob_outputs(rows, tokens, out_logprob, out_entropy, out_idx, out_val)
+    with _one_device(hidden, weight, tokens, out_logprob, out_entropy, out_idx, out_val, workspace, dev_status):
+        st = lib().ptd_lm_head_logprobs(hp, rows, hidden.stride(0), wp, weight.shape[0], weight.stride(0), d, tk, float(temperature),
+                                        k, pl, pe, pi, pv, _dev(workspace, "workspace"),
+                                        workspace.numel() * workspace.element_size(),
+                                        _dev(dev_status, "dev_status", torch.int32), _stream(stream))
+    _check(st, "ptd_lm_head_logprobs")
+    return last_launch_count()
+
+
+class PageSet:
+    """What a batch's sequences hold of a paged cache and its free pages: block_table [B, max_pages], held [B], free_pages
+    [num_pages], free_count [1], int32."""
+
+    def __init__(self, block_table: torch.Tensor, held: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor):
+        if block_table.dim() != 2 or held.numel() != block_table.shape[0]:
+            raise ValueError("block_table must be [sequences, pages], held needs an entry per sequence")
+        self.block_table, self.held, self.free_pages, self.free_count = block_table, held, free_pages, free_count
+        self.batch = held.numel()
+        self.c = _PageSet(self.batch, *(_dev(t, n, torch.int32) for t, n in (
+            (block_table, "block_table"), (held, "held"), (free_pages, "free_pages"), (free_count, "free_count"))))
+        with _one_device(block_table, held, free_pages, free_count):
+            self.sizes = (block_table.shape[1], free_pages.numel(), held.get_device())
+
+
+def _sets_of_cache(cache: KVCache, *sets: PageSet) -> None:
+    for s in sets:
+        if not cache.page_size or s.sizes[0] != cache.c.max_pages or s.sizes[1] != cache.c.num_pages:
+            raise ValueError(f"a page set of {s.sizes[0]} entries a row and {s.sizes[1]} pages, "
+                             f"the cache has {cache.c.max_pages} and {cache.c.num_pages}")
+
+
+def page_fork_workspace_size(cache: KVCache, source: PageSet, target: PageSet) -> int:
+    _sets_of_cache(cache, source, target)
+    return int(lib().ptd_page_fork_workspace_size(ctypes.byref(cache.c), ctypes.byref(source.c), ctypes.byref(target.c)))
+
+
+def page_fork(cache: KVCache, source: PageSet, target: PageSet, parents: torch.Tensor, lens: torch.Tensor,
+              workspace: torch.Tensor, dev_status: torch.Tensor, stream=None) -> int:
+    """ptd_page_fork: target sequence b goes on from the first lens[b] positions of source sequence parents[b]
+    (-1: empty); parents, lens [target.batch] int32."""
+    r = (_calls or _native()).page_fork(cache, source, target, parents, lens, workspace, dev_status,
+                                        stream if stream is None else _stream(stream))
+    if r is not None:
+        return _launched(r, "ptd_page_fork")
+    _sets_of_cache(cache, source, target)
+    with _one_device(cache.k, source.held, target.held, parents, lens, workspace, dev_status):
+        st = lib().ptd_page_fork(ctypes.byref(cache.c), ctypes.byref(source.c), ctypes.byref(target.c),
+                                 _shaped(parents, "parents", torch.int32, (target.batch,)),
+                                 _shaped(lens, "lens", torch.int32, (target.batch,)), _dev(workspace, "workspace"),
+                                 workspace.numel() * workspace.element_size(), _dev(dev_status, "dev_status", torch.int32),
+                                 _stream(stream))
+    _check(st, "ptd_page_fork")
     return last_launch_count()
 
 
