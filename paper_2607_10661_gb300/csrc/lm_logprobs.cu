@@ -218,8 +218,10 @@ __global__ void __launch_bounds__(kThreads, 1)
               m[q] = fmax3(m[q], __uint_as_float(v[e + 2 * q]), __uint_as_float(v[e + 2 * q + 1]));
           const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
           sums.raise(most, p.scale);
+          float x[32];
 #pragma unroll
-          for (int e = 0; e < 32; e += 2) sums.add2(__uint_as_float(v[e]), __uint_as_float(v[e + 1]), scale2);
+          for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
+          sums.add(x, scale2);
           if ((unsigned)(token - tb) < 32u) {
 #pragma unroll
             for (int e = 0; e < 32; ++e)
@@ -280,7 +282,7 @@ __global__ void __launch_bounds__(kMergeThreads) lm_logprobs_merge_kernel(const 
 #pragma unroll
     for (int j = 0; j < KM; ++j) insert(top, list[j]);
   }
-  const RowResult result(merge_lanes(sums, 32, p.scale));
+  const RowResult result(merge_lanes<32>(sums, p.scale));
   if (lane == 0) {
     const int token = p.tokens[row];
     p.logprob[row] = token >= 0 && token < p.vocab ? result.logprob(parts.token_logit[row], p.inv_temperature) : -INFINITY;

@@ -9,8 +9,10 @@
 // free[f - T + r] of the new stack: everything is a function of u, of each page's first holder and of two sums, and the
 // result does not depend on the order in which threads run (minima alone are made by atomics).
 //
-// One cluster plans (u and the holders; counts of each row; sums, the new tables and stack, the list of copies), with three
-// cluster barriers between these; then a grid copies rows, all layers of K and V, in chunks.
+// The plan has four parts: the sizes; u and the holders; the counts of each row; sums, the new tables and stack, the list of
+// copies.  Its latency is what it costs (each part a few dependent reads): one CTA does it with u and the holders in its shared
+// memory where they fit and the rows are few enough, else a cluster of eight with both in the scratch and a cluster barrier
+// between the parts.  Then a grid copies rows, all layers of K and V, in chunks.
 #include <cuda_runtime.h>
 
 #include <climits>
@@ -32,27 +34,23 @@ constexpr int kChunk = kCopyThreads * kCopyLoads * 16;   // bytes of one CTA's t
 struct Scratch {
   int32_t* bad;       // [1] a page number out of range
   int32_t* copies;    // [1]
+  int32_t* copy;      // [to_batch][3] from page, to page, rows
+  int32_t* gives;     // the cluster's: [from_batch] pages given back
+  int32_t* takes;     // [to_batch] 0 or 1
   int32_t* first;     // [num_pages] lowest source row that holds the page
   int32_t* user;      // [num_pages] u
-  int32_t* gives;     // [from_batch] pages given back
-  int32_t* takes;     // [to_batch] 0 or 1
-  int32_t* copy;      // [to_batch][3] from page, to page, rows
   __host__ __device__ Scratch(int32_t* at, int num_pages, int from_batch, int to_batch)
-      : bad(at), copies(at + 1), first(at + 4), user(first + num_pages), gives(user + num_pages), takes(gives + from_batch),
-        copy(takes + to_batch) {}
+      : bad(at), copies(at + 1), copy(at + 4), gives(copy + 3 * (size_t)to_batch), takes(gives + from_batch),
+        first(takes + to_batch), user(first + num_pages) {}
 };
 
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
-// Exclusive sums of in[0 .. n) (written by other CTAs) into out, by the whole CTA; the total to every thread.
-__device__ __forceinline__ int exclusive_sums(const int32_t* in, int n, int* out, int* warp_s) {
+// Exclusive sums of in[0 .. n) into out (may be the same), by the whole CTA; the total to every thread.
+template <typename Load>
+__device__ __forceinline__ int exclusive_sums(Load in, int n, int* out, int* warp_s) {
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int per = (n + kThreads - 1) / kThreads, i0 = min(n, t * per), i1 = min(n, i0 + per);
   int sum = 0;
-  for (int i = i0; i < i1; ++i) sum += __ldcg(in + i);
+  for (int i = i0; i < i1; ++i) sum += in(i);
   int incl = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -61,106 +59,151 @@ __device__ __forceinline__ int exclusive_sums(const int32_t* in, int n, int* out
   }
   if (lane == 31) warp_s[warp] = incl;
   __syncthreads();
-  int before = 0, total = 0;
-  for (int w = 0; w < kWarps; ++w) {
-    const int x = warp_s[w];
-    before += w < warp ? x : 0;
-    total += x;
-  }
+  const int w = warp_s[lane];   // as many warps as lanes
+  const int before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0), total = __reduce_add_sync(0xffffffffu, w);
   int at = before + incl - sum;
   for (int i = i0; i < i1; ++i) {
+    const int x = in(i);
     out[i] = at;
-    at += __ldcg(in + i);
+    at += x;
   }
   __syncthreads();   // warp_s is read, out is there
   return total;
 }
 
+// Rows' entries to threads: each row by a group of 2^k neighbouring threads of the cluster (8 at least), as many as there are
+// for a row, kUnroll entries of a thread at a time: f(row, index, entry's address) for every index below length(row).
+constexpr int kUnroll = 4;
+template <typename Length, typename Row, typename F>
+__device__ __forceinline__ void for_entries(int rows, int me, int all, Length length, Row row_of, F f) {
+  int group = 8;
+  while (group < all && (int64_t)rows * group * 2 <= all) group *= 2;
+  for (int b = me / group; b < rows; b += all / group) {
+    const int n = length(b);
+    const int32_t* row = row_of(b);
+    for (int i0 = me & (group - 1); i0 < n; i0 += kUnroll * group) {
+      int x[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) x[u] = i0 + u * group < n ? __ldg(row + i0 + u * group) : -1;
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u)
+        if (i0 + u * group < n) f(b, i0 + u * group, x[u]);
+    }
+  }
+}
+
+template <bool kOne>   // one CTA, else a cluster of kCtas
 __global__ void __launch_bounds__(kThreads, 1) page_fork_plan_kernel(const __grid_constant__ PageForkParams p) {
   extern __shared__ int smem[];
   __shared__ int warp_s[kWarps];
-  int* gives_s = smem;                  // [from_batch] exclusive sums
-  int* takes_s = smem + p.from_batch;   // [to_batch]
-  const Scratch sc(p.scratch, p.num_pages, p.from_batch, p.to_batch);
-  const int t = threadIdx.x, lane = t & 31, cta = blockIdx.x;
-  const int all = kCtas * kThreads, me = cta * kThreads + t;            // threads of the cluster
-  const int warps = kCtas * kWarps, my_warp = cta * kWarps + (t >> 5);
-  const int W = p.max_pages, log2p = p.page_log2, below = (1 << log2p) - 1;
+  __shared__ int bad_s;
+  const int F = p.from_batch, B = p.to_batch, W = p.max_pages, log2p = p.page_log2, below = (1 << log2p) - 1;
+  int* held = smem;             // [F]
+  int* parent = held + F;       // [B]
+  int* tokens = parent + B;     // [B] 0 without a parent
+  int* gives_s = tokens + B;    // [F] counts (one CTA), then exclusive sums
+  int* takes_s = gives_s + F;   // [B]
+  const Scratch sc(p.scratch, p.num_pages, F, B);
+  int* first = kOne ? takes_s + B : sc.first;
+  int* user = kOne ? first + p.num_pages : sc.user;
+  int* bad_page = kOne ? &bad_s : sc.bad;
+  const int t = threadIdx.x, lane = t & 31, cta = kOne ? 0 : blockIdx.x;
+  constexpr int all = (kOne ? 1 : kCtas) * kThreads, warps = all / 32;   // of the plan
+  const int me = cta * kThreads + t, my_warp = cta * kWarps + (t >> 5);
+  auto barrier = [&] {
+    if constexpr (kOne) {
+      __syncthreads();
+    } else {
+      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+  };
+  auto seen = [&](const int* x) { return kOne ? *(volatile const int*)x : __ldcg(x); };   // what other threads wrote
   if (t == 0) grid_launch_dependents();
   grid_dependency_wait();
 
-  // the sizes, checked by every CTA; nothing is known of any page
+  // the sizes, by every CTA; nothing is known of any page
   const int f = *p.free_count;
   bool bad = f < 0 || f > p.num_pages;
-  for (int b = t; b < p.from_batch; b += kThreads) bad = bad || p.held[b] < 0 || p.held[b] > W;
-  for (int b = t; b < p.to_batch; b += kThreads) {
-    const int from = p.parents[b], n = p.lens[b];
-    bad = bad || from < -1 || from >= p.from_batch || (from >= 0 && (n < 0 || (n + (int64_t)below) >> log2p > p.held[from]));
+  for (int b = t; b < F; b += kThreads) {
+    const int n = p.held[b];
+    held[b] = n;
+    if (kOne) gives_s[b] = 0;
+    bad = bad || n < 0 || n > W;
   }
-  for (int x = me; x < p.num_pages; x += all) sc.first[x] = sc.user[x] = kNone;
-  if (me == 0) *sc.bad = 0;
+  for (int b = t; b < B; b += kThreads) {
+    const int from = p.parents[b];
+    parent[b] = from;
+    tokens[b] = from == -1 ? 0 : p.lens[b];
+    bad = bad || from < -1 || from >= F;
+  }
+  for (int x = me; x < p.num_pages; x += all) first[x] = user[x] = kNone;
+  if (me == 0) *bad_page = 0;
   bad = __syncthreads_or(bad) != 0;   // the same in every CTA
-  auto tokens_of = [&](int b) { return p.parents[b] < 0 ? 0 : p.lens[b]; };
-  cluster_barrier();
-
-  // every page's first holder and u
   if (!bad) {
     bool out = false;
-    for (int b = my_warp; b < p.from_batch; b += warps) {
-      const int n = p.held[b];
-      for (int i = lane; i < n; i += 32) {
-        const int x = p.table[(size_t)b * W + i];
-        if (x >= 0 && x < p.num_pages) {
-          if (__ldcg(sc.first + x) > b) atomicMin(sc.first + x, b);
-        } else {
-          out = true;
-        }
-      }
-    }
-    for (int b = my_warp; b < p.to_batch; b += warps) {
-      const int n = tokens_of(b), full = n >> log2p;
-      const int32_t* row = p.table + (size_t)max(p.parents[b], 0) * W;
-      for (int i = lane; i < full; i += 32) {
-        const int x = row[i];
-        if (x >= 0 && x < p.num_pages && __ldcg(sc.user + x) != -1) atomicMin(sc.user + x, -1);
-      }
-      if (lane == 0 && (n & below) != 0) {
-        const int x = row[full];
-        if (x >= 0 && x < p.num_pages) atomicMin(sc.user + x, b);
-      }
-    }
+    for (int b = t; b < B; b += kThreads)
+      out = out || (parent[b] >= 0 && (tokens[b] < 0 || (tokens[b] + (int64_t)below) >> log2p > held[parent[b]]));
+    bad = out;
+  }
+  bad = __syncthreads_or(bad) != 0;
+  barrier();
+
+  // every page's first holder and u
+  auto held_of = [&](int b) { return held[b]; };
+  auto source_row = [&](int b) { return p.table + (size_t)b * W; };
+  auto parent_row = [&](int b) { return p.table + (size_t)max(parent[b], 0) * W; };
+  auto need_of = [&](int b) { return (int)(((unsigned)tokens[b] + (unsigned)below) >> log2p); };
+  if (!bad) {
+    bool out = false;
+    for_entries(F, me, all, held_of, source_row, [&](int b, int, int x) {
+      if (x >= 0 && x < p.num_pages) atomicMin(first + x, b); else out = true;
+    });
+    for_entries(B, me, all, need_of, parent_row, [&](int b, int i, int x) {
+      if (x >= 0 && x < p.num_pages) atomicMin(user + x, i < tokens[b] >> log2p ? -1 : b);
+    });
     for (int i = me; i < f; i += all) {
       const int x = p.free_pages[i];
       out = out || x < 0 || x >= p.num_pages;
     }
-    if (out) atomicOr(sc.bad, 1);
+    if (out) atomicOr(bad_page, 1);
   }
-  cluster_barrier();
-  bad = bad || __ldcg(sc.bad) != 0;
+  barrier();
+  bad = bad || seen(bad_page) != 0;
 
   // what each row gives and takes
   if (!bad) {
-    for (int b = my_warp; b < p.from_batch; b += warps) {
-      const int n = p.held[b];
-      int count = 0;
-      for (int i = lane; i < n; i += 32) {
-        const int x = p.table[(size_t)b * W + i];
-        count += __ldcg(sc.first + x) == b && __ldcg(sc.user + x) == kNone ? 1 : 0;
+    if constexpr (kOne) {
+      for_entries(F, me, all, held_of, source_row, [&](int b, int, int x) {
+        if (seen(first + x) == b && seen(user + x) == kNone) atomicAdd(gives_s + b, 1);
+      });
+    } else {
+      for (int b = my_warp; b < F; b += warps) {
+        int count = 0;
+        for (int i = lane; i < held[b]; i += 32) {
+          const int x = source_row(b)[i];
+          count += seen(first + x) == b && seen(user + x) == kNone ? 1 : 0;
+        }
+        count = __reduce_add_sync(0xffffffffu, count);
+        if (lane == 0) sc.gives[b] = count;
       }
-      count = __reduce_add_sync(0xffffffffu, count);
-      if (lane == 0) sc.gives[b] = count;
     }
-    for (int b = me; b < p.to_batch; b += all) {
-      const int n = tokens_of(b);
-      sc.takes[b] = (n & below) != 0 && __ldcg(sc.user + p.table[(size_t)p.parents[b] * W + (n >> log2p)]) != b ? 1 : 0;
+    for (int b = me; b < B; b += all) {
+      const int n = tokens[b], takes = (n & below) != 0 && seen(user + parent_row(b)[n >> log2p]) != b ? 1 : 0;
+      if (kOne) takes_s[b] = takes; else sc.takes[b] = takes;
     }
   }
-  cluster_barrier();
+  barrier();
 
   int G = 0, T = 0;
   if (!bad) {
-    G = exclusive_sums(sc.gives, p.from_batch, gives_s, warp_s);
-    T = exclusive_sums(sc.takes, p.to_batch, takes_s, warp_s);
+    if constexpr (kOne) {
+      G = exclusive_sums([&](int i) { return gives_s[i]; }, F, gives_s, warp_s);
+      T = exclusive_sums([&](int i) { return takes_s[i]; }, B, takes_s, warp_s);
+    } else {
+      G = exclusive_sums([&](int i) { return __ldcg(sc.gives + i); }, F, gives_s, warp_s);
+      T = exclusive_sums([&](int i) { return __ldcg(sc.takes + i); }, B, takes_s, warp_s);
+    }
   }
   bad = bad || (int64_t)f - T + G > p.num_pages;   // more pages than there are: some page is held and free
   const bool refused = bad || T > f;
@@ -170,37 +213,32 @@ __global__ void __launch_bounds__(kThreads, 1) page_fork_plan_kernel(const __gri
     if (refused) atomicMax(p.dev_status, bad ? (int)PTD_ERR_INVALID_BATCH : (int)PTD_ERR_NO_PAGES);
   }
   if (refused) {
-    for (int b = me; b < p.to_batch; b += all) p.new_held[b] = 0;
+    for (int b = me; b < B; b += all) p.new_held[b] = 0;
     return;
   }
-  for (int b = my_warp; b < p.to_batch; b += warps) {
-    const int n = tokens_of(b), full = n >> log2p;
-    const int32_t* row = p.table + (size_t)max(p.parents[b], 0) * W;
-    int32_t* to = p.new_table + (size_t)b * W;
-    for (int i = lane; i < full; i += 32) to[i] = row[i];
-    if (lane == 0) {
-      p.new_held[b] = full + ((n & below) != 0 ? 1 : 0);
-      if ((n & below) != 0) {
-        int x = row[full];
-        if (__ldcg(sc.takes + b) != 0) {
-          const int rank = takes_s[b], fresh = p.free_pages[f - 1 - rank];
-          sc.copy[3 * rank] = x;
-          sc.copy[3 * rank + 1] = fresh;
-          sc.copy[3 * rank + 2] = n & below;
-          x = fresh;
-        }
-        to[full] = x;
-      }
+  auto total_after = [&](const int* sums, int n, int total, int b) { return b + 1 < n ? sums[b + 1] : total; };
+  for (int b = me; b < B; b += all) {
+    p.new_held[b] = need_of(b);
+    const int rank = takes_s[b];
+    if (total_after(takes_s, B, T, b) != rank) {
+      const int full = tokens[b] >> log2p, fresh = p.free_pages[f - 1 - rank];
+      sc.copy[3 * rank] = parent_row(b)[full];
+      sc.copy[3 * rank + 1] = fresh;
+      sc.copy[3 * rank + 2] = tokens[b] & below;
+      p.new_table[(size_t)b * W + full] = fresh;
     }
   }
+  for_entries(B, me, all, need_of, parent_row, [&](int b, int i, int x) {
+    if (i < tokens[b] >> log2p || total_after(takes_s, B, T, b) == takes_s[b]) p.new_table[(size_t)b * W + i] = x;
+  });
   for (int i = me; i < f - T; i += all) p.new_free_pages[i] = p.free_pages[i];
-  for (int b = my_warp; b < p.from_batch; b += warps) {
-    if (__ldcg(sc.gives + b) == 0) continue;
-    const int n = p.held[b];
+  for (int b = my_warp; b < F; b += warps) {
+    if (total_after(gives_s, F, G, b) == gives_s[b]) continue;
+    const int n = held[b];
     int at = f - T + gives_s[b];
     for (int i0 = 0; i0 < n; i0 += 32) {
-      const int x = i0 + lane < n ? p.table[(size_t)b * W + i0 + lane] : -1;
-      const bool given = x >= 0 && __ldcg(sc.first + x) == b && __ldcg(sc.user + x) == kNone;
+      const int x = i0 + lane < n ? source_row(b)[i0 + lane] : -1;
+      const bool given = x >= 0 && seen(first + x) == b && seen(user + x) == kNone;
       const uint32_t mask = __ballot_sync(0xffffffffu, given);
       const int place = at + __popc(mask & ((1u << lane) - 1u));
       if (given && place < p.num_pages) p.new_free_pages[place] = x;
@@ -245,15 +283,19 @@ size_t page_fork_scratch_ints(int num_pages, int from_batch, int to_batch) {
 }
 
 cudaError_t launch_page_fork(const PageForkParams& p, int sms, cudaStream_t stream) {
-  constexpr size_t kMostSmem = 2 * (size_t)PTD_MAX_PROMPT_BATCH * sizeof(int);
-  const size_t smem = ((size_t)p.from_batch + p.to_batch) * sizeof(int);
-  if (smem > 47 * 1024) {   // the limit is the kernel's, the same for every call
+  constexpr size_t kMostSmem = 5 * (size_t)PTD_MAX_PROMPT_BATCH * sizeof(int), kMostOneSmem = 200 * 1024;
+  const size_t sizes = (2 * (size_t)p.from_batch + 3 * (size_t)p.to_batch) * sizeof(int);
+  const size_t with_pages = sizes + 2 * (size_t)p.num_pages * sizeof(int);
+  const bool one = with_pages <= kMostOneSmem && p.from_batch + p.to_batch <= 1024;
+  const size_t smem = one ? with_pages : sizes;
+  if (smem > 47 * 1024) {   // the limits are the kernels', the same for every call
     const cudaError_t e =
-        cudaFuncSetAttribute(pf::page_fork_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem);
+        one ? cudaFuncSetAttribute(pf::page_fork_plan_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostOneSmem)
+            : cudaFuncSetAttribute(pf::page_fork_plan_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem);
     if (e != cudaSuccess) return e;
   }
-  const cudaError_t e =
-      launch_chained(pf::page_fork_plan_kernel, dim3(pf::kCtas), dim3(pf::kThreads), smem, stream, pf::kCtas, p);
+  const cudaError_t e = launch_chained(one ? pf::page_fork_plan_kernel<true> : pf::page_fork_plan_kernel<false>,
+                                       dim3(one ? 1 : pf::kCtas), dim3(pf::kThreads), smem, stream, one ? 0 : pf::kCtas, p);
   if (e != cudaSuccess) return e;
   const int64_t page_bytes = p.row_bytes << p.page_log2;
   const int chunks = (int)((page_bytes + pf::kChunk - 1) / pf::kChunk);

@@ -39,13 +39,21 @@ __device__ __forceinline__ RowSums merge_sums(const RowSums& x, const RowSums& y
           __fadd_rn(__fmul_rn(ex, fmaf(dx, x.s, x.a)), __fmul_rn(ey, fmaf(dy, y.s, y.a)))};
 }
 
-__device__ __forceinline__ RowSums merge_lanes(RowSums x, int lanes, float scale) {
-  for (int o = 1; o < lanes; o <<= 1) {
-    const RowSums y = {__shfl_xor_sync(0xffffffffu, x.ref, o), __shfl_xor_sync(0xffffffffu, x.s, o),
-                       __shfl_xor_sync(0xffffffffu, x.a, o)};
-    x = merge_sums(x, y, scale);
+// The sums of a warp's lanes together, to every lane (the same bits: pairs are added, and a sum does not depend on its order).
+// With lanes < 32 the lanes' values repeat every `lanes`, and one period counts.
+template <int kLanes>
+__device__ __forceinline__ RowSums merge_lanes(const RowSums& x, float scale) {
+  const uint32_t u = __float_as_uint(x.ref);
+  const uint32_t most = __reduce_max_sync(0xffffffffu, (u & 0x80000000u) ? ~u : (u | 0x80000000u));   // in the order of floats
+  const float r = __uint_as_float((most & 0x80000000u) ? (most & 0x7FFFFFFFu) : ~most);
+  const float d = fmaxf((x.ref - r) * scale, kLeastExponent), e = ptx_exp2(d);   // (-inf - -inf counts as the least)
+  float s = e * x.s, a = e * fmaf(d, x.s, x.a);
+#pragma unroll
+  for (int o = 1; o < kLanes; o <<= 1) {
+    s += __shfl_xor_sync(0xffffffffu, s, o);
+    a += __shfl_xor_sync(0xffffffffu, a, o);
   }
-  return x;
+  return {r, s, a};
 }
 
 // A thread's sums, in packed pairs.
@@ -61,13 +69,23 @@ struct ThreadSums {
     a = f2_fma(f2_pack(d, d), s, f2_mul(a, f2_pack(e, e)));
     most = m, neg = -m;
   }
-  __device__ __forceinline__ void add2(float x0, float x1, unsigned long long scale2) {
-    float t0, t1;
-    f2_unpack(f2_mul(f2_add(f2_pack(x0, x1), f2_pack(neg, neg)), scale2), t0, t1);
-    t0 = max_nan(t0, kLeastExponent), t1 = max_nan(t1, kLeastExponent);
-    const unsigned long long e = f2_pack(ptx_exp2(t0), ptx_exp2(t1));
-    s = f2_add(s, e);
-    a = f2_fma(f2_pack(t0, t1), e, a);
+  // Adds N logits (even; none above `most`).  They are summed by themselves first: a row's sum then has a rounding per block of
+  // N rather than one per pair.
+  template <int N>
+  __device__ __forceinline__ void add(const float (&x)[N], unsigned long long scale2) {
+    const unsigned long long neg2 = f2_pack(neg, neg);
+    unsigned long long bs = 0ull, ba = 0ull;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      float t0, t1;
+      f2_unpack(f2_mul(f2_add(f2_pack(x[i], x[i + 1]), neg2), scale2), t0, t1);
+      t0 = max_nan(t0, kLeastExponent), t1 = max_nan(t1, kLeastExponent);
+      const unsigned long long e = f2_pack(ptx_exp2(t0), ptx_exp2(t1));
+      bs = f2_add(bs, e);
+      ba = f2_fma(f2_pack(t0, t1), e, ba);
+    }
+    s = f2_add(s, bs);
+    a = f2_add(a, ba);
   }
   __device__ __forceinline__ RowSums sums() const {
     float s0, s1, a0, a1;

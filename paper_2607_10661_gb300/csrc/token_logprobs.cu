@@ -28,7 +28,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxParts = 8, kMaxK = 16;
 constexpr int kCand = 256;         // candidate buffer (keys)
 constexpr int kLoads = 4;          // vectors of a thread in flight
-constexpr int kCtas = 5;           // of an SM
+constexpr int kCtas = 4;           // of an SM
 constexpr int kTargetVec = 2048;   // 32 KB: the part that the cluster size aims at
 
 template <typename T, bool kCluster>
@@ -41,7 +41,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) token_logprobs_kernel(const _
   __shared__ __align__(8) uint64_t parts_bar_s;
   __shared__ uint64_t round_s[kWarps];
   __shared__ RowSums warp_sums[kWarps];
-  __shared__ int n_cand_s, abort_s;
+  __shared__ uint8_t owners_s[kThreads];
+  __shared__ int n_cand_s, n_owners_s, abort_s;
 
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)blockIdx.x, parts = (int)gridDim.x;   // the grid's x is one row's parts
@@ -56,6 +57,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) token_logprobs_kernel(const _
     }
     abort_s = 0;
     n_cand_s = 0;
+    n_owners_s = 0;
   }
   if (kCluster && rank == 0 && tid < kMaxParts * kMaxK) all_keys[tid] = 0ull;
   __syncthreads();
@@ -80,30 +82,40 @@ __global__ void __launch_bounds__(kThreads, kCtas) token_logprobs_kernel(const _
   {
     constexpr uint32_t kNone = VN == 8 ? kBf16x2NegInf : 0xFF800000u;   // -inf
     const unsigned long long scale2 = f2_pack(p.scale, p.scale);
+    uint4 next[kLoads];
+    auto load = [&](int v0) {
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        const int v = v0 + u * kThreads;
+        next[u] = v < nv ? __ldg(vrow + v) : make_uint4(kNone, kNone, kNone, kNone);
+      }
+    };
+    load(tid);
 #pragma unroll 1
     for (int v0 = tid; v0 < nv; v0 += kLoads * kThreads) {
       uint4 x[kLoads];
 #pragma unroll
-      for (int u = 0; u < kLoads; ++u) {
-        const int v = v0 + u * kThreads;
-        x[u] = v < nv ? __ldg(vrow + v) : make_uint4(kNone, kNone, kNone, kNone);
-      }
+      for (int u = 0; u < kLoads; ++u) x[u] = next[u];
+      load(v0 + kLoads * kThreads);   // the next batch is on its way while this one is added
       float m = vec_max<T>(x[0]);
 #pragma unroll
       for (int u = 1; u < kLoads; ++u) m = fmaxf(m, vec_max<T>(x[u]));
       vmax = fmaxf(vmax, m);
       sums.raise(m, p.scale);
+      float f[kLoads * VN];
 #pragma unroll
       for (int u = 0; u < kLoads; ++u) {
-        float f[8];
-        Vec<T>::unpack(x[u], f);
+        float g[8];
+        Vec<T>::unpack(x[u], g);
 #pragma unroll
-        for (int e = 0; e < VN; e += 2) sums.add2(f[e], f[e + 1], scale2);
+        for (int e = 0; e < VN; ++e) f[u * VN + e] = g[e];
       }
+      sums.add(f, scale2);
     }
     auto add1 = [&](float f) {
       sums.raise(f, p.scale);
-      sums.add2(f, -INFINITY, scale2);
+      const float pair[2] = {f, -INFINITY};
+      sums.add(pair, scale2);
     };
     if (own_head)
       for (int i = 0; i < a0; ++i) add1(Vec<T>::scalar(row + i));
@@ -116,7 +128,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) token_logprobs_kernel(const _
 #pragma unroll
     for (int d = 1; d < 8; d <<= 1) o = max(o, __shfl_xor_sync(0xffffffffu, o, d));
     if ((lane & 7) == 0) group_max_s[warp * 4 + (lane >> 3)] = o;
-    const RowSums w = merge_lanes(sums.sums(), 32, p.scale);
+    const RowSums w = merge_lanes<32>(sums.sums(), p.scale);
     if (lane == 0) warp_sums[warp] = w;
   }
   __syncthreads();
@@ -144,30 +156,35 @@ __global__ void __launch_bounds__(kThreads, kCtas) token_logprobs_kernel(const _
         const float f = Vec<T>::scalar(row + i);
         if (f >= thr) push(f, (uint32_t)i);
       }
-    if (vmax >= thr) {   // about k lanes of the 256
-#pragma unroll 1
-      for (int v0 = tid; v0 < nv; v0 += kLoads * kThreads) {
-        uint4 x[kLoads];
+    // the vectors of the lanes whose maximum reaches the threshold (about k of the 256), by all threads
+    if (vmax >= thr && tid < nv) owners_s[atomicAdd(&n_owners_s, 1)] = (uint8_t)tid;
+    __syncthreads();
+    const int owners = n_owners_s, each = (nv + kThreads - 1) / kThreads, items = owners * each;
+    for (int i0 = tid; i0 < items; i0 += kLoads * kThreads) {
+      uint4 x[kLoads];
+      int v[kLoads];
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) x[u] = __ldg(vrow + min(v0 + u * kThreads, nv - 1));
-        if (*(volatile int*)&n_cand_s > kCand) break;   // the buffer is already lost
+      for (int u = 0; u < kLoads; ++u) {
+        const int i = i0 + u * kThreads, round = i / owners;
+        v[u] = i < items ? owners_s[i - round * owners] + round * kThreads : nv;
+        x[u] = __ldg(vrow + min(v[u], nv - 1));
+      }
+      if (*(volatile int*)&n_cand_s > kCand) break;   // the buffer is already lost
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) {
-          const int v = v0 + u * kThreads;
-          if (v < nv && vec_max<T>(x[u]) >= thr) {
-            float f[8];
-            Vec<T>::unpack(x[u], f);
-            const uint32_t i0 = (uint32_t)(a0 + (v_begin + v) * VN);
+      for (int u = 0; u < kLoads; ++u) {
+        if (v[u] < nv && vec_max<T>(x[u]) >= thr) {
+          float f[8];
+          Vec<T>::unpack(x[u], f);
+          const uint32_t at = (uint32_t)(a0 + (v_begin + v[u]) * VN);
 #pragma unroll
-            for (int e = 0; e < VN; ++e)
-              if (f[e] >= thr) push(f[e], i0 + e);
-          }
+          for (int e = 0; e < VN; ++e)
+            if (f[e] >= thr) push(f[e], at + e);
         }
       }
     }
   }
   // meanwhile every warp merges the warps' sums (none is written before the next barrier)
-  const RowSums part = merge_lanes(warp_sums[lane & (kWarps - 1)], kWarps, p.scale);
+  const RowSums part = merge_lanes<kWarps>(warp_sums[lane & (kWarps - 1)], p.scale);
   __syncthreads();
   uint64_t* dst_keys = nullptr;
   uint32_t dst_bar = 0;
@@ -256,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) token_logprobs_kernel(const _
     mbar_wait_cluster(parts_bar, 0u, &abort_s, p.dev_status);
     __syncwarp();
     const int at_part = lane & (kMaxParts - 1);
-    const RowResult result(merge_lanes(at_part < parts ? all_sums[at_part] : RowSums{-INFINITY, 0.f, 0.f}, kMaxParts, p.scale));
+    const RowResult result(merge_lanes<kMaxParts>(at_part < parts ? all_sums[at_part] : RowSums{-INFINITY, 0.f, 0.f}, p.scale));
     if (tid == 0) write_row(result);
     const uint64_t key = all_keys[tid];
     if (key != 0ull) {
