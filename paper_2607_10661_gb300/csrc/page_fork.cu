@@ -9,10 +9,11 @@
 // free[f - T + r] of the new stack: everything is a function of u, of each page's first holder and of two sums, and the
 // result does not depend on the order in which threads run (minima alone are made by atomics).
 //
-// The plan has four parts: the sizes; u and the holders; the counts of each row; sums, the new tables and stack, the list of
-// copies.  Its latency is what it costs (each part a few dependent reads): one CTA does it with u and the holders in its shared
-// memory where they fit and the rows are few enough, else a cluster of eight with both in the scratch and a cluster barrier
-// between the parts.  Then a grid copies rows, all layers of K and V, in chunks.
+// The plan reads every source entry once: with m the most full pages that a target has of the row, entry i < m is full
+// somewhere (u = -1), and only what lies behind can be given or kept.  Between its parts (sizes and m; u and the holders; counts;
+// sums, stack and list of copies) all threads wait for one another: one CTA does it with u and the holders in its shared memory
+// where they fit and the rows are few enough, else a cluster of eight with both in the scratch.  Then a grid copies: table
+// rows, the rest of the stack, and K/V rows of all layers in chunks.
 #include <cuda_runtime.h>
 
 #include <climits>
@@ -31,17 +32,20 @@ constexpr int kNone = INT_MAX;
 constexpr int kCopyThreads = 256, kCopyLoads = 4;
 constexpr int kChunk = kCopyThreads * kCopyLoads * 16;   // bytes of one CTA's turn
 
+constexpr int kRefused = -1;
 struct Scratch {
   int32_t* bad;       // [1] a page number out of range
-  int32_t* copies;    // [1]
+  int32_t* copies;    // [1] T, or kRefused
+  int32_t* fresh;     // [to_batch] the page taken, or -1
   int32_t* copy;      // [to_batch][3] from page, to page, rows
   int32_t* gives;     // the cluster's: [from_batch] pages given back
+  int32_t* lead;      // [from_batch] the index of the first of them
   int32_t* takes;     // [to_batch] 0 or 1
-  int32_t* first;     // [num_pages] lowest source row that holds the page
+  int32_t* first;     // [num_pages] lowest source row that could give the page
   int32_t* user;      // [num_pages] u
   __host__ __device__ Scratch(int32_t* at, int num_pages, int from_batch, int to_batch)
-      : bad(at), copies(at + 1), copy(at + 4), gives(copy + 3 * (size_t)to_batch), takes(gives + from_batch),
-        first(takes + to_batch), user(first + num_pages) {}
+      : bad(at), copies(at + 1), fresh(at + 4), copy(fresh + to_batch), gives(copy + 3 * (size_t)to_batch),
+        lead(gives + from_batch), takes(lead + from_batch), first(takes + to_batch), user(first + num_pages) {}
 };
 
 // Exclusive sums of in[0 .. n) into out (may be the same), by the whole CTA; the total to every thread.
@@ -71,17 +75,21 @@ __device__ __forceinline__ int exclusive_sums(Load in, int n, int* out, int* war
   return total;
 }
 
-// Rows' entries to threads: each row by a group of 2^k neighbouring threads of the cluster (8 at least), as many as there are
-// for a row, kUnroll entries of a thread at a time: f(row, index, entry's address) for every index below length(row).
-constexpr int kUnroll = 4;
-template <typename Length, typename Row, typename F>
-__device__ __forceinline__ void for_entries(int rows, int me, int all, Length length, Row row_of, F f) {
+// Rows' entries to threads: each row by a group of 2^k neighbouring threads of the plan (8 at least), as many as there are
+// for a row, kUnroll entries of a thread in flight: f(row, index, entry) for every index of [begin(row), end(row)).
+constexpr int kUnroll = 8;
+__device__ __forceinline__ int group_of(int rows, int all) {
   int group = 8;
   while (group < all && (int64_t)rows * group * 2 <= all) group *= 2;
+  return group;
+}
+template <typename Begin, typename End, typename Row, typename F>
+__device__ __forceinline__ void for_entries(int rows, int me, int all, Begin begin, End end, Row row_of, F f) {
+  const int group = group_of(rows, all);
   for (int b = me / group; b < rows; b += all / group) {
-    const int n = length(b);
+    const int n = end(b);
     const int32_t* row = row_of(b);
-    for (int i0 = me & (group - 1); i0 < n; i0 += kUnroll * group) {
+    for (int i0 = begin(b) + (me & (group - 1)); i0 < n; i0 += kUnroll * group) {
       int x[kUnroll];
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) x[u] = i0 + u * group < n ? __ldg(row + i0 + u * group) : -1;
@@ -92,6 +100,19 @@ __device__ __forceinline__ void for_entries(int rows, int me, int all, Length le
   }
 }
 
+// f(i, a[i]) for i = me, me + all, ... < n, kUnroll of them in flight.
+template <typename F>
+__device__ __forceinline__ void for_stack(const int32_t* a, int n, int me, int all, F f) {
+  for (int i0 = me; i0 < n; i0 += kUnroll * all) {
+    int x[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) x[u] = i0 + u * all < n ? __ldg(a + i0 + u * all) : 0;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (i0 + u * all < n) f(i0 + u * all, x[u]);
+  }
+}
+
 template <bool kOne>   // one CTA, else a cluster of kCtas
 __global__ void __launch_bounds__(kThreads, 1) page_fork_plan_kernel(const __grid_constant__ PageForkParams p) {
   extern __shared__ int smem[];
@@ -99,12 +120,14 @@ __global__ void __launch_bounds__(kThreads, 1) page_fork_plan_kernel(const __gri
   __shared__ int bad_s;
   const int F = p.from_batch, B = p.to_batch, W = p.max_pages, log2p = p.page_log2, below = (1 << log2p) - 1;
   int* held = smem;             // [F]
-  int* parent = held + F;       // [B]
+  int* most = held + F;         // [F] m
+  int* gives_s = most + F;      // [F] counts (one CTA), then exclusive sums
+  int* parent = gives_s + F;    // [B]
   int* tokens = parent + B;     // [B] 0 without a parent
-  int* gives_s = tokens + B;    // [F] counts (one CTA), then exclusive sums
-  int* takes_s = gives_s + F;   // [B]
+  int* takes_s = tokens + B;    // [B]
   const Scratch sc(p.scratch, p.num_pages, F, B);
-  int* first = kOne ? takes_s + B : sc.first;
+  int* lead = kOne ? takes_s + B : sc.lead;
+  int* first = kOne ? lead + F : sc.first;
   int* user = kOne ? first + p.num_pages : sc.user;
   int* bad_page = kOne ? &bad_s : sc.bad;
   const int t = threadIdx.x, lane = t & 31, cta = kOne ? 0 : blockIdx.x;
@@ -122,19 +145,21 @@ __global__ void __launch_bounds__(kThreads, 1) page_fork_plan_kernel(const __gri
   if (t == 0) grid_launch_dependents();
   grid_dependency_wait();
 
-  // the sizes, by every CTA; nothing is known of any page
+  // the sizes and m, by every CTA; nothing is known of any page
   const int f = *p.free_count;
   bool bad = f < 0 || f > p.num_pages;
   for (int b = t; b < F; b += kThreads) {
     const int n = p.held[b];
     held[b] = n;
-    if (kOne) gives_s[b] = 0;
+    most[b] = 0;
+    if (kOne) gives_s[b] = 0; else if (cta == 0) sc.gives[b] = 0;
+    if (cta == 0) lead[b] = kNone;
     bad = bad || n < 0 || n > W;
   }
   for (int b = t; b < B; b += kThreads) {
-    const int from = p.parents[b];
+    const int from = p.parents[b], n = p.lens[b];
     parent[b] = from;
-    tokens[b] = from == -1 ? 0 : p.lens[b];
+    tokens[b] = from == -1 ? 0 : n;
     bad = bad || from < -1 || from >= F;
   }
   for (int x = me; x < p.num_pages; x += all) first[x] = user[x] = kNone;
@@ -142,54 +167,70 @@ __global__ void __launch_bounds__(kThreads, 1) page_fork_plan_kernel(const __gri
   bad = __syncthreads_or(bad) != 0;   // the same in every CTA
   if (!bad) {
     bool out = false;
-    for (int b = t; b < B; b += kThreads)
-      out = out || (parent[b] >= 0 && (tokens[b] < 0 || (tokens[b] + (int64_t)below) >> log2p > held[parent[b]]));
+    for (int b = t; b < B; b += kThreads) {
+      const int from = parent[b], n = tokens[b];
+      if (from < 0) continue;
+      out = out || n < 0 || (n + (int64_t)below) >> log2p > held[from];
+      if (n >> log2p > most[from]) atomicMax(most + from, n >> log2p);
+    }
     bad = out;
   }
   bad = __syncthreads_or(bad) != 0;
   barrier();
 
-  // every page's first holder and u
+  auto zero = [](int) { return 0; };
   auto held_of = [&](int b) { return held[b]; };
   auto source_row = [&](int b) { return p.table + (size_t)b * W; };
-  auto parent_row = [&](int b) { return p.table + (size_t)max(parent[b], 0) * W; };
-  auto need_of = [&](int b) { return (int)(((unsigned)tokens[b] + (unsigned)below) >> log2p); };
+  auto last_page = [&](int b) { return __ldg(source_row(parent[b]) + (tokens[b] >> log2p)); };   // of a target with a partial one
   if (!bad) {
     bool out = false;
-    for_entries(F, me, all, held_of, source_row, [&](int b, int, int x) {
-      if (x >= 0 && x < p.num_pages) atomicMin(first + x, b); else out = true;
+    for_entries(F, me, all, zero, held_of, source_row, [&](int b, int i, int x) {
+      if (x < 0 || x >= p.num_pages) {
+        out = true;
+      } else if (i >= most[b]) {
+        atomicMin(first + x, b);
+      } else {
+        atomicMin(user + x, -1);
+      }
     });
-    for_entries(B, me, all, need_of, parent_row, [&](int b, int i, int x) {
-      if (x >= 0 && x < p.num_pages) atomicMin(user + x, i < tokens[b] >> log2p ? -1 : b);
-    });
-    for (int i = me; i < f; i += all) {
-      const int x = p.free_pages[i];
-      out = out || x < 0 || x >= p.num_pages;
-    }
+    for (int b = me; b < B; b += all)
+      if ((tokens[b] & below) != 0) {
+        const int x = last_page(b);
+        if (x >= 0 && x < p.num_pages) atomicMin(user + x, b);
+      }
+    for_stack(p.free_pages, f, me, all, [&](int, int x) { out = out || x < 0 || x >= p.num_pages; });
     if (out) atomicOr(bad_page, 1);
   }
   barrier();
   bad = bad || seen(bad_page) != 0;
 
   // what each row gives and takes
+  auto given = [&](int b, int x) { return seen(first + x) == b && seen(user + x) == kNone; };
   if (!bad) {
-    if constexpr (kOne) {
-      for_entries(F, me, all, held_of, source_row, [&](int b, int, int x) {
-        if (seen(first + x) == b && seen(user + x) == kNone) atomicAdd(gives_s + b, 1);
-      });
-    } else {
-      for (int b = my_warp; b < F; b += warps) {
-        int count = 0;
-        for (int i = lane; i < held[b]; i += 32) {
-          const int x = source_row(b)[i];
-          count += seen(first + x) == b && seen(user + x) == kNone ? 1 : 0;
-        }
-        count = __reduce_add_sync(0xffffffffu, count);
-        if (lane == 0) sc.gives[b] = count;
+    const int group = group_of(F, all);
+    for (int b = me / group; b < F; b += all / group) {   // (uniform in a warp where the group is one or more)
+      int count = 0, least = kNone;
+      const int n = held[b];
+      for (int i0 = most[b] + (me & (group - 1)); i0 < n; i0 += kUnroll * group) {
+        int x[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) x[u] = i0 + u * group < n ? __ldg(source_row(b) + i0 + u * group) : -1;
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+          if (x[u] >= 0 && given(b, x[u])) ++count, least = min(least, i0 + u * group);
+      }
+      if (group >= 32) {
+        const int sum = __reduce_add_sync(0xffffffffu, count);
+        least = __reduce_min_sync(0xffffffffu, least);
+        count = lane == 0 ? sum : 0;
+      }
+      if (count > 0) {
+        atomicAdd(kOne ? gives_s + b : sc.gives + b, count);
+        atomicMin(lead + b, least);
       }
     }
     for (int b = me; b < B; b += all) {
-      const int n = tokens[b], takes = (n & below) != 0 && seen(user + parent_row(b)[n >> log2p]) != b ? 1 : 0;
+      const int takes = (tokens[b] & below) != 0 && seen(user + last_page(b)) != b ? 1 : 0;
       if (kOne) takes_s[b] = takes; else sc.takes[b] = takes;
     }
   }
@@ -209,50 +250,52 @@ __global__ void __launch_bounds__(kThreads, 1) page_fork_plan_kernel(const __gri
   const bool refused = bad || T > f;
   if (me == 0) {
     *p.new_free_count = refused ? 0 : f - T + G;
-    *sc.copies = refused ? 0 : T;
+    *sc.copies = refused ? kRefused : T;
     if (refused) atomicMax(p.dev_status, bad ? (int)PTD_ERR_INVALID_BATCH : (int)PTD_ERR_NO_PAGES);
   }
-  if (refused) {
-    for (int b = me; b < B; b += all) p.new_held[b] = 0;
-    return;
-  }
-  auto total_after = [&](const int* sums, int n, int total, int b) { return b + 1 < n ? sums[b + 1] : total; };
   for (int b = me; b < B; b += all) {
-    p.new_held[b] = need_of(b);
+    p.new_held[b] = refused ? 0 : (int)(((unsigned)tokens[b] + (unsigned)below) >> log2p);
+    if (refused) continue;
     const int rank = takes_s[b];
-    if (total_after(takes_s, B, T, b) != rank) {
-      const int full = tokens[b] >> log2p, fresh = p.free_pages[f - 1 - rank];
-      sc.copy[3 * rank] = parent_row(b)[full];
+    int fresh = -1;
+    if ((b + 1 < B ? takes_s[b + 1] : T) != rank) {
+      fresh = p.free_pages[f - 1 - rank];
+      sc.copy[3 * rank] = last_page(b);
       sc.copy[3 * rank + 1] = fresh;
       sc.copy[3 * rank + 2] = tokens[b] & below;
-      p.new_table[(size_t)b * W + full] = fresh;
     }
+    sc.fresh[b] = fresh;
   }
-  for_entries(B, me, all, need_of, parent_row, [&](int b, int i, int x) {
-    if (i < tokens[b] >> log2p || total_after(takes_s, B, T, b) == takes_s[b]) p.new_table[(size_t)b * W + i] = x;
-  });
-  for (int i = me; i < f - T; i += all) p.new_free_pages[i] = p.free_pages[i];
+  if (refused) return;
   for (int b = my_warp; b < F; b += warps) {
-    if (total_after(gives_s, F, G, b) == gives_s[b]) continue;
-    const int n = held[b];
+    if ((b + 1 < F ? gives_s[b + 1] : G) == gives_s[b]) continue;
     int at = f - T + gives_s[b];
-    for (int i0 = 0; i0 < n; i0 += 32) {
-      const int x = i0 + lane < n ? source_row(b)[i0 + lane] : -1;
-      const bool given = x >= 0 && seen(first + x) == b && seen(user + x) == kNone;
-      const uint32_t mask = __ballot_sync(0xffffffffu, given);
-      const int place = at + __popc(mask & ((1u << lane) - 1u));
-      if (given && place < p.num_pages) p.new_free_pages[place] = x;
-      at += __popc(mask);
+    for (int i0 = seen(lead + b); i0 < held[b]; i0 += 32 * kUnroll) {
+      int x[kUnroll];
+      bool mine[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) x[u] = i0 + 32 * u + lane < held[b] ? __ldg(source_row(b) + i0 + 32 * u + lane) : -1;
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) mine[u] = x[u] >= 0 && given(b, x[u]);
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const uint32_t mask = __ballot_sync(0xffffffffu, mine[u]);
+        const int place = at + __popc(mask & ((1u << lane) - 1u));
+        if (mine[u] && place < p.num_pages) p.new_free_pages[place] = x[u];
+        at += __popc(mask);
+      }
     }
   }
 }
 
-// Item: (copy, layer, K or V, chunk of a page's bytes).
+// Table rows by warps and what stays of the stack by threads, then items (copy, layer, K or V, chunk of a page's bytes).
 __global__ void __launch_bounds__(kCopyThreads) page_copy_kernel(const __grid_constant__ PageForkParams p, int chunks) {
   const Scratch sc(p.scratch, p.num_pages, p.from_batch, p.to_batch);
   if (threadIdx.x == 0) grid_launch_dependents();
   grid_dependency_wait();
-  const int64_t per_copy = (int64_t)p.num_layers * 2 * chunks, items = (int64_t)*sc.copies * per_copy;
+  const int copies = *sc.copies;
+  if (copies == kRefused) return;
+  const int64_t per_copy = (int64_t)p.num_layers * 2 * chunks, items = copies * per_copy;
   const int64_t page_bytes = p.row_bytes << p.page_log2;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int c = (int)(item / per_copy);
@@ -269,24 +312,33 @@ __global__ void __launch_bounds__(kCopyThreads) page_copy_kernel(const __grid_co
     uint4 x[kCopyLoads];
 #pragma unroll
     for (int u = 0; u < kCopyLoads; ++u)
-      if (threadIdx.x + u * kCopyThreads < left) x[u] = __ldcs(src + threadIdx.x + u * kCopyThreads);
+      if (threadIdx.x + u * kCopyThreads < left) x[u] = src[threadIdx.x + u * kCopyThreads];
 #pragma unroll
     for (int u = 0; u < kCopyLoads; ++u)
       if (threadIdx.x + u * kCopyThreads < left) dst[threadIdx.x + u * kCopyThreads] = x[u];
   }
+  // the last CTAs first: the first ones have the copies
+  const int cta = (int)gridDim.x - 1 - (int)blockIdx.x, all = (int)gridDim.x * kCopyThreads, me = cta * kCopyThreads + (int)threadIdx.x;
+  for (int b = me >> 5; b < p.to_batch; b += all >> 5) {
+    const int need = p.new_held[b], fresh = sc.fresh[b];
+    const int32_t* row = p.table + (size_t)max(p.parents[b], 0) * p.max_pages;
+    int32_t* to = p.new_table + (size_t)b * p.max_pages;
+    for_stack(row, need, threadIdx.x & 31, 32, [&](int i, int x) { to[i] = i == need - 1 && fresh >= 0 ? fresh : x; });
+  }
+  for_stack(p.free_pages, *p.free_count - copies, me, all, [&](int i, int x) { p.new_free_pages[i] = x; });
 }
 
 }  // namespace pf
 
 size_t page_fork_scratch_ints(int num_pages, int from_batch, int to_batch) {
-  return 4 + 2 * (size_t)num_pages + (size_t)from_batch + 4 * (size_t)to_batch;
+  return 4 + 2 * (size_t)num_pages + 2 * (size_t)from_batch + 5 * (size_t)to_batch;
 }
 
 cudaError_t launch_page_fork(const PageForkParams& p, int sms, cudaStream_t stream) {
-  constexpr size_t kMostSmem = 5 * (size_t)PTD_MAX_PROMPT_BATCH * sizeof(int), kMostOneSmem = 200 * 1024;
-  const size_t sizes = (2 * (size_t)p.from_batch + 3 * (size_t)p.to_batch) * sizeof(int);
-  const size_t with_pages = sizes + 2 * (size_t)p.num_pages * sizeof(int);
-  const bool one = with_pages <= kMostOneSmem && p.from_batch + p.to_batch <= 1024;
+  constexpr size_t kMostSmem = 6 * (size_t)PTD_MAX_PROMPT_BATCH * sizeof(int), kMostOneSmem = 200 * 1024;
+  const size_t sizes = 3 * ((size_t)p.from_batch + p.to_batch) * sizeof(int);
+  const size_t with_pages = sizes + ((size_t)p.from_batch + 2 * (size_t)p.num_pages) * sizeof(int);
+  const bool one = with_pages <= kMostOneSmem && (int64_t)p.from_batch * p.max_pages <= 8192;
   const size_t smem = one ? with_pages : sizes;
   if (smem > 47 * 1024) {   // the limits are the kernels', the same for every call
     const cudaError_t e =
@@ -299,7 +351,7 @@ cudaError_t launch_page_fork(const PageForkParams& p, int sms, cudaStream_t stre
   if (e != cudaSuccess) return e;
   const int64_t page_bytes = p.row_bytes << p.page_log2;
   const int chunks = (int)((page_bytes + pf::kChunk - 1) / pf::kChunk);
-  const int64_t most = (int64_t)p.to_batch * p.num_layers * 2 * chunks, places = 8 * (int64_t)sms;
+  const int64_t most = (int64_t)p.to_batch * p.num_layers * 2 * chunks + p.to_batch, places = 8 * (int64_t)sms;
   return launch_chained(pf::page_copy_kernel, dim3((unsigned)(most < places ? most : places)), dim3(pf::kCopyThreads), 0, stream, 0,
                         p, chunks);
 }
