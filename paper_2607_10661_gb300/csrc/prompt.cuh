@@ -49,6 +49,8 @@ struct PromptRopeParams {
 };
 cudaError_t launch_prompt_rope(const PromptRopeParams& p, bool bf16, const RopeFreqs& freqs, int sms,
                                cudaStream_t stream);
+// The same with norms (called by it).
+cudaError_t launch_prompt_norm_rope(const PromptRopeParams& p, bool bf16, const RopeFreqs& freqs, int sms, cudaStream_t stream);
 
 struct PromptAttnParams {
   const void* q;

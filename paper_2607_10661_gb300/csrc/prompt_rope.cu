@@ -27,9 +27,8 @@ using namespace rope;
 
 constexpr int kMaxTokens = 8;   // of one CTA
 
-// kItems of each thread in flight, kCtas on an SM.  kNorm: a head's D / 2 / V items lie in neighbouring lanes (chunks is
-// a power of two that divides kThreads, so that a thread has one column j for all its items), which sum its squares.
-template <typename T, int kThreads, int kItems, int kCtas, bool kNorm>
+// kItems of each thread in flight, kCtas on an SM.
+template <typename T, int kThreads, int kItems, int kCtas>
 __global__ void __launch_bounds__(kThreads, kCtas)
     prompt_rope_kernel(const PromptRopeParams p, const __grid_constant__ RopeFreqs freqs, int tokens_per_cta,
                        GroupDivisor by_token, GroupDivisor by_chunks) {
@@ -49,7 +48,6 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     j = (r - h * chunks) * V;
   };
   const int first_slot = p.slots[n0 + min(t, tokens - 1)];
-  const float inv_d = 1.f / (float)D;
   uint4 lo[kItems], hi[kItems];
   auto load_items = [&](int e0) {
 #pragma unroll
@@ -64,19 +62,10 @@ __global__ void __launch_bounds__(kThreads, kCtas)
                                       : static_cast<const T*>(p.v) + n * p.v_stride + (size_t)(h - hq - hkv) * D + j;
         lo[u] = *reinterpret_cast<const uint4*>(src);   // plain loads: q may also be written
         hi[u] = *reinterpret_cast<const uint4*>(src + half);
-      } else if constexpr (kNorm) {
-        lo[u] = hi[u] = make_uint4(0u, 0u, 0u, 0u);
       }
     }
   };
   load_items(t);
-  uint4 wq[2] = {}, wk[2] = {};   // this thread's columns of the norms' weights
-  if constexpr (kNorm) {
-    const int j = (t & (chunks - 1)) * V;
-    const T *q_weight = static_cast<const T*>(p.norms.q_weight) + j, *k_weight = static_cast<const T*>(p.norms.k_weight) + j;
-    wq[0] = *reinterpret_cast<const uint4*>(q_weight), wq[1] = *reinterpret_cast<const uint4*>(q_weight + half);
-    wk[0] = *reinterpret_cast<const uint4*>(k_weight), wk[1] = *reinterpret_cast<const uint4*>(k_weight + half);
-  }
   if (t < tokens) {
     const bool fits = first_slot >= 0 && first_slot < p.layer_rows;
     slot_s[t] = fits ? first_slot : -1;
@@ -89,21 +78,14 @@ __global__ void __launch_bounds__(kThreads, kCtas)
 #pragma unroll
     for (int u = 0; u < kItems; ++u) {
       const int e = e0 + u * kThreads;
-      uint4 a = lo[u], b = hi[u];
-      float norm = 1.f;
-      if constexpr (kNorm) norm = norm_of_head(unpack16<T>(a), unpack16<T>(b), chunks, inv_d, p.norms.eps);   // every lane, in range or not
       if (e >= items) continue;
       int i, h, j;
       place_of(e, i, h, j);
       const int slot = slot_s[i];
       if (slot < 0) continue;
+      uint4 a = lo[u], b = hi[u];
       if (h < hq + hkv) {
-        Vec<T> x = unpack16<T>(a), y = unpack16<T>(b);
-        if constexpr (kNorm) {
-          const bool isq = h < hq;
-          scale_by(x, norm, unpack16<T>(isq ? wq[0] : wk[0]));
-          scale_by(y, norm, unpack16<T>(isq ? wq[1] : wk[1]));
-        }
+        const Vec<T> x = unpack16<T>(a), y = unpack16<T>(b);
         Vec<T> rx, ry;
 #pragma unroll
         for (int c = 0; c < V; ++c) {
@@ -130,10 +112,9 @@ __global__ void __launch_bounds__(kThreads, kCtas)
   }
 }
 
-// Rows that are not 16-byte vectors (or heads that a norm cannot take from a warp's lanes): one element at a time, one
-// CTA per token.
+// Rows that are not 16-byte vectors: one element at a time, one CTA per token.
 constexpr int kScalarThreads = 256;
-template <typename T, bool kNorm>
+template <typename T>
 __global__ void __launch_bounds__(kScalarThreads)
     prompt_rope_scalar_kernel(const PromptRopeParams p, const __grid_constant__ RopeFreqs freqs) {
   __shared__ float cos_s[kMaxRopeHalf], sin_s[kMaxRopeHalf];
@@ -147,81 +128,63 @@ __global__ void __launch_bounds__(kScalarThreads)
     return;
   }
   for (int j = t; j < half; j += kScalarThreads) turn_of(freqs, p.positions[n], j, cos_s[j], sin_s[j]);
+  __syncthreads();
   const T* q = static_cast<const T*>(p.q) + n * p.q_stride;
   const T* k = static_cast<const T*>(p.k) + n * p.k_stride;
   const T* v = static_cast<const T*>(p.v) + n * p.v_stride;
   T* qo = static_cast<T*>(p.q_out) + n * p.q_out_stride;
   T* ko = static_cast<T*>(p.k_layer) + (size_t)slot * p.hkv * D;
   T* vo = static_cast<T*>(p.v_layer) + (size_t)slot * p.hkv * D;
-  __syncthreads();
-  if constexpr (kNorm) {   // a warp per head
-    for (int h = t >> 5; h < p.hq + p.hkv; h += kScalarThreads / 32) {
-      const bool isq = h < p.hq;
-      const T* src = isq ? q + (size_t)h * D : k + (size_t)(h - p.hq) * D;
-      T* dst = isq ? qo + (size_t)h * D : ko + (size_t)(h - p.hq) * D;
-      norm_and_turn_row(src, dst, static_cast<const T*>(isq ? p.norms.q_weight : p.norms.k_weight), D, p.norms.eps, cos_s, sin_s);
-    }
-  } else {
-    for (int e = t; e < (p.hq + p.hkv) * half; e += kScalarThreads) {
-      const bool isq = e < p.hq * half;
-      const int e2 = isq ? e : e - p.hq * half;
-      const int h = e2 / half, j = e2 - h * half;
-      const T* src = (isq ? q : k) + (size_t)h * D;
-      T* dst = (isq ? qo : ko) + (size_t)h * D;
-      const float a = ld(src + j), b = ld(src + j + half);
-      const float c = cos_s[j], s = sin_s[j];
-      st(dst + j, a * c - b * s);
-      st(dst + j + half, a * s + b * c);
-    }
+  for (int e = t; e < (p.hq + p.hkv) * half; e += kScalarThreads) {
+    const bool isq = e < p.hq * half;
+    const int e2 = isq ? e : e - p.hq * half;
+    const int h = e2 / half, j = e2 - h * half;
+    const T* src = (isq ? q : k) + (size_t)h * D;
+    T* dst = (isq ? qo : ko) + (size_t)h * D;
+    const float a = ld(src + j), b = ld(src + j + half);
+    const float c = cos_s[j], s = sin_s[j];
+    st(dst + j, a * c - b * s);
+    st(dst + j + half, a * s + b * c);
   }
   for (int e = t; e < p.hkv * D; e += kScalarThreads) vo[e] = v[e];
 }
 
-template <typename T, int kThreads, int kItems, int kCtas, bool kNorm>
+template <typename T, int kThreads, int kItems, int kCtas>
 cudaError_t launch(const PromptRopeParams& p, const RopeFreqs& freqs, int chunks, int per_token, int sms, cudaStream_t stream) {
   // as many tokens a CTA as fill the items of its threads, fewer where the CTAs would not fill the SMs
   int tokens = kItems * kThreads / per_token;
   const int64_t fill = p.n_tokens / (kCtas * (int64_t)sms);
   if (tokens > fill) tokens = (int)fill;
   tokens = tokens < 1 ? 1 : (tokens > kMaxTokens ? kMaxTokens : tokens);
-  return launch_chained(prompt_rope_kernel<T, kThreads, kItems, kCtas, kNorm>,
-                        dim3((unsigned)((p.n_tokens + tokens - 1) / tokens)), dim3(kThreads), 0, stream, 0, p, freqs, tokens,
-                        group_divisor(per_token), group_divisor(chunks));
-}
-
-template <typename T, bool kNorm>
-cudaError_t launch_typed(const PromptRopeParams& p, const RopeFreqs& freqs, int sms, cudaStream_t stream) {
-  constexpr int64_t es = sizeof(T);
-  constexpr int vec = 16 / (int)es;
-  const auto al16 = [](const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15u) == 0; };
-  const bool aligned = al16(p.q) && al16(p.k) && al16(p.v) && al16(p.q_out) && al16(p.k_layer) && al16(p.v_layer) &&
-                       al16(p.norms.q_weight) && al16(p.norms.k_weight) &&
-                       (p.q_stride * es | p.k_stride * es | p.v_stride * es | p.q_out_stride * es) % 16 == 0;
-  const int half = p.head_dim / 2, chunks = half / vec;
-  const bool lanes = !kNorm || (chunks & (chunks - 1)) == 0;   // (at most 32: D <= 256)
-  // (2^22 items a token: the bound of the kernel's quotients)
-  if (aligned && half % vec == 0 && lanes && ((int64_t)p.hq + 2 * (int64_t)p.hkv) * chunks < (1 << 22)) {
-    const int per_token = (p.hq + 2 * p.hkv) * chunks;
-    // While all CTAs have a place at once a token is done soonest by many threads, then small CTAs turn over best.
-    // Measured (us, 384 threads of one item each and 128 of three, bf16 with D = 128; SMs 152): 8 tokens of 32/8 heads
-    // 2.1 and 2.6, 300 2.9 and 4.0, 600 3.2 and 4.1, [the rule's bound] 620 4.2 and 4.5, 1000 5.0 and 4.6, 8192 37.3 and
-    // 31.5; of 64/8 heads 500 4.6 and 6.6, 8000 57.1 and 49.1; fp32 4000 31.8 and 30.3.
-    if (p.n_tokens <= 4 * (int64_t)sms) return launch<T, 384, 1, 4, kNorm>(p, freqs, chunks, per_token, sms, stream);
-    return launch<T, 128, 3, 8, kNorm>(p, freqs, chunks, per_token, sms, stream);
-  }
-  return launch_chained(prompt_rope_scalar_kernel<T, kNorm>, dim3((unsigned)p.n_tokens), dim3(kScalarThreads), 0, stream, 0, p,
-                        freqs);
+  return launch_chained(prompt_rope_kernel<T, kThreads, kItems, kCtas>, dim3((unsigned)((p.n_tokens + tokens - 1) / tokens)),
+                        dim3(kThreads), 0, stream, 0, p, freqs, tokens, group_divisor(per_token), group_divisor(chunks));
 }
 
 }  // namespace pr
 
 cudaError_t launch_prompt_rope(const PromptRopeParams& p, bool bf16, const RopeFreqs& freqs, int sms,
                                cudaStream_t stream) {
-  if (p.norms.q_weight != nullptr)
-    return bf16 ? pr::launch_typed<__nv_bfloat16, true>(p, freqs, sms, stream)
-                : pr::launch_typed<float, true>(p, freqs, sms, stream);
-  return bf16 ? pr::launch_typed<__nv_bfloat16, false>(p, freqs, sms, stream)
-              : pr::launch_typed<float, false>(p, freqs, sms, stream);
+  if (p.norms.q_weight != nullptr) return launch_prompt_norm_rope(p, bf16, freqs, sms, stream);
+  const int64_t es = bf16 ? 2 : 4;
+  const auto al16 = [](const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15u) == 0; };
+  const bool aligned = al16(p.q) && al16(p.k) && al16(p.v) && al16(p.q_out) && al16(p.k_layer) && al16(p.v_layer) &&
+                       (p.q_stride * es | p.k_stride * es | p.v_stride * es | p.q_out_stride * es) % 16 == 0;
+  const int vec = bf16 ? 8 : 4, half = p.head_dim / 2;
+  // (2^22 items a token: the bound of the kernel's quotients)
+  if (aligned && half % vec == 0 && ((int64_t)p.hq + 2 * (int64_t)p.hkv) * (half / vec) < (1 << 22)) {
+    const int chunks = half / vec, per_token = (p.hq + 2 * p.hkv) * chunks;
+    // While all CTAs have a place at once a token is done soonest by many threads, then small CTAs turn over best.
+    // Measured (us, 384 threads of one item each and 128 of three, bf16 with D = 128; SMs 152): 8 tokens of 32/8 heads
+    // 2.1 and 2.6, 300 2.9 and 4.0, 600 3.2 and 4.1, [the rule's bound] 620 4.2 and 4.5, 1000 5.0 and 4.6, 8192 37.3 and
+    // 31.5; of 64/8 heads 500 4.6 and 6.6, 8000 57.1 and 49.1; fp32 4000 31.8 and 30.3.
+    if (p.n_tokens <= 4 * (int64_t)sms)
+      return bf16 ? pr::launch<__nv_bfloat16, 384, 1, 4>(p, freqs, chunks, per_token, sms, stream)
+                  : pr::launch<float, 384, 1, 4>(p, freqs, chunks, per_token, sms, stream);
+    return bf16 ? pr::launch<__nv_bfloat16, 128, 3, 8>(p, freqs, chunks, per_token, sms, stream)
+                : pr::launch<float, 128, 3, 8>(p, freqs, chunks, per_token, sms, stream);
+  }
+  const auto kernel = bf16 ? pr::prompt_rope_scalar_kernel<__nv_bfloat16> : pr::prompt_rope_scalar_kernel<float>;
+  return launch_chained(kernel, dim3((unsigned)p.n_tokens), dim3(pr::kScalarThreads), 0, stream, 0, p, freqs);
 }
 
 }  // namespace ptd

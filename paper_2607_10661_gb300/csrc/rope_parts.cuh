@@ -7,6 +7,7 @@
 
 #include <cstdint>
 
+#include "ptd_device.cuh"
 #include "tree_rope.cuh"
 
 namespace ptd {
@@ -74,22 +75,111 @@ __device__ __forceinline__ void turn_of(const RopeFreqs& freqs, int pos, int j, 
   c = fmaf(-e, s0, c0);
 }
 
-// The norm of a head that lies across `lanes` lanes (a power of two, whole within its aligned group of lanes), each with
-// two vectors: 1 / sqrt(mean_D(x^2) + eps).  Every lane of the warp takes part; the lanes' sums meet pairwise, so that all
-// have the same.
+// Norm and rotation of a head in one: with r = 1 / sqrt(mean(x^2) + eps), weights w and the angle's (c, s), the pair (x, y) =
+// (x_j, x_{j+D/2}) becomes r (x w_j c - y w_{j+D/2} s), r (x w_j s + y w_{j+D/2} c).  The four products of weights and
+// angle do not depend on the head, so they are tables in shared memory: [4][D / 2] floats for the queries' weights, then the
+// same for the keys', the columns of a thread's vector in runs of four so that neighbouring lanes read neighbouring runs.
+constexpr int kNormTables = 8;   // of D / 2 floats: -w' s, w c, w s, w' c of the queries, of the keys
+
+// Column x of a table: of vector x / N, its element x % N.
 template <typename T>
-__device__ __forceinline__ float norm_of_head(const Vec<T>& x, const Vec<T>& y, int lanes, float inv_d, float eps) {
-  float s0 = 0.f, s1 = 0.f;
-#pragma unroll
-  for (int i = 0; i < Vec<T>::N; ++i) s0 = fmaf(x.x[i], x.x[i], s0), s1 = fmaf(y.x[i], y.x[i], s1);
-  float s = s0 + s1;
-  for (int o = lanes >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  return __frsqrt_rn(fmaf(s, inv_d, eps));
+__device__ __forceinline__ int norm_column(int x, int half) {
+  constexpr int N = 16 / (int)sizeof(T);
+  const int lane = x / N, c = x % N;
+  return N == 4 ? x : ((c >> 2) * (half / N) + lane) * 4 + (c & 3);
+}
+// The weights of column x (row pointers of the queries' and the keys'), and that column of both sets of tables at `table`.
+struct NormWeights {
+  float q_lo, q_hi, k_lo, k_hi;
+};
+template <typename T>
+__device__ __forceinline__ NormWeights load_norm_weights(const void* q_weight, const void* k_weight, size_t row, int x, int half) {
+  const T *q = static_cast<const T*>(q_weight) + row + x, *k = static_cast<const T*>(k_weight) + row + x;
+  return {ld(q), ld(q + half), ld(k), ld(k + half)};
 }
 template <typename T>
-__device__ __forceinline__ void scale_by(Vec<T>& x, float r, const Vec<T>& w) {
+__device__ __forceinline__ void make_norm_columns(float* table, const NormWeights& w, int x, int half, float c, float s) {
+  float* t = table + norm_column<T>(x, half);
+  t[0] = -w.q_hi * s;
+  t[half] = w.q_lo * c;
+  t[2 * half] = w.q_lo * s;
+  t[3 * half] = w.q_hi * c;
+  t[4 * half] = -w.k_hi * s;
+  t[5 * half] = w.k_lo * c;
+  t[6 * half] = w.k_lo * s;
+  t[7 * half] = w.k_hi * c;
+}
+
+// A 16-byte vector as packed pairs of fp32, and back.
+template <typename T>
+struct Pairs {
+  static constexpr int N = 8 / (int)sizeof(T);   // pairs
+  unsigned long long x[N];
+};
+template <typename T>
+__device__ __forceinline__ Pairs<T> unpack_pairs(const uint4& u) {
+  Pairs<T> r;
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-  for (int i = 0; i < Vec<T>::N; ++i) x.x[i] *= r * w.x[i];
+  for (int i = 0; i < Pairs<T>::N; ++i) {
+    if constexpr (sizeof(T) == 2)
+      r.x[i] = f2_pack(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+    else
+      r.x[i] = f2_pack(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+  }
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack_pairs(const Pairs<T>& r) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < Pairs<T>::N; ++i) {
+    float lo, hi;
+    f2_unpack(r.x[i], lo, hi);
+    if constexpr (sizeof(T) == 2) {
+      w[i] = pack_bf16x2(lo, hi);
+    } else {
+      w[2 * i] = __float_as_uint(lo), w[2 * i + 1] = __float_as_uint(hi);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// r of a head that lies across `lanes` lanes (a power of two, whole within its aligned group of lanes), each with two
+// vectors.  Every lane of the warp takes part; the lanes' sums meet pairwise, so that all have the same.
+template <typename T>
+__device__ __forceinline__ float norm_of_head(const uint4& lo, const uint4& hi, int lanes, float inv_d, float eps) {
+  const Pairs<T> x = unpack_pairs<T>(lo), y = unpack_pairs<T>(hi);
+  unsigned long long s2 = 0ull, t2 = 0ull;
+#pragma unroll
+  for (int i = 0; i < Pairs<T>::N; ++i) s2 = f2_fma(x.x[i], x.x[i], s2), t2 = f2_fma(y.x[i], y.x[i], t2);
+  float s0, s1;
+  f2_unpack(f2_add(s2, t2), s0, s1);
+  float s = s0 + s1;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    if (o < lanes) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return __frsqrt_rn(fmaf(s, inv_d, eps));
+}
+// The two vectors of columns j .. and j + D / 2 .. of a head, normed and turned in place; table: of the head's weights.
+template <typename T>
+__device__ __forceinline__ void norm_and_turn(uint4& lo, uint4& hi, float r, const float* table, int j, int half) {
+  const Pairs<T> x = unpack_pairs<T>(lo), y = unpack_pairs<T>(hi);
+  const float* t = table + norm_column<T>(j, half);
+  const unsigned long long r2 = f2_pack(r, r);
+  Pairs<T> a, b;
+#pragma unroll
+  for (int i = 0; i < Pairs<T>::N; i += 2) {   // a run of four columns
+    const float* run = t + (i >> 1) * (half / Pairs<T>::N / 2 * 4);
+    const ulonglong2 ns = *reinterpret_cast<const ulonglong2*>(run), c = *reinterpret_cast<const ulonglong2*>(run + half);
+    const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(run + 2 * half), d = *reinterpret_cast<const ulonglong2*>(run + 3 * half);
+    a.x[i] = f2_mul(r2, f2_fma(x.x[i], c.x, f2_mul(y.x[i], ns.x)));
+    b.x[i] = f2_mul(r2, f2_fma(x.x[i], s.x, f2_mul(y.x[i], d.x)));
+    a.x[i + 1] = f2_mul(r2, f2_fma(x.x[i + 1], c.y, f2_mul(y.x[i + 1], ns.y)));
+    b.x[i + 1] = f2_mul(r2, f2_fma(x.x[i + 1], s.y, f2_mul(y.x[i + 1], d.y)));
+  }
+  lo = pack_pairs<T>(a);
+  hi = pack_pairs<T>(b);
 }
 
 // Norm and rotation of a head's D elements by one warp, element by element (dst may be src: the warp has read the

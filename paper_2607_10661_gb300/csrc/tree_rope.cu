@@ -112,7 +112,8 @@ __global__ void __launch_bounds__(kThreads, kItems == 3 ? 4 : 5)
                      const int32_t* block_table, int max_pages, const __grid_constant__ RopeFreqs freqs,
                      int32_t* positions_out, int32_t* dev_status, GroupDivisor by_layer, GroupDivisor by_chunks) {
   __shared__ int par_s[kThreads];
-  __shared__ float cos_s[kMaxRopeHalf], sin_s[kMaxRopeHalf];
+  __shared__ float cos_s[kNorm ? 1 : kMaxRopeHalf], sin_s[kNorm ? 1 : kMaxRopeHalf];
+  extern __shared__ __align__(16) float norm_tables[];   // [layers][kNormTables][half]
   const int n = blockIdx.x, t = threadIdx.x;
   const int l0 = blockIdx.y * layers_per_cta;   // first layer of this CTA, relative to layer_begin
   const int layers = min(num_layers - l0, layers_per_cta);
@@ -157,7 +158,17 @@ __global__ void __launch_bounds__(kThreads, kItems == 3 ? 4 : 5)
                   l0 == 0, par_s, positions_out, dev_status, at))
     return;
   if (!at.fits) return;   // the node's slot is outside the cache: nothing is written
-  make_table(freqs, at.pos, half, cos_s, sin_s);
+  if constexpr (kNorm) {
+    for (int x = t; x < layers * half; x += kThreads) {
+      const int lq = x / half, j = x - lq * half;
+      const NormWeights w = load_norm_weights<T>(norms.q_weight, norms.k_weight, (size_t)(l0 + lq) * D, j, half);
+      float c, s;
+      turn_of(freqs, at.pos, j, c, s);
+      make_norm_columns<T>(norm_tables + lq * (kNormTables * half), w, j, half, c, s);
+    }
+  } else {
+    make_table(freqs, at.pos, half, cos_s, sin_s);
+  }
   __syncthreads();
   const size_t layer_rows = page_size > 0 ? (size_t)num_pages * page_size : (size_t)batch * seq_capacity;
   for (int e0 = t;; load_items(e0)) {
@@ -166,26 +177,25 @@ __global__ void __launch_bounds__(kThreads, kItems == 3 ? 4 : 5)
       const int e = e0 + u * kThreads;
       uint4 a = lo[u], b = hi[u];
       float norm = 1.f;
-      if constexpr (kNorm) norm = norm_of_head(unpack16<T>(a), unpack16<T>(b), chunks, inv_d, norms.eps);   // every lane
+      if constexpr (kNorm) norm = norm_of_head<T>(a, b, chunks, inv_d, norms.eps);   // every lane, in range or not
       if (e >= items) continue;
       int lq, h, j;
       place_of(e, lq, h, j);
       if (h < hq + hkv) {
-        Vec<T> x = unpack16<T>(a), y = unpack16<T>(b);
         if constexpr (kNorm) {
-          const T* w = static_cast<const T*>(h < hq ? norms.q_weight : norms.k_weight) + (size_t)(l0 + lq) * D + j;
-          scale_by(x, norm, unpack16<T>(__ldg(reinterpret_cast<const uint4*>(w))));
-          scale_by(y, norm, unpack16<T>(__ldg(reinterpret_cast<const uint4*>(w + half))));
-        }
-        Vec<T> rx, ry;
+          norm_and_turn<T>(a, b, norm, norm_tables + (lq * kNormTables + (h < hq ? 0 : 4)) * half, j, half);
+        } else {
+          const Vec<T> x = unpack16<T>(a), y = unpack16<T>(b);
+          Vec<T> rx, ry;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float c = cos_s[j + i], s = sin_s[j + i];
-          rx.x[i] = x.x[i] * c - y.x[i] * s;
-          ry.x[i] = x.x[i] * s + y.x[i] * c;
+          for (int i = 0; i < V; ++i) {
+            const float c = cos_s[j + i], s = sin_s[j + i];
+            rx.x[i] = x.x[i] * c - y.x[i] * s;
+            ry.x[i] = x.x[i] * s + y.x[i] * c;
+          }
+          a = pack16(rx);
+          b = pack16(ry);
         }
-        a = pack16(rx);
-        b = pack16(ry);
       }
       T* dst;
       if (h < hq) {
@@ -284,8 +294,10 @@ cudaError_t launch_typed(const int32_t* node_offsets, const int32_t* parents, co
     const bool five = ctas > slots && ctas_of(layers_of(2)) <= 5 * (int64_t)sms;
     if (five) layers = layers_of(2);
     if (ctas > 2 * slots) layers = layers_of(6);
+    const size_t table = kNorm ? kNormTables * (size_t)(head_dim / 2) * sizeof(float) : 0;   // of a layer; at most 4 KB
+    if (kNorm && layers * table > 46 * 1024) layers = (int)(46 * 1024 / table);
     const dim3 grid(n_total, (num_layers + layers - 1) / layers);
-    return launch_chained(five ? tree_rope_kernel<T, 2, kNorm> : tree_rope_kernel<T, 3, kNorm>, grid, dim3(kThreads), 0, stream, 0,
+    return launch_chained(five ? tree_rope_kernel<T, 2, kNorm> : tree_rope_kernel<T, 3, kNorm>, grid, dim3(kThreads), layers * table, stream, 0,
                           node_offsets, parents, ctx_lens, batch, n_total, num_layers, layers, head_dim, hq, hkv, q, q_out, k,
                           v, k_cache, v_cache, norms, layer_begin, page_size, seq_capacity, num_pages, block_table, max_pages,
                           freqs, positions_out, dev_status, group_divisor(per_layer), group_divisor(chunks));
