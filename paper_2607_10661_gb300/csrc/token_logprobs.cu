@@ -1,10 +1,16 @@
 // Log probabilities of given tokens, entropies and the k best alternatives of rows of logits: one read of them.
 //
-// A row is cut into contiguous parts, one CTA each, the parts of a row a cluster.  Every thread keeps the sums of
-// row_sums.cuh over its vectors, against the largest logit that it has seen: a batch of vectors in registers gives a
-// maximum, then the exponentials.  The alternatives are selected as in topk.cu (a threshold from the maxima of 32 groups of
-// lanes, the few elements at or above it read again from L2, each placed by counting the larger ones); the parts' sums and
-// keys go to the shared memory of the cluster's first CTA, which writes the row.
+// A row belongs to one CTA, or, where there are few rows, is cut into contiguous parts of 32 KB, one CTA of a cluster each.
+// Every thread keeps the sums of row_sums.cuh over its vectors, against the largest logit that it has seen: a batch of vectors
+// in registers gives a maximum, then the exponentials, while the next batch is on its way.  The alternatives: with T the k-th
+// largest of the maxima of 32 groups of lanes, k elements at least reach T, and few more; the vectors of the lanes whose maximum
+// does are read again (L2) by all threads, what reaches T goes to a buffer, and an element's place is the number of larger
+// ones in it.  A cluster's CTAs send their sums and keys to its first one, which writes the row.
+//
+// What bounds it: the one read, 1021 fp32 rows of 32000, k = 16 27.3 us in graph replays (4.8 TB/s; 23.2 with k = 0: a CTA's selection
+// takes some 1.5 us that its own reads do not overlap), 512 bf16 rows of 128256 30.2 (4.3 TB/s); for few rows the chain
+// of reads, exponentials, selection and merge: one row of 128256, k = 8 6.1 us, 63 rows, k = 4 9.1.  At first (no batch in
+// flight, the owners of candidates reading alone) 37.3, -, 7.2 and 11.1.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -24,16 +30,16 @@ namespace tl {
 
 using namespace topk;
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxParts = 8, kMaxK = 16;
 constexpr int kCand = 256;         // candidate buffer (keys)
 constexpr int kLoads = 4;          // vectors of a thread in flight
-constexpr int kCtas = 4;           // of an SM
+constexpr int kSmThreads = 1024;   // that an SM holds
 constexpr int kTargetVec = 2048;   // 32 KB: the part that the cluster size aims at
 
-template <typename T, bool kCluster>
-__global__ void __launch_bounds__(kThreads, kCtas) token_logprobs_kernel(const __grid_constant__ TokenLogprobsParams p) {
-  constexpr int VN = Vec<T>::kN;
+template <typename T, int kThreads, bool kCluster>
+__global__ void __launch_bounds__(kThreads, kSmThreads / kThreads)
+    token_logprobs_kernel(const __grid_constant__ TokenLogprobsParams p) {
+  constexpr int VN = Vec<T>::kN, kWarps = kThreads / 32, kGroup = kThreads / 32;   // lanes of one of the 32 groups
   __shared__ __align__(16) uint64_t cand_s[kCand];
   __shared__ __align__(16) uint64_t all_keys[kMaxParts * kMaxK];   // the parts' keys, in the cluster's first CTA
   __shared__ RowSums all_sums[kMaxParts];                          // and their sums
@@ -41,7 +47,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) token_logprobs_kernel(const _
   __shared__ __align__(8) uint64_t parts_bar_s;
   __shared__ uint64_t round_s[kWarps];
   __shared__ RowSums warp_sums[kWarps];
-  __shared__ uint8_t owners_s[kThreads];
+  __shared__ uint16_t owners_s[kThreads];
   __shared__ int n_cand_s, n_owners_s, abort_s;
 
   cg::cluster_group cluster = cg::this_cluster();
@@ -76,7 +82,16 @@ __global__ void __launch_bounds__(kThreads, kCtas) token_logprobs_kernel(const _
   const uint4* vrow = reinterpret_cast<const uint4*>(row + a0) + v_begin;
   const bool own_head = rank == 0 && tid == 0, own_tail = rank == parts - 1 && tid == kThreads - 1;
 
-  // 1. the sums; lane maxima, then of eight lanes
+  // the token's logit, asked for before the row (two dependent reads)
+  float token_logit = 0.f;
+  bool inside = false;
+  if (own_head) {
+    const int token = p.tokens[r];
+    inside = token >= 0 && token < p.vocab;
+    if (inside) token_logit = Vec<T>::scalar(row + token);
+  }
+
+  // 1. the sums; lane maxima, then of a group's lanes
   ThreadSums sums;
   float vmax = -INFINITY;   // of the vectors alone
   {
@@ -126,8 +141,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) token_logprobs_kernel(const _
     const bool has_elems = tid < nv || (own_head && a0 > 0) || (own_tail && a1 < p.vocab);
     uint32_t o = has_elems ? ordered_bits(sums.most) : 0u;
 #pragma unroll
-    for (int d = 1; d < 8; d <<= 1) o = max(o, __shfl_xor_sync(0xffffffffu, o, d));
-    if ((lane & 7) == 0) group_max_s[warp * 4 + (lane >> 3)] = o;
+    for (int d = 1; d < kGroup; d <<= 1) o = max(o, __shfl_xor_sync(0xffffffffu, o, d));
+    if ((lane & (kGroup - 1)) == 0) group_max_s[tid / kGroup] = o;
     const RowSums w = merge_lanes<32>(sums.sums(), p.scale);
     if (lane == 0) warp_sums[warp] = w;
   }
@@ -156,8 +171,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) token_logprobs_kernel(const _
         const float f = Vec<T>::scalar(row + i);
         if (f >= thr) push(f, (uint32_t)i);
       }
-    // the vectors of the lanes whose maximum reaches the threshold (about k of the 256), by all threads
-    if (vmax >= thr && tid < nv) owners_s[atomicAdd(&n_owners_s, 1)] = (uint8_t)tid;
+    // the vectors of the lanes whose maximum reaches the threshold (about k), by all threads
+    if (vmax >= thr && tid < nv) owners_s[atomicAdd(&n_owners_s, 1)] = (uint16_t)tid;
     __syncthreads();
     const int owners = n_owners_s, each = (nv + kThreads - 1) / kThreads, items = owners * each;
     for (int i0 = tid; i0 < items; i0 += kLoads * kThreads) {
@@ -207,8 +222,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) token_logprobs_kernel(const _
     p.top_val[r * k + at] = result.logprob(ord != 0u ? from_ordered(ord) : __int_as_float(0x7fffffff), p.inv_temperature);   // 0: NaN
   };
   auto write_row = [&](const RowResult& result) {
-    const int token = p.tokens[r];
-    p.logprob[r] = token >= 0 && token < p.vocab ? result.logprob(Vec<T>::scalar(row + token), p.inv_temperature) : -INFINITY;
+    p.logprob[r] = inside ? result.logprob(token_logit, p.inv_temperature) : -INFINITY;
     if (p.entropy != nullptr) p.entropy[r] = result.entropy;
   };
   if (k > 0) {
@@ -285,27 +299,29 @@ __global__ void __launch_bounds__(kThreads, kCtas) token_logprobs_kernel(const _
   }
 }
 
-// Parts of a row: 32 KB each, at most eight, and for many rows fewer (a power of two) while a part stays under 128 KB and
-// they are more than the CTAs that run at once.
-template <typename T>
-int row_parts(int vocab, int64_t rows, int sms) {
-  const int64_t by_size = ((int64_t)vocab / Vec<T>::kN + kTargetVec) / kTargetVec;
-  const int most = by_size > kMaxParts ? kMaxParts : (int)by_size;
-  const int64_t slots = (int64_t)kCtas * sms, bytes = (int64_t)vocab * (int64_t)sizeof(T);
-  if (rows * most <= slots) return most;
-  int parts = kMaxParts;
-  while (parts > 1 && (parts >= most || rows * parts > slots) && bytes / (parts / 2) <= 128000) parts /= 2;
-  return parts < most ? parts : most;
+template <typename T, int kThreads, bool kCluster>
+cudaError_t launch_as(TokenLogprobsParams p, int parts, cudaStream_t stream) {
+  p.per = (p.vocab / Vec<T>::kN + parts - 1) / parts;   // (rows off 16 bytes have one vector fewer)
+  const unsigned gy = (unsigned)(p.rows < 32768 ? p.rows : 32768), gz = (unsigned)((p.rows + gy - 1) / gy);
+  return launch_chained(token_logprobs_kernel<T, kThreads, kCluster>, dim3((unsigned)parts, gy, gz), dim3(kThreads), 0, stream,
+                        kCluster ? (unsigned)parts : 0u, p);
 }
 
 template <typename T>
-cudaError_t launch(TokenLogprobsParams p, int sms, cudaStream_t stream) {
-  const int parts = row_parts<T>(p.vocab, p.rows, sms);
-  p.per = (p.vocab / Vec<T>::kN + parts - 1) / parts;   // (rows off 16 bytes have one vector fewer)
-  const unsigned gy = (unsigned)(p.rows < 32768 ? p.rows : 32768), gz = (unsigned)((p.rows + gy - 1) / gy);
-  if (parts == 1)
-    return launch_chained(token_logprobs_kernel<T, false>, dim3(1, gy, gz), dim3(kThreads), 0, stream, 0, p);
-  return launch_chained(token_logprobs_kernel<T, true>, dim3((unsigned)parts, gy, gz), dim3(kThreads), 0, stream, (unsigned)parts, p);
+cudaError_t launch(const TokenLogprobsParams& p, int sms, cudaStream_t stream) {
+  int64_t parts = ((int64_t)p.vocab / Vec<T>::kN + kTargetVec) / kTargetVec;   // 32 KB each
+  if (parts > kMaxParts) parts = kMaxParts;
+  if (parts > 1 && p.rows * parts <= sms) return launch_as<T, 256, true>(p, (int)parts, stream);
+  // One CTA per row: the most threads with which the rows are less than two waves of CTAs (four where a row is 384 KB or more and
+  // its reads outweigh a CTA's fixed part), at most 512 and no more than its vectors, so that every group of lanes has some.  Measured (us with
+  // 1024 / 512 / 256 / 128 threads): 100 bf16 rows of 32000, k = 4 5.9 / 6.0 / 5.6 / 5.9; 300 of 50257 15.2 / 10.1 / 11.1 / 11.4;
+  // 512 of 128256, k = 8 40.2 / 30.2 / 30.4 / 50.0; 700 of 32000 25.7 / 15.4 / 11.9 / 15.2; 4096 of 32000 148 / 81.8 / 57.9 / 51.5;
+  // fp32, 1021 rows of 32000, k = 16 48.5 / 34.1 / 27.3 / 31.4; 894 of 128256 86.6 / 77.1 / 90.7 / 99.9; 2000 of 1000
+  // 54.7 / 26.1 / 14.6 / 8.4.  Clusters for more rows were slower: 1021 rows in two parts 36.9, in four 51.9.
+  const int64_t vectors = (int64_t)p.vocab / Vec<T>::kN, threads = 1792 * (int64_t)sms / p.rows * (vectors >= 24000 ? 2 : 1);
+  if (threads >= 512 && vectors >= 512) return launch_as<T, 512, false>(p, 1, stream);
+  if (threads >= 256 && vectors >= 256) return launch_as<T, 256, false>(p, 1, stream);
+  return launch_as<T, 128, false>(p, 1, stream);
 }
 
 }  // namespace tl
