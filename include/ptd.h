@@ -408,7 +408,8 @@ ptd_status ptd_token_logprobs(const void* logits, ptd_dtype dtype, int64_t rows,
 
 /* As ptd_token_logprobs of the logits h_r W^T, which never reach memory: hidden and weight as ptd_lm_head_topk takes them,
  * but any number of rows up to PTD_MAX_LOGPROB_ROWS (a prompt's tokens, a decoding batch).  Logits are accumulated in fp32 by
- * the tensor cores in an order of their own (see ptd_lm_head_topk); in a row with NaN the indices are unspecified.
+ * the tensor cores in an order of their own (see ptd_lm_head_topk).  Tokens with logits of -inf or NaN are no alternatives:
+ * where fewer than k are left, -1 and -inf (NaN in a row with NaN or +inf) follow.
  * workspace: ptd_lm_head_logprobs_workspace_size(rows, vocab, k) bytes (of the current device), 16-byte aligned, for the
  * parts of each row; it and the outputs overlap no input and not one another.  Two launches: the product, and the
  * merge of a row's parts. */

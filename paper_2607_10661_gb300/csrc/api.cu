@@ -1183,7 +1183,7 @@ ptd_status ptd_lm_head_logprobs(const void* hidden, int32_t rows, int64_t hidden
   const ptd::MemoryRows scratch[4] = {in[0], in[1], in[2], ptd::memory_rows(tokens, (int64_t)rows * 4)};
   if (written_rows_meet(scratch, 1, 4)) return PTD_ERR_INVALID_ARG;
   CUtensorMap map_h, map_w;
-  if (!encode_rows(&map_h, hidden, rows, d_model, hidden_stride, ptd::kLmTileRows) ||
+  if (!encode_rows(&map_h, hidden, rows, d_model, hidden_stride, plan.box_rows) ||
       !encode_rows(&map_w, weight, vocab, d_model, weight_stride, plan.tile_tokens))
     return PTD_ERR_CUDA;
   ptd::LmLogprobsParams p = {};

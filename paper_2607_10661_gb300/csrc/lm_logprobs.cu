@@ -26,7 +26,7 @@ constexpr uint32_t kTmemCols = 512;
 template <int kTile>   // tokens of a tile
 struct Smem {
   static constexpr int kStages = kTile == 256 ? 4 : 7;
-  static constexpr uint32_t kHBytes = kLmTileRows * 128, kWBytes = kTile * 128, kStageBytes = kHBytes + kWBytes;
+  static constexpr uint32_t kHBytes = kLmTileRows * 128, kWBytes = kTile * 128, kStageBytes = kHBytes + kWBytes;   // at most
   static constexpr uint32_t kOffBar = kStages * kStageBytes;
   static constexpr int kNumBars = 2 * kStages + 5;   // full, empty, acc_full[2], acc_empty[2], drain
   static constexpr uint32_t kOffTmemPtr = kOffBar + kNumBars * 8, kOffAbort = kOffTmemPtr + 4;
@@ -63,6 +63,48 @@ __device__ __forceinline__ void insert(uint64_t (&top)[KM], uint64_t key) {
     }
   }
 }
+
+// The best KM logits of a row that come in the order of their tokens: an equal logit that comes later stays behind.
+// Tokens of -inf (and NaN) are never taken.
+template <int KM>
+struct Best {
+  float x[KM > 0 ? KM : 1];   // descending, -inf: none
+  int token[KM > 0 ? KM : 1];
+
+  __device__ __forceinline__ Best() {
+#pragma unroll
+    for (int j = 0; j < KM; ++j) x[j] = -INFINITY, token[j] = 0;
+  }
+  __device__ __forceinline__ void insert(float v, int t) {
+#pragma unroll
+    for (int j = KM - 1; j >= 0; --j) {
+      const bool above = j > 0 && v > x[j > 0 ? j - 1 : 0], here = v > x[j];
+      token[j] = above ? token[j > 0 ? j - 1 : 0] : (here ? t : token[j]);
+      x[j] = j > 0 ? fmaxf(fminf(v, x[j > 0 ? j - 1 : 0]), x[j]) : fmaxf(v, x[j]);
+    }
+  }
+  // Takes what belongs here of 32 logits of tokens t0 ..., whose largest is `most` (v is used up): the largest that is left,
+  // its first place, again while some lane has one.  A row of n logits takes about KM ln(n / KM) of them.
+  __device__ __forceinline__ void take(float (&v)[32], float most, int t0) {
+    while (__any_sync(0xffffffffu, most > x[KM - 1])) {
+      int at = 0;
+#pragma unroll
+      for (int e = 31; e >= 0; --e) at = v[e] == most ? e : at;
+      if (most > x[KM - 1]) insert(most, t0 + at);
+#pragma unroll
+      for (int e = 0; e < 32; ++e) v[e] = e == at ? -INFINITY : v[e];
+      most = largest(v);
+    }
+  }
+  static __device__ __forceinline__ float largest(const float (&v)[32]) {
+    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int e = 0; e < 32; e += 8)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) m[q] = fmax3(m[q], v[e + 2 * q], v[e + 2 * q + 1]);
+    return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+  }
+};
 
 // The CTA's units, phase by phase: f(phase, row tile, first vocabulary tile, step).
 template <typename F>
@@ -133,7 +175,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int c = 0; c < n_chunks; ++c) {
             if (!(ok = mbar_wait(empty_bar(s), phase_bit, abort_flag, p.dev_status))) return false;
             const uint32_t dst = base + (uint32_t)s * S::kStageBytes;
-            mbar_arrive_expect_tx(full_bar(s), S::kStageBytes);
+            mbar_arrive_expect_tx(full_bar(s), (uint32_t)p.plan.box_rows * 128u + S::kWBytes);
             tma_load_2d(dst, &map_h, full_bar(s), c * 64, row_tile * kLmTileRows);
             tma_load_2d(dst + S::kHBytes, &map_w, full_bar(s), c * 64, tile * kTile);
             ++g;
@@ -190,51 +232,36 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int r = wq * 32 + lane, row = row_tile * kLmTileRows + r;
       const int token = row < p.rows ? p.tokens[row] : -1;
       ThreadSums sums;
-      uint64_t top[KM > 0 ? KM : 1];
-#pragma unroll
-      for (int j = 0; j < KM; ++j) top[j] = 0ull;
-      float worst = -INFINITY;   // of a full list
+      Best<KM> best;
+      const bool any_row = row - lane < p.rows;   // of the warp's rows
       for (; tile < vocab_tiles; tile += step, ++it) {
         const int buf = it & 1;
         if (!mbar_wait_warp(accf_bar(buf), (uint32_t)((it >> 1) & 1), abort_flag, p.dev_status)) return false;
         tc_fence_after();
         const int t0 = tile * kTile;
 #pragma unroll 1
-        for (int c0 = 0; c0 < kTile; c0 += 32) {
+        for (int c0 = 0; c0 < kTile && any_row; c0 += 32) {
           uint32_t v[32];
           tmem_ld32(tmem + lane_base + (uint32_t)(buf * kTile + c0), v);
           tmem_ld_wait();
           const int tb = t0 + c0;
-          if (tb + 32 > p.vocab) {   // rows of W past the last one were read as zeros
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (tb + e >= p.vocab) v[e] = 0xFF800000u;   // -inf
-          }
-          float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int e = 0; e < 32; e += 8)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              m[q] = fmax3(m[q], __uint_as_float(v[e + 2 * q]), __uint_as_float(v[e + 2 * q + 1]));
-          const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-          sums.raise(most, p.scale);
           float x[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
+          if (tb + 32 > p.vocab) {   // rows of W past the last one were read as zeros
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (tb + e >= p.vocab) x[e] = -INFINITY;
+          }
+          const float most = Best<KM>::largest(x);
+          sums.raise(most, p.scale);
           sums.add(x, scale2);
           if ((unsigned)(token - tb) < 32u) {
 #pragma unroll
             for (int e = 0; e < 32; ++e)
-              if (token == tb + e && token < p.vocab) parts.token_logit[row] = __uint_as_float(v[e]);
+              if (token == tb + e && token < p.vocab) parts.token_logit[row] = x[e];
           }
-          if constexpr (KM > 0) {
-            if (most > worst || top[KM - 1] == 0ull) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (tb + e < p.vocab) insert<KM>(top, topk::make_key(topk::ordered_bits(__uint_as_float(v[e])), (uint32_t)(tb + e)));
-              if (top[KM - 1] != 0ull) worst = topk::from_ordered((uint32_t)(top[KM - 1] >> 32));
-            }
-          }
+          if constexpr (KM > 0) best.take(x, most, tb);
         }
         tc_fence_before();
         __syncwarp();
@@ -244,7 +271,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const size_t at = ((size_t)phase * p.plan.ctas + blockIdx.x) * kLmTileRows + r;
         parts.sums[at] = sums.sums();
 #pragma unroll
-        for (int j = 0; j < KM; ++j) parts.keys[at * KM + j] = top[j];
+        for (int j = 0; j < KM; ++j)
+          parts.keys[at * KM + j] =
+              best.x[j] == -INFINITY ? 0ull : topk::make_key(topk::ordered_bits(best.x[j]), (uint32_t)best.token[j]);
       }
       return true;
     });
@@ -297,8 +326,9 @@ __global__ void __launch_bounds__(kMergeThreads) lm_logprobs_merge_kernel(const 
       top[KM - 1] = 0ull;
     }
     if (lane == 0 && j < p.k) {
-      p.top_idx[(size_t)row * p.k + j] = (int32_t)(~(uint32_t)best);
-      p.top_val[(size_t)row * p.k + j] = result.logprob(topk::from_ordered((uint32_t)(best >> 32)), p.inv_temperature);
+      p.top_idx[(size_t)row * p.k + j] = best != 0ull ? (int32_t)(~(uint32_t)best) : -1;
+      p.top_val[(size_t)row * p.k + j] =
+          result.logprob(best != 0ull ? topk::from_ordered((uint32_t)(best >> 32)) : -INFINITY, p.inv_temperature);
     }
   }
 }
@@ -325,6 +355,7 @@ LmLogprobsPlan plan_lm_logprobs(int rows, int vocab, int k, int sms) {
   LmLogprobsPlan plan;
   plan.row_tiles = (rows + kLmTileRows - 1) / kLmTileRows;
   plan.per_phase = sms < 8 ? sms : 8;
+  plan.box_rows = rows < kLmTileRows ? (rows + 7) / 8 * 8 : kLmTileRows;
   plan.tile_tokens = plan.row_tiles > 1 ? 256 : 128;
   plan.vocab_tiles = (vocab + plan.tile_tokens - 1) / plan.tile_tokens;
   plan.keys = k == 0 ? 0 : (k <= 4 ? 4 : (k <= 8 ? 8 : 16));
