@@ -1158,7 +1158,7 @@ ptd_status ptd_token_logprobs(const void* logits, ptd_dtype dtype, int64_t rows,
 
 size_t ptd_lm_head_logprobs_workspace_size(int32_t rows, int32_t vocab, int32_t k) {
   if (rows < 1 || rows > PTD_MAX_LOGPROB_ROWS || vocab < 1 || vocab > PTD_MAX_PROMPT_TOKENS || k < 0 || k > PTD_MAX_TOPK) return 0;
-  return ptd::lm_logprobs_workspace_bytes(ptd::plan_lm_logprobs(rows, vocab, k, num_sms_of_current_device()), rows);
+  return ptd::lm_logprobs_workspace_bytes(rows, vocab, k, num_sms_of_current_device());
 }
 
 ptd_status ptd_lm_head_logprobs(const void* hidden, int32_t rows, int64_t hidden_stride, const void* weight, int32_t vocab,
@@ -1172,8 +1172,10 @@ ptd_status ptd_lm_head_logprobs(const void* hidden, int32_t rows, int64_t hidden
       scale == 0.f || hidden_stride > (INT64_MAX >> 2) / rows || weight_stride > (INT64_MAX >> 2) / vocab)
     return PTD_ERR_INVALID_ARG;
   if (rows > PTD_MAX_LOGPROB_ROWS || vocab > PTD_MAX_PROMPT_TOKENS) return PTD_ERR_UNSUPPORTED;
-  const ptd::LmLogprobsPlan plan = ptd::plan_lm_logprobs(rows, vocab, k, num_sms_of_current_device());
-  const size_t need = ptd::lm_logprobs_workspace_bytes(plan, rows);
+  if (k < 0 || k > PTD_MAX_TOPK) return PTD_ERR_INVALID_ARG;
+  const int sms = num_sms_of_current_device();
+  const ptd::LmLogprobsPlan plan = ptd::plan_lm_logprobs(rows, vocab, d_model, k, sms);
+  const size_t need = ptd::lm_logprobs_workspace_bytes(rows, vocab, k, sms);
   const ptd::MemoryRows in[3] = {ptd::memory_rows(workspace, (int64_t)need),
                                  ptd::memory_rows(hidden, (int64_t)d_model * 2, hidden_stride * 2, rows),
                                  ptd::memory_rows(weight, (int64_t)d_model * 2, weight_stride * 2, vocab)};

@@ -1,7 +1,7 @@
 // Log probabilities of given tokens, entropies and best alternatives from hidden states: the LM-head product with the
 // softmax statistics of row_sums.cuh as its epilogue.  The logits never reach memory.
 //
-// Tiles of 128 rows of H by 256 (or 128) rows of W, one CTA per SM:
+// Tiles of 128 rows of H by 64 to 256 rows of W, one CTA per SM:
 //   warp 0     TMA producer: per 64 columns of d_model the tile's rows of H and of W, 128-byte swizzle, into a ring;
 //   warp 1     allocates TMEM, one thread issues the MMAs (M 128, K 16, bf16 -> fp32) into one of two accumulators;
 //   warps 2-5  epilogue: TMEM lane r holds row r's logits; thread r keeps its row's sums, its best alternatives
@@ -23,29 +23,35 @@ namespace ll {
 constexpr int kThreads = 192;
 constexpr uint32_t kTmemCols = 512;
 
-template <int kTile>   // tokens of a tile
-struct Smem {
-  static constexpr int kStages = kTile == 256 ? 4 : 7;
-  static constexpr uint32_t kHBytes = kLmTileRows * 128, kWBytes = kTile * 128, kStageBytes = kHBytes + kWBytes;   // at most
-  static constexpr uint32_t kOffBar = kStages * kStageBytes;
-  static constexpr int kNumBars = 2 * kStages + 5;   // full, empty, acc_full[2], acc_empty[2], drain
-  static constexpr uint32_t kOffTmemPtr = kOffBar + kNumBars * 8, kOffAbort = kOffTmemPtr + 4;
-  static constexpr uint32_t kBytes = kOffAbort + 16 + 1024;   // slack to align the base to 1024 B
-  static_assert(kBytes <= 232448, "shared memory budget");
-};
+// Shared memory: the ring (the plan's stages), then barriers.
+constexpr int kMostStages = 12;
+constexpr uint32_t kRingBytes = 222 * 1024;
+constexpr uint32_t kOffBar = kRingBytes;
+constexpr int kNumBars = 2 * kMostStages + 5;   // full, empty, acc_full[2], acc_empty[2], drain
+constexpr uint32_t kOffTmemPtr = kOffBar + kNumBars * 8, kOffAbort = kOffTmemPtr + 4;
+constexpr uint32_t kSmemBytes = kOffAbort + 16 + 1024;   // slack to align the base to 1024 B
+static_assert(kSmemBytes <= 232448, "shared memory budget");
+constexpr int kAccColumns = 256;   // of TMEM, of each accumulator
+
+// H of a stage: whole groups of eight rows, the swizzle's period.  The MMA reads 128 rows from there: behind the tile's last
+// one what the W of the stage (or the next stages', or the ring's last 16 KB) holds, for rows that nobody reads.
+__host__ __device__ constexpr uint32_t h_bytes(const LmLogprobsPlan& plan) { return (uint32_t)plan.box_rows * 128u; }
+__host__ __device__ constexpr uint32_t stage_bytes(const LmLogprobsPlan& plan) {
+  return h_bytes(plan) + (uint32_t)plan.tile_tokens * 128u;
+}
+
 // The parts of rows in the workspace: part (phase, cta) has 128 rows.
 struct Parts {
   RowSums* sums;
   uint64_t* keys;       // [part rows][KM]
   float* token_logit;   // [rows]
 };
-__host__ __device__ __forceinline__ Parts parts_of(void* workspace, const LmLogprobsPlan& plan, int rows) {
+__device__ __forceinline__ Parts parts_of(void* workspace, const LmLogprobsPlan& plan) {
   const size_t part_rows = (size_t)((plan.row_tiles + plan.per_phase - 1) / plan.per_phase) * plan.ctas * kLmTileRows;
   Parts p;
   p.keys = static_cast<uint64_t*>(workspace);
   p.sums = reinterpret_cast<RowSums*>(p.keys + part_rows * plan.keys);
   p.token_logit = reinterpret_cast<float*>(p.sums + part_rows);
-  (void)rows;
   return p;
 }
 
@@ -117,29 +123,28 @@ __device__ __forceinline__ void for_units(const LmLogprobsPlan& plan, F&& f) {
   }
 }
 
-template <int KM, int kTile>
+template <int KM>
 __global__ void __launch_bounds__(kThreads, 1)
     lm_logprobs_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_constant__ CUtensorMap map_w,
                        const __grid_constant__ LmLogprobsParams p) {
-  using S = Smem<kTile>;
-  constexpr int kStages = S::kStages;
-  constexpr uint32_t kIdesc = idesc_bf16_f32(kLmTileRows, kTile, 0, 0);
+  const int stages = p.plan.stages, tile_tokens = p.plan.tile_tokens;
+  const uint32_t stage = stage_bytes(p.plan), h = h_bytes(p.plan);
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint32_t base = smem_u32(smem_raw);
   const uint32_t pad = (1024u - (base & 1023u)) & 1023u;
   uint8_t* smem = smem_raw + pad;
   base += pad;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  auto bar = [&](int i) { return base + S::kOffBar + 8u * (uint32_t)i; };
+  auto bar = [&](int i) { return base + kOffBar + 8u * (uint32_t)i; };
   auto full_bar = [&](int s) { return bar(s); };
-  auto empty_bar = [&](int s) { return bar(kStages + s); };
-  auto accf_bar = [&](int b) { return bar(2 * kStages + b); };
-  auto acce_bar = [&](int b) { return bar(2 * kStages + 2 + b); };
-  const uint32_t drain_bar = bar(2 * kStages + 4);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::kOffAbort);
+  auto empty_bar = [&](int s) { return bar(kMostStages + s); };
+  auto accf_bar = [&](int b) { return bar(2 * kMostStages + b); };
+  auto acce_bar = [&](int b) { return bar(2 * kMostStages + 2 + b); };
+  const uint32_t drain_bar = bar(2 * kMostStages + 4);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kOffAbort);
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < stages; ++s) {
       mbar_init(full_bar(s), 1);
       mbar_init(empty_bar(s), 1);
     }
@@ -152,14 +157,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_mbar_init();
   }
   if (warp == 1) {
-    tmem_alloc(base + S::kOffTmemPtr, kTmemCols);
+    tmem_alloc(base + kOffTmemPtr, kTmemCols);
     tmem_relinquish();
     tc_fence_before();
   }
   grid_dependency_wait();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + S::kOffTmemPtr);
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + kOffTmemPtr);
   const int n_chunks = p.d_model / 64, vocab_tiles = p.plan.vocab_tiles;
 
   if (warp == 0) {
@@ -174,24 +179,25 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (; tile < vocab_tiles; tile += step) {
           for (int c = 0; c < n_chunks; ++c) {
             if (!(ok = mbar_wait(empty_bar(s), phase_bit, abort_flag, p.dev_status))) return false;
-            const uint32_t dst = base + (uint32_t)s * S::kStageBytes;
-            mbar_arrive_expect_tx(full_bar(s), (uint32_t)p.plan.box_rows * 128u + S::kWBytes);
+            const uint32_t dst = base + (uint32_t)s * stage;
+            mbar_arrive_expect_tx(full_bar(s), stage);
             tma_load_2d(dst, &map_h, full_bar(s), c * 64, row_tile * kLmTileRows);
-            tma_load_2d(dst + S::kHBytes, &map_w, full_bar(s), c * 64, tile * kTile);
+            tma_load_2d(dst + h, &map_w, full_bar(s), c * 64, tile * tile_tokens);
             ++g;
-            if (++s == kStages) s = 0, phase_bit ^= 1u;
+            if (++s == stages) s = 0, phase_bit ^= 1u;
           }
         }
         return true;
       });
       if (!ok) {   // let the copies already issued land before the CTA can exit
-        for (int back = 1; back <= kStages && g - back >= 0; ++back)
-          mbar_drain(full_bar((g - back) % kStages), (uint32_t)(((g - back) / kStages) & 1), 100000000ull);
+        for (int back = 1; back <= stages && g - back >= 0; ++back)
+          mbar_drain(full_bar((g - back) % stages), (uint32_t)(((g - back) / stages) & 1), 100000000ull);
       }
     }
   } else if (warp == 1) {
     // ================================================================ MMA issuer
     if (lane == 0) {
+      const uint32_t idesc = idesc_bf16_f32(kLmTileRows, tile_tokens, 0, 0);
       bool ok = true;
       int s = 0, it = 0;
       uint32_t phase_bit = 0;
@@ -200,17 +206,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int buf = it & 1;
           if (!(ok = mbar_wait(acce_bar(buf), (uint32_t)(((it >> 1) & 1) ^ 1), abort_flag, p.dev_status))) return false;
           tc_fence_after();
-          const uint32_t d = tmem + (uint32_t)(buf * kTile);
+          const uint32_t d = tmem + (uint32_t)(buf * kAccColumns);
           for (int c = 0; c < n_chunks; ++c) {
             if (!(ok = mbar_wait(full_bar(s), phase_bit, abort_flag, p.dev_status))) return false;
             tc_fence_after();
-            const uint32_t a0 = base + (uint32_t)s * S::kStageBytes, b0 = a0 + S::kHBytes;
+            const uint32_t a0 = base + (uint32_t)s * stage, b0 = a0 + h;
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
               mma_bf16_ss(d, smem_desc_sw128(a0 + (uint32_t)kk * 32u, 16, 1024), smem_desc_sw128(b0 + (uint32_t)kk * 32u, 16, 1024),
-                          kIdesc, (c > 0 || kk > 0) ? 1u : 0u);
+                          idesc, (c > 0 || kk > 0) ? 1u : 0u);
             mma_commit(empty_bar(s));   // the stage is free once these MMAs have read it
-            if (++s == kStages) s = 0, phase_bit ^= 1u;
+            if (++s == stages) s = 0, phase_bit ^= 1u;
           }
           mma_commit(accf_bar(buf));
         }
@@ -226,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int wq = warp & 3;                     // TMEM lane quarter of this warp
     const uint32_t lane_base = (uint32_t)(wq * 32) << 16;
     const unsigned long long scale2 = f2_pack(p.scale, p.scale);
-    const Parts parts = parts_of(p.workspace, p.plan, p.rows);
+    const Parts parts = parts_of(p.workspace, p.plan);
     int it = 0;
     for_units(p.plan, [&](int phase, int row_tile, int tile, int step) {
       const int r = wq * 32 + lane, row = row_tile * kLmTileRows + r;
@@ -238,11 +244,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int buf = it & 1;
         if (!mbar_wait_warp(accf_bar(buf), (uint32_t)((it >> 1) & 1), abort_flag, p.dev_status)) return false;
         tc_fence_after();
-        const int t0 = tile * kTile;
+        const int t0 = tile * tile_tokens;
 #pragma unroll 1
-        for (int c0 = 0; c0 < kTile && any_row; c0 += 32) {
+        for (int c0 = 0; c0 < tile_tokens && any_row; c0 += 32) {
           uint32_t v[32];
-          tmem_ld32(tmem + lane_base + (uint32_t)(buf * kTile + c0), v);
+          tmem_ld32(tmem + lane_base + (uint32_t)(buf * kAccColumns + c0), v);
           tmem_ld_wait();
           const int tb = t0 + c0;
           float x[32];
@@ -295,7 +301,7 @@ __global__ void __launch_bounds__(kMergeThreads) lm_logprobs_merge_kernel(const 
   grid_dependency_wait();
   const int row = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (row >= p.rows) return;
-  const Parts parts = parts_of(p.workspace, p.plan, p.rows);
+  const Parts parts = parts_of(p.workspace, p.plan);
   const int row_tile = row / kLmTileRows, phase = row_tile / p.plan.per_phase, t0 = phase * p.plan.per_phase;
   const int R = min(p.plan.per_phase, p.plan.row_tiles - t0), C = min(p.plan.ctas / R, p.plan.vocab_tiles);
   RowSums sums = {-INFINITY, 0.f, 0.f};
@@ -333,48 +339,78 @@ __global__ void __launch_bounds__(kMergeThreads) lm_logprobs_merge_kernel(const 
   }
 }
 
-template <int KM, int kTile>
+template <int KM>
 cudaError_t launch(const CUtensorMap& map_h, const CUtensorMap& map_w, const LmLogprobsParams& p, cudaStream_t stream) {
-  cudaError_t e = cudaFuncSetAttribute(lm_logprobs_kernel<KM, kTile>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       (int)Smem<kTile>::kBytes);
+  cudaError_t e = cudaFuncSetAttribute(lm_logprobs_kernel<KM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
   if (e != cudaSuccess) return e;
-  e = launch_chained(lm_logprobs_kernel<KM, kTile>, dim3(p.plan.ctas), dim3(kThreads), Smem<kTile>::kBytes, stream, 0, map_h, map_w, p);
+  e = launch_chained(lm_logprobs_kernel<KM>, dim3(p.plan.ctas), dim3(kThreads), kSmemBytes, stream, 0, map_h, map_w, p);
   if (e != cudaSuccess) return e;
   constexpr int kRows = kMergeThreads / 32;
   return launch_chained(lm_logprobs_merge_kernel<KM>, dim3((p.rows + kRows - 1) / kRows), dim3(kMergeThreads), 0, stream, 0, p);
 }
 
-template <int KM>
-cudaError_t launch_tile(const CUtensorMap& map_h, const CUtensorMap& map_w, const LmLogprobsParams& p, cudaStream_t stream) {
-  return p.plan.tile_tokens == 256 ? launch<KM, 256>(map_h, map_w, p, stream) : launch<KM, 128>(map_h, map_w, p, stream);
-}
-
 }  // namespace ll
 
-LmLogprobsPlan plan_lm_logprobs(int rows, int vocab, int k, int sms) {
+// Tokens of a tile, by what the phases would take.  Per 64 columns of d_model (ns, all SMs busy): the four MMAs 270 up to 192
+// tokens (the rows of H are read from shared memory anew for each), 291 with 224 and 340 with 256; W 128 bytes a token from
+// HBM, at 44.6 a ns and SM, once for the phase's row tiles; the lesser of the two hides but for some 15 %.  After a phase's last
+// tile its epilogue, some 35 ns a token.  GB300, d = 4096, 128256 tokens, us with 128 / 192 / 224 / 256 tokens: 63 rows 169 / 169 /
+// 166 / 171, 200 rows 254 / 189 / 184 / 196, 500 rows 477 / 330 / 305 / 322, 4096 rows 3678 / 2548 / 2251 / 2300; 5707 rows of
+// 10605 tokens, d = 2752 348 / 223 / 227 / 242; 2000 rows of 1000, d = 512 25.1 / 30.0 / 32.2 / 34.2 (with 64 19.7).
+constexpr int kLeastTile = 64;
+static int choose_tile_tokens(int row_tiles, int per_phase, int vocab, int d_model, int sms) {
+  int best = 0;
+  double least = 0.;
+  for (int tile = kLeastTile; tile <= 256; tile += 32) {
+    const int64_t vocab_tiles = ((int64_t)vocab + tile - 1) / tile;
+    const double mma = tile <= 192 ? 270. : (tile == 224 ? 291. : 340.);
+    double total = 0.;
+    const auto add = [&](int64_t phases, int R) {
+      const int64_t C = sms / R, rounds = (vocab_tiles + C - 1) / C;
+      const double load = tile * 128. / (44.6 * R), chunk = (mma > load ? mma : load) + 0.15 * (mma > load ? load : mma);
+      total += (double)phases * ((double)rounds * (d_model / 64) * chunk + 35. * tile);
+    };
+    add(row_tiles / per_phase, per_phase);
+    if (row_tiles % per_phase != 0) add(1, row_tiles % per_phase);
+    if (best == 0 || total < least) best = tile, least = total;
+  }
+  return best;
+}
+
+static LmLogprobsPlan make_plan(int rows, int vocab, int tile_tokens, int k, int sms) {
   LmLogprobsPlan plan;
   plan.row_tiles = (rows + kLmTileRows - 1) / kLmTileRows;
   plan.per_phase = sms < 8 ? sms : 8;
   plan.box_rows = rows < kLmTileRows ? (rows + 7) / 8 * 8 : kLmTileRows;
-  plan.tile_tokens = plan.row_tiles > 1 ? 256 : 128;
-  plan.vocab_tiles = (vocab + plan.tile_tokens - 1) / plan.tile_tokens;
+  plan.tile_tokens = tile_tokens;
+  plan.vocab_tiles = (vocab + tile_tokens - 1) / tile_tokens;
+  // the MMA reads 128 rows from the last stage's H too
+  const uint32_t stages = (ll::kRingBytes - (kLmTileRows - plan.box_rows) * 128u) / ll::stage_bytes(plan);
+  plan.stages = stages < (uint32_t)ll::kMostStages ? (int)stages : ll::kMostStages;
   plan.keys = k == 0 ? 0 : (k <= 4 ? 4 : (k <= 8 ? 8 : 16));
   const int64_t most = (int64_t)(plan.row_tiles < plan.per_phase ? plan.row_tiles : plan.per_phase) * plan.vocab_tiles;
   plan.ctas = most < sms ? (int)most : sms;
   return plan;
 }
 
-size_t lm_logprobs_workspace_bytes(const LmLogprobsPlan& plan, int rows) {
+LmLogprobsPlan plan_lm_logprobs(int rows, int vocab, int d_model, int k, int sms) {
+  const int row_tiles = (rows + kLmTileRows - 1) / kLmTileRows;
+  return make_plan(rows, vocab, choose_tile_tokens(row_tiles, sms < 8 ? sms : 8, vocab, d_model, sms), k, sms);
+}
+
+size_t lm_logprobs_workspace_bytes(int rows, int vocab, int k, int sms) {
+  // (of the plan with the most CTAs: the tile goes by d_model too)
+  const LmLogprobsPlan plan = make_plan(rows, vocab, kLeastTile, k, sms);
   const size_t part_rows = (size_t)((plan.row_tiles + plan.per_phase - 1) / plan.per_phase) * plan.ctas * kLmTileRows;
   return part_rows * (plan.keys * sizeof(uint64_t) + sizeof(RowSums)) + (size_t)rows * sizeof(float);
 }
 
 cudaError_t launch_lm_logprobs(const CUtensorMap& map_h, const CUtensorMap& map_w, const LmLogprobsParams& p, cudaStream_t stream) {
   switch (p.plan.keys) {
-    case 0: return ll::launch_tile<0>(map_h, map_w, p, stream);
-    case 4: return ll::launch_tile<4>(map_h, map_w, p, stream);
-    case 8: return ll::launch_tile<8>(map_h, map_w, p, stream);
-    default: return ll::launch_tile<16>(map_h, map_w, p, stream);
+    case 0: return ll::launch<0>(map_h, map_w, p, stream);
+    case 4: return ll::launch<4>(map_h, map_w, p, stream);
+    case 8: return ll::launch<8>(map_h, map_w, p, stream);
+    default: return ll::launch<16>(map_h, map_w, p, stream);
   }
 }
 

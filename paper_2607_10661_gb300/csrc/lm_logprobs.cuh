@@ -14,10 +14,11 @@ struct RowSums;
 struct LmLogprobsPlan {
   int ctas, row_tiles, per_phase, tile_tokens, vocab_tiles;
   int box_rows;   // rows of H that are loaded of a tile: a multiple of 8, the others of the tile are anything
+  int stages;     // of the ring
   int keys;       // kept of each row's part (>= k)
 };
-LmLogprobsPlan plan_lm_logprobs(int rows, int vocab, int k, int sms);
-size_t lm_logprobs_workspace_bytes(const LmLogprobsPlan& plan, int rows);
+LmLogprobsPlan plan_lm_logprobs(int rows, int vocab, int d_model, int k, int sms);
+size_t lm_logprobs_workspace_bytes(int rows, int vocab, int k, int sms);   // for any d_model
 
 struct LmLogprobsParams {
   int rows, d_model, vocab, k;
