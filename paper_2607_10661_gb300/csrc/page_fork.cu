@@ -340,13 +340,15 @@ cudaError_t launch_page_fork(const PageForkParams& p, int sms, cudaStream_t stre
   const size_t with_pages = sizes + ((size_t)p.from_batch + 2 * (size_t)p.num_pages) * sizeof(int);
   const bool one = with_pages <= kMostOneSmem && (int64_t)p.from_batch * p.max_pages <= 8192;
   const size_t smem = one ? with_pages : sizes;
+  cudaError_t e = cudaSuccess;
   if (smem > 47 * 1024) {   // the limits are the kernels', the same for every call
-    const cudaError_t e =
-        one ? cudaFuncSetAttribute(pf::page_fork_plan_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostOneSmem)
-            : cudaFuncSetAttribute(pf::page_fork_plan_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem);
+    if (one)
+      e = cudaFuncSetAttribute(pf::page_fork_plan_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostOneSmem);
+    else
+      e = cudaFuncSetAttribute(pf::page_fork_plan_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem);
     if (e != cudaSuccess) return e;
   }
-  const cudaError_t e = launch_chained(one ? pf::page_fork_plan_kernel<true> : pf::page_fork_plan_kernel<false>,
+  e = launch_chained(one ? pf::page_fork_plan_kernel<true> : pf::page_fork_plan_kernel<false>,
                                        dim3(one ? 1 : pf::kCtas), dim3(pf::kThreads), smem, stream, one ? 0 : pf::kCtas, p);
   if (e != cudaSuccess) return e;
   const int64_t page_bytes = p.row_bytes << p.page_log2;

@@ -78,6 +78,16 @@ struct Args {
     }
     return pointer(o);
   }
+  // as tensor_of, on the device of the tensors seen by on() (which tells a host tensor too)
+  void* tensor_on(PyObject* o, PyObject* dtype) {
+    on(o);
+    if (!ok) return nullptr;
+    if (!attr_true(o, s_is_contiguous, true) || (dtype != nullptr && dtype_of(o) != dtype)) {
+      fail();
+      return nullptr;
+    }
+    return pointer(o);
+  }
   void* tensor(PyObject* dtype = nullptr) {
     PyObject* o = next();
     return tensor_of(o, dtype);
@@ -176,9 +186,8 @@ struct Args {
   // a tensor of `count` elements of 32 bits, an int32 one
   void* word_of(PyObject* dtype, int64_t count) {
     PyObject* o = next();
-    void* p = tensor_of(o, dtype);
     if (!ok) return nullptr;
-    on(o);
+    void* p = tensor_on(o, dtype);
     PyObject* r = ok ? PyObject_GetAttr(o, s_nbytes) : nullptr;
     if (r == nullptr || !PyLong_CheckExact(r) || PyLong_AsLongLong(r) != 4 * count) fail();
     Py_XDECREF(r);
@@ -204,12 +213,11 @@ struct Args {
   // a contiguous tensor of `dtype`, of this shape
   void* shaped(PyObject* dtype, int n, const int64_t* want) {
     PyObject* o = next();
-    void* p = tensor_of(o, dtype);
     if (!ok) return nullptr;
+    void* p = tensor_on(o, dtype);
     int64_t d[4];
     if (dims(o, d) != n) ok = false;
     for (int i = 0; i < n; ++i) ok = ok && d[i] == want[i];
-    on(o);
     return p;
   }
   // log probabilities: tokens, out_logprob, out_entropy (or None), out_idx and out_val (or None) of `rows` rows
@@ -240,11 +248,11 @@ struct Args {
   // a [rows, heads, dim] tensor whose tokens may be apart, a token's heads back to back (*heads 0: any)
   void* rows3(PyObject* dtype, int64_t rows, int64_t dim, int64_t* heads, int64_t* stride) {
     PyObject* o = next();
-    if (!ok || (PyObject*)Py_TYPE(o) != g_tensor || !attr_true(o, s_is_cuda, false) || dtype_of(o) != dtype) {
+    on(o);   // (a host tensor has no device)
+    if (!ok || dtype_of(o) != dtype) {
       fail();
       return nullptr;
     }
-    on(o);
     PyObject* d = PyObject_GetAttr(o, s_shape);
     PyObject* s = PyObject_CallMethodNoArgs(o, s_stride);
     bool good = d != nullptr && s != nullptr && PyTuple_Check(d) && PyTuple_Check(s) && PyTuple_GET_SIZE(d) == 3 &&
@@ -702,8 +710,7 @@ PyObject* prompt_norm_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const void* qw = g.shaped(dt, 1, want);
   const void* kw = g.shaped(dt, 1, want);
   const float eps = g.real(), base = g.real();
-  g.on(a[13]);
-  int32_t* status = g.i32();
+  int32_t* status = static_cast<int32_t*>(g.tensor_on(g.next(), g_i32));
   g.on_attr(a[1], s_k);
   g.on_current();
   void* s = g.stream();
@@ -733,8 +740,7 @@ PyObject* tree_norm_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const void* qw = g.shaped(dt, 2, w_shape);
   const void* kw = g.shaped(dt, 2, w_shape);
   const float eps = g.real(), base = g.real();
-  g.on(a[11]);
-  int32_t* status = g.i32();
+  int32_t* status = static_cast<int32_t*>(g.tensor_on(g.next(), g_i32));
   int32_t* pos = a[12] == Py_None ? (g.next(), nullptr) : g.i32_of(tree->total_nodes);
   g.on_attr(a[0], s_ctx_lens);
   g.on_attr(a[1], s_k);
@@ -756,8 +762,7 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
   g.on(lg);
   if (!g.ok) Py_RETURN_NONE;
   const Args::Logprobs x = g.logprobs(rows);
-  g.on(a[6]);
-  int32_t* status = g.i32();
+  int32_t* status = static_cast<int32_t*>(g.tensor_on(g.next(), g_i32));
   const float temperature = g.real();
   g.on_current();
   void* s = g.stream();
@@ -782,8 +787,7 @@ PyObject* lm_head_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (a[7] == Py_None) Py_RETURN_NONE;
   g.on(a[7]);
   void* ws = g.optional(&wsb);
-  g.on(a[8]);
-  int32_t* status = g.i32();
+  int32_t* status = static_cast<int32_t*>(g.tensor_on(g.next(), g_i32));
   const float temperature = g.real();
   g.on_current();
   void* s = g.stream();
@@ -819,8 +823,7 @@ PyObject* page_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (a[5] == Py_None) Py_RETURN_NONE;
   g.on(a[5]);
   void* ws = g.optional(&wsb);
-  g.on(a[6]);
-  int32_t* status = g.i32();
+  int32_t* status = static_cast<int32_t*>(g.tensor_on(g.next(), g_i32));
   g.on_attr(a[0], s_k);
   g.on_current();
   void* s = g.stream();
