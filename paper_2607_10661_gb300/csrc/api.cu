@@ -720,26 +720,18 @@ int64_t cache_bytes(const ptd_kv_cache* c, int batch, int layers) {
 }
 int64_t table_bytes(const ptd_kv_cache* c, int batch) { return c->page_size > 0 ? (int64_t)batch * c->max_pages * 4 : 0; }
 
-// ptd_tree_rope_append (no weights, q_out is q) and ptd_tree_norm_rope_append.
-ptd_status tree_rope_append(const ptd_tree* tree, const ptd_kv_cache* cache, int32_t layer_begin, int32_t num_layers,
-                            const void* q, int32_t num_q_heads, const void* k, const void* v, const ptd::HeadNorms& norms,
-                            float rope_base, void* q_out, int32_t* positions_out, int32_t* dev_status, void* stream) {
+// Host checks of both tree appends (no launch).
+ptd_status check_tree_append(const ptd_kv_cache* cache, int32_t layer_begin, int32_t num_layers, const void* q, int32_t num_q_heads,
+                             const void* k, const void* v, float rope_base, const int32_t* dev_status) {
   const int D = cache->head_dim, hkv = cache->num_kv_heads;
   if (layer_begin < 0 || num_layers < 1 || num_layers > 65535 || layer_begin + num_layers > cache->num_layers ||
       num_q_heads < hkv || num_q_heads % hkv != 0 || D % 2 != 0 ||
       D / 2 > ptd::kMaxRopeHalf || !q || !k || !v || !dev_status || !(rope_base > 1.f) || !std::isfinite(rope_base))
     return PTD_ERR_INVALID_ARG;
   const size_t es = dtype_size(cache->dtype);
-  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) |
-       reinterpret_cast<uintptr_t>(q_out)) % es != 0)
-    return PTD_ERR_INVALID_ARG;
-  const ptd_status st = cuda_status(ptd::launch_tree_rope(
-      tree->node_offsets, tree->parents, tree->ctx_lens, tree->batch, tree->total_nodes, cache->dtype == PTD_BF16, D,
-      num_q_heads, hkv, q, q_out, k, v, norms, cache->k, cache->v, layer_begin, num_layers, cache->page_size,
-      cache->seq_capacity, cache->num_pages, cache->block_table, cache->max_pages, rope_freqs(rope_base, D), positions_out,
-      dev_status, num_sms_of_current_device(), static_cast<cudaStream_t>(stream)));
-  if (st == PTD_OK) g_last_launches = 1;
-  return st;
+  return (reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) % es == 0
+             ? PTD_OK
+             : PTD_ERR_INVALID_ARG;
 }
 }  // namespace
 
@@ -750,8 +742,17 @@ ptd_status ptd_tree_rope_append(const ptd_tree* tree, const ptd_kv_cache* cache,
   ptd_status st = check_tree(tree);
   if (st != PTD_OK) return st;
   if ((st = check_cache(cache)) != PTD_OK) return st;
-  return tree_rope_append(tree, cache, layer_begin, num_layers, q, num_q_heads, k, v, ptd::HeadNorms{}, rope_base, q,
-                          positions_out, dev_status, stream);
+  if ((st = check_tree_append(cache, layer_begin, num_layers, q, num_q_heads, k, v, rope_base, dev_status)) != PTD_OK) return st;
+  const int D = cache->head_dim;
+  st = cuda_status(ptd::launch_tree_rope(tree->node_offsets, tree->parents, tree->ctx_lens, tree->batch,
+                                         tree->total_nodes, cache->dtype == PTD_BF16, D, num_q_heads, cache->num_kv_heads, q, k, v,
+                                         cache->k, cache->v, layer_begin, num_layers, cache->page_size,
+                                         cache->seq_capacity,
+                                         cache->num_pages, cache->block_table, cache->max_pages, rope_freqs(rope_base, D), positions_out,
+                                         dev_status, num_sms_of_current_device(),
+                                         static_cast<cudaStream_t>(stream)));
+  if (st == PTD_OK) g_last_launches = 1;
+  return st;
 }
 
 ptd_status ptd_tree_norm_rope_append(const ptd_tree* tree, const ptd_kv_cache* cache, int32_t layer_begin,
@@ -763,8 +764,8 @@ ptd_status ptd_tree_norm_rope_append(const ptd_tree* tree, const ptd_kv_cache* c
   if (st != PTD_OK) return st;
   if ((st = check_cache(cache)) != PTD_OK) return st;
   const int64_t es = (int64_t)dtype_size(cache->dtype), D = cache->head_dim, L = num_layers, N = tree->total_nodes;
-  if (!q_out || !norms_ok(q_weight, k_weight, eps, es) || num_layers < 1 || num_layers > 65535 || num_q_heads < 1)
-    return PTD_ERR_INVALID_ARG;
+  if ((st = check_tree_append(cache, layer_begin, num_layers, q, num_q_heads, k, v, rope_base, dev_status)) != PTD_OK) return st;
+  if (!q_out || reinterpret_cast<uintptr_t>(q_out) % es != 0 || !norms_ok(q_weight, k_weight, eps, es)) return PTD_ERR_INVALID_ARG;
   if (((int64_t)num_q_heads + 2 * (int64_t)cache->num_kv_heads) * D > INT32_MAX) return PTD_ERR_UNSUPPORTED;   // a node's elements
   // what is written overlaps nothing else that the call touches: other CTAs still read it
   const int64_t qb = L * N * num_q_heads * D * es, kb = L * N * cache->num_kv_heads * D * es;
@@ -777,8 +778,36 @@ ptd_status ptd_tree_norm_rope_append(const ptd_tree* tree, const ptd_kv_cache* c
                                     memory_rows(tree->parents, N * 4), memory_rows(tree->ctx_lens, (int64_t)tree->batch * 4),
                                     memory_rows(cache->block_table, table_bytes(cache, tree->batch))};
   if (written_rows_meet(rows, 5, 14)) return PTD_ERR_INVALID_ARG;
-  return tree_rope_append(tree, cache, layer_begin, num_layers, q, num_q_heads, k, v, ptd::HeadNorms{q_weight, k_weight, eps},
-                          rope_base, q_out, positions_out, dev_status, stream);
+  ptd::TreeNormRopeParams p = {};
+  p.node_offsets = tree->node_offsets;
+  p.parents = tree->parents;
+  p.ctx_lens = tree->ctx_lens;
+  p.batch = tree->batch;
+  p.n_total = tree->total_nodes;
+  p.num_layers = num_layers;
+  p.head_dim = cache->head_dim;
+  p.hq = num_q_heads;
+  p.hkv = cache->num_kv_heads;
+  p.q = q;
+  p.q_out = q_out;
+  p.k = k;
+  p.v = v;
+  p.norms = {q_weight, k_weight, eps};
+  p.layer_rows = cache_rows_per_layer(cache, tree->batch);
+  const size_t layers_before = (size_t)layer_begin * p.layer_rows * cache->num_kv_heads * D * es;
+  p.k_cache = static_cast<uint8_t*>(cache->k) + layers_before;
+  p.v_cache = static_cast<uint8_t*>(cache->v) + layers_before;
+  p.page_size = cache->page_size;
+  p.seq_capacity = cache->seq_capacity;
+  p.num_pages = cache->num_pages;
+  p.max_pages = cache->max_pages;
+  p.block_table = cache->block_table;
+  p.positions_out = positions_out;
+  p.dev_status = dev_status;
+  st = cuda_status(ptd::launch_tree_norm_rope(p, cache->dtype == PTD_BF16, rope_freqs(rope_base, cache->head_dim),
+                                              num_sms_of_current_device(), static_cast<cudaStream_t>(stream)));
+  if (st == PTD_OK) g_last_launches = 1;
+  return st;
 }
 
 namespace {

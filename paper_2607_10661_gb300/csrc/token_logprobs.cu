@@ -1,15 +1,15 @@
 // Log probabilities of given tokens, entropies and the k best alternatives of rows of logits: one read of them.
 //
-// A row belongs to one CTA, or, where there are few rows, is cut into contiguous parts of 32 KB, one CTA of a cluster each.
+// A row belongs to one CTA, or, where there are few long rows, is cut into contiguous parts, one CTA of a cluster each.
 // Every thread keeps the sums of row_sums.cuh over its vectors, against the largest logit that it has seen: a batch of vectors
 // in registers gives a maximum, then the exponentials, while the next batch is on its way.  The alternatives: with T the k-th
 // largest of the maxima of 32 groups of lanes, k elements at least reach T, and few more; the vectors of the lanes whose maximum
 // does are read again (L2) by all threads, what reaches T goes to a buffer, and an element's place is the number of larger
 // ones in it.  A cluster's CTAs send their sums and keys to its first one, which writes the row.
 //
-// What bounds it: the one read, 1021 fp32 rows of 32000, k = 16 27.3 us in graph replays (4.8 TB/s; 23.2 with k = 0: a CTA's selection
-// takes some 1.5 us that its own reads do not overlap), 512 bf16 rows of 128256 30.2 (4.3 TB/s); for few rows the chain
-// of reads, exponentials, selection and merge: one row of 128256, k = 8 6.1 us, 63 rows, k = 4 9.1.  At first (no batch in
+// What bounds it: the one read, 1021 fp32 rows of 32000, k = 16 25.7 us in graph replays (5.1 TB/s; some 22 with k = 0: a CTA's selection
+// takes some 1.5 us that its own reads do not overlap), 512 bf16 rows of 128256 29.6 (4.4 TB/s); for few rows the chain
+// of reads, exponentials, selection and merge: one row of 128256, k = 8 6.0 us, 63 rows, k = 4 8.7.  At first (no batch in
 // flight, the owners of candidates reading alone) 37.3, -, 7.2 and 11.1.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -34,7 +34,6 @@ constexpr int kMaxParts = 8, kMaxK = 16;
 constexpr int kCand = 256;         // candidate buffer (keys)
 constexpr int kLoads = 4;          // vectors of a thread in flight
 constexpr int kSmThreads = 1024;   // that an SM holds
-constexpr int kTargetVec = 2048;   // 32 KB: the part that the cluster size aims at
 
 template <typename T, int kThreads, bool kCluster>
 __global__ void __launch_bounds__(kThreads, kSmThreads / kThreads)
@@ -310,16 +309,19 @@ cudaError_t launch_as(TokenLogprobsParams p, int parts, cudaStream_t stream) {
 
 template <typename T>
 cudaError_t launch(const TokenLogprobsParams& p, int sms, cudaStream_t stream) {
-  int64_t parts = ((int64_t)p.vocab / Vec<T>::kN + kTargetVec) / kTargetVec;   // 32 KB each
-  if (parts > kMaxParts) parts = kMaxParts;
-  if (parts > 1 && p.rows * parts <= sms) return launch_as<T, 256, true>(p, (int)parts, stream);
+  // Long rows that are few: a cluster each, while every CTA has an SM.  Measured (us in 8, in 4 parts of 256 threads, in one of
+  // 512; bf16 rows of 128256, k = 4): 1 row 5.8 / 6.2 / 8.6, 19 rows 6.6 / 6.4 / 8.8, 32 rows 7.5 / 7.2 / 8.8, 63 rows 9.0 /
+  // 8.8 / 8.8; rows of 32000: 1 row 5.3 / 5.1 / 4.8, 19 rows 5.9 / 5.4 / 4.9.
+  const int64_t vectors = (int64_t)p.vocab / Vec<T>::kN;
+  for (int parts = kMaxParts; vectors >= 8192 && parts >= 4; parts /= 2)
+    if (p.rows * parts <= sms) return launch_as<T, 256, true>(p, parts, stream);
   // One CTA per row: the most threads with which the rows are less than two waves of CTAs (four where a row is 384 KB or more and
   // its reads outweigh a CTA's fixed part), at most 512 and no more than its vectors, so that every group of lanes has some.  Measured (us with
   // 1024 / 512 / 256 / 128 threads): 100 bf16 rows of 32000, k = 4 5.9 / 6.0 / 5.6 / 5.9; 300 of 50257 15.2 / 10.1 / 11.1 / 11.4;
   // 512 of 128256, k = 8 40.2 / 30.2 / 30.4 / 50.0; 700 of 32000 25.7 / 15.4 / 11.9 / 15.2; 4096 of 32000 148 / 81.8 / 57.9 / 51.5;
   // fp32, 1021 rows of 32000, k = 16 48.5 / 34.1 / 27.3 / 31.4; 894 of 128256 86.6 / 77.1 / 90.7 / 99.9; 2000 of 1000
   // 54.7 / 26.1 / 14.6 / 8.4.  Clusters for more rows were slower: 1021 rows in two parts 36.9, in four 51.9.
-  const int64_t vectors = (int64_t)p.vocab / Vec<T>::kN, threads = 1792 * (int64_t)sms / p.rows * (vectors >= 24000 ? 2 : 1);
+  const int64_t threads = 1792 * (int64_t)sms / p.rows * (vectors >= 24000 ? 2 : 1);
   if (threads >= 512 && vectors >= 512) return launch_as<T, 512, false>(p, 1, stream);
   if (threads >= 256 && vectors >= 256) return launch_as<T, 256, false>(p, 1, stream);
   return launch_as<T, 128, false>(p, 1, stream);
