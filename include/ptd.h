@@ -398,7 +398,7 @@ ptd_status ptd_lm_head_topk(const void* hidden, int32_t rows, int64_t hidden_str
  *   out_idx [rows][k] int32, out_val [rows][k] fp32: the k most probable tokens, in ptd_topk_draft's order (the lower one
  *     first on equal logits), and their log p; k in 0 .. PTD_MAX_TOPK (with 0 both may be NULL), at most vocab.
  * logits [rows][row_stride] bf16 or fp32, aligned to their elements; sums and exponentials in fp32: a log probability is
- * within 2^-20 (1 + entropy + max z - z) of the exact one.  A logit of -inf (a masked token) has probability 0; a row of
+ * within (2^-20 + vocab 2^-35) (1 + entropy + max z - z) of the exact one.  A logit of -inf (a masked token) has probability 0; a row of
  * nothing else has log probabilities -inf and entropy 0.  A row with NaN or +inf has NaN for all but tokens
  * outside the vocabulary.  The outputs overlap no input and not one another
  * (PTD_ERR_INVALID_ARG).  temperature finite, > 0.  rows and vocab at most PTD_MAX_PROMPT_TOKENS.  One launch. */
@@ -408,7 +408,7 @@ ptd_status ptd_token_logprobs(const void* logits, ptd_dtype dtype, int64_t rows,
 
 /* As ptd_token_logprobs of the logits h_r W^T, which never reach memory: hidden and weight as ptd_lm_head_topk takes them,
  * but any number of rows up to PTD_MAX_LOGPROB_ROWS (a prompt's tokens, a decoding batch).  Logits are accumulated in fp32 by
- * the tensor cores in an order of their own (see ptd_lm_head_topk).  Tokens with logits of -inf or NaN are no alternatives:
+ * the tensor cores in an order of their own (see ptd_lm_head_topk), then summed as there with vocab 2^-33 in the bound.  Tokens with logits of -inf or NaN are no alternatives:
  * where fewer than k are left, -1 and -inf (NaN in a row with NaN or +inf) follow.
  * workspace: ptd_lm_head_logprobs_workspace_size(rows, vocab, k) bytes (of the current device), 16-byte aligned, for the
  * parts of each row; it and the outputs overlap no input and not one another.  Two launches: the product, and the
@@ -617,8 +617,8 @@ typedef struct {
  * `from` is not written: a call on the same state writes the same.  What is written (the buffers of `to`, the cache, the
  * workspace, dev_status) overlaps nothing else (PTD_ERR_INVALID_ARG).  Sizes, parents or page numbers out of range
  * (lens[b] beyond the pages held among them) set PTD_ERR_INVALID_BATCH, too few free pages PTD_ERR_NO_PAGES: then
- * to->held and to->free_count are zeros and nothing else of `to` or the cache is written.  Pages that are both held and free
- * give unspecified results.
+ * to->held and to->free_count are zeros and nothing else of `to` or the cache is written.  Pages that are both held and free,
+ * or twice in a row or on the stack, give unspecified results (nothing outside the buffers is touched).
  *   cache: its k, v and sizes; its block_table is not read.  A layer has fewer than 2^31 rows.
  *   workspace: ptd_page_fork_workspace_size bytes, 16-byte aligned, in any state.
  * Two launches: the plan, and the copies. */

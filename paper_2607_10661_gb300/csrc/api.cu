@@ -1246,7 +1246,12 @@ ptd_status check_page_sets(const ptd_kv_cache* cache, const ptd_page_set* from, 
     if (s->batch < 1 || !s->block_table || !s->held || !s->free_pages || !s->free_count) return PTD_ERR_INVALID_ARG;
     if (s->batch > PTD_MAX_PROMPT_BATCH || (int64_t)s->batch * cache->max_pages > INT32_MAX) return PTD_ERR_UNSUPPORTED;
   }
-  return cache_rows_per_layer(cache, 1) > INT32_MAX || cache->num_pages > PTD_MAX_PROMPT_TOKENS / 2 ? PTD_ERR_UNSUPPORTED : PTD_OK;
+  // rows of a layer, and chunks of copied pages, are counted in an int
+  const int64_t page_bytes = (int64_t)cache->page_size * cache->num_kv_heads * cache->head_dim * (int64_t)dtype_size(cache->dtype);
+  return cache_rows_per_layer(cache, 1) > INT32_MAX || cache->num_pages > PTD_MAX_PROMPT_TOKENS / 2 ||
+                 (int64_t)to->batch * ptd::page_copy_chunks(page_bytes) > INT32_MAX
+             ? PTD_ERR_UNSUPPORTED
+             : PTD_OK;
 }
 }  // namespace
 

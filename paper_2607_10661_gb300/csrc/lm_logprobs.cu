@@ -7,6 +7,14 @@
 //   warps 2-5  epilogue: TMEM lane r holds row r's logits; thread r keeps its row's sums, its best alternatives
 //              (64-bit keys: value, then the lower token) and its token's logit over the CTA's tiles of a phase.
 // A second kernel merges the parts that a row's CTAs left in the workspace.
+//
+// What bounds it: for many rows the tensor pipe and the power cap, 4096 rows of 4096 columns by 128256 tokens 2.23 ms in graph
+// replays (1.93 PFLOP/s; 2.35 - 2.44 ms, 1.76 - 1.83 PFLOP/s, among other passes); for up to a tile of rows the one read of W, 63 rows
+// 162.6 us (6.46 TB/s, 156 of it the product at 6.75), the merge and its launch the rest.  An MMA reads its 128 rows of H from
+// shared memory whatever the tile's width, some 68 ns: tiles narrower than 224 tokens leave the pipe waiting.  Steps (us, 63
+// rows with k = 8, 4096 with k = 4): tiles of 128 / 256 tokens, every logit of a block inserted where one might belong 174, 2320
+// (4096 rows with k = 16 4940); the block's largest taken while it belongs, only the rows of H there are 168, 2300 (2374); tile
+// by cost 166, 2240; four warps a row in the merge 162.6.
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -292,51 +300,81 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-// A warp per row: each lane merges some of the row's parts, then KM rounds of a warp-wide maximum (the owning lane pops its head).
+// kWarps warps per row: each lane merges some of the row's parts, a warp its lanes' by KM rounds of a warp-wide maximum (the owning
+// lane pops its head), the first warp the warps'.
 constexpr int kMergeThreads = 128;
 
 template <int KM>
-__global__ void __launch_bounds__(kMergeThreads) lm_logprobs_merge_kernel(const __grid_constant__ LmLogprobsParams p) {
-  if (threadIdx.x == 0) grid_launch_dependents();
-  grid_dependency_wait();
-  const int row = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (row >= p.rows) return;
-  const Parts parts = parts_of(p.workspace, p.plan);
-  const int row_tile = row / kLmTileRows, phase = row_tile / p.plan.per_phase, t0 = phase * p.plan.per_phase;
-  const int R = min(p.plan.per_phase, p.plan.row_tiles - t0), C = min(p.plan.ctas / R, p.plan.vocab_tiles);
-  RowSums sums = {-INFINITY, 0.f, 0.f};
-  uint64_t top[KM > 0 ? KM : 1];
-#pragma unroll
-  for (int j = 0; j < KM; ++j) top[j] = 0ull;
-  for (int c = lane; c < C; c += 32) {
-    const size_t at = ((size_t)phase * p.plan.ctas + c * R + (row_tile - t0)) * kLmTileRows + row % kLmTileRows;
-    sums = merge_sums(sums, parts.sums[at], p.scale);
-    uint64_t list[KM > 0 ? KM : 1];   // read together: an insertion may end early, and the next load would wait for it
-#pragma unroll
-    for (int j = 0; j < KM; ++j) list[j] = parts.keys[at * KM + j];
-#pragma unroll
-    for (int j = 0; j < KM; ++j) insert(top, list[j]);
-  }
-  const RowResult result(merge_lanes<32>(sums, p.scale));
-  if (lane == 0) {
-    const int token = p.tokens[row];
-    p.logprob[row] = token >= 0 && token < p.vocab ? result.logprob(parts.token_logit[row], p.inv_temperature) : -INFINITY;
-    if (p.entropy != nullptr) p.entropy[row] = result.entropy;
-  }
+__device__ __forceinline__ void warp_top(uint64_t (&top)[KM > 0 ? KM : 1], uint64_t (&out)[KM > 0 ? KM : 1]) {
 #pragma unroll
   for (int j = 0; j < KM; ++j) {
     const uint64_t best = topk::warp_max_u64(top[0]);
+    out[j] = best;
     if (best != 0ull && top[0] == best) {   // keys are distinct
 #pragma unroll
       for (int q = 0; q < KM - 1; ++q) top[q] = top[q + 1];
       top[KM - 1] = 0ull;
     }
-    if (lane == 0 && j < p.k) {
-      p.top_idx[(size_t)row * p.k + j] = best != 0ull ? (int32_t)(~(uint32_t)best) : -1;
-      p.top_val[(size_t)row * p.k + j] =
-          result.logprob(best != 0ull ? topk::from_ordered((uint32_t)(best >> 32)) : -INFINITY, p.inv_temperature);
-    }
   }
+}
+
+template <int KM, int kWarps>
+__global__ void __launch_bounds__(kMergeThreads) lm_logprobs_merge_kernel(const __grid_constant__ LmLogprobsParams p) {
+  constexpr int kList = KM > 0 ? KM : 1, kRowWarps = kMergeThreads / 32 / kWarps;   // rows of a CTA
+  __shared__ RowSums sums_s[kWarps];
+  __shared__ uint64_t keys_s[kWarps * kList];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int row = kWarps > 1 ? (int)blockIdx.x : (int)blockIdx.x * kRowWarps + warp;
+  if (threadIdx.x == 0) grid_launch_dependents();
+  grid_dependency_wait();
+  if (row >= p.rows) return;   // (a whole CTA where its warps share a row)
+  const Parts parts = parts_of(p.workspace, p.plan);
+  const int row_tile = row / kLmTileRows, phase = row_tile / p.plan.per_phase, t0 = phase * p.plan.per_phase;
+  const int R = min(p.plan.per_phase, p.plan.row_tiles - t0), C = min(p.plan.ctas / R, p.plan.vocab_tiles);
+  const int token = p.tokens[row];
+  const bool inside = token >= 0 && token < p.vocab;
+  const float token_logit = inside ? parts.token_logit[row] : 0.f;
+  RowSums sums = {-INFINITY, 0.f, 0.f};
+  uint64_t top[kList];
+#pragma unroll
+  for (int j = 0; j < KM; ++j) top[j] = 0ull;
+  for (int c = (kWarps > 1 ? warp * 32 : 0) + lane; c < C; c += 32 * kWarps) {
+    const size_t at = ((size_t)phase * p.plan.ctas + c * R + (row_tile - t0)) * kLmTileRows + row % kLmTileRows;
+    uint64_t list[kList];   // read together: an insertion may end early, and the next load would wait for it
+#pragma unroll
+    for (int j = 0; j < KM; ++j) list[j] = parts.keys[at * KM + j];
+    sums = merge_sums(sums, parts.sums[at], p.scale);
+#pragma unroll
+    for (int j = 0; j < KM; ++j) insert(top, list[j]);
+  }
+  sums = merge_lanes<32>(sums, p.scale);
+  uint64_t best[kList];
+  warp_top<KM>(top, best);
+  if constexpr (kWarps > 1) {
+    if (lane == 0) {
+      sums_s[warp] = sums;
+#pragma unroll
+      for (int j = 0; j < KM; ++j) keys_s[warp * kList + j] = best[j];
+    }
+    __syncthreads();
+    if (warp != 0) return;
+    sums = merge_lanes<kWarps>(sums_s[lane & (kWarps - 1)], p.scale);
+#pragma unroll
+    for (int j = 0; j < KM; ++j) top[j] = lane < kWarps ? keys_s[lane * kList + j] : 0ull;
+    warp_top<KM>(top, best);
+  }
+  const RowResult result(sums);
+  if (lane == 0) {
+    p.logprob[row] = inside ? result.logprob(token_logit, p.inv_temperature) : -INFINITY;
+    if (p.entropy != nullptr) p.entropy[row] = result.entropy;
+  }
+#pragma unroll
+  for (int j = 0; j < KM; ++j)
+    if (lane == j && j < p.k) {
+      p.top_idx[(size_t)row * p.k + j] = best[j] != 0ull ? (int32_t)(~(uint32_t)best[j]) : -1;
+      p.top_val[(size_t)row * p.k + j] =
+          result.logprob(best[j] != 0ull ? topk::from_ordered((uint32_t)(best[j] >> 32)) : -INFINITY, p.inv_temperature);
+    }
 }
 
 template <int KM>
@@ -345,8 +383,11 @@ cudaError_t launch(const CUtensorMap& map_h, const CUtensorMap& map_w, const LmL
   if (e != cudaSuccess) return e;
   e = launch_chained(lm_logprobs_kernel<KM>, dim3(p.plan.ctas), dim3(kThreads), kSmemBytes, stream, 0, map_h, map_w, p);
   if (e != cudaSuccess) return e;
-  constexpr int kRows = kMergeThreads / 32;
-  return launch_chained(lm_logprobs_merge_kernel<KM>, dim3((p.rows + kRows - 1) / kRows), dim3(kMergeThreads), 0, stream, 0, p);
+  // a CTA per row where a row has many parts, which is where the rows are few
+  constexpr int kWarps = kMergeThreads / 32;
+  if (p.plan.row_tiles < 4)
+    return launch_chained(lm_logprobs_merge_kernel<KM, kWarps>, dim3(p.rows), dim3(kMergeThreads), 0, stream, 0, p);
+  return launch_chained(lm_logprobs_merge_kernel<KM, 1>, dim3((p.rows + kWarps - 1) / kWarps), dim3(kMergeThreads), 0, stream, 0, p);
 }
 
 }  // namespace ll

@@ -29,6 +29,7 @@
 #include "launch.cuh"
 #include "page_fork.cuh"
 #include "ptd_device.cuh"
+#include "row_division.cuh"
 
 namespace ptd {
 namespace pf {
@@ -295,37 +296,39 @@ __global__ void __launch_bounds__(kThreads, 1) page_fork_plan_kernel(const __gri
   }
 }
 
-// Table rows by warps and what stays of the stack by threads, then items (copy, layer, K or V, chunk of a page's bytes).
-__global__ void __launch_bounds__(kCopyThreads) page_copy_kernel(const __grid_constant__ PageForkParams p, int chunks) {
+// K and V rows: a CTA's turn is one chunk of a copy's bytes in one layer's K or V (the grid's y); then table rows by warps and what
+// stays of the stack by threads.
+__global__ void __launch_bounds__(kCopyThreads)
+    page_copy_kernel(const __grid_constant__ PageForkParams p, int chunks, IndexDivisor by_chunks) {
   const Scratch sc(p.scratch, p.num_pages, p.from_batch, p.to_batch);
   if (threadIdx.x == 0) grid_launch_dependents();
   grid_dependency_wait();
   const int copies = *sc.copies;
   if (copies == kRefused) return;
-  const int64_t per_copy = (int64_t)p.num_layers * 2 * chunks, items = copies * per_copy;
-  const int64_t page_bytes = p.row_bytes << p.page_log2;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int c = (int)(item / per_copy);
-    int rest = (int)(item - c * per_copy);
-    const int chunk = rest % chunks;
-    rest /= chunks;
-    const int layer = rest >> 1;
+  const int64_t page_bytes = p.row_bytes << p.page_log2, layer_bytes = p.num_pages * page_bytes;
+  for (int turn = blockIdx.x; turn < copies * chunks; turn += gridDim.x) {
+    const int c = divide(turn, by_chunks);
     const int from = sc.copy[3 * c], to = sc.copy[3 * c + 1];
-    const int64_t bytes = sc.copy[3 * c + 2] * p.row_bytes, at = (int64_t)chunk * kChunk;
-    uint8_t* base = static_cast<uint8_t*>((rest & 1) != 0 ? p.v : p.k) + (int64_t)layer * p.num_pages * page_bytes + at;
-    const uint4* src = reinterpret_cast<const uint4*>(base + from * page_bytes);
-    uint4* dst = reinterpret_cast<uint4*>(base + to * page_bytes);
-    const int64_t left = (bytes - at) / 16;
-    uint4 x[kCopyLoads];
+    const int64_t at = (int64_t)(turn - c * chunks) * kChunk, left = (sc.copy[3 * c + 2] * p.row_bytes - at) / 16;
+    if (left <= 0) continue;
+    const int n = (int)min(left, (int64_t)(kChunk / 16)) - (int)threadIdx.x;   // vectors from this thread's first on
+    const int64_t src_at = from * page_bytes + at, dst_at = to * page_bytes + at;
+    for (int plane = blockIdx.y; plane < 2 * p.num_layers; plane += gridDim.y) {
+      uint8_t* base = static_cast<uint8_t*>((plane & 1) != 0 ? p.v : p.k) + (plane >> 1) * layer_bytes;
+      const uint4* src = reinterpret_cast<const uint4*>(base + src_at) + threadIdx.x;
+      uint4* dst = reinterpret_cast<uint4*>(base + dst_at) + threadIdx.x;
+      uint4 x[kCopyLoads];
 #pragma unroll
-    for (int u = 0; u < kCopyLoads; ++u)
-      if (threadIdx.x + u * kCopyThreads < left) x[u] = src[threadIdx.x + u * kCopyThreads];
+      for (int u = 0; u < kCopyLoads; ++u)
+        if (u * kCopyThreads < n) x[u] = src[u * kCopyThreads];
 #pragma unroll
-    for (int u = 0; u < kCopyLoads; ++u)
-      if (threadIdx.x + u * kCopyThreads < left) dst[threadIdx.x + u * kCopyThreads] = x[u];
+      for (int u = 0; u < kCopyLoads; ++u)
+        if (u * kCopyThreads < n) dst[u * kCopyThreads] = x[u];
+    }
   }
   // the last CTAs first: the first ones have the copies
-  const int cta = (int)gridDim.x - 1 - (int)blockIdx.x, all = (int)gridDim.x * kCopyThreads, me = cta * kCopyThreads + (int)threadIdx.x;
+  const int ctas = (int)(gridDim.x * gridDim.y), cta = ctas - 1 - (int)(blockIdx.y * gridDim.x + blockIdx.x);
+  const int all = ctas * kCopyThreads, me = cta * kCopyThreads + (int)threadIdx.x;
   for (int b = me >> 5; b < p.to_batch; b += all >> 5) {
     const int need = p.new_held[b], fresh = sc.fresh[b];
     const int32_t* row = p.table + (size_t)max(p.parents[b], 0) * p.max_pages;
@@ -336,6 +339,11 @@ __global__ void __launch_bounds__(kCopyThreads) page_copy_kernel(const __grid_co
 }
 
 }  // namespace pf
+
+int page_copy_chunks(int64_t page_bytes) {
+  const int64_t n = (page_bytes + pf::kChunk - 1) / pf::kChunk;
+  return n < INT_MAX ? (int)n : INT_MAX;
+}
 
 size_t page_fork_scratch_ints(int num_pages, int from_batch, int to_batch) {
   return 4 + 2 * (size_t)num_pages + 2 * (size_t)from_batch + 5 * (size_t)to_batch;
@@ -360,11 +368,12 @@ cudaError_t launch_page_fork(const PageForkParams& p, int sms, cudaStream_t stre
   e = launch_chained(one ? pf::page_fork_plan_kernel<true> : pf::page_fork_plan_kernel<false>,
                                        dim3(one ? 1 : pf::kCtas), dim3(pf::kThreads), smem, stream, one ? 0 : pf::kCtas, p);
   if (e != cudaSuccess) return e;
-  const int64_t page_bytes = p.row_bytes << p.page_log2;
-  const int chunks = (int)((page_bytes + pf::kChunk - 1) / pf::kChunk);
-  const int64_t most = (int64_t)p.to_batch * p.num_layers * 2 * chunks + p.to_batch, places = 8 * (int64_t)sms;
-  return launch_chained(pf::page_copy_kernel, dim3((unsigned)(most < places ? most : places)), dim3(pf::kCopyThreads), 0, stream, 0,
-                        p, chunks);
+  const int chunks = page_copy_chunks(p.row_bytes << p.page_log2);
+  // eight CTAs an SM, but no more than there may be turns
+  const int64_t planes = 2 * (int64_t)p.num_layers < 64 ? 2 * (int64_t)p.num_layers : 64, turns = (int64_t)p.to_batch * chunks;
+  const int64_t places = (8 * (int64_t)sms + planes - 1) / planes;
+  return launch_chained(pf::page_copy_kernel, dim3((unsigned)(turns < places ? turns : places), (unsigned)planes),
+                        dim3(pf::kCopyThreads), 0, stream, 0, p, chunks, index_divisor(chunks));
 }
 
 }  // namespace ptd

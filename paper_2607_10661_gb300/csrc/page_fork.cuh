@@ -26,6 +26,8 @@ struct PageForkParams {
   int32_t* dev_status;
   int32_t* scratch;            // page_fork_scratch_ints() of them
 };
+// Turns of a CTA that copy a page of K (or V); a call's, to_batch times as many, fit in an int.
+int page_copy_chunks(int64_t page_bytes);
 size_t page_fork_scratch_ints(int num_pages, int from_batch, int to_batch);
 cudaError_t launch_page_fork(const PageForkParams& p, int sms, cudaStream_t stream);
 }  // namespace ptd
