@@ -14,12 +14,15 @@ from .ptd_oracle import (  # noqa: F401
     depths,
     draft_tree_update,
     eligible_edges,
+    head_norm_rope,
     kv_compact,
     lm_head_logits,
     lm_head_topk,
+    page_fork,
     prompt_pages,
     prompt_slots,
     softmax_row,
+    token_logprobs,
     topk,
     topk_rows,
     tree_positions,

@@ -574,3 +574,68 @@ def lm_head_logits(hidden, weight) -> np.ndarray:
 def lm_head_topk(hidden, weight, k: int):
     """topk_rows of the LM-head logits: (indices [N, k], values [N, k])."""
     return topk_rows(lm_head_logits(hidden, weight), k)
+
+
+# ---------------------------------------------------------------------------
+# Several continuations: head norms, log probabilities, forks of paged sequences
+# ---------------------------------------------------------------------------
+
+def head_norm_rope(x, weight, positions, base: float, eps: float) -> np.ndarray:
+    """x [N, H, D]: every head divided by the root of its mean square (+ eps), times weight [D], then rotated (rope)."""
+    x = np.asarray(x, np.float64)
+    with np.errstate(invalid="ignore", divide="ignore"):
+        y = x / np.sqrt((x ** 2).mean(axis=-1, keepdims=True) + eps) * np.asarray(weight, np.float64)
+    return rope(y, positions, base)
+
+
+def token_logprobs(logits, tokens, temperature: float, k: int):
+    """(log p of the tokens, entropies, alternatives, their log p) of rows of logits: p = softmax(logits / temperature), a
+    token outside the vocabulary has probability 0, a row of -inf log probabilities -inf and entropy 0."""
+    logits = np.asarray(logits, np.float64)
+    lp, ent, idx, val = [], [], [], []
+    for row, t in zip(logits, tokens):
+        z = row / temperature
+        if (z == -np.inf).all():
+            p = np.full_like(z, -np.inf)
+            ent.append(0.0)
+        else:
+            p = z - z.max() - np.log(np.exp(z - z.max()).sum())
+            ent.append(-sum(math.exp(x) * x for x in p if x > -np.inf))
+        lp.append(p[t] if 0 <= t < len(p) else -np.inf)
+        best = topk(row, k)[0] if k else []
+        idx.append([int(i) for i in best])
+        val.append([p[i] for i in best])
+    return np.array(lp), np.array(ent), np.array(idx, dtype=np.int64), np.array(val)
+
+
+def page_fork(table, held, free, parents, lens, page_size: int):
+    """Target b goes on from the first lens[b] positions of sequence parents[b] (-1: empty).  Full pages are shared; of the
+    targets with the same partial page the first keeps it, unless it is somebody's full page; the others take pages from
+    the top of the stack `free` (a list, top last) into which its first positions are copied.  Pages held before and by
+    nobody now go on top, by (first holder, index).  Returns (rows, free, [(page from, page to, positions)]), or None if
+    there are too few free pages."""
+    whole, keeper = set(), {}
+    for b, (p, n) in enumerate(zip(parents, lens)):
+        if p >= 0:
+            whole.update(table[p][:n // page_size])
+            if n % page_size:
+                keeper.setdefault(table[p][n // page_size], b)
+    stack, rows, copies = list(free), [], []
+    for b, (p, n) in enumerate(zip(parents, lens)):
+        row = [] if p < 0 else list(table[p][:n // page_size])
+        if p >= 0 and n % page_size:
+            page = table[p][n // page_size]
+            if page in whole or keeper[page] != b:
+                if not stack:
+                    return None
+                copies.append((page, stack.pop(), n % page_size))
+                page = copies[-1][1]
+            row.append(page)
+        rows.append(row)
+    kept = whole | set(keeper)
+    for row, h in zip(table, held):
+        for page in row[:h]:
+            if page not in kept:
+                kept.add(page)
+                stack.append(page)
+    return rows, stack, copies

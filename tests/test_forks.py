@@ -1,9 +1,13 @@
 """The operators around several continuations without a GPU: the host's refusals, what the native calls take, and the
 binding's own checks."""
 import ctypes
+import math
 import os
 
+import numpy as np
 import pytest
+
+import oracle
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 A = 1 << 30
@@ -282,3 +286,36 @@ def test_trees_beyond_the_cache_are_refused(monkeypatch):
             ptd.tree_norm_rope_append(tree, cache, 0, q, q, q, q, q, q, 1e-6, 1e4, None)
     with pytest.raises(ValueError, match="layers"):
         ptd.tree_norm_rope_append(tree, cache, 0, q[0], q, q, q, q, q, 1e-6, 1e4, None)
+
+
+def test_oracle_forks_by_hand():
+    """Pages of 16.  Sequence 0 has 36 positions in pages 4, 2, 6, sequence 1 20 in 4, 1 (page 4 shared), sequence 2 has
+    page 7.  Two targets go on from sequence 0 (the first keeps page 6), one from its first 20 (page 2 is somebody's full
+    page: copied), one from sequence 1; sequence 2 ends."""
+    table = [[4, 2, 6, -1], [4, 1, -1, -1], [7, -1, -1, -1]]
+    rows, free, copies = oracle.page_fork(table, [3, 2, 1], [0, 3, 5], [1, 0, 0, 0, -1], [20, 36, 36, 20, 9], 16)
+    assert rows == [[4, 1], [4, 2, 6], [4, 2, 5], [4, 3], []] and free == [0, 7] and copies == [(6, 5, 4), (2, 3, 4)]
+    # everything ends: the shared page comes back once
+    assert oracle.page_fork(table, [3, 2, 1], [0], [-1], [0], 16) == ([[]], [0, 4, 2, 6, 1, 7], [])
+    # cut to a page's end: nothing is copied, nothing kept by itself
+    assert oracle.page_fork(table, [3, 2, 1], [], [0, 0], [32, 16], 16) == ([[4, 2], [4]], [6, 1, 7], [])
+    assert oracle.page_fork(table, [3, 2, 1], [], [0, 0], [36, 36], 16) is None
+
+
+def test_oracle_log_probabilities_by_hand():
+    lp, ent, idx, val = oracle.token_logprobs([[0.0, 0.0, -np.inf, 0.0], [math.log(4), 0.0, 0.0, -np.inf], [-np.inf] * 4],
+                                              [1, 0, 2], 1.0, 3)
+    assert np.allclose(lp[:2], [-math.log(3), math.log(4 / 6)]) and lp[2] == -np.inf
+    assert np.allclose(ent, [math.log(3), -(4 / 6) * math.log(4 / 6) + 2 * (1 / 6) * math.log(6), 0.0])
+    assert idx.tolist() == [[0, 1, 3], [0, 1, 2], [0, 1, 2]] and np.allclose(val[1], np.log([4 / 6, 1 / 6, 1 / 6]))
+    lp, ent, _, _ = oracle.token_logprobs([[2.0, 4.0]], [-1], 2.0, 0)
+    assert lp[0] == -np.inf and np.allclose(ent, oracle.token_logprobs([[1.0, 2.0]], [0], 1.0, 0)[1])
+
+
+def test_oracle_head_norm():
+    """A head of equal values has norm |x|: +-1 times the weight, then the rotation; the mean square of any other is 1."""
+    x = np.array([[[3.0, 3.0, -3.0, -3.0], [1.0, 2.0, 3.0, 4.0]]])
+    w = np.array([1.0, 2.0, 3.0, 4.0])
+    assert np.allclose(oracle.head_norm_rope(x, w, [0], 10.0, 0.0)[0, 0], [1.0, 2.0, -3.0, -4.0])
+    assert np.allclose((oracle.head_norm_rope(x, np.ones(4), [7], 10.0, 0.0) ** 2).mean(-1), 1.0)
+    assert np.allclose(oracle.head_norm_rope(x, w, [7], 10.0, 0.0), oracle.rope(oracle.head_norm_rope(x, w, [0], 10.0, 0.0), [7], 10.0))

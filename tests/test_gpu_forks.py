@@ -16,6 +16,7 @@ import numpy as np
 import pytest
 import torch
 
+import oracle
 from paper_2607_10661_gb300 import ptd
 
 pytestmark = pytest.mark.gpu
@@ -40,12 +41,10 @@ def _half_step(dtype):
 def _norm_turn(x, w, pos, base, eps, dtype):
     """[n, h, D] normed and turned in 64 bits, and the tolerance of each element."""
     x, w, d = x.double().cpu().numpy(), w.double().cpu().numpy(), x.shape[-1]
+    out = oracle.head_norm_rope(x, w, pos, float(base), eps)
     with np.errstate(all="ignore"):
         y = x * w / np.sqrt((x ** 2).mean(-1, keepdims=True) + eps)
-    ang = np.asarray(pos, np.float64)[:, None] * float(base) ** (-2.0 * np.arange(d // 2) / d)
-    c, s = np.cos(ang)[:, None, :], np.sin(ang)[:, None, :]
     a, b = y[..., :d // 2], y[..., d // 2:]
-    out = np.concatenate([a * c - b * s, a * s + b * c], -1)
     m = np.concatenate([np.abs(a) + np.abs(b)] * 2, -1)
     return out, m * ((d / 2 + 8) * 2.0 ** -24 + np.abs(np.asarray(pos, np.float64))[:, None, None] * 2.0 ** -50) \
         + np.abs(out) * _half_step(dtype) * 1.01 + 1e-30
@@ -296,6 +295,11 @@ def test_token_logprobs_of_masked_and_broken_rows(dtype, vocab):
     assert lp[1] == 0 and e[1] == 0 and out[2][1, 0] == vocab - 1 and (out[3][1, 1:] == -INF).all()
     for r in (5, 6, 9):
         assert lp[r].isnan() and e[r].isnan() and out[3][r].isnan().all()
+    if vocab == 40:
+        want = oracle.token_logprobs(logits.double().cpu().numpy()[[0, 1, 2, 7, 8, 11]], tokens.cpu().numpy()[[0, 1, 2, 7, 8, 11]], 1.0, 16)
+        for got, w in zip(out, want):
+            got = got.double().cpu().numpy()[[0, 1, 2, 7, 8, 11]]
+            assert ((got == w) | (np.abs(got - w) <= 2.0 ** -16)).all()
     good = [r for r in range(12) if r not in (0, 5, 6, 9)]
     sel = torch.tensor(good, device=DEV)
     _check_logprobs(logits[sel], tokens[sel], 1.0, 16, *(o[sel] for o in out))
@@ -360,33 +364,6 @@ def test_lm_head_logprobs_of_broken_rows():
 
 
 # ------------------------------------------------------------------ forks
-def _fork(table, held, free, parents, lens, P):
-    """(new table rows, stack, copies) by the definition, page by page."""
-    whole, heir = set(), {}
-    for b, (p, n) in enumerate(zip(parents, lens)):
-        if p >= 0:
-            whole.update(table[p][:n // P])
-            if n % P:
-                heir.setdefault(table[p][n // P], b)
-    stack, rows, copies = list(free), [], []
-    for b, (p, n) in enumerate(zip(parents, lens)):
-        row = [] if p < 0 else list(table[p][:n // P])
-        if p >= 0 and n % P:
-            x = table[p][n // P]
-            if x in whole or heir[x] != b:
-                copies.append((x, stack.pop(), n % P))
-                x = copies[-1][1]
-            row.append(x)
-        rows.append(row)
-    kept = whole | set(heir)
-    for row, h in zip(table, held):
-        for x in row[:h]:
-            if x not in kept:
-                kept.add(x)
-                stack.append(x)
-    return rows, stack, copies
-
-
 class Pages:
     """A random paged state: sequences that share prefixes, a stack of free pages, K and V of random values."""
 
@@ -431,7 +408,7 @@ class Pages:
         return ptd.page_fork(self.cache, self.source, self.target, p, n, ws, self.status)
 
     def check(self, k0, v0):
-        rows, stack, copies = _fork(self.table, self.held, self.free, self.parents, self.lens, self.P)
+        rows, stack, copies = oracle.page_fork(self.table, self.held, self.free, self.parents, self.lens, self.P)
         t = self.target
         got = t.block_table.cpu().tolist()
         assert t.held.tolist() == [len(r) for r in rows]
