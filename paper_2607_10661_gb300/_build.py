@@ -38,9 +38,16 @@ def _compile(src: str) -> str:
 
 
 def _compile_calls() -> None:
+    import torch
+
+    root = os.path.dirname(os.path.abspath(torch.__file__))   # its headers and libraries: the module looks at its tensors
+    include, lib = os.path.join(root, "include"), os.path.join(root, "lib")
     tmp = CALLS + ".tmp"
     cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
-           "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "pycall.cpp"), "-o", tmp, "-ldl"]
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-isystem", include,
+           "-isystem", os.path.join(include, "torch", "csrc", "api", "include"), "-I", sysconfig.get_paths()["include"],
+           os.path.join(CSRC, "pycall.cpp"), "-o", tmp, "-ldl", "-L", lib, f"-Wl,-rpath,{lib}", "-ltorch_python", "-ltorch_cpu",
+           "-lc10"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"g++ failed on pycall.cpp:\n{r.stdout}\n{r.stderr}")

@@ -8,9 +8,14 @@
 // when the library refuses the call, or None when an argument is not of the plain form
 // expected here: nothing has been enqueued then, and ptd.py's own path handles the call or
 // raises its error.  Nothing is kept between calls.
+//
+// A torch.Tensor is looked at through torch's own C++ class (an attribute read by name costs 0.07 - 0.16 us, and a call has up
+// to a dozen tensors with five or six each: prompt_norm_rope_append 3.0 us without the launch); an object of another type that load() was
+// given by its Python attributes.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <dlfcn.h>
+#include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/ptd.h"
 
@@ -29,6 +34,143 @@ PyObject *s_is_cuda, *s_is_contiguous, *s_dtype, *s_data_ptr, *s_nbytes, *s_shap
 #define PTD_DECLARE(f) decltype(&f) p_##f;
 PTD_FUNCTIONS(PTD_DECLARE)
 #undef PTD_DECLARE
+
+bool g_direct = false;   // g_tensor is torch.Tensor
+
+// What the calls ask of an object of type g_tensor.  Whatever fails, on the Python side or as a C++ exception, is
+// an answer that no call takes (nullptr, -1 or false), with no Python error left.
+namespace look {
+
+const at::Tensor& direct(PyObject* o) { return THPVariable_Unpack(o); }
+
+bool truth(PyObject* r) {   // (True outlives the reference dropped here)
+  Py_XDECREF(r);
+  if (r == nullptr) PyErr_Clear();
+  return r == Py_True;
+}
+int64_t number(PyObject* r) {
+  const int64_t v = r != nullptr && PyLong_CheckExact(r) ? PyLong_AsLongLong(r) : -1;
+  Py_XDECREF(r);
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    return -1;
+  }
+  return v;
+}
+// the numbers of a tuple of at most four, how many there are
+int numbers(PyObject* r, int64_t (&v)[4]) {
+  int n = -1;
+  if (r != nullptr && PyTuple_Check(r) && PyTuple_GET_SIZE(r) <= 4) {
+    n = (int)PyTuple_GET_SIZE(r);
+    for (int i = 0; i < n; ++i) v[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(r, i));
+  }
+  Py_XDECREF(r);
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    return -1;
+  }
+  return n;
+}
+int numbers(at::IntArrayRef a, int64_t (&v)[4]) {
+  if (a.size() > 4) return -1;
+  for (size_t i = 0; i < a.size(); ++i) v[i] = a[i];
+  return (int)a.size();
+}
+
+bool is_cuda(PyObject* o) {
+  try {
+    return g_direct ? direct(o).is_cuda() : truth(PyObject_GetAttr(o, s_is_cuda));
+  } catch (...) {
+    return false;
+  }
+}
+int64_t device(PyObject* o) {   // -1: not on one
+  try {
+    return g_direct ? (direct(o).is_cuda() ? direct(o).get_device() : -1) : number(PyObject_CallMethodNoArgs(o, s_get_device));
+  } catch (...) {
+    return -1;
+  }
+}
+bool is_contiguous(PyObject* o) {
+  try {
+    return g_direct ? direct(o).is_contiguous() : truth(PyObject_CallMethodNoArgs(o, s_is_contiguous));
+  } catch (...) {
+    return false;
+  }
+}
+// whether the dtype is this one of int32, float32 and bfloat16
+bool has_dtype(PyObject* o, PyObject* dtype) {
+  if (g_direct) {
+    const auto want = dtype == g_i32 ? at::kInt : (dtype == g_f32 ? at::kFloat : at::kBFloat16);
+    return direct(o).scalar_type() == want;
+  }
+  PyObject* d = PyObject_GetAttr(o, s_dtype);   // (the dtypes outlive the reference dropped here)
+  Py_XDECREF(d);
+  if (d == nullptr) PyErr_Clear();
+  return d == dtype;
+}
+// false: the tensor has no address
+bool address(PyObject* o, void** p) {
+  *p = nullptr;
+  try {
+    if (g_direct) {
+      *p = direct(o).data_ptr();
+      return true;
+    }
+  } catch (...) {
+    return false;
+  }
+  PyObject* r = PyObject_CallMethodNoArgs(o, s_data_ptr);
+  if (r != nullptr) *p = PyLong_AsVoidPtr(r);
+  Py_XDECREF(r);
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    return false;
+  }
+  return r != nullptr;
+}
+int64_t nbytes(PyObject* o) {
+  try {
+    return g_direct ? direct(o).numel() * (int64_t)direct(o).element_size() : number(PyObject_GetAttr(o, s_nbytes));
+  } catch (...) {
+    return -1;
+  }
+}
+int shape(PyObject* o, int64_t (&d)[4]) {
+  try {
+    return g_direct ? numbers(direct(o).sizes(), d) : numbers(PyObject_GetAttr(o, s_shape), d);
+  } catch (...) {
+    return -1;
+  }
+}
+// the size of dimension i of one with two or more
+int64_t named_size(PyObject* o, int i) {
+  PyObject* d = PyObject_GetAttr(o, s_shape);
+  int64_t n = -1;
+  if (d != nullptr && PyTuple_Check(d) && PyTuple_GET_SIZE(d) >= 2) n = PyLong_AsLongLong(PyTuple_GET_ITEM(d, i));
+  Py_XDECREF(d);
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    return -1;
+  }
+  return n;
+}
+int64_t size(PyObject* o, int i) {
+  try {
+    return g_direct ? (direct(o).dim() >= 2 ? direct(o).size(i) : -1) : named_size(o, i);
+  } catch (...) {
+    return -1;
+  }
+}
+int strides(PyObject* o, int64_t (&d)[4]) {
+  try {
+    return g_direct ? numbers(direct(o).strides(), d) : numbers(PyObject_CallMethodNoArgs(o, s_stride), d);
+  } catch (...) {
+    return -1;
+  }
+}
+
+}  // namespace look
 
 // Reads one call's arguments; the first that is not of the expected form clears `ok`.
 struct Args {
@@ -50,29 +192,16 @@ struct Args {
     PyErr_Clear();
   }
   PyObject* next() { return a[i++]; }
-  bool attr_true(PyObject* o, PyObject* name, bool call) {
-    PyObject* r = call ? PyObject_CallMethodNoArgs(o, name) : PyObject_GetAttr(o, name);
-    Py_XDECREF(r);
-    return r == Py_True;
-  }
-  // (dtype singletons and True outlive the references dropped here)
-  PyObject* dtype_of(PyObject* o) {
-    PyObject* d = PyObject_GetAttr(o, s_dtype);
-    Py_XDECREF(d);
-    return d;
-  }
+  bool is_tensor(PyObject* o) { return (PyObject*)Py_TYPE(o) == g_tensor; }
   void* pointer(PyObject* o) {
-    PyObject* r = PyObject_CallMethodNoArgs(o, s_data_ptr);
-    void* p = r != nullptr ? PyLong_AsVoidPtr(r) : nullptr;
-    Py_XDECREF(r);
-    if (PyErr_Occurred()) fail();
+    void* p;
+    if (!look::address(o, &p)) fail();
     return p;
   }
   // a contiguous CUDA tensor of `dtype` (NULL: any)
   void* tensor_of(PyObject* o, PyObject* dtype) {
     if (!ok) return nullptr;
-    if ((PyObject*)Py_TYPE(o) != g_tensor || !attr_true(o, s_is_cuda, false) || !attr_true(o, s_is_contiguous, true) ||
-        (dtype != nullptr && dtype_of(o) != dtype)) {
+    if (!is_tensor(o) || !look::is_cuda(o) || !look::is_contiguous(o) || (dtype != nullptr && !look::has_dtype(o, dtype))) {
       fail();
       return nullptr;
     }
@@ -82,7 +211,7 @@ struct Args {
   void* tensor_on(PyObject* o, PyObject* dtype) {
     on(o);
     if (!ok) return nullptr;
-    if (!attr_true(o, s_is_contiguous, true) || (dtype != nullptr && dtype_of(o) != dtype)) {
+    if (!look::is_contiguous(o) || (dtype != nullptr && !look::has_dtype(o, dtype))) {
       fail();
       return nullptr;
     }
@@ -101,62 +230,45 @@ struct Args {
     if (o == Py_None) return nullptr;
     void* p = tensor_of(o, nullptr);
     if (!ok) return nullptr;
-    PyObject* r = PyObject_GetAttr(o, s_nbytes);
-    if (r != nullptr && PyLong_CheckExact(r)) *bytes = PyLong_AsSize_t(r); else ok = false;
-    Py_XDECREF(r);
-    if (PyErr_Occurred()) fail();
+    const int64_t n = look::nbytes(o);
+    if (n < 0) fail(); else *bytes = (size_t)n;
     return p;
   }
   // the dtype of a bf16 or fp32 tensor
   ptd_dtype kind(PyObject* o) {
     if (!ok) return PTD_F32;
-    PyObject* d = (PyObject*)Py_TYPE(o) == g_tensor ? dtype_of(o) : nullptr;
-    if (d != g_bf16 && d != g_f32) fail();
-    return d == g_bf16 ? PTD_BF16 : PTD_F32;
+    const bool bf16 = is_tensor(o) && look::has_dtype(o, g_bf16);
+    if (!bf16 && !(is_tensor(o) && look::has_dtype(o, g_f32))) fail();
+    return bf16 ? PTD_BF16 : PTD_F32;
   }
   // the sizes of a 2-D tensor
   void dims2(PyObject* o, int64_t* d0, int64_t* d1) {
     *d0 = *d1 = 0;
-    if (!ok) return;
-    PyObject* s = PyObject_GetAttr(o, s_shape);
-    if (s != nullptr && PyTuple_Check(s) && PyTuple_GET_SIZE(s) == 2) {
-      *d0 = PyLong_AsLongLong(PyTuple_GET_ITEM(s, 0));
-      *d1 = PyLong_AsLongLong(PyTuple_GET_ITEM(s, 1));
-    } else {
-      ok = false;
+    int64_t d[4];
+    if (!ok || !is_tensor(o) || look::shape(o, d) != 2) {
+      fail();
+      return;
     }
-    Py_XDECREF(s);
-    if (PyErr_Occurred()) fail();
+    *d0 = d[0], *d1 = d[1];
   }
   // a 2-D tensor's rows: CUDA, unit column stride, rows at least a row apart
   void* rows2(PyObject* o, PyObject* dtype, int64_t* rows, int64_t* cols, int64_t* stride) {
     *stride = 0;
     dims2(o, rows, cols);
-    if (!ok || (PyObject*)Py_TYPE(o) != g_tensor || !attr_true(o, s_is_cuda, false) || dtype_of(o) != dtype) {
+    int64_t st[4];
+    if (!ok || !look::is_cuda(o) || !look::has_dtype(o, dtype) || look::strides(o, st) != 2 || st[1] != 1 || st[0] < *cols) {
       fail();
       return nullptr;
     }
-    PyObject* s = PyObject_CallMethodNoArgs(o, s_stride);
-    int64_t unit = 0;
-    if (s != nullptr && PyTuple_Check(s) && PyTuple_GET_SIZE(s) == 2) {
-      *stride = PyLong_AsLongLong(PyTuple_GET_ITEM(s, 0));
-      unit = PyLong_AsLongLong(PyTuple_GET_ITEM(s, 1));
-    }
-    Py_XDECREF(s);
-    if (PyErr_Occurred() || unit != 1 || *stride < *cols) {
-      fail();
-      return nullptr;
-    }
+    *stride = st[0];
     return pointer(o);
   }
   // The device of the tensors seen by on(): the prompt calls run on it only where it is the current one.
   int64_t device = -1;
   void on(PyObject* o) {
     if (!ok) return;
-    PyObject* r = (PyObject*)Py_TYPE(o) == g_tensor ? PyObject_CallMethodNoArgs(o, s_get_device) : nullptr;
-    const int64_t d = r != nullptr && PyLong_CheckExact(r) ? PyLong_AsLongLong(r) : -1;
-    Py_XDECREF(r);
-    if (PyErr_Occurred() || d < 0 || (device >= 0 && d != device)) fail();
+    const int64_t d = is_tensor(o) ? look::device(o) : -1;
+    if (d < 0 || (device >= 0 && d != device)) fail();
     device = d;
   }
   void on_attr(PyObject* o, PyObject* name) {
@@ -176,10 +288,7 @@ struct Args {
     if (!ok || prompt->batch < 1) return;
     const bool paged = cache->page_size > 0;
     PyObject* t = PyObject_GetAttr(o, paged ? s_block_table : s_k);
-    PyObject* d = t != nullptr ? PyObject_GetAttr(t, s_shape) : nullptr;
-    int64_t rows = -1;
-    if (d != nullptr && PyTuple_Check(d) && PyTuple_GET_SIZE(d) >= 2) rows = PyLong_AsLongLong(PyTuple_GET_ITEM(d, paged ? 0 : 1));
-    Py_XDECREF(d);
+    const int64_t rows = t == nullptr ? -1 : (is_tensor(t) ? look::size(t, paged ? 0 : 1) : look::named_size(t, paged ? 0 : 1));
     Py_XDECREF(t);
     if (PyErr_Occurred() || (paged ? rows < prompt->batch : rows != prompt->batch)) fail();
   }
@@ -188,26 +297,15 @@ struct Args {
     PyObject* o = next();
     if (!ok) return nullptr;
     void* p = tensor_on(o, dtype);
-    PyObject* r = ok ? PyObject_GetAttr(o, s_nbytes) : nullptr;
-    if (r == nullptr || !PyLong_CheckExact(r) || PyLong_AsLongLong(r) != 4 * count) fail();
-    Py_XDECREF(r);
+    if (!ok || look::nbytes(o) != 4 * count) fail();
     return p;
   }
   int32_t* i32_of(int64_t count) { return static_cast<int32_t*>(word_of(g_i32, count)); }
   // the sizes of a tensor of 2 to 4 dimensions; how many there are
   int dims(PyObject* o, int64_t (&d)[4]) {
     d[0] = d[1] = d[2] = d[3] = 0;
-    if (!ok) return 0;
-    PyObject* s = PyObject_GetAttr(o, s_shape);
-    int n = 0;
-    if (s != nullptr && PyTuple_Check(s) && PyTuple_GET_SIZE(s) >= 1 && PyTuple_GET_SIZE(s) <= 4) {
-      n = (int)PyTuple_GET_SIZE(s);
-      for (int i = 0; i < n; ++i) d[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(s, i));
-    } else {
-      ok = false;
-    }
-    Py_XDECREF(s);
-    if (PyErr_Occurred()) fail();
+    const int n = ok && is_tensor(o) ? look::shape(o, d) : -1;
+    if (n < 1) fail();
     return n;
   }
   // a contiguous tensor of `dtype`, of this shape
@@ -249,31 +347,14 @@ struct Args {
   void* rows3(PyObject* dtype, int64_t rows, int64_t dim, int64_t* heads, int64_t* stride) {
     PyObject* o = next();
     on(o);   // (a host tensor has no device)
-    if (!ok || dtype_of(o) != dtype) {
+    int64_t n[4], st[4];
+    if (!ok || !look::has_dtype(o, dtype) || look::shape(o, n) != 3 || look::strides(o, st) != 3 || n[0] != rows || n[2] != dim ||
+        n[1] < 1 || (*heads != 0 && n[1] != *heads) || (dim != 1 && st[2] != 1) || (n[1] != 1 && st[1] != dim) || st[0] < n[1] * dim) {
       fail();
       return nullptr;
     }
-    PyObject* d = PyObject_GetAttr(o, s_shape);
-    PyObject* s = PyObject_CallMethodNoArgs(o, s_stride);
-    bool good = d != nullptr && s != nullptr && PyTuple_Check(d) && PyTuple_Check(s) && PyTuple_GET_SIZE(d) == 3 &&
-                PyTuple_GET_SIZE(s) == 3;
-    if (good) {
-      int64_t n[3], st[3];
-      for (int k = 0; k < 3; ++k) {
-        n[k] = PyLong_AsLongLong(PyTuple_GET_ITEM(d, k));
-        st[k] = PyLong_AsLongLong(PyTuple_GET_ITEM(s, k));
-      }
-      good = n[0] == rows && n[2] == dim && n[1] > 0 && (*heads == 0 || n[1] == *heads) && (dim == 1 || st[2] == 1) &&
-             (n[1] == 1 || st[1] == dim) && st[0] >= n[1] * dim;
-      *heads = n[1];
-      *stride = st[0];
-    }
-    Py_XDECREF(d);
-    Py_XDECREF(s);
-    if (PyErr_Occurred() || !good) {
-      fail();
-      return nullptr;
-    }
+    *heads = n[1];
+    *stride = st[0];
     return pointer(o);
   }
   int64_t i64() {
@@ -541,9 +622,7 @@ PyObject* pool_retrieve(PyObject*, PyObject* const* a, Py_ssize_t n) {
     PyObject* t = a[g.i];
     o = g.i32();
     if (!g.ok) Py_RETURN_NONE;
-    PyObject* r = PyObject_GetAttr(t, s_nbytes);
-    if (r == nullptr || !PyLong_CheckExact(r) || PyLong_AsLongLong(r) < 4 * (int64_t)max_nodes) g.fail();
-    Py_XDECREF(r);
+    if (look::nbytes(t) < 4 * (int64_t)max_nodes) g.fail();
   }
   void* s = g.stream();
   if (!g.ok) Py_RETURN_NONE;
@@ -850,6 +929,7 @@ PyObject* load(PyObject*, PyObject* args) {
   PTD_FUNCTIONS(PTD_RESOLVE)
 #undef PTD_RESOLVE
   for (PyObject* x : o) Py_INCREF(x);
+  g_direct = o[0] == THPVariableClass;
   g_tensor = o[0], g_i32 = o[1], g_f32 = o[2], g_bf16 = o[3], g_raw_stream = o[4], g_get_device = o[5];
   Py_RETURN_NONE;
 }
