@@ -408,11 +408,12 @@ ptd_status ptd_token_logprobs(const void* logits, ptd_dtype dtype, int64_t rows,
 
 /* As ptd_token_logprobs of the logits h_r W^T, which never reach memory: hidden and weight as ptd_lm_head_topk takes them,
  * but any number of rows up to PTD_MAX_LOGPROB_ROWS (a prompt's tokens, a decoding batch).  Logits are accumulated in fp32 by
- * the tensor cores in an order of their own (see ptd_lm_head_topk), then summed as there with vocab 2^-33 in the bound.  Tokens with logits of -inf or NaN are no alternatives:
- * where fewer than k are left, -1 and -inf (NaN in a row with NaN or +inf) follow.
+ * the tensor cores in an order of their own (see ptd_lm_head_topk), then summed as there with vocab 2^-33 in the bound.
+ * Tokens with logits of -inf or NaN are no alternatives: where fewer than k are left, -1 and -inf (NaN in a row with
+ * NaN or +inf) follow.
  * workspace: ptd_lm_head_logprobs_workspace_size(rows, vocab, k) bytes (of the current device), 16-byte aligned, for the
- * parts of each row; it and the outputs overlap no input and not one another.  Two launches: the product, and the
- * merge of a row's parts. */
+ * parts of each row; it and the outputs overlap no input and not one another, and calls that may overlap on the GPU need
+ * workspaces of their own.  Two launches: the product, and the merge of a row's parts. */
 #define PTD_MAX_LOGPROB_ROWS (1 << 22)
 size_t ptd_lm_head_logprobs_workspace_size(int32_t rows, int32_t vocab, int32_t k);
 ptd_status ptd_lm_head_logprobs(const void* hidden, int32_t rows, int64_t hidden_stride, const void* weight, int32_t vocab,
@@ -620,7 +621,8 @@ typedef struct {
  * to->held and to->free_count are zeros and nothing else of `to` or the cache is written.  Pages that are both held and free,
  * or twice in a row or on the stack, give unspecified results (nothing outside the buffers is touched).
  *   cache: its k, v and sizes; its block_table is not read.  A layer has fewer than 2^31 rows.
- *   workspace: ptd_page_fork_workspace_size bytes, 16-byte aligned, in any state.
+ *   workspace: ptd_page_fork_workspace_size bytes, 16-byte aligned, in any state; calls that may overlap on the GPU need
+ *   workspaces (and targets) of their own.
  * Two launches: the plan, and the copies. */
 size_t ptd_page_fork_workspace_size(const ptd_kv_cache* cache, const ptd_page_set* from, const ptd_page_set* to);
 ptd_status ptd_page_fork(const ptd_kv_cache* cache, const ptd_page_set* from, const ptd_page_set* to, const int32_t* parents,

@@ -299,7 +299,8 @@ def test_token_logprobs_of_masked_and_broken_rows(dtype, vocab):
         want = oracle.token_logprobs(logits.double().cpu().numpy()[[0, 1, 2, 7, 8, 11]], tokens.cpu().numpy()[[0, 1, 2, 7, 8, 11]], 1.0, 16)
         for got, w in zip(out, want):
             got = got.double().cpu().numpy()[[0, 1, 2, 7, 8, 11]]
-            assert ((got == w) | (np.abs(got - w) <= 2.0 ** -16)).all()
+            with np.errstate(invalid="ignore"):   # -inf - -inf
+                assert ((got == w) | (np.abs(got - w) <= 2.0 ** -16)).all()
     good = [r for r in range(12) if r not in (0, 5, 6, 9)]
     sel = torch.tensor(good, device=DEV)
     _check_logprobs(logits[sel], tokens[sel], 1.0, 16, *(o[sel] for o in out))
