@@ -15,12 +15,13 @@
 // where they fit and the rows are few enough, else a cluster of eight with both in the scratch.  Then a grid copies: table
 // rows, the rest of the stack, and K/V rows of all layers in chunks.
 //
-// What bounds it: the plan's latency, then the copies' writes.  GB300, graph replays: one prompt of 2043 positions continued 64
-// times, 32 layers of 8 KV heads, 23.3 us (91 MB written, the source comes from L2: 3.9 TB/s over the whole call, some 7 of it
-// the plan); 128 beams of some 60 pages, 8 layers, 13.9; 2048 beams of 140 pages in one layer 57.  At first, with target
-// entries marked one by one, every row's entries ranked and the tables written by the plan, 36.3, 20.2 and 90.
-// (A CTA that keeps a source chunk in registers for the next copy of the same page: 24.0; table and stack prefetched
-// while the sizes are looked at: 24.9 and 15.2.)
+// What bounds it: the plan's latency (a chain of small reads, barriers and code that runs once: entries eight or sixteen at a
+// time, or the two sums one after the other, were slower for their longer code), then the copies' writes.  GB300, graph replays:
+// one prompt of 2043 positions continued 64 times, 32 layers of 8 KV heads, 20.1 us (91 MB written, the source comes from L2);
+// 128 beams of some 60 pages, 8 layers, 12.5; 2048 beams of 140 pages in one layer 56.  At first, with target entries marked
+// one by one, every row's entries ranked and the tables written by the plan, 36.3, 20.2 and 90.
+// (A CTA that keeps a source chunk in registers for the next copy of the same page, or the table prefetched while the sizes
+// are looked at: 0.5 - 1 us more.)
 #include <cuda_runtime.h>
 
 #include <climits>
@@ -56,36 +57,42 @@ struct Scratch {
         lead(gives + from_batch), takes(lead + from_batch), first(takes + to_batch), user(first + num_pages) {}
 };
 
-// Exclusive sums of in[0 .. n) into out (may be the same), by the whole CTA; the total to every thread.
-template <typename Load>
-__device__ __forceinline__ int exclusive_sums(Load in, int n, int* out, int* warp_s) {
+// Exclusive sums of n pairs (two counts in one word), by the whole CTA: load(i) is a pair, store(i, sums) takes what comes before
+// it (after every load of the thread's own run); the totals to every thread.
+template <typename Load, typename Store>
+__device__ __forceinline__ unsigned long long exclusive_sums(int n, unsigned long long* warp_s, Load load, Store store) {
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int per = (n + kThreads - 1) / kThreads, i0 = min(n, t * per), i1 = min(n, i0 + per);
-  int sum = 0;
-  for (int i = i0; i < i1; ++i) sum += in(i);
-  int incl = sum;
+  unsigned long long sum = 0ull;
+#pragma unroll 1
+  for (int i = i0; i < i1; ++i) sum += load(i);
+  unsigned long long incl = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, incl, o);
+    const unsigned long long y = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += y;
   }
   if (lane == 31) warp_s[warp] = incl;
   __syncthreads();
-  const int w = warp_s[lane];   // as many warps as lanes
-  const int before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0), total = __reduce_add_sync(0xffffffffu, w);
-  int at = before + incl - sum;
+  const unsigned long long w = warp_s[lane], b = lane < warp ? w : 0ull;   // as many warps as lanes
+  const auto add = [](unsigned long long x) {
+    return (unsigned long long)__reduce_add_sync(0xffffffffu, (unsigned)(x >> 32)) << 32 | __reduce_add_sync(0xffffffffu, (unsigned)x);
+  };
+  unsigned long long at = add(b) + incl - sum;
+#pragma unroll 1
   for (int i = i0; i < i1; ++i) {
-    const int x = in(i);
-    out[i] = at;
+    const unsigned long long x = load(i);
+    store(i, at);
     at += x;
   }
-  __syncthreads();   // warp_s is read, out is there
+  const unsigned long long total = add(w);
+  __syncthreads();
   return total;
 }
 
 // Rows' entries to threads: each row by a group of 2^k neighbouring threads of the plan (8 at least), as many as there are
 // for a row, kUnroll entries of a thread in flight: f(row, index, entry) for every index of [begin(row), end(row)).
-constexpr int kUnroll = 8;
+constexpr int kUnroll = 4;
 __device__ __forceinline__ int group_of(int rows, int all) {
   int group = 8;
   while (group < all && (int64_t)rows * group * 2 <= all) group *= 2;
@@ -124,7 +131,7 @@ __device__ __forceinline__ void for_stack(const int32_t* a, int n, int me, int a
 template <bool kOne>   // one CTA, else a cluster of kCtas
 __global__ void __launch_bounds__(kThreads, 1) page_fork_plan_kernel(const __grid_constant__ PageForkParams p) {
   extern __shared__ int smem[];
-  __shared__ int warp_s[kWarps];
+  __shared__ unsigned long long warp_s[kWarps];
   __shared__ int bad_s;
   const int F = p.from_batch, B = p.to_batch, W = p.max_pages, log2p = p.page_log2, below = (1 << log2p) - 1;
   int* held = smem;             // [F]
@@ -246,13 +253,19 @@ __global__ void __launch_bounds__(kThreads, 1) page_fork_plan_kernel(const __gri
 
   int G = 0, T = 0;
   if (!bad) {
-    if constexpr (kOne) {
-      G = exclusive_sums([&](int i) { return gives_s[i]; }, F, gives_s, warp_s);
-      T = exclusive_sums([&](int i) { return takes_s[i]; }, B, takes_s, warp_s);
-    } else {
-      G = exclusive_sums([&](int i) { return __ldcg(sc.gives + i); }, F, gives_s, warp_s);
-      T = exclusive_sums([&](int i) { return __ldcg(sc.takes + i); }, B, takes_s, warp_s);
-    }
+    const unsigned long long total = exclusive_sums(
+        max(F, B), warp_s,
+        [&](int i) {
+          const unsigned gives = i < F ? (unsigned)(kOne ? gives_s[i] : __ldcg(sc.gives + i)) : 0u;
+          const unsigned takes = i < B ? (unsigned)(kOne ? takes_s[i] : __ldcg(sc.takes + i)) : 0u;
+          return (unsigned long long)takes << 32 | gives;
+        },
+        [&](int i, unsigned long long before) {
+          if (i < F) gives_s[i] = (int)(unsigned)before;
+          if (i < B) takes_s[i] = (int)(before >> 32);
+        });
+    G = (int)(unsigned)total;
+    T = (int)(total >> 32);
   }
   bad = bad || (int64_t)f - T + G > p.num_pages;   // more pages than there are: some page is held and free
   const bool refused = bad || T > f;
@@ -353,9 +366,9 @@ cudaError_t launch_page_fork(const PageForkParams& p, int sms, cudaStream_t stre
   constexpr size_t kMostSmem = 6 * (size_t)PTD_MAX_PROMPT_BATCH * sizeof(int), kMostOneSmem = 200 * 1024;
   const size_t sizes = 3 * ((size_t)p.from_batch + p.to_batch) * sizeof(int);
   const size_t with_pages = sizes + ((size_t)p.from_batch + 2 * (size_t)p.num_pages) * sizeof(int);
-  // (us, one CTA and the cluster: 1 source row of 1000 entries 13.3 and 15.6, [the rule's bound] 128 rows of 71 14.6 and 13.9,
-  // 256 of 140 22.0 and 16.2)
-  const bool one = with_pages <= kMostOneSmem && (int64_t)p.from_batch * p.max_pages <= 8192;
+  // (us, one CTA and the cluster: 32 source rows of 71 entries 7.5 and 10.9, 1 of 1000 9.1 and 11.2, 128 of 71 12.5 and 13.0,
+  // [the rule's bound] 256 of 140 19.7 and 14.4, 512 of 140 33 and 21.6)
+  const bool one = with_pages <= kMostOneSmem && (int64_t)p.from_batch * p.max_pages <= 12288;
   const size_t smem = one ? with_pages : sizes;
   cudaError_t e = cudaSuccess;
   if (smem > 47 * 1024) {   // the limits are the kernels', the same for every call
