@@ -31,7 +31,7 @@ using tr::kThreads;
 using tr::Place;
 
 constexpr int kCtas = 5;                         // of an SM
-constexpr size_t kMostSmem = 42 * 1024;          // of one of them: rows and tables of its layers
+constexpr size_t kMostSmem = 42 * 1024;          // of one of them: rows and tables of its layers (under the 48 KB of any kernel)
 
 __device__ __forceinline__ bool place_of_node(const TreeNormRopeParams& p, int n, bool first, int* par_s, Place& at) {
   return find_place(p.node_offsets, p.parents, p.ctx_lens, p.batch, n, p.page_size, p.seq_capacity, p.num_pages, p.block_table,
@@ -156,14 +156,8 @@ cudaError_t launch(TreeNormRopeParams p, const RopeFreqs& freqs, size_t per_laye
   const int64_t places = kCtas * (int64_t)sms, fill = ((int64_t)p.n_total * p.num_layers + places - 1) / places;
   if (layers > fill) layers = (int)fill;
   p.layers_per_cta = layers < 1 ? 1 : (layers > p.num_layers ? p.num_layers : layers);
-  const size_t smem = p.layers_per_cta * per_layer;
-  if (smem > 46 * 1024) {
-    const cudaError_t e =
-        cudaFuncSetAttribute(tree_norm_rope_kernel<T, kHalf>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem);
-    if (e != cudaSuccess) return e;
-  }
   return launch_chained(tree_norm_rope_kernel<T, kHalf>, dim3(p.n_total, (p.num_layers + p.layers_per_cta - 1) / p.layers_per_cta),
-                        dim3(kThreads), smem, stream, 0, p, freqs);
+                        dim3(kThreads), p.layers_per_cta * per_layer, stream, 0, p, freqs);
 }
 
 template <typename T>
