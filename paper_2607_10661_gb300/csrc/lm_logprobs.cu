@@ -300,6 +300,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
+// Latency: the parts' reads, insertions and rounds of maxima; four warps a row where the parts are many (63 rows, 152 parts:
+// the whole call 162.6 us, 166 with one warp a row).
 // kWarps warps per row: each lane merges some of the row's parts, a warp its lanes' by KM rounds of a warp-wide maximum (the owning
 // lane pops its head), the first warp the warps'.
 constexpr int kMergeThreads = 128;
