@@ -100,7 +100,7 @@ struct Best {
   // Takes what belongs here of 32 logits of tokens t0 ..., whose largest is `most` (v is used up): the largest that is left,
   // its first place, again while some lane has one.  A row of n logits takes about KM ln(n / KM) of them.
   __device__ __forceinline__ void take(float (&v)[32], float most, int t0) {
-    while (__any_sync(0xffffffffu, most > x[KM - 1])) {
+    for (int i = 0; i < 32 && __any_sync(0xffffffffu, most > x[KM - 1]); ++i) {   // (each takes one)
       int at = 0;
 #pragma unroll
       for (int e = 31; e >= 0; --e) at = v[e] == most ? e : at;
