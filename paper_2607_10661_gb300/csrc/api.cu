@@ -955,18 +955,13 @@ ptd_status prompt_rope_append(const ptd_prompt* prompt, const ptd_kv_cache* cach
   const ptd::MemoryRows rows[4] = {rows_of(q_out, qe, q_out_stride), rows_of(in_place ? nullptr : q, qe, q_stride),
                                    rows_of(k, ke, k_stride), rows_of(v, ke, v_stride)};
   if (written_rows_meet(rows, 1, 4)) return PTD_ERR_INVALID_ARG;
-  if (norms.q_weight) {   // nor do the norms' weights and a token's rows meet what is written
-    const ptd::MemoryRows more[6] = {rows[0],
-                                     ptd::memory_rows(dev_status, 4),
-                                     ptd::memory_rows(norms.q_weight, D * (int64_t)es),
-                                     ptd::memory_rows(norms.k_weight, D * (int64_t)es),
-                                     ptd::memory_rows(slots, (int64_t)N * 4),
-                                     ptd::memory_rows(positions, (int64_t)N * 4)};
-    if (written_rows_meet(more, 2, 6)) return PTD_ERR_INVALID_ARG;
-    const int64_t cb = cache_bytes(cache, prompt->batch, cache->num_layers);
-    const ptd::MemoryRows reads[10] = {ptd::memory_rows(cache->k, cb), ptd::memory_rows(cache->v, cb), rows[0], rows_of(q, qe, q_stride),
-                                       rows[2], rows[3], more[2], more[3], more[4], more[5]};
-    if (written_rows_meet(reads, 2, 10)) return PTD_ERR_INVALID_ARG;
+  if (norms.q_weight) {   // nor does anything else that is written meet what is read
+    const int64_t cb = cache_bytes(cache, prompt->batch, cache->num_layers), wb = D * (int64_t)es;
+    using ptd::memory_rows;
+    const ptd::MemoryRows all[11] = {rows[0], memory_rows(dev_status, 4), memory_rows(cache->k, cb), memory_rows(cache->v, cb),
+                                     rows[1], rows[2], rows[3], memory_rows(norms.q_weight, wb), memory_rows(norms.k_weight, wb),
+                                     memory_rows(slots, (int64_t)N * 4), memory_rows(positions, (int64_t)N * 4)};
+    if (written_rows_meet(all, 4, 11)) return PTD_ERR_INVALID_ARG;
   }
   ptd::PromptRopeParams p = {};
   p.slots = slots;

@@ -58,6 +58,23 @@ def test_prompt_norm_rope_append_refusals(lib):
     assert call(prompt=ptd._Prompt(8193, 10, 8, 100, A, A + 4096)) == ptd.UNSUPPORTED
 
 
+def test_prompt_norm_rope_append_refuses_a_status_on_other_memory(lib):
+    """dev_status is written: it lies on no input, not on q_out and not in the cache."""
+    from paper_2607_10661_gb300 import ptd
+
+    row, cache_bytes = 32 * 128 * 2, 2 * 40 * 16 * 1024 * 2
+
+    def call(status, out=10 * A):
+        prompt = ptd._Prompt(2, 10, 8, 100, A, A + 4096)
+        return lib.ptd_prompt_norm_rope_append(ctypes.byref(prompt), ctypes.byref(_cache(ptd)), 0, 4 * A, 5 * A, 7 * A, 4096, 32, 8 * A,
+                                               1024, 9 * A, 1024, 11 * A, 12 * A, 1e-6, 1e4, out, 4096, status, None)
+
+    for status in (2 * A, 2 * A + cache_bytes - 4, 3 * A + 64, 7 * A, 7 * A + 10 * row - 4, 8 * A, 9 * A + 16, 10 * A, 11 * A, 12 * A + 252,
+                   4 * A + 36, 5 * A):
+        assert call(status) == ptd.INVALID_ARG, hex(status)
+    assert call(7 * A + 8, out=7 * A) == ptd.INVALID_ARG   # in place too
+
+
 def test_tree_norm_rope_append_refusals(lib):
     from paper_2607_10661_gb300 import ptd
 
