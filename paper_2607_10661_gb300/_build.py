@@ -13,6 +13,7 @@ CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libptd.so")
 CALLS = os.path.join(PKG, "_ptdcall.so")
+CALLS_FOR = os.path.join(OUT, "ptdcall_for")   # what the call module was compiled against
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC"]
 
@@ -37,6 +38,13 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _calls_for() -> str:
+    """What the call module has to be compiled against anew for: it reads torch's tensors by the layout of one version."""
+    import torch
+
+    return f"torch {torch.__version__}, C++11 ABI {int(torch._C._GLIBCXX_USE_CXX11_ABI)}, {sysconfig.get_config_var('SOABI')}"
+
+
 def _compile_calls() -> None:
     import torch
 
@@ -44,14 +52,26 @@ def _compile_calls() -> None:
     include, lib = os.path.join(root, "include"), os.path.join(root, "lib")
     tmp = CALLS + ".tmp"
     cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-isystem", include,
-           "-isystem", os.path.join(include, "torch", "csrc", "api", "include"), "-I", sysconfig.get_paths()["include"],
-           os.path.join(CSRC, "pycall.cpp"), "-o", tmp, "-ldl", "-L", lib, f"-Wl,-rpath,{lib}", "-ltorch_python", "-ltorch_cpu",
-           "-lc10"]
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DPTD_TORCH_VERSION="{torch.__version__}"',
+           "-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"),
+           "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "pycall.cpp"), "-o", tmp, "-ldl", "-L", lib,
+           f"-Wl,-rpath,{lib}", "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    if os.path.exists(CALLS_FOR):   # (written behind the module: one left half made is made again)
+        os.remove(CALLS_FOR)
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"g++ failed on pycall.cpp:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, CALLS)
+    with open(CALLS_FOR, "w") as f:
+        f.write(_calls_for())
+
+
+def _calls_fit() -> bool:
+    """Whether the call module there is was compiled for this torch and this interpreter."""
+    if not os.path.exists(CALLS_FOR):
+        return False
+    with open(CALLS_FOR) as f:
+        return f.read() == _calls_for()
 
 
 def build(force: bool = False) -> str:
@@ -60,10 +80,12 @@ def build(force: bool = False) -> str:
     srcs = _sources()
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [
         os.path.join(os.path.dirname(PKG), "include", "ptd.h")]
-    if not force and os.path.exists(LIB) and os.path.exists(CALLS):
-        newest = max(os.path.getmtime(d) for d in deps)
-        if min(os.path.getmtime(LIB), os.path.getmtime(CALLS)) >= newest:
-            return LIB
+    newest = max(os.path.getmtime(d) for d in deps)
+    fresh = [not force and os.path.exists(f) and os.path.getmtime(f) >= newest for f in (LIB, CALLS)]
+    if all(fresh):
+        if not _calls_fit():
+            _compile_calls()
+        return LIB
     with cf.ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
         calls = ex.submit(_compile_calls)
         objs = list(ex.map(_compile, srcs))

@@ -11,11 +11,13 @@
 //
 // A torch.Tensor is looked at through torch's own C++ class (an attribute read by name costs 0.07 - 0.16 us, and a call has up
 // to a dozen tensors with five or six each: prompt_norm_rope_append 3.0 us without the launch); an object of another type that load() was
-// given by its Python attributes.
+// given by its Python attributes.  That class is the one of the torch compiled against: load() refuses another version.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <cstring>
 
 #include "../../include/ptd.h"
 
@@ -910,11 +912,26 @@ PyObject* page_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
   PTD_CALL(p_ptd_page_fork(cache, from, to, parents, lens, ws, wsb, status, s));
 }
 
+// Whether the process's torch is the version that the tensors' layout was compiled from (else a Python error).
+bool same_torch() {
+  PyObject* torch = PyImport_ImportModule("torch");
+  PyObject* version = torch != nullptr ? PyObject_GetAttrString(torch, "__version__") : nullptr;
+  const char* here = version != nullptr ? PyUnicode_AsUTF8(version) : nullptr;
+  const bool same = here != nullptr && strcmp(here, PTD_TORCH_VERSION) == 0;
+  if (!same && !PyErr_Occurred())
+    PyErr_Format(PyExc_RuntimeError, "_ptdcall.so was compiled for torch " PTD_TORCH_VERSION ", this is %s: run __graft_entry__.build()",
+                 here);
+  Py_XDECREF(version);
+  Py_XDECREF(torch);
+  return same;
+}
+
 // load(path of libptd.so, Tensor type, int32, float32, bfloat16, raw stream getter, device getter)
 PyObject* load(PyObject*, PyObject* args) {
   const char* path;
   PyObject* o[6];
   if (!PyArg_ParseTuple(args, "sOOOOOO", &path, &o[0], &o[1], &o[2], &o[3], &o[4], &o[5])) return nullptr;
+  if (!same_torch()) return nullptr;
   void* h = dlopen(path, RTLD_NOW | RTLD_LOCAL);
   if (h == nullptr) {
     PyErr_SetString(PyExc_RuntimeError, dlerror());
