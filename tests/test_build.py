@@ -61,6 +61,16 @@ def test_call_module_is_made_anew_where_nothing_says_what_it_is_for(tree):
     assert tree.build() == ["_ptdcall.so.tmp"] and tree.build() == []
 
 
+def test_library_is_linked_where_the_call_module_does_not_compile(tree):
+    tree.failing = ("_ptdcall.so.tmp",)
+    with pytest.raises(RuntimeError, match=r"pycall.cpp[^$]*no such header"):
+        tree.build()
+    assert sorted(tree.ran) == ALL and os.path.exists(_build.LIB) and not os.path.exists(_build.CALLS)
+    tree.failing = ()
+    tree.build()
+    assert os.path.exists(_build.CALLS) and tree.build() == []
+
+
 def test_call_module_of_another_torch_is_refused(monkeypatch):
     import __graft_entry__
 
