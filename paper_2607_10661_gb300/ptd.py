@@ -93,6 +93,16 @@ class _HostIO(ctypes.Structure):
         "topk_idx_h", "topk_val_h", "accepted_h", "accept_len_h", "bonus_h", "new_ctx_h", "status_h")]
 
 
+class _Int32:
+    """An int32 argument: ctypes would take a larger number modulo 2^32."""
+
+    @classmethod
+    def from_param(cls, x):
+        if not -(1 << 31) <= x < 1 << 31:
+            raise OverflowError(f"{x} does not fit the library's 32 bits")
+        return ctypes.c_int32(x)
+
+
 _lib = None
 _calls = None   # the _ptdcall module, once the library is loaded
 
@@ -104,15 +114,15 @@ def lib() -> ctypes.CDLL:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"libptd.so not built ({LIB_PATH}); run __graft_entry__.build()")
         L = ctypes.CDLL(LIB_PATH)
-        vp, i32, i64, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+        vp, i32, i64, f32, sz = ctypes.c_void_p, _Int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
         P = ctypes.POINTER
         L.ptd_status_string.restype = ctypes.c_char_p
         L.ptd_status_string.argtypes = [ctypes.c_int]
-        L.ptd_last_launch_count.restype = i32
+        L.ptd_last_launch_count.restype = ctypes.c_int32
         L.ptd_last_launch_count.argtypes = []
-        L.ptd_step_topk_policy.restype = i32
+        L.ptd_step_topk_policy.restype = ctypes.c_int32
         L.ptd_step_topk_policy.argtypes = [i32]
-        L.ptd_step_tail.restype = i32
+        L.ptd_step_tail.restype = ctypes.c_int32
         L.ptd_step_tail.argtypes = [P(_Tree), P(_Cache), P(_StepArgs)]
         L.ptd_attention_workspace_size.restype = sz
         L.ptd_attention_workspace_size.argtypes = [P(_Tree), P(_Cache), i32, i32]
@@ -125,7 +135,7 @@ def lib() -> ctypes.CDLL:
         L.ptd_tree_attention_as.restype = ctypes.c_int
         L.ptd_tree_attention_as.argtypes = [P(_Tree), P(_Cache), i32, i32, vp, i32, f32, vp, vp, sz, vp, i32, i32, vp]
         L.ptd_attention_plan.restype = ctypes.c_int
-        L.ptd_attention_plan.argtypes = [P(_Tree), P(_Cache), i32, i32, sz, P(i32), P(i32)]
+        L.ptd_attention_plan.argtypes = [P(_Tree), P(_Cache), i32, i32, sz, P(ctypes.c_int32), P(ctypes.c_int32)]
         L.ptd_topk_draft.restype = ctypes.c_int
         L.ptd_topk_draft.argtypes = [vp, ctypes.c_int, i64, i32, i64, i32, vp, vp, vp]
         L.ptd_verify_greedy.restype = ctypes.c_int

@@ -336,3 +336,50 @@ def test_oracle_head_norm():
     assert np.allclose(oracle.head_norm_rope(x, w, [0], 10.0, 0.0)[0, 0], [1.0, 2.0, -3.0, -4.0])
     assert np.allclose((oracle.head_norm_rope(x, np.ones(4), [7], 10.0, 0.0) ** 2).mean(-1), 1.0)
     assert np.allclose(oracle.head_norm_rope(x, w, [7], 10.0, 0.0), oracle.rope(oracle.head_norm_rope(x, w, [0], 10.0, 0.0), [7], 10.0))
+
+
+def test_sizes_beyond_32_bits_are_not_cut_off(lib, monkeypatch):
+    """A size or a layer that the library takes in 32 bits is refused where it has more, not taken modulo 2^32."""
+    import contextlib
+    import types
+
+    import torch
+
+    from paper_2607_10661_gb300 import ptd
+
+    class Refuse:
+        def __getattr__(self, name):
+            return lambda *a: None
+
+    monkeypatch.setattr(ptd, "_calls", Refuse())
+    monkeypatch.setattr(ptd, "_dev", lambda t, name, dtype=None, row_strided=False: None if t is None else A)
+    monkeypatch.setattr(ptd, "_one_device", lambda *t: contextlib.nullcontext())
+    far = 1 << 32
+    meta = lambda *shape, dtype=torch.bfloat16: torch.empty(shape, dtype=dtype, device="meta")
+    i32, f32 = (lambda *s: meta(*s, dtype=torch.int32)), (lambda *s: meta(*s, dtype=torch.float32))
+    refused = pytest.raises(ctypes.ArgumentError, match="32 bits")
+    with refused:
+        ptd.token_logprobs(meta(1, far + 5), i32(1), f32(1), None, None, None, i32(1), stream=0)
+    with refused:
+        ptd.lm_head_logprobs(meta(2, 64), meta(far + 5, 64), i32(2), f32(2), None, None, None, meta(8), i32(1), stream=0)
+    with refused:
+        ptd.lm_head_logprobs(meta(2, far + 64), meta(5, far + 64), i32(2), f32(2), None, None, None, meta(8), i32(1), stream=0)
+    with refused:
+        ptd.lm_head_logprobs(meta(far + 2, 64), meta(5, 64), i32(far + 2), f32(far + 2), None, None, None, meta(8), i32(1), stream=0)
+    for sizes in ((far + 5, 100, 1), (5, far + 100, 1), (5, 100, far)):
+        with refused:
+            ptd.lm_head_logprobs_workspace_size(*sizes)
+    cache = types.SimpleNamespace(c=_cache(ptd), k=meta(2, 40, 16, 8, 128), head_dim=128, num_kv_heads=8, sequences=2, page_size=16)
+    tree = types.SimpleNamespace(c=ptd._Tree(2, 20, 16, 100, A, A, A), batch=2, total_nodes=20, ctx_lens=None)
+    q, kv, w = meta(2, 20, 32, 128), meta(2, 20, 8, 128), meta(2, 128)
+    with refused:
+        ptd.tree_norm_rope_append(tree, cache, far, q, kv, kv, q, w, w, 1e-6, 1e4, i32(1), stream=0)
+    wide = meta(1, 20, far + 32, 128)
+    with refused:
+        ptd.tree_norm_rope_append(tree, cache, 0, wide, kv[:1], kv[:1], wide, w[:1], w[:1], 1e-6, 1e4, i32(1), stream=0)
+    monkeypatch.setattr(ptd, "_batch_of_cache", lambda *a: None)
+    monkeypatch.setattr(ptd, "_rows3", lambda t, name, dt, n, heads, d: (A, t.stride(0), t.shape[1]))
+    prompt = types.SimpleNamespace(c=ptd._Prompt(2, 20, 8, 100, A, A), total_tokens=20)
+    with refused:
+        ptd.prompt_norm_rope_append(prompt, cache, far + 1, i32(20), i32(20), q[0], kv[0], kv[0], q[0], w[0], w[0], 1e-6, 1e4, i32(1),
+                                    stream=0)
