@@ -407,14 +407,16 @@ ptd_status ptd_token_logprobs(const void* logits, ptd_dtype dtype, int64_t rows,
                               int32_t* out_idx, float* out_val, int32_t* dev_status, void* stream);
 
 /* As ptd_token_logprobs of the logits h_r W^T, which never reach memory: hidden and weight as ptd_lm_head_topk takes them,
- * but any number of rows up to PTD_MAX_LOGPROB_ROWS (a prompt's tokens, a decoding batch).  Logits are accumulated in fp32 by
- * the tensor cores in an order of their own (see ptd_lm_head_topk), then summed as there with vocab 2^-33 in the bound.
+ * but any number of rows up to PTD_MAX_LOGPROB_ROWS (a prompt's tokens, a decoding batch), of at most
+ * PTD_MAX_LOGPROB_COLUMNS columns.  Logits are accumulated in fp32 by the tensor cores in an order of their own (see
+ * ptd_lm_head_topk), then summed as there with vocab 2^-33 in the bound.
  * Tokens with logits of -inf or NaN are no alternatives: where fewer than k are left, -1 and -inf (NaN in a row with
  * NaN or +inf) follow.
  * workspace: ptd_lm_head_logprobs_workspace_size(rows, vocab, k) bytes (of the current device), 16-byte aligned, for the
  * parts of each row; it and the outputs overlap no input and not one another, and calls that may overlap on the GPU need
  * workspaces of their own.  Two launches: the product, and the merge of a row's parts. */
 #define PTD_MAX_LOGPROB_ROWS (1 << 22)
+#define PTD_MAX_LOGPROB_COLUMNS (1 << 26) /* the product of a tile's rows ends well within a bounded wait */
 size_t ptd_lm_head_logprobs_workspace_size(int32_t rows, int32_t vocab, int32_t k);
 ptd_status ptd_lm_head_logprobs(const void* hidden, int32_t rows, int64_t hidden_stride, const void* weight, int32_t vocab,
                                 int64_t weight_stride, int32_t d_model, const int32_t* tokens, float temperature, int32_t k,

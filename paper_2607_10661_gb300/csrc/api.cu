@@ -1195,7 +1195,7 @@ ptd_status ptd_lm_head_logprobs(const void* hidden, int32_t rows, int64_t hidden
       weight_stride < d_model || hidden_stride % 8 != 0 || weight_stride % 8 != 0 || !aligned16(hidden) || !aligned16(weight) ||
       scale == 0.f || hidden_stride > (INT64_MAX >> 2) / rows || weight_stride > (INT64_MAX >> 2) / vocab)
     return PTD_ERR_INVALID_ARG;
-  if (rows > PTD_MAX_LOGPROB_ROWS || vocab > PTD_MAX_PROMPT_TOKENS) return PTD_ERR_UNSUPPORTED;
+  if (rows > PTD_MAX_LOGPROB_ROWS || vocab > PTD_MAX_PROMPT_TOKENS || d_model > PTD_MAX_LOGPROB_COLUMNS) return PTD_ERR_UNSUPPORTED;
   if (k < 0 || k > PTD_MAX_TOPK) return PTD_ERR_INVALID_ARG;
   const int sms = num_sms_of_current_device();
   const ptd::LmLogprobsPlan plan = ptd::plan_lm_logprobs(rows, vocab, d_model, k, sms);

@@ -142,6 +142,16 @@ def test_lm_head_logprobs_refusals(lib):
     assert call(rows=2**22 + 1) == ptd.UNSUPPORTED and call(vocab=2**30 + 1) == ptd.UNSUPPORTED
 
 
+def test_lm_head_logprobs_refuses_rows_whose_tile_outlasts_a_wait(lib):
+    """A tile's product is waited for at most 2 s: 4 MMAs of 0.34 us per 64 columns, 0.36 s at the limit."""
+    from paper_2607_10661_gb300 import ptd
+
+    need = lib.ptd_lm_head_logprobs_workspace_size(1, 5, 0)
+    for d in (2**26 + 64, 2**28, 2**31 - 64):
+        assert lib.ptd_lm_head_logprobs(16 * A, 1, d, 32 * A, 5, d, d, 3 * A, 1.0, 0, 4 * A, None, None, None, 5 * A, need, 6 * A,
+                                        None) == ptd.UNSUPPORTED
+
+
 def test_page_fork_refusals(lib):
     from paper_2607_10661_gb300 import ptd
 
