@@ -9,12 +9,16 @@
 // A second kernel merges the parts that a row's CTAs left in the workspace.
 //
 // What bounds it: for many rows the tensor pipe and the power cap, 4096 rows of 4096 columns by 128256 tokens 2.23 ms in graph
-// replays (1.93 PFLOP/s; 2.35 - 2.44 ms, 1.76 - 1.83 PFLOP/s, among other passes); for up to a tile of rows the one read of W, 63 rows
-// 162.6 us (6.46 TB/s, 156 of it the product at 6.75), the merge and its launch the rest.  An MMA reads its 128 rows of H from
-// shared memory whatever the tile's width, some 68 ns: tiles narrower than 224 tokens leave the pipe waiting.  Steps (us, 63
-// rows with k = 8, 4096 with k = 4): tiles of 128 / 256 tokens, every logit of a block inserted where one might belong 174, 2320
-// (4096 rows with k = 16 4940); the block's largest taken while it belongs, only the rows of H there are 168, 2300 (2374); tile
-// by cost 166, 2240; four warps a row in the merge 162.6.
+// replays (1.93 PFLOP/s; 2.44 - 2.59 ms, 1.66 - 1.76 PFLOP/s, among other passes); for up to a tile of rows the one read of W, 63 rows
+// 158 - 163 us (6.5 TB/s; 156 of 162.6 the product at 6.75), the merge and its launch the rest.  Where d_model is short the
+// epilogue, some 3.6 us a tile of 224 tokens once the lists are full, which is the product of 800 columns: 4096 rows of 151936
+// tokens 757 us with d = 1024 (1.68 PFLOP/s), 512 with d = 512 (1.24; 144 tiles a CTA).  A CTA with few tiles fills its
+// lists where little hides it: 20 rows of 45725 tokens, d = 1792, k = 16 52.5 us (24 of bytes), 700 rows of 50000, d = 2048,
+// k = 16 122 (84 of products).
+// An MMA reads its 128 rows of H from shared memory whatever the tile's width, some 68 ns: tiles narrower than 224 tokens leave
+// the pipe waiting.  Steps (us, 63 rows with k = 8, 4096 with k = 4): tiles of 128 / 256 tokens, every logit of a block inserted
+// where one might belong 174, 2320 (4096 rows with k = 16 4940); the block's largest taken while it belongs, only the rows of H
+// there are 168, 2300 (2374); tile by cost 166, 2240; four warps a row in the merge 162.6.
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -397,7 +401,7 @@ cudaError_t launch(const CUtensorMap& map_h, const CUtensorMap& map_w, const LmL
 // Tokens of a tile, by what the phases would take.  Per 64 columns of d_model (ns, all SMs busy): the four MMAs 270 up to 192
 // tokens (the rows of H are read from shared memory anew for each), 291 with 224 and 340 with 256; W 128 bytes a token from
 // HBM, at 44.6 a ns and SM, once for the phase's row tiles; the lesser of the two hides but for some 15 %.  After a phase's last
-// tile its epilogue, some 35 ns a token.  GB300, d = 4096, 128256 tokens, us with 128 / 192 / 224 / 256 tokens: 63 rows 169 / 169 /
+// tile its epilogue, some 35 ns a token (those of the tiles before are taken as hidden, which they are from d = 800 on).  GB300, d = 4096, 128256 tokens, us with 128 / 192 / 224 / 256 tokens: 63 rows 169 / 169 /
 // 166 / 171, 200 rows 254 / 189 / 184 / 196, 500 rows 477 / 330 / 305 / 322, 4096 rows 3678 / 2548 / 2251 / 2300; 5707 rows of
 // 10605 tokens, d = 2752 348 / 223 / 227 / 242; 2000 rows of 1000, d = 512 25.1 / 30.0 / 32.2 / 34.2 (with 64 19.7).
 constexpr int kLeastTile = 64;

@@ -17,9 +17,11 @@
 //
 // What bounds it: the plan's latency (a chain of small reads, barriers and code that runs once: entries eight or sixteen at a
 // time, or the two sums one after the other, were slower for their longer code), then the copies' writes.  GB300, graph replays:
-// one prompt of 2043 positions continued 64 times, 32 layers of 8 KV heads, 20.1 us (91 MB written, the source comes from L2);
-// 128 beams of some 60 pages, 8 layers, 12.5; 2048 beams of 140 pages in one layer 56.  At first, with target entries marked
+// one prompt of 2043 positions continued 64 times, 32 layers of 8 KV heads, 20.1 - 22.4 us (91 MB written, the source comes from L2);
+// 128 beams of some 60 pages, 8 layers, 12.5 - 13.4; 2048 beams of 140 pages in one layer 56.  At first, with target entries marked
 // one by one, every row's entries ranked and the tables written by the plan, 36.3, 20.2 and 90.
+// The pool counts too (u and the holders are cleared, the stack is looked over and copied): that prompt in 4 layers with 300 pages
+// 8.9 us, with 20000 10.5, with 30000, which the cluster plans, 12.4, with 100000 14.0.
 // (A CTA that keeps a source chunk in registers for the next copy of the same page, or the table prefetched while the sizes
 // are looked at: 0.5 - 1 us more.)
 #include <cuda_runtime.h>

@@ -1,4 +1,5 @@
-// Log probabilities of given tokens, entropies and the k best alternatives of rows of logits: one read of them.
+// Log probabilities of given tokens, entropies and the k best alternatives of rows of logits: one read of them
+// all, and a second one of the few vectors that the alternatives may lie in.
 //
 // A row belongs to one CTA, or, where there are few long rows, is cut into contiguous parts, one CTA of a cluster each.
 // Every thread keeps the sums of row_sums.cuh over its vectors, against the largest logit that it has seen: a batch of vectors
@@ -7,10 +8,15 @@
 // does are read again (L2) by all threads, what reaches T goes to a buffer, and an element's place is the number of larger
 // ones in it.  A cluster's CTAs send their sums and keys to its first one, which writes the row.
 //
-// What bounds it: the one read, 1021 fp32 rows of 32000, k = 16 25.7 us in graph replays (5.1 TB/s; some 22 with k = 0: a CTA's selection
-// takes some 1.5 us that its own reads do not overlap), 512 bf16 rows of 128256 29.6 (4.4 TB/s); for few rows the chain
-// of reads, exponentials, selection and merge: one row of 128256, k = 8 6.0 us, 63 rows, k = 4 8.7.  At first (no batch in
-// flight, the owners of candidates reading alone) 37.3, -, 7.2 and 11.1.
+// Where fewer than k groups hold a number above -inf (rows that a mask leaves few tokens, next to none in a part of a row) T is
+// -inf and every masked element reaches it, and where long runs are equal to T: the buffer is lost and k rounds follow, a read of
+// the part each.
+//
+// What bounds it: the one read, 1021 fp32 rows of 32000, k = 16 25.7 - 26.7 us in graph replays (4.9 - 5.1 TB/s; some 22
+// with k = 0: a CTA's selection takes some 1.5 us that its own reads do not overlap), 512 bf16 rows of 128256 29.6 (4.4
+// TB/s); for few rows the chain of reads, exponentials, selection and merge: one row of 128256, k = 8 6.0 us, 63 rows, k = 4
+// 8.7.  At first (no batch in flight, the owners of candidates reading alone) 37.3, -, 7.2 and 11.1.  Where the rounds follow,
+// they: with one to seven tokens of a row allowed, k = 8, one row 33 us, 63 rows 158 (fp32 36 and 190).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

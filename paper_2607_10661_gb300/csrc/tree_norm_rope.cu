@@ -121,8 +121,9 @@ __global__ void __launch_bounds__(kThreads, kCtas)
   if (t == 0) bulk_store_drain();
 }
 
-// Rows that are not 16-byte vectors, heads whose items are not a power of two, or rows that do not fit: a warp per head, element
-// by element, one CTA per (node, layer).
+// Rows that are not 16-byte vectors, heads whose items are not a power of two, or rows that do not fit (64/64 heads of bf16, 32/32 of
+// fp32 at D = 128): a warp per head, element by element, one CTA per (node, layer).  63 nodes, 8 layers of those heads: 28.8 us
+// and 15.6 in graph replays, 49.5 MB each.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
     tree_norm_rope_scalar_kernel(const __grid_constant__ TreeNormRopeParams p, const __grid_constant__ RopeFreqs freqs) {
